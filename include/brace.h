@@ -45,7 +45,7 @@ enum {
   BRACE_ERR_BAD_STEP = 3,    /* hop called out of order; nothing was launched                   */
   BRACE_ERR_WORKSPACE = 4,   /* workspace missing, too small or misaligned                      */
   BRACE_ERR_CUDA = 5,        /* a CUDA runtime call failed; see brace_last_cuda_error           */
-  BRACE_ERR_TIMEOUT = 6      /* reserved: a bounded device-side wait ran out                    */
+  BRACE_ERR_TIMEOUT = 6      /* a bounded device-side wait ran out (brace_ortho_status)             */
 };
 
 /* aggregation rules.  All but SUM share Phases I, II and IV of Section 3 (sign,
@@ -166,7 +166,8 @@ int brace_segment(const brace_ctx* ctx, int32_t j, int64_t* begin, int64_t* end)
 
 /* cudaError_t of the last failed runtime call on this context (0 if none).  With ctx = NULL: of the
  * last failed runtime call made on the calling host thread by an entry point that takes no context
- * (brace_aggregate_static, brace_draw_matrix, brace_minmax_rate_probe, brace_debug_status). */
+ * (brace_aggregate_static, brace_draw_matrix, brace_minmax_rate_probe, brace_debug_status, and the
+ * operators at the end of this file). */
 int brace_last_cuda_error(const brace_ctx* ctx);
 
 /* Threat model of Section 3: Byzantine clients alter their vectors before the
@@ -387,6 +388,104 @@ int brace_debug_status(int32_t* h_code);
  * serialise them.  Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE, CUDA. */
 int brace_aggregate_static(int32_t n, int64_t d, const brace_params* params, const float* d_updates,
                            int64_t ld, void* d_out, int64_t out_ld, brace_stream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * Operators of a language model's round: the embedding table at both ends of a
+ * client's local step, and the orthogonalised update of the weight matrices
+ * after the aggregation.  They need no context; the conventions at the top of
+ * this file hold (status codes, stream order, no device allocation).  A CUDA
+ * failure of these calls is kept per host thread: brace_last_cuda_error(NULL).
+ * Matrices are row-major; `ld` and strides count elements, are 64-bit and need
+ * no alignment beyond the element's own (rows that start on 16-byte boundaries
+ * are read and written in wider words).
+ * ------------------------------------------------------------------------- */
+
+/* element types */
+enum {
+  BRACE_TYPE_F32 = 0,
+  BRACE_TYPE_BF16 = 1,
+  BRACE_TYPE_F16 = 2,
+  BRACE_TYPE_BITS = 3 /* packed bits as an aggregation round leaves them: 1 = +1, 0 = -1          */
+};
+
+/* accuracy of the orthogonalisation */
+enum {
+  BRACE_ORTHO_AUTO = 0,  /* SINGLE for float32 results, HALF for 16-bit ones                      */
+  BRACE_ORTHO_HALF = 1,  /* operands of the products rounded to 11 bits, sums in float32          */
+  BRACE_ORTHO_SINGLE = 2 /* operands held to 22 bits, sums in float32: three times the products   */
+};
+
+/* The iteration X <- a X + (b S + c S^2) X, S = X X^T (on the longer side: X S),
+ * `steps` times from X_0 = G / (||G||_F + eps).  Every singular value s of X_0
+ * goes to a s + b s^3 + c s^5 per step; singular vectors stay. */
+typedef struct brace_ortho_params {
+  int32_t steps;     /* >= 1                                                                      */
+  float a, b, c;     /* coefficients; singular values in [0, 1] must stay below 1.9 through all
+                        steps, and |b s^2 + c s^4| below 7.5 (else BRACE_ERR_INVALID_ARG)         */
+  float eps;         /* added to the Frobenius norm; finite, >= 1e-30                             */
+  int32_t precision; /* BRACE_ORTHO_*                                                             */
+} brace_ortho_params;
+
+/* steps = 5, (a, b, c) = (3.4445, -4.7750, 2.0315), eps = 1e-7, precision = AUTO. */
+int brace_ortho_default_params(brace_ortho_params* params);
+
+/* Bytes of workspace for `batch` matrices of rows x cols whose result has
+ * `out_type`; 0 if the arguments are invalid.  With precision AUTO a workspace
+ * sized for BRACE_TYPE_F32 serves every result type. */
+size_t brace_ortho_workspace_bytes(int32_t batch, int32_t rows, int32_t cols, const brace_ortho_params* params,
+                                   int32_t out_type);
+
+/* d_out[e] = the orthogonalised d_g[e] for `batch` matrices, `stride_*` elements
+ * apart.  g_type: F32, BF16, F16, or BITS (d_g is uint32 words; element (i, j)
+ * of matrix e is bit bit_offset + e*stride_g + i*ld_g + j, least significant
+ * first; bit_offset is ignored for the other types).  out_type: F32, BF16, F16.
+ * A matrix of zeros gives zeros; a matrix with a NaN or an infinity gives NaN
+ * (that matrix only).  batch, rows or cols of 0 does nothing.  d_out may not
+ * overlap d_g.  Errors: INVALID_ARG (null, negative size, ld < cols, bad type /
+ * coefficients, misaligned pointer), WORKSPACE (missing, too small or not 256-byte
+ * aligned), UNSUPPORTED (batch > 32767, or rows * cols / 8 >= 2^31), CUDA. */
+int brace_orthogonalize(int32_t batch, int32_t rows, int32_t cols, const brace_ortho_params* params, const void* d_g,
+                        int32_t g_type, int64_t ld_g, int64_t stride_g, int64_t bit_offset, void* d_out,
+                        int32_t out_type, int64_t ld_out, int64_t stride_out, void* d_workspace,
+                        size_t workspace_bytes, brace_stream_t stream);
+
+/* The update that follows a round, for weight matrices (brace_apply_update moves
+ * every coordinate by the aggregate itself; this orthogonalises it first):
+ *   M' = beta * M + g          g: the aggregate, as in brace_orthogonalize (BITS reads an output row of a round)
+ *   u  = nesterov ? g + beta * M' : M'
+ *   O  = orthogonalised u
+ *   W' = (1 - lr * weight_decay) * W - lr * scale * O     for each of `replicas` copies of W
+ * d_momentum_out may equal d_momentum and d_weights_out may equal d_weights (in
+ * place, with equal layouts); otherwise no buffers overlap.  M is float32, sums
+ * and products are float32, W' is rounded once. */
+typedef struct brace_muon {
+  const void* d_grad;
+  int64_t ld_grad, stride_grad, bit_offset;
+  const float* d_momentum;
+  int64_t ld_momentum, stride_momentum;
+  float* d_momentum_out;
+  int64_t ld_momentum_out, stride_momentum_out;
+  const void* d_weights;
+  int64_t ld_weights, stride_weights, replica_weights; /* replica r starts r * replica_weights further on  */
+  void* d_weights_out;
+  int64_t ld_weights_out, stride_weights_out, replica_weights_out;
+  int32_t grad_type;    /* F32, BF16, F16 or BITS                                                 */
+  int32_t weights_type; /* F32, BF16 or F16                                                       */
+  int32_t replicas;     /* >= 1: clients whose rows of weights take the same step                 */
+  int32_t nesterov;
+  float beta, lr, weight_decay, scale;
+} brace_muon;
+
+/* Workspace: brace_ortho_workspace_bytes with out_type = weights_type.  Errors as
+ * for brace_orthogonalize, and INVALID_ARG for non-finite beta, lr, weight_decay
+ * or scale and for replicas < 1. */
+int brace_muon_step(int32_t batch, int32_t rows, int32_t cols, const brace_ortho_params* params,
+                    const brace_muon* step, void* d_workspace, size_t workspace_bytes, brace_stream_t stream);
+
+/* Waits for `stream` and says whether a bounded device-side wait of the last
+ * brace_orthogonalize / brace_muon_step on this workspace ran out: BRACE_OK, or
+ * BRACE_ERR_TIMEOUT (its results are not valid).  Not for use in a capture. */
+int brace_ortho_status(const void* d_workspace, brace_stream_t stream);
 
 #ifdef __cplusplus
 }

@@ -23,6 +23,8 @@ STAT_MEDIAN, STAT_TRIMMED_MEAN = 0, 1
 ATTACK_NONE, ATTACK_SCALE_OWN, ATTACK_GAUSSIAN, ATTACK_SCALED_MEAN, ATTACK_MEAN_SHIFT, ATTACK_SPARSE_NOISE = range(6)
 DRAWS_SUPPLIED, DRAWS_GENERATED = 0, 1
 DRAW_UNIFORM, DRAW_NORMAL = 0, 1
+TYPE_F32, TYPE_BF16, TYPE_F16, TYPE_BITS = range(4)
+ORTHO_AUTO, ORTHO_HALF, ORTHO_SINGLE = 0, 1, 2
 
 
 class Params(C.Structure):
@@ -42,6 +44,23 @@ class Cost(C.Structure):
                 ("brace_bits_min", C.c_int64), ("brace_bits_max", C.c_int64), ("packed_bits_min", C.c_int64),
                 ("packed_bits_max", C.c_int64), ("rar_closed_form", C.c_double), ("brace_closed_form", C.c_double),
                 ("partial_bits_used", C.c_int32), ("partial_bits_min", C.c_int32)]
+
+
+class OrthoParams(C.Structure):
+    _fields_ = [("steps", C.c_int32), ("a", C.c_float), ("b", C.c_float), ("c", C.c_float), ("eps", C.c_float),
+                ("precision", C.c_int32)]
+
+
+class Muon(C.Structure):
+    _fields_ = [("d_grad", C.c_void_p), ("ld_grad", C.c_int64), ("stride_grad", C.c_int64),
+                ("bit_offset", C.c_int64), ("d_momentum", C.c_void_p), ("ld_momentum", C.c_int64),
+                ("stride_momentum", C.c_int64), ("d_momentum_out", C.c_void_p), ("ld_momentum_out", C.c_int64),
+                ("stride_momentum_out", C.c_int64), ("d_weights", C.c_void_p), ("ld_weights", C.c_int64),
+                ("stride_weights", C.c_int64), ("replica_weights", C.c_int64), ("d_weights_out", C.c_void_p),
+                ("ld_weights_out", C.c_int64), ("stride_weights_out", C.c_int64),
+                ("replica_weights_out", C.c_int64), ("grad_type", C.c_int32), ("weights_type", C.c_int32),
+                ("replicas", C.c_int32), ("nesterov", C.c_int32), ("beta", C.c_float), ("lr", C.c_float),
+                ("weight_decay", C.c_float), ("scale", C.c_float)]
 
 
 class BraceError(RuntimeError):
@@ -84,6 +103,14 @@ SIGNATURES = {
     "brace_minmax_rate_probe": (C.c_int, [C.c_int32, C.c_int32, C.c_void_p, C.POINTER(C.c_int64), C.c_void_p]),
     "brace_aggregate_static": (C.c_int, [C.c_int32, C.c_int64, C.POINTER(Params), C.c_void_p, C.c_int64, C.c_void_p,
                                          C.c_int64, C.c_void_p]),
+    "brace_ortho_default_params": (C.c_int, [C.POINTER(OrthoParams)]),
+    "brace_ortho_workspace_bytes": (C.c_size_t, [C.c_int32, C.c_int32, C.c_int32, C.POINTER(OrthoParams), C.c_int32]),
+    "brace_orthogonalize": (C.c_int, [C.c_int32, C.c_int32, C.c_int32, C.POINTER(OrthoParams), C.c_void_p, C.c_int32,
+                                      C.c_int64, C.c_int64, C.c_int64, C.c_void_p, C.c_int32, C.c_int64, C.c_int64,
+                                      C.c_void_p, C.c_size_t, C.c_void_p]),
+    "brace_muon_step": (C.c_int, [C.c_int32, C.c_int32, C.c_int32, C.POINTER(OrthoParams), C.POINTER(Muon),
+                                  C.c_void_p, C.c_size_t, C.c_void_p]),
+    "brace_ortho_status": (C.c_int, [C.c_void_p, C.c_void_p]),
 }
 
 STATIC_SCRATCH_BYTES = 8 * 1024 * 1024
@@ -340,3 +367,118 @@ class Brace:
         raw = self.workspace[off: off + ln * eb]
         dt = {1: torch.int8, 2: torch.int16, 4: torch.float32}[eb]
         return seg, raw.view(dt).cpu()
+
+
+# ---- operators of a language model's round -----------------------------------------------------------------------
+
+_TYPES = {torch.float32: TYPE_F32, torch.bfloat16: TYPE_BF16, torch.float16: TYPE_F16, torch.int32: TYPE_BITS}
+
+
+def ortho_params(**over) -> OrthoParams:
+    p = OrthoParams()
+    _check(lib().brace_ortho_default_params(C.byref(p)), "brace_ortho_default_params")
+    for k, v in over.items():
+        setattr(p, k, v)
+    return p
+
+
+def ortho_workspace_bytes(batch: int, rows: int, cols: int, params: OrthoParams, out_type: int = TYPE_F32) -> int:
+    return int(lib().brace_ortho_workspace_bytes(batch, rows, cols, C.byref(params), out_type))
+
+
+class Orthogonalizer:
+    """Workspace and parameters of the orthogonalised update of `batch` matrices of rows x cols.
+
+    Matrices are float32, bfloat16 or float16 tensors [batch, rows, cols] (or [rows, cols] where batch is 1) whose
+    last stride is 1; an int32 tensor is a row of packed bits as a round leaves it, with the matrices one after the
+    other from `bit_offset` on."""
+
+    def __init__(self, rows: int, cols: int, batch: int = 1, params: OrthoParams | None = None, device="cuda",
+                 workspace: torch.Tensor | None = None):
+        self.batch, self.rows, self.cols = batch, rows, cols
+        self.params = params if params is not None else ortho_params()
+        if workspace is None:
+            need = ortho_workspace_bytes(batch, rows, cols, self.params)
+            # 0: the arguments are refused; the calls give the reason
+            workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=device)
+        self.workspace = workspace
+        self._step = Muon()
+
+    def _matrix(self, t: torch.Tensor, name: str):
+        """(element type, ld, stride between matrices) of a tensor argument."""
+        shape = tuple(t.shape)
+        if shape != (self.batch, self.rows, self.cols) and not (self.batch == 1 and shape == (self.rows, self.cols)):
+            raise ValueError(f"{name} has shape {shape}, not {(self.batch, self.rows, self.cols)}")
+        if t.dtype not in _TYPES or t.dtype == torch.int32:
+            raise ValueError(f"{name} is of type {t.dtype}")
+        st = t.stride()
+        if self.cols > 1 and st[-1] != 1:
+            raise ValueError(f"{name}: the last dimension is not contiguous")
+        # the stride of a dimension of one (or no) element has no meaning
+        ld = st[-2] if self.rows > 1 else max(self.cols, 1)
+        return _TYPES[t.dtype], ld, st[0] if self.batch > 1 else 0
+
+    def _update(self, g: torch.Tensor, name: str, bit_offset: int):
+        if g.dtype == torch.int32:
+            need = bit_offset + self.batch * self.rows * self.cols
+            if g.dim() != 1 or (g.numel() > 1 and g.stride(0) != 1) or bit_offset < 0 or 32 * g.numel() < need:
+                raise ValueError(f"{name}: packed bits are a contiguous row of at least {need} bits")
+            return TYPE_BITS, self.cols, self.rows * self.cols
+        return self._matrix(g, name)
+
+    def orthogonalize_status(self, g: torch.Tensor, out: torch.Tensor, bit_offset: int = 0, stream=None) -> int:
+        gt, gld, gs = self._update(g, "g", bit_offset)
+        ot, old, os_ = self._matrix(out, "out")
+        return lib().brace_orthogonalize(self.batch, self.rows, self.cols, self.params, g.data_ptr(), gt, gld, gs,
+                                         bit_offset, out.data_ptr(), ot, old, os_, self.workspace.data_ptr(),
+                                         self.workspace.numel(), _stream(stream))
+
+    def orthogonalize(self, g: torch.Tensor, out: torch.Tensor, bit_offset: int = 0, stream=None):
+        """out = g with its singular values pushed to 1."""
+        _check(self.orthogonalize_status(g, out, bit_offset, stream), "brace_orthogonalize")
+
+    def muon_step_status(self, grad: torch.Tensor, momentum: torch.Tensor, weights: torch.Tensor, lr: float,
+                         beta: float = 0.95, nesterov: bool = True, weight_decay: float = 0.0, scale: float = 1.0,
+                         bit_offset: int = 0, momentum_out: torch.Tensor | None = None,
+                         weights_out: torch.Tensor | None = None, stream=None) -> int:
+        momentum_out = momentum if momentum_out is None else momentum_out
+        weights_out = weights if weights_out is None else weights_out
+        s = self._step
+        s.grad_type, s.ld_grad, s.stride_grad = self._update(grad, "grad", bit_offset)
+        s.d_grad, s.bit_offset = grad.data_ptr(), bit_offset
+        for t, name in ((momentum, "momentum"), (momentum_out, "momentum_out")):
+            if t.dtype != torch.float32:
+                raise ValueError(f"{name} is of type {t.dtype}, not float32")
+        _, s.ld_momentum, s.stride_momentum = self._matrix(momentum, "momentum")
+        _, s.ld_momentum_out, s.stride_momentum_out = self._matrix(momentum_out, "momentum_out")
+        s.d_momentum, s.d_momentum_out = momentum.data_ptr(), momentum_out.data_ptr()
+        replicas = 1
+        s.replica_weights = s.replica_weights_out = 0
+        w, wo = weights, weights_out
+        if weights.dim() == 4:      # [replicas, batch, rows, cols]
+            replicas = weights.shape[0]
+            if weights_out.dim() != 4 or weights_out.shape[0] != replicas or replicas < 1:
+                raise ValueError("weights and weights_out have different shapes")
+            s.replica_weights, s.replica_weights_out = weights.stride(0), weights_out.stride(0)
+            w, wo = weights[0], weights_out[0]
+        if w.dtype != wo.dtype:
+            raise ValueError("weights and weights_out have different types")
+        s.weights_type, s.ld_weights, s.stride_weights = self._matrix(w, "weights")
+        _, s.ld_weights_out, s.stride_weights_out = self._matrix(wo, "weights_out")
+        s.d_weights, s.d_weights_out, s.replicas = w.data_ptr(), wo.data_ptr(), replicas
+        s.nesterov, s.beta, s.lr, s.weight_decay, s.scale = int(nesterov), beta, lr, weight_decay, scale
+        return lib().brace_muon_step(self.batch, self.rows, self.cols, self.params, s, self.workspace.data_ptr(),
+                                     self.workspace.numel(), _stream(stream))
+
+    def muon_step(self, grad: torch.Tensor, momentum: torch.Tensor, weights: torch.Tensor, lr: float,
+                  beta: float = 0.95, nesterov: bool = True, weight_decay: float = 0.0, scale: float = 1.0,
+                  bit_offset: int = 0, momentum_out: torch.Tensor | None = None,
+                  weights_out: torch.Tensor | None = None, stream=None):
+        """One step of momentum, orthogonalisation and weight update, in place unless *_out are given.  Weights of
+        shape [replicas, batch, rows, cols] all take the same step."""
+        _check(self.muon_step_status(grad, momentum, weights, lr, beta, nesterov, weight_decay, scale, bit_offset,
+                                     momentum_out, weights_out, stream), "brace_muon_step")
+
+    def check(self, stream=None):
+        """Wait for the stream; raise if a bounded device-side wait of the last call ran out."""
+        _check(lib().brace_ortho_status(self.workspace.data_ptr(), _stream(stream)), "brace_ortho_status")

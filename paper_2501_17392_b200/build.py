@@ -11,8 +11,9 @@ PKG_DIR = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG_DIR)
 LIB_PATH = os.path.join(PKG_DIR, "libbrace.so")
 DEBUG_LIB_PATH = os.path.join(PKG_DIR, "libbrace_debug.so")
-SOURCES = [os.path.join(PKG_DIR, "csrc", "brace.cu")]
-DEPS = SOURCES + [os.path.join(PKG_DIR, "csrc", "brace_kernels.cuh"), os.path.join(ROOT, "include", "brace.h")]
+SOURCES = [os.path.join(PKG_DIR, "csrc", f) for f in ("brace.cu", "operators.cu")]
+DEPS = SOURCES + [os.path.join(PKG_DIR, "csrc", f) for f in ("brace_kernels.cuh", "ortho_kernels.cuh", "sm100.cuh")]
+DEPS += [os.path.join(ROOT, "include", "brace.h")]
 
 
 def _nvcc() -> str:
@@ -31,7 +32,7 @@ def needs_build(path: str = LIB_PATH) -> bool:
 
 def _compile(out_path: str, defines, verbose: bool) -> str:
     cmd = [_nvcc(), "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-           "-shared", "-Xcompiler", "-fPIC", "-I", os.path.join(ROOT, "include"),
+           "-shared", "--threads", "0", "-Xcompiler", "-fPIC", "-I", os.path.join(ROOT, "include"),
            "-I", os.path.join(PKG_DIR, "csrc")] + list(defines) + ["-o", out_path] + SOURCES
     if verbose:
         cmd[1:1] = ["-Xptxas", "-v"]

@@ -137,6 +137,18 @@ void consensus_thresholds(const brace_params* p, int n, int* hi, int* lo) {
 // cudaError_t of the last failed runtime call made by a context-free entry point on this thread
 thread_local int g_last_cuda_no_ctx = 0;
 
+}  // namespace
+
+// for the operators of the other translation unit
+namespace brace {
+int cuda_fail_no_ctx(cudaError_t err) {
+  g_last_cuda_no_ctx = (int)err;
+  return BRACE_ERR_CUDA;
+}
+}  // namespace brace
+
+namespace {
+
 int cuda_fail(brace_ctx* ctx, cudaError_t err) {
   ctx->last_cuda = (int)err;
   if (ctx->no_ctx_call) g_last_cuda_no_ctx = (int)err;

@@ -1,0 +1,421 @@
+// Host side of the language-model operators: argument checks, workspaces, tensor maps and kernel launches.
+// C ABI declared in brace.h.
+#include "brace.h"
+
+#include <cuda.h>
+#include <cuda_runtime.h>
+
+#include <atomic>
+#include <cmath>
+
+#include "ortho_kernels.cuh"
+
+namespace brace {
+int cuda_fail_no_ctx(cudaError_t err);   // brace.cu: keeps the error for brace_last_cuda_error(NULL)
+}
+
+using namespace brace;
+
+namespace {
+
+inline int64_t round_up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
+inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+
+int elem_bytes(int type) { return type == BRACE_TYPE_F32 || type == BRACE_TYPE_BITS ? 4 : 2; }
+bool float_type(int t) { return t == BRACE_TYPE_F32 || t == BRACE_TYPE_BF16 || t == BRACE_TYPE_F16; }
+
+// Rows and matrices whose 8-element groups are whole 16-byte words.
+bool wide_rows(const void* p, int type, int64_t ld, int64_t s1, int64_t s2 = 0) {
+  const int64_t per = 16 / elem_bytes(type);
+  return aligned(p, 16) && ld % per == 0 && s1 % per == 0 && s2 % per == 0;
+}
+
+int sm_count() {
+  static std::atomic<int> cached[64];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 148;
+  int n = cached[dev].load(std::memory_order_relaxed);
+  if (n == 0) {
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) n = 148;
+    cached[dev].store(n, std::memory_order_relaxed);
+  }
+  return n;
+}
+
+// Every kernel here waits on the device for the one before it (griddepcontrol.wait) and may be set up while that one
+// drains.  `cluster`: CTAs per cluster.
+template <typename... KArgs, typename... Args>
+cudaError_t launch(void (*kernel)(KArgs...), dim3 grid, int block, size_t smem, int cluster, cudaStream_t st,
+                   const Args&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3((unsigned)block);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = (unsigned)cluster;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+// ---- the orthogonalisation --------------------------------------------------------------------------------------
+
+constexpr int kMaxNormBlocks = 512;
+constexpr int kPrepBlocks = 1184;   // CTAs of the element-wise passes that fill the GPU: 148 SMs x 8
+
+bool coefficients_ok(const brace_ortho_params* p) {
+  if (!p || p->steps < 1 || p->steps > 1000) return false;
+  if (!std::isfinite(p->a) || !std::isfinite(p->b) || !std::isfinite(p->c)) return false;
+  if (!std::isfinite(p->eps) || !(p->eps >= 1e-30f)) return false;
+  if (p->precision < BRACE_ORTHO_AUTO || p->precision > BRACE_ORTHO_SINGLE) return false;
+  // upper bound of the singular values, step by step: the extremes of s -> a s + b s^3 + c s^5 on [0, top]
+  const double a = p->a, b = p->b, c = p->c;
+  double top = 1.0;
+  for (int k = 0; k < p->steps; ++k) {
+    const double t_top = top * top;
+    double q = std::fabs(b * t_top + c * t_top * t_top), next = std::fabs(top * (a + b * t_top + c * t_top * t_top));
+    if (c != 0.0) {
+      const double tq = -b / (2 * c);   // extreme of b t + c t^2
+      if (tq > 0 && tq < t_top) q = std::fmax(q, std::fabs(b * tq + c * tq * tq));
+      const double disc = 9 * b * b - 20 * a * c;
+      if (disc >= 0)
+        for (int sg = -1; sg <= 1; sg += 2) {
+          const double t = (-3 * b + sg * std::sqrt(disc)) / (10 * c);
+          if (t > 0 && t < t_top) next = std::fmax(next, std::fabs(std::sqrt(t) * (a + b * t + c * t * t)));
+        }
+    } else if (b != 0.0) {
+      const double t = -a / (3 * b);
+      if (t > 0 && t < t_top) next = std::fmax(next, std::fabs(std::sqrt(t) * (a + b * t)));
+    }
+    if (!(q <= 7.5) || !(next <= 1.9)) return false;
+    if (k > 64 && next <= top) break;   // the bound has settled
+    top = std::fmax(next, 0.0);
+  }
+  return true;
+}
+
+struct OrthoPlan {
+  int batch, rows, cols, m;   // m: the short side
+  int planes;
+  int64_t ld_x, ld_s;
+  int norm_blocks;
+  size_t off_partial, off_x[2], off_s, off_p, bytes;
+};
+
+bool make_plan(OrthoPlan& q, int32_t batch, int32_t rows, int32_t cols, const brace_ortho_params* p, int out_type) {
+  q.batch = batch;
+  q.rows = rows;
+  q.cols = cols;
+  q.m = rows < cols ? rows : cols;
+  const bool single = p->precision == BRACE_ORTHO_SINGLE || (p->precision == BRACE_ORTHO_AUTO && out_type == BRACE_TYPE_F32);
+  q.planes = single ? 2 : 1;
+  q.ld_x = round_up(cols, 64);
+  q.ld_s = round_up(q.m, 64);
+  const int64_t units = (int64_t)rows * ((cols + 7) / 8);
+  int64_t nb = (units + 511) / 512;
+  const int64_t per = (kPrepBlocks + batch - 1) / batch;
+  if (nb > per) nb = per;
+  if (nb > kMaxNormBlocks) nb = kMaxNormBlocks;
+  q.norm_blocks = (int)(nb < 1 ? 1 : nb);
+  size_t at = 256;   // status word
+  auto take = [&at](int64_t bytes) {
+    const size_t here = at;
+    at += (size_t)round_up(bytes, 256);
+    return here;
+  };
+  q.off_partial = take((int64_t)batch * q.norm_blocks * 8);
+  const int64_t xb = (int64_t)batch * q.planes * rows * q.ld_x * 2, sb = (int64_t)batch * q.planes * q.m * q.ld_s * 2;
+  q.off_x[0] = take(xb);
+  q.off_x[1] = take(xb);
+  q.off_s = take(sb);
+  q.off_p = take(sb);
+  q.bytes = at;
+  return true;
+}
+
+bool sizes_ok(int32_t batch, int32_t rows, int32_t cols) { return batch >= 0 && rows >= 0 && cols >= 0; }
+bool sizes_served(int32_t batch, int32_t rows, int32_t cols) {
+  return batch <= 32767 && (int64_t)rows * (((int64_t)cols + 63) / 64 * 8) < (int64_t)1 << 31;
+}
+
+using EncodeFn = decltype(&cuTensorMapEncodeTiled);
+EncodeFn encode_fn() {
+  static std::atomic<void*> fn{nullptr};
+  void* f = fn.load(std::memory_order_acquire);
+  if (!f) {
+    cudaDriverEntryPointQueryResult found;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+        found != cudaDriverEntryPointSuccess)
+      return nullptr;
+    fn.store(f, std::memory_order_release);
+  }
+  return (EncodeFn)f;
+}
+
+// [planes of all matrices][rows][cols] float16 with rows of `ld`; boxes of 64 x 64, 128-byte swizzle, zeros outside.
+int make_map(CUtensorMap* map, void* base, int64_t cols, int64_t rows, int64_t ld, int64_t planes) {
+  EncodeFn enc = encode_fn();
+  if (!enc) return cuda_fail_no_ctx(cudaErrorNotSupported);
+  const cuuint64_t dim[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)planes};
+  const cuuint64_t stride[2] = {(cuuint64_t)ld * 2, (cuuint64_t)ld * 2 * (cuuint64_t)rows};
+  const cuuint32_t box[3] = {64, 64, 1}, one[3] = {1, 1, 1};
+  const CUresult r = enc(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, base, dim, stride, box, one,
+                         CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? BRACE_OK : cuda_fail_no_ctx(cudaErrorInvalidValue);
+}
+
+template <int CG, int NP, bool A_MN, bool B_MN, int MODE>
+cudaError_t launch_gemm(const CUtensorMap& a, const CUtensorMap& b, const GemmArgs& g, cudaStream_t st) {
+  using Shape = GemmShape<CG, NP>;
+  auto* kernel = ortho_gemm_kernel<CG, NP, A_MN, B_MN, MODE>;
+  static std::atomic<uint64_t> granted{0};   // devices on which this kernel may use its shared memory
+  int dev = 0;
+  cudaError_t err = cudaGetDevice(&dev);
+  if (err != cudaSuccess) return err;
+  const uint64_t bit = 1ull << (dev & 63);
+  if (!(granted.load(std::memory_order_relaxed) & bit)) {
+    err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape::kSmem);
+    if (err != cudaSuccess) return err;
+    granted.fetch_or(bit, std::memory_order_relaxed);
+  }
+  int clusters = sm_count() / CG;
+  if (clusters > g.total) clusters = g.total;
+  return launch(kernel, dim3((unsigned)(clusters * CG)), Shape::kThreads, Shape::kSmem, CG, st, a, b, g);
+}
+
+template <int CG, int NP>
+cudaError_t launch_products(const OrthoPlan& q, const brace_ortho_params* p, char* ws, const CUtensorMap map_x[2],
+                            const CUtensorMap& map_s, const CUtensorMap& map_p, GemmArgs last, cudaStream_t st) {
+  constexpr int T = GemmShape<CG, NP>::kTile;
+  const bool tall = q.rows > q.cols;
+  const int tm = (q.m + T - 1) / T;
+  GemmArgs sym = {};
+  sym.M = sym.N = q.m;
+  sym.tiles_n = tm;
+  sym.tiles = tm * (tm + 1) / 2;
+  sym.total = sym.tiles * q.batch;
+  sym.ld_dst = sym.ld_src = q.ld_s;
+  sym.status = (int*)ws;
+  GemmArgs step = last;
+  step.M = q.rows;
+  step.N = q.cols;
+  step.K = q.m;
+  step.tiles_n = (q.cols + T - 1) / T;
+  step.tiles = step.tiles_n * ((q.rows + T - 1) / T);
+  step.total = step.tiles * q.batch;
+  step.ld_src = step.ld_dst = q.ld_x;
+  step.alpha = p->a;
+  step.beta = kStepAcc;
+  step.status = (int*)ws;
+  __half* s = (__half*)(ws + q.off_s);
+  __half* poly = (__half*)(ws + q.off_p);
+  for (int k = 0; k < p->steps; ++k) {
+    const int cur = k & 1;
+    const CUtensorMap& x = map_x[cur];
+    GemmArgs g = sym;
+    g.K = tall ? q.rows : q.cols;
+    g.beta = kScaleSInv;
+    g.dst = s;
+    cudaError_t err = tall ? launch_gemm<CG, NP, true, true, kModeGram>(x, x, g, st)
+                           : launch_gemm<CG, NP, false, false, kModeGram>(x, x, g, st);
+    if (err != cudaSuccess) return err;
+    g = sym;
+    g.K = q.m;
+    g.alpha = p->b * kPolyB;
+    g.beta = p->c * kPolyC;
+    g.src = s;
+    g.dst = poly;
+    err = launch_gemm<CG, NP, false, false, kModePoly>(map_s, map_s, g, st);
+    if (err != cudaSuccess) return err;
+    step.src = (const __half*)(ws + q.off_x[cur]);
+    step.dst = (__half*)(ws + q.off_x[cur ^ 1]);
+    if (k + 1 < p->steps)
+      err = tall ? launch_gemm<CG, NP, false, false, kModeStep>(x, map_p, step, st)
+                 : launch_gemm<CG, NP, false, true, kModeStep>(map_p, x, step, st);
+    else
+      err = tall ? launch_gemm<CG, NP, false, false, kModeLast>(x, map_p, step, st)
+                 : launch_gemm<CG, NP, false, true, kModeLast>(map_p, x, step, st);
+    if (err != cudaSuccess) return err;
+  }
+  return cudaSuccess;
+}
+
+cudaError_t launch_prep(const OrthoPlan& q, const PrepArgs& a, cudaStream_t st) {
+  int64_t nb = ((int64_t)q.rows * (q.ld_x >> 3) + 511) / 512;
+  const int64_t per = (kPrepBlocks + q.batch - 1) / q.batch;
+  if (nb > per) nb = per;
+  if (nb < 1) nb = 1;
+  const dim3 g1((unsigned)q.norm_blocks, (unsigned)q.batch), g2((unsigned)nb, (unsigned)q.batch);
+  cudaError_t err;
+  switch (a.g.type) {
+    case kTypeF32:
+      err = launch(ortho_norm_kernel<kTypeF32>, g1, 256, 0, 1, st, a);
+      return err != cudaSuccess ? err : launch(ortho_scale_kernel<kTypeF32>, g2, 256, 0, 1, st, a);
+    case kTypeBF16:
+      err = launch(ortho_norm_kernel<kTypeBF16>, g1, 256, 0, 1, st, a);
+      return err != cudaSuccess ? err : launch(ortho_scale_kernel<kTypeBF16>, g2, 256, 0, 1, st, a);
+    case kTypeF16:
+      err = launch(ortho_norm_kernel<kTypeF16>, g1, 256, 0, 1, st, a);
+      return err != cudaSuccess ? err : launch(ortho_scale_kernel<kTypeF16>, g2, 256, 0, 1, st, a);
+    default:
+      err = launch(ortho_norm_kernel<kTypeBits>, g1, 256, 0, 1, st, a);
+      return err != cudaSuccess ? err : launch(ortho_scale_kernel<kTypeBits>, g2, 256, 0, 1, st, a);
+  }
+}
+
+// Everything after the argument checks.
+int run_ortho(const OrthoPlan& q, const brace_ortho_params* p, PrepArgs prep, const GemmArgs& last, char* ws,
+              cudaStream_t st) {
+  CUtensorMap map_x[2], map_s, map_p;
+  int rc;
+  const int64_t z = (int64_t)q.batch * q.planes;
+  for (int i = 0; i < 2; ++i)
+    if ((rc = make_map(&map_x[i], ws + q.off_x[i], q.cols, q.rows, q.ld_x, z)) != BRACE_OK) return rc;
+  if ((rc = make_map(&map_s, ws + q.off_s, q.m, q.m, q.ld_s, z)) != BRACE_OK) return rc;
+  if ((rc = make_map(&map_p, ws + q.off_p, q.m, q.m, q.ld_s, z)) != BRACE_OK) return rc;
+  prep.rows = q.rows;
+  prep.cols = q.cols;
+  prep.units_row = (q.cols + 7) / 8;
+  prep.norm_blocks = q.norm_blocks;
+  prep.partial = (double*)(ws + q.off_partial);
+  prep.eps = p->eps;
+  prep.x = (__half*)(ws + q.off_x[0]);
+  prep.ld_x = q.ld_x;
+  prep.planes = q.planes;
+  prep.status = (int*)ws;
+  cudaGetLastError();
+  cudaError_t err = launch_prep(q, prep, st);
+  if (err == cudaSuccess)
+    err = q.planes == 1 ? launch_products<1, 1>(q, p, ws, map_x, map_s, map_p, last, st)
+                        : launch_products<1, 2>(q, p, ws, map_x, map_s, map_p, last, st);
+  return err == cudaSuccess ? BRACE_OK : cuda_fail_no_ctx(err);
+}
+
+bool grad_ok(const void* p, int type, int64_t ld, int64_t bit_offset, int cols) {
+  if (!p || (!float_type(type) && type != BRACE_TYPE_BITS) || ld < cols) return false;
+  if (!aligned(p, (size_t)elem_bytes(type))) return false;
+  return type != BRACE_TYPE_BITS || bit_offset >= 0;
+}
+
+MatRef mat_ref(const void* p, int type, int64_t ld, int64_t stride, int64_t bit0) {
+  MatRef r = {};
+  r.p = p;
+  r.ld = ld;
+  r.batch = stride;
+  r.type = type;
+  r.vec = type != BRACE_TYPE_BITS && wide_rows(p, type, ld, stride);
+  r.bit0 = type == BRACE_TYPE_BITS ? bit0 : 0;
+  return r;
+}
+
+}  // namespace
+
+extern "C" {
+
+int brace_ortho_default_params(brace_ortho_params* params) {
+  if (!params) return BRACE_ERR_INVALID_ARG;
+  *params = brace_ortho_params{5, 3.4445f, -4.7750f, 2.0315f, 1e-7f, BRACE_ORTHO_AUTO};
+  return BRACE_OK;
+}
+
+size_t brace_ortho_workspace_bytes(int32_t batch, int32_t rows, int32_t cols, const brace_ortho_params* params,
+                                   int32_t out_type) {
+  if (!coefficients_ok(params) || !float_type(out_type) || !sizes_ok(batch, rows, cols)) return 0;
+  if (!sizes_served(batch, rows, cols)) return 0;
+  if (batch == 0 || rows == 0 || cols == 0) return 256;
+  OrthoPlan q;
+  make_plan(q, batch, rows, cols, params, out_type);
+  return q.bytes;
+}
+
+int brace_orthogonalize(int32_t batch, int32_t rows, int32_t cols, const brace_ortho_params* params, const void* d_g,
+                        int32_t g_type, int64_t ld_g, int64_t stride_g, int64_t bit_offset, void* d_out,
+                        int32_t out_type, int64_t ld_out, int64_t stride_out, void* d_workspace,
+                        size_t workspace_bytes, brace_stream_t stream) {
+  if (!coefficients_ok(params) || !float_type(out_type) || !sizes_ok(batch, rows, cols)) return BRACE_ERR_INVALID_ARG;
+  if (batch == 0 || rows == 0 || cols == 0) return BRACE_OK;
+  if (!grad_ok(d_g, g_type, ld_g, bit_offset, cols)) return BRACE_ERR_INVALID_ARG;
+  if (!d_out || ld_out < cols || !aligned(d_out, (size_t)elem_bytes(out_type))) return BRACE_ERR_INVALID_ARG;
+  if (!sizes_served(batch, rows, cols)) return BRACE_ERR_UNSUPPORTED;
+  OrthoPlan q;
+  make_plan(q, batch, rows, cols, params, out_type);
+  if (!d_workspace || workspace_bytes < q.bytes || !aligned(d_workspace, 256)) return BRACE_ERR_WORKSPACE;
+  PrepArgs prep = {};
+  prep.g = mat_ref(d_g, g_type, ld_g, stride_g, bit_offset);
+  GemmArgs last = {};
+  last.out = d_out;
+  last.ld_out = ld_out;
+  last.batch_out = stride_out;
+  last.out_type = out_type;
+  last.vec_out = wide_rows(d_out, out_type, ld_out, stride_out);
+  last.replicas = 1;
+  return run_ortho(q, params, prep, last, (char*)d_workspace, (cudaStream_t)stream);
+}
+
+int brace_muon_step(int32_t batch, int32_t rows, int32_t cols, const brace_ortho_params* params,
+                    const brace_muon* s, void* d_workspace, size_t workspace_bytes, brace_stream_t stream) {
+  if (!s || !coefficients_ok(params) || !float_type(s->weights_type) || !sizes_ok(batch, rows, cols))
+    return BRACE_ERR_INVALID_ARG;
+  if (!std::isfinite(s->beta) || !std::isfinite(s->lr) || !std::isfinite(s->weight_decay) || !std::isfinite(s->scale))
+    return BRACE_ERR_INVALID_ARG;
+  if (s->replicas < 1) return BRACE_ERR_INVALID_ARG;
+  if (batch == 0 || rows == 0 || cols == 0) return BRACE_OK;
+  if (!grad_ok(s->d_grad, s->grad_type, s->ld_grad, s->bit_offset, cols)) return BRACE_ERR_INVALID_ARG;
+  if (!s->d_momentum || !s->d_momentum_out || s->ld_momentum < cols || s->ld_momentum_out < cols ||
+      !aligned(s->d_momentum, 4) || !aligned(s->d_momentum_out, 4))
+    return BRACE_ERR_INVALID_ARG;
+  const size_t wb = (size_t)elem_bytes(s->weights_type);
+  if (!s->d_weights || !s->d_weights_out || s->ld_weights < cols || s->ld_weights_out < cols ||
+      !aligned(s->d_weights, wb) || !aligned(s->d_weights_out, wb))
+    return BRACE_ERR_INVALID_ARG;
+  if (!sizes_served(batch, rows, cols)) return BRACE_ERR_UNSUPPORTED;
+  OrthoPlan q;
+  make_plan(q, batch, rows, cols, params, s->weights_type);
+  if (!d_workspace || workspace_bytes < q.bytes || !aligned(d_workspace, 256)) return BRACE_ERR_WORKSPACE;
+  PrepArgs prep = {};
+  prep.g = mat_ref(s->d_grad, s->grad_type, s->ld_grad, s->stride_grad, s->bit_offset);
+  prep.m_in = s->d_momentum;
+  prep.ld_m_in = s->ld_momentum;
+  prep.batch_m_in = s->stride_momentum;
+  prep.vec_m_in = wide_rows(s->d_momentum, BRACE_TYPE_F32, s->ld_momentum, s->stride_momentum);
+  prep.m_out = s->d_momentum_out;
+  prep.ld_m_out = s->ld_momentum_out;
+  prep.batch_m_out = s->stride_momentum_out;
+  prep.vec_m_out = wide_rows(s->d_momentum_out, BRACE_TYPE_F32, s->ld_momentum_out, s->stride_momentum_out);
+  prep.beta = s->beta;
+  prep.nesterov = s->nesterov != 0;
+  GemmArgs last = {};
+  last.out = s->d_weights_out;
+  last.ld_out = s->ld_weights_out;
+  last.batch_out = s->stride_weights_out;
+  last.rep_out = s->replica_weights_out;
+  last.out_type = s->weights_type;
+  last.vec_out = wide_rows(s->d_weights_out, s->weights_type, s->ld_weights_out, s->stride_weights_out, s->replica_weights_out);
+  last.w_in = s->d_weights;
+  last.ld_in = s->ld_weights;
+  last.batch_in = s->stride_weights;
+  last.rep_in = s->replica_weights;
+  last.vec_in = wide_rows(s->d_weights, s->weights_type, s->ld_weights, s->stride_weights, s->replica_weights);
+  last.replicas = s->replicas;
+  last.keep = 1.f - s->lr * s->weight_decay;
+  last.rate = s->lr * s->scale;
+  return run_ortho(q, params, prep, last, (char*)d_workspace, (cudaStream_t)stream);
+}
+
+int brace_ortho_status(const void* d_workspace, brace_stream_t stream) {
+  if (!d_workspace) return BRACE_ERR_WORKSPACE;
+  int code = 0;
+  cudaError_t err = cudaMemcpyAsync(&code, d_workspace, sizeof(code), cudaMemcpyDeviceToHost, (cudaStream_t)stream);
+  if (err == cudaSuccess) err = cudaStreamSynchronize((cudaStream_t)stream);
+  if (err != cudaSuccess) return cuda_fail_no_ctx(err);
+  return code ? BRACE_ERR_TIMEOUT : BRACE_OK;
+}
+
+}  // extern "C"
