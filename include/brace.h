@@ -487,6 +487,45 @@ int brace_muon_step(int32_t batch, int32_t rows, int32_t cols, const brace_ortho
  * BRACE_ERR_TIMEOUT (its results are not valid).  Not for use in a capture. */
 int brace_ortho_status(const void* d_workspace, brace_stream_t stream);
 
+/* The embedding table at the two ends of a client's local step, for `clients`
+ * clients at once, each with `tokens` ids of its own.  Client c's table (or its
+ * gradient: a part of its row of the update matrix) starts c * stride_table
+ * elements after d_table, its activations (or their gradient) c * stride_act
+ * after d_act, its ids c * stride_ids after d_ids.  An id outside [0, vocab) is
+ * no token: its activations are 0 and it adds nothing to the gradient. */
+typedef struct brace_embedding {
+  int32_t clients;         /* 0..65535                                                            */
+  int32_t dim;             /* >= 1                                                                */
+  int64_t tokens;          /* per client, 0..2^31-1                                               */
+  int64_t vocab;           /* rows of a table, 1..2^31-1                                          */
+  void* d_table;           /* lookup: read; gradient: written                                     */
+  int64_t ld_table, stride_table;   /* stride 0 (one table for all clients): lookup only          */
+  const void* d_ids;
+  int64_t stride_ids;
+  void* d_act;             /* lookup: written; gradient: read                                     */
+  int64_t ld_act, stride_act;       /* 0 in the gradient: one row for all tokens, one set for all clients */
+  int32_t table_type, act_type;     /* F32, BF16, F16                                             */
+  int32_t id_bytes;        /* 4 (int32) or 8 (int64)                                              */
+  int32_t accumulate;      /* gradient: add to what the table's gradient holds (rows that no token
+                              hits are not touched) instead of writing every row                  */
+  float scale;
+} brace_embedding;
+
+/* d_act[c][t] = scale * d_table[c][id[c][t]], the product rounded once to act_type.
+ * Errors: INVALID_ARG (null, size out of range, ld < dim, bad type, misaligned
+ * pointer, non-finite scale, stride_act 0 with several clients), CUDA. */
+int brace_embedding_lookup(const brace_embedding* e, brace_stream_t stream);
+
+/* Bytes of workspace of brace_embedding_grad: the sorted ids and the partial sums
+ * of frequent tokens; 0 if the arguments are invalid. */
+size_t brace_embedding_workspace_bytes(int32_t clients, int64_t tokens, int32_t dim);
+
+/* d_table[c][v] = scale * sum of d_act[c][t] over the tokens t with id v, in
+ * float32 in one order (increasing t, in groups), rounded once to table_type: the
+ * same bits every time.  Errors as for the lookup (stride_table 0 with several
+ * clients), and WORKSPACE (missing, too small or not 256-byte aligned). */
+int brace_embedding_grad(const brace_embedding* e, void* d_workspace, size_t workspace_bytes, brace_stream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

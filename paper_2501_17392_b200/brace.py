@@ -63,6 +63,14 @@ class Muon(C.Structure):
                 ("weight_decay", C.c_float), ("scale", C.c_float)]
 
 
+class EmbeddingArgs(C.Structure):
+    _fields_ = [("clients", C.c_int32), ("dim", C.c_int32), ("tokens", C.c_int64), ("vocab", C.c_int64),
+                ("d_table", C.c_void_p), ("ld_table", C.c_int64), ("stride_table", C.c_int64), ("d_ids", C.c_void_p),
+                ("stride_ids", C.c_int64), ("d_act", C.c_void_p), ("ld_act", C.c_int64), ("stride_act", C.c_int64),
+                ("table_type", C.c_int32), ("act_type", C.c_int32), ("id_bytes", C.c_int32),
+                ("accumulate", C.c_int32), ("scale", C.c_float)]
+
+
 class BraceError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -111,6 +119,9 @@ SIGNATURES = {
     "brace_muon_step": (C.c_int, [C.c_int32, C.c_int32, C.c_int32, C.POINTER(OrthoParams), C.POINTER(Muon),
                                   C.c_void_p, C.c_size_t, C.c_void_p]),
     "brace_ortho_status": (C.c_int, [C.c_void_p, C.c_void_p]),
+    "brace_embedding_lookup": (C.c_int, [C.POINTER(EmbeddingArgs), C.c_void_p]),
+    "brace_embedding_workspace_bytes": (C.c_size_t, [C.c_int32, C.c_int64, C.c_int32]),
+    "brace_embedding_grad": (C.c_int, [C.POINTER(EmbeddingArgs), C.c_void_p, C.c_size_t, C.c_void_p]),
 }
 
 STATIC_SCRATCH_BYTES = 8 * 1024 * 1024
@@ -482,3 +493,67 @@ class Orthogonalizer:
     def check(self, stream=None):
         """Wait for the stream; raise if a bounded device-side wait of the last call ran out."""
         _check(lib().brace_ortho_status(self.workspace.data_ptr(), _stream(stream)), "brace_ortho_status")
+
+
+class Embedding:
+    """The embedding table of `clients` clients with up to `tokens` ids each per call.
+
+    Tables (and their gradients) are tensors [clients, vocab, dim] -- views of the clients' rows of weights or updates
+    -- or [vocab, dim]; activations [clients, n, dim] or [n, dim]; ids int64 or int32 [clients, n] or [n].  The last
+    stride is 1.  `grad` = False leaves the gradient's workspace out."""
+
+    def __init__(self, vocab: int, dim: int, tokens: int, clients: int = 1, grad: bool = True, device="cuda",
+                 workspace: torch.Tensor | None = None):
+        self.clients, self.vocab, self.dim, self.tokens = clients, vocab, dim, tokens
+        if grad and workspace is None:
+            need = int(lib().brace_embedding_workspace_bytes(clients, tokens, dim))
+            workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=device)
+        self.workspace = workspace
+        self._args = EmbeddingArgs()
+
+    def _fill(self, table: torch.Tensor, ids: torch.Tensor, act: torch.Tensor, scale: float, shared: bool):
+        c, d, e = self.clients, self.dim, self._args
+        n = ids.shape[-1]
+        if tuple(ids.shape) not in ((c, n), (n,) if c == 1 else (c, n)) or n > self.tokens:
+            raise ValueError(f"ids have shape {tuple(ids.shape)}, not {(c, n)} with at most {self.tokens} tokens")
+        if ids.dtype not in (torch.int64, torch.int32) or (n > 1 and ids.stride(-1) != 1):
+            raise ValueError("ids are int64 or int32 with a contiguous last dimension")
+        tables = ((c, self.vocab, d),) + (((self.vocab, d),) if c == 1 or shared else ())
+        if tuple(table.shape) not in tables:
+            raise ValueError(f"table has shape {tuple(table.shape)}, not {tables[0]}")
+        if tuple(act.shape) != (c, n, d) and not (c == 1 and tuple(act.shape) == (n, d)):
+            raise ValueError(f"activations have shape {tuple(act.shape)}, not {(c, n, d)}")
+        for t, name in ((table, "table"), (act, "activations")):
+            if t.dtype not in _TYPES or t.dtype == torch.int32:
+                raise ValueError(f"{name} is of type {t.dtype}")
+            if d > 1 and t.stride(-1) != 1:
+                raise ValueError(f"{name}: the last dimension is not contiguous")
+        e.clients, e.dim, e.tokens, e.vocab, e.scale = c, d, n, self.vocab, scale
+        e.d_table, e.table_type = table.data_ptr(), _TYPES[table.dtype]
+        e.ld_table = table.stride(-2) if self.vocab > 1 else d
+        e.stride_table = table.stride(0) if table.dim() == 3 and c > 1 else 0
+        e.d_ids, e.id_bytes = ids.data_ptr(), 8 if ids.dtype == torch.int64 else 4
+        e.stride_ids = ids.stride(0) if c > 1 else 0
+        e.d_act, e.act_type = act.data_ptr(), _TYPES[act.dtype]
+        e.ld_act = act.stride(-2) if n > 1 else d
+        e.stride_act = act.stride(0) if c > 1 else 0
+        return e
+
+    def lookup_status(self, table, ids, out, scale: float = 1.0, stream=None) -> int:
+        return lib().brace_embedding_lookup(self._fill(table, ids, out, scale, True), _stream(stream))
+
+    def lookup(self, table: torch.Tensor, ids: torch.Tensor, out: torch.Tensor, scale: float = 1.0, stream=None):
+        """out[c, t] = scale * table[c, ids[c, t]]; 0 for an id outside the table.  A two-dimensional table serves
+        all clients."""
+        _check(self.lookup_status(table, ids, out, scale, stream), "brace_embedding_lookup")
+
+    def grad_status(self, dy, ids, grad, scale: float = 1.0, accumulate: bool = False, stream=None) -> int:
+        e = self._fill(grad, ids, dy, scale, False)
+        e.accumulate = int(accumulate)
+        ws = self.workspace
+        return lib().brace_embedding_grad(e, _ptr(ws), ws.numel() if ws is not None else 0, _stream(stream))
+
+    def grad(self, dy: torch.Tensor, ids: torch.Tensor, grad: torch.Tensor, scale: float = 1.0,
+             accumulate: bool = False, stream=None):
+        """grad[c, v] = scale * the sum of dy[c, t] over the tokens with id v (added to grad with `accumulate`)."""
+        _check(self.grad_status(dy, ids, grad, scale, accumulate, stream), "brace_embedding_grad")

@@ -12,7 +12,8 @@ ROOT = os.path.dirname(PKG_DIR)
 LIB_PATH = os.path.join(PKG_DIR, "libbrace.so")
 DEBUG_LIB_PATH = os.path.join(PKG_DIR, "libbrace_debug.so")
 SOURCES = [os.path.join(PKG_DIR, "csrc", f) for f in ("brace.cu", "operators.cu")]
-DEPS = SOURCES + [os.path.join(PKG_DIR, "csrc", f) for f in ("brace_kernels.cuh", "ortho_kernels.cuh", "sm100.cuh")]
+DEPS = SOURCES + [os.path.join(PKG_DIR, "csrc", f) for f in ("brace_kernels.cuh", "elements.cuh", "embedding_kernels.cuh",
+                                                            "ortho_kernels.cuh", "sm100.cuh")]
 DEPS += [os.path.join(ROOT, "include", "brace.h")]
 
 

@@ -1,0 +1,43 @@
+// Element types of the operators' tensors and their conversions.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+namespace brace {
+
+enum { kTypeF32 = 0, kTypeBF16 = 1, kTypeF16 = 2, kTypeBits = 3 };
+
+template <int TYPE>
+struct Elem { using T = float; };
+template <>
+struct Elem<kTypeBF16> { using T = __nv_bfloat16; };
+template <>
+struct Elem<kTypeF16> { using T = __half; };
+
+__device__ __forceinline__ float to_f32(float x) { return x; }
+__device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ float to_f32(__half x) { return __half2float(x); }
+template <typename T>
+__device__ __forceinline__ T from_f32(float x);
+template <>
+__device__ __forceinline__ float from_f32<float>(float x) { return x; }
+template <>
+__device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
+template <>
+__device__ __forceinline__ __half from_f32<__half>(float x) { return __float2half_rn(x); }
+
+template <int BYTES>
+struct WideWord;
+template <>
+struct WideWord<16> { using T = uint4; };
+template <>
+struct WideWord<8> { using T = uint2; };
+template <>
+struct WideWord<4> { using T = uint32_t; };
+template <>
+struct WideWord<2> { using T = unsigned short; };
+
+}  // namespace brace

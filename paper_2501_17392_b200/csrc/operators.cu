@@ -8,6 +8,7 @@
 #include <atomic>
 #include <cmath>
 
+#include "embedding_kernels.cuh"
 #include "ortho_kernels.cuh"
 
 namespace brace {
@@ -315,9 +316,205 @@ MatRef mat_ref(const void* p, int type, int64_t ld, int64_t stride, int64_t bit0
   return r;
 }
 
+// ---- the embedding table ----------------------------------------------------------------------------------------
+
+struct EmbPlan {
+  int64_t parts;
+  size_t off_key[2], off_pos[2], off_part, bytes;
+};
+
+EmbPlan emb_plan(int32_t clients, int64_t tokens, int32_t dim) {
+  EmbPlan q;
+  size_t at = 0;
+  auto take = [&at](int64_t bytes) {
+    const size_t here = at;
+    at += (size_t)round_up(bytes, 256);
+    return here;
+  };
+  const int64_t n = (int64_t)clients * tokens;
+  const bool merged = tokens > kSortTile;
+  for (int i = 0; i < 2; ++i) {
+    q.off_key[i] = take(i == 0 || merged ? 4 * n : 0);
+    q.off_pos[i] = take(i == 0 || merged ? 4 * n : 0);
+  }
+  q.parts = tokens / kPart;
+  q.off_part = take((int64_t)clients * q.parts * dim * 4);
+  q.bytes = at > 256 ? at : 256;
+  return q;
+}
+
+bool emb_sizes_ok(int32_t clients, int64_t tokens, int32_t dim) {
+  return clients >= 0 && clients <= 65535 && tokens >= 0 && tokens < ((int64_t)1 << 31) && dim >= 1;
+}
+
+int emb_check(const brace_embedding* e, bool grad) {
+  if (!e || !emb_sizes_ok(e->clients, e->tokens, e->dim)) return BRACE_ERR_INVALID_ARG;
+  if (e->vocab < 1 || e->vocab >= ((int64_t)1 << 31)) return BRACE_ERR_INVALID_ARG;
+  if (!float_type(e->table_type) || !float_type(e->act_type)) return BRACE_ERR_INVALID_ARG;
+  if ((e->id_bytes != 4 && e->id_bytes != 8) || !std::isfinite(e->scale)) return BRACE_ERR_INVALID_ARG;
+  // what is only read may be broadcast: rows of the gradient's activations that are all the same one
+  if (e->ld_table < e->dim || (e->ld_act < e->dim && !(grad && e->ld_act == 0))) return BRACE_ERR_INVALID_ARG;
+  return BRACE_OK;
+}
+bool emb_table_ok(const brace_embedding* e) { return e->d_table && aligned(e->d_table, (size_t)elem_bytes(e->table_type)); }
+bool emb_act_ok(const brace_embedding* e) {
+  return e->d_act && e->d_ids && aligned(e->d_act, (size_t)elem_bytes(e->act_type)) && aligned(e->d_ids, (size_t)e->id_bytes);
+}
+
+// Elements per thread: 8 where rows of both tensors are whole 16-byte words, 2 where pairs are aligned, else 1
+// (neighbouring threads then take neighbouring elements, so the accesses still coalesce).
+int emb_width(const brace_embedding* e) {
+  auto pairs = [](const void* p, int type, int64_t ld, int64_t stride) {
+    return aligned(p, 2 * (size_t)elem_bytes(type)) && ld % 2 == 0 && stride % 2 == 0;
+  };
+  if (e->dim % 8 == 0 && wide_rows(e->d_table, e->table_type, e->ld_table, e->stride_table) &&
+      wide_rows(e->d_act, e->act_type, e->ld_act, e->stride_act))
+    return 8;
+  if (e->dim % 2 == 0 && pairs(e->d_table, e->table_type, e->ld_table, e->stride_table) &&
+      pairs(e->d_act, e->act_type, e->ld_act, e->stride_act))
+    return 2;
+  return 1;
+}
+
+EmbArgs emb_args(const brace_embedding* e) {
+  EmbArgs a = {};
+  a.ids = e->d_ids;
+  a.ld_table = e->ld_table;
+  a.stride_table = e->stride_table;
+  a.stride_ids = e->stride_ids;
+  a.ld_act = e->ld_act;
+  a.stride_act = e->stride_act;
+  a.tokens = e->tokens;
+  a.vocab = e->vocab;
+  a.clients = e->clients;
+  a.dim = e->dim;
+  a.id_bytes = e->id_bytes;
+  a.scale = e->scale;
+  a.accumulate = e->accumulate != 0;
+  return a;
+}
+
+// Calls f.template operator()<T>() with the element type.
+template <typename F>
+cudaError_t with_type(int type, F&& f) {
+  if (type == BRACE_TYPE_F32) return f(float{});
+  if (type == BRACE_TYPE_BF16) return f(__nv_bfloat16{});
+  return f(__half{});
+}
+
+template <typename TI, typename TO, int V>
+cudaError_t launch_lookup(const EmbArgs& a, cudaStream_t st) {
+  const int64_t groups = a.tokens * (a.dim / V);
+  // four groups per thread once that still gives every SM work
+  if (groups * a.clients >= (int64_t)4 * 256 * 4 * sm_count())
+    return launch(embedding_lookup_kernel<TI, TO, V, 4>, dim3((unsigned)((groups + 1023) / 1024), (unsigned)a.clients), 256, 0, 1, st, a);
+  return launch(embedding_lookup_kernel<TI, TO, V, 1>, dim3((unsigned)((groups + 255) / 256), (unsigned)a.clients), 256, 0, 1, st, a);
+}
+
+cudaError_t launch_sort(const EmbArgs& a, cudaStream_t st) {
+  int bits = 0;
+  while ((a.vocab >> bits) != 0) ++bits;   // the largest value of these bits stands for "no token"
+  if (a.tokens <= 1024) {
+    const int threads = (int)round_up(a.tokens, 32);
+    const size_t smem = (size_t)threads * 8 + (size_t)kDigits * (threads / 32) * 4;
+    return launch(embedding_sort_kernel<1>, dim3(1, (unsigned)a.clients), threads, smem, 1, st, a, threads, bits);
+  }
+  const int threads = (int)(a.tokens < kSortTile ? round_up(a.tokens, 32 * kSortItems) / kSortItems : 1024);
+  const int tile = threads * kSortItems;
+  const size_t smem = (size_t)tile * 8 + (size_t)kDigits * (threads / 32) * 4;
+  cudaError_t err = cudaFuncSetAttribute(embedding_sort_kernel<kSortItems>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                         kSortTile * 8 + kDigits * 32 * 4);
+  if (err != cudaSuccess) return err;
+  return launch(embedding_sort_kernel<kSortItems>, dim3((unsigned)((a.tokens + tile - 1) / tile), (unsigned)a.clients),
+                threads, smem, 1, st, a, tile, bits);
+}
+
+template <typename TI, typename TO, int V>
+cudaError_t launch_grad(EmbArgs a, cudaStream_t st) {
+  if (a.parts > 0) {
+    const cudaError_t err =
+        launch(embedding_part_kernel<TI, V>,
+               dim3((unsigned)a.parts, (unsigned)((a.dim / V + 127) / 128), (unsigned)a.clients), 128, 0, 1, st, a);
+    if (err != cudaSuccess) return err;
+  }
+  const int rows = 16384 / a.dim;
+  a.rows_cta = rows < 1 ? 1 : rows > 64 ? 64 : rows;
+  return launch(embedding_grad_kernel<TI, TO, V>,
+                dim3((unsigned)((a.vocab + a.rows_cta - 1) / a.rows_cta), (unsigned)a.clients), 256, 0, 1, st, a);
+}
+
 }  // namespace
 
 extern "C" {
+
+int brace_embedding_lookup(const brace_embedding* e, brace_stream_t stream) {
+  const int rc = emb_check(e, false);
+  if (rc != BRACE_OK) return rc;
+  if (e->clients == 0 || e->tokens == 0) return BRACE_OK;
+  if (!emb_table_ok(e) || !emb_act_ok(e) || (e->clients > 1 && e->stride_act == 0)) return BRACE_ERR_INVALID_ARG;
+  EmbArgs a = emb_args(e);
+  a.table = e->d_table;
+  a.out = e->d_act;
+  const cudaStream_t st = (cudaStream_t)stream;
+  const int width = emb_width(e);
+  cudaGetLastError();
+  const cudaError_t err = with_type(e->table_type, [&](auto ti) {
+    return with_type(e->act_type, [&](auto to) {
+      using TI = decltype(ti);
+      using TO = decltype(to);
+      return width == 8 ? launch_lookup<TI, TO, 8>(a, st) : width == 2 ? launch_lookup<TI, TO, 2>(a, st) : launch_lookup<TI, TO, 1>(a, st);
+    });
+  });
+  return err == cudaSuccess ? BRACE_OK : cuda_fail_no_ctx(err);
+}
+
+size_t brace_embedding_workspace_bytes(int32_t clients, int64_t tokens, int32_t dim) {
+  return emb_sizes_ok(clients, tokens, dim) ? emb_plan(clients, tokens, dim).bytes : 0;
+}
+
+int brace_embedding_grad(const brace_embedding* e, void* d_workspace, size_t workspace_bytes, brace_stream_t stream) {
+  const int rc = emb_check(e, true);
+  if (rc != BRACE_OK) return rc;
+  if (e->clients == 0) return BRACE_OK;
+  if (!emb_table_ok(e) || (e->tokens > 0 && !emb_act_ok(e)) || (e->clients > 1 && e->stride_table == 0))
+    return BRACE_ERR_INVALID_ARG;
+  const EmbPlan q = emb_plan(e->clients, e->tokens, e->dim);
+  if (!d_workspace || workspace_bytes < q.bytes || !aligned(d_workspace, 256)) return BRACE_ERR_WORKSPACE;
+  if (e->tokens == 0 && e->accumulate) return BRACE_OK;
+  char* ws = (char*)d_workspace;
+  EmbArgs a = emb_args(e);
+  a.grad = e->d_table;
+  a.in = e->d_act;
+  a.key = (uint32_t*)(ws + q.off_key[0]);
+  a.pos = (uint32_t*)(ws + q.off_pos[0]);
+  a.part = (float*)(ws + q.off_part);
+  a.parts = q.parts;
+  const cudaStream_t st = (cudaStream_t)stream;
+  cudaGetLastError();
+  cudaError_t err = cudaSuccess;
+  if (a.tokens > 0) {
+    err = launch_sort(a, st);
+    int from = 0;
+    for (int64_t run = kSortTile; err == cudaSuccess && run < a.tokens; run *= kMergeRuns) {
+      uint32_t *key = (uint32_t*)(ws + q.off_key[from ^ 1]), *pos = (uint32_t*)(ws + q.off_pos[from ^ 1]);
+      err = launch(embedding_merge_kernel, dim3((unsigned)((a.tokens + 255) / 256), (unsigned)a.clients), 256, 0, 1, st, a, run, key, pos);
+      a.key = key;
+      a.pos = pos;
+      from ^= 1;
+    }
+  }
+  if (err == cudaSuccess) {
+    const int width = emb_width(e);
+    err = with_type(e->act_type, [&](auto ti) {
+      return with_type(e->table_type, [&](auto to) {
+        using TI = decltype(ti);
+        using TO = decltype(to);
+        return width == 8 ? launch_grad<TI, TO, 8>(a, st) : width == 2 ? launch_grad<TI, TO, 2>(a, st) : launch_grad<TI, TO, 1>(a, st);
+      });
+    });
+  }
+  return err == cudaSuccess ? BRACE_OK : cuda_fail_no_ctx(err);
+}
 
 int brace_ortho_default_params(brace_ortho_params* params) {
   if (!params) return BRACE_ERR_INVALID_ARG;

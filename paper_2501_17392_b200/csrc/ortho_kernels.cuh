@@ -18,14 +18,10 @@
 // their mirror images.  That takes a step from 2 m^2 k + 2 m^3 + 2 m^2 k operations to m^2 k + m^3 + 2 m^2 k.
 #pragma once
 
-#include <cuda_bf16.h>
-#include <cuda_fp16.h>
-
+#include "elements.cuh"
 #include "sm100.cuh"
 
 namespace brace {
-
-enum { kTypeF32 = 0, kTypeBF16 = 1, kTypeF16 = 2, kTypeBits = 3 };
 
 constexpr float kScaleX = 16384.f;                  // stored X = X * 2^14
 constexpr float kScaleSInv = 1.f / 16384.f;         // X X^T * 2^28 -> S * 2^14
@@ -41,25 +37,6 @@ struct MatRef {
   int vec;   // 8 consecutive elements of a row, from a multiple of 8, can be read as whole 16-byte words
   int64_t bit0;
 };
-
-template <int TYPE>
-struct Elem { using T = float; };
-template <>
-struct Elem<kTypeBF16> { using T = __nv_bfloat16; };
-template <>
-struct Elem<kTypeF16> { using T = __half; };
-
-__device__ __forceinline__ float to_f32(float x) { return x; }
-__device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
-__device__ __forceinline__ float to_f32(__half x) { return __half2float(x); }
-template <typename T>
-__device__ __forceinline__ T from_f32(float x);
-template <>
-__device__ __forceinline__ float from_f32<float>(float x) { return x; }
-template <>
-__device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
-template <>
-__device__ __forceinline__ __half from_f32<__half>(float x) { return __float2half_rn(x); }
 
 // 8 elements of a row from column `col`; `n` of them exist (the others read as 0).
 template <typename T>
