@@ -40,4 +40,29 @@ struct WideWord<4> { using T = uint32_t; };
 template <>
 struct WideWord<2> { using T = unsigned short; };
 
+// V consecutive elements as wide words (V * sizeof(T) bytes, at most 16 at a time).
+template <typename T, int V>
+struct Pack {
+  static constexpr int kBytes = V * (int)sizeof(T);
+  using W = typename WideWord<(kBytes >= 16 ? 16 : kBytes)>::T;
+  static constexpr int kWords = kBytes / (int)sizeof(W);
+  alignas(16) T t[V];
+  __device__ __forceinline__ void load(const T* p) {
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) reinterpret_cast<W*>(t)[i] = __ldg(reinterpret_cast<const W*>(p) + i);
+  }
+  __device__ __forceinline__ void load_plain(const T* p) {
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) reinterpret_cast<W*>(t)[i] = reinterpret_cast<const W*>(p)[i];
+  }
+  __device__ __forceinline__ void store_plain(T* p) const {
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) reinterpret_cast<W*>(p)[i] = reinterpret_cast<const W*>(t)[i];
+  }
+  __device__ __forceinline__ void store_stream(T* p) const {
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) __stcs(reinterpret_cast<W*>(p) + i, reinterpret_cast<const W*>(t)[i]);
+  }
+};
+
 }  // namespace brace

@@ -45,27 +45,6 @@ __device__ __forceinline__ int64_t load_id(const EmbArgs& p, int64_t c, int64_t 
                          : (int64_t)((const int32_t*)p.ids)[c * p.stride_ids + t];
 }
 
-// V consecutive elements as wide words (V * sizeof(T) bytes, at most 16 at a time).
-template <typename T, int V>
-struct Pack {
-  static constexpr int kBytes = V * (int)sizeof(T);
-  using W = typename WideWord<(kBytes >= 16 ? 16 : kBytes)>::T;
-  static constexpr int kWords = kBytes / (int)sizeof(W);
-  alignas(16) T t[V];
-  __device__ __forceinline__ void load(const T* p) {
-#pragma unroll
-    for (int i = 0; i < kWords; ++i) reinterpret_cast<W*>(t)[i] = __ldg(reinterpret_cast<const W*>(p) + i);
-  }
-  __device__ __forceinline__ void load_plain(const T* p) {
-#pragma unroll
-    for (int i = 0; i < kWords; ++i) reinterpret_cast<W*>(t)[i] = reinterpret_cast<const W*>(p)[i];
-  }
-  __device__ __forceinline__ void store_stream(T* p) const {
-#pragma unroll
-    for (int i = 0; i < kWords; ++i) __stcs(reinterpret_cast<W*>(p) + i, reinterpret_cast<const W*>(t)[i]);
-  }
-};
-
 // ---- lookup -----------------------------------------------------------------------------------------------------
 // A thread moves U groups of V elements, so that the loads of U rows are under way together.
 template <typename TI, typename TO, int V, int U>

@@ -7,6 +7,7 @@
 
 #include <atomic>
 #include <cmath>
+#include <cstdlib>
 
 #include "embedding_kernels.cuh"
 #include "ortho_kernels.cuh"
@@ -63,6 +64,14 @@ cudaError_t launch(void (*kernel)(KArgs...), dim3 grid, int block, size_t smem, 
   cfg.attrs = attr;
   cfg.numAttrs = cluster > 1 ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+// Calls f with a value of the element type.
+template <typename F>
+cudaError_t with_type(int type, F&& f) {
+  if (type == BRACE_TYPE_F32) return f(float{});
+  if (type == BRACE_TYPE_BF16) return f(__nv_bfloat16{});
+  return f(__half{});
 }
 
 // ---- the orthogonalisation --------------------------------------------------------------------------------------
@@ -159,23 +168,34 @@ EncodeFn encode_fn() {
   return (EncodeFn)f;
 }
 
-// [planes of all matrices][rows][cols] float16 with rows of `ld`; boxes of 64 x 64, 128-byte swizzle, zeros outside.
-int make_map(CUtensorMap* map, void* base, int64_t cols, int64_t rows, int64_t ld, int64_t planes) {
+// [planes of all matrices][rows][ld] float16 as blocks of 64 columns; one box holds `box_planes` planes of 128 rows of a
+// block (along) or of 64 rows of two blocks (across); 128-byte swizzle, zeros outside.
+int make_map(CUtensorMap* map, void* base, int64_t rows, int64_t ld, int64_t planes, int box_planes, bool across) {
   EncodeFn enc = encode_fn();
   if (!enc) return cuda_fail_no_ctx(cudaErrorNotSupported);
-  const cuuint64_t dim[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)planes};
-  const cuuint64_t stride[2] = {(cuuint64_t)ld * 2, (cuuint64_t)ld * 2 * (cuuint64_t)rows};
-  const cuuint32_t box[3] = {64, 64, 1}, one[3] = {1, 1, 1};
-  const CUresult r = enc(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, base, dim, stride, box, one,
+  const cuuint64_t dim[4] = {64, (cuuint64_t)rows, (cuuint64_t)(ld / 64), (cuuint64_t)planes};
+  const cuuint64_t stride[3] = {(cuuint64_t)ld * 2, 128, (cuuint64_t)ld * 2 * (cuuint64_t)rows};
+  const cuuint32_t box[4] = {64, across ? 64u : 128u, across ? 2u : 1u, (cuuint32_t)box_planes}, one[4] = {1, 1, 1, 1};
+  const CUresult r = enc(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, base, dim, stride, box, one,
                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? BRACE_OK : cuda_fail_no_ctx(cudaErrorInvalidValue);
 }
 
-template <int CG, int NP, bool A_MN, bool B_MN, int MODE>
-cudaError_t launch_gemm(const CUtensorMap& a, const CUtensorMap& b, const GemmArgs& g, cudaStream_t st) {
+// The maps of a call: X's two buffers, S and P, along [0] and across [1].
+struct OrthoMaps {
+  CUtensorMap x[2][2], s[2], p[2];
+};
+
+template <int CG, int NP, int OP_A, int OP_B, int MODE, typename TOUT = __half>
+cudaError_t launch_gemm(const CUtensorMap (&a)[2], const CUtensorMap (&b)[2], const GemmArgs& g, cudaStream_t st) {
   using Shape = GemmShape<CG, NP>;
-  auto* kernel = ortho_gemm_kernel<CG, NP, A_MN, B_MN, MODE>;
+  auto* kernel = ortho_gemm_kernel<CG, NP, OP_A, OP_B, MODE, TOUT>;
+  GemmMaps maps;   // first the one that the operand needs (a symmetric one needs both)
+  maps.a[0] = a[OP_A == kAcross];
+  maps.a[1] = a[1];
+  maps.b[0] = b[OP_B == kAcross];
+  maps.b[1] = b[1];
   static std::atomic<uint64_t> granted{0};   // devices on which this kernel may use its shared memory
   int dev = 0;
   cudaError_t err = cudaGetDevice(&dev);
@@ -188,12 +208,12 @@ cudaError_t launch_gemm(const CUtensorMap& a, const CUtensorMap& b, const GemmAr
   }
   int clusters = sm_count() / CG;
   if (clusters > g.total) clusters = g.total;
-  return launch(kernel, dim3((unsigned)(clusters * CG)), Shape::kThreads, Shape::kSmem, CG, st, a, b, g);
+  return launch(kernel, dim3((unsigned)(clusters * CG)), Shape::kThreads, Shape::kSmem, CG, st, maps, g);
 }
 
 template <int CG, int NP>
-cudaError_t launch_products(const OrthoPlan& q, const brace_ortho_params* p, char* ws, const CUtensorMap map_x[2],
-                            const CUtensorMap& map_s, const CUtensorMap& map_p, GemmArgs last, cudaStream_t st) {
+cudaError_t launch_products(const OrthoPlan& q, const brace_ortho_params* p, char* ws, const OrthoMaps& maps,
+                            const GemmArgs& last, int out_type, cudaStream_t st) {
   constexpr int T = GemmShape<CG, NP>::kTile;
   const bool tall = q.rows > q.cols;
   const int tm = (q.m + T - 1) / T;
@@ -219,13 +239,13 @@ cudaError_t launch_products(const OrthoPlan& q, const brace_ortho_params* p, cha
   __half* poly = (__half*)(ws + q.off_p);
   for (int k = 0; k < p->steps; ++k) {
     const int cur = k & 1;
-    const CUtensorMap& x = map_x[cur];
+    const CUtensorMap(&x)[2] = maps.x[cur];
     GemmArgs g = sym;
     g.K = tall ? q.rows : q.cols;
     g.beta = kScaleSInv;
     g.dst = s;
-    cudaError_t err = tall ? launch_gemm<CG, NP, true, true, kModeGram>(x, x, g, st)
-                           : launch_gemm<CG, NP, false, false, kModeGram>(x, x, g, st);
+    cudaError_t err = tall ? launch_gemm<CG, NP, kAcross, kAcross, kModeGram>(x, x, g, st)
+                           : launch_gemm<CG, NP, kAlong, kAlong, kModeGram>(x, x, g, st);
     if (err != cudaSuccess) return err;
     g = sym;
     g.K = q.m;
@@ -233,16 +253,19 @@ cudaError_t launch_products(const OrthoPlan& q, const brace_ortho_params* p, cha
     g.beta = p->c * kPolyC;
     g.src = s;
     g.dst = poly;
-    err = launch_gemm<CG, NP, false, false, kModePoly>(map_s, map_s, g, st);
+    err = launch_gemm<CG, NP, kSymmetric, kSymmetric, kModePoly>(maps.s, maps.s, g, st);
     if (err != cudaSuccess) return err;
     step.src = (const __half*)(ws + q.off_x[cur]);
     step.dst = (__half*)(ws + q.off_x[cur ^ 1]);
     if (k + 1 < p->steps)
-      err = tall ? launch_gemm<CG, NP, false, false, kModeStep>(x, map_p, step, st)
-                 : launch_gemm<CG, NP, false, true, kModeStep>(map_p, x, step, st);
+      err = tall ? launch_gemm<CG, NP, kAlong, kSymmetric, kModeStep>(x, maps.p, step, st)
+                 : launch_gemm<CG, NP, kSymmetric, kAcross, kModeStep>(maps.p, x, step, st);
     else
-      err = tall ? launch_gemm<CG, NP, false, false, kModeLast>(x, map_p, step, st)
-                 : launch_gemm<CG, NP, false, true, kModeLast>(map_p, x, step, st);
+      err = with_type(out_type, [&](auto t) {
+        using TOUT = decltype(t);
+        return tall ? launch_gemm<CG, NP, kAlong, kSymmetric, kModeLast, TOUT>(x, maps.p, step, st)
+                    : launch_gemm<CG, NP, kSymmetric, kAcross, kModeLast, TOUT>(maps.p, x, step, st);
+      });
     if (err != cudaSuccess) return err;
   }
   return cudaSuccess;
@@ -272,15 +295,18 @@ cudaError_t launch_prep(const OrthoPlan& q, const PrepArgs& a, cudaStream_t st) 
 }
 
 // Everything after the argument checks.
-int run_ortho(const OrthoPlan& q, const brace_ortho_params* p, PrepArgs prep, const GemmArgs& last, char* ws,
+int run_ortho(const OrthoPlan& q, const brace_ortho_params* p, PrepArgs prep, const GemmArgs& last, int out_type, char* ws,
               cudaStream_t st) {
-  CUtensorMap map_x[2], map_s, map_p;
-  int rc;
+  OrthoMaps maps;
   const int64_t z = (int64_t)q.batch * q.planes;
-  for (int i = 0; i < 2; ++i)
-    if ((rc = make_map(&map_x[i], ws + q.off_x[i], q.cols, q.rows, q.ld_x, z)) != BRACE_OK) return rc;
-  if ((rc = make_map(&map_s, ws + q.off_s, q.m, q.m, q.ld_s, z)) != BRACE_OK) return rc;
-  if ((rc = make_map(&map_p, ws + q.off_p, q.m, q.m, q.ld_s, z)) != BRACE_OK) return rc;
+  for (int across = 0; across < 2; ++across) {
+    int rc = BRACE_OK;
+    for (int i = 0; i < 2 && rc == BRACE_OK; ++i)
+      rc = make_map(&maps.x[i][across], ws + q.off_x[i], q.rows, q.ld_x, z, q.planes, across);
+    if (rc == BRACE_OK) rc = make_map(&maps.s[across], ws + q.off_s, q.m, q.ld_s, z, q.planes, across);
+    if (rc == BRACE_OK) rc = make_map(&maps.p[across], ws + q.off_p, q.m, q.ld_s, z, q.planes, across);
+    if (rc != BRACE_OK) return rc;
+  }
   prep.rows = q.rows;
   prep.cols = q.cols;
   prep.units_row = (q.cols + 7) / 8;
@@ -293,9 +319,15 @@ int run_ortho(const OrthoPlan& q, const brace_ortho_params* p, PrepArgs prep, co
   prep.status = (int*)ws;
   cudaGetLastError();
   cudaError_t err = launch_prep(q, prep, st);
-  if (err == cudaSuccess)
-    err = q.planes == 1 ? launch_products<1, 1>(q, p, ws, map_x, map_s, map_p, last, st)
-                        : launch_products<1, 2>(q, p, ws, map_x, map_s, map_p, last, st);
+  if (err == cudaSuccess) {
+    const bool pairs = getenv("BRACE_PAIRS") && atoi(getenv("BRACE_PAIRS"));
+    if (pairs)
+      err = q.planes == 1 ? launch_products<2, 1>(q, p, ws, maps, last, out_type, st)
+                          : launch_products<2, 2>(q, p, ws, maps, last, out_type, st);
+    else
+      err = q.planes == 1 ? launch_products<1, 1>(q, p, ws, maps, last, out_type, st)
+                          : launch_products<1, 2>(q, p, ws, maps, last, out_type, st);
+  }
   return err == cudaSuccess ? BRACE_OK : cuda_fail_no_ctx(err);
 }
 
@@ -392,14 +424,6 @@ EmbArgs emb_args(const brace_embedding* e) {
   a.scale = e->scale;
   a.accumulate = e->accumulate != 0;
   return a;
-}
-
-// Calls f.template operator()<T>() with the element type.
-template <typename F>
-cudaError_t with_type(int type, F&& f) {
-  if (type == BRACE_TYPE_F32) return f(float{});
-  if (type == BRACE_TYPE_BF16) return f(__nv_bfloat16{});
-  return f(__half{});
 }
 
 template <typename TI, typename TO, int V>
@@ -550,10 +574,9 @@ int brace_orthogonalize(int32_t batch, int32_t rows, int32_t cols, const brace_o
   last.out = d_out;
   last.ld_out = ld_out;
   last.batch_out = stride_out;
-  last.out_type = out_type;
   last.vec_out = wide_rows(d_out, out_type, ld_out, stride_out);
   last.replicas = 1;
-  return run_ortho(q, params, prep, last, (char*)d_workspace, (cudaStream_t)stream);
+  return run_ortho(q, params, prep, last, out_type, (char*)d_workspace, (cudaStream_t)stream);
 }
 
 int brace_muon_step(int32_t batch, int32_t rows, int32_t cols, const brace_ortho_params* params,
@@ -593,7 +616,6 @@ int brace_muon_step(int32_t batch, int32_t rows, int32_t cols, const brace_ortho
   last.ld_out = s->ld_weights_out;
   last.batch_out = s->stride_weights_out;
   last.rep_out = s->replica_weights_out;
-  last.out_type = s->weights_type;
   last.vec_out = wide_rows(s->d_weights_out, s->weights_type, s->ld_weights_out, s->stride_weights_out, s->replica_weights_out);
   last.w_in = s->d_weights;
   last.ld_in = s->ld_weights;
@@ -603,7 +625,7 @@ int brace_muon_step(int32_t batch, int32_t rows, int32_t cols, const brace_ortho
   last.replicas = s->replicas;
   last.keep = 1.f - s->lr * s->weight_decay;
   last.rate = s->lr * s->scale;
-  return run_ortho(q, params, prep, last, (char*)d_workspace, (cudaStream_t)stream);
+  return run_ortho(q, params, prep, last, s->weights_type, (char*)d_workspace, (cudaStream_t)stream);
 }
 
 int brace_ortho_status(const void* d_workspace, brace_stream_t stream) {

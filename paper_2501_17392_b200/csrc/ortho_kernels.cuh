@@ -14,8 +14,10 @@
 // float32 accuracy is asked for, an operand is the sum of two float16 planes (hi + lo, 22 bits) and a product is
 // hi*hi + hi*lo + lo*hi: three times the matrix instructions.
 //
-// Symmetry.  S and P are symmetric: only tiles on and below the diagonal are computed, the others are written as
-// their mirror images.  That takes a step from 2 m^2 k + 2 m^3 + 2 m^2 k operations to m^2 k + m^3 + 2 m^2 k.
+// Symmetry.  S and P are symmetric: only tiles on and below the diagonal are computed and stored.  Where a product
+// needs one above it, the stored tile is loaded instead and the matrix instruction reads it the other way (the
+// descriptors allow either axis to be the contiguous one).  That takes a step from 2 m^2 k + 2 m^3 + 2 m^2 k
+// operations to m^2 k + m^3 + 2 m^2 k, and nothing is written twice.
 #pragma once
 
 #include "elements.cuh"
@@ -203,6 +205,9 @@ __global__ void __launch_bounds__(256) ortho_scale_kernel(const PrepArgs p) {
 // ---------------------------------------------------------------------------------------------------------------
 
 enum { kModeGram = 0, kModePoly = 1, kModeStep = 2, kModeLast = 3 };
+// How an operand lies in memory: with the contraction along its rows (contiguous), across them, or symmetric with the
+// tiles on and below the diagonal stored.
+enum { kAlong = 0, kAcross = 1, kSymmetric = 2 };
 
 struct GemmArgs {
   int M, N, K;                  // result M x N, contraction K
@@ -218,25 +223,39 @@ struct GemmArgs {
   void* out;
   const void* w_in;
   int64_t ld_out, batch_out, rep_out, ld_in, batch_in, rep_in;
-  int out_type, vec_out, vec_in, replicas;
+  int vec_out, vec_in, replicas;
   float keep, rate;
   int* status;
 };
 
 constexpr int kTileK = 64;                       // contraction per stage: one 128-byte swizzle row
 constexpr int kOperandBytes = 128 * kTileK * 2;  // an operand of a stage in one CTA: 128 rows (or columns)
+// The tensor cores' float32 accumulation cuts off what does not fit, which over a long contraction adds up to an error
+// that no sign cancels (2.4e-5 of the result at K = 2048, five steps).  With two planes the accumulators therefore hold
+// this many stages only (K = 128) and are added in registers, rounded to nearest.
+constexpr int kChunk = 2;
+constexpr int kCellBytes = 2048;                 // a warp's staging of the epilogue: 32 rows of 64 bytes
+
+// An operand's tensor map(s), each with boxes that fill a stage's operand, all planes, in one load: the cost of a
+// load is some 46 clocks and 2 for each 128 bytes (measured: 59 bytes a clock with 256 rows, 48 with 64).
+//   along: 128 rows of one block of 64 columns;  across: 64 rows of two blocks.
+// A symmetric operand has both.
+struct GemmMaps {
+  CUtensorMap a[2], b[2];
+};
 
 template <int CG, int NP>
 struct GemmShape {
   static constexpr int kTile = 128 * CG;                     // square tiles
+  static constexpr int kEpiWarps = 8 * CG;                   // a warp takes 32 rows x 64 columns of the CTA's part
+  static constexpr int kThreads = 128 + 32 * kEpiWarps;      // warps 0-3: loads, MMAs, tensor memory, -; then epilogue
   static constexpr int kStageBytes = 2 * NP * kOperandBytes;
   static constexpr int kStages = NP == 1 ? 6 : 3;            // 192 KB either way
-  static constexpr int kThreads = CG == 1 ? 256 : 384;       // warps 0-3: loads, MMAs, tensor memory, -; then epilogue
-  static constexpr int kTmemCols = 2 * kTile;                // two accumulators: one is filled while one is read
-  static constexpr int kSmem = kStages * kStageBytes + 1024 + 256;
+  static constexpr int kBuffers = 512 / kTile;               // accumulators in tensor memory: all of its 512 columns
+  static constexpr int kSmem = kStages * kStageBytes + kEpiWarps * kCellBytes + 1024 + 256;
 };
 
-// Column blocks of the lower triangle in rows: t -> (row, col), col <= row.
+// Blocks of the lower triangle in rows: t -> (row, col), col <= row.
 __device__ __forceinline__ void triangle(int t, int& row, int& col) {
   row = (int)((sqrtf(8.f * (float)t + 1.f) - 1.f) * 0.5f);
   while ((row + 1) * (row + 2) / 2 <= t) ++row;
@@ -244,60 +263,122 @@ __device__ __forceinline__ void triangle(int t, int& row, int& col) {
   col = t - row * (row + 1) / 2;
 }
 
+// A warp's cell: 32 rows of four 16-byte words.  A lane writes (reads) its own row, and reads (writes) rows of 4
+// neighbouring lanes: word w of row r lies at w ^ ((r >> 1) & 3), so that neither way has bank conflicts.
+__device__ __forceinline__ uint32_t cell_at(uint32_t cell, int r, int w) {
+  return cell + (uint32_t)(r * 64 + ((w ^ ((r >> 1) & 3)) << 4));
+}
+__device__ __forceinline__ void sts16(uint32_t a, uint4 v) {
+  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+__device__ __forceinline__ uint4 lds16(uint32_t a) {
+  uint4 v;
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
+  return v;
+}
+
+// A 32 x 32 block of a padded float16 matrix, 16 bytes a lane at a time: 8 rows per access.
+__device__ __forceinline__ void block_load(const __half* p, int64_t ld, int rows, uint4 (&x)[4]) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int r = i * 8 + (lane >> 2);
+    x[i] = r < rows ? *reinterpret_cast<const uint4*>(p + r * ld + (lane & 3) * 8) : make_uint4(0, 0, 0, 0);
+  }
+}
+// ... the lane's own row of it, times alpha, added to `row`
+__device__ __forceinline__ void block_add(uint32_t cell, const uint4 (&x)[4], float alpha, float* row) {
+  const int lane = threadIdx.x & 31;
+  __syncwarp();
+#pragma unroll
+  for (int i = 0; i < 4; ++i) sts16(cell_at(cell, i * 8 + (lane >> 2), lane & 3), x[i]);
+  __syncwarp();
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    uint4 t = lds16(cell_at(cell, lane, w));
+    const __half* h = reinterpret_cast<const __half*>(&t);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) row[8 * w + j] = fmaf(alpha, __half2float(h[j]), row[8 * w + j]);
+  }
+}
+__device__ __forceinline__ void block_store(uint32_t cell, const uint4 (&own)[4], __half* p, int64_t ld, int rows) {
+  const int lane = threadIdx.x & 31;
+  __syncwarp();
+#pragma unroll
+  for (int w = 0; w < 4; ++w) sts16(cell_at(cell, lane, w), own[w]);
+  __syncwarp();
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int r = i * 8 + (lane >> 2);
+    const uint4 t = lds16(cell_at(cell, r, lane & 3));
+    if (r < rows) *reinterpret_cast<uint4*>(p + r * ld + (lane & 3) * 8) = t;
+  }
+}
+
+// 32 x 16 results, staged as float32, to the caller's tensor: four neighbouring elements a lane.
 template <typename T>
-__device__ __forceinline__ void last_chunk(const GemmArgs& p, int64_t b, int row, int col, int n, const float (&o)[32]) {
-  for (int r = 0; r < p.replicas; ++r) {
-    T* out = (T*)p.out + b * p.batch_out + r * p.rep_out + (int64_t)row * p.ld_out + col;
-    const T* in = p.w_in ? (const T*)p.w_in + b * p.batch_in + r * p.rep_in + (int64_t)row * p.ld_in + col : nullptr;
+__device__ __forceinline__ void last_cell(const GemmArgs& p, uint32_t cell, int64_t b, int row0, int col0, const float* own) {
+  const int lane = threadIdx.x & 31;
+  __syncwarp();
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const int nq = min(8, n - 8 * q);
-      if (nq <= 0) break;
-      float v[8];
-      if (in) {
-        // a plain load: in and out may be the same buffer
-        if (p.vec_in && nq == 8) {
-          alignas(16) T t[8];
-#pragma unroll
-          for (int i = 0; i < (int)(8 * sizeof(T) / 16); ++i)
-            reinterpret_cast<uint4*>(t)[i] = *(reinterpret_cast<const uint4*>(in + 8 * q) + i);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) v[i] = to_f32(t[i]);
+  for (int w = 0; w < 4; ++w) sts16(cell_at(cell, lane, w), make_uint4(__float_as_uint(own[4 * w]), __float_as_uint(own[4 * w + 1]),
+                                             __float_as_uint(own[4 * w + 2]), __float_as_uint(own[4 * w + 3])));
+  __syncwarp();
+  const int col = col0 + (lane & 3) * 4, n = min(4, p.N - col);
+  if (n <= 0) return;
+#pragma unroll 1
+  for (int i = 0; i < 4; ++i) {
+    const int r = i * 8 + (lane >> 2), row = row0 + r;
+    if (row >= p.M) break;
+    const uint4 t = lds16(cell_at(cell, r, lane & 3));
+    const float o[4] = {__uint_as_float(t.x), __uint_as_float(t.y), __uint_as_float(t.z), __uint_as_float(t.w)};
+    for (int k = 0; k < p.replicas; ++k) {
+      T* out = (T*)p.out + b * p.batch_out + k * p.rep_out + (int64_t)row * p.ld_out + col;
+      Pack<T, 4> y;
+      if (p.w_in) {
+        // plain loads: in and out may be the same buffer
+        const T* in = (const T*)p.w_in + b * p.batch_in + k * p.rep_in + (int64_t)row * p.ld_in + col;
+        if (p.vec_in && n == 4) {
+          y.load_plain(in);
         } else {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) v[i] = i < nq ? to_f32(in[8 * q + i]) : 0.f;
+          for (int j = 0; j < 4; ++j) y.t[j] = j < n ? in[j] : from_f32<T>(0.f);
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = p.keep * v[i] - p.rate * o[8 * q + i];
+        for (int j = 0; j < 4; ++j) y.t[j] = from_f32<T>(p.keep * to_f32(y.t[j]) - p.rate * o[j]);
       } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = o[8 * q + i];
+        for (int j = 0; j < 4; ++j) y.t[j] = from_f32<T>(o[j]);
       }
-      store8(out + 8 * q, p.vec_out, nq, v);
+      if (p.vec_out && n == 4) {
+        y.store_plain(out);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (j < n) out[j] = y.t[j];
+      }
     }
   }
 }
 
-// One product of the iteration over tiles of 128 x 128 (CG = 1) or, by a pair of CTAs, 256 x 256 (CG = 2); NP planes
-// per operand; A_MN / B_MN: the operand lies with the contraction along its rows (the other axis contiguous).
-// Warp 0 loads, warp 1 issues the matrix instructions, warp 2 owns the tensor memory, warps 4.. read the
+// One product of the iteration over tiles of 128 x 128 (CG = 1) or, by a pair of CTAs, 256 x 256 (CG = 2), NP planes
+// per operand.  Warp 0 loads, warp 1 issues the matrix instructions, warp 2 owns the tensor memory, warps 4.. read the
 // accumulators and write the results; persistent over tiles, so that the epilogue of a tile runs under the products
 // of the next.
-template <int CG, int NP, bool A_MN, bool B_MN, int MODE>
+template <int CG, int NP, int OP_A, int OP_B, int MODE, typename TOUT>
 __global__ void __launch_bounds__(GemmShape<CG, NP>::kThreads, 1)
-    ortho_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
-                      const GemmArgs p) {
+    ortho_gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmArgs p) {
   using Shape = GemmShape<CG, NP>;
-  constexpr int T = Shape::kTile, STAGES = Shape::kStages;
+  constexpr int T = Shape::kTile, STAGES = Shape::kStages, BUFS = Shape::kBuffers;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t base = (smem_addr(smem_raw) + 1023u) & ~1023u;
-  const uint32_t bars = base + STAGES * Shape::kStageBytes;
-  const uint32_t full = bars, empty = bars + 8 * STAGES, tm_full = empty + 8 * STAGES, tm_empty = tm_full + 16;
-  volatile int* dead = (volatile int*)(smem_raw + (tm_empty + 16 - smem_addr(smem_raw)));
-  uint32_t* tmem_slot = (uint32_t*)(smem_raw + (tm_empty + 24 - smem_addr(smem_raw)));
+  const uint32_t cells = base + STAGES * Shape::kStageBytes;
+  const uint32_t full = cells + Shape::kEpiWarps * kCellBytes, empty = full + 8 * STAGES;
+  const uint32_t tm_full = empty + 8 * STAGES, tm_empty = tm_full + 8 * BUFS, tail = tm_empty + 8 * BUFS;
+  volatile int* dead = (volatile int*)(smem_raw + (tail - smem_addr(smem_raw)));
+  uint32_t* tmem_slot = (uint32_t*)(smem_raw + (tail + 8 - smem_addr(smem_raw)));
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = CG == 1 ? 0u : cluster_rank();
-  constexpr int kEpiWarps = Shape::kThreads / 32 - 4;
 
   if (threadIdx.x == 0) {
     *dead = 0;
@@ -305,15 +386,17 @@ __global__ void __launch_bounds__(GemmShape<CG, NP>::kThreads, 1)
       mbar_init(full + 8 * s, 1);
       mbar_init(empty + 8 * s, 1);
     }
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < BUFS; ++i) {
       mbar_init(tm_full + 8 * i, 1);
-      mbar_init(tm_empty + 8 * i, CG * kEpiWarps);
+      mbar_init(tm_empty + 8 * i, CG * Shape::kEpiWarps);
     }
     mbar_init_visible();
-    tma_prefetch(&map_a);
-    tma_prefetch(&map_b);
+    tma_prefetch(&maps.a[0]);
+    tma_prefetch(&maps.b[0]);
+    if (OP_A == kSymmetric) tma_prefetch(&maps.a[1]);
+    if (OP_B == kSymmetric) tma_prefetch(&maps.b[1]);
   }
-  if (warp == 2) tmem_alloc<CG>(smem_addr(tmem_slot), Shape::kTmemCols);
+  if (warp == 2) tmem_alloc<CG>(smem_addr(tmem_slot), 512);
   tc_fence_before();
   __syncthreads();
   if (CG == 2) cluster_sync();
@@ -325,6 +408,7 @@ __global__ void __launch_bounds__(GemmShape<CG, NP>::kThreads, 1)
 
   const int cluster = blockIdx.x / CG, clusters = gridDim.x / CG;
   const int kblocks = (p.K + kTileK - 1) / kTileK;
+  constexpr int kPerChunk = NP == 1 ? (1 << 30) : kChunk;   // stages per accumulator
   auto place = [&](int tile, int& b, int& ti, int& tj) {
     b = tile / p.tiles;
     const int t = tile - b * p.tiles;
@@ -335,176 +419,129 @@ __global__ void __launch_bounds__(GemmShape<CG, NP>::kThreads, 1)
       tj = t - ti * p.tiles_n;
     }
   };
+  // whether the operand of tile row `t` lies across the contraction in stage kb
+  auto across = [](int op, int t, int kb) { return op == kAcross || (op == kSymmetric && t < kb * kTileK / T); };
 
+  // the launch's registers (640 threads x 96) go to the warps that hold accumulators: 4 x 32 x 32 + 16 x 32 x 112
+  if (CG == 2 && warp < 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 32;");
   if (warp == 0) {
-    if (lane == 0) {
-      const uint32_t full0 = CG == 1 ? full : map_to_rank(full, 0);
-      int s = 0;
-      uint32_t ph = 0, issued = 0;
-      bool ok = true;
-      for (int tile = cluster; ok && tile < p.total; tile += clusters) {
-        int b, ti, tj;
-        place(tile, b, ti, tj);
-        const int ra = ti * T + (int)rank * 128, rb = tj * T + (int)rank * 128;
-        for (int kb = 0; kb < kblocks; ++kb) {
-          if (!mbar_wait(empty + 8 * s, ph ^ 1u, dead)) {
-            ok = false;
-            break;
-          }
+    const bool lead = elect_one();
+    const uint32_t full0 = CG == 1 ? full : map_to_rank(full, 0);
+    int s = 0;
+    uint32_t ph = 0, issued = 0;
+    bool ok = true;
+    for (int tile = cluster; ok && tile < p.total; tile += clusters) {
+      int b, ti, tj;
+      place(tile, b, ti, tj);
+      const int ra = ti * T + (int)rank * 128, rb = tj * T + (int)rank * 128;
+      for (int kb = 0; kb < kblocks; ++kb) {
+        if (!mbar_wait(empty + 8 * s, ph ^ 1u, dead)) {
+          ok = false;
+          break;
+        }
+        const uint32_t st = base + s * Shape::kStageBytes, bar = full0 + 8 * s;
+        const bool a_across = across(OP_A, ti, kb), b_across = across(OP_B, tj, kb);
+        // the tensors as blocks of 64 columns: (column in the block, row, block, plane)
+        const CUtensorMap* ma = &maps.a[OP_A == kSymmetric && a_across ? 1 : 0];
+        const CUtensorMap* mb = &maps.b[OP_B == kSymmetric && b_across ? 1 : 0];
+        if (lead) {
           if (rank == 0) mbar_expect_tx(full + 8 * s, CG * Shape::kStageBytes);
-          const uint32_t st = base + s * Shape::kStageBytes;
-#pragma unroll
-          for (int pl = 0; pl < NP; ++pl) {
-            const int z = b * NP + pl;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {   // boxes of 64 x 64: two make an operand, whichever way it lies
-              const uint32_t da = st + pl * kOperandBytes + h * (kOperandBytes / 2), db = da + NP * kOperandBytes;
-              if (A_MN)
-                tma_load<CG>(da, &map_a, ra + 64 * h, kb * kTileK, z, full0 + 8 * s);
-              else
-                tma_load<CG>(da, &map_a, kb * kTileK, ra + 64 * h, z, full0 + 8 * s);
-              if (B_MN)
-                tma_load<CG>(db, &map_b, rb + 64 * h, kb * kTileK, z, full0 + 8 * s);
-              else
-                tma_load<CG>(db, &map_b, kb * kTileK, rb + 64 * h, z, full0 + 8 * s);
-            }
-          }
-          ++issued;
-          if (++s == STAGES) {
-            s = 0;
-            ph ^= 1u;
-          }
+          tma_load<CG>(st, ma, 0, a_across ? kb * kTileK : ra, a_across ? ra / 64 : kb, b * NP, bar);
+          tma_load<CG>(st + NP * kOperandBytes, mb, 0, b_across ? kb * kTileK : rb, b_across ? rb / 64 : kb, b * NP, bar);
+        }
+        __syncwarp();
+        ++issued;
+        if (++s == STAGES) {
+          s = 0;
+          ph ^= 1u;
         }
       }
-      if (!ok && rank == 0) {   // gave up: let the copies in flight land before the memory goes
-        for (uint32_t i = issued > (uint32_t)STAGES ? issued - STAGES : 0; i < issued; ++i)
-          mbar_wait(full + 8 * (i % STAGES), (i / STAGES) & 1u, dead);
-      }
+    }
+    if (!ok && rank == 0) {   // gave up: let the copies in flight land before the memory goes
+      for (uint32_t i = issued > (uint32_t)STAGES ? issued - STAGES : 0; i < issued; ++i)
+        mbar_wait(full + 8 * (i % STAGES), (i / STAGES) & 1u, dead);
     }
   } else if (warp == 1) {
-    if (lane == 0 && rank == 0) {
-      constexpr uint32_t idesc = f16_idesc(128 * CG, 128 * CG, A_MN, B_MN);
-      // per 16 of the contraction: 32 bytes along a swizzled row, or 16 rows of 128 bytes
-      constexpr uint64_t step_a = (A_MN ? 2048 : 32) >> 4, step_b = (B_MN ? 2048 : 32) >> 4;
+    if (rank == 0) {
+      const bool lead = elect_one();
+      const uint64_t desc0 = operand_desc(base, kOperandBytes / 2);
       int s = 0, buf = 0;
       uint32_t ph = 0, tph = 0;
       bool ok = true;
       for (int tile = cluster; ok && tile < p.total; tile += clusters) {
-        if (!mbar_wait(tm_empty + 8 * buf, tph ^ 1u, dead)) break;
-        tc_fence_after();
-        const uint32_t d = tmem + buf * T;
-        for (int kb = 0; kb < kblocks; ++kb) {
-          if (!mbar_wait(full + 8 * s, ph, dead)) {
+        int b, ti, tj;
+        place(tile, b, ti, tj);
+        for (int kb = 0; ok && kb < kblocks;) {
+          if (!mbar_wait(tm_empty + 8 * buf, tph ^ 1u, dead)) {
             ok = false;
             break;
           }
           tc_fence_after();
-          const uint32_t st = base + s * Shape::kStageBytes;
-          uint64_t da[NP], db[NP];
+          const uint32_t d = tmem + buf * T;
+          const int kend = NP == 1 ? kblocks : min(kblocks, kb + kPerChunk);
+          for (uint32_t add = 0; kb < kend; ++kb) {
+            if (!mbar_wait(full + 8 * s, ph, dead)) {
+              ok = false;
+              break;
+            }
+            tc_fence_after();
+            const bool a_across = across(OP_A, ti, kb), b_across = across(OP_B, tj, kb);
+            const uint32_t idesc = f16_idesc(128 * CG, 128 * CG, a_across, b_across);
+            // per 16 of the contraction: 32 bytes along a swizzled row, or 16 rows of 128 bytes
+            const uint64_t step_a = (a_across ? 2048 : 32) >> 4, step_b = (b_across ? 2048 : 32) >> 4;
+            const uint64_t da = desc0 + (uint64_t)(s * Shape::kStageBytes >> 4), db = da + (NP * kOperandBytes >> 4);
+            constexpr uint64_t lo = kOperandBytes >> 4;   // the second plane
+            if (lead) {
+              if (kb + 1 < kblocks) {
 #pragma unroll
-          for (int pl = 0; pl < NP; ++pl) {
-            da[pl] = operand_desc(st + pl * kOperandBytes, kOperandBytes / 2);
-            db[pl] = operand_desc(st + (NP + pl) * kOperandBytes, kOperandBytes / 2);
-          }
-#pragma unroll
-          for (int k = 0; k < kTileK / 16; ++k) {
-            if (NP == 2) {   // the small terms first
-              mma_f16<CG>(d, da[NP - 1] + k * step_a, db[0] + k * step_b, idesc, kb | k);
-              mma_f16<CG>(d, da[0] + k * step_a, db[NP - 1] + k * step_b, idesc, 1);
-              mma_f16<CG>(d, da[0] + k * step_a, db[0] + k * step_b, idesc, 1);
-            } else {
-              mma_f16<CG>(d, da[0] + k * step_a, db[0] + k * step_b, idesc, kb | k);
+                for (int k = 0; k < kTileK / 16; ++k) {
+                  if (NP == 2) {   // the small terms first
+                    mma_f16<CG>(d, da + lo + k * step_a, db + k * step_b, idesc, k ? 1 : add);
+                    mma_f16<CG>(d, da + k * step_a, db + lo + k * step_b, idesc, 1);
+                  }
+                  mma_f16<CG>(d, da + k * step_a, db + k * step_b, idesc, NP == 2 || k ? 1 : add);
+                }
+              } else {             // past K the stage holds zeros: only as many as are needed
+                const int steps = (p.K - kb * kTileK + 15) / 16;
+#pragma unroll 1
+                for (int k = 0; k < steps; ++k) {
+                  if (NP == 2) {
+                    mma_f16<CG>(d, da + lo + k * step_a, db + k * step_b, idesc, k ? 1 : add);
+                    mma_f16<CG>(d, da + k * step_a, db + lo + k * step_b, idesc, 1);
+                  }
+                  mma_f16<CG>(d, da + k * step_a, db + k * step_b, idesc, NP == 2 || k ? 1 : add);
+                }
+              }
+              mma_commit<CG>(empty + 8 * s);
+            }
+            __syncwarp();
+            add = 1;
+            if (++s == STAGES) {
+              s = 0;
+              ph ^= 1u;
             }
           }
-          mma_commit<CG>(empty + 8 * s);
-          if (++s == STAGES) {
-            s = 0;
-            ph ^= 1u;
+          if (!ok) break;
+          if (lead) mma_commit<CG>(tm_full + 8 * buf);
+          __syncwarp();
+          if (++buf == BUFS) {
+            buf = 0;
+            tph ^= 1u;
           }
-        }
-        if (!ok) break;
-        mma_commit<CG>(tm_full + 8 * buf);
-        if (++buf == 2) {
-          buf = 0;
-          tph ^= 1u;
         }
       }
     }
   } else if (warp >= 4) {
+    if (CG == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 112;");
     const uint32_t tm_empty0 = CG == 1 ? tm_empty : map_to_rank(tm_empty, 0);
     const int quarter = warp & 3;                          // the 32 lanes of tensor memory this warp can read
-    const int col0 = CG == 1 ? 0 : ((warp - 4) >> 2) * 128;
+    const int cols0 = ((warp - 4) >> 2) * 64;
+    const uint32_t cell = cells + (warp - 4) * kCellBytes;
+    const uint32_t tm_mine = tmem + ((uint32_t)(quarter * 32) << 16) + cols0;
     int buf = 0;
     uint32_t tph = 0;
-    for (int tile = cluster; tile < p.total; tile += clusters) {
-      int b, ti, tj;
-      place(tile, b, ti, tj);
-      if (!mbar_wait(tm_full + 8 * buf, tph, dead)) break;
-      tc_fence_after();
-      const int row = ti * T + (int)rank * 128 + quarter * 32 + lane;
-      const bool mirror = (MODE == kModeGram || MODE == kModePoly) && ti != tj;
-      const int64_t plane_s = (int64_t)p.M * p.ld_src, plane_d = (int64_t)p.M * p.ld_dst;
-      const __half* src = p.src + b * NP * plane_s + (int64_t)row * p.ld_src;
-      __half* dst = p.dst + b * NP * plane_d;
-#pragma unroll 1
-      for (int c = 0; c < 4; ++c) {
-        const int col = tj * T + col0 + 32 * c;
-        float v[32];
-        tmem_load32(tmem + ((uint32_t)(quarter * 32) << 16) + buf * T + col0 + 32 * c, v);
-        if (row < p.M && col < p.N) {
-          if (MODE == kModeGram) {
-  #pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] *= p.beta;
-          } else {
-  #pragma unroll
-            for (int q = 0; q < 4; ++q) {   // rows are padded to 64, so a chunk of 32 columns never leaves its row
-              alignas(16) __half h[8], l[8];
-              *reinterpret_cast<uint4*>(h) = *reinterpret_cast<const uint4*>(src + col + 8 * q);
-              if (NP == 2) *reinterpret_cast<uint4*>(l) = *reinterpret_cast<const uint4*>(src + plane_s + col + 8 * q);
-  #pragma unroll
-              for (int i = 0; i < 8; ++i) {
-                float x = __half2float(h[i]);
-                if (NP == 2) x += __half2float(l[i]);
-                v[8 * q + i] = fmaf(p.alpha, x, p.beta * v[8 * q + i]);
-              }
-            }
-          }
-          if (MODE == kModeLast) {
-  #pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] *= 1.f / kScaleX;
-            const int n = min(32, p.N - col);
-            if (p.out_type == kTypeF32)
-              last_chunk<float>(p, b, row, col, n, v);
-            else if (p.out_type == kTypeBF16)
-              last_chunk<__nv_bfloat16>(p, b, row, col, n, v);
-            else
-              last_chunk<__half>(p, b, row, col, n, v);
-          } else {
-            alignas(16) __half h[32], l[32];
-  #pragma unroll
-            for (int i = 0; i < 32; ++i) {
-              h[i] = __float2half_rn(v[i]);
-              if (NP == 2) l[i] = __float2half_rn(v[i] - __half2float(h[i]));
-            }
-            __half* to = dst + (int64_t)row * p.ld_dst + col;
-  #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              reinterpret_cast<uint4*>(to)[q] = reinterpret_cast<uint4*>(h)[q];
-              if (NP == 2) reinterpret_cast<uint4*>(to + plane_d)[q] = reinterpret_cast<uint4*>(l)[q];
-            }
-            if (mirror) {   // 32 lanes write 32 neighbours of a row
-  #pragma unroll
-              for (int i = 0; i < 32; ++i) {
-                if (col + i < p.N) {
-                  dst[(int64_t)(col + i) * p.ld_dst + row] = h[i];
-                  if (NP == 2) dst[plane_d + (int64_t)(col + i) * p.ld_dst + row] = l[i];
-                }
-              }
-            }
-          }
-        }
-        __syncwarp();
-      }
+    bool ok = true;
+    auto release = [&] {
       tc_fence_before();
       __syncwarp();
       if (lane == 0) {
@@ -513,9 +550,90 @@ __global__ void __launch_bounds__(GemmShape<CG, NP>::kThreads, 1)
         else
           mbar_arrive_cluster(tm_empty0 + 8 * buf);
       }
-      if (++buf == 2) {
+      if (++buf == BUFS) {
         buf = 0;
         tph ^= 1u;
+      }
+    };
+    for (int tile = cluster; ok && tile < p.total; tile += clusters) {
+      int b, ti, tj;
+      place(tile, b, ti, tj);
+      const int row0 = ti * T + (int)rank * 128 + quarter * 32, col0 = tj * T + cols0;
+      const int rows = min(32, p.M - row0);   // may be none: the accumulators are then read for nothing
+      const int64_t plane_s = (int64_t)p.M * p.ld_src, plane_d = (int64_t)p.M * p.ld_dst;
+      const __half* src = p.src + b * NP * plane_s + (int64_t)row0 * p.ld_src + col0;
+      // rows are padded to 64 columns; the pad is written too (the operands' pads are zeros, so it stays zero)
+      const bool live0 = rows > 0 && col0 < p.N, live1 = live0;
+      uint4 x0[4] = {}, x1[4] = {};
+      if (MODE != kModeGram && NP == 1) {     // the source is on its way before the accumulators are complete
+        if (live0) block_load(src, p.ld_src, rows, x0);
+        if (live1) block_load(src + 32, p.ld_src, rows, x1);
+      }
+      float acc[NP == 1 ? 32 : 64];
+      if (NP == 2) {
+        for (int kb = 0; kb < kblocks; kb += kPerChunk) {
+          if (!mbar_wait(tm_full + 8 * buf, tph, dead)) {
+            ok = false;
+            break;
+          }
+          tc_fence_after();
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            float v[16];
+            tmem_load16(tm_mine + buf * T + 16 * q, v);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[(16 * q + i) & (NP * 32 - 1)] = (kb ? acc[(16 * q + i) & (NP * 32 - 1)] : 0.f) + v[i];
+          }
+          release();
+        }
+      } else if (!mbar_wait(tm_full + 8 * buf, tph, dead)) {
+        ok = false;
+      } else {
+        tc_fence_after();
+      }
+      if (!ok) break;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        float* v = acc + (NP == 1 ? 0 : 32 * h);
+        if (NP == 1) {
+          tmem_load32(tm_mine + buf * T + 32 * h, *reinterpret_cast<float(*)[32]>(v));
+          if (h == 1) release();
+        }
+        if (h == 0 ? live0 : live1) {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) v[i] *= p.beta;
+          if (MODE != kModeGram) {
+            if (NP == 2) {
+              block_load(src + plane_s + 32 * h, p.ld_src, rows, x0);
+              block_add(cell, x0, p.alpha, v);
+              block_load(src + 32 * h, p.ld_src, rows, x0);
+              block_add(cell, x0, p.alpha, v);
+            } else {
+              block_add(cell, h == 0 ? x0 : x1, p.alpha, v);
+            }
+          }
+          if (MODE == kModeLast) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] *= 1.f / kScaleX;
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+              const int col = col0 + 32 * h + 16 * q;
+              last_cell<TOUT>(p, cell, b, row0, col, v + 16 * q);
+            }
+          } else {
+            __half* dst = p.dst + b * NP * plane_d + (int64_t)row0 * p.ld_dst + col0 + 32 * h;
+            uint4 o[4];
+            __half* oh = reinterpret_cast<__half*>(o);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) oh[i] = __float2half_rn(v[i]);
+            block_store(cell, o, dst, p.ld_dst, rows);
+            if (NP == 2) {
+#pragma unroll
+              for (int i = 0; i < 32; ++i) oh[i] = __float2half_rn(v[i] - __half2float(oh[i]));
+              block_store(cell, o, dst + plane_d, p.ld_dst, rows);
+            }
+          }
+        }
       }
     }
     fence_async_global();
@@ -530,7 +648,7 @@ __global__ void __launch_bounds__(GemmShape<CG, NP>::kThreads, 1)
   if (CG == 2) cluster_sync();
   if (warp == 2) {
     tc_fence_after();
-    tmem_free<CG>(tmem, Shape::kTmemCols);
+    tmem_free<CG>(tmem, 512);
   }
 }
 
