@@ -421,7 +421,7 @@ enum {
 typedef struct brace_ortho_params {
   int32_t steps;     /* >= 1                                                                      */
   float a, b, c;     /* coefficients; singular values in [0, 1] must stay below 1.9 through all
-                        steps, and |b s^2 + c s^4| below 7.5 (else BRACE_ERR_INVALID_ARG)         */
+                        steps, |a + b s^2 + c s^4| and |b + c s^2| below 7.5 (else INVALID_ARG)   */
   float eps;         /* added to the Frobenius norm; finite, >= 1e-30                             */
   int32_t precision; /* BRACE_ORTHO_*                                                             */
 } brace_ortho_params;

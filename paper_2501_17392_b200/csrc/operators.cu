@@ -89,10 +89,13 @@ bool coefficients_ok(const brace_ortho_params* p) {
   double top = 1.0;
   for (int k = 0; k < p->steps; ++k) {
     const double t_top = top * top;
-    double q = std::fabs(b * t_top + c * t_top * t_top), next = std::fabs(top * (a + b * t_top + c * t_top * t_top));
+    // eigenvalues of T = b + c t and of P = a + b t + c t^2, t up to top^2
+    double q = std::fmax(std::fmax(std::fabs(a), std::fabs(a + b * t_top + c * t_top * t_top)),
+                         std::fmax(std::fabs(b), std::fabs(b + c * t_top)));
+    double next = std::fabs(top * (a + b * t_top + c * t_top * t_top));
     if (c != 0.0) {
-      const double tq = -b / (2 * c);   // extreme of b t + c t^2
-      if (tq > 0 && tq < t_top) q = std::fmax(q, std::fabs(b * tq + c * tq * tq));
+      const double tq = -b / (2 * c);   // extreme of P
+      if (tq > 0 && tq < t_top) q = std::fmax(q, std::fabs(a + b * tq + c * tq * tq));
       const double disc = 9 * b * b - 20 * a * c;
       if (disc >= 0)
         for (int sg = -1; sg <= 1; sg += 2) {
@@ -115,7 +118,7 @@ struct OrthoPlan {
   int planes;
   int64_t ld_x, ld_s;
   int norm_blocks;
-  size_t off_partial, off_x[2], off_s, off_p, bytes;
+  size_t off_partial, off_x[2], off_s, off_t, off_p, bytes;
 };
 
 bool make_plan(OrthoPlan& q, int32_t batch, int32_t rows, int32_t cols, const brace_ortho_params* p, int out_type) {
@@ -144,6 +147,7 @@ bool make_plan(OrthoPlan& q, int32_t batch, int32_t rows, int32_t cols, const br
   q.off_x[0] = take(xb);
   q.off_x[1] = take(xb);
   q.off_s = take(sb);
+  q.off_t = take(single ? sb : 0);
   q.off_p = take(sb);
   q.bytes = at;
   return true;
@@ -182,9 +186,9 @@ int make_map(CUtensorMap* map, void* base, int64_t rows, int64_t ld, int64_t pla
   return r == CUDA_SUCCESS ? BRACE_OK : cuda_fail_no_ctx(cudaErrorInvalidValue);
 }
 
-// The maps of a call: X's two buffers, S and P, along [0] and across [1].
+// The maps of a call: X's two buffers, S, T and P, along [0] and across [1].
 struct OrthoMaps {
-  CUtensorMap x[2][2], s[2], p[2];
+  CUtensorMap x[2][2], s[2], t[2], p[2];
 };
 
 template <int CG, int NP, int OP_A, int OP_B, int MODE, typename TOUT = __half>
@@ -222,7 +226,7 @@ cudaError_t launch_products(const OrthoPlan& q, const brace_ortho_params* p, cha
   sym.tiles_n = tm;
   sym.tiles = tm * (tm + 1) / 2;
   sym.total = sym.tiles * q.batch;
-  sym.ld_dst = sym.ld_src = q.ld_s;
+  sym.ld_dst = q.ld_s;
   sym.status = (int*)ws;
   GemmArgs step = last;
   step.M = q.rows;
@@ -231,31 +235,35 @@ cudaError_t launch_products(const OrthoPlan& q, const brace_ortho_params* p, cha
   step.tiles_n = (q.cols + T - 1) / T;
   step.tiles = step.tiles_n * ((q.rows + T - 1) / T);
   step.total = step.tiles * q.batch;
-  step.ld_src = step.ld_dst = q.ld_x;
-  step.alpha = p->a;
-  step.beta = kStepAcc;
+  step.ld_dst = q.ld_x;
+  step.scale = kStepScale;
   step.status = (int*)ws;
-  __half* s = (__half*)(ws + q.off_s);
-  __half* poly = (__half*)(ws + q.off_p);
   for (int k = 0; k < p->steps; ++k) {
     const int cur = k & 1;
     const CUtensorMap(&x)[2] = maps.x[cur];
     GemmArgs g = sym;
     g.K = tall ? q.rows : q.cols;
-    g.beta = kScaleSInv;
-    g.dst = s;
+    g.scale = kGramScale;
+    g.dst = (__half*)(ws + q.off_s);
+    g.dst2 = (__half*)(ws + q.off_t);
+    g.scale2 = p->c * kFromGram;
+    g.diagonal2 = p->b * kSquareScale;
     cudaError_t err = tall ? launch_gemm<CG, NP, kAcross, kAcross, kModeGram>(x, x, g, st)
                            : launch_gemm<CG, NP, kAlong, kAlong, kModeGram>(x, x, g, st);
     if (err != cudaSuccess) return err;
     g = sym;
     g.K = q.m;
-    g.alpha = p->b * kPolyB;
-    g.beta = p->c * kPolyC;
-    g.src = s;
-    g.dst = poly;
-    err = launch_gemm<CG, NP, kSymmetric, kSymmetric, kModePoly>(maps.s, maps.s, g, st);
+    if (NP == 2) {
+      g.scale = kPolyScale;
+    } else {
+      g.scale = p->c * kFromGram * kGramScale;   // S S * 2^28
+      g.scale2 = p->b * kFromGram;
+      g.src = (const __half*)(ws + q.off_s);
+    }
+    g.diagonal = p->a * kSquareScale;
+    g.dst = (__half*)(ws + q.off_p);
+    err = launch_gemm<CG, NP, kSymmetric, kSymmetric, kModePoly>(maps.s, NP == 2 ? maps.t : maps.s, g, st);
     if (err != cudaSuccess) return err;
-    step.src = (const __half*)(ws + q.off_x[cur]);
     step.dst = (__half*)(ws + q.off_x[cur ^ 1]);
     if (k + 1 < p->steps)
       err = tall ? launch_gemm<CG, NP, kAlong, kSymmetric, kModeStep>(x, maps.p, step, st)
@@ -269,6 +277,21 @@ cudaError_t launch_products(const OrthoPlan& q, const brace_ortho_params* p, cha
     if (err != cudaSuccess) return err;
   }
   return cudaSuccess;
+}
+
+// Time of a step's three products in microseconds, tiles of 128 (cg = 1) or of 256 by pairs of CTAs (cg = 2): waves of
+// tiles times the stages of one, and what a launch takes beside them.  A pair does four times the work of a single CTA
+// in 1.5 times the time (0.40 against 0.27 us a stage; with two planes 1.27 against 0.82), but has to find that many
+// tiles: at 4096 x 4096 it takes 1.04 ms against 1.32, at 2048 x 2048 0.28 against 0.24.
+double tiled_cost(const OrthoPlan& q, int cg) {
+  const int tile = 128 * cg, slots = sm_count() / cg;
+  const int64_t tm = (q.m + tile - 1) / tile, tr = (q.rows + tile - 1) / tile, tc = (q.cols + tile - 1) / tile;
+  const int n = q.rows < q.cols ? q.cols : q.rows;
+  auto waves = [&](int64_t tiles) { return (double)((tiles * q.batch + slots - 1) / slots); };
+  const double stages = waves(tm * (tm + 1) / 2) * ((n + 63) / 64 + (q.m + 63) / 64) + waves(tr * tc) * ((q.m + 63) / 64);
+  const double stage = cg == 1 ? (q.planes == 1 ? 0.27 : 0.82) : (q.planes == 1 ? 0.40 : 1.27);
+  const double fixed = cg == 1 ? (q.planes == 1 ? 4.0 : 6.0) : (q.planes == 1 ? 6.5 : 10.0);
+  return stages * stage + 3 * fixed;
 }
 
 cudaError_t launch_prep(const OrthoPlan& q, const PrepArgs& a, cudaStream_t st) {
@@ -294,19 +317,55 @@ cudaError_t launch_prep(const OrthoPlan& q, const PrepArgs& a, cudaStream_t st) 
   }
 }
 
+// One launch for matrices that a cluster of CTAs can hold; false: this one has to go through the tiled products.
+template <int NP, int TYPE>
+cudaError_t launch_resident_as(const ResidentArgs& r, int ctas, cudaStream_t st) {
+  auto* kernel = ortho_resident_kernel<NP, TYPE>;
+  static std::atomic<uint64_t> granted{0};
+  int dev = 0;
+  cudaError_t err = cudaGetDevice(&dev);
+  if (err != cudaSuccess) return err;
+  const uint64_t bit = 1ull << (dev & 63);
+  if (!(granted.load(std::memory_order_relaxed) & bit)) {
+    err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kResidentSmem);
+    if (err == cudaSuccess) err = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (err != cudaSuccess) return err;
+    granted.fetch_or(bit, std::memory_order_relaxed);
+  }
+  int64_t smem = resident_smem(NP, r.slice, ctas);
+  // CTAs of two clusters must not share an SM: each would hold tensor memory that the other's cluster waits for
+  if (ctas > 1 && smem < 118 * 1024) smem = 118 * 1024;
+  return launch(kernel, dim3((unsigned)(r.last.total * ctas)), kResidentThreads, (size_t)smem, ctas, st, r);
+}
+
+template <int NP>
+cudaError_t launch_resident(const ResidentArgs& r, int ctas, cudaStream_t st) {
+  switch (r.prep.g.type) {
+    case kTypeF32: return launch_resident_as<NP, kTypeF32>(r, ctas, st);
+    case kTypeBF16: return launch_resident_as<NP, kTypeBF16>(r, ctas, st);
+    case kTypeF16: return launch_resident_as<NP, kTypeF16>(r, ctas, st);
+    default: return launch_resident_as<NP, kTypeBits>(r, ctas, st);
+  }
+}
+
+// Long side per CTA and CTAs per matrix of the one-launch kernel; 0 CTAs where the matrix does not fit.
+int resident_ctas(const OrthoPlan& q, int* slice) {
+  const int n = q.rows < q.cols ? q.cols : q.rows;
+  if (q.m > 128) return 0;
+  const int widest = q.planes == 1 ? 256 : 128;   // what fits in shared memory
+  if (n <= 256) {   // one CTA: nothing to exchange
+    *slice = (int)round_up(n, 64);
+    return 1;
+  }
+  const int ctas = (n + widest - 1) / widest;
+  if (ctas > 16) return 0;
+  *slice = (int)round_up((n + ctas - 1) / ctas, 64);
+  return (n + *slice - 1) / *slice;
+}
+
 // Everything after the argument checks.
 int run_ortho(const OrthoPlan& q, const brace_ortho_params* p, PrepArgs prep, const GemmArgs& last, int out_type, char* ws,
               cudaStream_t st) {
-  OrthoMaps maps;
-  const int64_t z = (int64_t)q.batch * q.planes;
-  for (int across = 0; across < 2; ++across) {
-    int rc = BRACE_OK;
-    for (int i = 0; i < 2 && rc == BRACE_OK; ++i)
-      rc = make_map(&maps.x[i][across], ws + q.off_x[i], q.rows, q.ld_x, z, q.planes, across);
-    if (rc == BRACE_OK) rc = make_map(&maps.s[across], ws + q.off_s, q.m, q.ld_s, z, q.planes, across);
-    if (rc == BRACE_OK) rc = make_map(&maps.p[across], ws + q.off_p, q.m, q.ld_s, z, q.planes, across);
-    if (rc != BRACE_OK) return rc;
-  }
   prep.rows = q.rows;
   prep.cols = q.cols;
   prep.units_row = (q.cols + 7) / 8;
@@ -318,9 +377,40 @@ int run_ortho(const OrthoPlan& q, const brace_ortho_params* p, PrepArgs prep, co
   prep.planes = q.planes;
   prep.status = (int*)ws;
   cudaGetLastError();
+  int slice = 0;
+  const int ctas = resident_ctas(q, &slice);
+  if (ctas > 0) {
+    ResidentArgs r = {};
+    r.prep = prep;
+    r.last = last;
+    r.last.M = q.rows;
+    r.last.N = q.cols;
+    r.last.total = q.batch;
+    r.m = q.m;
+    r.slice = slice;
+    r.tall = q.rows > q.cols;
+    r.steps = p->steps;
+    r.out_type = out_type;
+    r.a = p->a;
+    r.b = p->b;
+    r.c = p->c;
+    const cudaError_t e = q.planes == 1 ? launch_resident<1>(r, ctas, st) : launch_resident<2>(r, ctas, st);
+    return e == cudaSuccess ? BRACE_OK : cuda_fail_no_ctx(e);
+  }
+  OrthoMaps maps;
+  const int64_t z = (int64_t)q.batch * q.planes;
+  for (int across = 0; across < 2; ++across) {
+    int rc = BRACE_OK;
+    for (int i = 0; i < 2 && rc == BRACE_OK; ++i)
+      rc = make_map(&maps.x[i][across], ws + q.off_x[i], q.rows, q.ld_x, z, q.planes, across);
+    if (rc == BRACE_OK) rc = make_map(&maps.s[across], ws + q.off_s, q.m, q.ld_s, z, q.planes, across);
+    if (rc == BRACE_OK && q.planes == 2) rc = make_map(&maps.t[across], ws + q.off_t, q.m, q.ld_s, z, q.planes, across);
+    if (rc == BRACE_OK) rc = make_map(&maps.p[across], ws + q.off_p, q.m, q.ld_s, z, q.planes, across);
+    if (rc != BRACE_OK) return rc;
+  }
   cudaError_t err = launch_prep(q, prep, st);
   if (err == cudaSuccess) {
-    const bool pairs = getenv("BRACE_PAIRS") && atoi(getenv("BRACE_PAIRS"));
+    const bool pairs = tiled_cost(q, 2) < tiled_cost(q, 1);
     if (pairs)
       err = q.planes == 1 ? launch_products<2, 1>(q, p, ws, maps, last, out_type, st)
                           : launch_products<2, 2>(q, p, ws, maps, last, out_type, st);

@@ -2,15 +2,18 @@
 //
 // The iteration.  For a matrix G (rows x cols), X_0 = G / (||G||_F + eps) and
 //     S = X X^T  (X^T X when rows > cols: the Gram matrix of the short side, m x m)
-//     P = b S + c S^2
-//     X <- a X + P X  (a X + X P)
-// `steps` times.  All singular vectors stay, every singular value s goes to a s + b s^3 + c s^5, so the values are
+//     X <- a X + (b S + c S^2) X  (a X + X (b S + c S^2))
+// `steps` times, computed as
+//     S = X X^T;   P = a I + b S + c S S   or   T = b I + c S, P = a I + S T;   X <- P X  (X P)
+// so that a product's epilogue scales, adds a constant on the diagonal and stores.  With two planes the form with T is
+// taken: its epilogues read nothing.  With one plane T's own rounding would show (2.9e-3 against 2.2e-3 of the result
+// at 512 x 2048), and S is read while the product still runs.  All singular vectors stay, every singular value s goes to a s + b s^3 + c s^5, so the values are
 // pushed towards 1 and X towards the nearest matrix with orthonormal rows (columns).
 //
 // Number format.  The operands of all products are float16 times a power of two, with float32 accumulators.  That is
-// possible because the iteration's values are bounded (the host checks the coefficients: singular values below 2,
-// |b s^2 + c s^4| below 8), so X 2^14, S 2^14 and P 2^13 cannot overflow and entries down to 4e-9 stay normal; it
-// keeps 11 bits where bfloat16, at the same rate, keeps 8.  For a 16-bit result one float16 holds an operand.  Where
+// possible because the iteration's values are bounded (the host checks the coefficients: singular values below 1.9,
+// eigenvalues of T and P below 7.5), so X 2^14, S 2^14, T 2^13 and P 2^13 cannot overflow and entries down to 8e-9 stay
+// normal; it keeps 11 bits where bfloat16, at the same rate, keeps 8.  For a 16-bit result one float16 holds an operand.  Where
 // float32 accuracy is asked for, an operand is the sum of two float16 planes (hi + lo, 22 bits) and a product is
 // hi*hi + hi*lo + lo*hi: three times the matrix instructions.
 //
@@ -26,10 +29,11 @@
 namespace brace {
 
 constexpr float kScaleX = 16384.f;                  // stored X = X * 2^14
-constexpr float kScaleSInv = 1.f / 16384.f;         // X X^T * 2^28 -> S * 2^14
-constexpr float kPolyB = 0.5f;                      // S * 2^14 -> P * 2^13
-constexpr float kPolyC = 1.f / 32768.f;             // S S * 2^28 -> P * 2^13
-constexpr float kStepAcc = 1.f / 8192.f;            // P X * 2^27 -> X * 2^14
+constexpr float kGramScale = 1.f / 16384.f;         // X X^T * 2^28 -> S * 2^14
+constexpr float kSquareScale = 8192.f;              // T, P -> T * 2^13, P * 2^13
+constexpr float kFromGram = 0.5f;                   // S * 2^14 -> S * 2^13
+constexpr float kPolyScale = 1.f / 16384.f;         // S T * 2^27 -> P * 2^13
+constexpr float kStepScale = 1.f / 8192.f;          // P X * 2^27 -> X * 2^14
 
 // A matrix of a user's: `type`, rows `ld` elements apart, matrices of a batch `batch` elements apart.
 struct MatRef {
@@ -213,12 +217,12 @@ struct GemmArgs {
   int M, N, K;                  // result M x N, contraction K
   int tiles_n, tiles;           // tile columns, tiles per matrix
   int total;                    // tiles of all matrices
-  float alpha;                  // times the source (S or X)
-  float beta;                   // times the product
-  const __half* src;            // [batch][planes][M][ld_src]
-  int64_t ld_src;
+  float scale, diagonal;        // of the product, and added on its diagonal
   __half* dst;                  // [batch][planes][M][ld_dst]
   int64_t ld_dst;
+  __half* dst2;                 // two planes, kModeGram: T beside S, scale2 * S + diagonal2 on the diagonal
+  float scale2, diagonal2;      // one plane, kModePoly: scale2 * src is added
+  const __half* src;            // S, laid out as dst
   // kModeLast: the result O, or the weights W_out = keep * W_in - rate * O for `replicas` copies
   void* out;
   const void* w_in;
@@ -277,30 +281,7 @@ __device__ __forceinline__ uint4 lds16(uint32_t a) {
   return v;
 }
 
-// A 32 x 32 block of a padded float16 matrix, 16 bytes a lane at a time: 8 rows per access.
-__device__ __forceinline__ void block_load(const __half* p, int64_t ld, int rows, uint4 (&x)[4]) {
-  const int lane = threadIdx.x & 31;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int r = i * 8 + (lane >> 2);
-    x[i] = r < rows ? *reinterpret_cast<const uint4*>(p + r * ld + (lane & 3) * 8) : make_uint4(0, 0, 0, 0);
-  }
-}
-// ... the lane's own row of it, times alpha, added to `row`
-__device__ __forceinline__ void block_add(uint32_t cell, const uint4 (&x)[4], float alpha, float* row) {
-  const int lane = threadIdx.x & 31;
-  __syncwarp();
-#pragma unroll
-  for (int i = 0; i < 4; ++i) sts16(cell_at(cell, i * 8 + (lane >> 2), lane & 3), x[i]);
-  __syncwarp();
-#pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    uint4 t = lds16(cell_at(cell, lane, w));
-    const __half* h = reinterpret_cast<const __half*>(&t);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) row[8 * w + j] = fmaf(alpha, __half2float(h[j]), row[8 * w + j]);
-  }
-}
+// A 32 x 32 block to a padded float16 matrix: the lane's own row goes through the cell, 8 rows of 64 bytes per store.
 __device__ __forceinline__ void block_store(uint32_t cell, const uint4 (&own)[4], __half* p, int64_t ld, int rows) {
   const int lane = threadIdx.x & 31;
   __syncwarp();
@@ -312,6 +293,59 @@ __device__ __forceinline__ void block_store(uint32_t cell, const uint4 (&own)[4]
     const int r = i * 8 + (lane >> 2);
     const uint4 t = lds16(cell_at(cell, r, lane & 3));
     if (r < rows) *reinterpret_cast<uint4*>(p + r * ld + (lane & 3) * 8) = t;
+  }
+}
+
+__device__ __forceinline__ uint4 pack8(const float* v) {
+  uint4 t;
+  __half2* h = reinterpret_cast<__half2*>(&t);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) h[i] = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
+  return t;
+}
+// what 8 values lose in pack8
+__device__ __forceinline__ uint4 pack8_rest(const float* v, const uint4& hi) {
+  const __half* h = reinterpret_cast<const __half*>(&hi);
+  float r[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) r[i] = v[i] - __half2float(h[i]);
+  return pack8(r);
+}
+
+// ... and back: fetched 8 rows at a time, the lane's own row times `scale` added to v.
+__device__ __forceinline__ void block_fetch(const __half* p, int64_t ld, int rows, uint4 (&x)[4]) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int r = i * 8 + (lane >> 2);
+    x[i] = r < rows ? *reinterpret_cast<const uint4*>(p + r * ld + (lane & 3) * 8) : make_uint4(0, 0, 0, 0);
+  }
+}
+__device__ __forceinline__ void block_add(uint32_t cell, const uint4 (&x)[4], float scale, float* v) {
+  const int lane = threadIdx.x & 31;
+  __syncwarp();
+#pragma unroll
+  for (int i = 0; i < 4; ++i) sts16(cell_at(cell, i * 8 + (lane >> 2), lane & 3), x[i]);
+  __syncwarp();
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const uint4 t = lds16(cell_at(cell, lane, w));
+    const __half* h = reinterpret_cast<const __half*>(&t);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[8 * w + j] = fmaf(scale, __half2float(h[j]), v[8 * w + j]);
+  }
+}
+
+template <int NP>
+__device__ __forceinline__ void store_planes(uint32_t cell, const float* v, __half* p, int64_t plane, int64_t ld, int rows) {
+  uint4 o[4];
+#pragma unroll
+  for (int w = 0; w < 4; ++w) o[w] = pack8(v + 8 * w);
+  block_store(cell, o, p, ld, rows);
+  if (NP == 2) {
+#pragma unroll
+    for (int w = 0; w < 4; ++w) o[w] = pack8_rest(v + 8 * w, o[w]);
+    block_store(cell, o, p + plane, ld, rows);
   }
 }
 
@@ -495,12 +529,14 @@ __global__ void __launch_bounds__(GemmShape<CG, NP>::kThreads, 1)
               if (kb + 1 < kblocks) {
 #pragma unroll
                 for (int k = 0; k < kTileK / 16; ++k) {
-                  if (NP == 2) {   // the small terms first
+                  if (NP == 2) {   // the small terms first: what is cut off goes by the accumulators' size
                     mma_f16<CG>(d, da + lo + k * step_a, db + k * step_b, idesc, k ? 1 : add);
                     mma_f16<CG>(d, da + k * step_a, db + lo + k * step_b, idesc, 1);
                   }
-                  mma_f16<CG>(d, da + k * step_a, db + k * step_b, idesc, NP == 2 || k ? 1 : add);
                 }
+#pragma unroll
+                for (int k = 0; k < kTileK / 16; ++k)
+                  mma_f16<CG>(d, da + k * step_a, db + k * step_b, idesc, NP == 2 || k ? 1 : add);
               } else {             // past K the stage holds zeros: only as many as are needed
                 const int steps = (p.K - kb * kTileK + 15) / 16;
 #pragma unroll 1
@@ -509,8 +545,10 @@ __global__ void __launch_bounds__(GemmShape<CG, NP>::kThreads, 1)
                     mma_f16<CG>(d, da + lo + k * step_a, db + k * step_b, idesc, k ? 1 : add);
                     mma_f16<CG>(d, da + k * step_a, db + lo + k * step_b, idesc, 1);
                   }
-                  mma_f16<CG>(d, da + k * step_a, db + k * step_b, idesc, NP == 2 || k ? 1 : add);
                 }
+#pragma unroll 1
+                for (int k = 0; k < steps; ++k)
+                  mma_f16<CG>(d, da + k * step_a, db + k * step_b, idesc, NP == 2 || k ? 1 : add);
               }
               mma_commit<CG>(empty + 8 * s);
             }
@@ -560,14 +598,14 @@ __global__ void __launch_bounds__(GemmShape<CG, NP>::kThreads, 1)
       place(tile, b, ti, tj);
       const int row0 = ti * T + (int)rank * 128 + quarter * 32, col0 = tj * T + cols0;
       const int rows = min(32, p.M - row0);   // may be none: the accumulators are then read for nothing
-      const int64_t plane_s = (int64_t)p.M * p.ld_src, plane_d = (int64_t)p.M * p.ld_dst;
-      const __half* src = p.src + b * NP * plane_s + (int64_t)row0 * p.ld_src + col0;
+      const int64_t plane = (int64_t)p.M * p.ld_dst;
       // rows are padded to 64 columns; the pad is written too (the operands' pads are zeros, so it stays zero)
-      const bool live0 = rows > 0 && col0 < p.N, live1 = live0;
-      uint4 x0[4] = {}, x1[4] = {};
-      if (MODE != kModeGram && NP == 1) {     // the source is on its way before the accumulators are complete
-        if (live0) block_load(src, p.ld_src, rows, x0);
-        if (live1) block_load(src + 32, p.ld_src, rows, x1);
+      const bool live = rows > 0 && col0 < p.N;
+      const int64_t at = b * NP * plane + (int64_t)row0 * p.ld_dst + col0;
+      uint4 x0[4], x1[4];
+      if (MODE == kModePoly && NP == 1 && live) {
+        block_fetch(p.src + at, p.ld_dst, rows, x0);
+        block_fetch(p.src + at + 32, p.ld_dst, rows, x1);
       }
       float acc[NP == 1 ? 32 : 64];
       if (NP == 2) {
@@ -599,38 +637,22 @@ __global__ void __launch_bounds__(GemmShape<CG, NP>::kThreads, 1)
           tmem_load32(tm_mine + buf * T + 32 * h, *reinterpret_cast<float(*)[32]>(v));
           if (h == 1) release();
         }
-        if (h == 0 ? live0 : live1) {
-#pragma unroll
-          for (int i = 0; i < 32; ++i) v[i] *= p.beta;
-          if (MODE != kModeGram) {
-            if (NP == 2) {
-              block_load(src + plane_s + 32 * h, p.ld_src, rows, x0);
-              block_add(cell, x0, p.alpha, v);
-              block_load(src + 32 * h, p.ld_src, rows, x0);
-              block_add(cell, x0, p.alpha, v);
-            } else {
-              block_add(cell, h == 0 ? x0 : x1, p.alpha, v);
-            }
-          }
+        if (live) {
+          const int own = row0 + lane - (col0 + 32 * h);   // the diagonal's column in this lane's row
           if (MODE == kModeLast) {
 #pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] *= 1.f / kScaleX;
+            for (int i = 0; i < 32; ++i) v[i] *= kStepScale / kScaleX;
 #pragma unroll
-            for (int q = 0; q < 2; ++q) {
-              const int col = col0 + 32 * h + 16 * q;
-              last_cell<TOUT>(p, cell, b, row0, col, v + 16 * q);
-            }
+            for (int q = 0; q < 2; ++q) last_cell<TOUT>(p, cell, b, row0, col0 + 32 * h + 16 * q, v + 16 * q);
           } else {
-            __half* dst = p.dst + b * NP * plane_d + (int64_t)row0 * p.ld_dst + col0 + 32 * h;
-            uint4 o[4];
-            __half* oh = reinterpret_cast<__half*>(o);
 #pragma unroll
-            for (int i = 0; i < 32; ++i) oh[i] = __float2half_rn(v[i]);
-            block_store(cell, o, dst, p.ld_dst, rows);
-            if (NP == 2) {
+            for (int i = 0; i < 32; ++i) v[i] = fmaf(v[i], p.scale, MODE == kModePoly && i == own ? p.diagonal : 0.f);
+            if (MODE == kModePoly && NP == 1) block_add(cell, h == 0 ? x0 : x1, p.scale2, v);
+            store_planes<NP>(cell, v, p.dst + at + 32 * h, plane, p.ld_dst, rows);
+            if (MODE == kModeGram && NP == 2) {
 #pragma unroll
-              for (int i = 0; i < 32; ++i) oh[i] = __float2half_rn(v[i] - __half2float(oh[i]));
-              block_store(cell, o, dst + plane_d, p.ld_dst, rows);
+              for (int i = 0; i < 32; ++i) v[i] = fmaf(v[i], p.scale2, i == own ? p.diagonal2 : 0.f);
+              store_planes<NP>(cell, v, p.dst2 + at + 32 * h, plane, p.ld_dst, rows);
             }
           }
         }
@@ -649,6 +671,360 @@ __global__ void __launch_bounds__(GemmShape<CG, NP>::kThreads, 1)
   if (warp == 2) {
     tc_fence_after();
     tmem_free<CG>(tmem, 512);
+  }
+}
+
+// ---------------------------------------------------------------------------------------------------------------
+// Matrices with a short side of at most 128: the whole iteration in one launch, on chip.
+//
+// A cluster of CTAs holds one matrix; each keeps a slice of the long side as float16 operand planes in shared memory
+// for all steps.  Per step a CTA forms its slice's share of S, the
+// cluster adds the shares through distributed shared memory (each CTA adds the rows that it owns and hands them to
+// all), and every CTA forms P itself and takes its slice to P X.
+// At these sizes nothing is bound by bandwidth or by the products (a 128 x 128 product is some 0.3 us); what counts is
+// the chain of dependent steps, which as separate launches costs a launch and a round trip through L2 each.
+// ---------------------------------------------------------------------------------------------------------------
+
+struct ResidentArgs {
+  PrepArgs prep;
+  GemmArgs last;
+  int m;              // short side
+  int slice;          // long side per CTA, a multiple of 64
+  int tall;           // the long side are the rows
+  int steps;
+  int out_type;
+  float a, b, c;
+};
+
+constexpr int kResidentThreads = 512;
+constexpr int kSquareBytes = 128 * 128 * 2;   // one plane of S or P
+constexpr int kResidentSmem = 226 * 1024;     // at most
+
+// The operand planes of X, of S / P, and (several CTAs) the shares of S.
+inline int64_t resident_smem(int planes, int slice, int ctas) {
+  return (int64_t)planes * (128 * slice * 2 + kSquareBytes) + (ctas > 1 ? (128 + ctas) * 512 : 0) + 1024;
+}
+
+// A 16-byte word of a swizzled operand: `word` of row `row` of a block of 64 columns.
+__device__ __forceinline__ uint32_t swizzled(uint32_t block, int row, int word) {
+  return block + (uint32_t)(row * 128 + ((word ^ (row & 7)) << 4));
+}
+
+// 32 columns of the accumulators of a tall matrix: the lanes hold neighbours of a row of the result.
+template <typename T>
+__device__ __forceinline__ void last_columns(const GemmArgs& p, int64_t b, int row0, int rows, int col, const float (&o)[32]) {
+  if (col >= p.N) return;
+  for (int k = 0; k < p.replicas; ++k) {
+    T* out = (T*)p.out + b * p.batch_out + k * p.rep_out + (int64_t)row0 * p.ld_out + col;
+    const T* in = p.w_in ? (const T*)p.w_in + b * p.batch_in + k * p.rep_in + (int64_t)row0 * p.ld_in + col : nullptr;
+    T w[32];
+    if (in) {
+#pragma unroll
+      for (int j = 0; j < 32; ++j) w[j] = j < rows ? in[j * p.ld_in] : from_f32<T>(0.f);
+    }
+#pragma unroll
+    for (int j = 0; j < 32; ++j)
+      if (j < rows) out[j * p.ld_out] = from_f32<T>(in ? p.keep * to_f32(w[j]) - p.rate * o[j] : o[j]);
+  }
+}
+
+template <int NP, int TYPE>
+__global__ void __launch_bounds__(kResidentThreads, 1) ortho_resident_kernel(const __grid_constant__ ResidentArgs p) {
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ double s_sum[16], s_part[16];
+  __shared__ alignas(8) uint64_t s_bar;
+  __shared__ uint32_t s_tmem;
+  __shared__ int s_dead;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  uint32_t ctas;
+  asm volatile("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(ctas));
+  const int rank = ctas > 1 ? (int)cluster_rank() : 0;
+  const int64_t b = blockIdx.x / ctas;
+  const uint32_t base = (smem_addr(smem_raw) + 1023u) & ~1023u;
+  const uint32_t x_plane = 128u * (uint32_t)p.slice * 2u;
+  const uint32_t sm_x = base, sm_s = sm_x + NP * x_plane, sm_share = sm_s + NP * kSquareBytes;
+  const uint32_t x_block = p.tall ? (uint32_t)p.slice * 128u : 128u * 128u;   // 64 columns of all rows
+  const uint32_t bar = smem_addr(&s_bar);
+  volatile int* dead = &s_dead;
+  const int m = p.m;
+  // this CTA's part of the matrix
+  const int long_side = p.tall ? p.prep.rows : p.prep.cols;
+  const int at = rank * p.slice, width = min(p.slice, long_side - at);   // never empty
+  const int row0 = p.tall ? at : 0, col0 = p.tall ? 0 : at;
+  const int rows = p.tall ? width : m, cols = p.tall ? m : width;
+
+  if (tid == 0) {
+    s_dead = 0;
+    mbar_init(bar, 1);
+    mbar_init_visible();
+  }
+  const uint32_t tmem_cols = p.slice <= 128 ? 256 : 512;
+  if (warp == 0) tmem_alloc<1>(smem_addr(&s_tmem), tmem_cols);
+  // pads of the operands are zeros: rows and columns past the matrix take part in the products
+  for (uint32_t i = tid * 16; i < NP * (x_plane + kSquareBytes); i += kResidentThreads * 16)
+    sts16(sm_x + i, make_uint4(0, 0, 0, 0));
+  __syncthreads();
+  grid_trigger();   // after the allocation of tensor memory: what is launched next cannot take it first
+  grid_wait();
+  if (blockIdx.x == 0 && tid == 0) *p.prep.status = 0;
+
+  // momentum and sum of squares, as in ortho_norm_kernel
+  const int units_row = (cols + 7) / 8, units = rows * units_row;
+  double sum = 0;
+  for (int u = tid; u < units; u += kResidentThreads) {
+    const int r = u / units_row, col = col0 + (u - r * units_row) * 8, row = row0 + r, n = min(8, col0 + cols - col);
+    float g[8];
+    load_g<TYPE>(p.prep, b, row, col, n, g);
+    if (p.prep.m_in) {
+      float mo[8];
+      load8(p.prep.m_in + b * p.prep.batch_m_in + (int64_t)row * p.prep.ld_m_in + col, p.prep.vec_m_in, n, mo);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) mo[i] = fmaf(p.prep.beta, mo[i], g[i]);
+      store8(p.prep.m_out + b * p.prep.batch_m_out + (int64_t)row * p.prep.ld_m_out + col, p.prep.vec_m_out, n, mo);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) g[i] = p.prep.nesterov ? fmaf(p.prep.beta, mo[i], g[i]) : mo[i];
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < n) sum = fma((double)g[i], (double)g[i], sum);
+  }
+  sum = block_sum(sum, s_sum);
+  if (ctas > 1) {
+    cluster_sync();   // every CTA runs before its memory is written
+    if (tid < (int)ctas) st_cluster_f64(map_to_rank(smem_addr(&s_part[rank]), (uint32_t)tid), sum);
+    cluster_sync();
+    sum = 0;
+    for (uint32_t i = 0; i < ctas; ++i) sum += s_part[i];
+  }
+  const float inv = (float)((double)kScaleX / (sqrt(sum) + (double)p.prep.eps));
+
+  // X_0: the operand planes
+  for (int u = tid; u < units; u += kResidentThreads) {
+    const int r = u / units_row, c8 = u - r * units_row, col = col0 + c8 * 8, row = row0 + r, n = min(8, col0 + cols - col);
+    float g[8];
+    if (!p.prep.m_in || p.prep.nesterov) {
+      load_g<TYPE>(p.prep, b, row, col, n, g);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) g[i] = 0.f;
+    }
+    if (p.prep.m_in) {   // this thread wrote the same elements above
+      float mo[8];
+      load8((const float*)p.prep.m_out + b * p.prep.batch_m_out + (int64_t)row * p.prep.ld_m_out + col, p.prep.vec_m_out, n, mo);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) g[i] = p.prep.nesterov ? fmaf(p.prep.beta, mo[i], g[i]) : mo[i];
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) g[i] *= inv;
+    const uint32_t to = swizzled(sm_x + (uint32_t)(c8 >> 3) * x_block, r, c8 & 7);
+    const uint4 hi = pack8(g);
+    sts16(to, hi);
+    if (NP == 2) sts16(to + x_plane, pack8_rest(g, hi));
+  }
+  fence_async();
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = s_tmem;
+  const int quarter = warp & 3, group = warp >> 2;   // lanes of tensor memory, and which 32 columns of every 128
+  const uint32_t tm_s = tmem + ((uint32_t)(quarter * 32) << 16), tm_x = tm_s + 128;
+  const int mrow = quarter * 32 + lane;              // this thread's row of the short side
+  const int k_long = (width + 15) / 16, k_short = (m + 15) / 16;
+  const uint32_t n_short = (uint32_t)k_short * 16, n_long = (uint32_t)k_long * 16;
+  const int x_groups = (width + 31) / 32;            // groups of 32 columns of the accumulators of X
+  uint32_t ph = 0;
+
+  // One product, issued by one lane of warp 0 and waited for by all: D = A B over `ks` steps of 16, operands at
+  // desc + k * step (within a block of 64 of the contraction: `fold` steps) + block steps.
+  auto product = [&](uint32_t d, uint32_t a, uint32_t a_lo, uint32_t a_blocks, bool a_across, uint32_t bb, uint32_t b_lo,
+                     uint32_t b_blocks, bool b_across, int ks, uint32_t n) {
+    if (warp == 0) {
+      tc_fence_after();
+      const bool lead = elect_one();
+      const uint32_t idesc = f16_idesc(128, (int)n, a_across, b_across);
+      const uint64_t da0 = operand_desc(a, a_blocks), db0 = operand_desc(bb, b_blocks);
+      for (int pass = NP == 2 ? 0 : 1; pass < 2; ++pass)
+      for (int k = 0; k < ks; ++k) {
+        const uint64_t da = da0 + (a_across ? (uint32_t)k * 128u : (uint32_t)(k >> 2) * (a_blocks >> 4) + (uint32_t)(k & 3) * 2u);
+        const uint64_t db = db0 + (b_across ? (uint32_t)k * 128u : (uint32_t)(k >> 2) * (b_blocks >> 4) + (uint32_t)(k & 3) * 2u);
+        if (lead) {
+          if (pass == 0) {   // the small terms first: what is cut off goes by the accumulators' size
+            mma_f16<1>(d, da + (a_lo >> 4), db, idesc, k);
+            mma_f16<1>(d, da, db + (b_lo >> 4), idesc, 1);
+          } else {
+            mma_f16<1>(d, da, db, idesc, NP == 2 || k);
+          }
+        }
+      }
+      if (lead) mma_commit<1>(bar);
+      __syncwarp();
+    }
+    mbar_wait(bar, ph, dead);   // where it runs out the results are not valid, but every CTA goes the same way
+    ph ^= 1u;
+    tc_fence_after();
+  };
+
+  for (int step = 0; step < p.steps; ++step) {
+    // S = X X^T over this slice
+    product(tmem, sm_x, x_plane, x_block, p.tall, sm_x, x_plane, x_block, p.tall, k_long, n_short);
+    const bool mine = 32 * group < m;   // this warp's 32 columns of S exist
+    float v[32];
+    if (mine) tmem_load32(tm_s + 32 * group, v);
+    if (ctas == 1) {
+      if (mine) {
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[8 * w + j] *= kGramScale;
+          const uint32_t to = swizzled(sm_s + (uint32_t)(group >> 1) * 16384u, mrow, (group & 1) * 4 + w);
+          const uint4 hi = pack8(v + 8 * w);
+          sts16(to, hi);
+          if (NP == 2) sts16(to + kSquareBytes, pack8_rest(v + 8 * w, hi));
+        }
+      }
+    } else {
+      // the shares to the rows' owners: [share][row of the owner][128], words swizzled by the row
+      const int own = (m + (int)ctas - 1) / (int)ctas;
+      if (mine && mrow < m) {
+        const int owner = mrow / own, r = mrow - owner * own;
+        const uint32_t to = map_to_rank(sm_share + (uint32_t)((rank * own + r) * 512 + group * 128), (uint32_t)owner);
+#pragma unroll
+        for (int w = 0; w < 8; ++w)
+          st_cluster16(to + (uint32_t)((w ^ (r & 7)) << 4),
+                       make_uint4(__float_as_uint(v[4 * w]), __float_as_uint(v[4 * w + 1]), __float_as_uint(v[4 * w + 2]),
+                                  __float_as_uint(v[4 * w + 3])));
+      }
+      cluster_sync();
+      // the owner adds its rows' shares, in the order of the CTAs, and hands 8 columns at a time to all
+      const int words = (int)n_short / 8, first = rank * own, have = max(0, min(own, m - first));
+      for (int u = tid; u < have * words; u += kResidentThreads) {
+        const int r = u / words, c8 = u - r * words;
+        float t[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) t[j] = 0.f;
+        for (int q = 0; q < (int)ctas; ++q) {
+          const uint32_t from = sm_share + (uint32_t)((q * own + r) * 512 + (c8 >> 2) * 128);
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const uint4 x = lds16(from + (uint32_t)(((((c8 & 3) * 2) + h) ^ (r & 7)) << 4));
+            t[4 * h] += __uint_as_float(x.x);
+            t[4 * h + 1] += __uint_as_float(x.y);
+            t[4 * h + 2] += __uint_as_float(x.z);
+            t[4 * h + 3] += __uint_as_float(x.w);
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) t[j] *= kGramScale;
+        const uint32_t to = swizzled(sm_s + (uint32_t)(c8 >> 3) * 16384u, first + r, c8 & 7);
+        const uint4 hi = pack8(t), lo = NP == 2 ? pack8_rest(t, hi) : hi;
+        for (uint32_t q = 0; q < ctas; ++q) {
+          st_cluster16(map_to_rank(to, q), hi);
+          if (NP == 2) st_cluster16(map_to_rank(to + kSquareBytes, q), lo);
+        }
+      }
+      fence_async();
+      cluster_sync();
+    }
+    fence_async();
+    tc_fence_before();
+    __syncthreads();
+
+    // P = a I + b S + c S^2, in place of S
+    product(tmem, sm_s, kSquareBytes, 16384u, false, sm_s, kSquareBytes, 16384u, false, k_short, n_short);
+    if (mine) {
+      tmem_load32(tm_s + 32 * group, v);
+      const int own = mrow - 32 * group;   // the diagonal's column in this lane's row
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const uint32_t at_s = swizzled(sm_s + (uint32_t)(group >> 1) * 16384u, mrow, (group & 1) * 4 + w);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          v[8 * w + j] = fmaf(v[8 * w + j], p.c * kFromGram * kGramScale, own == 8 * w + j && mrow < m ? p.a * kSquareScale : 0.f);
+#pragma unroll
+        for (int pl = NP - 1; pl >= 0; --pl) {
+          const uint4 x = lds16(at_s + pl * kSquareBytes);
+          const __half* h = reinterpret_cast<const __half*>(&x);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[8 * w + j] = fmaf(p.b * kFromGram, __half2float(h[j]), v[8 * w + j]);
+        }
+        const uint4 hi = pack8(v + 8 * w);
+        sts16(at_s, hi);
+        if (NP == 2) sts16(at_s + kSquareBytes, pack8_rest(v + 8 * w, hi));
+      }
+    }
+    fence_async();
+    tc_fence_before();
+    __syncthreads();
+
+    // X <- P X
+    product(tmem + 128, sm_s, kSquareBytes, 16384u, false, sm_x, x_plane, x_block, !p.tall, k_short, n_long);
+    if (step + 1 == p.steps) break;
+    for (int g = group; g < x_groups; g += 4) {
+      tmem_load32(tm_x + 32 * g, v);
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[8 * w + j] *= kStepScale;
+        const uint4 hi = pack8(v + 8 * w), lo = NP == 2 ? pack8_rest(v + 8 * w, hi) : hi;
+        if (p.tall) {   // neighbouring lanes are neighbours in memory: two bytes each
+#pragma unroll
+          for (int pl = 0; pl < NP; ++pl) {
+            const unsigned short* h = reinterpret_cast<const unsigned short*>(pl ? &lo : &hi);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              const uint32_t to = swizzled(sm_x + pl * x_plane + (uint32_t)(mrow >> 6) * x_block, 32 * g + 8 * w + j, (mrow & 63) >> 3);
+              asm volatile("st.shared.u16 [%0], %1;" ::"r"(to + (uint32_t)(mrow & 7) * 2u), "h"(h[j]) : "memory");
+            }
+          }
+        } else {
+          const uint32_t to = swizzled(sm_x + (uint32_t)(g >> 1) * x_block, mrow, (g & 1) * 4 + w);
+          sts16(to, hi);
+          if (NP == 2) sts16(to + x_plane, lo);
+        }
+      }
+    }
+    fence_async();
+    tc_fence_before();
+    __syncthreads();
+  }
+
+  // the result, or the weights
+  for (int g = group; g < x_groups; g += 4) {
+    float v[32];
+    tmem_load32(tm_x + 32 * g, v);
+#pragma unroll
+    for (int j = 0; j < 32; ++j) v[j] *= kStepScale / kScaleX;
+    if (p.tall) {
+      const int first = at + 32 * g, n = min(32, long_side - first);
+      if (p.out_type == kTypeF32)
+        last_columns<float>(p.last, b, first, n, mrow, v);
+      else if (p.out_type == kTypeBF16)
+        last_columns<__nv_bfloat16>(p.last, b, first, n, mrow, v);
+      else
+        last_columns<__half>(p.last, b, first, n, mrow, v);
+    } else {
+      const uint32_t cell = sm_s + (uint32_t)warp * kCellBytes;   // P is used up
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        if (p.out_type == kTypeF32)
+          last_cell<float>(p.last, cell, b, quarter * 32, at + 32 * g + 16 * q, v + 16 * q);
+        else if (p.out_type == kTypeBF16)
+          last_cell<__nv_bfloat16>(p.last, cell, b, quarter * 32, at + 32 * g + 16 * q, v + 16 * q);
+        else
+          last_cell<__half>(p.last, cell, b, quarter * 32, at + 32 * g + 16 * q, v + 16 * q);
+      }
+    }
+  }
+  __syncthreads();
+  if (*dead) {   // a wait ran out: let what may still be under way end before the memory goes
+    if (tid == 0) atomicExch(p.prep.status, 1);
+    for (int i = 0; i < 200; ++i) __nanosleep(1000);
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 0) {
+    tc_fence_after();
+    tmem_free<1>(tmem, tmem_cols);
   }
 }
 
