@@ -410,7 +410,7 @@ enum {
 
 /* accuracy of the orthogonalisation */
 enum {
-  BRACE_ORTHO_AUTO = 0,  /* SINGLE for float32 results, HALF for 16-bit ones                      */
+  BRACE_ORTHO_AUTO = 0,  /* HALF for bfloat16 results, SINGLE for float32 and float16              */
   BRACE_ORTHO_HALF = 1,  /* operands of the products rounded to 11 bits, sums in float32          */
   BRACE_ORTHO_SINGLE = 2 /* operands held to 22 bits, sums in float32: three times the products   */
 };

@@ -126,7 +126,9 @@ bool make_plan(OrthoPlan& q, int32_t batch, int32_t rows, int32_t cols, const br
   q.rows = rows;
   q.cols = cols;
   q.m = rows < cols ? rows : cols;
-  const bool single = p->precision == BRACE_ORTHO_SINGLE || (p->precision == BRACE_ORTHO_AUTO && out_type == BRACE_TYPE_F32);
+  // a float16 result keeps 11 bits, about what a rounding of each operand to 11 bits would use up: only bfloat16 is
+  // content with that
+  const bool single = p->precision == BRACE_ORTHO_SINGLE || (p->precision == BRACE_ORTHO_AUTO && out_type != BRACE_TYPE_BF16);
   q.planes = single ? 2 : 1;
   q.ld_x = round_up(cols, 64);
   q.ld_s = round_up(q.m, 64);
@@ -227,6 +229,7 @@ cudaError_t launch_products(const OrthoPlan& q, const brace_ortho_params* p, cha
   sym.tiles = tm * (tm + 1) / 2;
   sym.total = sym.tiles * q.batch;
   sym.ld_dst = q.ld_s;
+  sym.chunk = q.m >= kLongChunkFrom ? 2 : 1;
   sym.status = (int*)ws;
   GemmArgs step = last;
   step.M = q.rows;
@@ -236,6 +239,7 @@ cudaError_t launch_products(const OrthoPlan& q, const brace_ortho_params* p, cha
   step.tiles = step.tiles_n * ((q.rows + T - 1) / T);
   step.total = step.tiles * q.batch;
   step.ld_dst = q.ld_x;
+  step.chunk = sym.chunk;
   step.scale = kStepScale;
   step.status = (int*)ws;
   for (int k = 0; k < p->steps; ++k) {

@@ -217,6 +217,7 @@ struct GemmArgs {
   int M, N, K;                  // result M x N, contraction K
   int tiles_n, tiles;           // tile columns, tiles per matrix
   int total;                    // tiles of all matrices
+  int chunk;                    // stages per accumulator (two planes)
   float scale, diagonal;        // of the product, and added on its diagonal
   __half* dst;                  // [batch][planes][M][ld_dst]
   int64_t ld_dst;
@@ -234,10 +235,13 @@ struct GemmArgs {
 
 constexpr int kTileK = 64;                       // contraction per stage: one 128-byte swizzle row
 constexpr int kOperandBytes = 128 * kTileK * 2;  // an operand of a stage in one CTA: 128 rows (or columns)
-// The tensor cores' float32 accumulation cuts off what does not fit, which over a long contraction adds up to an error
-// that no sign cancels (2.4e-5 of the result at K = 2048, five steps).  With two planes the accumulators therefore hold
-// this many stages only (K = 128) and are added in registers, rounded to nearest.
-constexpr int kChunk = 2;
+// The tensor cores' float32 accumulation cuts off what does not fit, an error that no sign cancels: over a long
+// contraction it adds up (2.4e-5 of the result at 512 x 2048, five steps).  With two planes the accumulators therefore
+// hold `chunk` stages only and are added in registers, rounded to nearest.  One stage (K = 64) leaves less error than
+// products in plain float32 arithmetic (1.6e-6 against 2.3e-6 at 768 x 768); two stages leave 3.0e-6 there, and from
+// about that size on no more than 1.3 times plain float32's, whose error grows with K: they are used from there, since
+// at 4096 x 4096 they take 3.4 ms where one takes 4.3.
+constexpr int kLongChunkFrom = 768;
 constexpr int kCellBytes = 2048;                 // a warp's staging of the epilogue: 32 rows of 64 bytes
 
 // An operand's tensor map(s), each with boxes that fill a stage's operand, all planes, in one load: the cost of a
@@ -442,7 +446,6 @@ __global__ void __launch_bounds__(GemmShape<CG, NP>::kThreads, 1)
 
   const int cluster = blockIdx.x / CG, clusters = gridDim.x / CG;
   const int kblocks = (p.K + kTileK - 1) / kTileK;
-  constexpr int kPerChunk = NP == 1 ? (1 << 30) : kChunk;   // stages per accumulator
   auto place = [&](int tile, int& b, int& ti, int& tj) {
     b = tile / p.tiles;
     const int t = tile - b * p.tiles;
@@ -512,7 +515,7 @@ __global__ void __launch_bounds__(GemmShape<CG, NP>::kThreads, 1)
           }
           tc_fence_after();
           const uint32_t d = tmem + buf * T;
-          const int kend = NP == 1 ? kblocks : min(kblocks, kb + kPerChunk);
+          const int kend = NP == 1 ? kblocks : min(kblocks, kb + p.chunk);
           for (uint32_t add = 0; kb < kend; ++kb) {
             if (!mbar_wait(full + 8 * s, ph, dead)) {
               ok = false;
@@ -609,7 +612,7 @@ __global__ void __launch_bounds__(GemmShape<CG, NP>::kThreads, 1)
       }
       float acc[NP == 1 ? 32 : 64];
       if (NP == 2) {
-        for (int kb = 0; kb < kblocks; kb += kPerChunk) {
+        for (int kb = 0; kb < kblocks; kb += p.chunk) {
           if (!mbar_wait(tm_full + 8 * buf, tph, dead)) {
             ok = false;
             break;
@@ -758,7 +761,7 @@ __global__ void __launch_bounds__(kResidentThreads, 1) ortho_resident_kernel(con
     mbar_init(bar, 1);
     mbar_init_visible();
   }
-  const uint32_t tmem_cols = p.slice <= 128 ? 256 : 512;
+  const uint32_t tmem_cols = NP == 1 && p.slice <= 128 ? 256 : 512;
   if (warp == 0) tmem_alloc<1>(smem_addr(&s_tmem), tmem_cols);
   // pads of the operands are zeros: rows and columns past the matrix take part in the products
   for (uint32_t i = tid * 16; i < NP * (x_plane + kSquareBytes); i += kResidentThreads * 16)
@@ -827,34 +830,41 @@ __global__ void __launch_bounds__(kResidentThreads, 1) ortho_resident_kernel(con
   tc_fence_after();
   const uint32_t tmem = s_tmem;
   const int quarter = warp & 3, group = warp >> 2;   // lanes of tensor memory, and which 32 columns of every 128
-  const uint32_t tm_s = tmem + ((uint32_t)(quarter * 32) << 16), tm_x = tm_s + 128;
+  const uint32_t tm_s = tmem + ((uint32_t)(quarter * 32) << 16);
   const int mrow = quarter * 32 + lane;              // this thread's row of the short side
   const int k_long = (width + 15) / 16, k_short = (m + 15) / 16;
   const uint32_t n_short = (uint32_t)k_short * 16, n_long = (uint32_t)k_long * 16;
   const int x_groups = (width + 31) / 32;            // groups of 32 columns of the accumulators of X
   uint32_t ph = 0;
 
-  // One product, issued by one lane of warp 0 and waited for by all: D = A B over `ks` steps of 16, operands at
+  // One product, issued by one lane of warp 0 and waited for by all: D = A B, with two planes in parts of 64 of the
+  // contraction in accumulators of their own (d_part columns apart), which are added in registers: see kLongChunkFrom.
+  // Operands: A B over `ks` steps of 16, operands at
   // desc + k * step (within a block of 64 of the contraction: `fold` steps) + block steps.
-  auto product = [&](uint32_t d, uint32_t a, uint32_t a_lo, uint32_t a_blocks, bool a_across, uint32_t bb, uint32_t b_lo,
+  auto product = [&](uint32_t d, uint32_t d_part, uint32_t a, uint32_t a_lo, uint32_t a_blocks, bool a_across, uint32_t bb, uint32_t b_lo,
                      uint32_t b_blocks, bool b_across, int ks, uint32_t n) {
     if (warp == 0) {
       tc_fence_after();
       const bool lead = elect_one();
       const uint32_t idesc = f16_idesc(128, (int)n, a_across, b_across);
       const uint64_t da0 = operand_desc(a, a_blocks), db0 = operand_desc(bb, b_blocks);
-      for (int pass = NP == 2 ? 0 : 1; pass < 2; ++pass)
-      for (int k = 0; k < ks; ++k) {
-        const uint64_t da = da0 + (a_across ? (uint32_t)k * 128u : (uint32_t)(k >> 2) * (a_blocks >> 4) + (uint32_t)(k & 3) * 2u);
-        const uint64_t db = db0 + (b_across ? (uint32_t)k * 128u : (uint32_t)(k >> 2) * (b_blocks >> 4) + (uint32_t)(k & 3) * 2u);
-        if (lead) {
-          if (pass == 0) {   // the small terms first: what is cut off goes by the accumulators' size
-            mma_f16<1>(d, da + (a_lo >> 4), db, idesc, k);
-            mma_f16<1>(d, da, db + (b_lo >> 4), idesc, 1);
-          } else {
-            mma_f16<1>(d, da, db, idesc, NP == 2 || k);
+      for (int k0 = 0; k0 < ks; k0 += 4) {
+        // the small terms first: what is cut off goes by the accumulators' size
+        for (int pass = NP == 2 ? 0 : 1; pass < 2; ++pass) {
+          for (int k = k0; k < min(ks, k0 + 4); ++k) {
+            const uint64_t da = da0 + (a_across ? (uint32_t)k * 128u : (uint32_t)(k >> 2) * (a_blocks >> 4) + (uint32_t)(k & 3) * 2u);
+            const uint64_t db = db0 + (b_across ? (uint32_t)k * 128u : (uint32_t)(k >> 2) * (b_blocks >> 4) + (uint32_t)(k & 3) * 2u);
+            if (lead) {
+              if (pass == 0) {
+                mma_f16<1>(d, da + (a_lo >> 4), db, idesc, k > k0);
+                mma_f16<1>(d, da, db + (b_lo >> 4), idesc, 1);
+              } else {
+                mma_f16<1>(d, da, db, idesc, NP == 2 || k);
+              }
+            }
           }
         }
+        if (NP == 2) d += d_part;
       }
       if (lead) mma_commit<1>(bar);
       __syncwarp();
@@ -864,12 +874,30 @@ __global__ void __launch_bounds__(kResidentThreads, 1) ortho_resident_kernel(con
     tc_fence_after();
   };
 
+  // 32 columns of a product
+  auto result = [&](uint32_t at, uint32_t part, int ks, float (&v)[32]) {
+    tmem_load32(at, v);
+    if (NP == 2) {
+      for (int k = 4; k < ks; k += 4) {
+        at += part;
+        float y[16];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          tmem_load16(at + 16 * h, y);
+#pragma unroll
+          for (int j = 0; j < 16; ++j) v[16 * h + j] += y[j];
+        }
+      }
+    }
+  };
+  const uint32_t x_at = NP == 1 ? 128u : 0u, x_part = (uint32_t)p.slice;   // accumulators of P X
+
   for (int step = 0; step < p.steps; ++step) {
     // S = X X^T over this slice
-    product(tmem, sm_x, x_plane, x_block, p.tall, sm_x, x_plane, x_block, p.tall, k_long, n_short);
+    product(tmem, 128, sm_x, x_plane, x_block, p.tall, sm_x, x_plane, x_block, p.tall, k_long, n_short);
     const bool mine = 32 * group < m;   // this warp's 32 columns of S exist
     float v[32];
-    if (mine) tmem_load32(tm_s + 32 * group, v);
+    if (mine) result(tm_s + 32 * group, 128, k_long, v);
     if (ctas == 1) {
       if (mine) {
 #pragma unroll
@@ -930,9 +958,9 @@ __global__ void __launch_bounds__(kResidentThreads, 1) ortho_resident_kernel(con
     __syncthreads();
 
     // P = a I + b S + c S^2, in place of S
-    product(tmem, sm_s, kSquareBytes, 16384u, false, sm_s, kSquareBytes, 16384u, false, k_short, n_short);
+    product(tmem, 128, sm_s, kSquareBytes, 16384u, false, sm_s, kSquareBytes, 16384u, false, k_short, n_short);
     if (mine) {
-      tmem_load32(tm_s + 32 * group, v);
+      result(tm_s + 32 * group, 128, k_short, v);
       const int own = mrow - 32 * group;   // the diagonal's column in this lane's row
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
@@ -957,10 +985,10 @@ __global__ void __launch_bounds__(kResidentThreads, 1) ortho_resident_kernel(con
     __syncthreads();
 
     // X <- P X
-    product(tmem + 128, sm_s, kSquareBytes, 16384u, false, sm_x, x_plane, x_block, !p.tall, k_short, n_long);
+    product(tmem + x_at, x_part, sm_s, kSquareBytes, 16384u, false, sm_x, x_plane, x_block, !p.tall, k_short, n_long);
     if (step + 1 == p.steps) break;
     for (int g = group; g < x_groups; g += 4) {
-      tmem_load32(tm_x + 32 * g, v);
+      result(tm_s + x_at + 32 * g, x_part, k_short, v);
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
 #pragma unroll
@@ -991,7 +1019,7 @@ __global__ void __launch_bounds__(kResidentThreads, 1) ortho_resident_kernel(con
   // the result, or the weights
   for (int g = group; g < x_groups; g += 4) {
     float v[32];
-    tmem_load32(tm_x + 32 * g, v);
+    result(tm_s + x_at + 32 * g, x_part, k_short, v);
 #pragma unroll
     for (int j = 0; j < 32; ++j) v[j] *= kStepScale / kScaleX;
     if (p.tall) {

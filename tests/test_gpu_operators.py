@@ -22,6 +22,7 @@ U = {torch.float32: 2.0 ** -24, torch.float16: 2.0 ** -11, torch.bfloat16: 2.0 *
 TINY = {torch.float32: 0.0, torch.float16: 2.0 ** -25, torch.bfloat16: 0.0}
 TOL = {B.ORTHO_HALF: 15 * 2.0 ** -11 / math.sqrt(3), B.ORTHO_SINGLE: 1e-5}
 F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+AUTO = {F32: B.ORTHO_SINGLE, F16: B.ORTHO_SINGLE, BF16: B.ORTHO_HALF}   # by the result's type
 
 
 def gen(seed=0):
@@ -84,8 +85,7 @@ def test_orthogonalize_types(tin, tout):
     g = randn(2, 70, 190, seed=3).to(tin)
     out = torch.empty(2, 70, 190, device="cuda", dtype=tout)
     B.Orthogonalizer(70, 190, batch=2).orthogonalize(g, out)
-    precision = B.ORTHO_SINGLE if tout == F32 else B.ORTHO_HALF
-    assert rel(out, direction64(g)) <= bound(precision, tout)
+    assert rel(out, direction64(g)) <= bound(AUTO[tout], tout)
 
 
 @pytest.mark.parametrize("steps", [1, 2, 3, 8])
@@ -108,7 +108,7 @@ def test_orthogonalize_strides_and_guard_bands(shape, dtype):
     store = torch.full((b * st + 11,), 9.0, device="cuda", dtype=dtype)
     out = store.as_strided((b, r, c), (st, ld, 1), 7)
     B.Orthogonalizer(r, c, batch=b).orthogonalize(g, out)
-    assert rel(out, direction64(g)) <= bound(B.ORTHO_SINGLE if dtype == F32 else B.ORTHO_HALF, dtype)
+    assert rel(out, direction64(g)) <= bound(AUTO[dtype], dtype)
     out.fill_(9.0)
     assert bool((store == 9.0).all())
 
@@ -227,7 +227,7 @@ def test_muon_step(shape, tg, tw, nesterov):
     plan.check()
     size = (args[1] * m.double()).abs() + gf.double().abs()
     assert bool(((m_out.double() - want_m).abs() <= 2 ** -23 * size).all())
-    precision = B.ORTHO_SINGLE if tw == F32 else B.ORTHO_HALF
+    precision = AUTO[tw]
     # float32 arithmetic on w and o: four roundings of values up to |w| + |step|; then the type's own
     off = (w_out.double() - want_w).norm()
     limit = TOL[precision] * step.norm() + (4 * U[F32] + U[tw]) * (w.double().norm() + step.norm())
@@ -252,7 +252,7 @@ def test_muon_step_for_replicas(tw):
     assert torch.equal(w[1], one) and torch.equal(m, m1)
     _, want, step = muon64(g, torch.zeros_like(g) + randn(1, r, c, seed=12), before.as_strided(w.shape, w.stride(), at),
                            0.02, 0.95, True, 0.0, 0.3)
-    limit = TOL[B.ORTHO_SINGLE if tw == F32 else B.ORTHO_HALF] * step.norm() * n ** 0.5 + (4 * U[F32] + U[tw]) * want.norm()
+    limit = TOL[AUTO[tw]] * step.norm() * n ** 0.5 + (4 * U[F32] + U[tw]) * want.norm()
     assert float((w.double() - want).norm()) <= float(limit)
     rows.as_strided(w.shape, w.stride(), at).zero_()
     before.as_strided(w.shape, w.stride(), at).zero_()
