@@ -516,9 +516,9 @@ typedef struct brace_embedding {
  * pointer, non-finite scale, stride_act 0 with several clients), CUDA. */
 int brace_embedding_lookup(const brace_embedding* e, brace_stream_t stream);
 
-/* Bytes of workspace of brace_embedding_grad: the sorted ids and the partial sums
- * of frequent tokens; 0 if the arguments are invalid. */
-size_t brace_embedding_workspace_bytes(int32_t clients, int64_t tokens, int32_t dim);
+/* Bytes of workspace of brace_embedding_grad: the sorted ids, where each begins,
+ * and the partial sums of frequent tokens; 0 if the arguments are invalid. */
+size_t brace_embedding_workspace_bytes(int32_t clients, int64_t tokens, int64_t vocab, int32_t dim);
 
 /* d_table[c][v] = scale * sum of d_act[c][t] over the tokens t with id v, in
  * float32 in one order (increasing t, in groups), rounded once to table_type: the

@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 import torch
 
@@ -120,7 +121,7 @@ SIGNATURES = {
                                   C.c_void_p, C.c_size_t, C.c_void_p]),
     "brace_ortho_status": (C.c_int, [C.c_void_p, C.c_void_p]),
     "brace_embedding_lookup": (C.c_int, [C.POINTER(EmbeddingArgs), C.c_void_p]),
-    "brace_embedding_workspace_bytes": (C.c_size_t, [C.c_int32, C.c_int64, C.c_int32]),
+    "brace_embedding_workspace_bytes": (C.c_size_t, [C.c_int32, C.c_int64, C.c_int64, C.c_int32]),
     "brace_embedding_grad": (C.c_int, [C.POINTER(EmbeddingArgs), C.c_void_p, C.c_size_t, C.c_void_p]),
 }
 
@@ -166,8 +167,14 @@ def workspace_bytes(n: int, d: int, params: Params) -> int:
     return int(lib().brace_workspace_bytes(n, d, C.byref(params)))
 
 
+# the current stream's handle without a Stream object around it (a microsecond of a call's ten)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(stream) -> int:
     if stream is None:
+        if _raw_stream is not None and torch.cuda.is_initialized():
+            return _raw_stream(torch.cuda.current_device())
         stream = torch.cuda.current_stream()
     return int(stream.cuda_stream)
 
@@ -382,7 +389,9 @@ class Brace:
 
 # ---- operators of a language model's round -----------------------------------------------------------------------
 
-_TYPES = {torch.float32: TYPE_F32, torch.bfloat16: TYPE_BF16, torch.float16: TYPE_F16, torch.int32: TYPE_BITS}
+_FLOATS = {torch.float32: TYPE_F32, torch.bfloat16: TYPE_BF16, torch.float16: TYPE_F16}
+_ID_BYTES = {torch.int64: 8, torch.int32: 4}
+_EMBEDDING = struct.Struct("@ii10q4if")       # the fields of EmbeddingArgs
 
 
 def ortho_params(**over) -> OrthoParams:
@@ -417,17 +426,17 @@ class Orthogonalizer:
 
     def _matrix(self, t: torch.Tensor, name: str):
         """(element type, ld, stride between matrices) of a tensor argument."""
-        shape = tuple(t.shape)
+        shape = t.shape
         if shape != (self.batch, self.rows, self.cols) and not (self.batch == 1 and shape == (self.rows, self.cols)):
-            raise ValueError(f"{name} has shape {shape}, not {(self.batch, self.rows, self.cols)}")
-        if t.dtype not in _TYPES or t.dtype == torch.int32:
+            raise ValueError(f"{name} has shape {tuple(shape)}, not {(self.batch, self.rows, self.cols)}")
+        kind = _FLOATS.get(t.dtype)
+        if kind is None:
             raise ValueError(f"{name} is of type {t.dtype}")
         st = t.stride()
         if self.cols > 1 and st[-1] != 1:
             raise ValueError(f"{name}: the last dimension is not contiguous")
         # the stride of a dimension of one (or no) element has no meaning
-        ld = st[-2] if self.rows > 1 else max(self.cols, 1)
-        return _TYPES[t.dtype], ld, st[0] if self.batch > 1 else 0
+        return kind, st[-2] if self.rows > 1 else max(self.cols, 1), st[0] if self.batch > 1 else 0
 
     def _update(self, g: torch.Tensor, name: str, bit_offset: int):
         if g.dtype == torch.int32:
@@ -506,37 +515,36 @@ class Embedding:
                  workspace: torch.Tensor | None = None):
         self.clients, self.vocab, self.dim, self.tokens = clients, vocab, dim, tokens
         if grad and workspace is None:
-            need = int(lib().brace_embedding_workspace_bytes(clients, tokens, dim))
+            need = int(lib().brace_embedding_workspace_bytes(clients, tokens, vocab, dim))
             workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=device)
         self.workspace = workspace
         self._args = EmbeddingArgs()
 
-    def _fill(self, table: torch.Tensor, ids: torch.Tensor, act: torch.Tensor, scale: float, shared: bool):
+    def _fill(self, table: torch.Tensor, ids: torch.Tensor, act: torch.Tensor, scale: float, shared: bool,
+              accumulate: bool = False):
         c, d, e = self.clients, self.dim, self._args
-        n = ids.shape[-1]
-        if tuple(ids.shape) not in ((c, n), (n,) if c == 1 else (c, n)) or n > self.tokens:
-            raise ValueError(f"ids have shape {tuple(ids.shape)}, not {(c, n)} with at most {self.tokens} tokens")
-        if ids.dtype not in (torch.int64, torch.int32) or (n > 1 and ids.stride(-1) != 1):
+        shape = ids.shape
+        n = shape[-1] if len(shape) else 0
+        if (shape != (c, n) and (c != 1 or shape != (n,))) or n > self.tokens:
+            raise ValueError(f"ids have shape {tuple(shape)}, not {(c, n)} with at most {self.tokens} tokens")
+        id_bytes, id_stride = _ID_BYTES.get(ids.dtype), ids.stride()
+        if id_bytes is None or (n > 1 and id_stride[-1] != 1):
             raise ValueError("ids are int64 or int32 with a contiguous last dimension")
-        tables = ((c, self.vocab, d),) + (((self.vocab, d),) if c == 1 or shared else ())
-        if tuple(table.shape) not in tables:
-            raise ValueError(f"table has shape {tuple(table.shape)}, not {tables[0]}")
-        if tuple(act.shape) != (c, n, d) and not (c == 1 and tuple(act.shape) == (n, d)):
+        if table.shape != (c, self.vocab, d) and not ((c == 1 or shared) and table.shape == (self.vocab, d)):
+            raise ValueError(f"table has shape {tuple(table.shape)}, not {(c, self.vocab, d)}")
+        if act.shape != (c, n, d) and not (c == 1 and act.shape == (n, d)):
             raise ValueError(f"activations have shape {tuple(act.shape)}, not {(c, n, d)}")
-        for t, name in ((table, "table"), (act, "activations")):
-            if t.dtype not in _TYPES or t.dtype == torch.int32:
-                raise ValueError(f"{name} is of type {t.dtype}")
-            if d > 1 and t.stride(-1) != 1:
-                raise ValueError(f"{name}: the last dimension is not contiguous")
-        e.clients, e.dim, e.tokens, e.vocab, e.scale = c, d, n, self.vocab, scale
-        e.d_table, e.table_type = table.data_ptr(), _TYPES[table.dtype]
-        e.ld_table = table.stride(-2) if self.vocab > 1 else d
-        e.stride_table = table.stride(0) if table.dim() == 3 and c > 1 else 0
-        e.d_ids, e.id_bytes = ids.data_ptr(), 8 if ids.dtype == torch.int64 else 4
-        e.stride_ids = ids.stride(0) if c > 1 else 0
-        e.d_act, e.act_type = act.data_ptr(), _TYPES[act.dtype]
-        e.ld_act = act.stride(-2) if n > 1 else d
-        e.stride_act = act.stride(0) if c > 1 else 0
+        table_type, act_type = _FLOATS.get(table.dtype), _FLOATS.get(act.dtype)
+        if table_type is None or act_type is None:
+            raise ValueError(f"table and activations are of type {table.dtype} and {act.dtype}")
+        ts, as_ = table.stride(), act.stride()
+        if d > 1 and (ts[-1] != 1 or as_[-1] != 1):
+            raise ValueError("the last dimension of table and activations is contiguous")
+        # the stride of a dimension of one element has no meaning
+        _EMBEDDING.pack_into(e, 0, c, d, n, self.vocab, table.data_ptr(), ts[-2] if self.vocab > 1 else d,
+                             ts[0] if c > 1 and len(ts) == 3 else 0, ids.data_ptr(), id_stride[0] if c > 1 else 0,
+                             act.data_ptr(), as_[-2] if n > 1 else d, as_[0] if c > 1 else 0, table_type, act_type,
+                             id_bytes, accumulate, scale)
         return e
 
     def lookup_status(self, table, ids, out, scale: float = 1.0, stream=None) -> int:
@@ -548,8 +556,7 @@ class Embedding:
         _check(self.lookup_status(table, ids, out, scale, stream), "brace_embedding_lookup")
 
     def grad_status(self, dy, ids, grad, scale: float = 1.0, accumulate: bool = False, stream=None) -> int:
-        e = self._fill(grad, ids, dy, scale, False)
-        e.accumulate = int(accumulate)
+        e = self._fill(grad, ids, dy, scale, False, accumulate)
         ws = self.workspace
         return lib().brace_embedding_grad(e, _ptr(ws), ws.numel() if ws is not None else 0, _stream(stream))
 

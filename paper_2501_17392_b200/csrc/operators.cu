@@ -446,10 +446,10 @@ MatRef mat_ref(const void* p, int type, int64_t ld, int64_t stride, int64_t bit0
 
 struct EmbPlan {
   int64_t parts;
-  size_t off_key[2], off_pos[2], off_part, bytes;
+  size_t off_key[2], off_pos[2], off_span, off_part, bytes;
 };
 
-EmbPlan emb_plan(int32_t clients, int64_t tokens, int32_t dim) {
+EmbPlan emb_plan(int32_t clients, int64_t tokens, int64_t vocab, int32_t dim) {
   EmbPlan q;
   size_t at = 0;
   auto take = [&at](int64_t bytes) {
@@ -463,19 +463,20 @@ EmbPlan emb_plan(int32_t clients, int64_t tokens, int32_t dim) {
     q.off_key[i] = take(i == 0 || merged ? 4 * n : 0);
     q.off_pos[i] = take(i == 0 || merged ? 4 * n : 0);
   }
-  q.parts = tokens / kPart;
-  q.off_part = take((int64_t)clients * q.parts * dim * 4);
+  q.off_span = take(8 * (int64_t)clients * vocab);
+  q.parts = (tokens + kPart - 1) / kPart;
+  q.off_part = take((int64_t)clients * q.parts * 2 * dim * 4);
   q.bytes = at > 256 ? at : 256;
   return q;
 }
 
-bool emb_sizes_ok(int32_t clients, int64_t tokens, int32_t dim) {
-  return clients >= 0 && clients <= 65535 && tokens >= 0 && tokens < ((int64_t)1 << 31) && dim >= 1;
+bool emb_sizes_ok(int32_t clients, int64_t tokens, int64_t vocab, int32_t dim) {
+  const int64_t most = (int64_t)1 << 31;
+  return clients >= 0 && clients <= 65535 && tokens >= 0 && tokens < most && vocab >= 1 && vocab < most && dim >= 1;
 }
 
 int emb_check(const brace_embedding* e, bool grad) {
-  if (!e || !emb_sizes_ok(e->clients, e->tokens, e->dim)) return BRACE_ERR_INVALID_ARG;
-  if (e->vocab < 1 || e->vocab >= ((int64_t)1 << 31)) return BRACE_ERR_INVALID_ARG;
+  if (!e || !emb_sizes_ok(e->clients, e->tokens, e->vocab, e->dim)) return BRACE_ERR_INVALID_ARG;
   if (!float_type(e->table_type) || !float_type(e->act_type)) return BRACE_ERR_INVALID_ARG;
   if ((e->id_bytes != 4 && e->id_bytes != 8) || !std::isfinite(e->scale)) return BRACE_ERR_INVALID_ARG;
   // what is only read may be broadcast: rows of the gradient's activations that are all the same one
@@ -534,30 +535,29 @@ cudaError_t launch_sort(const EmbArgs& a, cudaStream_t st) {
   while ((a.vocab >> bits) != 0) ++bits;   // the largest value of these bits stands for "no token"
   if (a.tokens <= 1024) {
     const int threads = (int)round_up(a.tokens, 32);
-    const size_t smem = (size_t)threads * 8 + (size_t)kDigits * (threads / 32) * 4;
+    const size_t smem = (size_t)threads * 8 + (size_t)kCountRow * (threads / 32) * 4;
     return launch(embedding_sort_kernel<1>, dim3(1, (unsigned)a.clients), threads, smem, 1, st, a, threads, bits);
   }
-  const int threads = (int)(a.tokens < kSortTile ? round_up(a.tokens, 32 * kSortItems) / kSortItems : 1024);
-  const int tile = threads * kSortItems;
-  const size_t smem = (size_t)tile * 8 + (size_t)kDigits * (threads / 32) * 4;
-  cudaError_t err = cudaFuncSetAttribute(embedding_sort_kernel<kSortItems>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                         kSortTile * 8 + kDigits * 32 * 4);
-  if (err != cudaSuccess) return err;
+  const int threads = kSortThreads, tile = kSortTile;
+  const size_t smem = (size_t)tile * 8 + (size_t)kCountRow * (threads / 32) * 4;
   return launch(embedding_sort_kernel<kSortItems>, dim3((unsigned)((a.tokens + tile - 1) / tile), (unsigned)a.clients),
                 threads, smem, 1, st, a, tile, bits);
 }
 
+constexpr int64_t kGradElements = 32768;   // of a CTA's rows
+
 template <typename TI, typename TO, int V>
 cudaError_t launch_grad(EmbArgs a, cudaStream_t st) {
-  if (a.parts > 0) {
-    const cudaError_t err =
-        launch(embedding_part_kernel<TI, V>,
-               dim3((unsigned)a.parts, (unsigned)((a.dim / V + 127) / 128), (unsigned)a.clients), 128, 0, 1, st, a);
+  if (a.tokens > 0) {
+    const cudaError_t err = launch(embedding_sum_kernel<TI, TO, V>, dim3((unsigned)a.parts, (unsigned)a.clients), 256, 0, 1, st, a);
     if (err != cudaSuccess) return err;
   }
-  const int rows = 16384 / a.dim;
-  a.rows_cta = rows < 1 ? 1 : rows > 64 ? 64 : rows;
-  return launch(embedding_grad_kernel<TI, TO, V>,
+  // long runs of zeros, but 16 CTAs for each SM while the table has the rows
+  int64_t rows = kGradElements / a.dim;
+  const int64_t even = a.vocab * a.clients / (16 * sm_count());
+  if (rows > even) rows = even;
+  a.rows_cta = rows < 1 ? 1 : rows > 64 ? 64 : (int)rows;
+  return launch(embedding_grad_kernel<TO, V>,
                 dim3((unsigned)((a.vocab + a.rows_cta - 1) / a.rows_cta), (unsigned)a.clients), 256, 0, 1, st, a);
 }
 
@@ -586,8 +586,8 @@ int brace_embedding_lookup(const brace_embedding* e, brace_stream_t stream) {
   return err == cudaSuccess ? BRACE_OK : cuda_fail_no_ctx(err);
 }
 
-size_t brace_embedding_workspace_bytes(int32_t clients, int64_t tokens, int32_t dim) {
-  return emb_sizes_ok(clients, tokens, dim) ? emb_plan(clients, tokens, dim).bytes : 0;
+size_t brace_embedding_workspace_bytes(int32_t clients, int64_t tokens, int64_t vocab, int32_t dim) {
+  return emb_sizes_ok(clients, tokens, vocab, dim) ? emb_plan(clients, tokens, vocab, dim).bytes : 0;
 }
 
 int brace_embedding_grad(const brace_embedding* e, void* d_workspace, size_t workspace_bytes, brace_stream_t stream) {
@@ -596,7 +596,7 @@ int brace_embedding_grad(const brace_embedding* e, void* d_workspace, size_t wor
   if (e->clients == 0) return BRACE_OK;
   if (!emb_table_ok(e) || (e->tokens > 0 && !emb_act_ok(e)) || (e->clients > 1 && e->stride_table == 0))
     return BRACE_ERR_INVALID_ARG;
-  const EmbPlan q = emb_plan(e->clients, e->tokens, e->dim);
+  const EmbPlan q = emb_plan(e->clients, e->tokens, e->vocab, e->dim);
   if (!d_workspace || workspace_bytes < q.bytes || !aligned(d_workspace, 256)) return BRACE_ERR_WORKSPACE;
   if (e->tokens == 0 && e->accumulate) return BRACE_OK;
   char* ws = (char*)d_workspace;
@@ -605,6 +605,7 @@ int brace_embedding_grad(const brace_embedding* e, void* d_workspace, size_t wor
   a.in = e->d_act;
   a.key = (uint32_t*)(ws + q.off_key[0]);
   a.pos = (uint32_t*)(ws + q.off_pos[0]);
+  a.span = (uint2*)(ws + q.off_span);
   a.part = (float*)(ws + q.off_part);
   a.parts = q.parts;
   const cudaStream_t st = (cudaStream_t)stream;
@@ -615,7 +616,9 @@ int brace_embedding_grad(const brace_embedding* e, void* d_workspace, size_t wor
     int from = 0;
     for (int64_t run = kSortTile; err == cudaSuccess && run < a.tokens; run *= kMergeRuns) {
       uint32_t *key = (uint32_t*)(ws + q.off_key[from ^ 1]), *pos = (uint32_t*)(ws + q.off_pos[from ^ 1]);
-      err = launch(embedding_merge_kernel, dim3((unsigned)((a.tokens + 255) / 256), (unsigned)a.clients), 256, 0, 1, st, a, run, key, pos);
+      const dim3 grid((unsigned)((a.tokens + 255) / 256), (unsigned)a.clients);
+      err = a.tokens <= 4 * run ? launch(embedding_merge_kernel<4>, grid, 256, 0, 1, st, a, (int)run, key, pos)
+                                : launch(embedding_merge_kernel<kMergeRuns>, grid, 256, 0, 1, st, a, (int)run, key, pos);
       a.key = key;
       a.pos = pos;
       from ^= 1;
