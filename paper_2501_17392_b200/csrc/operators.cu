@@ -193,10 +193,10 @@ struct OrthoMaps {
   CUtensorMap x[2][2], s[2], t[2], p[2];
 };
 
-template <int CG, int NP, int OP_A, int OP_B, int MODE, typename TOUT = __half>
-cudaError_t launch_gemm(const CUtensorMap (&a)[2], const CUtensorMap (&b)[2], const GemmArgs& g, cudaStream_t st) {
+template <int CG, int NP, int OP_A, int OP_B, int MODE, typename TOUT, int KS>
+cudaError_t launch_gemm_as(const CUtensorMap (&a)[2], const CUtensorMap (&b)[2], const GemmArgs& g, cudaStream_t st) {
   using Shape = GemmShape<CG, NP>;
-  auto* kernel = ortho_gemm_kernel<CG, NP, OP_A, OP_B, MODE, TOUT>;
+  auto* kernel = ortho_gemm_kernel<CG, NP, OP_A, OP_B, MODE, TOUT, KS>;
   GemmMaps maps;   // first the one that the operand needs (a symmetric one needs both)
   maps.a[0] = a[OP_A == kAcross];
   maps.a[1] = a[1];
@@ -212,9 +212,39 @@ cudaError_t launch_gemm(const CUtensorMap (&a)[2], const CUtensorMap (&b)[2], co
     if (err != cudaSuccess) return err;
     granted.fetch_or(bit, std::memory_order_relaxed);
   }
-  int clusters = sm_count() / CG;
+  int clusters = KS > 1 ? g.total : sm_count() / CG;
   if (clusters > g.total) clusters = g.total;
-  return launch(kernel, dim3((unsigned)(clusters * CG)), Shape::kThreads, Shape::kSmem, CG, st, maps, g);
+  return launch(kernel, dim3((unsigned)(clusters * CG * KS)), Shape::kThreads, Shape::kSmem, CG * KS, st, maps, g);
+}
+
+// CTAs that share the contraction of a tile, where the tiles alone leave SMs idle: sharing costs about 2 us for the
+// exchange and saves its part of the stages (0.2 us each, 0.65 with two planes): 512 x 2048 in float32 259 -> 182 us.
+// All clusters have to run at once, and one of 4 CTAs lies within a group of SMs that the hardware wires together: 28
+// always find room, 36 did not (1024 x 1024 took 210 us for 119).
+int split_of(int tiles, int kblocks, int planes) {
+  const double stage = planes == 1 ? 0.2 : 0.65;
+  int best = 1;
+  double least = kblocks * stage;
+  for (int ks = 2; ks <= 4; ks *= 2) {
+    if (tiles * ks > (ks == 2 ? sm_count() * 7 / 8 : sm_count() * 3 / 4) || kblocks < ks) break;
+    const double t = (kblocks + ks - 1) / ks * stage + 2.0;
+    if (t < least) {
+      least = t;
+      best = ks;
+    }
+  }
+  return best;
+}
+
+template <int CG, int NP, int OP_A, int OP_B, int MODE, typename TOUT = __half>
+cudaError_t launch_gemm(const CUtensorMap (&a)[2], const CUtensorMap (&b)[2], const GemmArgs& g, cudaStream_t st) {
+  if constexpr (CG == 1) {
+    switch (split_of(g.total, (g.K + kTileK - 1) / kTileK, NP)) {
+      case 4: return launch_gemm_as<CG, NP, OP_A, OP_B, MODE, TOUT, 4>(a, b, g, st);
+      case 2: return launch_gemm_as<CG, NP, OP_A, OP_B, MODE, TOUT, 2>(a, b, g, st);
+    }
+  }
+  return launch_gemm_as<CG, NP, OP_A, OP_B, MODE, TOUT, 1>(a, b, g, st);
 }
 
 template <int CG, int NP>
@@ -552,9 +582,9 @@ cudaError_t launch_grad(EmbArgs a, cudaStream_t st) {
     const cudaError_t err = launch(embedding_sum_kernel<TI, TO, V>, dim3((unsigned)a.parts, (unsigned)a.clients), 256, 0, 1, st, a);
     if (err != cudaSuccess) return err;
   }
-  // long runs of zeros, but 16 CTAs for each SM while the table has the rows
+  // long runs of zeros, but 4 CTAs for each SM while the table has the rows
   int64_t rows = kGradElements / a.dim;
-  const int64_t even = a.vocab * a.clients / (16 * sm_count());
+  const int64_t even = a.vocab * a.clients / (4 * sm_count());
   if (rows > even) rows = even;
   a.rows_cta = rows < 1 ? 1 : rows > 64 ? 64 : (int)rows;
   return launch(embedding_grad_kernel<TO, V>,

@@ -399,11 +399,43 @@ __device__ __forceinline__ void last_cell(const GemmArgs& p, uint32_t cell, int6
   }
 }
 
+// Where there are too few tiles for the GPU, a cluster of KS CTAs shares the contraction of one (CG = 1): each sums its
+// part of it, hands every other one its share of the columns through distributed shared memory, and finishes its own.
+template <int KS>
+__device__ __forceinline__ uint32_t share_at(uint32_t base, int from, int row, int word) {
+  constexpr int kWords = 32 / KS;   // 16-byte words of a row of an owner's columns
+  return base + (uint32_t)(((from * 128 + row) * kWords + (word ^ (row & (kWords - 1)))) << 4);
+}
+
+// 32 rows x 32 columns of a finished product: scaled, and stored as operand planes or as the caller's result.
+template <int NP, int MODE, typename TOUT>
+__device__ __forceinline__ void finish_block(const GemmArgs& p, uint32_t cell, int64_t b, int row0, int col0, int rows,
+                                             const uint4 (&source)[4], float* v) {
+  const int64_t plane = (int64_t)p.M * p.ld_dst, at = b * NP * plane + (int64_t)row0 * p.ld_dst + col0;
+  const int own = row0 + (int)(threadIdx.x & 31) - col0;   // the diagonal's column in this lane's row
+  if (MODE == kModeLast) {
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v[i] *= kStepScale / kScaleX;
+#pragma unroll
+    for (int q = 0; q < 2; ++q) last_cell<TOUT>(p, cell, b, row0, col0 + 16 * q, v + 16 * q);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v[i] = fmaf(v[i], p.scale, MODE == kModePoly && i == own ? p.diagonal : 0.f);
+    if (MODE == kModePoly && NP == 1) block_add(cell, source, p.scale2, v);
+    store_planes<NP>(cell, v, p.dst + at, plane, p.ld_dst, rows);
+    if (MODE == kModeGram && NP == 2) {
+#pragma unroll
+      for (int i = 0; i < 32; ++i) v[i] = fmaf(v[i], p.scale2, i == own ? p.diagonal2 : 0.f);
+      store_planes<NP>(cell, v, p.dst2 + at, plane, p.ld_dst, rows);
+    }
+  }
+}
+
 // One product of the iteration over tiles of 128 x 128 (CG = 1) or, by a pair of CTAs, 256 x 256 (CG = 2), NP planes
 // per operand.  Warp 0 loads, warp 1 issues the matrix instructions, warp 2 owns the tensor memory, warps 4.. read the
 // accumulators and write the results; persistent over tiles, so that the epilogue of a tile runs under the products
 // of the next.
-template <int CG, int NP, int OP_A, int OP_B, int MODE, typename TOUT>
+template <int CG, int NP, int OP_A, int OP_B, int MODE, typename TOUT, int KS>
 __global__ void __launch_bounds__(GemmShape<CG, NP>::kThreads, 1)
     ortho_gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmArgs p) {
   using Shape = GemmShape<CG, NP>;
@@ -416,7 +448,9 @@ __global__ void __launch_bounds__(GemmShape<CG, NP>::kThreads, 1)
   volatile int* dead = (volatile int*)(smem_raw + (tail - smem_addr(smem_raw)));
   uint32_t* tmem_slot = (uint32_t*)(smem_raw + (tail + 8 - smem_addr(smem_raw)));
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  static_assert(KS == 1 || CG == 1, "a pair of CTAs does not share a contraction");
   const uint32_t rank = CG == 1 ? 0u : cluster_rank();
+  const int part = KS == 1 ? 0 : (int)cluster_rank();
 
   if (threadIdx.x == 0) {
     *dead = 0;
@@ -444,8 +478,8 @@ __global__ void __launch_bounds__(GemmShape<CG, NP>::kThreads, 1)
   grid_wait();
   fence_async_global();
 
-  const int cluster = blockIdx.x / CG, clusters = gridDim.x / CG;
-  const int kblocks = (p.K + kTileK - 1) / kTileK;
+  const int cluster = blockIdx.x / (CG * KS), clusters = gridDim.x / (CG * KS);
+  const int kall = (p.K + kTileK - 1) / kTileK, kfirst = kall * part / KS, kblocks = kall * (part + 1) / KS;
   auto place = [&](int tile, int& b, int& ti, int& tj) {
     b = tile / p.tiles;
     const int t = tile - b * p.tiles;
@@ -461,6 +495,7 @@ __global__ void __launch_bounds__(GemmShape<CG, NP>::kThreads, 1)
 
   // the launch's registers (640 threads x 96) go to the warps that hold accumulators: 4 x 32 x 32 + 16 x 32 x 112
   if (CG == 2 && warp < 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 32;");
+  float acc[NP == 1 && KS == 1 ? 32 : 64];
   if (warp == 0) {
     const bool lead = elect_one();
     const uint32_t full0 = CG == 1 ? full : map_to_rank(full, 0);
@@ -471,7 +506,7 @@ __global__ void __launch_bounds__(GemmShape<CG, NP>::kThreads, 1)
       int b, ti, tj;
       place(tile, b, ti, tj);
       const int ra = ti * T + (int)rank * 128, rb = tj * T + (int)rank * 128;
-      for (int kb = 0; kb < kblocks; ++kb) {
+      for (int kb = kfirst; kb < kblocks; ++kb) {
         if (!mbar_wait(empty + 8 * s, ph ^ 1u, dead)) {
           ok = false;
           break;
@@ -508,7 +543,7 @@ __global__ void __launch_bounds__(GemmShape<CG, NP>::kThreads, 1)
       for (int tile = cluster; ok && tile < p.total; tile += clusters) {
         int b, ti, tj;
         place(tile, b, ti, tj);
-        for (int kb = 0; ok && kb < kblocks;) {
+        for (int kb = kfirst; ok && kb < kblocks;) {
           if (!mbar_wait(tm_empty + 8 * buf, tph ^ 1u, dead)) {
             ok = false;
             break;
@@ -529,7 +564,7 @@ __global__ void __launch_bounds__(GemmShape<CG, NP>::kThreads, 1)
             const uint64_t da = desc0 + (uint64_t)(s * Shape::kStageBytes >> 4), db = da + (NP * kOperandBytes >> 4);
             constexpr uint64_t lo = kOperandBytes >> 4;   // the second plane
             if (lead) {
-              if (kb + 1 < kblocks) {
+              if (kb + 1 < kall) {
 #pragma unroll
                 for (int k = 0; k < kTileK / 16; ++k) {
                   if (NP == 2) {   // the small terms first: what is cut off goes by the accumulators' size
@@ -601,18 +636,16 @@ __global__ void __launch_bounds__(GemmShape<CG, NP>::kThreads, 1)
       place(tile, b, ti, tj);
       const int row0 = ti * T + (int)rank * 128 + quarter * 32, col0 = tj * T + cols0;
       const int rows = min(32, p.M - row0);   // may be none: the accumulators are then read for nothing
-      const int64_t plane = (int64_t)p.M * p.ld_dst;
       // rows are padded to 64 columns; the pad is written too (the operands' pads are zeros, so it stays zero)
       const bool live = rows > 0 && col0 < p.N;
-      const int64_t at = b * NP * plane + (int64_t)row0 * p.ld_dst + col0;
       uint4 x0[4], x1[4];
-      if (MODE == kModePoly && NP == 1 && live) {
-        block_fetch(p.src + at, p.ld_dst, rows, x0);
-        block_fetch(p.src + at + 32, p.ld_dst, rows, x1);
+      if (MODE == kModePoly && NP == 1 && KS == 1 && live) {
+        const __half* src = p.src + b * p.M * p.ld_dst + (int64_t)row0 * p.ld_dst + col0;
+        block_fetch(src, p.ld_dst, rows, x0);
+        block_fetch(src + 32, p.ld_dst, rows, x1);
       }
-      float acc[NP == 1 ? 32 : 64];
       if (NP == 2) {
-        for (int kb = 0; kb < kblocks; kb += p.chunk) {
+        for (int kb = kfirst; kb < kblocks; kb += p.chunk) {
           if (!mbar_wait(tm_full + 8 * buf, tph, dead)) {
             ok = false;
             break;
@@ -623,7 +656,7 @@ __global__ void __launch_bounds__(GemmShape<CG, NP>::kThreads, 1)
             float v[16];
             tmem_load16(tm_mine + buf * T + 16 * q, v);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) acc[(16 * q + i) & (NP * 32 - 1)] = (kb ? acc[(16 * q + i) & (NP * 32 - 1)] : 0.f) + v[i];
+            for (int i = 0; i < 16; ++i) acc[(16 * q + i) & (NP * 32 - 1)] = (kb > kfirst ? acc[(16 * q + i) & (NP * 32 - 1)] : 0.f) + v[i];
           }
           release();
         }
@@ -633,6 +666,14 @@ __global__ void __launch_bounds__(GemmShape<CG, NP>::kThreads, 1)
         tc_fence_after();
       }
       if (!ok) break;
+      if (KS > 1) {
+        if (NP == 1) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+            tmem_load32(tm_mine + buf * T + 32 * h, *reinterpret_cast<float(*)[32]>(acc + (KS > 1 ? 32 * h : 0)));
+        }
+        break;   // one tile; it is finished below
+      }
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         float* v = acc + (NP == 1 ? 0 : 32 * h);
@@ -640,25 +681,47 @@ __global__ void __launch_bounds__(GemmShape<CG, NP>::kThreads, 1)
           tmem_load32(tm_mine + buf * T + 32 * h, *reinterpret_cast<float(*)[32]>(v));
           if (h == 1) release();
         }
-        if (live) {
-          const int own = row0 + lane - (col0 + 32 * h);   // the diagonal's column in this lane's row
-          if (MODE == kModeLast) {
+        if (live) finish_block<NP, MODE, TOUT>(p, cell, b, row0, col0 + 32 * h, rows, h == 0 ? x0 : x1, v);
+      }
+    }
+    if (KS == 1) fence_async_global();
+  }
+  if (KS > 1) {
+    int b, ti, tj;
+    place(cluster, b, ti, tj);
+    const int quarter = warp & 3, cols0 = ((warp - 4) >> 2) * 64;
+    cluster_sync();   // no matrix instruction reads the stages any more, here or in the other CTAs
+    if (warp >= 4) {
+      constexpr int kWords = 32 / KS;
 #pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] *= kStepScale / kScaleX;
+      for (int w = 0; w < 16; ++w) {
+        const int word = cols0 / 4 + w, owner = word / kWords;
+        st_cluster16(map_to_rank(share_at<KS>(base, part, quarter * 32 + lane, word - owner * kWords), (uint32_t)owner),
+                     make_uint4(__float_as_uint(acc[4 * w]), __float_as_uint(acc[4 * w + 1]),
+                                __float_as_uint(acc[4 * w + 2]), __float_as_uint(acc[4 * w + 3])));
+      }
+    }
+    cluster_sync();
+    constexpr int kBlocks = 4 / KS;   // blocks of 32 columns of this CTA's share
+    const int block = (warp - 4) >> 2;
+    if (warp >= 4 && block < kBlocks) {
+      const int row0 = ti * T + quarter * 32, col0 = tj * T + (part * kBlocks + block) * 32, rows = min(32, p.M - row0);
+      if (rows > 0 && col0 < ((p.N + 63) & ~63)) {
+        uint4 x0[4];
+        if (MODE == kModePoly && NP == 1)
+          block_fetch(p.src + b * p.M * p.ld_dst + (int64_t)row0 * p.ld_dst + col0, p.ld_dst, rows, x0);
 #pragma unroll
-            for (int q = 0; q < 2; ++q) last_cell<TOUT>(p, cell, b, row0, col0 + 32 * h + 16 * q, v + 16 * q);
-          } else {
+        for (int i = 0; i < 32; ++i) acc[i] = 0.f;
+        for (int q = 0; q < KS; ++q)
 #pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] = fmaf(v[i], p.scale, MODE == kModePoly && i == own ? p.diagonal : 0.f);
-            if (MODE == kModePoly && NP == 1) block_add(cell, h == 0 ? x0 : x1, p.scale2, v);
-            store_planes<NP>(cell, v, p.dst + at + 32 * h, plane, p.ld_dst, rows);
-            if (MODE == kModeGram && NP == 2) {
-#pragma unroll
-              for (int i = 0; i < 32; ++i) v[i] = fmaf(v[i], p.scale2, i == own ? p.diagonal2 : 0.f);
-              store_planes<NP>(cell, v, p.dst2 + at + 32 * h, plane, p.ld_dst, rows);
-            }
+          for (int w = 0; w < 8; ++w) {
+            const uint4 t = lds16(share_at<KS>(base, q, quarter * 32 + lane, block * 8 + w));
+            acc[4 * w] += __uint_as_float(t.x);
+            acc[4 * w + 1] += __uint_as_float(t.y);
+            acc[4 * w + 2] += __uint_as_float(t.z);
+            acc[4 * w + 3] += __uint_as_float(t.w);
           }
-        }
+        finish_block<NP, MODE, TOUT>(p, cells + (warp - 4) * kCellBytes, b, row0, col0, rows, x0, acc);
       }
     }
     fence_async_global();
