@@ -7,7 +7,6 @@
 
 #include <atomic>
 #include <cmath>
-#include <cstdlib>
 
 #include "embedding_kernels.cuh"
 #include "ortho_kernels.cuh"
@@ -174,34 +173,48 @@ EncodeFn encode_fn() {
   return (EncodeFn)f;
 }
 
-// [planes of all matrices][rows][ld] float16 as blocks of 64 columns; one box holds `box_planes` planes of 128 rows of a
-// block (along) or of 64 rows of two blocks (across); 128-byte swizzle, zeros outside.
-int make_map(CUtensorMap* map, void* base, int64_t rows, int64_t ld, int64_t planes, int box_planes, bool across) {
-  EncodeFn enc = encode_fn();
-  if (!enc) return cuda_fail_no_ctx(cudaErrorNotSupported);
-  const cuuint64_t dim[4] = {64, (cuuint64_t)rows, (cuuint64_t)(ld / 64), (cuuint64_t)planes};
-  const cuuint64_t stride[3] = {(cuuint64_t)ld * 2, 128, (cuuint64_t)ld * 2 * (cuuint64_t)rows};
-  const cuuint32_t box[4] = {64, across ? 64u : 128u, across ? 2u : 1u, (cuuint32_t)box_planes}, one[4] = {1, 1, 1, 1};
-  const CUresult r = enc(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, base, dim, stride, box, one,
-                         CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-  return r == CUDA_SUCCESS ? BRACE_OK : cuda_fail_no_ctx(cudaErrorInvalidValue);
-}
-
-// The maps of a call: X's two buffers, S, T and P, along [0] and across [1].
-struct OrthoMaps {
-  CUtensorMap x[2][2], s[2], t[2], p[2];
+// A matrix of operand planes in the workspace and its tensor maps, made when a launch first needs them: [planes of all
+// matrices][rows][ld] float16 as blocks of 64 columns; a box holds the planes of `span` rows of a block (along) or of
+// 64 rows of span / 64 blocks (across); 128-byte swizzle, zeros outside.
+struct Operand {
+  void* base;
+  int64_t rows, ld, z;
+  int planes;
+  CUtensorMap map[2][2];   // [across][span 64 or 128]
+  bool made[2][2];
+  const CUtensorMap* get(bool across, int span) {
+    const int s = span == 128;
+    if (!made[across][s]) {
+      EncodeFn enc = encode_fn();
+      if (!enc) return nullptr;
+      const cuuint64_t dim[4] = {64, (cuuint64_t)rows, (cuuint64_t)(ld / 64), (cuuint64_t)z};
+      const cuuint64_t stride[3] = {(cuuint64_t)ld * 2, 128, (cuuint64_t)ld * 2 * (cuuint64_t)rows};
+      const cuuint32_t box[4] = {64, across ? 64u : (cuuint32_t)span, across ? (cuuint32_t)span / 64 : 1u, (cuuint32_t)planes};
+      const cuuint32_t one[4] = {1, 1, 1, 1};
+      if (enc(&map[across][s], CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, base, dim, stride, box, one,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+        return nullptr;
+      made[across][s] = true;
+    }
+    return &map[across][s];
+  }
 };
 
-template <int CG, int NP, int OP_A, int OP_B, int MODE, typename TOUT, int KS>
-cudaError_t launch_gemm_as(const CUtensorMap (&a)[2], const CUtensorMap (&b)[2], const GemmArgs& g, cudaStream_t st) {
-  using Shape = GemmShape<CG, NP>;
-  auto* kernel = ortho_gemm_kernel<CG, NP, OP_A, OP_B, MODE, TOUT, KS>;
-  GemmMaps maps;   // first the one that the operand needs (a symmetric one needs both)
-  maps.a[0] = a[OP_A == kAcross];
-  maps.a[1] = a[1];
-  maps.b[0] = b[OP_B == kAcross];
-  maps.b[1] = b[1];
+template <int CG, int TN, int NP, int OP_A, int OP_B, int MODE, typename TOUT, int KS>
+cudaError_t launch_gemm_as(Operand& a, Operand& b, const GemmArgs& g, cudaStream_t st) {
+  using Shape = GemmShape<CG, TN, NP>;
+  auto* kernel = ortho_gemm_kernel<CG, TN, NP, OP_A, OP_B, MODE, TOUT, KS>;
+  GemmMaps maps = {};   // first the one that the operand needs (a symmetric one needs both)
+  auto put = [](CUtensorMap* to, Operand& x, int op, int span) {
+    const CUtensorMap* first = x.get(op == kAcross, span);
+    const CUtensorMap* second = op == kSymmetric ? x.get(true, span) : first;
+    if (!first || !second) return false;
+    to[0] = *first;
+    to[1] = *second;
+    return true;
+  };
+  if (!put(maps.a, a, OP_A, 128) || !put(maps.b, b, OP_B, TN / CG)) return cudaErrorNotSupported;
   static std::atomic<uint64_t> granted{0};   // devices on which this kernel may use its shared memory
   int dev = 0;
   cudaError_t err = cudaGetDevice(&dev);
@@ -221,13 +234,14 @@ cudaError_t launch_gemm_as(const CUtensorMap (&a)[2], const CUtensorMap (&b)[2],
 // exchange and saves its part of the stages (0.2 us each, 0.65 with two planes): 512 x 2048 in float32 259 -> 182 us.
 // All clusters have to run at once, and one of 4 CTAs lies within a group of SMs that the hardware wires together: 28
 // always find room, 36 did not (1024 x 1024 took 210 us for 119).
-int split_of(int tiles, int kblocks, int planes) {
+constexpr double kSplitCost = 2.0;
+int split_of(int64_t tiles, int kblocks, int planes) {
   const double stage = planes == 1 ? 0.2 : 0.65;
   int best = 1;
   double least = kblocks * stage;
   for (int ks = 2; ks <= 4; ks *= 2) {
     if (tiles * ks > (ks == 2 ? sm_count() * 7 / 8 : sm_count() * 3 / 4) || kblocks < ks) break;
-    const double t = (kblocks + ks - 1) / ks * stage + 2.0;
+    const double t = (kblocks + ks - 1) / ks * stage + kSplitCost;
     if (t < least) {
       least = t;
       best = ks;
@@ -236,27 +250,40 @@ int split_of(int tiles, int kblocks, int planes) {
   return best;
 }
 
-template <int CG, int NP, int OP_A, int OP_B, int MODE, typename TOUT = __half>
-cudaError_t launch_gemm(const CUtensorMap (&a)[2], const CUtensorMap (&b)[2], const GemmArgs& g, cudaStream_t st) {
+template <int CG, int TN, int NP, int OP_A, int OP_B, int MODE, typename TOUT = __half>
+cudaError_t launch_gemm(Operand& a, Operand& b, const GemmArgs& g, cudaStream_t st) {
   if constexpr (CG == 1) {
     switch (split_of(g.total, (g.K + kTileK - 1) / kTileK, NP)) {
-      case 4: return launch_gemm_as<CG, NP, OP_A, OP_B, MODE, TOUT, 4>(a, b, g, st);
-      case 2: return launch_gemm_as<CG, NP, OP_A, OP_B, MODE, TOUT, 2>(a, b, g, st);
+      case 4: return launch_gemm_as<CG, TN, NP, OP_A, OP_B, MODE, TOUT, 4>(a, b, g, st);
+      case 2: return launch_gemm_as<CG, TN, NP, OP_A, OP_B, MODE, TOUT, 2>(a, b, g, st);
     }
   }
-  return launch_gemm_as<CG, NP, OP_A, OP_B, MODE, TOUT, 1>(a, b, g, st);
+  return launch_gemm_as<CG, TN, NP, OP_A, OP_B, MODE, TOUT, 1>(a, b, g, st);
 }
 
-template <int CG, int NP>
-cudaError_t launch_products(const OrthoPlan& q, const brace_ortho_params* p, char* ws, const OrthoMaps& maps,
+template <int CG, int TN, int NP>
+cudaError_t launch_products(const OrthoPlan& q, const brace_ortho_params* p, char* ws,
                             const GemmArgs& last, int out_type, cudaStream_t st) {
-  constexpr int T = GemmShape<CG, NP>::kTile;
+  constexpr int TM = GemmShape<CG, TN, NP>::kRows;
   const bool tall = q.rows > q.cols;
-  const int tm = (q.m + T - 1) / T;
+  const int64_t z = (int64_t)q.batch * q.planes;
+  Operand xs[2] = {}, s = {}, t = {}, poly = {};
+  auto place = [&](Operand& x, size_t off, int64_t rows, int64_t ld) {
+    x.base = ws + off;
+    x.rows = rows;
+    x.ld = ld;
+    x.z = z;
+    x.planes = q.planes;
+  };
+  place(xs[0], q.off_x[0], q.rows, q.ld_x);
+  place(xs[1], q.off_x[1], q.rows, q.ld_x);
+  place(s, q.off_s, q.m, q.ld_s);
+  place(t, q.off_t, q.m, q.ld_s);
+  place(poly, q.off_p, q.m, q.ld_s);
+  const int tm = (q.m + TM - 1) / TM;
   GemmArgs sym = {};
   sym.M = sym.N = q.m;
-  sym.tiles_n = tm;
-  sym.tiles = tm * (tm + 1) / 2;
+  sym.tiles = TM / TN * (tm * (tm + 1) / 2);
   sym.total = sym.tiles * q.batch;
   sym.ld_dst = q.ld_s;
   sym.chunk = q.m >= kLongChunkFrom ? 2 : 1;
@@ -265,8 +292,8 @@ cudaError_t launch_products(const OrthoPlan& q, const brace_ortho_params* p, cha
   step.M = q.rows;
   step.N = q.cols;
   step.K = q.m;
-  step.tiles_n = (q.cols + T - 1) / T;
-  step.tiles = step.tiles_n * ((q.rows + T - 1) / T);
+  step.tiles_n = (q.cols + TN - 1) / TN;
+  step.tiles = step.tiles_n * ((q.rows + TM - 1) / TM);
   step.total = step.tiles * q.batch;
   step.ld_dst = q.ld_x;
   step.chunk = sym.chunk;
@@ -274,7 +301,7 @@ cudaError_t launch_products(const OrthoPlan& q, const brace_ortho_params* p, cha
   step.status = (int*)ws;
   for (int k = 0; k < p->steps; ++k) {
     const int cur = k & 1;
-    const CUtensorMap(&x)[2] = maps.x[cur];
+    Operand& x = xs[cur];
     GemmArgs g = sym;
     g.K = tall ? q.rows : q.cols;
     g.scale = kGramScale;
@@ -282,8 +309,8 @@ cudaError_t launch_products(const OrthoPlan& q, const brace_ortho_params* p, cha
     g.dst2 = (__half*)(ws + q.off_t);
     g.scale2 = p->c * kFromGram;
     g.diagonal2 = p->b * kSquareScale;
-    cudaError_t err = tall ? launch_gemm<CG, NP, kAcross, kAcross, kModeGram>(x, x, g, st)
-                           : launch_gemm<CG, NP, kAlong, kAlong, kModeGram>(x, x, g, st);
+    cudaError_t err = tall ? launch_gemm<CG, TN, NP, kAcross, kAcross, kModeGram>(x, x, g, st)
+                           : launch_gemm<CG, TN, NP, kAlong, kAlong, kModeGram>(x, x, g, st);
     if (err != cudaSuccess) return err;
     g = sym;
     g.K = q.m;
@@ -296,36 +323,40 @@ cudaError_t launch_products(const OrthoPlan& q, const brace_ortho_params* p, cha
     }
     g.diagonal = p->a * kSquareScale;
     g.dst = (__half*)(ws + q.off_p);
-    err = launch_gemm<CG, NP, kSymmetric, kSymmetric, kModePoly>(maps.s, NP == 2 ? maps.t : maps.s, g, st);
+    err = launch_gemm<CG, TN, NP, kSymmetric, kSymmetric, kModePoly>(s, NP == 2 ? t : s, g, st);
     if (err != cudaSuccess) return err;
     step.dst = (__half*)(ws + q.off_x[cur ^ 1]);
     if (k + 1 < p->steps)
-      err = tall ? launch_gemm<CG, NP, kAlong, kSymmetric, kModeStep>(x, maps.p, step, st)
-                 : launch_gemm<CG, NP, kSymmetric, kAcross, kModeStep>(maps.p, x, step, st);
+      err = tall ? launch_gemm<CG, TN, NP, kAlong, kSymmetric, kModeStep>(x, poly, step, st)
+                 : launch_gemm<CG, TN, NP, kSymmetric, kAcross, kModeStep>(poly, x, step, st);
     else
       err = with_type(out_type, [&](auto t) {
         using TOUT = decltype(t);
-        return tall ? launch_gemm<CG, NP, kAlong, kSymmetric, kModeLast, TOUT>(x, maps.p, step, st)
-                    : launch_gemm<CG, NP, kSymmetric, kAcross, kModeLast, TOUT>(maps.p, x, step, st);
+        return tall ? launch_gemm<CG, TN, NP, kAlong, kSymmetric, kModeLast, TOUT>(x, poly, step, st)
+                    : launch_gemm<CG, TN, NP, kSymmetric, kAcross, kModeLast, TOUT>(poly, x, step, st);
       });
     if (err != cudaSuccess) return err;
   }
   return cudaSuccess;
 }
 
-// Time of a step's three products in microseconds, tiles of 128 (cg = 1) or of 256 by pairs of CTAs (cg = 2): waves of
-// tiles times the stages of one, and what a launch takes beside them.  A pair does four times the work of a single CTA
-// in 1.5 times the time (0.40 against 0.27 us a stage; with two planes 1.27 against 0.82), but has to find that many
-// tiles: at 4096 x 4096 it takes 1.04 ms against 1.32, at 2048 x 2048 0.28 against 0.24.
-double tiled_cost(const OrthoPlan& q, int cg) {
-  const int tile = 128 * cg, slots = sm_count() / cg;
-  const int64_t tm = (q.m + tile - 1) / tile, tr = (q.rows + tile - 1) / tile, tc = (q.cols + tile - 1) / tile;
-  const int n = q.rows < q.cols ? q.cols : q.rows;
-  auto waves = [&](int64_t tiles) { return (double)((tiles * q.batch + slots - 1) / slots); };
-  const double stages = waves(tm * (tm + 1) / 2) * ((n + 63) / 64 + (q.m + 63) / 64) + waves(tr * tc) * ((q.m + 63) / 64);
-  const double stage = cg == 1 ? (q.planes == 1 ? 0.27 : 0.82) : (q.planes == 1 ? 0.40 : 1.27);
-  const double fixed = cg == 1 ? (q.planes == 1 ? 4.0 : 6.0) : (q.planes == 1 ? 6.5 : 10.0);
-  return stages * stage + 3 * fixed;
+// Microseconds of a step's three products with tiles of 128 x 128 (shape 0), 256 x 128 (1) or 256 x 256 (2), the last
+// two by pairs of CTAs: waves of tiles times the stages of one, and what a launch takes beside them.  Fitted to 17 sizes
+// from 200 x 200 to 4096 x 4096, off by at most a sixth.  Both sides, one plane: at 512 x 512 shape 0 takes 91 us and 2
+// takes 137, at 4096 x 4096 1.37 ms and 1.04; two planes: at 1500 x 1500 shape 0 takes 329 us and 1 takes 291.
+double tiled_cost(const OrthoPlan& q, int shape) {
+  static const double kStage[2][3] = {{0.272, 0.239, 0.345}, {0.709, 0.669, 1.15}};
+  static const double kFixed[2][3] = {{3.35, 4.1, 5.8}, {5.4, 5.0, 8.7}};
+  const int tm = shape == 0 ? 128 : 256, tn = shape == 2 ? 256 : 128, slots = sm_count() / (shape == 0 ? 1 : 2);
+  const int64_t sym = (q.m + tm - 1) / tm, tr = (q.rows + tm - 1) / tm, tc = (q.cols + tn - 1) / tn;
+  auto product = [&](int64_t tiles, int contraction) {
+    const int64_t kb = (contraction + kTileK - 1) / kTileK;
+    const int ks = shape == 0 ? split_of(tiles, (int)kb, q.planes) : 1;
+    const double stages = ks > 1 ? (double)((kb + ks - 1) / ks) : (double)((tiles + slots - 1) / slots * kb);
+    return stages * kStage[q.planes - 1][shape] + (ks > 1 ? kSplitCost : 0.0) + kFixed[q.planes - 1][shape];
+  };
+  const int64_t half = tm / tn * (sym * (sym + 1) / 2) * q.batch;
+  return product(half, q.rows < q.cols ? q.cols : q.rows) + product(half, q.m) + product(tr * tc * q.batch, q.m);
 }
 
 cudaError_t launch_prep(const OrthoPlan& q, const PrepArgs& a, cudaStream_t st) {
@@ -431,26 +462,19 @@ int run_ortho(const OrthoPlan& q, const brace_ortho_params* p, PrepArgs prep, co
     const cudaError_t e = q.planes == 1 ? launch_resident<1>(r, ctas, st) : launch_resident<2>(r, ctas, st);
     return e == cudaSuccess ? BRACE_OK : cuda_fail_no_ctx(e);
   }
-  OrthoMaps maps;
-  const int64_t z = (int64_t)q.batch * q.planes;
-  for (int across = 0; across < 2; ++across) {
-    int rc = BRACE_OK;
-    for (int i = 0; i < 2 && rc == BRACE_OK; ++i)
-      rc = make_map(&maps.x[i][across], ws + q.off_x[i], q.rows, q.ld_x, z, q.planes, across);
-    if (rc == BRACE_OK) rc = make_map(&maps.s[across], ws + q.off_s, q.m, q.ld_s, z, q.planes, across);
-    if (rc == BRACE_OK && q.planes == 2) rc = make_map(&maps.t[across], ws + q.off_t, q.m, q.ld_s, z, q.planes, across);
-    if (rc == BRACE_OK) rc = make_map(&maps.p[across], ws + q.off_p, q.m, q.ld_s, z, q.planes, across);
-    if (rc != BRACE_OK) return rc;
-  }
   cudaError_t err = launch_prep(q, prep, st);
   if (err == cudaSuccess) {
-    const bool pairs = tiled_cost(q, 2) < tiled_cost(q, 1);
-    if (pairs)
-      err = q.planes == 1 ? launch_products<2, 1>(q, p, ws, maps, last, out_type, st)
-                          : launch_products<2, 2>(q, p, ws, maps, last, out_type, st);
+    int shape = 0;
+    for (int i = 1; i < 3; ++i)
+      if (tiled_cost(q, i) < tiled_cost(q, shape)) shape = i;
+    if (q.planes == 1)
+      err = shape == 2   ? launch_products<2, 256, 1>(q, p, ws, last, out_type, st)
+            : shape == 1 ? launch_products<2, 128, 1>(q, p, ws, last, out_type, st)
+                         : launch_products<1, 128, 1>(q, p, ws, last, out_type, st);
     else
-      err = q.planes == 1 ? launch_products<1, 1>(q, p, ws, maps, last, out_type, st)
-                          : launch_products<1, 2>(q, p, ws, maps, last, out_type, st);
+      err = shape == 2   ? launch_products<2, 256, 2>(q, p, ws, last, out_type, st)
+            : shape == 1 ? launch_products<2, 128, 2>(q, p, ws, last, out_type, st)
+                         : launch_products<1, 128, 2>(q, p, ws, last, out_type, st);
   }
   return err == cudaSuccess ? BRACE_OK : cuda_fail_no_ctx(err);
 }
@@ -702,6 +726,7 @@ int brace_orthogonalize(int32_t batch, int32_t rows, int32_t cols, const brace_o
   last.ld_out = ld_out;
   last.batch_out = stride_out;
   last.vec_out = wide_rows(d_out, out_type, ld_out, stride_out);
+  last.vec_in = 1;   // there is none
   last.replicas = 1;
   return run_ortho(q, params, prep, last, out_type, (char*)d_workspace, (cudaStream_t)stream);
 }

@@ -246,29 +246,32 @@ constexpr int kCellBytes = 2048;                 // a warp's staging of the epil
 
 // An operand's tensor map(s), each with boxes that fill a stage's operand, all planes, in one load: the cost of a
 // load is some 46 clocks and 2 for each 128 bytes (measured: 59 bytes a clock with 256 rows, 48 with 64).
-//   along: 128 rows of one block of 64 columns;  across: 64 rows of two blocks.
+//   along: 128 (64) rows of one block of 64 columns;  across: 64 rows of two blocks (one).
 // A symmetric operand has both.
 struct GemmMaps {
   CUtensorMap a[2], b[2];
 };
 
-template <int CG, int NP>
+// Tiles of 128 CG rows and TN columns by CG CTAs.
+template <int CG, int TN, int NP>
 struct GemmShape {
-  static constexpr int kTile = 128 * CG;                     // square tiles
-  static constexpr int kEpiWarps = 8 * CG;                   // a warp takes 32 rows x 64 columns of the CTA's part
+  static constexpr int kRows = 128 * CG;
+  static constexpr int kEpiWarps = TN / 16;                  // a warp takes 32 rows x 64 columns of the CTA's part
   static constexpr int kThreads = 128 + 32 * kEpiWarps;      // warps 0-3: loads, MMAs, tensor memory, -; then epilogue
-  static constexpr int kStageBytes = 2 * NP * kOperandBytes;
-  static constexpr int kStages = NP == 1 ? 6 : 3;            // 192 KB either way
-  static constexpr int kBuffers = 512 / kTile;               // accumulators in tensor memory: all of its 512 columns
+  static constexpr int kBytesB = TN / CG * kTileK * 2;       // each CTA of a pair loads half of the columns' operand
+  static constexpr int kStageBytes = NP * (kOperandBytes + kBytesB);
+  static constexpr int kStages = 192 * 1024 / kStageBytes;
+  static constexpr int kBuffers = 512 / TN;                  // accumulators in tensor memory: all of its 512 columns
   static constexpr int kSmem = kStages * kStageBytes + kEpiWarps * kCellBytes + 1024 + 256;
 };
 
-// Blocks of the lower triangle in rows: t -> (row, col), col <= row.
-__device__ __forceinline__ void triangle(int t, int& row, int& col) {
-  row = (int)((sqrtf(8.f * (float)t + 1.f) - 1.f) * 0.5f);
-  while ((row + 1) * (row + 2) / 2 <= t) ++row;
-  while (row * (row + 1) / 2 > t) --row;
-  col = t - row * (row + 1) / 2;
+// Tiles on and below the diagonal, row by row, `per` columns of tiles to a row of tiles: t -> (row, col).
+__device__ __forceinline__ void triangle(int t, int per, int& row, int& col) {
+  const int u = t / per;
+  row = (int)((sqrtf(8.f * (float)u + 1.f) - 1.f) * 0.5f);
+  while ((row + 1) * (row + 2) / 2 <= u) ++row;
+  while (row * (row + 1) / 2 > u) --row;
+  col = t - per * (row * (row + 1) / 2);
 }
 
 // A warp's cell: 32 rows of four 16-byte words.  A lane writes (reads) its own row, and reads (writes) rows of 4
@@ -364,38 +367,53 @@ __device__ __forceinline__ void last_cell(const GemmArgs& p, uint32_t cell, int6
   __syncwarp();
   const int col = col0 + (lane & 3) * 4, n = min(4, p.N - col);
   if (n <= 0) return;
+  const int r0 = lane >> 2;
+  if (p.vec_out && p.vec_in && n == 4 && row0 + 32 <= p.M) {
+    for (int k = 0; k < p.replicas; ++k) {
+      T* out = (T*)p.out + b * p.batch_out + k * p.rep_out + (int64_t)(row0 + r0) * p.ld_out + col;
+      Pack<T, 4> y[4];
+      if (p.w_in) {
+        // plain loads: in and out may be the same buffer
+        const T* in = (const T*)p.w_in + b * p.batch_in + k * p.rep_in + (int64_t)(row0 + r0) * p.ld_in + col;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i].load_plain(in + i * 8 * p.ld_in);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint4 t = lds16(cell_at(cell, i * 8 + r0, lane & 3));
+        const float o[4] = {__uint_as_float(t.x), __uint_as_float(t.y), __uint_as_float(t.z), __uint_as_float(t.w)};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) y[i].t[j] = from_f32<T>(p.w_in ? p.keep * to_f32(y[i].t[j]) - p.rate * o[j] : o[j]);
+        y[i].store_plain(out + i * 8 * p.ld_out);
+      }
+    }
+    return;
+  }
 #pragma unroll 1
   for (int i = 0; i < 4; ++i) {
-    const int r = i * 8 + (lane >> 2), row = row0 + r;
+    const int r = i * 8 + r0, row = row0 + r;
     if (row >= p.M) break;
     const uint4 t = lds16(cell_at(cell, r, lane & 3));
     const float o[4] = {__uint_as_float(t.x), __uint_as_float(t.y), __uint_as_float(t.z), __uint_as_float(t.w)};
     for (int k = 0; k < p.replicas; ++k) {
       T* out = (T*)p.out + b * p.batch_out + k * p.rep_out + (int64_t)row * p.ld_out + col;
-      Pack<T, 4> y;
-      if (p.w_in) {
-        // plain loads: in and out may be the same buffer
-        const T* in = (const T*)p.w_in + b * p.batch_in + k * p.rep_in + (int64_t)row * p.ld_in + col;
-        if (p.vec_in && n == 4) {
-          y.load_plain(in);
-        } else {
+      const T* in = (const T*)p.w_in + b * p.batch_in + k * p.rep_in + (int64_t)row * p.ld_in + col;
 #pragma unroll
-          for (int j = 0; j < 4; ++j) y.t[j] = j < n ? in[j] : from_f32<T>(0.f);
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) y.t[j] = from_f32<T>(p.keep * to_f32(y.t[j]) - p.rate * o[j]);
-      } else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) y.t[j] = from_f32<T>(o[j]);
-      }
-      if (p.vec_out && n == 4) {
-        y.store_plain(out);
-      } else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-          if (j < n) out[j] = y.t[j];
-      }
+      for (int j = 0; j < 4; ++j)
+        if (j < n) out[j] = from_f32<T>(p.w_in ? p.keep * to_f32(in[j]) - p.rate * o[j] : o[j]);
     }
+  }
+}
+
+// Asks for the weights that a lane's row of `cols` columns will be added to, while the products still run.
+template <typename T>
+__device__ __forceinline__ void prefetch_weights(const GemmArgs& p, int64_t b, int row, int col, int cols) {
+  const int n = min(cols, p.N - col);
+  if (!p.w_in || row >= p.M || n <= 0) return;
+  for (int k = 0; k < p.replicas; ++k) {
+    const T* in = (const T*)p.w_in + b * p.batch_in + k * p.rep_in + (int64_t)row * p.ld_in + col;
+    for (int j = 0; j < n; j += 128 / (int)sizeof(T)) asm volatile("prefetch.global.L2 [%0];" ::"l"(in + j));
+    asm volatile("prefetch.global.L2 [%0];" ::"l"(in + n - 1));
   }
 }
 
@@ -431,15 +449,15 @@ __device__ __forceinline__ void finish_block(const GemmArgs& p, uint32_t cell, i
   }
 }
 
-// One product of the iteration over tiles of 128 x 128 (CG = 1) or, by a pair of CTAs, 256 x 256 (CG = 2), NP planes
+// One product of the iteration over tiles of 128 x 128 (CG = 1) or, by a pair of CTAs, 256 x TN (CG = 2), NP planes
 // per operand.  Warp 0 loads, warp 1 issues the matrix instructions, warp 2 owns the tensor memory, warps 4.. read the
 // accumulators and write the results; persistent over tiles, so that the epilogue of a tile runs under the products
 // of the next.
-template <int CG, int NP, int OP_A, int OP_B, int MODE, typename TOUT, int KS>
-__global__ void __launch_bounds__(GemmShape<CG, NP>::kThreads, 1)
+template <int CG, int TN, int NP, int OP_A, int OP_B, int MODE, typename TOUT, int KS>
+__global__ void __launch_bounds__(GemmShape<CG, TN, NP>::kThreads, 1)
     ortho_gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmArgs p) {
-  using Shape = GemmShape<CG, NP>;
-  constexpr int T = Shape::kTile, STAGES = Shape::kStages, BUFS = Shape::kBuffers;
+  using Shape = GemmShape<CG, TN, NP>;
+  constexpr int TM = Shape::kRows, STAGES = Shape::kStages, BUFS = Shape::kBuffers;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t base = (smem_addr(smem_raw) + 1023u) & ~1023u;
   const uint32_t cells = base + STAGES * Shape::kStageBytes;
@@ -484,17 +502,18 @@ __global__ void __launch_bounds__(GemmShape<CG, NP>::kThreads, 1)
     b = tile / p.tiles;
     const int t = tile - b * p.tiles;
     if (MODE == kModeGram || MODE == kModePoly) {
-      triangle(t, ti, tj);
+      triangle(t, TM / TN, ti, tj);
     } else {
       ti = t / p.tiles_n;
       tj = t - ti * p.tiles_n;
     }
   };
-  // whether the operand of tile row `t` lies across the contraction in stage kb
-  auto across = [](int op, int t, int kb) { return op == kAcross || (op == kSymmetric && t < kb * kTileK / T); };
+  // whether the operand from row `row` on lies across the contraction in stage kb: of a symmetric one the blocks of TM
+  // rows up to the diagonal block are stored
+  auto across = [](int op, int row, int kb) { return op == kAcross || (op == kSymmetric && kb * kTileK >= (row / TM + 1) * TM); };
 
   // the launch's registers (640 threads x 96) go to the warps that hold accumulators: 4 x 32 x 32 + 16 x 32 x 112
-  if (CG == 2 && warp < 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 32;");
+  if (TN == 256 && warp < 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 32;");
   float acc[NP == 1 && KS == 1 ? 32 : 64];
   if (warp == 0) {
     const bool lead = elect_one();
@@ -505,14 +524,14 @@ __global__ void __launch_bounds__(GemmShape<CG, NP>::kThreads, 1)
     for (int tile = cluster; ok && tile < p.total; tile += clusters) {
       int b, ti, tj;
       place(tile, b, ti, tj);
-      const int ra = ti * T + (int)rank * 128, rb = tj * T + (int)rank * 128;
+      const int ra = ti * TM + (int)rank * 128, rb = tj * TN + (int)rank * (TN / CG);
       for (int kb = kfirst; kb < kblocks; ++kb) {
         if (!mbar_wait(empty + 8 * s, ph ^ 1u, dead)) {
           ok = false;
           break;
         }
         const uint32_t st = base + s * Shape::kStageBytes, bar = full0 + 8 * s;
-        const bool a_across = across(OP_A, ti, kb), b_across = across(OP_B, tj, kb);
+        const bool a_across = across(OP_A, ti * TM, kb), b_across = across(OP_B, tj * TN, kb);
         // the tensors as blocks of 64 columns: (column in the block, row, block, plane)
         const CUtensorMap* ma = &maps.a[OP_A == kSymmetric && a_across ? 1 : 0];
         const CUtensorMap* mb = &maps.b[OP_B == kSymmetric && b_across ? 1 : 0];
@@ -549,7 +568,7 @@ __global__ void __launch_bounds__(GemmShape<CG, NP>::kThreads, 1)
             break;
           }
           tc_fence_after();
-          const uint32_t d = tmem + buf * T;
+          const uint32_t d = tmem + buf * TN;
           const int kend = NP == 1 ? kblocks : min(kblocks, kb + p.chunk);
           for (uint32_t add = 0; kb < kend; ++kb) {
             if (!mbar_wait(full + 8 * s, ph, dead)) {
@@ -557,19 +576,19 @@ __global__ void __launch_bounds__(GemmShape<CG, NP>::kThreads, 1)
               break;
             }
             tc_fence_after();
-            const bool a_across = across(OP_A, ti, kb), b_across = across(OP_B, tj, kb);
-            const uint32_t idesc = f16_idesc(128 * CG, 128 * CG, a_across, b_across);
+            const bool a_across = across(OP_A, ti * TM, kb), b_across = across(OP_B, tj * TN, kb);
+            const uint32_t idesc = f16_idesc(TM, TN, a_across, b_across);
             // per 16 of the contraction: 32 bytes along a swizzled row, or 16 rows of 128 bytes
             const uint64_t step_a = (a_across ? 2048 : 32) >> 4, step_b = (b_across ? 2048 : 32) >> 4;
             const uint64_t da = desc0 + (uint64_t)(s * Shape::kStageBytes >> 4), db = da + (NP * kOperandBytes >> 4);
-            constexpr uint64_t lo = kOperandBytes >> 4;   // the second plane
+            constexpr uint64_t lo_a = kOperandBytes >> 4, lo_b = Shape::kBytesB >> 4;   // the second plane
             if (lead) {
               if (kb + 1 < kall) {
 #pragma unroll
                 for (int k = 0; k < kTileK / 16; ++k) {
                   if (NP == 2) {   // the small terms first: what is cut off goes by the accumulators' size
-                    mma_f16<CG>(d, da + lo + k * step_a, db + k * step_b, idesc, k ? 1 : add);
-                    mma_f16<CG>(d, da + k * step_a, db + lo + k * step_b, idesc, 1);
+                    mma_f16<CG>(d, da + lo_a + k * step_a, db + k * step_b, idesc, k ? 1 : add);
+                    mma_f16<CG>(d, da + k * step_a, db + lo_b + k * step_b, idesc, 1);
                   }
                 }
 #pragma unroll
@@ -580,8 +599,8 @@ __global__ void __launch_bounds__(GemmShape<CG, NP>::kThreads, 1)
 #pragma unroll 1
                 for (int k = 0; k < steps; ++k) {
                   if (NP == 2) {
-                    mma_f16<CG>(d, da + lo + k * step_a, db + k * step_b, idesc, k ? 1 : add);
-                    mma_f16<CG>(d, da + k * step_a, db + lo + k * step_b, idesc, 1);
+                    mma_f16<CG>(d, da + lo_a + k * step_a, db + k * step_b, idesc, k ? 1 : add);
+                    mma_f16<CG>(d, da + k * step_a, db + lo_b + k * step_b, idesc, 1);
                   }
                 }
 #pragma unroll 1
@@ -608,7 +627,7 @@ __global__ void __launch_bounds__(GemmShape<CG, NP>::kThreads, 1)
       }
     }
   } else if (warp >= 4) {
-    if (CG == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 112;");
+    if (TN == 256) asm volatile("setmaxnreg.inc.sync.aligned.u32 112;");
     const uint32_t tm_empty0 = CG == 1 ? tm_empty : map_to_rank(tm_empty, 0);
     const int quarter = warp & 3;                          // the 32 lanes of tensor memory this warp can read
     const int cols0 = ((warp - 4) >> 2) * 64;
@@ -634,10 +653,11 @@ __global__ void __launch_bounds__(GemmShape<CG, NP>::kThreads, 1)
     for (int tile = cluster; ok && tile < p.total; tile += clusters) {
       int b, ti, tj;
       place(tile, b, ti, tj);
-      const int row0 = ti * T + (int)rank * 128 + quarter * 32, col0 = tj * T + cols0;
+      const int row0 = ti * TM + (int)rank * 128 + quarter * 32, col0 = tj * TN + cols0;
       const int rows = min(32, p.M - row0);   // may be none: the accumulators are then read for nothing
       // rows are padded to 64 columns; the pad is written too (the operands' pads are zeros, so it stays zero)
       const bool live = rows > 0 && col0 < p.N;
+      if (MODE == kModeLast) prefetch_weights<TOUT>(p, b, row0 + lane, col0, 64);
       uint4 x0[4], x1[4];
       if (MODE == kModePoly && NP == 1 && KS == 1 && live) {
         const __half* src = p.src + b * p.M * p.ld_dst + (int64_t)row0 * p.ld_dst + col0;
@@ -654,7 +674,7 @@ __global__ void __launch_bounds__(GemmShape<CG, NP>::kThreads, 1)
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
             float v[16];
-            tmem_load16(tm_mine + buf * T + 16 * q, v);
+            tmem_load16(tm_mine + buf * TN + 16 * q, v);
 #pragma unroll
             for (int i = 0; i < 16; ++i) acc[(16 * q + i) & (NP * 32 - 1)] = (kb > kfirst ? acc[(16 * q + i) & (NP * 32 - 1)] : 0.f) + v[i];
           }
@@ -666,27 +686,28 @@ __global__ void __launch_bounds__(GemmShape<CG, NP>::kThreads, 1)
         tc_fence_after();
       }
       if (!ok) break;
-      if (KS > 1) {
+      if constexpr (KS > 1) {
         if (NP == 1) {
 #pragma unroll
           for (int h = 0; h < 2; ++h)
-            tmem_load32(tm_mine + buf * T + 32 * h, *reinterpret_cast<float(*)[32]>(acc + (KS > 1 ? 32 * h : 0)));
+            tmem_load32(tm_mine + buf * TN + 32 * h, *reinterpret_cast<float(*)[32]>(acc + 32 * h));
         }
         break;   // one tile; it is finished below
-      }
+      } else {
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        float* v = acc + (NP == 1 ? 0 : 32 * h);
-        if (NP == 1) {
-          tmem_load32(tm_mine + buf * T + 32 * h, *reinterpret_cast<float(*)[32]>(v));
-          if (h == 1) release();
+        for (int h = 0; h < 2; ++h) {
+          float* v = acc + (NP == 1 ? 0 : 32 * h);
+          if (NP == 1) {
+            tmem_load32(tm_mine + buf * TN + 32 * h, *reinterpret_cast<float(*)[32]>(v));
+            if (h == 1) release();
+          }
+          if (live) finish_block<NP, MODE, TOUT>(p, cell, b, row0, col0 + 32 * h, rows, h == 0 ? x0 : x1, v);
         }
-        if (live) finish_block<NP, MODE, TOUT>(p, cell, b, row0, col0 + 32 * h, rows, h == 0 ? x0 : x1, v);
       }
     }
     if (KS == 1) fence_async_global();
   }
-  if (KS > 1) {
+  if constexpr (KS > 1) {
     int b, ti, tj;
     place(cluster, b, ti, tj);
     const int quarter = warp & 3, cols0 = ((warp - 4) >> 2) * 64;
@@ -705,7 +726,7 @@ __global__ void __launch_bounds__(GemmShape<CG, NP>::kThreads, 1)
     constexpr int kBlocks = 4 / KS;   // blocks of 32 columns of this CTA's share
     const int block = (warp - 4) >> 2;
     if (warp >= 4 && block < kBlocks) {
-      const int row0 = ti * T + quarter * 32, col0 = tj * T + (part * kBlocks + block) * 32, rows = min(32, p.M - row0);
+      const int row0 = ti * TM + quarter * 32, col0 = tj * TN + (part * kBlocks + block) * 32, rows = min(32, p.M - row0);
       if (rows > 0 && col0 < ((p.N + 63) & ~63)) {
         uint4 x0[4];
         if (MODE == kModePoly && NP == 1)
