@@ -52,39 +52,55 @@ __device__ __forceinline__ int64_t load_id(const EmbArgs& p, int64_t c, int64_t 
 }
 
 // ---- lookup -----------------------------------------------------------------------------------------------------
-// A thread moves U groups of V elements, so that the loads of U rows are under way together.
-template <typename TI, typename TO, int V, int U>
+// A warp takes kLookupRows rows and of each a stretch of 32 V Q columns, all loads first.  Rows that do not start on
+// whole words are read and written element by element, 32 neighbours at a time.
+constexpr int kLookupRows = 4;
+
+template <typename TI, typename TO, int V>
 __global__ void __launch_bounds__(256) embedding_lookup_kernel(const EmbArgs p) {
+  constexpr int Q = V >= 8 ? 1 : V == 2 ? 2 : 4, R = kLookupRows;
   grid_wait();
   grid_trigger();
-  const uint32_t groups = (uint32_t)(p.dim / V);
-  const int64_t c = blockIdx.y;
-  const uint64_t total = (uint64_t)p.tokens * groups;
-  uint64_t u = (uint64_t)blockIdx.x * (256 * U) + threadIdx.x;
-  Pack<TI, V> x[U];
-  bool live[U], hit[U];
-  TO* to[U];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int64_t c = blockIdx.y, t0 = ((int64_t)blockIdx.x * 8 + warp) * R;
+  const int rows = (int)min((int64_t)R, p.tokens - t0);
+  if (rows <= 0) return;
+  const int col = (int)blockIdx.z * (32 * V * Q) + lane * V, left = p.dim - col;
+  // lane r knows row r's id; what is no token is -1
+  int64_t id = -1;
+  if (lane < rows) {
+    id = load_id(p, c, t0 + lane);
+    if (id >= p.vocab) id = -1;
+  }
+  const TI* table = (const TI*)p.table + c * p.stride_table + col;
+  TO* out = (TO*)p.out + c * p.stride_act + t0 * p.ld_act + col;
+  Pack<TI, V> x[R][Q];
 #pragma unroll
-  for (int i = 0; i < U; ++i, u += 256) {
-    live[i] = u < total;
-    hit[i] = false;
-    if (live[i]) {
-      const int64_t t = (int64_t)(total >> 32 ? u / groups : (uint32_t)u / groups);
-      const int col = (int)(u - (uint64_t)t * groups) * V;
-      const int64_t id = load_id(p, c, t);
-      to[i] = (TO*)p.out + c * p.stride_act + t * p.ld_act + col;
-      hit[i] = id >= 0 && id < p.vocab;
-      if (hit[i]) x[i].load((const TI*)p.table + c * p.stride_table + id * p.ld_table + col);
+  for (int r = 0; r < R; ++r) {
+    const int64_t v = __shfl_sync(0xffffffffu, id, r);
+    const TI* row = table + v * p.ld_table;
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+      if (v >= 0 && 32 * V * q < left) {
+        x[r][q].load(row + 32 * V * q);
+      } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j) x[r][q].t[j] = from_f32<TI>(0.f);
+      }
     }
   }
 #pragma unroll
-  for (int i = 0; i < U; ++i)
-    if (live[i]) {
-      Pack<TO, V> y;
+  for (int r = 0; r < R; ++r) {
+    if (r >= rows) break;
 #pragma unroll
-      for (int j = 0; j < V; ++j) y.t[j] = from_f32<TO>(hit[i] ? to_f32(x[i].t[j]) * p.scale : 0.f);
-      y.store_stream(to[i]);
-    }
+    for (int q = 0; q < Q; ++q)
+      if (32 * V * q < left) {
+        Pack<TO, V> y;
+#pragma unroll
+        for (int j = 0; j < V; ++j) y.t[j] = from_f32<TO>(to_f32(x[r][q].t[j]) * p.scale);
+        y.store_stream(out + r * p.ld_act + 32 * V * q);
+      }
+  }
 }
 
 // ---- gradient: sort ---------------------------------------------------------------------------------------------
@@ -251,12 +267,13 @@ struct Share {
 #pragma unroll 1
     for (int i = 0; i < n; i += 2) {
       Pack<T, V> x[2][Q];
-      const T *p0 = at(i), *p1 = at(min(i + 1, n - 1));
+      const bool two = i + 1 < n;
+      const T *p0 = at(i), *p1 = two ? at(i + 1) : p0;
 #pragma unroll
       for (int q = 0; q < Q; ++q)
         if (32 * V * q < left) {
           x[0][q].load(p0 + 32 * V * q);
-          x[1][q].load(p1 + 32 * V * q);
+          if (two) x[1][q].load(p1 + 32 * V * q);
         }
 #pragma unroll
       for (int q = 0; q < Q; ++q)
@@ -264,7 +281,7 @@ struct Share {
 #pragma unroll
           for (int j = 0; j < V; ++j) {
             sum[q][j] += to_f32(x[0][q].t[j]);
-            if (i + 1 < n) sum[q][j] += to_f32(x[1][q].t[j]);
+            if (two) sum[q][j] += to_f32(x[1][q].t[j]);
           }
     }
   }
@@ -326,7 +343,7 @@ __global__ void __launch_bounds__(256, 6) embedding_sum_kernel(const EmbArgs p) 
     if (lane == 0) before = i > 0 ? key[i - 1] : kNoToken;
     if (lane == 31) after = i + 1 < p.tokens ? key[i + 1] : kNoToken;
     const bool token = k != kNoToken;
-    if (token) {
+    if (token) {   // (every CTA of a group writes the same)
       if (before != k) p.span[c * p.vocab + k].x = (uint32_t)i;
       if (after != k) p.span[c * p.vocab + k].y = (uint32_t)i + 1;
       s_key[lane] = k;
@@ -344,14 +361,19 @@ __global__ void __launch_bounds__(256, 6) embedding_sum_kernel(const EmbArgs p) 
   }
   __syncthreads();
   const int segments = s_segments, goes = s_goes;
-  const int blocks = (p.dim + S::kWide - 1) / S::kWide, tasks = segments * blocks;
+  // the row's columns are shared by gridDim.z CTAs
+  const int all = (p.dim + S::kWide - 1) / S::kWide, block0 = all * (int)blockIdx.z / (int)gridDim.z;
+  const int blocks = all * ((int)blockIdx.z + 1) / (int)gridDim.z - block0, tasks = segments * blocks;
   const int warps = tasks > 4 ? 1 : tasks > 2 ? 2 : tasks > 1 ? 4 : 8;   // per task; several: all tasks at once
   const TI* dy = (const TI*)p.in + c * p.stride_act;
-  for (int u0 = 0; u0 < tasks; u0 += 8 / warps) {
-    const int u = u0 + warp / warps, s = warp % warps;
+  const int s = warp & (warps - 1), stride = 8 / warps;
+  int q = 0, block = warp / warps;   // this warp's task: a segment and a stretch of its columns
+  for (int u0 = 0; u0 < tasks; u0 += stride, block += stride) {
+    const int u = u0 + warp / warps;
+    for (; block >= blocks; block -= blocks) ++q;
     S share;
     share.clear();
-    const int q = u / blocks, col = (u - q * blocks) * S::kWide + lane * V, left = p.dim - col;
+    const int col = (block0 + block) * S::kWide + lane * V, left = p.dim - col;
     if (u < tasks) {
       const int first = s_first[q], n = s_first[q + 1] - first, from = first + n * s / warps, to = first + n * (s + 1) / warps;
       share.template add<TI>(to - from, left, [&](int t) { return dy + (int64_t)s_pos[from + t] * p.ld_act + col; });
@@ -379,15 +401,15 @@ __device__ __forceinline__ uint2 span_of(const EmbArgs& p, int64_t c, int64_t v)
 
 // Zeros over n elements from p on by a warp: 16 bytes a lane between the first and the last 16-byte boundary.
 template <typename T>
-__device__ __forceinline__ void zero_run(T* p, int64_t n) {
-  constexpr int kPer = 16 / (int)sizeof(T);
-  const int lane = threadIdx.x & 31;
-  const int64_t head = min(n, (int64_t)((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15) / (int64_t)sizeof(T));
-  const int64_t words = (n - head) / kPer, tail = head + words * kPer;
+__device__ __forceinline__ void zero_run(T* p, uint32_t n) {
+  constexpr uint32_t kPer = 16 / sizeof(T);
+  const uint32_t lane = threadIdx.x & 31;
+  const uint32_t head = min(n, ((16u - ((uint32_t)reinterpret_cast<uintptr_t>(p) & 15u)) & 15u) / (uint32_t)sizeof(T));
+  const uint32_t words = (n - head) / kPer, tail = head + words * kPer;
   const T zero = from_f32<T>(0.f);
   if (lane < head) p[lane] = zero;
-  uint4* w = reinterpret_cast<uint4*>(p + head);
-  for (int64_t i = lane; i < words; i += 32) __stcs(w + i, make_uint4(0, 0, 0, 0));
+  uint4* w = reinterpret_cast<uint4*>(p + head) + lane;
+  for (uint32_t i = lane; i < words; i += 32, w += 32) __stcs(w, make_uint4(0, 0, 0, 0));
   if (tail + lane < n) p[tail + lane] = zero;
 }
 
@@ -399,6 +421,7 @@ __global__ void __launch_bounds__(256, 6) embedding_grad_kernel(const EmbArgs p)
   __shared__ float s_sum[8][S::kWide];
   __shared__ uint32_t s_start[64], s_end[64];
   __shared__ int s_row[64], s_rows[2];
+  __shared__ uint32_t s_some[2];
   const int64_t c = blockIdx.y, v0 = (int64_t)blockIdx.x * p.rows_cta;
   const int rows = (int)min((int64_t)p.rows_cta, p.vocab - v0);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -408,7 +431,8 @@ __global__ void __launch_bounds__(256, 6) embedding_grad_kernel(const EmbArgs p)
   if ((int)threadIdx.x < rows) span = span_of(p, c, v0 + threadIdx.x);
   if (warp < 2) {
     const bool wide = span.x < span.y && span.x / kPart != (span.y - 1) / kPart;
-    const uint32_t has = __ballot_sync(0xffffffffu, wide);
+    const uint32_t has = __ballot_sync(0xffffffffu, wide), some = __ballot_sync(0xffffffffu, span.x < span.y);
+    if (lane == 0) s_some[warp] = some;
     s_start[threadIdx.x] = span.x;
     s_end[threadIdx.x] = span.y;
     if (lane == 0) s_rows[warp] = __popc(has);
@@ -418,19 +442,10 @@ __global__ void __launch_bounds__(256, 6) embedding_grad_kernel(const EmbArgs p)
   __syncthreads();
   TO* grad = (TO*)p.grad + c * p.stride_table + v0 * p.ld_table;
   if (!p.accumulate) {
-    if (p.ld_table == p.dim) {   // rows that follow one another: the warps share the runs between rows with tokens
-      for (int r = 0; r < rows;) {
-        int e = r;
-        while (e < rows && s_start[e] == s_end[e]) ++e;
-        const int64_t n = (int64_t)(e - r) * p.dim, share = (n / 8 + 63) / 64 * 64;
-        const int64_t from = min(n, warp * share), to = warp == 7 ? n : min(n, from + share);
-        if (from < to) zero_run(grad + (int64_t)r * p.dim + from, to - from);
-        r = e + 1;
-      }
-    } else {
-      for (int r = warp; r < rows; r += 8)
-        if (s_start[r] == s_end[r]) zero_run(grad + (int64_t)r * p.ld_table, p.dim);
-    }
+    // the rows without tokens
+    uint64_t none = ~((uint64_t)s_some[1] << 32 | s_some[0]);
+    for (int r = warp; r < rows; r += 8)
+      if (none >> r & 1) zero_run(grad + (int64_t)r * p.ld_table, (uint32_t)p.dim);
   }
   const int blocks = (p.dim + S::kWide - 1) / S::kWide, first = s_rows[0], full = first + s_rows[1];
   const float* part = p.part + c * p.parts * 2 * p.dim;

@@ -531,6 +531,7 @@ bool emb_sizes_ok(int32_t clients, int64_t tokens, int64_t vocab, int32_t dim) {
 
 int emb_check(const brace_embedding* e, bool grad) {
   if (!e || !emb_sizes_ok(e->clients, e->tokens, e->vocab, e->dim)) return BRACE_ERR_INVALID_ARG;
+  if (e->dim > (1 << 22)) return BRACE_ERR_UNSUPPORTED;
   if (!float_type(e->table_type) || !float_type(e->act_type)) return BRACE_ERR_INVALID_ARG;
   if ((e->id_bytes != 4 && e->id_bytes != 8) || !std::isfinite(e->scale)) return BRACE_ERR_INVALID_ARG;
   // what is only read may be broadcast: rows of the gradient's activations that are all the same one
@@ -577,11 +578,10 @@ EmbArgs emb_args(const brace_embedding* e) {
 
 template <typename TI, typename TO, int V>
 cudaError_t launch_lookup(const EmbArgs& a, cudaStream_t st) {
-  const int64_t groups = a.tokens * (a.dim / V);
-  // four groups per thread once that still gives every SM work
-  if (groups * a.clients >= (int64_t)4 * 256 * 4 * sm_count())
-    return launch(embedding_lookup_kernel<TI, TO, V, 4>, dim3((unsigned)((groups + 1023) / 1024), (unsigned)a.clients), 256, 0, 1, st, a);
-  return launch(embedding_lookup_kernel<TI, TO, V, 1>, dim3((unsigned)((groups + 255) / 256), (unsigned)a.clients), 256, 0, 1, st, a);
+  constexpr int kWide = 32 * (V >= 8 ? V : V == 2 ? 4 : 4);   // columns of a warp's stretch
+  const int64_t x = (a.tokens + 8 * kLookupRows - 1) / (8 * kLookupRows), z = (a.dim + kWide - 1) / kWide;
+  if (z > 65535) return cudaErrorInvalidConfiguration;
+  return launch(embedding_lookup_kernel<TI, TO, V>, dim3((unsigned)x, (unsigned)a.clients, (unsigned)z), 256, 0, 1, st, a);
 }
 
 cudaError_t launch_sort(const EmbArgs& a, cudaStream_t st) {
@@ -603,7 +603,11 @@ constexpr int64_t kGradElements = 32768;   // of a CTA's rows
 template <typename TI, typename TO, int V>
 cudaError_t launch_grad(EmbArgs a, cudaStream_t st) {
   if (a.tokens > 0) {
-    const cudaError_t err = launch(embedding_sum_kernel<TI, TO, V>, dim3((unsigned)a.parts, (unsigned)a.clients), 256, 0, 1, st, a);
+    // few groups: their columns are shared out until every SM has six CTAs
+    const int64_t blocks = (a.dim + Share<V>::kWide - 1) / Share<V>::kWide, groups = a.parts * a.clients;
+    int64_t z = 6 * sm_count() / groups;
+    z = z < 1 ? 1 : z > blocks ? blocks : z;
+    const cudaError_t err = launch(embedding_sum_kernel<TI, TO, V>, dim3((unsigned)a.parts, (unsigned)a.clients, (unsigned)z), 256, 0, 1, st, a);
     if (err != cudaSuccess) return err;
   }
   // long runs of zeros, but 4 CTAs for each SM while the table has the rows
