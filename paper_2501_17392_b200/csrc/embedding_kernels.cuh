@@ -20,7 +20,10 @@ constexpr int kSortTile = kSortThreads * kSortItems;   // elements one CTA sorts
 constexpr int kDigitBits = 6;
 constexpr int kDigits = 1 << kDigitBits;
 constexpr int kCountRow = kDigits + 1;
-constexpr int kMergeRuns = 16;               // sorted runs merged at a time
+// More tokens than a CTA sorts: digits of 9 bits, tiles of a multiple of kSortTile tokens, at most kMostTiles a client.
+constexpr int kWideBits = 9;
+constexpr int kWideDigits = 1 << kWideBits;
+constexpr int kMostTiles = 256;
 constexpr int kPart = 32;                    // sorted tokens of a group: a CTA's share of the sums
 constexpr int kManyGroups = 16;              // from here on a whole CTA adds a row's partial sums
 
@@ -39,11 +42,12 @@ struct EmbArgs {
   // gradient
   uint32_t *key, *pos;    // [clients][tokens], sorted by (key, pos)
   uint2* span;            // [clients][vocab]: where an id's sorted tokens begin and end; only those of ids that occur
-                          // are written, what else is there is told by the keys (see span_of)
+                          // are written, what else is there is told by the keys (see has_tokens)
   float* part;            // [clients][parts][2][dim]: of each group of kPart sorted tokens, the sums of the first id
                           // if its tokens began in an earlier group, and of the last one if they only go on in the next
   int64_t parts;
-  int rows_cta;
+  int rows_cta;           // rows of a CTA that writes zeros
+  uint32_t zero_ctas, join_split;   // those CTAs, and the CTAs that share the columns of eight groups' joins
 };
 
 __device__ __forceinline__ int64_t load_id(const EmbArgs& p, int64_t c, int64_t t) {
@@ -104,6 +108,19 @@ __global__ void __launch_bounds__(256) embedding_lookup_kernel(const EmbArgs p) 
 }
 
 // ---- gradient: sort ---------------------------------------------------------------------------------------------
+// The lanes of a warp with this lane's digit, bit by bit (a match instruction takes several times as long).
+template <int BITS>
+__device__ __forceinline__ uint32_t same_digit(uint32_t digit) {
+  uint32_t same = 0xffffffffu;
+#pragma unroll
+  for (int b = 0; b < BITS; ++b) {
+    const bool set = (digit >> b) & 1u;
+    const uint32_t with = __ballot_sync(0xffffffffu, set);
+    same &= set ? with : ~with;
+  }
+  return same;
+}
+
 // One CTA sorts up to a tile of consecutive tokens of a client by id: least significant digit first, 6 bits at a
 // time.  A warp holds 32 * ITEMS consecutive elements; equal digits within 32 are ranked by ballots, across the warp's
 // rounds by a counter per (digit, warp), across warps by a scan of the counters.
@@ -137,14 +154,7 @@ __global__ void __launch_bounds__(1024) embedding_sort_kernel(const EmbArgs p, i
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
       const uint32_t digit = (key[i] >> shift) & (kDigits - 1);
-      // the lanes with this lane's digit, bit by bit (a match instruction takes several times as long)
-      uint32_t same = 0xffffffffu;
-#pragma unroll
-      for (int b = 0; b < kDigitBits; ++b) {
-        const bool set = (digit >> b) & 1u;
-        const uint32_t with = __ballot_sync(0xffffffffu, set);
-        same &= set ? with : ~with;
-      }
+      const uint32_t same = same_digit<kDigitBits>(digit);
       const uint32_t before = s_count[warp * kCountRow + digit];
       rank[i] = before + __popc(same & ((1u << lane) - 1u));
       __syncwarp();
@@ -209,42 +219,117 @@ __global__ void __launch_bounds__(1024) embedding_sort_kernel(const EmbArgs p, i
   }
 }
 
-// Merges groups of RUNS sorted runs of `run` elements: an element's place is its own index plus the number of elements
-// in front of it in each other run, found by searches that all runs make in step.
-template <int RUNS>
-__global__ void __launch_bounds__(256) embedding_merge_kernel(const EmbArgs p, int run, uint32_t* out_key, uint32_t* out_pos) {
+// Tokens beyond what one CTA sorts: least significant digit first over tiles.  hist[pass][client][tile][digit] counts
+// the digits of a pass in each tile of its input.  This kernel counts the first pass and clears the others' counts.
+__global__ void __launch_bounds__(kSortThreads) embedding_count_kernel(const EmbArgs p, uint32_t* hist, int64_t tile, int passes) {
+  __shared__ uint32_t s_count[kWideDigits];
   grid_wait();
   grid_trigger();
-  const int64_t c = blockIdx.y;
-  const uint32_t i = blockIdx.x * 256u + threadIdx.x, n = (uint32_t)p.tokens;
-  if (i >= n) return;
-  const uint32_t* key = p.key + c * p.tokens;
-  const uint32_t k = key[i], group = (uint32_t)(i / ((uint64_t)run * RUNS) * ((uint64_t)run * RUNS));
-  const uint32_t mine = (i - group) / (uint32_t)run;
-  uint32_t lo[RUNS], len[RUNS];
-#pragma unroll
-  for (uint32_t r = 0; r < RUNS; ++r) {
-    const uint64_t start = (uint64_t)group + (uint64_t)r * run;
-    lo[r] = (uint32_t)start;                       // the number in front is between lo - start and lo - start + len
-    len[r] = r == mine || start >= n ? 0 : min((uint32_t)run, n - (uint32_t)start);
+  const int64_t c = blockIdx.y, first = (int64_t)blockIdx.x * tile, last = min(p.tokens, first + tile);
+  s_count[threadIdx.x] = 0;
+  __syncthreads();
+  for (int64_t t = first + threadIdx.x; t < last; t += kSortThreads) {
+    const int64_t id = load_id(p, c, t);
+    const uint32_t key = id >= 0 && id < p.vocab ? (uint32_t)id : kNoToken;
+    atomicAdd(&s_count[key & (kWideDigits - 1)], 1u);
   }
-  for (uint32_t left = (uint32_t)run; left > 0; left >>= 1) {
-    uint32_t v[RUNS];
+  __syncthreads();
+  const int64_t plane = (int64_t)gridDim.y * gridDim.x * kWideDigits;
+  uint32_t* mine = hist + (c * gridDim.x + blockIdx.x) * kWideDigits + threadIdx.x;
+  *mine = s_count[threadIdx.x];
+  for (int q = 1; q < passes; ++q) mine[q * plane] = 0;
+}
+
+// One pass: a tile's elements go behind those of smaller digits and of earlier tiles, in their order.  Counts the next
+// pass's digits as it goes (adding whole numbers, so the order of the additions does not matter).
+template <bool FIRST>
+__global__ void __launch_bounds__(kSortThreads) embedding_scatter_kernel(const EmbArgs p, uint32_t* hist, int64_t tile, int pass,
+                                                                         int passes, uint32_t* out_key, uint32_t* out_pos) {
+  constexpr int kWarps = kSortThreads / 32;
+  static_assert(kSortThreads == kWideDigits, "a thread per digit");
+  __shared__ uint32_t s_count[kWarps][kWideDigits];
+  __shared__ uint32_t s_base[kWideDigits];
+  __shared__ uint32_t s_warp[kWarps];
+  grid_wait();
+  grid_trigger();
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int64_t c = blockIdx.y, first = (int64_t)blockIdx.x * tile, last = min(p.tokens, first + tile);
+  const int64_t plane = (int64_t)gridDim.y * gridDim.x * kWideDigits;
+  const uint32_t* counts = hist + pass * plane + c * gridDim.x * kWideDigits + tid;
+  uint32_t before = 0, total = 0;
+#pragma unroll 8
+  for (unsigned t = 0; t < gridDim.x; ++t) {
+    const uint32_t n = counts[(int64_t)t * kWideDigits];
+    total += n;
+    before += t < blockIdx.x ? n : 0;
+  }
+  uint32_t incl = total;
 #pragma unroll
-    for (uint32_t r = 0; r < RUNS; ++r) v[r] = len[r] > 0 ? key[lo[r] + (len[r] >> 1)] : 0;
+  for (int o = 1; o < 32; o <<= 1) {
+    const uint32_t v = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += v;
+  }
+  if (lane == 31) s_warp[warp] = incl;
+  __syncthreads();
+  uint32_t front = lane < warp ? s_warp[lane] : 0;
 #pragma unroll
-    for (uint32_t r = 0; r < RUNS; ++r) {
-      const uint32_t half = len[r] >> 1;
-      const bool front = len[r] > 0 && (v[r] < k || (v[r] == k && r < mine));
-      lo[r] += front ? half + 1 : 0;
-      len[r] = front ? len[r] - half - 1 : half;
+  for (int o = 16; o; o >>= 1) front += __shfl_xor_sync(0xffffffffu, front, o);
+  s_base[tid] = front + incl - total + before;
+  const int shift = pass * kWideBits;
+  uint32_t* next = hist + (pass + 1) * plane + c * gridDim.x * kWideDigits;
+  for (int64_t t0 = first; t0 < last; t0 += kSortTile) {
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) s_count[w][tid] = 0;
+    __syncthreads();
+    uint32_t key[kSortItems], pos[kSortItems], rank[kSortItems];
+#pragma unroll
+    for (int i = 0; i < kSortItems; ++i) {
+      const int64_t t = t0 + (warp * kSortItems + i) * 32 + lane;
+      key[i] = kNoToken;
+      pos[i] = (uint32_t)t;
+      if (t < last) {
+        if (FIRST) {
+          const int64_t id = load_id(p, c, t);
+          if (id >= 0 && id < p.vocab) key[i] = (uint32_t)id;
+        } else {
+          key[i] = p.key[c * p.tokens + t];
+          pos[i] = p.pos[c * p.tokens + t];
+        }
+      }
     }
-  }
-  uint32_t to = group + (i - group - mine * (uint32_t)run);
 #pragma unroll
-  for (uint32_t r = 0; r < RUNS; ++r) to += r == mine ? 0 : lo[r] - (uint32_t)((uint64_t)group + (uint64_t)r * run);
-  out_key[c * p.tokens + to] = k;
-  out_pos[c * p.tokens + to] = p.pos[c * p.tokens + i];
+    for (int i = 0; i < kSortItems; ++i) {
+      const bool live = t0 + (warp * kSortItems + i) * 32 + lane < last;
+      const uint32_t digit = (key[i] >> shift) & (kWideDigits - 1);
+      const uint32_t same = same_digit<kWideBits>(digit) & __ballot_sync(0xffffffffu, live);
+      const uint32_t already = s_count[warp][digit];
+      rank[i] = already + __popc(same & ((1u << lane) - 1u));
+      __syncwarp();
+      if (live && lane == __ffs(same) - 1) s_count[warp][digit] = already + __popc(same);
+      __syncwarp();
+    }
+    __syncthreads();
+    uint32_t run = s_base[tid];
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+      const uint32_t n = s_count[w][tid];
+      s_count[w][tid] = run;
+      run += n;
+    }
+    s_base[tid] = run;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kSortItems; ++i) {
+      if (t0 + (warp * kSortItems + i) * 32 + lane < last) {
+        const uint32_t to = s_count[warp][(key[i] >> shift) & (kWideDigits - 1)] + rank[i];
+        out_key[c * p.tokens + to] = key[i];
+        out_pos[c * p.tokens + to] = pos[i];
+        if (pass + 1 < passes)
+          atomicAdd(&next[(int64_t)(to / (uint32_t)tile) * kWideDigits + ((key[i] >> (shift + kWideBits)) & (kWideDigits - 1))], 1u);
+      }
+    }
+    __syncthreads();
+  }
 }
 
 // ---- gradient: sums ---------------------------------------------------------------------------------------------
@@ -261,29 +346,34 @@ struct Share {
 #pragma unroll
       for (int j = 0; j < V; ++j) sum[q][j] = 0.f;
   }
-  // Adds `n` rows at(0) .. at(n - 1), two at a time; `left`: elements of the row from the lane's first one on.
-  template <typename T, typename At>
-  __device__ __forceinline__ void add(int n, int left, At at) {
-#pragma unroll 1
-    for (int i = 0; i < n; i += 2) {
-      Pack<T, V> x[2][Q];
-      const bool two = i + 1 < n;
-      const T *p0 = at(i), *p1 = two ? at(i + 1) : p0;
+  // R rows at a time, all their loads first.
+  template <typename T, int R, typename At>
+  __device__ __forceinline__ void add_some(int i, int left, At at) {
+    Pack<T, V> x[R][Q];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const T* row = at(i + r);
 #pragma unroll
       for (int q = 0; q < Q; ++q)
-        if (32 * V * q < left) {
-          x[0][q].load(p0 + 32 * V * q);
-          if (two) x[1][q].load(p1 + 32 * V * q);
-        }
+        if (32 * V * q < left) x[r][q].load(row + 32 * V * q);
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r)
 #pragma unroll
       for (int q = 0; q < Q; ++q)
         if (32 * V * q < left)
 #pragma unroll
-          for (int j = 0; j < V; ++j) {
-            sum[q][j] += to_f32(x[0][q].t[j]);
-            if (two) sum[q][j] += to_f32(x[1][q].t[j]);
-          }
-    }
+          for (int j = 0; j < V; ++j) sum[q][j] += to_f32(x[r][q].t[j]);
+  }
+  // Adds `n` rows at(0) .. at(n - 1); `left`: elements of the row from the lane's first one on.
+  template <typename T, typename At>
+  __device__ __forceinline__ void add(int n, int left, At at) {
+    constexpr int R = V * sizeof(T) * Q <= 16 ? 4 : 2;
+    int i = 0;
+#pragma unroll 1
+    for (; i + R <= n; i += R) add_some<T, R>(i, left, at);
+#pragma unroll 1
+    for (; i < n; ++i) add_some<T, 1>(i, left, at);
   }
   // Warps first, first + 1, .. of the CTA hold shares of one sum; the first of them gets it.
   __device__ __forceinline__ void join(float (*scratch)[kWide], int first, int warps) {
@@ -325,7 +415,7 @@ struct Share {
 // A CTA takes a group of kPart sorted tokens: notes where each id's tokens begin and end, writes the rows of the ids
 // whose tokens all lie in the group, and leaves a partial sum of an id that goes on before ([0]) or only after ([1]).
 template <typename TI, typename TO, int V>
-__global__ void __launch_bounds__(256, 6) embedding_sum_kernel(const EmbArgs p) {
+__global__ void __launch_bounds__(256, 5) embedding_sum_kernel(const EmbArgs p) {
   static_assert(kPart == 32, "a lane per token of a group");
   using S = Share<V>;
   __shared__ float s_sum[8][S::kWide];
@@ -389,14 +479,12 @@ __global__ void __launch_bounds__(256, 6) embedding_sum_kernel(const EmbArgs p) 
   }
 }
 
-// The sorted tokens of id v.  The table's entry counts only where the key it points at says so: that of an id without
+// Whether id v has tokens.  The table's entry counts only where the key it points at says so: that of an id without
 // tokens holds whatever was in the workspace.
-__device__ __forceinline__ uint2 span_of(const EmbArgs& p, int64_t c, int64_t v) {
-  if (p.tokens == 0) return make_uint2(0, 0);
-  const uint2 s = p.span[c * p.vocab + v];
-  const uint32_t* key = p.key + c * p.tokens;
-  if ((int64_t)s.x >= p.tokens || key[s.x] != (uint32_t)v) return make_uint2(0, 0);
-  return s;
+__device__ __forceinline__ bool has_tokens(const EmbArgs& p, int64_t c, int64_t v) {
+  if (p.tokens == 0) return false;
+  const uint32_t at = p.span[c * p.vocab + v].x;
+  return (int64_t)at < p.tokens && p.key[c * p.tokens + at] == (uint32_t)v;
 }
 
 // Zeros over n elements from p on by a warp: 16 bytes a lane between the first and the last 16-byte boundary.
@@ -413,69 +501,79 @@ __device__ __forceinline__ void zero_run(T* p, uint32_t n) {
   if (tail + lane < n) p[tail + lane] = zero;
 }
 
-// The other rows of the table's gradient, rows_cta (up to 64) a CTA: zeros where an id has no tokens, and the sums of
-// the partial sums of the ids whose tokens lie in several groups.
+// The rest of the table's gradient.  The first zero_ctas CTAs of a client write zeros to the rows of ids without tokens,
+// rows_cta (up to 64) each.  The others look at 8 groups each for an id whose tokens begin there and go on, and add
+// the partial sums of its groups for their share of the columns.
 template <typename TO, int V>
 __global__ void __launch_bounds__(256, 6) embedding_grad_kernel(const EmbArgs p) {
   using S = Share<V>;
   __shared__ float s_sum[8][S::kWide];
-  __shared__ uint32_t s_start[64], s_end[64];
-  __shared__ int s_row[64], s_rows[2];
   __shared__ uint32_t s_some[2];
-  const int64_t c = blockIdx.y, v0 = (int64_t)blockIdx.x * p.rows_cta;
-  const int rows = (int)min((int64_t)p.rows_cta, p.vocab - v0);
+  __shared__ int64_t s_end[8];
+  __shared__ uint32_t s_key[8];
+  const int64_t c = blockIdx.y;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  TO* grad = (TO*)p.grad + c * p.stride_table;
   grid_wait();
   grid_trigger();
-  uint2 span = make_uint2(0, 0);
-  if ((int)threadIdx.x < rows) span = span_of(p, c, v0 + threadIdx.x);
-  if (warp < 2) {
-    const bool wide = span.x < span.y && span.x / kPart != (span.y - 1) / kPart;
-    const uint32_t has = __ballot_sync(0xffffffffu, wide), some = __ballot_sync(0xffffffffu, span.x < span.y);
-    if (lane == 0) s_some[warp] = some;
-    s_start[threadIdx.x] = span.x;
-    s_end[threadIdx.x] = span.y;
-    if (lane == 0) s_rows[warp] = __popc(has);
-    // the rows of several groups in order, those of the second warp from 32 on
-    if (wide) s_row[warp * 32 + __popc(has & ((1u << lane) - 1u))] = threadIdx.x;
+  if (blockIdx.x < p.zero_ctas) {
+    const int64_t v0 = (int64_t)blockIdx.x * p.rows_cta;
+    const int rows = (int)min((int64_t)p.rows_cta, p.vocab - v0);
+    if (warp < 2) {
+      const bool some = (int)threadIdx.x < rows && has_tokens(p, c, v0 + threadIdx.x);
+      const uint32_t mask = __ballot_sync(0xffffffffu, some);
+      if (lane == 0) s_some[warp] = mask;
+    }
+    __syncthreads();
+    const uint64_t some = (uint64_t)s_some[1] << 32 | s_some[0];
+    for (int r = warp; r < rows; r += 8)
+      if (!(some >> r & 1)) zero_run(grad + (v0 + r) * p.ld_table, (uint32_t)p.dim);
+    return;
+  }
+  const int blocks = (p.dim + S::kWide - 1) / S::kWide;
+  const uint32_t u = blockIdx.x - p.zero_ctas, z = u % p.join_split;
+  const int64_t g0 = (int64_t)(u / p.join_split) * 8;
+  const int first = blocks * (int)z / (int)p.join_split, last = blocks * (int)(z + 1) / (int)p.join_split;
+  if (lane == 0) {   // the warp's group: does its last token's id begin in it and go on?
+    const int64_t g = g0 + warp, i = g * kPart + kPart - 1;
+    const uint32_t* key = p.key + c * p.tokens;
+    s_end[warp] = 0;
+    if (i + 1 < p.tokens) {
+      const uint32_t k = key[i];
+      if (k != kNoToken && key[i + 1] == k) {
+        const uint2 span = p.span[c * p.vocab + k];
+        if (span.x / kPart == g) {
+          s_end[warp] = (span.y - 1) / kPart + 1;
+          s_key[warp] = k;
+        }
+      }
+    }
   }
   __syncthreads();
-  TO* grad = (TO*)p.grad + c * p.stride_table + v0 * p.ld_table;
-  if (!p.accumulate) {
-    // the rows without tokens
-    uint64_t none = ~((uint64_t)s_some[1] << 32 | s_some[0]);
-    for (int r = warp; r < rows; r += 8)
-      if (none >> r & 1) zero_run(grad + (int64_t)r * p.ld_table, (uint32_t)p.dim);
-  }
-  const int blocks = (p.dim + S::kWide - 1) / S::kWide, first = s_rows[0], full = first + s_rows[1];
   const float* part = p.part + c * p.parts * 2 * p.dim;
-  auto take = [&](S& share, int r, int col, int left, int64_t from, int64_t to) {   // groups from .. to - 1 of the row's
+  auto take = [&](S& share, int64_t g, int col, int left, int64_t from, int64_t to) {   // the id's groups from .. to - 1
     share.clear();
-    const int64_t g0 = s_start[r] / kPart;
     share.template add<float>((int)(to - from), left, [&](int t) {
-      const int64_t g = from + t;
-      return part + (g * 2 + (g == g0 ? 1 : 0)) * p.dim + col;
+      return part + ((from + t) * 2 + (from + t == g ? 1 : 0)) * p.dim + col;
     });
   };
-  for (int u = warp; u < full * blocks; u += 8) {   // a warp for each part of a row of few groups
-    const int k = u / blocks, r = s_row[k < first ? k : 32 + k - first];
-    const int64_t g0 = s_start[r] / kPart, g1 = (s_end[r] - 1) / kPart + 1;
-    if (g1 - g0 > kManyGroups) continue;
-    const int col = (u - k * blocks) * S::kWide + lane * V, left = p.dim - col;
-    S share;
-    take(share, r, col, left, g0, g1);
-    share.to_row(grad + (int64_t)r * p.ld_table + col, left, p.scale, p.accumulate);
-  }
-  for (int k = 0; k < full; ++k) {                  // the CTA together for one of many
-    const int r = s_row[k < first ? k : 32 + k - first];
-    const int64_t g0 = s_start[r] / kPart, g1 = (s_end[r] - 1) / kPart + 1, n = g1 - g0;
-    if (n <= kManyGroups) continue;
-    for (int b = 0; b < blocks; ++b) {
+  int turn = 0;
+  for (int w = 0; w < 8; ++w) {
+    const int64_t g = g0 + w, n = s_end[w] - g;
+    if (s_end[w] == 0) continue;
+    TO* row = grad + (int64_t)s_key[w] * p.ld_table;
+    for (int b = first; b < last; ++b) {
       const int col = b * S::kWide + lane * V, left = p.dim - col;
       S share;
-      take(share, r, col, left, g0 + n * warp / 8, g0 + n * (warp + 1) / 8);
-      share.join(s_sum, 0, 8);
-      if (warp == 0) share.to_row(grad + (int64_t)r * p.ld_table + col, left, p.scale, p.accumulate);
+      if (n <= kManyGroups) {   // a warp for each stretch
+        if ((turn++ & 7) != warp) continue;
+        take(share, g, col, left, g, g + n);
+        share.to_row(row + col, left, p.scale, p.accumulate);
+      } else {                  // all of them
+        take(share, g, col, left, g + n * warp / 8, g + n * (warp + 1) / 8);
+        share.join(s_sum, 0, 8);
+        if (warp == 0) share.to_row(row + col, left, p.scale, p.accumulate);
+      }
     }
   }
 }

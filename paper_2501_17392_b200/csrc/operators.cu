@@ -500,7 +500,9 @@ MatRef mat_ref(const void* p, int type, int64_t ld, int64_t stride, int64_t bit0
 
 struct EmbPlan {
   int64_t parts;
-  size_t off_key[2], off_pos[2], off_span, off_part, bytes;
+  int64_t tile;    // tokens of a tile of the wide sort
+  int tiles, passes;
+  size_t off_key[2], off_pos[2], off_hist, off_span, off_part, bytes;
 };
 
 EmbPlan emb_plan(int32_t clients, int64_t tokens, int64_t vocab, int32_t dim) {
@@ -512,11 +514,17 @@ EmbPlan emb_plan(int32_t clients, int64_t tokens, int64_t vocab, int32_t dim) {
     return here;
   };
   const int64_t n = (int64_t)clients * tokens;
-  const bool merged = tokens > kSortTile;
+  const bool wide = tokens > kSortTile;
+  const int64_t per = ((tokens + kSortTile - 1) / kSortTile + kMostTiles - 1) / kMostTiles;
+  q.tile = per * kSortTile;
+  q.tiles = wide ? (int)((tokens + q.tile - 1) / q.tile) : 0;
+  q.passes = 0;
+  while ((vocab >> (q.passes * kWideBits)) != 0) ++q.passes;   // the largest value of these bits stands for "no token"
   for (int i = 0; i < 2; ++i) {
-    q.off_key[i] = take(i == 0 || merged ? 4 * n : 0);
-    q.off_pos[i] = take(i == 0 || merged ? 4 * n : 0);
+    q.off_key[i] = take(i == 0 || wide ? 4 * n : 0);
+    q.off_pos[i] = take(i == 0 || wide ? 4 * n : 0);
   }
+  q.off_hist = take((int64_t)q.passes * clients * q.tiles * kWideDigits * 4);
   q.off_span = take(8 * (int64_t)clients * vocab);
   q.parts = (tokens + kPart - 1) / kPart;
   q.off_part = take((int64_t)clients * q.parts * 2 * dim * 4);
@@ -592,10 +600,23 @@ cudaError_t launch_sort(const EmbArgs& a, cudaStream_t st) {
     const size_t smem = (size_t)threads * 8 + (size_t)kCountRow * (threads / 32) * 4;
     return launch(embedding_sort_kernel<1>, dim3(1, (unsigned)a.clients), threads, smem, 1, st, a, threads, bits);
   }
-  const int threads = kSortThreads, tile = kSortTile;
-  const size_t smem = (size_t)tile * 8 + (size_t)kCountRow * (threads / 32) * 4;
-  return launch(embedding_sort_kernel<kSortItems>, dim3((unsigned)((a.tokens + tile - 1) / tile), (unsigned)a.clients),
-                threads, smem, 1, st, a, tile, bits);
+  const size_t smem = (size_t)kSortTile * 8 + (size_t)kCountRow * (kSortThreads / 32) * 4;
+  return launch(embedding_sort_kernel<kSortItems>, dim3(1, (unsigned)a.clients), kSortThreads, smem, 1, st, a, kSortTile, bits);
+}
+
+// Sorts more tokens than that; leaves a.key and a.pos at the result.
+cudaError_t launch_wide_sort(EmbArgs& a, const EmbPlan& q, char* ws, cudaStream_t st) {
+  const dim3 grid((unsigned)q.tiles, (unsigned)a.clients);
+  uint32_t* hist = (uint32_t*)(ws + q.off_hist);
+  cudaError_t err = launch(embedding_count_kernel, grid, kSortThreads, 0, 1, st, a, hist, q.tile, q.passes);
+  for (int pass = 0; err == cudaSuccess && pass < q.passes; ++pass) {
+    uint32_t *key = (uint32_t*)(ws + q.off_key[pass & 1]), *pos = (uint32_t*)(ws + q.off_pos[pass & 1]);
+    err = pass == 0 ? launch(embedding_scatter_kernel<true>, grid, kSortThreads, 0, 1, st, a, hist, q.tile, pass, q.passes, key, pos)
+                    : launch(embedding_scatter_kernel<false>, grid, kSortThreads, 0, 1, st, a, hist, q.tile, pass, q.passes, key, pos);
+    a.key = key;
+    a.pos = pos;
+  }
+  return err;
 }
 
 constexpr int64_t kGradElements = 32768;   // of a CTA's rows
@@ -603,9 +624,9 @@ constexpr int64_t kGradElements = 32768;   // of a CTA's rows
 template <typename TI, typename TO, int V>
 cudaError_t launch_grad(EmbArgs a, cudaStream_t st) {
   if (a.tokens > 0) {
-    // few groups: their columns are shared out until every SM has six CTAs
+    // few groups: their columns are shared out until every SM has five CTAs
     const int64_t blocks = (a.dim + Share<V>::kWide - 1) / Share<V>::kWide, groups = a.parts * a.clients;
-    int64_t z = 6 * sm_count() / groups;
+    int64_t z = 5 * sm_count() / groups;
     z = z < 1 ? 1 : z > blocks ? blocks : z;
     const cudaError_t err = launch(embedding_sum_kernel<TI, TO, V>, dim3((unsigned)a.parts, (unsigned)a.clients, (unsigned)z), 256, 0, 1, st, a);
     if (err != cudaSuccess) return err;
@@ -615,8 +636,12 @@ cudaError_t launch_grad(EmbArgs a, cudaStream_t st) {
   const int64_t even = a.vocab * a.clients / (4 * sm_count());
   if (rows > even) rows = even;
   a.rows_cta = rows < 1 ? 1 : rows > 64 ? 64 : (int)rows;
-  return launch(embedding_grad_kernel<TO, V>,
-                dim3((unsigned)((a.vocab + a.rows_cta - 1) / a.rows_cta), (unsigned)a.clients), 256, 0, 1, st, a);
+  a.zero_ctas = a.accumulate ? 0 : (unsigned)((a.vocab + a.rows_cta - 1) / a.rows_cta);
+  const int64_t blocks = (a.dim + Share<V>::kWide - 1) / Share<V>::kWide, eights = (a.parts + 7) / 8;
+  a.join_split = (unsigned)(blocks < 16 ? blocks : 16);
+  const int64_t ctas = a.zero_ctas + eights * a.join_split;
+  if (ctas == 0) return cudaSuccess;
+  return launch(embedding_grad_kernel<TO, V>, dim3((unsigned)ctas, (unsigned)a.clients), 256, 0, 1, st, a);
 }
 
 }  // namespace
@@ -670,17 +695,7 @@ int brace_embedding_grad(const brace_embedding* e, void* d_workspace, size_t wor
   cudaGetLastError();
   cudaError_t err = cudaSuccess;
   if (a.tokens > 0) {
-    err = launch_sort(a, st);
-    int from = 0;
-    for (int64_t run = kSortTile; err == cudaSuccess && run < a.tokens; run *= kMergeRuns) {
-      uint32_t *key = (uint32_t*)(ws + q.off_key[from ^ 1]), *pos = (uint32_t*)(ws + q.off_pos[from ^ 1]);
-      const dim3 grid((unsigned)((a.tokens + 255) / 256), (unsigned)a.clients);
-      err = a.tokens <= 4 * run ? launch(embedding_merge_kernel<4>, grid, 256, 0, 1, st, a, (int)run, key, pos)
-                                : launch(embedding_merge_kernel<kMergeRuns>, grid, 256, 0, 1, st, a, (int)run, key, pos);
-      a.key = key;
-      a.pos = pos;
-      from ^= 1;
-    }
+    err = a.tokens <= kSortTile ? launch_sort(a, st) : launch_wide_sort(a, q, ws, st);
   }
   if (err == cudaSuccess) {
     const int width = emb_width(e);
