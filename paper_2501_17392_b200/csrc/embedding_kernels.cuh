@@ -415,12 +415,14 @@ struct Share {
 // A CTA takes a group of kPart sorted tokens: notes where each id's tokens begin and end, writes the rows of the ids
 // whose tokens all lie in the group, and leaves a partial sum of an id that goes on before ([0]) or only after ([1]).
 template <typename TI, typename TO, int V>
-__global__ void __launch_bounds__(256, 5) embedding_sum_kernel(const EmbArgs p) {
+__global__ void __launch_bounds__(256, 4) embedding_sum_kernel(const EmbArgs p) {
   static_assert(kPart == 32, "a lane per token of a group");
   using S = Share<V>;
   __shared__ float s_sum[8][S::kWide];
   __shared__ uint32_t s_key[32], s_pos[32];
-  __shared__ int s_first[33], s_segments, s_goes;
+  // ids with one token, all of it here: where it is; the other segments: where they begin and end, and whether the id
+  // has tokens in an earlier group (1) or a later one (2)
+  __shared__ int s_single[32], s_first[32], s_last[32], s_goes[32], s_counts[2];
   grid_wait();
   grid_trigger();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -432,32 +434,73 @@ __global__ void __launch_bounds__(256, 5) embedding_sum_kernel(const EmbArgs p) 
     uint32_t before = __shfl_up_sync(0xffffffffu, k, 1), after = __shfl_down_sync(0xffffffffu, k, 1);
     if (lane == 0) before = i > 0 ? key[i - 1] : kNoToken;
     if (lane == 31) after = i + 1 < p.tokens ? key[i + 1] : kNoToken;
-    const bool token = k != kNoToken;
+    const bool token = k != kNoToken, head = token && (lane == 0 || before != k), tail = token && (lane == 31 || after != k);
     if (token) {   // (every CTA of a group writes the same)
       if (before != k) p.span[c * p.vocab + k].x = (uint32_t)i;
       if (after != k) p.span[c * p.vocab + k].y = (uint32_t)i + 1;
       s_key[lane] = k;
       s_pos[lane] = p.pos[c * p.tokens + i];
     }
-    const uint32_t heads = __ballot_sync(0xffffffffu, token && (lane == 0 || before != k));
-    const int tokens = __popc(__ballot_sync(0xffffffffu, token));
-    if (token && (heads >> lane & 1u)) s_first[__popc(heads & ((1u << lane) - 1u))] = lane;
-    const bool early = __shfl_sync(0xffffffffu, token && before == k, 0), late = __shfl_sync(0xffffffffu, token && after == k, 31);
+    const int goes = (lane == 0 && token && before == k ? 1 : 0) | (lane == 31 && token && after == k ? 2 : 0);
+    const bool single = head && tail && goes == 0;
+    const uint32_t singles = __ballot_sync(0xffffffffu, single);
+    const uint32_t heads = __ballot_sync(0xffffffffu, head && !single), tails = __ballot_sync(0xffffffffu, tail && !single);
+    const uint32_t below = (1u << lane) - 1u;
+    if (single) s_single[__popc(singles & below)] = lane;
+    if (head && !single) s_first[__popc(heads & below)] = lane;
+    if (tail && !single) s_last[__popc(tails & below)] = lane + 1;
+    const int early = __shfl_sync(0xffffffffu, goes, 0) & 1, late = __shfl_sync(0xffffffffu, goes, 31) & 2;
+    const int n = __popc(heads);
+    if (lane < n) s_goes[lane] = (lane == 0 ? early : 0) | (lane == n - 1 ? late : 0);
     if (lane == 0) {
-      s_segments = __popc(heads);
-      s_first[__popc(heads)] = tokens;
-      s_goes = (early ? 1 : 0) | (late ? 2 : 0);
+      s_counts[0] = __popc(singles);
+      s_counts[1] = n;
     }
   }
   __syncthreads();
-  const int segments = s_segments, goes = s_goes;
   // the row's columns are shared by gridDim.z CTAs
   const int all = (p.dim + S::kWide - 1) / S::kWide, block0 = all * (int)blockIdx.z / (int)gridDim.z;
-  const int blocks = all * ((int)blockIdx.z + 1) / (int)gridDim.z - block0, tasks = segments * blocks;
-  const int warps = tasks > 4 ? 1 : tasks > 2 ? 2 : tasks > 1 ? 4 : 8;   // per task; several: all tasks at once
+  const int blocks = all * ((int)blockIdx.z + 1) / (int)gridDim.z - block0;
   const TI* dy = (const TI*)p.in + c * p.stride_act;
+  TO* grad = (TO*)p.grad + c * p.stride_table;
+
+  // rows with one token: four at a time, their loads first
+  const int singles = s_counts[0], quads = (singles + 3) / 4 * blocks;
+  int q = 0, block = warp;
+  for (int u = warp; u < quads; u += 8, block += 8) {
+    for (; block >= blocks; block -= blocks) ++q;
+    const int col = (block0 + block) * S::kWide + lane * V, left = p.dim - col;
+    Pack<TI, V> x[4][S::Q];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const TI* row = dy + (int64_t)s_pos[s_single[min(4 * q + r, singles - 1)]] * p.ld_act + col;
+#pragma unroll
+      for (int k = 0; k < S::Q; ++k)
+        if (32 * V * k < left) x[r][k].load(row + 32 * V * k);
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      if (4 * q + r >= singles) break;
+      TO* row = grad + (int64_t)s_key[s_single[4 * q + r]] * p.ld_table + col;
+#pragma unroll
+      for (int k = 0; k < S::Q; ++k)
+        if (32 * V * k < left) {
+          Pack<TO, V> y;
+          if (p.accumulate) y.load_plain(row + 32 * V * k);
+#pragma unroll
+          for (int j = 0; j < V; ++j)
+            y.t[j] = from_f32<TO>((p.accumulate ? to_f32(y.t[j]) : 0.f) + to_f32(x[r][k].t[j]) * p.scale);
+          y.store_stream(row + 32 * V * k);
+        }
+    }
+  }
+
+  // the others: a warp, or several, for a stretch of a segment
+  const int segments = s_counts[1], tasks = segments * blocks;
+  const int warps = tasks > 4 ? 1 : tasks > 2 ? 2 : tasks > 1 ? 4 : 8;   // per task; several: all tasks at once
   const int s = warp & (warps - 1), stride = 8 / warps;
-  int q = 0, block = warp / warps;   // this warp's task: a segment and a stretch of its columns
+  q = 0;
+  block = warp / warps;
   for (int u0 = 0; u0 < tasks; u0 += stride, block += stride) {
     const int u = u0 + warp / warps;
     for (; block >= blocks; block -= blocks) ++q;
@@ -465,16 +508,15 @@ __global__ void __launch_bounds__(256, 5) embedding_sum_kernel(const EmbArgs p) 
     share.clear();
     const int col = (block0 + block) * S::kWide + lane * V, left = p.dim - col;
     if (u < tasks) {
-      const int first = s_first[q], n = s_first[q + 1] - first, from = first + n * s / warps, to = first + n * (s + 1) / warps;
+      const int first = s_first[q], n = s_last[q] - first, from = first + n * s / warps, to = first + n * (s + 1) / warps;
       share.template add<TI>(to - from, left, [&](int t) { return dy + (int64_t)s_pos[from + t] * p.ld_act + col; });
     }
     if (warps > 1) share.join(s_sum, warp - s, warps);
     if (u < tasks && s == 0) {
-      const bool early = q == 0 && (goes & 1), late = q + 1 == segments && (goes & 2);
-      if (early || late)
-        share.to_part(p.part + ((c * p.parts + g) * 2 + (early ? 0 : 1)) * p.dim + col, left);
+      if (s_goes[q])
+        share.to_part(p.part + ((c * p.parts + g) * 2 + (s_goes[q] & 1 ? 0 : 1)) * p.dim + col, left);
       else
-        share.to_row((TO*)p.grad + c * p.stride_table + (int64_t)s_key[s_first[q]] * p.ld_table + col, left, p.scale, p.accumulate);
+        share.to_row(grad + (int64_t)s_key[s_first[q]] * p.ld_table + col, left, p.scale, p.accumulate);
     }
   }
 }

@@ -624,9 +624,9 @@ constexpr int64_t kGradElements = 32768;   // of a CTA's rows
 template <typename TI, typename TO, int V>
 cudaError_t launch_grad(EmbArgs a, cudaStream_t st) {
   if (a.tokens > 0) {
-    // few groups: their columns are shared out until every SM has five CTAs
+    // few groups: their columns are shared out until every SM has four CTAs
     const int64_t blocks = (a.dim + Share<V>::kWide - 1) / Share<V>::kWide, groups = a.parts * a.clients;
-    int64_t z = 5 * sm_count() / groups;
+    int64_t z = 4 * sm_count() / groups;
     z = z < 1 ? 1 : z > blocks ? blocks : z;
     const cudaError_t err = launch(embedding_sum_kernel<TI, TO, V>, dim3((unsigned)a.parts, (unsigned)a.clients, (unsigned)z), 256, 0, 1, st, a);
     if (err != cudaSuccess) return err;
