@@ -455,3 +455,27 @@ def test_table_past_32_bits_of_offset():
     plan.grad(out, ids, table)
     total, size, count = grad64(out, ids, vocab, 1.0)
     assert bool(((table.double() - total).abs() <= (count + 3) * 2 ** -24 * size + U[BF16] * total.abs()).all())
+
+
+# ---- together -----------------------------------------------------------------------------------------------------
+
+def test_rounds_of_a_language_model():
+    from examples.language_model_round import train
+
+    losses = train(rounds=25)
+    # from chance (log 300 = 5.7) the loss falls although a fifth of the clients send ten times the opposite
+    assert 5.0 < losses[0] < 6.5 and losses[-1] < 0.5 * losses[0]
+
+
+def test_a_wait_that_ran_out_is_reported():
+    # the kernels note it in the workspace's first word; the next call clears it
+    plan = B.Orthogonalizer(20, 20)
+    g, out = randn(1, 20, 20), torch.empty(1, 20, 20, device="cuda")
+    plan.orthogonalize(g, out)
+    plan.check()
+    plan.workspace[:4] = torch.tensor([1, 0, 0, 0], dtype=torch.uint8)
+    with pytest.raises(B.BraceError) as err:
+        plan.check()
+    assert err.value.status == B.ERR_TIMEOUT
+    plan.orthogonalize(g, out)
+    plan.check()
