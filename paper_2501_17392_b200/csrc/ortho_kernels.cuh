@@ -418,12 +418,19 @@ __device__ __forceinline__ void prefetch_weights(const GemmArgs& p, int64_t b, i
 }
 
 // Where there are too few tiles for the GPU, a cluster of KS CTAs shares the contraction of one (CG = 1): each sums its
-// part of it, hands every other one its share of the columns through distributed shared memory, and finishes its own.
+// part of it, hands every other one its share of the columns, and finishes its own.  The shares go as bulk copies from
+// shared memory to shared memory (the same as 16-byte stores of the lanes took 5 us for 2).  In both places the share
+// of 32 / KS 16-byte words a row is swizzled by the row.
 template <int KS>
-__device__ __forceinline__ uint32_t share_at(uint32_t base, int from, int row, int word) {
-  constexpr int kWords = 32 / KS;   // 16-byte words of a row of an owner's columns
-  return base + (uint32_t)(((from * 128 + row) * kWords + (word ^ (row & (kWords - 1)))) << 4);
-}
+struct Exchange {
+  static constexpr int kWords = 32 / KS, kBytes = 128 * kWords * 16;   // of a share: 128 rows
+  // what goes to CTA `to`, and what came from CTA `from`: where the stages were
+  static __device__ __forceinline__ uint32_t out(uint32_t base, int to) { return base + (uint32_t)(to * kBytes); }
+  static __device__ __forceinline__ uint32_t in(uint32_t base, int from) { return base + (uint32_t)((KS + from) * kBytes); }
+  static __device__ __forceinline__ uint32_t word(uint32_t share, int row, int w) {
+    return share + (uint32_t)((row * kWords + (w ^ (row & (kWords - 1)))) << 4);
+  }
+};
 
 // 32 rows x 32 columns of a finished product: scaled, and stored as operand planes or as the caller's result.
 template <int NP, int MODE, typename TOUT>
@@ -462,7 +469,8 @@ __global__ void __launch_bounds__(GemmShape<CG, TN, NP>::kThreads, 1)
   const uint32_t base = (smem_addr(smem_raw) + 1023u) & ~1023u;
   const uint32_t cells = base + STAGES * Shape::kStageBytes;
   const uint32_t full = cells + Shape::kEpiWarps * kCellBytes, empty = full + 8 * STAGES;
-  const uint32_t tm_full = empty + 8 * STAGES, tm_empty = tm_full + 8 * BUFS, tail = tm_empty + 8 * BUFS;
+  const uint32_t tm_full = empty + 8 * STAGES, tm_empty = tm_full + 8 * BUFS, shared_bar = tm_empty + 8 * BUFS;
+  const uint32_t tail = shared_bar + 8;
   volatile int* dead = (volatile int*)(smem_raw + (tail - smem_addr(smem_raw)));
   uint32_t* tmem_slot = (uint32_t*)(smem_raw + (tail + 8 - smem_addr(smem_raw)));
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -479,6 +487,10 @@ __global__ void __launch_bounds__(GemmShape<CG, TN, NP>::kThreads, 1)
     for (int i = 0; i < BUFS; ++i) {
       mbar_init(tm_full + 8 * i, 1);
       mbar_init(tm_empty + 8 * i, CG * Shape::kEpiWarps);
+    }
+    if (KS > 1) {
+      mbar_init(shared_bar, 1);
+      mbar_expect_tx(shared_bar, (KS - 1) * Exchange<KS>::kBytes);
     }
     mbar_init_visible();
     tma_prefetch(&maps.a[0]);
@@ -708,21 +720,33 @@ __global__ void __launch_bounds__(GemmShape<CG, TN, NP>::kThreads, 1)
     if (KS == 1) fence_async_global();
   }
   if constexpr (KS > 1) {
+    using E = Exchange<KS>;
     int b, ti, tj;
     place(cluster, b, ti, tj);
     const int quarter = warp & 3, cols0 = ((warp - 4) >> 2) * 64;
-    cluster_sync();   // no matrix instruction reads the stages any more, here or in the other CTAs
+    cluster_arrive();   // once all are here, no matrix instruction or load uses the stages any more
     if (warp >= 4) {
-      constexpr int kWords = 32 / KS;
 #pragma unroll
       for (int w = 0; w < 16; ++w) {
-        const int word = cols0 / 4 + w, owner = word / kWords;
-        st_cluster16(map_to_rank(share_at<KS>(base, part, quarter * 32 + lane, word - owner * kWords), (uint32_t)owner),
-                     make_uint4(__float_as_uint(acc[4 * w]), __float_as_uint(acc[4 * w + 1]),
-                                __float_as_uint(acc[4 * w + 2]), __float_as_uint(acc[4 * w + 3])));
+        const int word = cols0 / 4 + w, owner = word / E::kWords;
+        sts16(E::word(E::out(base, owner), quarter * 32 + lane, word - owner * E::kWords),
+              make_uint4(__float_as_uint(acc[4 * w]), __float_as_uint(acc[4 * w + 1]), __float_as_uint(acc[4 * w + 2]),
+                         __float_as_uint(acc[4 * w + 3])));
       }
+      fence_async();
     }
-    cluster_sync();
+    __syncwarp();
+    cluster_wait();
+    if (warp >= 4) {
+      if (lane == 0) {   // this warp's 32 rows of the owners of its 64 columns
+        for (int owner = cols0 / (128 / KS); owner <= (cols0 + 63) / (128 / KS); ++owner)
+          if (owner != part)
+            copy_to_cta(map_to_rank(E::in(base, part) + quarter * (E::kBytes / 4), (uint32_t)owner),
+                        E::out(base, owner) + quarter * (E::kBytes / 4), E::kBytes / 4, map_to_rank(shared_bar, (uint32_t)owner));
+      }
+      asm volatile("bar.sync 1, 256;" ::: "memory");   // this CTA's own share is there
+      mbar_wait(shared_bar, 0, dead);
+    }
     constexpr int kBlocks = 4 / KS;   // blocks of 32 columns of this CTA's share
     const int block = (warp - 4) >> 2;
     if (warp >= 4 && block < kBlocks) {
@@ -733,19 +757,23 @@ __global__ void __launch_bounds__(GemmShape<CG, TN, NP>::kThreads, 1)
           block_fetch(p.src + b * p.M * p.ld_dst + (int64_t)row0 * p.ld_dst + col0, p.ld_dst, rows, x0);
 #pragma unroll
         for (int i = 0; i < 32; ++i) acc[i] = 0.f;
-        for (int q = 0; q < KS; ++q)
+        for (int q = 0; q < KS; ++q) {
+          const uint32_t share = q == part ? E::out(base, q) : E::in(base, q);
 #pragma unroll
           for (int w = 0; w < 8; ++w) {
-            const uint4 t = lds16(share_at<KS>(base, q, quarter * 32 + lane, block * 8 + w));
+            const uint4 t = lds16(E::word(share, quarter * 32 + lane, block * 8 + w));
             acc[4 * w] += __uint_as_float(t.x);
             acc[4 * w + 1] += __uint_as_float(t.y);
             acc[4 * w + 2] += __uint_as_float(t.z);
             acc[4 * w + 3] += __uint_as_float(t.w);
           }
+        }
         finish_block<NP, MODE, TOUT>(p, cells + (warp - 4) * kCellBytes, b, row0, col0, rows, x0, acc);
       }
     }
     fence_async_global();
+    __syncwarp();
+    cluster_sync();   // the others have what was copied to them from here
   }
   __syncthreads();
   if (*dead) {   // a wait ran out: matrix instructions and the other CTA's copies may still be under way
