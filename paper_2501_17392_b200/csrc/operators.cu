@@ -230,18 +230,20 @@ cudaError_t launch_gemm_as(Operand& a, Operand& b, const GemmArgs& g, cudaStream
   return launch(kernel, dim3((unsigned)(clusters * CG * KS)), Shape::kThreads, Shape::kSmem, CG * KS, st, maps, g);
 }
 
-// CTAs that share the contraction of a tile, where the tiles alone leave SMs idle: sharing costs about 2 us for the
-// exchange and saves its part of the stages (0.2 us each, 0.65 with two planes): 512 x 2048 in float32 259 -> 182 us.
+// CTAs that share the contraction of a tile, where the tiles alone leave SMs idle: sharing costs an exchange and saves
+// its part of the stages (0.2 us each, 0.65 with two planes): 512 x 2048 in float32 259 -> 166 us.  The costs are the
+// ones that choose best between 130 x 130 and 1500 x 1500: with 1 for one plane 512 x 512 takes 111 us for 89, with 2 for
+// two planes 200 x 200 takes 128 us for 119.
 // All clusters have to run at once, and one of 4 CTAs lies within a group of SMs that the hardware wires together: 28
 // always find room, 36 did not (1024 x 1024 took 210 us for 119).
-constexpr double kSplitCost = 2.0;
+constexpr double kSplitCost[2] = {2.0, 1.0};
 int split_of(int64_t tiles, int kblocks, int planes) {
   const double stage = planes == 1 ? 0.2 : 0.65;
   int best = 1;
   double least = kblocks * stage;
   for (int ks = 2; ks <= 4; ks *= 2) {
     if (tiles * ks > (ks == 2 ? sm_count() * 7 / 8 : sm_count() * 3 / 4) || kblocks < ks) break;
-    const double t = (kblocks + ks - 1) / ks * stage + kSplitCost;
+    const double t = (kblocks + ks - 1) / ks * stage + kSplitCost[planes - 1];
     if (t < least) {
       least = t;
       best = ks;
@@ -353,7 +355,7 @@ double tiled_cost(const OrthoPlan& q, int shape) {
     const int64_t kb = (contraction + kTileK - 1) / kTileK;
     const int ks = shape == 0 ? split_of(tiles, (int)kb, q.planes) : 1;
     const double stages = ks > 1 ? (double)((kb + ks - 1) / ks) : (double)((tiles + slots - 1) / slots * kb);
-    return stages * kStage[q.planes - 1][shape] + (ks > 1 ? kSplitCost : 0.0) + kFixed[q.planes - 1][shape];
+    return stages * kStage[q.planes - 1][shape] + (ks > 1 ? kSplitCost[q.planes - 1] : 0.0) + kFixed[q.planes - 1][shape];
   };
   const int64_t half = tm / tn * (sym * (sym + 1) / 2) * q.batch;
   return product(half, q.rows < q.cols ? q.cols : q.rows) + product(half, q.m) + product(tr * tc * q.batch, q.m);
