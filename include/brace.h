@@ -397,7 +397,10 @@ int brace_aggregate_static(int32_t n, int64_t d, const brace_params* params, con
  * failure of these calls is kept per host thread: brace_last_cuda_error(NULL).
  * Matrices are row-major; `ld` and strides count elements, are 64-bit and need
  * no alignment beyond the element's own (rows that start on 16-byte boundaries
- * are read and written in wider words).
+ * are read and written in wider words).  A workspace belongs to one call at a
+ * time: it is free again once that call's work on its stream is complete.  The
+ * first call on a device makes the CUDA runtime load the kernels there: make it
+ * outside any stream capture; later calls may be captured.
  * ------------------------------------------------------------------------- */
 
 /* element types */
@@ -495,7 +498,7 @@ int brace_ortho_status(const void* d_workspace, brace_stream_t stream);
  * no token: its activations are 0 and it adds nothing to the gradient. */
 typedef struct brace_embedding {
   int32_t clients;         /* 0..65535                                                            */
-  int32_t dim;             /* >= 1                                                                */
+  int32_t dim;             /* 1..2^22 (more: BRACE_ERR_UNSUPPORTED)                               */
   int64_t tokens;          /* per client, 0..2^31-1                                               */
   int64_t vocab;           /* rows of a table, 1..2^31-1                                          */
   void* d_table;           /* lookup: read; gradient: written                                     */

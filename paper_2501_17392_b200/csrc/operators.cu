@@ -7,6 +7,7 @@
 
 #include <atomic>
 #include <cmath>
+#include <type_traits>
 
 #include "embedding_kernels.cuh"
 #include "ortho_kernels.cuh"
@@ -263,10 +264,57 @@ cudaError_t launch_gemm(Operand& a, Operand& b, const GemmArgs& g, cudaStream_t 
   return launch_gemm_as<CG, TN, NP, OP_A, OP_B, MODE, TOUT, 1>(a, b, g, st);
 }
 
-template <int CG, int TN, int NP>
-cudaError_t launch_products(const OrthoPlan& q, const brace_ortho_params* p, char* ws,
+// Microseconds of one product in tiles of 128 x 128 (shape 0), 256 x 128 (1) or 256 x 256 (2), the last two by pairs of
+// CTAs: waves of tiles times the stages of one, and what a launch takes beside them.  Fitted to 17 sizes from 200 x 200
+// to 4096 x 4096, off by at most a sixth.  Both sides, one plane: at 512 x 512 shape 0 takes 91 us and 2 takes 137, at
+// 4096 x 4096 1.37 ms and 1.04; two planes: at 1500 x 1500 shape 0 takes 329 us and 1 takes 291.
+int64_t tiles_of(const OrthoPlan& q, bool symmetric, int shape) {
+  const int tm = shape == 0 ? 128 : 256, tn = shape == 2 ? 256 : 128;
+  const int64_t sym = (q.m + tm - 1) / tm, tr = (q.rows + tm - 1) / tm, tc = (q.cols + tn - 1) / tn;
+  return (symmetric ? tm / tn * (sym * (sym + 1) / 2) : tr * tc) * q.batch;
+}
+double product_cost(const OrthoPlan& q, bool symmetric, int contraction, int shape) {
+  static const double kStage[2][3] = {{0.272, 0.239, 0.345}, {0.709, 0.669, 1.15}};
+  static const double kFixed[2][3] = {{3.35, 4.1, 5.8}, {5.4, 5.0, 8.7}};
+  const int64_t slots = sm_count() / (shape == 0 ? 1 : 2), tiles = tiles_of(q, symmetric, shape);
+  const int64_t kb = (contraction + kTileK - 1) / kTileK;
+  const int ks = shape == 0 ? split_of(tiles, (int)kb, q.planes) : 1;
+  const double stages = ks > 1 ? (double)((kb + ks - 1) / ks) : (double)((tiles + slots - 1) / slots * kb);
+  return stages * kStage[q.planes - 1][shape] + (ks > 1 ? kSplitCost[q.planes - 1] : 0.0) + kFixed[q.planes - 1][shape];
+}
+
+// Which shapes a call's products take.  A symmetric result is stored by blocks of as many rows as the tiles have, so
+// either all products take shape 0, or each the better one of the other two.
+struct Shapes {
+  bool pairs, wide_gram, wide_poly, wide_step;
+};
+Shapes choose_shapes(const OrthoPlan& q) {
+  const int n = q.rows < q.cols ? q.cols : q.rows;
+  const bool symmetric[3] = {true, true, false};
+  const int contraction[3] = {n, q.m, q.m};
+  double one = 0, two = 0;
+  bool wide[3];
+  for (int i = 0; i < 3; ++i) {
+    const double narrow = product_cost(q, symmetric[i], contraction[i], 1), broad = product_cost(q, symmetric[i], contraction[i], 2);
+    one += product_cost(q, symmetric[i], contraction[i], 0);
+    wide[i] = broad < narrow;
+    two += wide[i] ? broad : narrow;
+  }
+  return Shapes{two < one, wide[0], wide[1], wide[2]};
+}
+
+// Calls f with the tile's columns: 256 (pairs of CTAs only) or 128.
+template <int CG, typename F>
+cudaError_t with_columns(bool wide, F&& f) {
+  if constexpr (CG == 2)
+    if (wide) return f(std::integral_constant<int, 256>{});
+  return f(std::integral_constant<int, 128>{});
+}
+
+template <int CG, int NP>
+cudaError_t launch_products(const OrthoPlan& q, const Shapes& shapes, const brace_ortho_params* p, char* ws,
                             const GemmArgs& last, int out_type, cudaStream_t st) {
-  constexpr int TM = GemmShape<CG, TN, NP>::kRows;
+  constexpr int TM = 128 * CG;
   const bool tall = q.rows > q.cols;
   const int64_t z = (int64_t)q.batch * q.planes;
   Operand xs[2] = {}, s = {}, t = {}, poly = {};
@@ -285,8 +333,10 @@ cudaError_t launch_products(const OrthoPlan& q, const brace_ortho_params* p, cha
   const int tm = (q.m + TM - 1) / TM;
   GemmArgs sym = {};
   sym.M = sym.N = q.m;
-  sym.tiles = TM / TN * (tm * (tm + 1) / 2);
-  sym.total = sym.tiles * q.batch;
+  auto sym_tiles = [&](GemmArgs& g, int tn) {
+    g.tiles = TM / tn * (tm * (tm + 1) / 2);
+    g.total = g.tiles * q.batch;
+  };
   sym.ld_dst = q.ld_s;
   sym.chunk = q.m >= kLongChunkFrom ? 2 : 1;
   sym.status = (int*)ws;
@@ -294,7 +344,8 @@ cudaError_t launch_products(const OrthoPlan& q, const brace_ortho_params* p, cha
   step.M = q.rows;
   step.N = q.cols;
   step.K = q.m;
-  step.tiles_n = (q.cols + TN - 1) / TN;
+  const int step_columns = CG == 2 && shapes.wide_step ? 256 : 128;
+  step.tiles_n = (q.cols + step_columns - 1) / step_columns;
   step.tiles = step.tiles_n * ((q.rows + TM - 1) / TM);
   step.total = step.tiles * q.batch;
   step.ld_dst = q.ld_x;
@@ -311,8 +362,12 @@ cudaError_t launch_products(const OrthoPlan& q, const brace_ortho_params* p, cha
     g.dst2 = (__half*)(ws + q.off_t);
     g.scale2 = p->c * kFromGram;
     g.diagonal2 = p->b * kSquareScale;
-    cudaError_t err = tall ? launch_gemm<CG, TN, NP, kAcross, kAcross, kModeGram>(x, x, g, st)
-                           : launch_gemm<CG, TN, NP, kAlong, kAlong, kModeGram>(x, x, g, st);
+    cudaError_t err = with_columns<CG>(shapes.wide_gram, [&](auto n) {
+      constexpr int TN = decltype(n)::value;
+      sym_tiles(g, TN);
+      return tall ? launch_gemm<CG, TN, NP, kAcross, kAcross, kModeGram>(x, x, g, st)
+                  : launch_gemm<CG, TN, NP, kAlong, kAlong, kModeGram>(x, x, g, st);
+    });
     if (err != cudaSuccess) return err;
     g = sym;
     g.K = q.m;
@@ -325,40 +380,27 @@ cudaError_t launch_products(const OrthoPlan& q, const brace_ortho_params* p, cha
     }
     g.diagonal = p->a * kSquareScale;
     g.dst = (__half*)(ws + q.off_p);
-    err = launch_gemm<CG, TN, NP, kSymmetric, kSymmetric, kModePoly>(s, NP == 2 ? t : s, g, st);
+    err = with_columns<CG>(shapes.wide_poly, [&](auto n) {
+      constexpr int TN = decltype(n)::value;
+      sym_tiles(g, TN);
+      return launch_gemm<CG, TN, NP, kSymmetric, kSymmetric, kModePoly>(s, NP == 2 ? t : s, g, st);
+    });
     if (err != cudaSuccess) return err;
     step.dst = (__half*)(ws + q.off_x[cur ^ 1]);
-    if (k + 1 < p->steps)
-      err = tall ? launch_gemm<CG, TN, NP, kAlong, kSymmetric, kModeStep>(x, poly, step, st)
-                 : launch_gemm<CG, TN, NP, kSymmetric, kAcross, kModeStep>(poly, x, step, st);
-    else
-      err = with_type(out_type, [&](auto t) {
+    err = with_columns<CG>(shapes.wide_step, [&](auto n) {
+      constexpr int TN = decltype(n)::value;
+      if (k + 1 < p->steps)
+        return tall ? launch_gemm<CG, TN, NP, kAlong, kSymmetric, kModeStep>(x, poly, step, st)
+                    : launch_gemm<CG, TN, NP, kSymmetric, kAcross, kModeStep>(poly, x, step, st);
+      return with_type(out_type, [&](auto t) {
         using TOUT = decltype(t);
         return tall ? launch_gemm<CG, TN, NP, kAlong, kSymmetric, kModeLast, TOUT>(x, poly, step, st)
                     : launch_gemm<CG, TN, NP, kSymmetric, kAcross, kModeLast, TOUT>(poly, x, step, st);
       });
+    });
     if (err != cudaSuccess) return err;
   }
   return cudaSuccess;
-}
-
-// Microseconds of a step's three products with tiles of 128 x 128 (shape 0), 256 x 128 (1) or 256 x 256 (2), the last
-// two by pairs of CTAs: waves of tiles times the stages of one, and what a launch takes beside them.  Fitted to 17 sizes
-// from 200 x 200 to 4096 x 4096, off by at most a sixth.  Both sides, one plane: at 512 x 512 shape 0 takes 91 us and 2
-// takes 137, at 4096 x 4096 1.37 ms and 1.04; two planes: at 1500 x 1500 shape 0 takes 329 us and 1 takes 291.
-double tiled_cost(const OrthoPlan& q, int shape) {
-  static const double kStage[2][3] = {{0.272, 0.239, 0.345}, {0.709, 0.669, 1.15}};
-  static const double kFixed[2][3] = {{3.35, 4.1, 5.8}, {5.4, 5.0, 8.7}};
-  const int tm = shape == 0 ? 128 : 256, tn = shape == 2 ? 256 : 128, slots = sm_count() / (shape == 0 ? 1 : 2);
-  const int64_t sym = (q.m + tm - 1) / tm, tr = (q.rows + tm - 1) / tm, tc = (q.cols + tn - 1) / tn;
-  auto product = [&](int64_t tiles, int contraction) {
-    const int64_t kb = (contraction + kTileK - 1) / kTileK;
-    const int ks = shape == 0 ? split_of(tiles, (int)kb, q.planes) : 1;
-    const double stages = ks > 1 ? (double)((kb + ks - 1) / ks) : (double)((tiles + slots - 1) / slots * kb);
-    return stages * kStage[q.planes - 1][shape] + (ks > 1 ? kSplitCost[q.planes - 1] : 0.0) + kFixed[q.planes - 1][shape];
-  };
-  const int64_t half = tm / tn * (sym * (sym + 1) / 2) * q.batch;
-  return product(half, q.rows < q.cols ? q.cols : q.rows) + product(half, q.m) + product(tr * tc * q.batch, q.m);
 }
 
 cudaError_t launch_prep(const OrthoPlan& q, const PrepArgs& a, cudaStream_t st) {
@@ -443,7 +485,6 @@ int run_ortho(const OrthoPlan& q, const brace_ortho_params* p, PrepArgs prep, co
   prep.ld_x = q.ld_x;
   prep.planes = q.planes;
   prep.status = (int*)ws;
-  cudaGetLastError();
   int slice = 0;
   const int ctas = resident_ctas(q, &slice);
   if (ctas > 0) {
@@ -466,17 +507,11 @@ int run_ortho(const OrthoPlan& q, const brace_ortho_params* p, PrepArgs prep, co
   }
   cudaError_t err = launch_prep(q, prep, st);
   if (err == cudaSuccess) {
-    int shape = 0;
-    for (int i = 1; i < 3; ++i)
-      if (tiled_cost(q, i) < tiled_cost(q, shape)) shape = i;
+    const Shapes shapes = choose_shapes(q);
     if (q.planes == 1)
-      err = shape == 2   ? launch_products<2, 256, 1>(q, p, ws, last, out_type, st)
-            : shape == 1 ? launch_products<2, 128, 1>(q, p, ws, last, out_type, st)
-                         : launch_products<1, 128, 1>(q, p, ws, last, out_type, st);
+      err = shapes.pairs ? launch_products<2, 1>(q, shapes, p, ws, last, out_type, st) : launch_products<1, 1>(q, shapes, p, ws, last, out_type, st);
     else
-      err = shape == 2   ? launch_products<2, 256, 2>(q, p, ws, last, out_type, st)
-            : shape == 1 ? launch_products<2, 128, 2>(q, p, ws, last, out_type, st)
-                         : launch_products<1, 128, 2>(q, p, ws, last, out_type, st);
+      err = shapes.pairs ? launch_products<2, 2>(q, shapes, p, ws, last, out_type, st) : launch_products<1, 2>(q, shapes, p, ws, last, out_type, st);
   }
   return err == cudaSuccess ? BRACE_OK : cuda_fail_no_ctx(err);
 }
@@ -539,9 +574,11 @@ bool emb_sizes_ok(int32_t clients, int64_t tokens, int64_t vocab, int32_t dim) {
   return clients >= 0 && clients <= 65535 && tokens >= 0 && tokens < most && vocab >= 1 && vocab < most && dim >= 1;
 }
 
+constexpr int kMostColumns = 1 << 22;   // stretches of columns are a grid's third dimension: at most 32768 of them
+
 int emb_check(const brace_embedding* e, bool grad) {
   if (!e || !emb_sizes_ok(e->clients, e->tokens, e->vocab, e->dim)) return BRACE_ERR_INVALID_ARG;
-  if (e->dim > (1 << 22)) return BRACE_ERR_UNSUPPORTED;
+  if (e->dim > kMostColumns) return BRACE_ERR_UNSUPPORTED;
   if (!float_type(e->table_type) || !float_type(e->act_type)) return BRACE_ERR_INVALID_ARG;
   if ((e->id_bytes != 4 && e->id_bytes != 8) || !std::isfinite(e->scale)) return BRACE_ERR_INVALID_ARG;
   // what is only read may be broadcast: rows of the gradient's activations that are all the same one
@@ -590,7 +627,6 @@ template <typename TI, typename TO, int V>
 cudaError_t launch_lookup(const EmbArgs& a, cudaStream_t st) {
   constexpr int kWide = 32 * (V >= 8 ? V : V == 2 ? 4 : 4);   // columns of a warp's stretch
   const int64_t x = (a.tokens + 8 * kLookupRows - 1) / (8 * kLookupRows), z = (a.dim + kWide - 1) / kWide;
-  if (z > 65535) return cudaErrorInvalidConfiguration;
   return launch(embedding_lookup_kernel<TI, TO, V>, dim3((unsigned)x, (unsigned)a.clients, (unsigned)z), 256, 0, 1, st, a);
 }
 
@@ -660,7 +696,6 @@ int brace_embedding_lookup(const brace_embedding* e, brace_stream_t stream) {
   a.out = e->d_act;
   const cudaStream_t st = (cudaStream_t)stream;
   const int width = emb_width(e);
-  cudaGetLastError();
   const cudaError_t err = with_type(e->table_type, [&](auto ti) {
     return with_type(e->act_type, [&](auto to) {
       using TI = decltype(ti);
@@ -694,7 +729,6 @@ int brace_embedding_grad(const brace_embedding* e, void* d_workspace, size_t wor
   a.part = (float*)(ws + q.off_part);
   a.parts = q.parts;
   const cudaStream_t st = (cudaStream_t)stream;
-  cudaGetLastError();
   cudaError_t err = cudaSuccess;
   if (a.tokens > 0) {
     err = a.tokens <= kSortTile ? launch_sort(a, st) : launch_wide_sort(a, q, ws, st);

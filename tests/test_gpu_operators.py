@@ -79,6 +79,25 @@ def test_orthogonalize_shapes(shape, precision):
         assert rel(out[e], want[e]) <= bound(precision, F32)
 
 
+# sizes that take the products' other tile shapes and the shared contractions, wide and tall
+@pytest.mark.parametrize("shape", [(1, 300, 2400), (1, 2400, 300), (1, 600, 600), (2, 700, 1100), (1, 1500, 1500),
+                                   (1, 1800, 2100), (1, 2100, 1800), (3, 1990, 2000), (1, 2900, 3300), (1, 3300, 2900)])
+@pytest.mark.parametrize("precision", [B.ORTHO_HALF, B.ORTHO_SINGLE])
+def test_orthogonalize_large(shape, precision):
+    b, r, c = shape
+    g = randn(b, r, c, seed=r + c, scale=10.0)
+    out = torch.full((b, r, c), 7.0, device="cuda")
+    plan = B.Orthogonalizer(r, c, batch=b, params=B.ortho_params(precision=precision))
+    plan.orthogonalize(g, out)
+    plan.check()
+    again = torch.empty_like(out)
+    plan.orthogonalize(g, again)
+    assert torch.equal(out, again)
+    want = direction64(g)
+    for e in range(b):
+        assert rel(out[e], want[e]) <= bound(precision, F32)
+
+
 @pytest.mark.parametrize("tin", [F32, BF16, F16])
 @pytest.mark.parametrize("tout", [F32, BF16, F16])
 def test_orthogonalize_types(tin, tout):
@@ -237,6 +256,18 @@ def test_muon_step(shape, tg, tw, nesterov):
     assert torch.equal(m, m_out) and torch.equal(w, w_out)
 
 
+@pytest.mark.parametrize("shape", [(1, 400, 1500), (1, 1600, 1600), (2, 2000, 1300)])
+@pytest.mark.parametrize("tw", [F32, BF16])
+def test_muon_step_large(shape, tw):
+    g, m, w = randn(*shape, seed=1).to(BF16), randn(*shape, seed=2), randn(*shape, seed=3, scale=0.05).to(tw)
+    want_m, want_w, step = muon64(g, m, w, 0.03, 0.9, True, 0.1, 1.5)
+    plan = B.Orthogonalizer(shape[1], shape[2], batch=shape[0])
+    plan.muon_step(g, m, w, 0.03, beta=0.9, weight_decay=0.1, scale=1.5)
+    plan.check()
+    limit = TOL[AUTO[tw]] * step.norm() + (4 * U[F32] + U[tw]) * (want_w.norm() + step.norm())
+    assert float((w.double() - want_w).norm()) <= float(limit)
+
+
 @pytest.mark.parametrize("tw", [F32, BF16])
 def test_muon_step_for_replicas(tw):
     # the weights are rows of clients' parameter vectors; all take the step, nothing between them is touched
@@ -375,6 +406,16 @@ def test_grad_of_broadcast_activations():
     out = torch.empty(2, 50, 32, device="cuda")
     B.Embedding(50, 32, 400, clients=2).grad(dy, ids, out)
     total, size, count = grad64(dy, ids, 50, 1.0)
+    assert bool(((out.double() - total).abs() <= (count + 3) * 2 ** -24 * size).all())
+
+
+@pytest.mark.parametrize("tokens,vocab", [(600_000, 5000), (524_289, 300_000)])
+def test_grad_of_long_texts(tokens, vocab):
+    # several tokens' tiles a CTA in the wide sort (256 tiles at most), two and three passes
+    dy, ids = randn(1, tokens, 4, seed=1), ids_of(1, tokens, vocab, seed=3)
+    out = torch.empty(1, vocab, 4, device="cuda")
+    B.Embedding(vocab, 4, tokens).grad(dy, ids, out)
+    total, size, count = grad64(dy, ids, vocab, 1.0)
     assert bool(((out.double() - total).abs() <= (count + 3) * 2 ** -24 * size).all())
 
 
