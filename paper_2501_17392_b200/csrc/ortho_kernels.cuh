@@ -256,7 +256,8 @@ struct GemmMaps {
 template <int CG, int TN, int NP>
 struct GemmShape {
   static constexpr int kRows = 128 * CG;
-  static constexpr int kEpiWarps = TN / 16;                  // a warp takes 32 rows x 64 columns of the CTA's part
+  static constexpr int kColumns = TN / 4;                    // an epilogue warp takes 32 rows of so many columns
+  static constexpr int kEpiWarps = 16;
   static constexpr int kThreads = 128 + 32 * kEpiWarps;      // warps 0-3: loads, MMAs, tensor memory, -; then epilogue
   static constexpr int kBytesB = TN / CG * kTileK * 2;       // each CTA of a pair loads half of the columns' operand
   static constexpr int kStageBytes = NP * (kOperandBytes + kBytesB);
@@ -526,7 +527,8 @@ __global__ void __launch_bounds__(GemmShape<CG, TN, NP>::kThreads, 1)
 
   // the launch's registers (640 threads x 96) go to the warps that hold accumulators: 4 x 32 x 32 + 16 x 32 x 112
   if (TN == 256 && warp < 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 32;");
-  float acc[NP == 1 && KS == 1 ? 32 : 64];
+  constexpr int kAcc = NP == 1 ? 32 : Shape::kColumns;
+  float acc[kAcc];
   if (warp == 0) {
     const bool lead = elect_one();
     const uint32_t full0 = CG == 1 ? full : map_to_rank(full, 0);
@@ -642,7 +644,7 @@ __global__ void __launch_bounds__(GemmShape<CG, TN, NP>::kThreads, 1)
     if (TN == 256) asm volatile("setmaxnreg.inc.sync.aligned.u32 112;");
     const uint32_t tm_empty0 = CG == 1 ? tm_empty : map_to_rank(tm_empty, 0);
     const int quarter = warp & 3;                          // the 32 lanes of tensor memory this warp can read
-    const int cols0 = ((warp - 4) >> 2) * 64;
+    const int cols0 = ((warp - 4) >> 2) * Shape::kColumns;
     const uint32_t cell = cells + (warp - 4) * kCellBytes;
     const uint32_t tm_mine = tmem + ((uint32_t)(quarter * 32) << 16) + cols0;
     int buf = 0;
@@ -669,12 +671,12 @@ __global__ void __launch_bounds__(GemmShape<CG, TN, NP>::kThreads, 1)
       const int rows = min(32, p.M - row0);   // may be none: the accumulators are then read for nothing
       // rows are padded to 64 columns; the pad is written too (the operands' pads are zeros, so it stays zero)
       const bool live = rows > 0 && col0 < p.N;
-      if (MODE == kModeLast) prefetch_weights<TOUT>(p, b, row0 + lane, col0, 64);
+      if (MODE == kModeLast) prefetch_weights<TOUT>(p, b, row0 + lane, col0, Shape::kColumns);
       uint4 x0[4], x1[4];
       if (MODE == kModePoly && NP == 1 && KS == 1 && live) {
         const __half* src = p.src + b * p.M * p.ld_dst + (int64_t)row0 * p.ld_dst + col0;
         block_fetch(src, p.ld_dst, rows, x0);
-        block_fetch(src + 32, p.ld_dst, rows, x1);
+        if (Shape::kColumns == 64) block_fetch(src + 32, p.ld_dst, rows, x1);
       }
       if (NP == 2) {
         for (int kb = kfirst; kb < kblocks; kb += p.chunk) {
@@ -684,11 +686,11 @@ __global__ void __launch_bounds__(GemmShape<CG, TN, NP>::kThreads, 1)
           }
           tc_fence_after();
 #pragma unroll
-          for (int q = 0; q < 4; ++q) {
+          for (int q = 0; q < Shape::kColumns / 16; ++q) {
             float v[16];
             tmem_load16(tm_mine + buf * TN + 16 * q, v);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) acc[(16 * q + i) & (NP * 32 - 1)] = (kb > kfirst ? acc[(16 * q + i) & (NP * 32 - 1)] : 0.f) + v[i];
+            for (int i = 0; i < 16; ++i) acc[(16 * q + i) % kAcc] = (kb > kfirst ? acc[(16 * q + i) % kAcc] : 0.f) + v[i];
           }
           release();
         }
@@ -699,19 +701,15 @@ __global__ void __launch_bounds__(GemmShape<CG, TN, NP>::kThreads, 1)
       }
       if (!ok) break;
       if constexpr (KS > 1) {
-        if (NP == 1) {
-#pragma unroll
-          for (int h = 0; h < 2; ++h)
-            tmem_load32(tm_mine + buf * TN + 32 * h, *reinterpret_cast<float(*)[32]>(acc + 32 * h));
-        }
+        if (NP == 1) tmem_load32(tm_mine + buf * TN, *reinterpret_cast<float(*)[32]>(acc));
         break;   // one tile; it is finished below
       } else {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        for (int h = 0; h < Shape::kColumns / 32; ++h) {
           float* v = acc + (NP == 1 ? 0 : 32 * h);
           if (NP == 1) {
             tmem_load32(tm_mine + buf * TN + 32 * h, *reinterpret_cast<float(*)[32]>(v));
-            if (h == 1) release();
+            if (h + 1 == Shape::kColumns / 32) release();
           }
           if (live) finish_block<NP, MODE, TOUT>(p, cell, b, row0, col0 + 32 * h, rows, h == 0 ? x0 : x1, v);
         }
@@ -723,28 +721,25 @@ __global__ void __launch_bounds__(GemmShape<CG, TN, NP>::kThreads, 1)
     using E = Exchange<KS>;
     int b, ti, tj;
     place(cluster, b, ti, tj);
-    const int quarter = warp & 3, cols0 = ((warp - 4) >> 2) * 64;
+    const int quarter = warp & 3, cols0 = ((warp - 4) >> 2) * 32, owner = cols0 / (128 / KS);   // of this warp's columns
     cluster_arrive();   // once all are here, no matrix instruction or load uses the stages any more
     if (warp >= 4) {
 #pragma unroll
-      for (int w = 0; w < 16; ++w) {
-        const int word = cols0 / 4 + w, owner = word / E::kWords;
-        sts16(E::word(E::out(base, owner), quarter * 32 + lane, word - owner * E::kWords),
+      for (int w = 0; w < 8; ++w)
+        sts16(E::word(E::out(base, owner), quarter * 32 + lane, cols0 / 4 + w - owner * E::kWords),
               make_uint4(__float_as_uint(acc[4 * w]), __float_as_uint(acc[4 * w + 1]), __float_as_uint(acc[4 * w + 2]),
                          __float_as_uint(acc[4 * w + 3])));
-      }
       fence_async();
+      // 32 rows of an owner's share are one piece: KS == 2 has two warps' words in each row
+      if (KS == 2) asm volatile("bar.sync %0, 64;" ::"r"(2 + quarter * 2 + owner) : "memory");
     }
     __syncwarp();
     cluster_wait();
     if (warp >= 4) {
-      if (lane == 0) {   // this warp's 32 rows of the owners of its 64 columns
-        for (int owner = cols0 / (128 / KS); owner <= (cols0 + 63) / (128 / KS); ++owner)
-          if (owner != part)
-            copy_to_cta(map_to_rank(E::in(base, part) + quarter * (E::kBytes / 4), (uint32_t)owner),
-                        E::out(base, owner) + quarter * (E::kBytes / 4), E::kBytes / 4, map_to_rank(shared_bar, (uint32_t)owner));
-      }
-      asm volatile("bar.sync 1, 256;" ::: "memory");   // this CTA's own share is there
+      if (lane == 0 && owner != part && (KS == 4 || ((warp - 4) >> 2) % 2 == 0))
+        copy_to_cta(map_to_rank(E::in(base, part) + quarter * (E::kBytes / 4), (uint32_t)owner),
+                    E::out(base, owner) + quarter * (E::kBytes / 4), E::kBytes / 4, map_to_rank(shared_bar, (uint32_t)owner));
+      asm volatile("bar.sync 1, 512;" ::: "memory");   // this CTA's own share is there
       mbar_wait(shared_bar, 0, dead);
     }
     constexpr int kBlocks = 4 / KS;   // blocks of 32 columns of this CTA's share
