@@ -14,18 +14,17 @@
 namespace brace {
 
 constexpr uint32_t kNoToken = 0xffffffffu;   // sorts behind every id
+constexpr int kDirectTokens = 2048;          // up to so many tokens no sort is needed: one launch does it all
 constexpr int kSortItems = 4;                // elements per thread of the sort
 constexpr int kSortThreads = 512;
-constexpr int kSortTile = kSortThreads * kSortItems;   // elements one CTA sorts
-constexpr int kDigitBits = 6;
-constexpr int kDigits = 1 << kDigitBits;
-constexpr int kCountRow = kDigits + 1;
-// More tokens than a CTA sorts: digits of 9 bits, tiles of a multiple of kSortTile tokens, at most kMostTiles a client.
+constexpr int kSortTile = kSortThreads * kSortItems;
+// The sort: digits of 9 bits, tiles of a multiple of kSortTile tokens, at most kMostTiles a client.
 constexpr int kWideBits = 9;
 constexpr int kWideDigits = 1 << kWideBits;
 constexpr int kMostTiles = 256;
 constexpr int kPart = 32;                    // sorted tokens of a group: a CTA's share of the sums
 constexpr int kManyGroups = 16;              // from here on a whole CTA adds a row's partial sums
+constexpr int kManyTokens = 16;              // ... or its tokens, where there are few in all
 
 struct EmbArgs {
   const void* table;      // lookup: the table
@@ -57,7 +56,8 @@ __device__ __forceinline__ int64_t load_id(const EmbArgs& p, int64_t c, int64_t 
 
 // ---- lookup -----------------------------------------------------------------------------------------------------
 // A warp takes kLookupRows rows and of each a stretch of 32 V Q columns, all loads first.  Rows that do not start on
-// whole words are read and written element by element, 32 neighbours at a time.
+// whole words are read and written element by element, 32 neighbours at a time.  Bound by HBM: 16 x 8192 rows of 768 in
+// 62 us, 0.92 of the copy rate by the rows read once and written once (threads that divided a flat index took 79 us).
 constexpr int kLookupRows = 4;
 
 template <typename TI, typename TO, int V>
@@ -121,105 +121,9 @@ __device__ __forceinline__ uint32_t same_digit(uint32_t digit) {
   return same;
 }
 
-// One CTA sorts up to a tile of consecutive tokens of a client by id: least significant digit first, 6 bits at a
-// time.  A warp holds 32 * ITEMS consecutive elements; equal digits within 32 are ranked by ballots, across the warp's
-// rounds by a counter per (digit, warp), across warps by a scan of the counters.
-template <int ITEMS>
-__global__ void __launch_bounds__(1024) embedding_sort_kernel(const EmbArgs p, int tile, int bits) {
-  extern __shared__ uint32_t sort_smem[];
-  uint32_t* s_key = sort_smem;                                   // [tile]
-  uint32_t* s_pos = s_key + tile;                                // [tile]
-  uint32_t* s_count = s_pos + tile;                              // [warps][kDigits + 1]: a warp's digits in different banks
-  __shared__ uint32_t s_warp[32];
-  grid_wait();
-  grid_trigger();
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
-  const int64_t c = blockIdx.y, first = (int64_t)blockIdx.x * tile;
-  const int n = (int)min((int64_t)tile, p.tokens - first);
-  uint32_t key[ITEMS], pos[ITEMS];
-#pragma unroll
-  for (int i = 0; i < ITEMS; ++i) {
-    const int k = (warp * ITEMS + i) * 32 + lane;
-    key[i] = kNoToken;
-    pos[i] = (uint32_t)(first + k);
-    if (k < n) {
-      const int64_t id = load_id(p, c, first + k);
-      if (id >= 0 && id < p.vocab) key[i] = (uint32_t)id;
-    }
-  }
-  for (int shift = 0; shift < bits; shift += kDigitBits) {
-    for (int i = tid; i < kCountRow * warps; i += blockDim.x) s_count[i] = 0;
-    __syncthreads();
-    uint32_t rank[ITEMS];
-#pragma unroll
-    for (int i = 0; i < ITEMS; ++i) {
-      const uint32_t digit = (key[i] >> shift) & (kDigits - 1);
-      const uint32_t same = same_digit<kDigitBits>(digit);
-      const uint32_t before = s_count[warp * kCountRow + digit];
-      rank[i] = before + __popc(same & ((1u << lane) - 1u));
-      __syncwarp();
-      if (lane == __ffs(same) - 1) s_count[warp * kCountRow + digit] = before + __popc(same);
-      __syncwarp();
-    }
-    __syncthreads();
-    // exclusive scan of the counters in (digit, warp) order: each thread takes two neighbours
-    constexpr int kPer = kDigits / 32;
-    uint32_t own[kPer], sum = 0;
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      const int k = tid * kPer + i;
-      own[i] = s_count[k % warps * kCountRow + k / warps];
-      sum += own[i];
-    }
-    uint32_t incl = sum;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const uint32_t v = __shfl_up_sync(0xffffffffu, incl, o);
-      if (lane >= o) incl += v;
-    }
-    if (lane == 31) s_warp[warp] = incl;
-    __syncthreads();
-    uint32_t offset = lane < warp ? s_warp[lane] : 0;
-#pragma unroll
-    for (int o = 16; o; o >>= 1) offset += __shfl_xor_sync(0xffffffffu, offset, o);
-    uint32_t run = offset + incl - sum;
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      const int k = tid * kPer + i;
-      s_count[k % warps * kCountRow + k / warps] = run;
-      run += own[i];
-    }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < ITEMS; ++i) {
-      const uint32_t digit = (key[i] >> shift) & (kDigits - 1);
-      const uint32_t to = s_count[warp * kCountRow + digit] + rank[i];
-      s_key[to] = key[i];
-      s_pos[to] = pos[i];
-    }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < ITEMS; ++i) {
-      const int k = (warp * ITEMS + i) * 32 + lane;
-      key[i] = s_key[k];
-      pos[i] = s_pos[k];
-    }
-    __syncthreads();
-  }
-  // what is no token was given the largest key and comes last, after the padding of the tile in its turn
-  uint32_t* out_key = p.key + c * p.tokens + first;
-  uint32_t* out_pos = p.pos + c * p.tokens + first;
-#pragma unroll
-  for (int i = 0; i < ITEMS; ++i) {
-    const int k = (warp * ITEMS + i) * 32 + lane;
-    if (k < n) {
-      out_key[k] = key[i];
-      out_pos[k] = pos[i];
-    }
-  }
-}
-
-// Tokens beyond what one CTA sorts: least significant digit first over tiles.  hist[pass][client][tile][digit] counts
+// More tokens: least significant digit first over tiles.  16 x 8192 ids of 17 bits take 21 us in three launches, bound by
+// the latency of each; sorting them in one CTA a client took 20 us and grew with the tokens, merging sorted runs by
+// searches 20 us a level.  hist[pass][client][tile][digit] counts
 // the digits of a pass in each tile of its input.  This kernel counts the first pass and clears the others' counts.
 __global__ void __launch_bounds__(kSortThreads) embedding_count_kernel(const EmbArgs p, uint32_t* hist, int64_t tile, int passes) {
   __shared__ uint32_t s_count[kWideDigits];
@@ -412,6 +316,8 @@ struct Share {
   }
 };
 
+// Bound by the latency of scattered rows: 16 x 8192 tokens of 768 in 85 us, 2.4 TB/s of activations (with one row in
+// flight a warp it took 98).
 // A CTA takes a group of kPart sorted tokens: notes where each id's tokens begin and end, writes the rows of the ids
 // whose tokens all lie in the group, and leaves a partial sum of an id that goes on before ([0]) or only after ([1]).
 template <typename TI, typename TO, int V>
@@ -524,7 +430,6 @@ __global__ void __launch_bounds__(256, 4) embedding_sum_kernel(const EmbArgs p) 
 // Whether id v has tokens.  The table's entry counts only where the key it points at says so: that of an id without
 // tokens holds whatever was in the workspace.
 __device__ __forceinline__ bool has_tokens(const EmbArgs& p, int64_t c, int64_t v) {
-  if (p.tokens == 0) return false;
   const uint32_t at = p.span[c * p.vocab + v].x;
   return (int64_t)at < p.tokens && p.key[c * p.tokens + at] == (uint32_t)v;
 }
@@ -543,6 +448,128 @@ __device__ __forceinline__ void zero_run(T* p, uint32_t n) {
   if (tail + lane < n) p[tail + lane] = zero;
 }
 
+// Few tokens (up to kDirectTokens): every CTA looks through all of a client's ids for those of its rows_cta rows, puts
+// what it finds in order by row, and writes its rows, zeros and sums.  One launch: at 33 tokens, 256 x 64, 3.6 us against
+// 8.2 for a sort, sums and zeros as launches of their own; at 2048 tokens, 50000 x 768, 31 us against 35.
+template <typename TI, typename TO, int V>
+__global__ void __launch_bounds__(256, 4) embedding_direct_kernel(const EmbArgs p) {
+  using S = Share<V>;
+  __shared__ float s_sum[8][S::kWide];
+  __shared__ uint16_t s_found[kDirectTokens], s_sorted[kDirectTokens];
+  __shared__ uint8_t s_of[kDirectTokens];
+  __shared__ int s_count[64], s_first[64], s_warp[8];
+  __shared__ uint8_t s_rows[64];
+  __shared__ int s_some;
+  const int64_t c = blockIdx.y, v0 = (int64_t)blockIdx.x * p.rows_cta;
+  const int rows = (int)min((int64_t)p.rows_cta, p.vocab - v0);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x < 64) s_count[threadIdx.x] = 0;
+  grid_wait();
+  grid_trigger();
+  __syncthreads();
+  // neighbouring tokens to a thread, so that the threads' finds follow one another in the tokens' order
+  const int tokens = (int)p.tokens, per = (tokens + 255) / 256, t0 = threadIdx.x * per;
+  int row[kDirectTokens / 256], n = 0;
+#pragma unroll
+  for (int i = 0; i < kDirectTokens / 256; ++i) {
+    row[i] = -1;
+    if (i < per && t0 + i < tokens) {
+      const int64_t r = load_id(p, c, t0 + i) - v0;
+      if (r >= 0 && r < rows) {
+        row[i] = (int)r;
+        ++n;
+        atomicAdd(&s_count[r], 1);
+      }
+    }
+  }
+  int incl = n;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int v = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += v;
+  }
+  if (lane == 31) s_warp[warp] = incl;
+  __syncthreads();
+  int at = incl - n, found = 0;
+#pragma unroll
+  for (int w = 0; w < 8; ++w) {
+    at += w < warp ? s_warp[w] : 0;
+    found += s_warp[w];
+  }
+#pragma unroll
+  for (int i = 0; i < kDirectTokens / 256; ++i)
+    if (row[i] >= 0) {
+      s_found[at] = (uint16_t)(t0 + i);
+      s_of[at++] = (uint8_t)row[i];
+    }
+  TO* grad = (TO*)p.grad + c * p.stride_table + v0 * p.ld_table;
+  // the columns are shared by gridDim.z CTAs, so that a frequent token's row is not one CTA's work
+  const int all_blocks = (p.dim + S::kWide - 1) / S::kWide;
+  const int block0 = all_blocks * (int)blockIdx.z / (int)gridDim.z, block1 = all_blocks * ((int)blockIdx.z + 1) / (int)gridDim.z;
+  const uint32_t width = (uint32_t)(min(block1 * S::kWide, p.dim) - block0 * S::kWide);
+  TO* zeros = grad + block0 * S::kWide;
+  if (found == 0) {   // most CTAs of a large table
+    if (!p.accumulate)
+      for (int r = warp; r < rows; r += 8) zero_run(zeros + (int64_t)r * p.ld_table, width);
+    return;
+  }
+  __syncthreads();
+  if (warp == 0) {   // by row, in the tokens' order: two rows' counts a lane, then 32 finds at a time
+    const int a = s_count[2 * lane], b = s_count[2 * lane + 1];
+    int sum = a + b;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int v = __shfl_up_sync(0xffffffffu, sum, o);
+      if (lane >= o) sum += v;
+    }
+    s_first[2 * lane] = sum - a - b;
+    s_first[2 * lane + 1] = sum - b;
+    const uint32_t ma = __ballot_sync(0xffffffffu, a > 0), mb = __ballot_sync(0xffffffffu, b > 0);
+    const uint32_t below = (1u << lane) - 1u;
+    int k = __popc(ma & below) + __popc(mb & below);   // rows that have tokens
+    if (a > 0) s_rows[k++] = (uint8_t)(2 * lane);
+    if (b > 0) s_rows[k] = (uint8_t)(2 * lane + 1);
+    if (lane == 0) s_some = __popc(ma) + __popc(mb);
+    __syncwarp();
+    for (int i = 0; i < found; i += 32) {
+      const bool live = i + lane < found;
+      const uint32_t r = live ? s_of[i + lane] : 0;
+      const uint32_t same = same_digit<6>(r) & __ballot_sync(0xffffffffu, live);
+      const int to = s_first[r] + __popc(same & below);
+      __syncwarp();
+      if (live) {
+        s_sorted[to] = s_found[i + lane];
+        if (lane == __ffs(same) - 1) s_first[r] = to + __popc(same);   // (the first lane's place is the rows' next one)
+      }
+      __syncwarp();
+    }
+  } else if (!p.accumulate) {
+    for (int r = warp - 1; r < rows; r += 7)
+      if (s_count[r] == 0) zero_run(zeros + (int64_t)r * p.ld_table, width);
+  }
+  __syncthreads();
+  // s_first now is where a row's tokens end
+  const int some = s_some;
+  const TI* dy = (const TI*)p.in + c * p.stride_act;
+  int turn = 0;
+  for (int k = 0; k < some; ++k) {
+    const int r = s_rows[k], m = s_count[r], first = s_first[r] - m;
+    TO* out = grad + (int64_t)r * p.ld_table;
+    for (int b = block0; b < block1; ++b) {
+      const int col = b * S::kWide + lane * V, left = p.dim - col;
+      const bool all = m > kManyTokens;   // the whole CTA for a frequent token, else a warp
+      if (!all && (turn++ & 7) != warp) continue;
+      const int from = all ? m * warp / 8 : 0, to = all ? m * (warp + 1) / 8 : m;
+      S share;
+      share.clear();
+      share.template add<TI>(to - from, left, [&](int t) { return dy + (int64_t)s_sorted[first + from + t] * p.ld_act + col; });
+      if (all) share.join(s_sum, 0, 8);
+      if (!all || warp == 0) share.to_row(out + col, left, p.scale, p.accumulate);
+    }
+  }
+}
+
+// Bound by HBM's writes: 16 x 50000 x 768 floats in 338 us, 6.7 TB/s.
 // The rest of the table's gradient.  The first zero_ctas CTAs of a client write zeros to the rows of ids without tokens,
 // rows_cta (up to 64) each.  The others look at 8 groups each for an id whose tokens begin there and go on, and add
 // the partial sums of its groups for their share of the columns.

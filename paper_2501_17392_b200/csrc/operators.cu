@@ -551,19 +551,19 @@ EmbPlan emb_plan(int32_t clients, int64_t tokens, int64_t vocab, int32_t dim) {
     return here;
   };
   const int64_t n = (int64_t)clients * tokens;
-  const bool wide = tokens > kSortTile;
+  const bool wide = tokens > kDirectTokens;
   const int64_t per = ((tokens + kSortTile - 1) / kSortTile + kMostTiles - 1) / kMostTiles;
   q.tile = per * kSortTile;
   q.tiles = wide ? (int)((tokens + q.tile - 1) / q.tile) : 0;
   q.passes = 0;
   while ((vocab >> (q.passes * kWideBits)) != 0) ++q.passes;   // the largest value of these bits stands for "no token"
   for (int i = 0; i < 2; ++i) {
-    q.off_key[i] = take(i == 0 || wide ? 4 * n : 0);
-    q.off_pos[i] = take(i == 0 || wide ? 4 * n : 0);
+    q.off_key[i] = take(wide ? 4 * n : 0);
+    q.off_pos[i] = take(wide ? 4 * n : 0);
   }
   q.off_hist = take((int64_t)q.passes * clients * q.tiles * kWideDigits * 4);
-  q.off_span = take(8 * (int64_t)clients * vocab);
-  q.parts = (tokens + kPart - 1) / kPart;
+  q.off_span = take(wide ? 8 * (int64_t)clients * vocab : 0);
+  q.parts = wide ? (tokens + kPart - 1) / kPart : 0;
   q.off_part = take((int64_t)clients * q.parts * 2 * dim * 4);
   q.bytes = at > 256 ? at : 256;
   return q;
@@ -630,20 +630,8 @@ cudaError_t launch_lookup(const EmbArgs& a, cudaStream_t st) {
   return launch(embedding_lookup_kernel<TI, TO, V>, dim3((unsigned)x, (unsigned)a.clients, (unsigned)z), 256, 0, 1, st, a);
 }
 
-cudaError_t launch_sort(const EmbArgs& a, cudaStream_t st) {
-  int bits = 0;
-  while ((a.vocab >> bits) != 0) ++bits;   // the largest value of these bits stands for "no token"
-  if (a.tokens <= 1024) {
-    const int threads = (int)round_up(a.tokens, 32);
-    const size_t smem = (size_t)threads * 8 + (size_t)kCountRow * (threads / 32) * 4;
-    return launch(embedding_sort_kernel<1>, dim3(1, (unsigned)a.clients), threads, smem, 1, st, a, threads, bits);
-  }
-  const size_t smem = (size_t)kSortTile * 8 + (size_t)kCountRow * (kSortThreads / 32) * 4;
-  return launch(embedding_sort_kernel<kSortItems>, dim3(1, (unsigned)a.clients), kSortThreads, smem, 1, st, a, kSortTile, bits);
-}
-
-// Sorts more tokens than that; leaves a.key and a.pos at the result.
-cudaError_t launch_wide_sort(EmbArgs& a, const EmbPlan& q, char* ws, cudaStream_t st) {
+// Sorts the tokens; leaves a.key and a.pos at the result.
+cudaError_t launch_sort(EmbArgs& a, const EmbPlan& q, char* ws, cudaStream_t st) {
   const dim3 grid((unsigned)q.tiles, (unsigned)a.clients);
   uint32_t* hist = (uint32_t*)(ws + q.off_hist);
   cudaError_t err = launch(embedding_count_kernel, grid, kSortThreads, 0, 1, st, a, hist, q.tile, q.passes);
@@ -661,24 +649,35 @@ constexpr int64_t kGradElements = 32768;   // of a CTA's rows
 
 template <typename TI, typename TO, int V>
 cudaError_t launch_grad(EmbArgs a, cudaStream_t st) {
-  if (a.tokens > 0) {
-    // few groups: their columns are shared out until every SM has four CTAs
-    const int64_t blocks = (a.dim + Share<V>::kWide - 1) / Share<V>::kWide, groups = a.parts * a.clients;
-    int64_t z = 4 * sm_count() / groups;
+  if (a.tokens <= kDirectTokens) {
+    const int64_t blocks = (a.dim + Share<V>::kWide - 1) / Share<V>::kWide;
+    // The columns are shared out, unless the table is far larger than L2: a frequent token's row is then more than one
+    // CTA's work (2000 tokens, 1000 x 777: 40 -> 21 us), but lines that two CTAs write in part cost DRAM accesses where
+    // L2 does not hold them (8 x 50000 x 777: 211 -> 370 us).
+    int64_t z = a.vocab * a.clients * a.dim > ((int64_t)32 << 20) ? 1 : a.dim / 256;
     z = z < 1 ? 1 : z > blocks ? blocks : z;
-    const cudaError_t err = launch(embedding_sum_kernel<TI, TO, V>, dim3((unsigned)a.parts, (unsigned)a.clients, (unsigned)z), 256, 0, 1, st, a);
-    if (err != cudaSuccess) return err;
+    int64_t rows = kGradElements * z / a.dim;
+    const int64_t even = a.vocab * a.clients * z / (4 * sm_count());
+    if (rows > even) rows = even;
+    a.rows_cta = rows < 1 ? 1 : rows > 64 ? 64 : (int)rows;
+    return launch(embedding_direct_kernel<TI, TO, V>,
+                  dim3((unsigned)((a.vocab + a.rows_cta - 1) / a.rows_cta), (unsigned)a.clients, (unsigned)z), 256, 0, 1, st, a);
   }
   // long runs of zeros, but 4 CTAs for each SM while the table has the rows
   int64_t rows = kGradElements / a.dim;
   const int64_t even = a.vocab * a.clients / (4 * sm_count());
   if (rows > even) rows = even;
   a.rows_cta = rows < 1 ? 1 : rows > 64 ? 64 : (int)rows;
-  a.zero_ctas = a.accumulate ? 0 : (unsigned)((a.vocab + a.rows_cta - 1) / a.rows_cta);
-  const int64_t blocks = (a.dim + Share<V>::kWide - 1) / Share<V>::kWide, eights = (a.parts + 7) / 8;
+  const unsigned row_ctas = (unsigned)((a.vocab + a.rows_cta - 1) / a.rows_cta);
+  const int64_t blocks = (a.dim + Share<V>::kWide - 1) / Share<V>::kWide, groups = a.parts * a.clients;
+  // few groups: their columns are shared out until every SM has four CTAs
+  int64_t z = 4 * sm_count() / groups;
+  z = z < 1 ? 1 : z > blocks ? blocks : z;
+  const cudaError_t err = launch(embedding_sum_kernel<TI, TO, V>, dim3((unsigned)a.parts, (unsigned)a.clients, (unsigned)z), 256, 0, 1, st, a);
+  if (err != cudaSuccess) return err;
+  a.zero_ctas = a.accumulate ? 0 : row_ctas;
   a.join_split = (unsigned)(blocks < 16 ? blocks : 16);
-  const int64_t ctas = a.zero_ctas + eights * a.join_split;
-  if (ctas == 0) return cudaSuccess;
+  const int64_t ctas = a.zero_ctas + (a.parts + 7) / 8 * a.join_split;
   return launch(embedding_grad_kernel<TO, V>, dim3((unsigned)ctas, (unsigned)a.clients), 256, 0, 1, st, a);
 }
 
@@ -730,9 +729,7 @@ int brace_embedding_grad(const brace_embedding* e, void* d_workspace, size_t wor
   a.parts = q.parts;
   const cudaStream_t st = (cudaStream_t)stream;
   cudaError_t err = cudaSuccess;
-  if (a.tokens > 0) {
-    err = a.tokens <= kSortTile ? launch_sort(a, st) : launch_wide_sort(a, q, ws, st);
-  }
+  if (a.tokens > kDirectTokens) err = launch_sort(a, q, ws, st);
   if (err == cudaSuccess) {
     const int width = emb_width(e);
     err = with_type(e->act_type, [&](auto ti) {
