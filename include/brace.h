@@ -413,7 +413,7 @@ enum {
 
 /* accuracy of the orthogonalisation */
 enum {
-  BRACE_ORTHO_AUTO = 0,  /* HALF for bfloat16 results, SINGLE for float32 and float16              */
+  BRACE_ORTHO_AUTO = 0,  /* HALF for bfloat16 results (short side above 32), SINGLE for all others */
   BRACE_ORTHO_HALF = 1,  /* operands of the products rounded to 11 bits, sums in float32          */
   BRACE_ORTHO_SINGLE = 2 /* operands held to 22 bits, sums in float32: three times the products   */
 };

@@ -76,6 +76,7 @@ cudaError_t with_type(int type, F&& f) {
 
 // ---- the orthogonalisation --------------------------------------------------------------------------------------
 
+constexpr int kFineUpTo = 32;       // short sides up to this one are computed with two planes for bfloat16 too
 constexpr int kMaxNormBlocks = 512;
 constexpr int kPrepBlocks = 1184;   // CTAs of the element-wise passes that fill the GPU: 148 SMs x 8
 
@@ -126,9 +127,11 @@ bool make_plan(OrthoPlan& q, int32_t batch, int32_t rows, int32_t cols, const br
   q.rows = rows;
   q.cols = cols;
   q.m = rows < cols ? rows : cols;
-  // a float16 result keeps 11 bits, about what a rounding of each operand to 11 bits would use up: only bfloat16 is
-  // content with that
-  const bool single = p->precision == BRACE_ORTHO_SINGLE || (p->precision == BRACE_ORTHO_AUTO && out_type != BRACE_TYPE_BF16);
+  // A float16 result keeps 11 bits, about what a rounding of each operand to 11 bits would use up: only bfloat16 is
+  // content with that.  In the smallest matrices single roundings show (18 x 18: 2.5e-3 where 128 x 128 has 2.1e-3), and
+  // two planes take 16 us for 13.
+  const bool single = p->precision == BRACE_ORTHO_SINGLE ||
+                      (p->precision == BRACE_ORTHO_AUTO && (out_type != BRACE_TYPE_BF16 || q.m <= kFineUpTo));
   q.planes = single ? 2 : 1;
   q.ld_x = round_up(cols, 64);
   q.ld_s = round_up(q.m, 64);
