@@ -5,6 +5,7 @@
 #include <cuda.h>
 #include <cuda_runtime.h>
 
+#include <algorithm>
 #include <atomic>
 #include <cmath>
 #include <type_traits>
@@ -564,7 +565,9 @@ EmbPlan emb_plan(int32_t clients, int64_t tokens, int64_t vocab, int32_t dim) {
     q.off_key[i] = take(wide ? 4 * n : 0);
     q.off_pos[i] = take(wide ? 4 * n : 0);
   }
-  q.off_hist = take((int64_t)q.passes * clients * q.tiles * kWideDigits * 4);
+  // for the most tiles that so many tokens or fewer can have: a workspace serves fewer tokens too
+  const int64_t most = wide ? std::min<int64_t>((tokens + kSortTile - 1) / kSortTile, kMostTiles) : 0;
+  q.off_hist = take(q.passes * clients * most * kWideDigits * 4);
   q.off_span = take(wide ? 8 * (int64_t)clients * vocab : 0);
   q.parts = wide ? (tokens + kPart - 1) / kPart : 0;
   q.off_part = take((int64_t)clients * q.parts * 2 * dim * 4);

@@ -7,14 +7,15 @@
 //     S = X X^T;   P = a I + b S + c S S   or   T = b I + c S, P = a I + S T;   X <- P X  (X P)
 // so that a product's epilogue scales, adds a constant on the diagonal and stores.  With two planes the form with T is
 // taken: its epilogues read nothing.  With one plane T's own rounding would show (2.9e-3 against 2.2e-3 of the result
-// at 512 x 2048), and S is read while the product still runs.  All singular vectors stay, every singular value s goes to a s + b s^3 + c s^5, so the values are
-// pushed towards 1 and X towards the nearest matrix with orthonormal rows (columns).
+// at 512 x 2048), and S is read while the product still runs.  All singular vectors stay, every singular value s goes
+// to a s + b s^3 + c s^5, so the values are pushed towards 1 and X towards the nearest matrix with orthonormal rows
+// (columns).
 //
 // Number format.  The operands of all products are float16 times a power of two, with float32 accumulators.  That is
 // possible because the iteration's values are bounded (the host checks the coefficients: singular values below 1.9,
 // eigenvalues of T and P below 7.5), so X 2^14, S 2^14, T 2^13 and P 2^13 cannot overflow and entries down to 8e-9 stay
-// normal; it keeps 11 bits where bfloat16, at the same rate, keeps 8.  For a 16-bit result one float16 holds an operand.  Where
-// float32 accuracy is asked for, an operand is the sum of two float16 planes (hi + lo, 22 bits) and a product is
+// normal; it keeps 11 bits where bfloat16, at the same rate, keeps 8.  For a bfloat16 result one float16 holds an
+// operand.  Where more is asked for, an operand is the sum of two float16 planes (hi + lo, 22 bits) and a product is
 // hi*hi + hi*lo + lo*hi: three times the matrix instructions.
 //
 // Symmetry.  S and P are symmetric: only tiles on and below the diagonal are computed and stored.  Where a product

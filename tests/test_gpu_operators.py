@@ -414,9 +414,14 @@ def test_grad_of_long_texts(tokens, vocab):
     # several tokens' tiles a CTA in the wide sort (256 tiles at most), two and three passes
     dy, ids = randn(1, tokens, 4, seed=1), ids_of(1, tokens, vocab, seed=3)
     out = torch.empty(1, vocab, 4, device="cuda")
-    B.Embedding(vocab, 4, tokens).grad(dy, ids, out)
+    plan = B.Embedding(vocab, 4, tokens)
+    plan.grad(dy, ids, out)
     total, size, count = grad64(dy, ids, vocab, 1.0)
     assert bool(((out.double() - total).abs() <= (count + 3) * 2 ** -24 * size).all())
+    for n in (524_288, 2049, 2048):     # fewer than the plan was made for, with more tiles or none
+        plan.grad(dy[:, :n], ids[:, :n], out)
+        total, size, count = grad64(dy[:, :n], ids[:, :n], vocab, 1.0)
+        assert bool(((out.double() - total).abs() <= (count + 3) * 2 ** -24 * size).all())
 
 
 @pytest.mark.parametrize("n", [31, 32, 33, 63, 64, 65, 95, 96, 97, 127, 128, 129, 4000])

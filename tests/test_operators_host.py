@@ -130,6 +130,11 @@ def test_embedding_workspace():
     assert f(1, 1, 10, 8) < f(1, 3000, 10, 8) < f(2, 3000, 10, 8)
     for bad in [(-1, 5, 10, 8), (2, -5, 10, 8), (2, 5, 0, 8), (2, 5, 10, 0)]:
         assert f(*bad) == 0
+    # a workspace for so many tokens serves any fewer
+    edge = 256 * 2048
+    sizes = [f(3, t, 5000, 8) for t in (0, 1, 2048, 2049, 4096, 4097, 5000, edge - 1, edge, edge + 1, edge + 2048, 2 * edge,
+                                        2 * edge + 1, 10 * edge)]
+    assert sizes == sorted(sizes)
     # far past 32 bits
     assert f(16, 1 << 30, 1 << 20, 4096) > 16 * (1 << 30) * 8
 
