@@ -796,9 +796,9 @@ __global__ void __launch_bounds__(GemmShape<CG, TN, NP>::kThreads, 1)
 // all), and every CTA forms P itself and takes its slice to P X.
 // At these sizes nothing is bound by bandwidth or by the products (a 128 x 128 product is some 0.3 us); what counts is
 // the chain of dependent steps, which as separate launches costs a launch and a round trip through L2 each: 128 x 128
-// takes 24 us (a step 4.2: products 0.6 each, epilogues 0.7 to 0.9) against 68 in launches of tiles, 16 x 16 12 against
-// 48.  Several CTAs spend 4 to 7 us a step on the exchange of S: 128 x 512 takes 52 us against 78, 128 x 1024 in float32
-// 69 against 154.
+// takes 23 us (a step 4.2: products 0.6 each, epilogues 0.7 to 0.9) against 68 in launches of tiles, 40 x 40 15.  Several
+// CTAs spend 4 to 7 us a step on the exchange of S: 128 x 512 takes 49 us against 78, 128 x 1024 in float32 72 against
+// 154.
 // ---------------------------------------------------------------------------------------------------------------
 
 struct ResidentArgs {
@@ -884,25 +884,41 @@ __global__ void __launch_bounds__(kResidentThreads, 1) ortho_resident_kernel(con
   grid_wait();
   if (blockIdx.x == 0 && tid == 0) *p.prep.status = 0;
 
-  // momentum and sum of squares, as in ortho_norm_kernel
+  // momentum and sum of squares, as in ortho_norm_kernel; what is orthogonalised stays in registers (at most 128 x 256
+  // elements, 8 groups of 8 a thread), all loads of four groups first
   const int units_row = (cols + 7) / 8, units = rows * units_row;
+  const bool whole = cols % 8 == 0;
+  float held[8][8];
   double sum = 0;
-  for (int u = tid; u < units; u += kResidentThreads) {
-    const int r = u / units_row, col = col0 + (u - r * units_row) * 8, row = row0 + r, n = min(8, col0 + cols - col);
-    float g[8];
-    load_g<TYPE>(p.prep, b, row, col, n, g);
-    if (p.prep.m_in) {
-      float mo[8];
-      load8(p.prep.m_in + b * p.prep.batch_m_in + (int64_t)row * p.prep.ld_m_in + col, p.prep.vec_m_in, n, mo);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) mo[i] = fmaf(p.prep.beta, mo[i], g[i]);
-      store8(p.prep.m_out + b * p.prep.batch_m_out + (int64_t)row * p.prep.ld_m_out + col, p.prep.vec_m_out, n, mo);
+  for (int h = 0; h < 8; h += 4) {
+    if (h * kResidentThreads >= units) break;
+    float mo[4][8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) g[i] = p.prep.nesterov ? fmaf(p.prep.beta, mo[i], g[i]) : mo[i];
+    for (int i = 0; i < 4; ++i) {
+      const int u = tid + (h + i) * kResidentThreads, at_u = min(u, units - 1);   // past the end: read again, not used
+      const int r = at_u / units_row, c = (at_u - r * units_row) * 8, row = row0 + r, col = col0 + c, n = min(8, cols - c);
+      load_g<TYPE>(p.prep, b, row, col, whole ? 8 : n, held[h + i]);
+      if (p.prep.m_in && u < units)   // in place, another thread's elements may be written at any time
+        load8(p.prep.m_in + b * p.prep.batch_m_in + (int64_t)row * p.prep.ld_m_in + col, p.prep.vec_m_in, whole ? 8 : n, mo[i]);
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (i < n) sum = fma((double)g[i], (double)g[i], sum);
+    for (int i = 0; i < 4; ++i) {
+      const int u = tid + (h + i) * kResidentThreads;
+      if (u >= units) continue;
+      const int r = u / units_row, c = (u - r * units_row) * 8, n = min(8, cols - c);
+      float(&g)[8] = held[h + i];
+      if (p.prep.m_in) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) mo[i][j] = fmaf(p.prep.beta, mo[i][j], g[j]);
+        store8(p.prep.m_out + b * p.prep.batch_m_out + (int64_t)(row0 + r) * p.prep.ld_m_out + col0 + c, p.prep.vec_m_out, n, mo[i]);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) g[j] = p.prep.nesterov ? fmaf(p.prep.beta, mo[i][j], g[j]) : mo[i][j];
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (j < n) sum = fma((double)g[j], (double)g[j], sum);
+    }
   }
   sum = block_sum(sum, s_sum);
   if (ctas > 1) {
@@ -915,27 +931,17 @@ __global__ void __launch_bounds__(kResidentThreads, 1) ortho_resident_kernel(con
   const float inv = (float)((double)kScaleX / (sqrt(sum) + (double)p.prep.eps));
 
   // X_0: the operand planes
-  for (int u = tid; u < units; u += kResidentThreads) {
-    const int r = u / units_row, c8 = u - r * units_row, col = col0 + c8 * 8, row = row0 + r, n = min(8, col0 + cols - col);
-    float g[8];
-    if (!p.prep.m_in || p.prep.nesterov) {
-      load_g<TYPE>(p.prep, b, row, col, n, g);
-    } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) g[i] = 0.f;
-    }
-    if (p.prep.m_in) {   // this thread wrote the same elements above
-      float mo[8];
-      load8((const float*)p.prep.m_out + b * p.prep.batch_m_out + (int64_t)row * p.prep.ld_m_out + col, p.prep.vec_m_out, n, mo);
+  for (int i = 0; i < 8; ++i) {
+    const int u = tid + i * kResidentThreads;
+    if (u >= units) break;
+    const int r = u / units_row, c8 = u - r * units_row;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) g[i] = p.prep.nesterov ? fmaf(p.prep.beta, mo[i], g[i]) : mo[i];
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) g[i] *= inv;
+    for (int j = 0; j < 8; ++j) held[i][j] *= inv;
     const uint32_t to = swizzled(sm_x + (uint32_t)(c8 >> 3) * x_block, r, c8 & 7);
-    const uint4 hi = pack8(g);
+    const uint4 hi = pack8(held[i]);
     sts16(to, hi);
-    if (NP == 2) sts16(to + x_plane, pack8_rest(g, hi));
+    if (NP == 2) sts16(to + x_plane, pack8_rest(held[i], hi));
   }
   fence_async();
   tc_fence_before();
