@@ -11,6 +11,7 @@ PKG_DIR = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG_DIR)
 LIB_PATH = os.path.join(PKG_DIR, "libbrace.so")
 DEBUG_LIB_PATH = os.path.join(PKG_DIR, "libbrace_debug.so")
+OBJ_DIR = os.path.join(PKG_DIR, "_build")
 SOURCES = [os.path.join(PKG_DIR, "csrc", f) for f in ("brace.cu", "operators.cu")]
 DEPS = SOURCES + [os.path.join(PKG_DIR, "csrc", f) for f in ("brace_kernels.cuh", "elements.cuh", "embedding_kernels.cuh",
                                                             "ortho_kernels.cuh", "sm100.cuh")]
@@ -31,23 +32,58 @@ def needs_build(path: str = LIB_PATH) -> bool:
     return any(os.path.getmtime(p) > t for p in DEPS)
 
 
+def _object(source: str, defines) -> str:
+    """Where a source's object lies; only brace.cu looks at the defines."""
+    name = os.path.splitext(os.path.basename(source))[0]
+    if defines and name == "brace":
+        name += "_debug"
+    return os.path.join(OBJ_DIR, name + ".o")
+
+
 def _compile(out_path: str, defines, verbose: bool) -> str:
-    cmd = [_nvcc(), "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-           "-shared", "--threads", "0", "-Xcompiler", "-fPIC", "-I", os.path.join(ROOT, "include"),
-           "-I", os.path.join(PKG_DIR, "csrc")] + list(defines) + ["-o", out_path] + SOURCES
-    if verbose:
-        cmd[1:1] = ["-Xptxas", "-v"]
-    res = subprocess.run(cmd, capture_output=True, text=True)
+    base = [_nvcc(), "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
+            "-Xcompiler", "-fPIC", "-I", os.path.join(ROOT, "include"), "-I", os.path.join(PKG_DIR, "csrc")]
+    os.makedirs(OBJ_DIR, exist_ok=True)
+    objects, running = [], []
+    for source in SOURCES:
+        obj = _object(source, defines)
+        objects.append(obj)
+        if not verbose and not needs_build(obj):
+            continue
+        # written elsewhere first: an object that is there is whole
+        part = f"{obj}.{os.getpid()}.o"
+        cmd = base + (["-Xptxas", "-v"] if verbose else []) + list(defines) + ["-c", source, "-o", part]
+        running.append((part, obj, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
+    failed = ""
+    for part, obj, proc in running:
+        said = proc.communicate()[0]
+        if proc.returncode != 0:
+            failed += said
+            continue
+        os.replace(part, obj)
+        if verbose:
+            sys.stderr.write(said)
+    if failed:
+        raise RuntimeError("nvcc failed:\n" + failed)
+    res = subprocess.run(base + ["-shared", "-o", out_path] + objects, capture_output=True, text=True)
     if res.returncode != 0:
         raise RuntimeError("nvcc failed:\n" + res.stdout + res.stderr)
-    if verbose:
-        sys.stderr.write(res.stderr)
     return out_path
+
+
+def _forget_objects(defines) -> None:
+    """A forced build compiles anew; the debug library shares what does not look at its define."""
+    for source in SOURCES:
+        obj = _object(source, defines)
+        if os.path.exists(obj) and not (defines and obj == _object(source, [])):
+            os.remove(obj)
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
     if not force and not needs_build():
         return LIB_PATH
+    if force:
+        _forget_objects([])
     return _compile(LIB_PATH, [], verbose)
 
 
@@ -56,6 +92,8 @@ def build_debug(force: bool = False, verbose: bool = False) -> str:
     brace_debug_status instead of trapping.  Load it by setting BRACE_LIBRARY to the returned path."""
     if not force and not needs_build(DEBUG_LIB_PATH):
         return DEBUG_LIB_PATH
+    if force:
+        _forget_objects(["-DBRACE_DEBUG"])
     return _compile(DEBUG_LIB_PATH, ["-DBRACE_DEBUG"], verbose)
 
 
