@@ -77,7 +77,6 @@ cudaError_t with_type(int type, F&& f) {
 
 // ---- the orthogonalisation --------------------------------------------------------------------------------------
 
-constexpr int kFineUpTo = 32;       // short sides up to this one are computed with two planes for bfloat16 too
 constexpr int kMaxNormBlocks = 512;
 constexpr int kPrepBlocks = 1184;   // CTAs of the element-wise passes that fill the GPU: 148 SMs x 8
 
@@ -120,7 +119,7 @@ struct OrthoPlan {
   int planes;
   int64_t ld_x, ld_s;
   int norm_blocks;
-  size_t off_partial, off_x[2], off_s, off_t, off_p, bytes;
+  size_t off_partial, off_x[2], off_s, off_t[2], off_p, bytes;   // T of even and of odd steps
 };
 
 bool make_plan(OrthoPlan& q, int32_t batch, int32_t rows, int32_t cols, const brace_ortho_params* p, int out_type) {
@@ -128,11 +127,11 @@ bool make_plan(OrthoPlan& q, int32_t batch, int32_t rows, int32_t cols, const br
   q.rows = rows;
   q.cols = cols;
   q.m = rows < cols ? rows : cols;
-  // A float16 result keeps 11 bits, about what a rounding of each operand to 11 bits would use up: only bfloat16 is
-  // content with that.  In the smallest matrices single roundings show (18 x 18: 2.5e-3 where 128 x 128 has 2.1e-3), and
-  // two planes take 16 us for 13.
-  const bool single = p->precision == BRACE_ORTHO_SINGLE ||
-                      (p->precision == BRACE_ORTHO_AUTO && (out_type != BRACE_TYPE_BF16 || q.m <= kFineUpTo));
+  // One plane only where the caller asks for it, for bfloat16 results too: what the rounding of an operand puts outside
+  // the matrix's range grows by a = 3.4445 a step, 485 times over five, which 11 bits have no room for (1024 x 4096 in
+  // bfloat16: rank 1 1.5e-1, rank 33 2.7e-2, full rank 1.9e-3 in 186 us; with two planes 1.7e-3, the result's own
+  // rounding, for all of them in 358 us).
+  const bool single = p->precision != BRACE_ORTHO_HALF;
   q.planes = single ? 2 : 1;
   q.ld_x = round_up(cols, 64);
   q.ld_s = round_up(q.m, 64);
@@ -153,7 +152,11 @@ bool make_plan(OrthoPlan& q, int32_t batch, int32_t rows, int32_t cols, const br
   q.off_x[0] = take(xb);
   q.off_x[1] = take(xb);
   q.off_s = take(sb);
-  q.off_t = take(single ? sb : 0);
+  // Where bfloat16 is asked for, T lies where the step's X goes: that place is free until then, and the workspace stays
+  // a fifth smaller than float32's.
+  const bool in_x = out_type == BRACE_TYPE_BF16;
+  const size_t apart = take(single && !in_x ? sb : 0);
+  for (int k = 0; k < 2; ++k) q.off_t[k] = in_x ? q.off_x[k ^ 1] : apart;
   q.off_p = take(sb);
   q.bytes = at;
   return true;
@@ -321,7 +324,7 @@ cudaError_t launch_products(const OrthoPlan& q, const Shapes& shapes, const brac
   constexpr int TM = 128 * CG;
   const bool tall = q.rows > q.cols;
   const int64_t z = (int64_t)q.batch * q.planes;
-  Operand xs[2] = {}, s = {}, t = {}, poly = {};
+  Operand xs[2] = {}, s = {}, ts[2] = {}, poly = {};
   auto place = [&](Operand& x, size_t off, int64_t rows, int64_t ld) {
     x.base = ws + off;
     x.rows = rows;
@@ -332,7 +335,7 @@ cudaError_t launch_products(const OrthoPlan& q, const Shapes& shapes, const brac
   place(xs[0], q.off_x[0], q.rows, q.ld_x);
   place(xs[1], q.off_x[1], q.rows, q.ld_x);
   place(s, q.off_s, q.m, q.ld_s);
-  place(t, q.off_t, q.m, q.ld_s);
+  for (int k = 0; k < 2; ++k) place(ts[k], q.off_t[k], q.m, q.ld_s);
   place(poly, q.off_p, q.m, q.ld_s);
   const int tm = (q.m + TM - 1) / TM;
   GemmArgs sym = {};
@@ -358,12 +361,12 @@ cudaError_t launch_products(const OrthoPlan& q, const Shapes& shapes, const brac
   step.status = (int*)ws;
   for (int k = 0; k < p->steps; ++k) {
     const int cur = k & 1;
-    Operand& x = xs[cur];
+    Operand &x = xs[cur], &t = ts[q.off_t[0] == q.off_t[1] ? 0 : cur];
     GemmArgs g = sym;
     g.K = tall ? q.rows : q.cols;
     g.scale = kGramScale;
     g.dst = (__half*)(ws + q.off_s);
-    g.dst2 = (__half*)(ws + q.off_t);
+    g.dst2 = (__half*)(ws + q.off_t[cur]);
     g.scale2 = p->c * kFromGram;
     g.diagonal2 = p->b * kSquareScale;
     cudaError_t err = with_columns<CG>(shapes.wide_gram, [&](auto n) {

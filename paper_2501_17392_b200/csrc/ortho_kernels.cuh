@@ -14,9 +14,10 @@
 // Number format.  The operands of all products are float16 times a power of two, with float32 accumulators.  That is
 // possible because the iteration's values are bounded (the host checks the coefficients: singular values below 1.9,
 // eigenvalues of T and P below 7.5), so X 2^14, S 2^14, T 2^13 and P 2^13 cannot overflow and entries down to 8e-9 stay
-// normal; it keeps 11 bits where bfloat16, at the same rate, keeps 8.  For a bfloat16 result one float16 holds an
-// operand.  Where more is asked for, an operand is the sum of two float16 planes (hi + lo, 22 bits) and a product is
-// hi*hi + hi*lo + lo*hi: three times the matrix instructions.
+// normal; it keeps 11 bits where bfloat16, at the same rate, keeps 8.  An operand is the sum of two such planes (hi + lo,
+// 22 bits) and a product is hi*hi + hi*lo + lo*hi: three times the matrix instructions.  One plane alone is there for
+// callers who ask for it: 11 bits are enough for updates of full rank only, since an error outside the matrix's range
+// grows by a a step.
 //
 // Symmetry.  S and P are symmetric: only tiles on and below the diagonal are computed and stored.  Where a product
 // needs one above it, the stored tile is loaded instead and the matrix instruction reads it the other way (the
