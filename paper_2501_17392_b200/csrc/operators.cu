@@ -116,7 +116,7 @@ bool coefficients_ok(const brace_ortho_params* p) {
 
 struct OrthoPlan {
   int batch, rows, cols, m;   // m: the short side
-  int planes;
+  int planes, chunk;          // chunk: stages per accumulator (two planes)
   int64_t ld_x, ld_s;
   int norm_blocks;
   size_t off_partial, off_x[2], off_s, off_t[2], off_p, bytes;   // T of even and of odd steps
@@ -133,6 +133,7 @@ bool make_plan(OrthoPlan& q, int32_t batch, int32_t rows, int32_t cols, const br
   // rounding, for all of them in 358 us).
   const bool single = p->precision != BRACE_ORTHO_HALF;
   q.planes = single ? 2 : 1;
+  q.chunk = out_type == BRACE_TYPE_BF16 || q.m >= kLongChunkFrom ? 2 : 1;
   q.ld_x = round_up(cols, 64);
   q.ld_s = round_up(q.m, 64);
   const int64_t units = (int64_t)rows * ((cols + 7) / 8);
@@ -345,7 +346,7 @@ cudaError_t launch_products(const OrthoPlan& q, const Shapes& shapes, const brac
     g.total = g.tiles * q.batch;
   };
   sym.ld_dst = q.ld_s;
-  sym.chunk = q.m >= kLongChunkFrom ? 2 : 1;
+  sym.chunk = q.chunk;
   sym.status = (int*)ws;
   GemmArgs step = last;
   step.M = q.rows;

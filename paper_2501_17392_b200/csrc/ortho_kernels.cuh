@@ -239,11 +239,14 @@ constexpr int kTileK = 64;                       // contraction per stage: one 1
 constexpr int kOperandBytes = 128 * kTileK * 2;  // an operand of a stage in one CTA: 128 rows (or columns)
 // The tensor cores' float32 accumulation cuts off what does not fit, an error that no sign cancels: over a long
 // contraction it adds up (2.4e-5 of the result at 512 x 2048, five steps).  With two planes the accumulators therefore
-// hold `chunk` stages only and are added in registers, rounded to nearest.  One stage (K = 64) leaves less error than
-// products in plain float32 arithmetic (1.6e-6 against 2.3e-6 at 768 x 768); two stages leave 3.0e-6 there, and from
-// about that size on no more than 1.3 times plain float32's, whose error grows with K: they are used from there, since
-// at 4096 x 4096 they take 3.4 ms where one takes 4.3.
-constexpr int kLongChunkFrom = 768;
+// hold `chunk` stages only and are added in registers, rounded to nearest.  One stage (K = 64) leaves no more error than
+// products in plain float32 arithmetic from a short side of about 500 on (768 x 768: full rank 1.7e-6 against 2.7e-6, rank 4
+// 5.6e-5 against 7.3e-5), and below that up to 1.7 times as much (64 x 64: 2.0e-6 against 1.2e-6).  Two stages leave up
+// to twice one's (768 x 768: 3.0e-6, rank 4 9.9e-5) but take less time (4096 x 4096: 3.5 ms against 4.3): they are used
+// where that is not seen, for bfloat16 results (rounded to 1.7e-3) and from the short side on where plain float32 is
+// worse on every spectrum tried, full rank, 1 / i^2 and ranks 1, 4, 33 and 128: at 1600 x 1600 full rank 3.2e-6 against
+// 3.5e-6, rank 4 1.12e-4 against 1.14e-4; at 1400 x 1400 rank 4 has 1.12e-4 against 1.05e-4.
+constexpr int kLongChunkFrom = 1600;
 constexpr int kCellBytes = 2048;                 // a warp's staging of the epilogue: 32 rows of 64 bytes
 
 // An operand's tensor map(s), each with boxes that fill a stage's operand, all planes, in one load: the cost of a
