@@ -47,24 +47,31 @@ int sm_count() {
 
 // Every kernel here waits on the device for the one before it (griddepcontrol.wait) and may be set up while that one
 // drains.  `cluster`: CTAs per cluster.
+struct LaunchConfig {
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute attr[2];
+  LaunchConfig(dim3 grid, int block, size_t smem, int cluster, cudaStream_t st) {
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3((unsigned)block);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)cluster;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
+  }
+  LaunchConfig(const LaunchConfig&) = delete;   // cfg points into it
+};
+
 template <typename... KArgs, typename... Args>
 cudaError_t launch(void (*kernel)(KArgs...), dim3 grid, int block, size_t smem, int cluster, cudaStream_t st,
                    const Args&... args) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = grid;
-  cfg.blockDim = dim3((unsigned)block);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = st;
-  cudaLaunchAttribute attr[2];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = (unsigned)cluster;
-  attr[1].val.clusterDim.y = 1;
-  attr[1].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = cluster > 1 ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, kernel, args...);
+  const LaunchConfig at(grid, block, smem, cluster, st);
+  return cudaLaunchKernelEx(&at.cfg, kernel, args...);
 }
 
 // Calls f with a value of the element type.
@@ -434,9 +441,11 @@ cudaError_t launch_prep(const OrthoPlan& q, const PrepArgs& a, cudaStream_t st) 
   }
 }
 
-// One launch for matrices that a cluster of CTAs can hold; false: this one has to go through the tiled products.
+// One launch for matrices that a cluster of CTAs can hold.  `placed` false: nothing was launched, the device has no place
+// for a cluster of that many CTAs (only up to 8 are certain: a part of a GPU may have fewer SMs wired together), and the
+// matrix has to go through the tiled products.
 template <int NP, int TYPE>
-cudaError_t launch_resident_as(const ResidentArgs& r, int ctas, cudaStream_t st) {
+cudaError_t launch_resident_as(const ResidentArgs& r, int ctas, cudaStream_t st, bool* placed) {
   auto* kernel = ortho_resident_kernel<NP, TYPE>;
   static std::atomic<uint64_t> granted{0};
   int dev = 0;
@@ -452,16 +461,36 @@ cudaError_t launch_resident_as(const ResidentArgs& r, int ctas, cudaStream_t st)
   int64_t smem = resident_smem(NP, r.slice, ctas);
   // CTAs of two clusters must not share an SM: each would hold tensor memory that the other's cluster waits for
   if (ctas > 1 && smem < 118 * 1024) smem = 118 * 1024;
-  return launch(kernel, dim3((unsigned)(r.last.total * ctas)), kResidentThreads, (size_t)smem, ctas, st, r);
+  const dim3 grid((unsigned)(r.last.total * ctas));
+  if (ctas > 8) {
+    // one CTA an SM whatever the matrix's size: the answer for a number of CTAs holds for all its launches
+    static std::atomic<uint32_t> known[64];   // by device: bit ctas - 9 for a place, bit ctas + 7 for none
+    std::atomic<uint32_t>& answers = known[dev & 63];
+    uint32_t bits = answers.load(std::memory_order_relaxed);
+    const uint32_t yes = 1u << (ctas - 9), no = 1u << (ctas + 7);
+    if (!(bits & (yes | no))) {
+      const LaunchConfig one(dim3((unsigned)ctas), kResidentThreads, (size_t)smem, ctas, st);
+      int clusters = 0;
+      err = cudaOccupancyMaxActiveClusters(&clusters, kernel, &one.cfg);
+      if (err != cudaSuccess) return err;
+      bits = clusters > 0 ? yes : no;
+      answers.fetch_or(bits, std::memory_order_relaxed);
+    }
+    if (bits & no) {
+      *placed = false;
+      return cudaSuccess;
+    }
+  }
+  return launch(kernel, grid, kResidentThreads, (size_t)smem, ctas, st, r);
 }
 
 template <int NP>
-cudaError_t launch_resident(const ResidentArgs& r, int ctas, cudaStream_t st) {
+cudaError_t launch_resident(const ResidentArgs& r, int ctas, cudaStream_t st, bool* placed) {
   switch (r.prep.g.type) {
-    case kTypeF32: return launch_resident_as<NP, kTypeF32>(r, ctas, st);
-    case kTypeBF16: return launch_resident_as<NP, kTypeBF16>(r, ctas, st);
-    case kTypeF16: return launch_resident_as<NP, kTypeF16>(r, ctas, st);
-    default: return launch_resident_as<NP, kTypeBits>(r, ctas, st);
+    case kTypeF32: return launch_resident_as<NP, kTypeF32>(r, ctas, st, placed);
+    case kTypeBF16: return launch_resident_as<NP, kTypeBF16>(r, ctas, st, placed);
+    case kTypeF16: return launch_resident_as<NP, kTypeF16>(r, ctas, st, placed);
+    default: return launch_resident_as<NP, kTypeBits>(r, ctas, st, placed);
   }
 }
 
@@ -510,8 +539,10 @@ int run_ortho(const OrthoPlan& q, const brace_ortho_params* p, PrepArgs prep, co
     r.a = p->a;
     r.b = p->b;
     r.c = p->c;
-    const cudaError_t e = q.planes == 1 ? launch_resident<1>(r, ctas, st) : launch_resident<2>(r, ctas, st);
-    return e == cudaSuccess ? BRACE_OK : cuda_fail_no_ctx(e);
+    bool placed = true;
+    const cudaError_t e = q.planes == 1 ? launch_resident<1>(r, ctas, st, &placed) : launch_resident<2>(r, ctas, st, &placed);
+    if (e != cudaSuccess) return cuda_fail_no_ctx(e);
+    if (placed) return BRACE_OK;
   }
   cudaError_t err = launch_prep(q, prep, st);
   if (err == cudaSuccess) {

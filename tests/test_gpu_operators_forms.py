@@ -1,0 +1,76 @@
+"""Forms of the matrix operators that sizes alone do not reach: large clusters, and what pairs of CTAs make of types, strides,
+packed bits, replicas and matrices that are not finite.  References and bounds are those of test_gpu_operators.py."""
+
+import pytest
+import torch
+
+from paper_2501_17392_b200 import brace as B
+from tests.test_gpu_operators import AUTO, BF16, F16, F32, TOL, U, bound, direction64, gen, muon64, randn, rel, signs
+
+pytestmark = pytest.mark.gpu
+
+# one launch by 9 to 16 CTAs: a short side up to 128, a long one of 1025 to 2048 (two planes) or 2049 to 4096 (one)
+LARGE_CLUSTERS = [(B.ORTHO_SINGLE, s) for s in [(1, 128, 1025), (2, 100, 1290), (1, 1500, 128), (3, 17, 1990), (1, 2048, 128),
+                                                (1, 2048, 1), (1, 128, 2048)]]
+LARGE_CLUSTERS += [(B.ORTHO_HALF, s) for s in [(1, 128, 2050), (2, 2700, 64), (1, 90, 3333), (3, 4096, 128), (1, 128, 4096)]]
+
+
+@pytest.mark.parametrize("precision,shape", LARGE_CLUSTERS)
+def test_clusters_of_9_to_16(precision, shape):
+    b, r, c = shape
+    g = randn(b, r, c, seed=r + c)
+    out = torch.full((b, r, c), 7.0, device="cuda")
+    plan = B.Orthogonalizer(r, c, batch=b, params=B.ortho_params(precision=precision))
+    plan.orthogonalize(g, out)
+    plan.check()
+    again = torch.empty_like(out)
+    plan.orthogonalize(g, again)
+    assert torch.equal(out, again)
+    want = direction64(g)
+    for e in range(b):
+        assert rel(out[e], want[e]) <= bound(precision, F32)
+
+
+@pytest.mark.parametrize("shape", [(12, 128, 2048), (30, 1100, 30)])
+def test_more_large_clusters_than_fit_at_once(shape):
+    b, r, c = shape
+    g = randn(b, r, c, seed=5)
+    out = torch.empty_like(g)
+    plan = B.Orthogonalizer(r, c, batch=b)
+    plan.orthogonalize(g, out)
+    plan.check()
+    want = direction64(g)
+    for e in range(b):
+        assert rel(out[e], want[e]) <= bound(B.ORTHO_SINGLE, F32)
+
+
+@pytest.mark.parametrize("tg", [F32, BF16, F16, torch.int32])
+@pytest.mark.parametrize("tw", [F32, BF16, F16])
+@pytest.mark.parametrize("shape", [(2, 120, 1800), (1, 1777, 99)])
+def test_muon_step_in_large_clusters(shape, tg, tw):
+    offset = 45 if tg == torch.int32 else 0
+    n = shape[0] * shape[1] * shape[2]
+    if tg == torch.int32:
+        g = torch.randint(-2 ** 31, 2 ** 31, ((offset + n + 31) // 32,), device="cuda", generator=gen(1)).int()
+        gf = signs(g, offset, shape)
+    else:
+        g = gf = randn(*shape, seed=1).to(tg)
+    m, w = randn(*shape, seed=2, scale=3.0), randn(*shape, seed=3, scale=0.05).to(tw)
+    want_m, want_w, step = muon64(gf, m, w, 0.03, 0.9, True, 0.1, 1.5)
+    plan = B.Orthogonalizer(shape[1], shape[2], batch=shape[0])
+    plan.muon_step(g, m, w, 0.03, beta=0.9, weight_decay=0.1, scale=1.5, bit_offset=offset)
+    plan.check()
+    assert rel(m, want_m) <= 2 ** -23
+    limit = TOL[AUTO[tw]] * step.norm() + (4 * U[F32] + U[tw]) * (want_w.norm() + step.norm())
+    assert float((w.double() - want_w).norm()) <= float(limit)
+
+
+def test_large_clusters_keep_bad_matrices_to_themselves():
+    g = randn(4, 100, 1900, seed=1)
+    g[1] = 0
+    g[2, 99, 1899] = float("nan")
+    out = torch.empty_like(g)
+    B.Orthogonalizer(100, 1900, batch=4).orthogonalize(g, out)
+    want = direction64(g)
+    assert rel(out[0], want[0]) <= bound(B.ORTHO_SINGLE, F32) and rel(out[3], want[3]) <= bound(B.ORTHO_SINGLE, F32)
+    assert bool((out[1] == 0).all()) and bool(out[2].isnan().all())
