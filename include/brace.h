@@ -454,7 +454,7 @@ size_t brace_ortho_workspace_bytes(int32_t batch, int32_t rows, int32_t cols, co
  * A matrix of zeros gives zeros; a matrix with a NaN or an infinity gives NaN
  * (that matrix only).  batch, rows or cols of 0 does nothing.  d_out may not
  * overlap d_g.  Errors: INVALID_ARG (null, negative size, ld < cols, bad type /
- * coefficients, misaligned pointer), WORKSPACE (missing, too small or not 256-byte
+ * coefficients, misaligned pointer, stride_out 0 with several matrices), WORKSPACE (missing, too small or not 256-byte
  * aligned), UNSUPPORTED (batch > 32767, or rows * cols / 8 >= 2^31), CUDA. */
 int brace_orthogonalize(int32_t batch, int32_t rows, int32_t cols, const brace_ortho_params* params, const void* d_g,
                         int32_t g_type, int64_t ld_g, int64_t stride_g, int64_t bit_offset, void* d_out,
@@ -490,7 +490,8 @@ typedef struct brace_muon {
 
 /* Workspace: brace_ortho_workspace_bytes with out_type = weights_type.  Errors as
  * for brace_orthogonalize, and INVALID_ARG for non-finite beta, lr, weight_decay
- * or scale and for replicas < 1. */
+ * or scale, for replicas < 1, and where one place would be written for several
+ * matrices or replicas (a stride of an output, or replica_weights_out, of 0). */
 int brace_muon_step(int32_t batch, int32_t rows, int32_t cols, const brace_ortho_params* params,
                     const brace_muon* step, void* d_workspace, size_t workspace_bytes, brace_stream_t stream);
 

@@ -808,6 +808,7 @@ int brace_orthogonalize(int32_t batch, int32_t rows, int32_t cols, const brace_o
   if (batch == 0 || rows == 0 || cols == 0) return BRACE_OK;
   if (!grad_ok(d_g, g_type, ld_g, bit_offset, cols)) return BRACE_ERR_INVALID_ARG;
   if (!d_out || ld_out < cols || !aligned(d_out, (size_t)elem_bytes(out_type))) return BRACE_ERR_INVALID_ARG;
+  if (batch > 1 && stride_out == 0) return BRACE_ERR_INVALID_ARG;   // what is written is a place of its own for each
   if (!sizes_served(batch, rows, cols)) return BRACE_ERR_UNSUPPORTED;
   OrthoPlan q;
   make_plan(q, batch, rows, cols, params, out_type);
@@ -840,6 +841,8 @@ int brace_muon_step(int32_t batch, int32_t rows, int32_t cols, const brace_ortho
   if (!s->d_weights || !s->d_weights_out || s->ld_weights < cols || s->ld_weights_out < cols ||
       !aligned(s->d_weights, wb) || !aligned(s->d_weights_out, wb))
     return BRACE_ERR_INVALID_ARG;
+  if (batch > 1 && (s->stride_momentum_out == 0 || s->stride_weights_out == 0)) return BRACE_ERR_INVALID_ARG;
+  if (s->replicas > 1 && s->replica_weights_out == 0) return BRACE_ERR_INVALID_ARG;
   if (!sizes_served(batch, rows, cols)) return BRACE_ERR_UNSUPPORTED;
   OrthoPlan q;
   make_plan(q, batch, rows, cols, params, s->weights_type);

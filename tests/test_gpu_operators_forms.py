@@ -74,3 +74,25 @@ def test_large_clusters_keep_bad_matrices_to_themselves():
     want = direction64(g)
     assert rel(out[0], want[0]) <= bound(B.ORTHO_SINGLE, F32) and rel(out[3], want[3]) <= bound(B.ORTHO_SINGLE, F32)
     assert bool((out[1] == 0).all()) and bool(out[2].isnan().all())
+
+
+def test_expanded_tensors_are_not_written():
+    # one matrix in memory for several: read, but not written
+    plan, g = B.Orthogonalizer(40, 60, batch=2), randn(2, 40, 60, seed=1)
+    one = randn(1, 40, 60, seed=2)
+    before, shared = one.clone(), one.expand(2, 40, 60)
+    m, w = torch.zeros_like(g), torch.zeros_like(g)
+    for call in (lambda: plan.orthogonalize(g, shared), lambda: plan.muon_step(g, shared, w, 0.1),
+                 lambda: plan.muon_step(g, m, shared, 0.1), lambda: plan.muon_step(g, m, w[None].expand(3, 2, 40, 60), 0.1)):
+        with pytest.raises(B.BraceError) as err:
+            call()
+        assert err.value.status == B.ERR_INVALID_ARG
+    torch.cuda.synchronize()
+    assert torch.equal(one, before) and not m.any() and not w.any()
+    out = torch.empty_like(g)
+    plan.orthogonalize(shared, out)
+    assert torch.equal(out[0], out[1]) and rel(out[0], direction64(one)[0]) <= bound(B.ORTHO_SINGLE, F32)
+    # three copies of the weights that begin as one
+    copies = torch.empty(3, 2, 40, 60, device="cuda")
+    plan.muon_step(shared, m, w[None].expand(3, 2, 40, 60), 0.1, weights_out=copies, nesterov=False)
+    assert rel(copies, -0.1 * direction64(one).expand(3, 2, 40, 60)) <= bound(B.ORTHO_SINGLE, F32)

@@ -90,6 +90,17 @@ def test_muon_step_refuses():
     assert muon(rows=0) == B.OK
 
 
+def test_one_place_is_not_written_for_several():
+    # a stride of 0 is a matrix for all: what is read may be that, what is written may not
+    assert ortho(batch=2, so=0) == BAD
+    assert muon(batch=2, stride_momentum_out=0) == BAD and muon(batch=2, stride_weights_out=0) == BAD
+    assert muon(replicas=2, replica_weights=64, replica_weights_out=0) == BAD
+    assert muon(replicas=2, replica_weights=64, replica_weights_out=64, ws=None) == WORKSPACE   # past those checks
+    assert ortho(so=0, ws=None) == WORKSPACE and ortho(batch=2, sg=0, ws=None) == WORKSPACE
+    assert muon(batch=2, stride_grad=0, stride_momentum=0, stride_weights=0, ws=None) == WORKSPACE
+    assert muon(replicas=2, replica_weights=0, replica_weights_out=64, ws=None) == WORKSPACE
+
+
 def embedding(grad, **over):
     e = B.EmbeddingArgs()
     e.clients, e.dim, e.tokens, e.vocab = 2, 8, 5, 10
