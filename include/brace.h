@@ -45,7 +45,7 @@ enum {
   BRACE_ERR_BAD_STEP = 3,    /* hop called out of order; nothing was launched                   */
   BRACE_ERR_WORKSPACE = 4,   /* workspace missing, too small or misaligned                      */
   BRACE_ERR_CUDA = 5,        /* a CUDA runtime call failed; see brace_last_cuda_error           */
-  BRACE_ERR_TIMEOUT = 6      /* a bounded device-side wait ran out (brace_ortho_status)             */
+  BRACE_ERR_TIMEOUT = 6      /* a bounded device-side wait ran out (brace_ortho_status)         */
 };
 
 /* aggregation rules.  All but SUM share Phases I, II and IV of Section 3 (sign,
@@ -497,7 +497,10 @@ int brace_muon_step(int32_t batch, int32_t rows, int32_t cols, const brace_ortho
 
 /* Waits for `stream` and says whether a bounded device-side wait of the last
  * brace_orthogonalize / brace_muon_step on this workspace ran out: BRACE_OK, or
- * BRACE_ERR_TIMEOUT (its results are not valid).  Not for use in a capture. */
+ * BRACE_ERR_TIMEOUT (its results are not valid).  A call that had nothing to do
+ * (batch, rows or cols of 0) writes no status, so the one before it is the last;
+ * of a workspace on which nothing was computed yet the answer has no meaning.
+ * Not for use in a capture. */
 int brace_ortho_status(const void* d_workspace, brace_stream_t stream);
 
 /* The embedding table at the two ends of a client's local step, for `clients`

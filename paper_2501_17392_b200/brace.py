@@ -423,6 +423,7 @@ class Orthogonalizer:
             workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=device)
         self.workspace = workspace
         self._step = Muon()
+        self._computed = False      # whether a call has written the workspace's status
 
     def _matrix(self, t: torch.Tensor, name: str):
         """(element type, ld, stride between matrices) of a tensor argument."""
@@ -449,9 +450,11 @@ class Orthogonalizer:
     def orthogonalize_status(self, g: torch.Tensor, out: torch.Tensor, bit_offset: int = 0, stream=None) -> int:
         gt, gld, gs = self._update(g, "g", bit_offset)
         ot, old, os_ = self._matrix(out, "out")
-        return lib().brace_orthogonalize(self.batch, self.rows, self.cols, self.params, g.data_ptr(), gt, gld, gs,
-                                         bit_offset, out.data_ptr(), ot, old, os_, self.workspace.data_ptr(),
-                                         self.workspace.numel(), _stream(stream))
+        status = lib().brace_orthogonalize(self.batch, self.rows, self.cols, self.params, g.data_ptr(), gt, gld, gs,
+                                           bit_offset, out.data_ptr(), ot, old, os_, self.workspace.data_ptr(),
+                                           self.workspace.numel(), _stream(stream))
+        self._computed |= status == OK and out.numel() > 0
+        return status
 
     def orthogonalize(self, g: torch.Tensor, out: torch.Tensor, bit_offset: int = 0, stream=None):
         """out = g with its singular values pushed to 1."""
@@ -487,8 +490,10 @@ class Orthogonalizer:
         _, s.ld_weights_out, s.stride_weights_out = self._matrix(wo, "weights_out")
         s.d_weights, s.d_weights_out, s.replicas = w.data_ptr(), wo.data_ptr(), replicas
         s.nesterov, s.beta, s.lr, s.weight_decay, s.scale = int(nesterov), beta, lr, weight_decay, scale
-        return lib().brace_muon_step(self.batch, self.rows, self.cols, self.params, s, self.workspace.data_ptr(),
-                                     self.workspace.numel(), _stream(stream))
+        status = lib().brace_muon_step(self.batch, self.rows, self.cols, self.params, s, self.workspace.data_ptr(),
+                                       self.workspace.numel(), _stream(stream))
+        self._computed |= status == OK and momentum.numel() > 0
+        return status
 
     def muon_step(self, grad: torch.Tensor, momentum: torch.Tensor, weights: torch.Tensor, lr: float,
                   beta: float = 0.95, nesterov: bool = True, weight_decay: float = 0.0, scale: float = 1.0,
@@ -501,6 +506,9 @@ class Orthogonalizer:
 
     def check(self, stream=None):
         """Wait for the stream; raise if a bounded device-side wait of the last call ran out."""
+        if not self._computed:      # there was none: the workspace holds whatever it held
+            (torch.cuda.current_stream() if stream is None else stream).synchronize()
+            return
         _check(lib().brace_ortho_status(self.workspace.data_ptr(), _stream(stream)), "brace_ortho_status")
 
 

@@ -96,3 +96,22 @@ def test_expanded_tensors_are_not_written():
     copies = torch.empty(3, 2, 40, 60, device="cuda")
     plan.muon_step(shared, m, w[None].expand(3, 2, 40, 60), 0.1, weights_out=copies, nesterov=False)
     assert rel(copies, -0.1 * direction64(one).expand(3, 2, 40, 60)) <= bound(B.ORTHO_SINGLE, F32)
+
+
+@pytest.mark.parametrize("b,r,c", [(1, 40, 60), (2, 0, 7), (0, 5, 5)])
+def test_check_of_a_plan_that_has_computed_nothing(b, r, c):
+    dirty = torch.full((1 << 20,), 0xFF, device="cuda", dtype=torch.uint8)
+    plan = B.Orthogonalizer(r, c, batch=b, workspace=dirty)
+    plan.check()
+    t = torch.zeros(b, r, c, device="cuda")
+    if not t.numel():
+        plan.orthogonalize(t, t)
+        plan.check(torch.cuda.current_stream())
+        plan.muon_step(t, t, t, 0.1)
+        plan.check()
+    else:
+        plan.orthogonalize(t, torch.empty_like(t))
+        plan.check()
+        plan.workspace[:4] = 0xFF       # and then it is the workspace that says it
+        with pytest.raises(B.BraceError):
+            plan.check()
