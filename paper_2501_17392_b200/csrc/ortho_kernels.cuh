@@ -676,7 +676,9 @@ __global__ void __launch_bounds__(GemmShape<CG, TN, NP>::kThreads, 1)
       place(tile, b, ti, tj);
       const int row0 = ti * TM + (int)rank * 128 + quarter * 32, col0 = tj * TN + cols0;
       const int rows = min(32, p.M - row0);   // may be none: the accumulators are then read for nothing
-      // rows are padded to 64 columns; the pad is written too (the operands' pads are zeros, so it stays zero)
+      // Rows are padded to 64 columns.  Of the pad this writes what shares 32 (with 256 columns a tile, 64) columns with the
+      // matrix: zeros, since the operands' are; the rest holds what the workspace held.  Those columns are never contracted
+      // (the last stage stops at the next multiple of 16), and as rows or columns of a result they end in pads alone.
       const bool live = rows > 0 && col0 < p.N;
       if (MODE == kModeLast) prefetch_weights<TOUT>(p, b, row0 + lane, col0, Shape::kColumns);
       uint4 x0[4], x1[4];

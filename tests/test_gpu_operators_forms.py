@@ -115,3 +115,63 @@ def test_check_of_a_plan_that_has_computed_nothing(b, r, c):
         plan.workspace[:4] = 0xFF       # and then it is the workspace that says it
         with pytest.raises(B.BraceError):
             plan.check()
+
+
+def guarded(need, fill, seed=0):
+    """A workspace of exactly `need` bytes with `fill` in it (None: random bytes) between guard bytes."""
+    store = torch.randint(0, 256, (need + 1024,), device="cuda", generator=gen(seed)).to(torch.uint8)
+    if fill is not None:
+        store[512:512 + need] = fill
+    guards = torch.cat([store[:512], store[512 + need:]])
+    return store, store[512:512 + need], guards
+
+
+def intact(store, need, guards):
+    return torch.equal(torch.cat([store[:512], store[512 + need:]]), guards)
+
+
+# 0xff: NaN in every operand, and no position in range; 0x7c: infinities and large numbers
+FILLS = [0xFF, 0x7C, None]
+
+
+@pytest.mark.parametrize("shape", [(1, 40, 60), (1, 100, 1500), (1, 130, 130), (2, 300, 130), (1, 161, 700), (3, 513, 770),
+                                   (1, 1030, 2070), (1, 1500, 1500), (1, 2083, 1811)])
+@pytest.mark.parametrize("precision", [B.ORTHO_HALF, B.ORTHO_SINGLE])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_what_the_workspace_held_does_not_matter(shape, precision, dtype):
+    b, r, c = shape
+    params, g = B.ortho_params(precision=precision), randn(b, r, c, seed=r)
+    need = B.ortho_workspace_bytes(b, r, c, params, {F32: B.TYPE_F32, BF16: B.TYPE_BF16}[dtype])
+    want = torch.empty(b, r, c, device="cuda", dtype=dtype)
+    B.Orthogonalizer(r, c, batch=b, params=params, workspace=torch.zeros(need, device="cuda", dtype=torch.uint8)).orthogonalize(g, want)
+    assert rel(want, direction64(g)) <= bound(precision, dtype)
+    for fill in FILLS:
+        store, workspace, guards = guarded(need, fill)
+        out = torch.empty_like(want)
+        plan = B.Orthogonalizer(r, c, batch=b, params=params, workspace=workspace)
+        plan.orthogonalize(g, out)
+        plan.check()
+        assert torch.equal(out, want) and intact(store, need, guards)
+
+
+@pytest.mark.parametrize("clients,tokens,vocab,dim", [(1, 2048, 300, 40), (2, 2049, 5000, 24), (3, 5001, 900, 33),
+                                                      (1, 70000, 3, 8), (1, 300_000, 70_000, 4)])
+def test_what_the_gradients_workspace_held_does_not_matter(clients, tokens, vocab, dim):
+    dy = randn(clients, tokens, dim, seed=1)
+    u = torch.rand(clients, tokens, device="cuda", generator=gen(2), dtype=torch.float64)
+    ids = ((vocab + 1.0) ** u).long() - 2           # few frequent ids, many without a token, -1 for none
+    need = int(B.lib().brace_embedding_workspace_bytes(clients, tokens, vocab, dim))
+    want = torch.empty(clients, vocab, dim, device="cuda")
+    B.Embedding(vocab, dim, tokens, clients=clients, workspace=torch.zeros(need, device="cuda", dtype=torch.uint8)).grad(dy, ids, want)
+    for fill in FILLS:
+        store, workspace, guards = guarded(need, fill)
+        out = torch.full_like(want, 9.0)
+        B.Embedding(vocab, dim, tokens, clients=clients, workspace=workspace).grad(dy, ids, out)
+        assert torch.equal(out, want) and intact(store, need, guards)
+    # positions in range that belong to other ids
+    store, workspace, guards = guarded(need, 0)
+    n = need // 4
+    workspace[:4 * n].view(torch.int32).copy_(torch.arange(n, device="cuda", dtype=torch.int32) % tokens)
+    out = torch.full_like(want, 9.0)
+    B.Embedding(vocab, dim, tokens, clients=clients, workspace=workspace).grad(dy, ids, out)
+    assert torch.equal(out, want) and intact(store, need, guards)
