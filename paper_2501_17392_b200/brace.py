@@ -394,6 +394,18 @@ _ID_BYTES = {torch.int64: 8, torch.int32: 4}
 _EMBEDDING = struct.Struct("@ii10q4if")       # the fields of EmbeddingArgs
 
 
+def _launch_stream(stream, device: int, same: bool) -> int:
+    """The stream of a call whose tensors are on `device` (all of them: `same`).  A kernel that is handed another device's
+    memory, or the host's, would fault."""
+    if not same or device < 0:
+        raise ValueError("the tensors and the workspace have to be on one GPU")
+    if device != torch.cuda.current_device():
+        raise ValueError(f"the tensors are on GPU {device}, the current one is {torch.cuda.current_device()}")
+    if stream is None and _raw_stream is not None:
+        return _raw_stream(device)
+    return _stream(stream)
+
+
 def ortho_params(**over) -> OrthoParams:
     p = OrthoParams()
     _check(lib().brace_ortho_default_params(C.byref(p)), "brace_ortho_default_params")
@@ -450,9 +462,11 @@ class Orthogonalizer:
     def orthogonalize_status(self, g: torch.Tensor, out: torch.Tensor, bit_offset: int = 0, stream=None) -> int:
         gt, gld, gs = self._update(g, "g", bit_offset)
         ot, old, os_ = self._matrix(out, "out")
+        at = g.get_device()
+        st = _launch_stream(stream, at, at == out.get_device() == self.workspace.get_device())
         status = lib().brace_orthogonalize(self.batch, self.rows, self.cols, self.params, g.data_ptr(), gt, gld, gs,
                                            bit_offset, out.data_ptr(), ot, old, os_, self.workspace.data_ptr(),
-                                           self.workspace.numel(), _stream(stream))
+                                           self.workspace.numel(), st)
         self._computed |= status == OK and out.numel() > 0
         return status
 
@@ -490,8 +504,11 @@ class Orthogonalizer:
         _, s.ld_weights_out, s.stride_weights_out = self._matrix(wo, "weights_out")
         s.d_weights, s.d_weights_out, s.replicas = w.data_ptr(), wo.data_ptr(), replicas
         s.nesterov, s.beta, s.lr, s.weight_decay, s.scale = int(nesterov), beta, lr, weight_decay, scale
+        at = grad.get_device()
+        st = _launch_stream(stream, at, at == momentum.get_device() == momentum_out.get_device() == weights.get_device()
+                            == weights_out.get_device() == self.workspace.get_device())
         status = lib().brace_muon_step(self.batch, self.rows, self.cols, self.params, s, self.workspace.data_ptr(),
-                                       self.workspace.numel(), _stream(stream))
+                                       self.workspace.numel(), st)
         self._computed |= status == OK and momentum.numel() > 0
         return status
 
@@ -557,7 +574,8 @@ class Embedding:
         return e
 
     def lookup_status(self, table, ids, out, scale: float = 1.0, stream=None) -> int:
-        return lib().brace_embedding_lookup(self._fill(table, ids, out, scale, True), _stream(stream))
+        e, at = self._fill(table, ids, out, scale, True), table.get_device()
+        return lib().brace_embedding_lookup(e, _launch_stream(stream, at, at == ids.get_device() == out.get_device()))
 
     def lookup(self, table: torch.Tensor, ids: torch.Tensor, out: torch.Tensor, scale: float = 1.0, stream=None):
         """out[c, t] = scale * table[c, ids[c, t]]; 0 for an id outside the table.  A two-dimensional table serves
@@ -565,9 +583,12 @@ class Embedding:
         _check(self.lookup_status(table, ids, out, scale, stream), "brace_embedding_lookup")
 
     def grad_status(self, dy, ids, grad, scale: float = 1.0, accumulate: bool = False, stream=None) -> int:
-        e = self._fill(grad, ids, dy, scale, False, accumulate)
-        ws = self.workspace
-        return lib().brace_embedding_grad(e, _ptr(ws), ws.numel() if ws is not None else 0, _stream(stream))
+        e, ws = self._fill(grad, ids, dy, scale, False, accumulate), self.workspace
+        if ws is None:      # refused
+            return lib().brace_embedding_grad(e, 0, 0, 0)
+        at = grad.get_device()
+        st = _launch_stream(stream, at, at == ids.get_device() == dy.get_device() == ws.get_device())
+        return lib().brace_embedding_grad(e, ws.data_ptr(), ws.numel(), st)
 
     def grad(self, dy: torch.Tensor, ids: torch.Tensor, grad: torch.Tensor, scale: float = 1.0,
              accumulate: bool = False, stream=None):

@@ -175,3 +175,21 @@ def test_what_the_gradients_workspace_held_does_not_matter(clients, tokens, voca
     out = torch.full_like(want, 9.0)
     B.Embedding(vocab, dim, tokens, clients=clients, workspace=workspace).grad(dy, ids, out)
     assert torch.equal(out, want) and intact(store, need, guards)
+
+
+def test_tensors_on_the_host_are_refused():
+    plan, g, h = B.Orthogonalizer(4, 6), torch.zeros(1, 4, 6, device="cuda"), torch.zeros(1, 4, 6)
+    bits = torch.zeros(1, dtype=torch.int32)
+    emb = B.Embedding(10, 8, 5)
+    t, i, a = torch.zeros(1, 10, 8, device="cuda"), torch.zeros(1, 5, dtype=torch.int64, device="cuda"), torch.zeros(1, 5, 8, device="cuda")
+    calls = [lambda: plan.orthogonalize(h, g), lambda: plan.orthogonalize(g, h), lambda: plan.orthogonalize(bits, g),
+             lambda: plan.muon_step(h, g, g, 0.1), lambda: plan.muon_step(g, h, g, 0.1), lambda: plan.muon_step(g, g, h, 0.1),
+             lambda: plan.muon_step(g, g, g, 0.1, momentum_out=h), lambda: plan.muon_step(g, g, g, 0.1, weights_out=h),
+             lambda: B.Orthogonalizer(4, 6, device="cpu").orthogonalize(g, torch.empty_like(g)),
+             lambda: B.Embedding(10, 8, 5, device="cpu").grad(a, i, t)]
+    for op in (lambda x, y, z: emb.lookup(x, y, z), lambda x, y, z: emb.grad(z, y, x)):
+        calls += [lambda op=op: op(t.cpu(), i, a), lambda op=op: op(t, i.cpu(), a), lambda op=op: op(t, i, a.cpu())]
+    for call in calls:
+        with pytest.raises(ValueError, match="GPU"):
+            call()
+    torch.cuda.synchronize()

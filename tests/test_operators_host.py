@@ -186,3 +186,16 @@ def test_binding_checks_shapes_types_and_strides():
 
 class _NoStream:
     cuda_stream = 0
+
+
+def test_binding_takes_tensors_of_one_gpu_only():
+    # the kernels would read host memory; nothing may get as far as a launch
+    o, g = B.Orthogonalizer(4, 6, batch=2, device="cpu"), torch.zeros(2, 4, 6)
+    bits = torch.zeros(2, dtype=torch.int32)
+    e = B.Embedding(10, 8, 5, clients=2, device="cpu")
+    table, ids, act = torch.zeros(2, 10, 8), torch.zeros(2, 5, dtype=torch.int64), torch.zeros(2, 5, 8)
+    for call in (lambda: o.orthogonalize(g, g.clone(), stream=_NoStream()), lambda: o.orthogonalize(bits, g, stream=_NoStream()),
+                 lambda: o.muon_step(g, g.clone(), g.clone(), 0.1, stream=_NoStream()),
+                 lambda: e.lookup(table, ids, act, stream=_NoStream()), lambda: e.grad(act, ids, table, stream=_NoStream())):
+        with pytest.raises(ValueError, match="GPU"):
+            call()
