@@ -47,11 +47,9 @@ struct Pack {
   using W = typename WideWord<(kBytes >= 16 ? 16 : kBytes)>::T;
   static constexpr int kWords = kBytes / (int)sizeof(W);
   alignas(16) T t[V];
+  // Ordinary loads, not those of the read-only path: a kernel here may start before the one that wrote its input has
+  // ended (it waits on the device), and what it reads and writes may be one buffer.
   __device__ __forceinline__ void load(const T* p) {
-#pragma unroll
-    for (int i = 0; i < kWords; ++i) reinterpret_cast<W*>(t)[i] = __ldg(reinterpret_cast<const W*>(p) + i);
-  }
-  __device__ __forceinline__ void load_plain(const T* p) {
 #pragma unroll
     for (int i = 0; i < kWords; ++i) reinterpret_cast<W*>(t)[i] = reinterpret_cast<const W*>(p)[i];
   }

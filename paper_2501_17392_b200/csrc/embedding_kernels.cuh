@@ -308,7 +308,7 @@ struct Share {
     for (int q = 0; q < Q; ++q)
       if (32 * V * q < left) {
         Pack<TO, V> y;
-        if (accumulate) y.load_plain(p + 32 * V * q);
+        if (accumulate) y.load(p + 32 * V * q);
 #pragma unroll
         for (int j = 0; j < V; ++j) y.t[j] = from_f32<TO>((accumulate ? to_f32(y.t[j]) : 0.f) + sum[q][j] * scale);
         y.store_stream(p + 32 * V * q);
@@ -392,7 +392,7 @@ __global__ void __launch_bounds__(256, 4) embedding_sum_kernel(const EmbArgs p) 
       for (int k = 0; k < S::Q; ++k)
         if (32 * V * k < left) {
           Pack<TO, V> y;
-          if (p.accumulate) y.load_plain(row + 32 * V * k);
+          if (p.accumulate) y.load(row + 32 * V * k);
 #pragma unroll
           for (int j = 0; j < V; ++j)
             y.t[j] = from_f32<TO>((p.accumulate ? to_f32(y.t[j]) : 0.f) + to_f32(x[r][k].t[j]) * p.scale);

@@ -79,8 +79,8 @@ __device__ __forceinline__ void store8(T* p, int vec, int n, const float (&v)[8]
 __device__ __forceinline__ void load_bits8(const uint32_t* words, int64_t k, int n, float (&v)[8]) {
   const int64_t w = k >> 5;
   const int sh = (int)(k & 31);
-  uint32_t x = __ldg(words + w) >> sh;
-  if (sh + n > 32) x |= __ldg(words + w + 1) << (32 - sh);
+  uint32_t x = words[w] >> sh;
+  if (sh + n > 32) x |= words[w + 1] << (32 - sh);
 #pragma unroll
   for (int i = 0; i < 8; ++i) v[i] = i < n ? ((x >> i) & 1u ? 1.f : -1.f) : 0.f;
 }
@@ -379,10 +379,9 @@ __device__ __forceinline__ void last_cell(const GemmArgs& p, uint32_t cell, int6
       T* out = (T*)p.out + b * p.batch_out + k * p.rep_out + (int64_t)(row0 + r0) * p.ld_out + col;
       Pack<T, 4> y[4];
       if (p.w_in) {
-        // plain loads: in and out may be the same buffer
         const T* in = (const T*)p.w_in + b * p.batch_in + k * p.rep_in + (int64_t)(row0 + r0) * p.ld_in + col;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) y[i].load_plain(in + i * 8 * p.ld_in);
+        for (int i = 0; i < 4; ++i) y[i].load(in + i * 8 * p.ld_in);
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
