@@ -281,8 +281,9 @@ cudaError_t launch_gemm(Operand& a, Operand& b, const GemmArgs& g, cudaStream_t 
 
 // Microseconds of one product in tiles of 128 x 128 (shape 0), 256 x 128 (1) or 256 x 256 (2), the last two by pairs of
 // CTAs: waves of tiles times the stages of one, and what a launch takes beside them.  Fitted to 17 sizes from 200 x 200
-// to 4096 x 4096, off by at most a sixth.  Both sides, one plane: at 512 x 512 shape 0 takes 91 us and 2 takes 137, at
-// 4096 x 4096 1.37 ms and 1.04; two planes: at 1500 x 1500 shape 0 takes 329 us and 1 takes 291.
+// to 4096 x 4096; at 40 sizes, batches of up to 24 among them, a call's 15 products and the passes before them are off
+// by at most a fifth.  Both sides, one plane: at 512 x 512 shape 0 takes 90 us and 2 takes 137, at 4096 x 4096 1.32 ms
+// and 1.03; two planes: at 1500 x 1500 (bfloat16 result) shape 0 takes 324 us and 1 takes 293.
 int64_t tiles_of(const OrthoPlan& q, bool symmetric, int shape) {
   const int tm = shape == 0 ? 128 : 256, tn = shape == 2 ? 256 : 128;
   const int64_t sym = (q.m + tm - 1) / tm, tr = (q.rows + tm - 1) / tm, tc = (q.cols + tn - 1) / tn;
@@ -299,11 +300,15 @@ double product_cost(const OrthoPlan& q, bool symmetric, int contraction, int sha
 }
 
 // Which shapes a call's products take.  A symmetric result is stored by blocks of as many rows as the tiles have, so
-// either all products take shape 0, or each the better one of the other two.
+// either all products take shape 0, or each the better one of the other two.  Two planes with accumulators of one stage
+// (kLongChunkFrom) always take shape 0: pairs would have to empty twice the accumulators every 64 of the contraction, and
+// at 34 sizes between 130 x 130 and 1590 x 4000 no shape of theirs was faster (12 x 768 x 768: 474 us against 554, 4 x 1300 x
+// 1700: 870 against 1263).
 struct Shapes {
   bool pairs, wide_gram, wide_poly, wide_step;
 };
 Shapes choose_shapes(const OrthoPlan& q) {
+  if (q.planes == 2 && q.chunk == 1) return Shapes{};
   const int n = q.rows < q.cols ? q.cols : q.rows;
   const bool symmetric[3] = {true, true, false};
   const int contraction[3] = {n, q.m, q.m};
