@@ -193,3 +193,100 @@ def test_tensors_on_the_host_are_refused():
         with pytest.raises(ValueError, match="GPU"):
             call()
     torch.cuda.synchronize()
+
+
+# ---- pairs of CTAs -------------------------------------------------------------------------------------------------
+# Products by pairs of CTAs: float32 and float16 results from a short side of 1600 on, bfloat16 ones and HALF from some
+# 1400 (tiles of 256 x 128 and, from 2000 or in batches, 256 x 256).
+
+PAIRS = [(1, 1610, 1700), (1, 2100, 1650), (2, 2048, 2048)]
+
+
+@pytest.mark.parametrize("shape", PAIRS)
+@pytest.mark.parametrize("precision", [B.ORTHO_HALF, B.ORTHO_SINGLE])
+def test_float16_results_by_pairs(shape, precision):
+    b, r, c = shape
+    g = randn(b, r, c, seed=r).half()
+    out = torch.empty_like(g)
+    plan = B.Orthogonalizer(r, c, batch=b, params=B.ortho_params(precision=precision))
+    plan.orthogonalize(g, out)
+    plan.check()
+    want = direction64(g)
+    for e in range(b):
+        # entries of some 0.02: subnormal ones lose half of 2^-24 at most
+        assert rel(out[e], want[e]) <= bound(precision, F16) + 2.0 ** -25 * (r * c) ** 0.5 / float(want[e].norm())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("precision", [B.ORTHO_HALF, B.ORTHO_SINGLE])
+@pytest.mark.parametrize("shape", [(1700, 1610), (2050, 2303)])
+def test_bad_matrices_by_pairs(shape, precision, dtype):
+    g = randn(4, *shape, seed=1)
+    g[0, -1, -1] = float("nan")
+    g[1] = 0
+    g[2, 0, 300] = float("inf")
+    out = torch.empty(4, *shape, device="cuda", dtype=dtype)
+    plan = B.Orthogonalizer(*shape, batch=4, params=B.ortho_params(precision=precision))
+    plan.orthogonalize(g, out)
+    plan.check()
+    assert bool(out[0].isnan().all()) and bool(out[2].isnan().all()) and bool((out[1] == 0).all())
+    assert rel(out[3], direction64(g[3:])[0]) <= bound(precision, dtype) + 2.0 ** -25 * 46
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("shape,gap,at", [((1650, 1611), 3, 5), ((2049, 2110), 1, 1), ((2304, 2048), 7, 3)])
+def test_odd_strides_by_pairs(shape, gap, at, dtype):
+    (r, c), b = shape, 2
+    ld = c + gap
+    st = ld * (r + 2) + 1
+    flat = randn(b * st + 16, seed=5).to(dtype)
+    g = flat.as_strided((b, r, c), (st, ld, 1), at)
+    store = torch.full((b * st + 16,), 9.0, device="cuda", dtype=dtype)
+    out = store.as_strided((b, r, c), (st, ld, 1), at + 2)
+    B.Orthogonalizer(r, c, batch=b).orthogonalize(g, out)
+    want = direction64(g)
+    assert rel(out, want) <= bound(AUTO[dtype], dtype) + 2.0 ** -25 * 46
+    out.fill_(9.0)
+    assert bool((store == 9.0).all())
+
+
+@pytest.mark.parametrize("tw", [F32, BF16, F16])
+@pytest.mark.parametrize("shape,offset", [((2, 1611, 1700), 45), ((1, 2111, 2050), 7)])
+def test_muon_step_from_packed_bits_by_pairs(shape, offset, tw):
+    n = shape[0] * shape[1] * shape[2]
+    words = torch.randint(-2 ** 31, 2 ** 31, ((offset + n + 31) // 32,), device="cuda", generator=gen(1)).int()
+    m, w = randn(*shape, seed=2, scale=3.0), randn(*shape, seed=3, scale=0.05).to(tw)
+    want_m, want_w, step = muon64(signs(words, offset, shape), m, w, 0.03, 0.9, False, 0.1, 1.5)
+    plan = B.Orthogonalizer(shape[1], shape[2], batch=shape[0])
+    plan.muon_step(words, m, w, 0.03, beta=0.9, nesterov=False, weight_decay=0.1, scale=1.5, bit_offset=offset)
+    plan.check()
+    assert rel(m, want_m) <= 2 ** -23
+    limit = TOL[AUTO[tw]] * step.norm() + (4 * U[F32] + U[tw]) * (want_w.norm() + step.norm()) + 2.0 ** -25 * n ** 0.5
+    assert float((w.double() - want_w).norm()) <= float(limit)
+
+
+@pytest.mark.parametrize("n,shape,at,gap", [(7, (60, 70), 3, 77), (5, (300, 200), 0, 64), (12, (1700, 130), 1, 5),
+                                            (4, (1620, 1700), 13, 3), (6, (120, 1500), 2, 2)])
+@pytest.mark.parametrize("tw", [F32, BF16])
+def test_many_replicas(n, shape, at, gap, tw):
+    # weights are rows of clients' parameter vectors, from odd elements on; what lies between them stays
+    r, c = shape
+    ld = r * c + gap + at
+    rows = randn(n, ld, seed=11).to(tw)
+    before = rows.clone()
+    w, w0 = rows.as_strided((n, 1, r, c), (ld, r * c, c, 1), at), before.as_strided((n, 1, r, c), (ld, r * c, c, 1), at)
+    m, g = randn(1, r, c, seed=12), randn(1, r, c, seed=13)
+    _, want, step = muon64(g, m, w0, 0.02, 0.95, True, 0.01, 0.3)
+    plan = B.Orthogonalizer(r, c)
+    other = torch.empty(n, 1, r, c, device="cuda", dtype=tw)
+    plan.muon_step(g, m.clone(), w, 0.02, weight_decay=0.01, scale=0.3, weights_out=other)
+    assert torch.equal(rows, before)
+    plan.muon_step(g, m, w, 0.02, weight_decay=0.01, scale=0.3)
+    plan.check()
+    assert torch.equal(w, other)
+    for k in range(n):
+        limit = TOL[AUTO[tw]] * step.norm() + (4 * U[F32] + U[tw]) * (want[k].norm() + step.norm())
+        assert float((w[k].double() - want[k]).norm()) <= float(limit)
+    w.zero_()
+    w0.zero_()
+    assert torch.equal(rows, before)
