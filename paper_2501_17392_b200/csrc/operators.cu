@@ -129,7 +129,8 @@ struct OrthoPlan {
   size_t off_partial, off_x[2], off_s, off_t[2], off_p, bytes;   // T of even and of odd steps
 };
 
-bool make_plan(OrthoPlan& q, int32_t batch, int32_t rows, int32_t cols, const brace_ortho_params* p, int out_type) {
+OrthoPlan make_plan(int32_t batch, int32_t rows, int32_t cols, const brace_ortho_params* p, int out_type) {
+  OrthoPlan q;
   q.batch = batch;
   q.rows = rows;
   q.cols = cols;
@@ -167,7 +168,7 @@ bool make_plan(OrthoPlan& q, int32_t batch, int32_t rows, int32_t cols, const br
   for (int k = 0; k < 2; ++k) q.off_t[k] = in_x ? q.off_x[k ^ 1] : apart;
   q.off_p = take(sb);
   q.bytes = at;
-  return true;
+  return q;
 }
 
 bool sizes_ok(int32_t batch, int32_t rows, int32_t cols) { return batch >= 0 && rows >= 0 && cols >= 0; }
@@ -671,7 +672,7 @@ EmbArgs emb_args(const brace_embedding* e) {
 
 template <typename TI, typename TO, int V>
 cudaError_t launch_lookup(const EmbArgs& a, cudaStream_t st) {
-  constexpr int kWide = 32 * (V >= 8 ? V : V == 2 ? 4 : 4);   // columns of a warp's stretch
+  constexpr int kWide = 32 * (V >= 8 ? V : 4);   // columns of a warp's stretch
   const int64_t x = (a.tokens + 8 * kLookupRows - 1) / (8 * kLookupRows), z = (a.dim + kWide - 1) / kWide;
   return launch(embedding_lookup_kernel<TI, TO, V>, dim3((unsigned)x, (unsigned)a.clients, (unsigned)z), 256, 0, 1, st, a);
 }
@@ -800,9 +801,7 @@ size_t brace_ortho_workspace_bytes(int32_t batch, int32_t rows, int32_t cols, co
   if (!coefficients_ok(params) || !float_type(out_type) || !sizes_ok(batch, rows, cols)) return 0;
   if (!sizes_served(batch, rows, cols)) return 0;
   if (batch == 0 || rows == 0 || cols == 0) return 256;
-  OrthoPlan q;
-  make_plan(q, batch, rows, cols, params, out_type);
-  return q.bytes;
+  return make_plan(batch, rows, cols, params, out_type).bytes;
 }
 
 int brace_orthogonalize(int32_t batch, int32_t rows, int32_t cols, const brace_ortho_params* params, const void* d_g,
@@ -815,8 +814,7 @@ int brace_orthogonalize(int32_t batch, int32_t rows, int32_t cols, const brace_o
   if (!d_out || ld_out < cols || !aligned(d_out, (size_t)elem_bytes(out_type))) return BRACE_ERR_INVALID_ARG;
   if (batch > 1 && stride_out == 0) return BRACE_ERR_INVALID_ARG;   // what is written is a place of its own for each
   if (!sizes_served(batch, rows, cols)) return BRACE_ERR_UNSUPPORTED;
-  OrthoPlan q;
-  make_plan(q, batch, rows, cols, params, out_type);
+  const OrthoPlan q = make_plan(batch, rows, cols, params, out_type);
   if (!d_workspace || workspace_bytes < q.bytes || !aligned(d_workspace, 256)) return BRACE_ERR_WORKSPACE;
   PrepArgs prep = {};
   prep.g = mat_ref(d_g, g_type, ld_g, stride_g, bit_offset);
@@ -849,8 +847,7 @@ int brace_muon_step(int32_t batch, int32_t rows, int32_t cols, const brace_ortho
   if (batch > 1 && (s->stride_momentum_out == 0 || s->stride_weights_out == 0)) return BRACE_ERR_INVALID_ARG;
   if (s->replicas > 1 && s->replica_weights_out == 0) return BRACE_ERR_INVALID_ARG;
   if (!sizes_served(batch, rows, cols)) return BRACE_ERR_UNSUPPORTED;
-  OrthoPlan q;
-  make_plan(q, batch, rows, cols, params, s->weights_type);
+  const OrthoPlan q = make_plan(batch, rows, cols, params, s->weights_type);
   if (!d_workspace || workspace_bytes < q.bytes || !aligned(d_workspace, 256)) return BRACE_ERR_WORKSPACE;
   PrepArgs prep = {};
   prep.g = mat_ref(s->d_grad, s->grad_type, s->ld_grad, s->stride_grad, s->bit_offset);
