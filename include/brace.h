@@ -399,8 +399,9 @@ int brace_aggregate_static(int32_t n, int64_t d, const brace_params* params, con
  * no alignment beyond the element's own (rows that start on 16-byte boundaries
  * are read and written in wider words).  A workspace belongs to one call at a
  * time: it is free again once that call's work on its stream is complete.  The
- * first call on a device makes the CUDA runtime load the kernels there: make it
- * outside any stream capture; later calls may be captured.
+ * first call of a form (shapes, types, alignment, precision) on a device makes
+ * the CUDA runtime load its kernels there: make it outside any stream capture;
+ * calls of the same form may be captured from then on.
  * ------------------------------------------------------------------------- */
 
 /* element types */
@@ -442,8 +443,8 @@ typedef struct brace_ortho_params {
 int brace_ortho_default_params(brace_ortho_params* params);
 
 /* Bytes of workspace for `batch` matrices of rows x cols whose result has
- * `out_type`; 0 if the arguments are invalid.  With precision AUTO a workspace
- * sized for BRACE_TYPE_F32 serves every result type. */
+ * `out_type`; 0 if the arguments are invalid.  A workspace sized for
+ * BRACE_TYPE_F32 serves every result type. */
 size_t brace_ortho_workspace_bytes(int32_t batch, int32_t rows, int32_t cols, const brace_ortho_params* params,
                                    int32_t out_type);
 

@@ -423,7 +423,8 @@ class Orthogonalizer:
 
     Matrices are float32, bfloat16 or float16 tensors [batch, rows, cols] (or [rows, cols] where batch is 1) whose
     last stride is 1; an int32 tensor is a row of packed bits as a round leaves it, with the matrices one after the
-    other from `bit_offset` on.  An object serves one host thread, and one stream at a time (its workspace)."""
+    other from `bit_offset` on.  All are on the current GPU.  An object serves one host thread, and one stream at a time (its
+    workspace)."""
 
     def __init__(self, rows: int, cols: int, batch: int = 1, params: OrthoParams | None = None, device="cuda",
                  workspace: torch.Tensor | None = None):
@@ -534,8 +535,8 @@ class Embedding:
 
     Tables (and their gradients) are tensors [clients, vocab, dim] -- views of the clients' rows of weights or updates
     -- or [vocab, dim]; activations [clients, n, dim] or [n, dim]; ids int64 or int32 [clients, n] or [n].  The last
-    stride is 1.  `grad` = False leaves the gradient's workspace out.  An object serves one host thread, and one stream
-    at a time (its workspace)."""
+    stride is 1.  All are on the current GPU.  `grad` = False leaves the gradient's workspace out.  An object serves one
+    host thread, and one stream at a time (its workspace)."""
 
     def __init__(self, vocab: int, dim: int, tokens: int, clients: int = 1, grad: bool = True, device="cuda",
                  workspace: torch.Tensor | None = None):

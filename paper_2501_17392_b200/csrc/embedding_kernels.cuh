@@ -57,7 +57,7 @@ __device__ __forceinline__ int64_t load_id(const EmbArgs& p, int64_t c, int64_t 
 // ---- lookup -----------------------------------------------------------------------------------------------------
 // A warp takes kLookupRows rows and of each a stretch of 32 V Q columns, all loads first.  Rows that do not start on
 // whole words are read and written element by element, 32 neighbours at a time.  Bound by HBM: 16 x 8192 rows of 768 in
-// 62 us, 0.92 of the copy rate by the rows read once and written once (threads that divided a flat index took 79 us).
+// 65.5 us, 0.87 of the copy rate by the rows read once and written once (threads that divided a flat index took 79 us).
 constexpr int kLookupRows = 4;
 
 template <typename TI, typename TO, int V>

@@ -464,9 +464,10 @@ __device__ __forceinline__ void finish_block(const GemmArgs& p, uint32_t cell, i
 // One product of the iteration over tiles of 128 x 128 (CG = 1) or, by a pair of CTAs, 256 x TN (CG = 2), NP planes
 // per operand.  Warp 0 loads, warp 1 issues the matrix instructions, warp 2 owns the tensor memory, warps 4.. read the
 // accumulators and write the results; persistent over tiles, so that the epilogue of a tile runs under the products
-// of the next.  Bound by the matrix rate at large sizes: 4096 x 4096, one plane, five steps in 1.03 ms, 1.33 PFLOP/s of
-// the 1.37 that the power cap sustains; by launches, first loads and epilogues (some 4.5 us a product, 7 with two
-// planes) below 1000.
+// of the next.  Bound by the matrix rate at large sizes: 4096 x 4096, five steps, one plane 1.03 ms, 1.33 PFLOP/s, in a
+// short loop and 1.23 ms in one of seconds, where the power cap sustains 1.37 PFLOP/s of a library product; two planes
+// 3.4 ms, 1.20 PFLOP/s, and 3.7; by launches, first loads and epilogues (some 4.5 us a product, 7 with two planes) below
+// 1000.
 template <int CG, int TN, int NP, int OP_A, int OP_B, int MODE, typename TOUT, int KS>
 __global__ void __launch_bounds__(GemmShape<CG, TN, NP>::kThreads, 1)
     ortho_gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmArgs p) {
@@ -800,10 +801,10 @@ __global__ void __launch_bounds__(GemmShape<CG, TN, NP>::kThreads, 1)
 // cluster adds the shares through distributed shared memory (each CTA adds the rows that it owns and hands them to
 // all), and every CTA forms P itself and takes its slice to P X.
 // At these sizes nothing is bound by bandwidth or by the products (a 128 x 128 product is some 0.3 us); what counts is
-// the chain of dependent steps, which as separate launches costs a launch and a round trip through L2 each: 128 x 128
-// takes 23 us (a step 4.2: products 0.6 each, epilogues 0.7 to 0.9) against 68 in launches of tiles, 40 x 40 15.  Several
-// CTAs spend 4 to 7 us a step on the exchange of S: 128 x 512 takes 49 us against 78, 128 x 1024 in float32 72 against
-// 154.
+// the chain of dependent steps, which as separate launches costs a launch and a round trip through L2 each: with one plane
+// 128 x 128 takes 23 us (a step 4.2: products 0.6 each, epilogues 0.7 to 0.9) against 68 in launches of tiles, with two
+// 38; 40 x 40 15 and 21.  Several CTAs spend 4 to 7 us a step on the exchange of S: one plane 128 x 512 takes 49 us against
+// 78, two planes 67, 128 x 1024 72 against 154 and 128 x 2048, by 16 CTAs, 83.
 // ---------------------------------------------------------------------------------------------------------------
 
 struct ResidentArgs {
