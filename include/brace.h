@@ -543,6 +543,100 @@ size_t brace_embedding_workspace_bytes(int32_t clients, int64_t tokens, int64_t 
  * clients), and WORKSPACE (missing, too small or not 256-byte aligned). */
 int brace_embedding_grad(const brace_embedding* e, void* d_workspace, size_t workspace_bytes, brace_stream_t stream);
 
+/* ---------------------------------------------------------------------------
+ * Operators inside a client's local step, and of its update before the ring.
+ * The conventions of the operators above hold.  No buffer that is written may
+ * overlap another one of the call, but where a call says so.
+ * ------------------------------------------------------------------------- */
+
+/* Layer norm of `clients` clients' activations, `rows` rows of `dim` values each,
+ * with each client's own weight and bias (pieces of its row of weights; a stride
+ * of 0: one for all clients; NULL: weight 1, bias 0):
+ *   mean = sum x / dim,  var = sum (x - mean)^2 / dim,  rstd = 1 / sqrt(var + eps)
+ *   y = (x - mean) rstd weight + bias
+ * Client c's rows start c * stride_* elements after the pointer, rows are ld_*
+ * apart.  Statistics and sums are float32, y is rounded once. */
+typedef struct brace_layer_norm {
+  int32_t clients;         /* 0..65535                                                            */
+  int32_t dim;             /* 1..2^22 (more: BRACE_ERR_UNSUPPORTED)                               */
+  int64_t rows;            /* per client, 0..2^31-1                                               */
+  const void* d_x;
+  int64_t ld_x, stride_x;  /* 0: one row for all rows, one set of rows for all clients             */
+  const void* d_weight;
+  int64_t stride_weight;
+  const void* d_bias;      /* forward                                                              */
+  int64_t stride_bias;
+  void* d_y;               /* forward: written; gradient: the gradient of y, read                  */
+  int64_t ld_y, stride_y;  /* gradient: may be 0 as ld_x and stride_x                              */
+  float* d_mean;           /* [clients][stride_stats]; forward: written, or NULL; gradient: read   */
+  float* d_rstd;
+  int64_t stride_stats;
+  void* d_dx;              /* the rest: gradient; of x_type                                        */
+  int64_t ld_dx, stride_dx;
+  void* d_dweight;         /* of grad_type, or NULL: not wanted                                    */
+  int64_t stride_dweight;
+  void* d_dbias;
+  int64_t stride_dbias;
+  int32_t x_type, y_type, weight_type, grad_type; /* F32, BF16, F16                                */
+  int32_t accumulate;      /* add to what dweight and dbias hold                                   */
+  float eps;               /* forward; finite, >= 0                                                */
+} brace_layer_norm;
+
+/* Errors: INVALID_ARG (null, size out of range, ld < dim, bad type, misaligned
+ * pointer, bad eps, stride_y 0 or stride_stats < rows with several clients),
+ * UNSUPPORTED, CUDA. */
+int brace_layer_norm_forward(const brace_layer_norm* e, brace_stream_t stream);
+
+/* Bytes of workspace of brace_layer_norm_grad (it serves fewer rows too); 0 if the
+ * arguments are invalid or not supported. */
+size_t brace_layer_norm_workspace_bytes(int32_t clients, int64_t rows, int32_t dim);
+
+/* With xh = (x - mean) rstd and g = dy weight:
+ *   dx = rstd (g - sum g / dim - xh sum(g xh) / dim)
+ *   dweight[c] = sum over the rows of dy xh,  dbias[c] = sum over the rows of dy
+ * The sums are float32 in one order: the same bits every time.  Rows of 0 give
+ * dweight = dbias = 0.  Errors as above (stride_dx, stride_dweight or
+ * stride_dbias 0 with several clients), and WORKSPACE. */
+int brace_layer_norm_grad(const brace_layer_norm* e, void* d_workspace, size_t workspace_bytes, brace_stream_t stream);
+
+/* One of the tensors of every client: rows x cols values at d_in + c * stride_in,
+ * rows ld_in apart; what is written goes to d_out the same way.  d_out may equal
+ * d_in (in place, of the same type and layout). */
+typedef struct brace_tensor {
+  const void* d_in;
+  void* d_out;
+  int64_t rows, cols;      /* >= 0                                                                 */
+  int64_t ld_in, stride_in;
+  int64_t ld_out, stride_out;
+  int32_t in_type, out_type; /* F32, BF16, F16                                                     */
+} brace_tensor;
+
+/* What becomes of a client whose norm is not finite. */
+enum {
+  BRACE_CLIP_PROPAGATE = 0, /* what the formula gives: an infinite norm makes finite values 0 and infinities NaN,
+                               a NaN makes all values NaN                                          */
+  BRACE_CLIP_ZERO = 1       /* zeros: the client has no part in a sum over the clients             */
+};
+
+/* Workspace of the two calls below; 0 if the arguments are invalid. */
+size_t brace_clip_workspace_bytes(int32_t clients, const brace_tensor* h_tensors, int32_t count);
+
+/* d_norms[c] = sqrt(sum over the tensors of the sum of x^2), for every client.
+ * Summed in float64 in one order (the same bits every time) whatever the values'
+ * size; rounded once to float32.  d_out is not used. */
+int brace_gradient_norm(int32_t clients, const brace_tensor* h_tensors, int32_t count, float* d_norms, void* d_workspace,
+                        size_t workspace_bytes, brace_stream_t stream);
+
+/* Every client's tensors times min(1, max_norm / (norm + eps)), norm as above over
+ * all of the client's tensors; the product is rounded once.  d_norms may be NULL.
+ * Errors of both: INVALID_ARG (null, negative size, ld < cols, bad type,
+ * misaligned pointer, stride_out 0 with several clients, d_out = d_in with another
+ * layout, max_norm or eps negative or not finite), WORKSPACE, UNSUPPORTED (more
+ * than 2^46 values a client), CUDA. */
+int brace_gradient_clip(int32_t clients, const brace_tensor* h_tensors, int32_t count, float max_norm, float eps,
+                        int32_t nonfinite, float* d_norms, void* d_workspace, size_t workspace_bytes,
+                        brace_stream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

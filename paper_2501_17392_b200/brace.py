@@ -26,6 +26,7 @@ DRAWS_SUPPLIED, DRAWS_GENERATED = 0, 1
 DRAW_UNIFORM, DRAW_NORMAL = 0, 1
 TYPE_F32, TYPE_BF16, TYPE_F16, TYPE_BITS = range(4)
 ORTHO_AUTO, ORTHO_HALF, ORTHO_SINGLE = 0, 1, 2
+CLIP_PROPAGATE, CLIP_ZERO = 0, 1
 
 
 class Params(C.Structure):
@@ -70,6 +71,23 @@ class EmbeddingArgs(C.Structure):
                 ("stride_ids", C.c_int64), ("d_act", C.c_void_p), ("ld_act", C.c_int64), ("stride_act", C.c_int64),
                 ("table_type", C.c_int32), ("act_type", C.c_int32), ("id_bytes", C.c_int32),
                 ("accumulate", C.c_int32), ("scale", C.c_float)]
+
+
+class LayerNormArgs(C.Structure):
+    _fields_ = [("clients", C.c_int32), ("dim", C.c_int32), ("rows", C.c_int64), ("d_x", C.c_void_p),
+                ("ld_x", C.c_int64), ("stride_x", C.c_int64), ("d_weight", C.c_void_p), ("stride_weight", C.c_int64),
+                ("d_bias", C.c_void_p), ("stride_bias", C.c_int64), ("d_y", C.c_void_p), ("ld_y", C.c_int64),
+                ("stride_y", C.c_int64), ("d_mean", C.c_void_p), ("d_rstd", C.c_void_p), ("stride_stats", C.c_int64),
+                ("d_dx", C.c_void_p), ("ld_dx", C.c_int64), ("stride_dx", C.c_int64), ("d_dweight", C.c_void_p),
+                ("stride_dweight", C.c_int64), ("d_dbias", C.c_void_p), ("stride_dbias", C.c_int64),
+                ("x_type", C.c_int32), ("y_type", C.c_int32), ("weight_type", C.c_int32), ("grad_type", C.c_int32),
+                ("accumulate", C.c_int32), ("eps", C.c_float)]
+
+
+class TensorArgs(C.Structure):
+    _fields_ = [("d_in", C.c_void_p), ("d_out", C.c_void_p), ("rows", C.c_int64), ("cols", C.c_int64),
+                ("ld_in", C.c_int64), ("stride_in", C.c_int64), ("ld_out", C.c_int64), ("stride_out", C.c_int64),
+                ("in_type", C.c_int32), ("out_type", C.c_int32)]
 
 
 class BraceError(RuntimeError):
@@ -123,6 +141,14 @@ SIGNATURES = {
     "brace_embedding_lookup": (C.c_int, [C.POINTER(EmbeddingArgs), C.c_void_p]),
     "brace_embedding_workspace_bytes": (C.c_size_t, [C.c_int32, C.c_int64, C.c_int64, C.c_int32]),
     "brace_embedding_grad": (C.c_int, [C.POINTER(EmbeddingArgs), C.c_void_p, C.c_size_t, C.c_void_p]),
+    "brace_layer_norm_forward": (C.c_int, [C.POINTER(LayerNormArgs), C.c_void_p]),
+    "brace_layer_norm_workspace_bytes": (C.c_size_t, [C.c_int32, C.c_int64, C.c_int32]),
+    "brace_layer_norm_grad": (C.c_int, [C.POINTER(LayerNormArgs), C.c_void_p, C.c_size_t, C.c_void_p]),
+    "brace_clip_workspace_bytes": (C.c_size_t, [C.c_int32, C.POINTER(TensorArgs), C.c_int32]),
+    "brace_gradient_norm": (C.c_int, [C.c_int32, C.POINTER(TensorArgs), C.c_int32, C.c_void_p, C.c_void_p, C.c_size_t,
+                                      C.c_void_p]),
+    "brace_gradient_clip": (C.c_int, [C.c_int32, C.POINTER(TensorArgs), C.c_int32, C.c_float, C.c_float, C.c_int32,
+                                      C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
 }
 
 STATIC_SCRATCH_BYTES = 8 * 1024 * 1024
@@ -595,3 +621,198 @@ class Embedding:
              accumulate: bool = False, stream=None):
         """grad[c, v] = scale * the sum of dy[c, t] over the tokens with id v (added to grad with `accumulate`)."""
         _check(self.grad_status(dy, ids, grad, scale, accumulate, stream), "brace_embedding_grad")
+
+
+class LayerNorm:
+    """Layer norm of the activations of `clients` clients with up to `rows` rows each per call.
+
+    Activations are tensors [clients, n, dim] or [n, dim], weight and bias [clients, dim] -- pieces of the clients' rows of
+    weights -- or [dim] (forward: one for all clients), their gradients [clients, dim] or, of one client, [dim]; mean and
+    rstd float32 [clients, n] or [n].  The last stride is 1.  All are on the current GPU.  `grad` = False leaves the
+    gradient's workspace out.  An object serves one host thread, and one stream at a time (its workspace)."""
+
+    def __init__(self, dim: int, rows: int, clients: int = 1, eps: float = 1e-5, grad: bool = True, device="cuda",
+                 workspace: torch.Tensor | None = None):
+        self.dim, self.rows, self.clients, self.eps = dim, rows, clients, eps
+        if grad and workspace is None:
+            need = int(lib().brace_layer_norm_workspace_bytes(clients, rows, dim))
+            workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=device)
+        self.workspace = workspace
+        self._args = LayerNormArgs()
+
+    def _rows(self, t: torch.Tensor, name: str, n: int):
+        """(element type, ld, stride between clients) of activations."""
+        c, d, shape = self.clients, self.dim, t.shape
+        if shape != (c, n, d) and not (c == 1 and shape == (n, d)):
+            raise ValueError(f"{name} has shape {tuple(shape)}, not {(c, n, d)}")
+        kind, st = _FLOATS.get(t.dtype), t.stride()
+        if kind is None or (d > 1 and st[-1] != 1):
+            raise ValueError(f"{name} is of type {t.dtype} with strides {st}")
+        # the stride of a dimension of one element has no meaning
+        return kind, st[-2] if n > 1 else d, st[0] if c > 1 else 0
+
+    def _vector(self, t, name: str, shared: bool):
+        """(element type, stride between clients) of a weight, a bias or a gradient of them."""
+        if t is None:
+            return None, 0
+        c, d = self.clients, self.dim
+        if t.shape != (c, d) and not ((c == 1 or shared) and t.shape == (d,)):
+            raise ValueError(f"{name} has shape {tuple(t.shape)}, not {(c, d)}")
+        kind, st = _FLOATS.get(t.dtype), t.stride()
+        if kind is None or (d > 1 and st[-1] != 1):
+            raise ValueError(f"{name} is of type {t.dtype} with strides {st}")
+        return kind, st[0] if c > 1 and len(st) == 2 else 0
+
+    def _fill(self, x, y, mean, rstd, weight, bias) -> LayerNormArgs:
+        e, n = self._args, x.shape[-2] if x.dim() >= 2 else -1
+        if not 0 <= n <= self.rows:
+            raise ValueError(f"x has shape {tuple(x.shape)}: at most {self.rows} rows")
+        e.clients, e.dim, e.rows, e.eps = self.clients, self.dim, n, self.eps
+        e.x_type, e.ld_x, e.stride_x = self._rows(x, "x", n)
+        e.y_type, e.ld_y, e.stride_y = self._rows(y, "y", n)
+        wt, e.stride_weight = self._vector(weight, "weight", True)
+        bt, e.stride_bias = self._vector(bias, "bias", True)
+        if wt is not None and bt is not None and wt != bt:
+            raise ValueError("weight and bias have different types")
+        e.weight_type = wt if wt is not None else bt if bt is not None else TYPE_F32
+        e.stride_stats = n
+        for t, name in ((mean, "mean"), (rstd, "rstd")):
+            if t is None:
+                continue
+            if t.dtype != torch.float32 or (t.shape != (self.clients, n) and not (self.clients == 1 and t.shape == (n,))):
+                raise ValueError(f"{name} has shape {tuple(t.shape)} and type {t.dtype}, not {(self.clients, n)} and float32")
+            if n > 1 and t.stride(-1) != 1:
+                raise ValueError(f"{name}: the last dimension is not contiguous")
+        if self.clients > 1:
+            strides = {t.stride(0) for t in (mean, rstd) if t is not None}
+            if len(strides) > 1:
+                raise ValueError("mean and rstd have different strides")
+            e.stride_stats = strides.pop() if strides else n
+        e.d_x, e.d_y, e.d_mean, e.d_rstd = x.data_ptr(), y.data_ptr(), _ptr(mean), _ptr(rstd)
+        e.d_weight, e.d_bias = _ptr(weight), _ptr(bias)
+        return e
+
+    def forward_status(self, x, y, weight=None, bias=None, mean=None, rstd=None, stream=None) -> int:
+        e, at = self._fill(x, y, mean, rstd, weight, bias), x.get_device()
+        same = all(t is None or t.get_device() == at for t in (y, weight, bias, mean, rstd))
+        return lib().brace_layer_norm_forward(e, _launch_stream(stream, at, same))
+
+    def forward(self, x: torch.Tensor, y: torch.Tensor, weight: torch.Tensor | None = None,
+                bias: torch.Tensor | None = None, mean: torch.Tensor | None = None, rstd: torch.Tensor | None = None,
+                stream=None):
+        """y = (x - mean) rstd weight + bias; mean and rstd of the rows are written where they are given."""
+        _check(self.forward_status(x, y, weight, bias, mean, rstd, stream), "brace_layer_norm_forward")
+
+    def grad_status(self, dy, x, mean, rstd, dx, weight=None, dweight=None, dbias=None, accumulate: bool = False,
+                    stream=None) -> int:
+        e, ws, n = self._fill(x, dy, mean, rstd, weight, None), self.workspace, x.shape[-2]
+        kind, e.ld_dx, e.stride_dx = self._rows(dx, "dx", n)
+        if kind != e.x_type:
+            raise ValueError(f"dx is of type {dx.dtype}, x of {x.dtype}")
+        wt, e.stride_dweight = self._vector(dweight, "dweight", False)
+        bt, e.stride_dbias = self._vector(dbias, "dbias", False)
+        if wt is not None and bt is not None and wt != bt:
+            raise ValueError("dweight and dbias have different types")
+        e.grad_type = wt if wt is not None else bt if bt is not None else TYPE_F32
+        e.d_dx, e.d_dweight, e.d_dbias, e.accumulate = dx.data_ptr(), _ptr(dweight), _ptr(dbias), int(accumulate)
+        if ws is None:      # refused
+            return lib().brace_layer_norm_grad(e, 0, 0, 0)
+        at = x.get_device()
+        same = all(t is None or t.get_device() == at for t in (dy, mean, rstd, dx, weight, dweight, dbias, ws))
+        return lib().brace_layer_norm_grad(e, ws.data_ptr(), ws.numel(), _launch_stream(stream, at, same))
+
+    def grad(self, dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor, dx: torch.Tensor,
+             weight: torch.Tensor | None = None, dweight: torch.Tensor | None = None,
+             dbias: torch.Tensor | None = None, accumulate: bool = False, stream=None):
+        """dx, and (where they are given) the gradients of weight and bias, added to what these hold with `accumulate`."""
+        _check(self.grad_status(dy, x, mean, rstd, dx, weight, dweight, dbias, accumulate, stream),
+               "brace_layer_norm_grad")
+
+
+class GradientClip:
+    """Every client's gradient norm over a list of tensors, and the tensors clipped by it.
+
+    A tensor is [clients, ...], one client's part of it contiguous or a matrix of contiguous rows, float32, bfloat16 or
+    float16; `outs` are tensors of the same shapes (pieces of the update matrix, for instance) that the clipped gradients
+    are written to, without them clipping is in place.  All are on the current GPU.  The object is a plan: it keeps the
+    tensors, and every call works on what they hold then.  It serves one host thread, and one stream at a time (its
+    workspace)."""
+
+    def __init__(self, tensors, outs=None, workspace: torch.Tensor | None = None):
+        self.tensors = list(tensors)
+        self.outs = self.tensors if outs is None else list(outs)
+        if not self.tensors or len(self.outs) != len(self.tensors):
+            raise ValueError(f"{len(self.tensors)} tensors and {len(self.outs)} outputs")
+        self.clients = self.tensors[0].shape[0] if self.tensors[0].dim() else 0
+        self._list = (TensorArgs * len(self.tensors))()
+        for e, x, y in zip(self._list, self.tensors, self.outs):
+            if x.dim() < 1 or x.shape[0] != self.clients or y.shape != x.shape:
+                raise ValueError(f"a tensor has shape {tuple(x.shape)}, its output {tuple(y.shape)}; {self.clients} clients")
+            e.in_type, e.out_type = (_FLOATS.get(t.dtype, -1) for t in (x, y))
+            if e.in_type < 0 or e.out_type < 0:
+                raise ValueError(f"a tensor is of type {x.dtype}, its output of {y.dtype}")
+            e.d_in, e.d_out = x.data_ptr(), y.data_ptr()
+            e.rows, e.cols, e.ld_in, e.ld_out = self._layout(x, y)
+            many = self.clients > 1
+            e.stride_in, e.stride_out = (x.stride(0), y.stride(0)) if many else (0, 0)
+        self._device = self.tensors[0].get_device()
+        self._same = all(t.get_device() == self._device for t in self.tensors + self.outs)
+        if workspace is None:
+            need = int(lib().brace_clip_workspace_bytes(self.clients, self._list, len(self.tensors)))
+            workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=self.tensors[0].device)
+        self.workspace = workspace
+
+    @staticmethod
+    def _layout(x, y):
+        """(rows, columns, ld of x, ld of y) of one client's part."""
+        shape = list(x.shape[1:])
+        if x.numel() == 0:
+            return 0, 0, 0, 0
+        sizes = [(n, s, t) for n, s, t in zip(shape, x.stride()[1:], y.stride()[1:]) if n > 1]
+        merged = []          # from the smallest strides on: (size, stride of x, stride of y), runs joined
+        for n, s, t in sorted(sizes, key=lambda d: d[1:]):
+            if merged and s == merged[-1][0] * merged[-1][1] and t == merged[-1][0] * merged[-1][2]:
+                merged[-1] = (n * merged[-1][0], merged[-1][1], merged[-1][2])
+            else:
+                merged.append((n, s, t))
+        if merged and merged[0][1:] != (1, 1):
+            merged.insert(0, (1, 1, 1))
+        if len(merged) > 2:
+            raise ValueError(f"a tensor of shape {tuple(x.shape)} with strides {x.stride()} and {y.stride()} is neither "
+                             "contiguous nor a matrix of contiguous rows")
+        if len(merged) < 2:
+            n = merged[0][0] if merged else 1
+            return 1, n, n, n
+        return merged[1][0], merged[0][0], merged[1][1], merged[1][2]
+
+    def _norms(self, norms):
+        if norms is not None and (norms.dtype != torch.float32 or norms.shape != (self.clients,)
+                                  or (self.clients > 1 and norms.stride(0) != 1)):
+            raise ValueError(f"norms have shape {tuple(norms.shape)} and type {norms.dtype}, not {(self.clients,)} and float32")
+        return _ptr(norms)
+
+    def _stream(self, stream, norms):
+        at = self._device
+        return _launch_stream(stream, at, self._same and self.workspace.get_device() == at
+                              and (norms is None or norms.get_device() == at))
+
+    def norms_status(self, norms: torch.Tensor, stream=None) -> int:
+        to, st = self._norms(norms), self._stream(stream, norms)
+        return lib().brace_gradient_norm(self.clients, self._list, len(self.tensors), to, self.workspace.data_ptr(),
+                                         self.workspace.numel(), st)
+
+    def norms(self, norms: torch.Tensor, stream=None):
+        """norms[c] = the 2-norm of all of client c's tensors together."""
+        _check(self.norms_status(norms, stream), "brace_gradient_norm")
+
+    def clip_status(self, max_norm: float, norms: torch.Tensor | None = None, eps: float = 1e-6,
+                    nonfinite: int = CLIP_PROPAGATE, stream=None) -> int:
+        to, st = self._norms(norms), self._stream(stream, norms)
+        return lib().brace_gradient_clip(self.clients, self._list, len(self.tensors), max_norm, eps, nonfinite, to,
+                                         self.workspace.data_ptr(), self.workspace.numel(), st)
+
+    def clip(self, max_norm: float, norms: torch.Tensor | None = None, eps: float = 1e-6,
+             nonfinite: int = CLIP_PROPAGATE, stream=None):
+        """Every client's tensors times min(1, max_norm / (norm + eps)), written to the outputs; the norms where `norms` is
+        given.  `nonfinite`: CLIP_ZERO gives zeros for a client whose norm is not finite."""
+        _check(self.clip_status(max_norm, norms, eps, nonfinite, stream), "brace_gradient_clip")

@@ -12,10 +12,13 @@ ROOT = os.path.dirname(PKG_DIR)
 LIB_PATH = os.path.join(PKG_DIR, "libbrace.so")
 DEBUG_LIB_PATH = os.path.join(PKG_DIR, "libbrace_debug.so")
 OBJ_DIR = os.path.join(PKG_DIR, "_build")
-SOURCES = [os.path.join(PKG_DIR, "csrc", f) for f in ("brace.cu", "operators.cu")]
-DEPS = SOURCES + [os.path.join(PKG_DIR, "csrc", f) for f in ("brace_kernels.cuh", "elements.cuh", "embedding_kernels.cuh",
-                                                            "ortho_kernels.cuh", "sm100.cuh")]
-DEPS += [os.path.join(ROOT, "include", "brace.h")]
+# what each source is compiled from, beside itself and the C header
+_HEADERS = {
+    "brace.cu": ("brace_kernels.cuh",),
+    "operators.cu": ("elements.cuh", "embedding_kernels.cuh", "host.cuh", "ortho_kernels.cuh", "sm100.cuh"),
+    "layers.cu": ("clip_kernels.cuh", "elements.cuh", "host.cuh", "norm_kernels.cuh", "sm100.cuh"),
+}
+SOURCES = [os.path.join(PKG_DIR, "csrc", f) for f in _HEADERS]
 
 
 def _nvcc() -> str:
@@ -25,11 +28,17 @@ def _nvcc() -> str:
     return cand
 
 
-def needs_build(path: str = LIB_PATH) -> bool:
+def _deps(source: str):
+    name = os.path.basename(source)
+    return [source, os.path.join(ROOT, "include", "brace.h")] + [os.path.join(PKG_DIR, "csrc", f) for f in _HEADERS[name]]
+
+
+def needs_build(path: str = LIB_PATH, sources=SOURCES) -> bool:
+    """Whether what is compiled from `sources` is missing or older than they are."""
     if not os.path.exists(path):
         return True
     t = os.path.getmtime(path)
-    return any(os.path.getmtime(p) > t for p in DEPS)
+    return any(os.path.getmtime(p) > t for s in sources for p in _deps(s))
 
 
 def _object(source: str, defines) -> str:
@@ -48,7 +57,7 @@ def _compile(out_path: str, defines, verbose: bool) -> str:
     for source in SOURCES:
         obj = _object(source, defines)
         objects.append(obj)
-        if not verbose and not needs_build(obj):
+        if not verbose and not needs_build(obj, [source]):
             continue
         # written elsewhere first: an object that is there is whole
         part = f"{obj}.{os.getpid()}.o"

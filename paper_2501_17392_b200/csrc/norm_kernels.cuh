@@ -1,0 +1,364 @@
+// Layer norm of the clients' activations, forward and backward.
+//
+// Row t of client c: mean = sum x / D, var = sum (x - mean)^2 / D, rstd = 1 / sqrt(var + eps), xh = (x - mean) rstd,
+// y = xh w + b.  Backward, g = dy w: dx = rstd (g - sum g / D - xh sum(g xh) / D), dw = sum_t dy xh, db = sum_t dy.
+// Bound by memory: every activation is read once and written once.  G threads hold a row in registers (so that the
+// variance is summed from differences, in a second pass that reads nothing), a thread always has the same columns, keeps
+// their weights in registers for all of its rows and, backward, the sums of their gradients; the CTAs' sums are joined by
+// a second launch, in one order.  Sums are float32.
+#pragma once
+
+#include "elements.cuh"
+#include "sm100.cuh"
+
+namespace brace {
+
+constexpr int kNormThreads = 256;
+constexpr int kNormShort = 8192;     // longest row that a CTA's registers hold, its weights and its gradients' sums beside it
+
+struct NormArgs {
+  const void *x, *weight, *bias;
+  void* y;                           // forward: written; backward: the gradient of y, read
+  float *mean, *rstd;
+  void *dx, *dweight, *dbias;
+  float* part;                       // [client][part][2][dim]
+  int64_t ld_x, stride_x, stride_weight, stride_bias, ld_y, stride_y, stride_stats, ld_dx, stride_dx, stride_dweight, stride_dbias;
+  int64_t rows;
+  int dim, weight_type, grad_type, group, parts, accumulate;
+  float eps;
+};
+
+// Element i of an array of any element type.
+__device__ __forceinline__ float load_any(const void* p, int type, int64_t i) {
+  if (type == kTypeF32) return static_cast<const float*>(p)[i];
+  if (type == kTypeBF16) return __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]);
+  return __half2float(static_cast<const __half*>(p)[i]);
+}
+__device__ __forceinline__ void store_any(void* p, int type, int64_t i, float v) {
+  if (type == kTypeF32)
+    static_cast<float*>(p)[i] = v;
+  else if (type == kTypeBF16)
+    static_cast<__nv_bfloat16*>(p)[i] = __float2bfloat16_rn(v);
+  else
+    static_cast<__half*>(p)[i] = __float2half_rn(v);
+}
+
+// Sums over the `group` threads of a row.  Groups of more than a warp are the whole CTA; `cell` is then used by turns.
+template <int N>
+__device__ __forceinline__ void group_sum(float (&v)[N], int group, float (*cell)[kNormThreads / 32][2], int& turn) {
+  const int first = group < 32 ? group : 32;
+  for (int o = first >> 1; o; o >>= 1)
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+  if (group <= 32) return;
+  turn ^= 1;
+  if ((threadIdx.x & 31) == 0)
+#pragma unroll
+    for (int i = 0; i < N; ++i) cell[turn][threadIdx.x >> 5][i] = v[i];
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = 0.f;
+  for (int w = 0; w < (group >> 5); ++w)
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] += cell[turn][w][i];
+}
+
+// Forward.  Thread g of a row's G has the NV groups of V columns (i G + g) V .. + V.
+template <typename TX, typename TY, int V, int NV>
+__global__ void __launch_bounds__(kNormThreads) norm_forward_kernel(const NormArgs p) {
+  __shared__ float cell[2][kNormThreads / 32][2];
+  grid_trigger();
+  grid_wait();
+  const int G = p.group, slot = threadIdx.x / G, g = threadIdx.x % G, slots = blockDim.x / G;
+  const int64_t c = blockIdx.y;
+  const float inv = 1.f / (float)p.dim;
+  float w[NV * V], b[NV * V];
+#pragma unroll
+  for (int i = 0; i < NV * V; ++i) {
+    const int col = (i / V * G + g) * V + i % V;
+    w[i] = p.weight && col < p.dim ? load_any(p.weight, p.weight_type, c * p.stride_weight + col) : 1.f;
+    b[i] = p.bias && col < p.dim ? load_any(p.bias, p.weight_type, c * p.stride_bias + col) : 0.f;
+  }
+  const TX* x = static_cast<const TX*>(p.x) + c * p.stride_x;
+  TY* y = static_cast<TY*>(p.y) + c * p.stride_y;
+  int turn = 0;
+  for (int64_t r0 = (int64_t)blockIdx.x * slots; r0 < p.rows; r0 += (int64_t)gridDim.x * slots) {
+    const int64_t row = r0 + slot;
+    const bool live = row < p.rows;
+    Pack<TX, V> raw[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int col = (i * G + g) * V;
+      if (live && col < p.dim) raw[i].load(x + row * p.ld_x + col);
+    }
+    float v[NV * V], s[1] = {0.f};
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const bool here = live && (i * G + g) * V < p.dim;
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        v[i * V + k] = here ? to_f32(raw[i].t[k]) : 0.f;
+        s[0] += v[i * V + k];
+      }
+    }
+    group_sum(s, G, cell, turn);
+    const float mean = s[0] * inv;
+    s[0] = 0.f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const bool here = live && (i * G + g) * V < p.dim;
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        v[i * V + k] -= mean;
+        if (here) s[0] = fmaf(v[i * V + k], v[i * V + k], s[0]);
+      }
+    }
+    group_sum(s, G, cell, turn);
+    const float rstd = 1.f / sqrtf(fmaf(s[0], inv, p.eps));
+    if (!live) continue;
+    if (g == 0) {
+      if (p.mean) p.mean[c * p.stride_stats + row] = mean;
+      if (p.rstd) p.rstd[c * p.stride_stats + row] = rstd;
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int col = (i * G + g) * V;
+      Pack<TY, V> o;
+#pragma unroll
+      for (int k = 0; k < V; ++k) o.t[k] = from_f32<TY>(fmaf(v[i * V + k] * rstd, w[i * V + k], b[i * V + k]));
+      if (col < p.dim) o.store_plain(y + row * p.ld_y + col);
+    }
+  }
+}
+
+// Backward: dx, and this CTA's part of dweight and dbias (the whole of it where there is one CTA for a client).
+template <typename TX, typename TY, int V, int NV>
+__global__ void __launch_bounds__(kNormThreads) norm_grad_kernel(const NormArgs p) {
+  __shared__ float cell[2][kNormThreads / 32][2];
+  __shared__ float sums[2][1024];    // rows of a warp or less have at most 1024 columns
+  grid_trigger();
+  grid_wait();
+  const int G = p.group, slot = threadIdx.x / G, g = threadIdx.x % G, slots = blockDim.x / G;
+  const int64_t c = blockIdx.y;
+  const float inv = 1.f / (float)p.dim;
+  const bool params = p.dweight || p.dbias;
+  float w[NV * V], dw[NV * V], db[NV * V];
+#pragma unroll
+  for (int i = 0; i < NV * V; ++i) {
+    const int col = (i / V * G + g) * V + i % V;
+    w[i] = p.weight && col < p.dim ? load_any(p.weight, p.weight_type, c * p.stride_weight + col) : 1.f;
+    dw[i] = db[i] = 0.f;
+  }
+  const TX* x = static_cast<const TX*>(p.x) + c * p.stride_x;
+  const TY* dy = static_cast<const TY*>(p.y) + c * p.stride_y;
+  TX* dx = static_cast<TX*>(p.dx) + c * p.stride_dx;
+  int turn = 0;
+  for (int64_t r0 = (int64_t)blockIdx.x * slots; r0 < p.rows; r0 += (int64_t)gridDim.x * slots) {
+    const int64_t row = r0 + slot;
+    const bool live = row < p.rows;
+    Pack<TX, V> xr[NV];
+    Pack<TY, V> yr[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int col = (i * G + g) * V;
+      if (live && col < p.dim) {
+        xr[i].load(x + row * p.ld_x + col);
+        yr[i].load(dy + row * p.ld_y + col);
+      }
+    }
+    const float mean = live ? p.mean[c * p.stride_stats + row] : 0.f, rstd = live ? p.rstd[c * p.stride_stats + row] : 0.f;
+    float s[2] = {0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      if (live && (i * G + g) * V < p.dim) {
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+          const int e = i * V + k;
+          const float xh = (to_f32(xr[i].t[k]) - mean) * rstd, d = to_f32(yr[i].t[k]), gr = d * w[e];
+          s[0] += gr;
+          s[1] = fmaf(gr, xh, s[1]);
+          dw[e] = fmaf(d, xh, dw[e]);
+          db[e] += d;
+        }
+      }
+    }
+    group_sum(s, G, cell, turn);
+    const float m1 = s[0] * inv, m2 = s[1] * inv;
+    if (!live) continue;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int col = (i * G + g) * V;
+      Pack<TX, V> o;
+      if (col >= p.dim) continue;
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        const float xh = (to_f32(xr[i].t[k]) - mean) * rstd;
+        o.t[k] = from_f32<TX>(rstd * (fmaf(-xh, m2, to_f32(yr[i].t[k]) * w[i * V + k]) - m1));
+      }
+      o.store_plain(dx + row * p.ld_dx + col);
+    }
+  }
+  if (!params) return;
+  // rows of one warp first, then the warps one after the other
+  for (int o = G; o < 32; o <<= 1)
+#pragma unroll
+    for (int i = 0; i < NV * V; ++i) {
+      dw[i] += __shfl_xor_sync(0xffffffffu, dw[i], o);
+      db[i] += __shfl_xor_sync(0xffffffffu, db[i], o);
+    }
+  const int warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+  if (G <= 32 && warps > 1) {
+    for (int t = 0; t < warps; ++t) {
+      if (warp == t && (threadIdx.x & 31) < G) {
+#pragma unroll
+        for (int i = 0; i < NV * V; ++i) {
+          const int col = (i / V * G + g) * V + i % V;
+          if (col < p.dim) {
+            if (t > 0) {
+              dw[i] += sums[0][col];
+              db[i] += sums[1][col];
+            }
+            sums[0][col] = dw[i];
+            sums[1][col] = db[i];
+          }
+        }
+      }
+      __syncthreads();
+    }
+    if (warp != warps - 1) return;
+  }
+  if ((threadIdx.x & 31) >= G) return;
+#pragma unroll
+  for (int i = 0; i < NV * V; ++i) {
+    const int col = (i / V * G + g) * V + i % V;
+    if (col >= p.dim) continue;
+    if (p.parts > 1) {
+      float* to = p.part + (c * p.parts + blockIdx.x) * 2 * (int64_t)p.dim + col;
+      to[0] = dw[i];
+      to[p.dim] = db[i];
+    } else {
+      const int64_t at_w = c * p.stride_dweight + col, at_b = c * p.stride_dbias + col;
+      if (p.dweight) store_any(p.dweight, p.grad_type, at_w, p.accumulate ? load_any(p.dweight, p.grad_type, at_w) + dw[i] : dw[i]);
+      if (p.dbias) store_any(p.dbias, p.grad_type, at_b, p.accumulate ? load_any(p.dbias, p.grad_type, at_b) + db[i] : db[i]);
+    }
+  }
+}
+
+// dweight and dbias from the CTAs' parts: 32 columns a CTA, a warp takes every 8th part.
+__global__ void __launch_bounds__(256) norm_join_kernel(const NormArgs p) {
+  __shared__ float cell[8][32];
+  grid_trigger();
+  grid_wait();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, at = blockIdx.x * 32 + lane;   // of both vectors
+  const int64_t c = blockIdx.y;
+  float sum = 0.f;
+  if (at < 2 * p.dim) {
+    const float* from = p.part + c * p.parts * 2 * (int64_t)p.dim + at;
+#pragma unroll 4
+    for (int k = warp; k < p.parts; k += 8) sum += from[(int64_t)k * 2 * p.dim];
+  }
+  cell[warp][lane] = sum;
+  __syncthreads();
+  if (warp || at >= 2 * p.dim) return;
+  for (int k = 1; k < 8; ++k) sum += cell[k][lane];
+  void* to = at < p.dim ? p.dweight : p.dbias;
+  if (!to) return;
+  const int64_t i = at < p.dim ? c * p.stride_dweight + at : c * p.stride_dbias + at - p.dim;
+  store_any(to, p.grad_type, i, p.accumulate ? load_any(to, p.grad_type, i) + sum : sum);
+}
+
+// ---- rows longer than kNormShort: a CTA walks a row more than once (the later passes find it in L1 or L2), and the
+// weights' gradients take a pass of their own.
+
+template <typename TX, typename TY>
+__global__ void __launch_bounds__(kNormThreads) norm_forward_long_kernel(const NormArgs p) {
+  __shared__ float cell[2][kNormThreads / 32][2];
+  grid_trigger();
+  grid_wait();
+  const int64_t c = blockIdx.y;
+  const float inv = 1.f / (float)p.dim;
+  int turn = 0;
+  for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
+    const TX* x = static_cast<const TX*>(p.x) + c * p.stride_x + row * p.ld_x;
+    TY* y = static_cast<TY*>(p.y) + c * p.stride_y + row * p.ld_y;
+    float s[1] = {0.f};
+#pragma unroll 8
+    for (int i = threadIdx.x; i < p.dim; i += kNormThreads) s[0] += to_f32(x[i]);
+    group_sum(s, kNormThreads, cell, turn);
+    const float mean = s[0] * inv;
+    s[0] = 0.f;
+#pragma unroll 8
+    for (int i = threadIdx.x; i < p.dim; i += kNormThreads) {
+      const float d = to_f32(x[i]) - mean;
+      s[0] = fmaf(d, d, s[0]);
+    }
+    group_sum(s, kNormThreads, cell, turn);
+    const float rstd = 1.f / sqrtf(fmaf(s[0], inv, p.eps));
+    if (threadIdx.x == 0) {
+      if (p.mean) p.mean[c * p.stride_stats + row] = mean;
+      if (p.rstd) p.rstd[c * p.stride_stats + row] = rstd;
+    }
+#pragma unroll 4
+    for (int i = threadIdx.x; i < p.dim; i += kNormThreads) {
+      const float w = p.weight ? load_any(p.weight, p.weight_type, c * p.stride_weight + i) : 1.f;
+      const float b = p.bias ? load_any(p.bias, p.weight_type, c * p.stride_bias + i) : 0.f;
+      y[i] = from_f32<TY>(fmaf((to_f32(x[i]) - mean) * rstd, w, b));
+    }
+  }
+}
+
+template <typename TX, typename TY>
+__global__ void __launch_bounds__(kNormThreads) norm_grad_long_kernel(const NormArgs p) {
+  __shared__ float cell[2][kNormThreads / 32][2];
+  grid_trigger();
+  grid_wait();
+  const int64_t c = blockIdx.y;
+  const float inv = 1.f / (float)p.dim;
+  int turn = 0;
+  for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
+    const TX* x = static_cast<const TX*>(p.x) + c * p.stride_x + row * p.ld_x;
+    const TY* dy = static_cast<const TY*>(p.y) + c * p.stride_y + row * p.ld_y;
+    TX* dx = static_cast<TX*>(p.dx) + c * p.stride_dx + row * p.ld_dx;
+    const float mean = p.mean[c * p.stride_stats + row], rstd = p.rstd[c * p.stride_stats + row];
+    float s[2] = {0.f, 0.f};
+#pragma unroll 4
+    for (int i = threadIdx.x; i < p.dim; i += kNormThreads) {
+      const float w = p.weight ? load_any(p.weight, p.weight_type, c * p.stride_weight + i) : 1.f;
+      const float gr = to_f32(dy[i]) * w;
+      s[0] += gr;
+      s[1] = fmaf(gr, (to_f32(x[i]) - mean) * rstd, s[1]);
+    }
+    group_sum(s, kNormThreads, cell, turn);
+    const float m1 = s[0] * inv, m2 = s[1] * inv;
+#pragma unroll 4
+    for (int i = threadIdx.x; i < p.dim; i += kNormThreads) {
+      const float w = p.weight ? load_any(p.weight, p.weight_type, c * p.stride_weight + i) : 1.f;
+      const float xh = (to_f32(x[i]) - mean) * rstd;
+      dx[i] = from_f32<TX>(rstd * (fmaf(-xh, m2, to_f32(dy[i]) * w) - m1));
+    }
+  }
+}
+
+// Part blockIdx.y (every parts-th row) of dweight and dbias, a column a thread.
+template <typename TX, typename TY>
+__global__ void __launch_bounds__(kNormThreads) norm_columns_kernel(const NormArgs p) {
+  grid_trigger();
+  grid_wait();
+  const int64_t c = blockIdx.z;
+  const int col = blockIdx.x * kNormThreads + threadIdx.x;
+  if (col >= p.dim) return;
+  const TX* x = static_cast<const TX*>(p.x) + c * p.stride_x + col;
+  const TY* dy = static_cast<const TY*>(p.y) + c * p.stride_y + col;
+  float dw = 0.f, db = 0.f;
+#pragma unroll 4
+  for (int64_t row = blockIdx.y; row < p.rows; row += p.parts) {
+    const float d = to_f32(dy[row * p.ld_y]);
+    dw = fmaf(d, (to_f32(x[row * p.ld_x]) - p.mean[c * p.stride_stats + row]) * p.rstd[c * p.stride_stats + row], dw);
+    db += d;
+  }
+  float* to = p.part + (c * p.parts + blockIdx.y) * 2 * (int64_t)p.dim + col;
+  to[0] = dw;
+  to[p.dim] = db;
+}
+
+}  // namespace brace

@@ -2,85 +2,18 @@
 // C ABI declared in brace.h.
 #include "brace.h"
 
-#include <cuda.h>
-#include <cuda_runtime.h>
-
 #include <algorithm>
 #include <atomic>
 #include <cmath>
 #include <type_traits>
 
 #include "embedding_kernels.cuh"
+#include "host.cuh"
 #include "ortho_kernels.cuh"
-
-namespace brace {
-int cuda_fail_no_ctx(cudaError_t err);   // brace.cu: keeps the error for brace_last_cuda_error(NULL)
-}
 
 using namespace brace;
 
 namespace {
-
-inline int64_t round_up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
-inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
-
-int elem_bytes(int type) { return type == BRACE_TYPE_F32 || type == BRACE_TYPE_BITS ? 4 : 2; }
-bool float_type(int t) { return t == BRACE_TYPE_F32 || t == BRACE_TYPE_BF16 || t == BRACE_TYPE_F16; }
-
-// Rows and matrices whose 8-element groups are whole 16-byte words.
-bool wide_rows(const void* p, int type, int64_t ld, int64_t s1, int64_t s2 = 0) {
-  const int64_t per = 16 / elem_bytes(type);
-  return aligned(p, 16) && ld % per == 0 && s1 % per == 0 && s2 % per == 0;
-}
-
-int sm_count() {
-  static std::atomic<int> cached[64];
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 148;
-  int n = cached[dev].load(std::memory_order_relaxed);
-  if (n == 0) {
-    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) n = 148;
-    cached[dev].store(n, std::memory_order_relaxed);
-  }
-  return n;
-}
-
-// Every kernel here waits on the device for the one before it (griddepcontrol.wait) and may be set up while that one
-// drains.  `cluster`: CTAs per cluster.
-struct LaunchConfig {
-  cudaLaunchConfig_t cfg = {};
-  cudaLaunchAttribute attr[2];
-  LaunchConfig(dim3 grid, int block, size_t smem, int cluster, cudaStream_t st) {
-    cfg.gridDim = grid;
-    cfg.blockDim = dim3((unsigned)block);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = st;
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = (unsigned)cluster;
-    attr[1].val.clusterDim.y = 1;
-    attr[1].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = cluster > 1 ? 2 : 1;
-  }
-  LaunchConfig(const LaunchConfig&) = delete;   // cfg points into it
-};
-
-template <typename... KArgs, typename... Args>
-cudaError_t launch(void (*kernel)(KArgs...), dim3 grid, int block, size_t smem, int cluster, cudaStream_t st,
-                   const Args&... args) {
-  const LaunchConfig at(grid, block, smem, cluster, st);
-  return cudaLaunchKernelEx(&at.cfg, kernel, args...);
-}
-
-// Calls f with a value of the element type.
-template <typename F>
-cudaError_t with_type(int type, F&& f) {
-  if (type == BRACE_TYPE_F32) return f(float{});
-  if (type == BRACE_TYPE_BF16) return f(__nv_bfloat16{});
-  return f(__half{});
-}
 
 // ---- the orthogonalisation --------------------------------------------------------------------------------------
 
@@ -174,20 +107,6 @@ OrthoPlan make_plan(int32_t batch, int32_t rows, int32_t cols, const brace_ortho
 bool sizes_ok(int32_t batch, int32_t rows, int32_t cols) { return batch >= 0 && rows >= 0 && cols >= 0; }
 bool sizes_served(int32_t batch, int32_t rows, int32_t cols) {
   return batch <= 32767 && (int64_t)rows * (((int64_t)cols + 63) / 64 * 8) < (int64_t)1 << 31;
-}
-
-using EncodeFn = decltype(&cuTensorMapEncodeTiled);
-EncodeFn encode_fn() {
-  static std::atomic<void*> fn{nullptr};
-  void* f = fn.load(std::memory_order_acquire);
-  if (!f) {
-    cudaDriverEntryPointQueryResult found;
-    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found) != cudaSuccess ||
-        found != cudaDriverEntryPointSuccess)
-      return nullptr;
-    fn.store(f, std::memory_order_release);
-  }
-  return (EncodeFn)f;
 }
 
 // A matrix of operand planes in the workspace and its tensor maps, made when a launch first needs them: [planes of all
