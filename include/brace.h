@@ -637,6 +637,57 @@ int brace_gradient_clip(int32_t clients, const brace_tensor* h_tensors, int32_t 
                         int32_t nonfinite, float* d_norms, void* d_workspace, size_t workspace_bytes,
                         brace_stream_t stream);
 
+/* A tensor of heads: element (sequence b, token t, head h, dimension d) lies at
+ * d + b * stride + t * ld + h * head + d; strides count elements, are not
+ * negative, and may be 0 in what is only read. */
+typedef struct brace_heads {
+  void* d;
+  int64_t ld, head, stride;
+} brace_heads;
+
+/* Causal attention with a sliding window, and a few first tokens that stay
+ * visible behind it.  Of a sequence of n tokens, query i sees key j iff
+ *   j <= i  and  (i - j < window  or  j < sinks)
+ * head h reads key and value head h / (heads / kv_heads), and
+ *   s_ij = scale q_i.k_j,  lse_i = log sum_j exp s_ij,  out_i = sum_j exp(s_ij - lse_i) v_j
+ * over the keys that i sees; what a hidden place holds has no effect.  Rows from
+ * a sequence's length on are 0 in every result, and lse -infinity there, whatever
+ * the inputs hold.  Products and sums are float32 (of bfloat16 and float16 inputs
+ * on the tensor cores: exp(..) is rounded to the inputs' type for the sum over
+ * v), results are rounded once. */
+typedef struct brace_window_attention {
+  int32_t batch;           /* sequences, 0..65535                                                  */
+  int32_t tokens;          /* rows of a sequence, >= 0                                             */
+  int32_t heads, kv_heads; /* heads is a multiple of kv_heads; 0..65535                            */
+  int32_t dim;             /* of a head, 1..256 (more: BRACE_ERR_UNSUPPORTED)                      */
+  int32_t window, sinks;   /* window >= 1, sinks >= 0                                              */
+  int32_t type;            /* of all tensors: F32, BF16, F16                                       */
+  float scale;             /* finite                                                               */
+  const int32_t* d_lengths;/* tokens of each sequence (held to 0..tokens), or NULL: all            */
+  brace_heads q, k, v;
+  brace_heads out;         /* forward: written; gradient: read                                     */
+  float* d_lse;            /* (b, h, t) at b * stride_lse + h * head_lse + t; forward: written, or NULL */
+  int64_t head_lse, stride_lse;
+  brace_heads dout, dq, dk, dv; /* gradient: dout is read                                          */
+} brace_window_attention;
+
+/* Errors: INVALID_ARG (null, size out of range, bad type, misaligned pointer,
+ * negative stride, rows of a result or of lse that overlap), UNSUPPORTED, CUDA. */
+int brace_window_attention_forward(const brace_window_attention* e, brace_stream_t stream);
+
+/* Bytes of workspace of brace_window_attention_grad; 0 if the arguments are
+ * invalid or not supported. */
+size_t brace_window_attention_workspace_bytes(int32_t batch, int32_t tokens, int32_t heads, int32_t kv_heads, int32_t dim,
+                                              int32_t sinks);
+
+/* The gradients of sum(out * dout), out and lse as the forward pass left them.
+ * With p_ij = exp(s_ij - lse_i) and ds_ij = p_ij (dout_i.v_j - dout_i.out_i):
+ *   dq_i = scale sum_j ds_ij k_j
+ *   dk_j = scale sum ds_ij q_i,  dv_j = sum p_ij dout_i   over the queries and heads that read j
+ * in one order: the same bits every time.  Errors as above, and WORKSPACE. */
+int brace_window_attention_grad(const brace_window_attention* e, void* d_workspace, size_t workspace_bytes,
+                                brace_stream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

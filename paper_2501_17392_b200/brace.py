@@ -90,6 +90,18 @@ class TensorArgs(C.Structure):
                 ("in_type", C.c_int32), ("out_type", C.c_int32)]
 
 
+class Heads(C.Structure):
+    _fields_ = [("d", C.c_void_p), ("ld", C.c_int64), ("head", C.c_int64), ("stride", C.c_int64)]
+
+
+class WindowAttentionArgs(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("tokens", C.c_int32), ("heads", C.c_int32), ("kv_heads", C.c_int32),
+                ("dim", C.c_int32), ("window", C.c_int32), ("sinks", C.c_int32), ("type", C.c_int32),
+                ("scale", C.c_float), ("d_lengths", C.c_void_p), ("q", Heads), ("k", Heads), ("v", Heads),
+                ("out", Heads), ("d_lse", C.c_void_p), ("head_lse", C.c_int64), ("stride_lse", C.c_int64),
+                ("dout", Heads), ("dq", Heads), ("dk", Heads), ("dv", Heads)]
+
+
 class BraceError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -144,6 +156,9 @@ SIGNATURES = {
     "brace_layer_norm_forward": (C.c_int, [C.POINTER(LayerNormArgs), C.c_void_p]),
     "brace_layer_norm_workspace_bytes": (C.c_size_t, [C.c_int32, C.c_int64, C.c_int32]),
     "brace_layer_norm_grad": (C.c_int, [C.POINTER(LayerNormArgs), C.c_void_p, C.c_size_t, C.c_void_p]),
+    "brace_window_attention_forward": (C.c_int, [C.POINTER(WindowAttentionArgs), C.c_void_p]),
+    "brace_window_attention_workspace_bytes": (C.c_size_t, [C.c_int32] * 6),
+    "brace_window_attention_grad": (C.c_int, [C.POINTER(WindowAttentionArgs), C.c_void_p, C.c_size_t, C.c_void_p]),
     "brace_clip_workspace_bytes": (C.c_size_t, [C.c_int32, C.POINTER(TensorArgs), C.c_int32]),
     "brace_gradient_norm": (C.c_int, [C.c_int32, C.POINTER(TensorArgs), C.c_int32, C.c_void_p, C.c_void_p, C.c_size_t,
                                       C.c_void_p]),
@@ -727,6 +742,88 @@ class LayerNorm:
         """dx, and (where they are given) the gradients of weight and bias, added to what these hold with `accumulate`."""
         _check(self.grad_status(dy, x, mean, rstd, dx, weight, dweight, dbias, accumulate, stream),
                "brace_layer_norm_grad")
+
+
+class WindowAttention:
+    """Causal attention over `batch` sequences of up to `tokens` tokens each, with a sliding window and `sinks` first
+    tokens that stay visible: query i sees key j iff j <= i and (i - j < window or j < sinks).
+
+    Queries, outputs and their gradients are tensors [batch, n, heads, dim], keys and values [batch, n, kv_heads, dim], all
+    of one type (float32, bfloat16 or float16) with a contiguous last dimension -- views of one projection's result, for
+    instance; lse is float32 [batch, heads, n], lengths int32 [batch]: the tokens of each sequence, rows behind them are 0
+    in every result.  All are on the current GPU.  `scale` is 1 / sqrt(dim) where it is not given.  `grad` = False leaves
+    the gradient's workspace out.  An object serves one host thread, and one stream at a time (its workspace)."""
+
+    def __init__(self, heads: int, dim: int, tokens: int, batch: int = 1, kv_heads: int | None = None, window: int = 1024,
+                 sinks: int = 0, scale: float | None = None, grad: bool = True, device="cuda",
+                 workspace: torch.Tensor | None = None):
+        self.heads, self.dim, self.tokens, self.batch = heads, dim, tokens, batch
+        self.kv_heads = heads if kv_heads is None else kv_heads
+        self.window, self.sinks, self.scale = window, sinks, dim ** -0.5 if scale is None else scale
+        if grad and workspace is None:
+            need = int(lib().brace_window_attention_workspace_bytes(batch, tokens, heads, self.kv_heads, dim, sinks))
+            workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=device)
+        self.workspace = workspace
+        e = self._args = WindowAttentionArgs()
+        e.batch, e.heads, e.kv_heads, e.dim = batch, heads, self.kv_heads, dim
+        e.window, e.sinks, e.scale = window, sinks, self.scale
+
+    def _heads(self, to: Heads, t: torch.Tensor, name: str, n: int, heads: int, dtype):
+        if t.shape != (self.batch, n, heads, self.dim):
+            raise ValueError(f"{name} has shape {tuple(t.shape)}, not {(self.batch, n, heads, self.dim)}")
+        st = t.stride()
+        if t.dtype != dtype or (self.dim > 1 and st[3] != 1):
+            raise ValueError(f"{name} is of type {t.dtype} with strides {st}, q of type {dtype}")
+        # the stride of a dimension of one element has no meaning
+        to.d, to.stride, to.ld, to.head = t.data_ptr(), st[0] if self.batch > 1 else 0, st[1], st[2] if heads > 1 else 0
+
+    def _fill(self, q, k, v, out, lse, lengths) -> WindowAttentionArgs:
+        e, n, dtype = self._args, q.shape[1] if q.dim() == 4 else -1, q.dtype
+        if not 0 <= n <= self.tokens or dtype not in _FLOATS:
+            raise ValueError(f"q has shape {tuple(q.shape)} and type {dtype}: at most {self.tokens} tokens")
+        e.tokens, e.type = n, _FLOATS[dtype]
+        self._heads(e.q, q, "q", n, self.heads, dtype)
+        self._heads(e.k, k, "k", n, self.kv_heads, dtype)
+        self._heads(e.v, v, "v", n, self.kv_heads, dtype)
+        self._heads(e.out, out, "out", n, self.heads, dtype)
+        if lse is not None:
+            if lse.dtype != torch.float32 or lse.shape != (self.batch, self.heads, n) or (n > 1 and lse.stride(2) != 1):
+                raise ValueError(f"lse has shape {tuple(lse.shape)} and type {lse.dtype}, not "
+                                 f"{(self.batch, self.heads, n)} and float32")
+            e.stride_lse, e.head_lse = lse.stride(0), lse.stride(1)
+        if lengths is not None and (lengths.dtype != torch.int32 or lengths.shape != (self.batch,)
+                                    or (self.batch > 1 and lengths.stride(0) != 1)):
+            raise ValueError(f"lengths have shape {tuple(lengths.shape)} and type {lengths.dtype}, not {(self.batch,)} and int32")
+        e.d_lse, e.d_lengths = _ptr(lse), _ptr(lengths)
+        return e
+
+    def forward_status(self, q, k, v, out, lse=None, lengths=None, stream=None) -> int:
+        e, at = self._fill(q, k, v, out, lse, lengths), q.get_device()
+        same = all(t is None or t.get_device() == at for t in (k, v, out, lse, lengths))
+        return lib().brace_window_attention_forward(e, _launch_stream(stream, at, same))
+
+    def forward(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor,
+                lse: torch.Tensor | None = None, lengths: torch.Tensor | None = None, stream=None):
+        """out = softmax(scale q k^T over the keys seen) v; the logarithms of the softmax's sums where lse is given."""
+        _check(self.forward_status(q, k, v, out, lse, lengths, stream), "brace_window_attention_forward")
+
+    def grad_status(self, dout, q, k, v, out, lse, dq, dk, dv, lengths=None, stream=None) -> int:
+        e, ws, n = self._fill(q, k, v, out, lse, lengths), self.workspace, q.shape[1]
+        self._heads(e.dout, dout, "dout", n, self.heads, q.dtype)
+        self._heads(e.dq, dq, "dq", n, self.heads, q.dtype)
+        self._heads(e.dk, dk, "dk", n, self.kv_heads, q.dtype)
+        self._heads(e.dv, dv, "dv", n, self.kv_heads, q.dtype)
+        if ws is None:      # refused
+            return lib().brace_window_attention_grad(e, 0, 0, 0)
+        at = q.get_device()
+        same = all(t is None or t.get_device() == at for t in (dout, k, v, out, lse, dq, dk, dv, lengths, ws))
+        return lib().brace_window_attention_grad(e, ws.data_ptr(), ws.numel(), _launch_stream(stream, at, same))
+
+    def grad(self, dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor,
+             lse: torch.Tensor, dq: torch.Tensor, dk: torch.Tensor, dv: torch.Tensor,
+             lengths: torch.Tensor | None = None, stream=None):
+        """dq, dk and dv of sum(out * dout); out and lse are the forward pass's."""
+        _check(self.grad_status(dout, q, k, v, out, lse, dq, dk, dv, lengths, stream), "brace_window_attention_grad")
 
 
 class GradientClip:

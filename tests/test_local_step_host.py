@@ -136,3 +136,74 @@ def test_clip_binding_refuses():
             p.norms(norms)
     with pytest.raises(ValueError):      # the host's memory
         p.clip(1.0)
+
+
+# ---- attention
+
+def attention(grad=False, ws=P, nbytes=1 << 40, **over):
+    e = B.WindowAttentionArgs()
+    e.batch, e.tokens, e.heads, e.kv_heads, e.dim, e.window, e.sinks, e.type, e.scale = 2, 16, 4, 2, 8, 5, 1, 0, 0.3
+    e.d_lse, e.head_lse, e.stride_lse = P, 16, 64
+    for name in ("q", "k", "v", "out", "dout", "dq", "dk", "dv"):
+        h = getattr(e, name)
+        h.d, h.ld, h.head, h.stride = P, 32, 8, 512
+    for k, v in over.items():
+        if "_" in k and k.split("_")[0] in ("q", "k", "v", "out", "dout", "dq", "dk", "dv"):
+            setattr(getattr(e, k.split("_")[0]), k.split("_")[1], v)
+        else:
+            setattr(e, k, v)
+    if grad:
+        return B.lib().brace_window_attention_grad(e, ws, nbytes, None)
+    return B.lib().brace_window_attention_forward(e, None)
+
+
+def test_attention_refuses():
+    common = [dict(batch=-1), dict(tokens=-1), dict(heads=-1), dict(kv_heads=-1), dict(kv_heads=0), dict(kv_heads=3),
+              dict(dim=0), dict(window=0), dict(window=-4), dict(sinks=-1), dict(type=3), dict(type=-1),
+              dict(scale=float("nan")), dict(scale=float("inf")), dict(d_lse=P + 2), dict(d_lengths=P + 1),
+              dict(head_lse=15), dict(stride_lse=8)]
+    common += [{f"{t}_{k}": v} for t in ("q", "k", "v", "out") for k, v in (("d", None), ("d", P + 2), ("ld", -1), ("head", -8), ("stride", -1))]
+    for bad in common + [dict(out_ld=7), dict(out_head=0), dict(out_stride=0)]:
+        assert attention(**bad) == BAD, bad
+    for bad in common + [dict(d_lse=None)] + [{f"{t}_{k}": v} for t in ("dq", "dk", "dv") for k, v in
+                                              (("d", None), ("d", P + 1), ("ld", 7), ("head", 0), ("stride", 0), ("ld", -8))]:
+        assert attention(True, **bad) == BAD, bad
+    assert attention(True, dout_d=None) == attention(True, dout_ld=-1) == BAD
+    for kw in (dict(dim=257), dict(batch=70000), dict(heads=70000, kv_heads=70000)):
+        assert attention(**kw) == attention(True, **kw) == UNSUPPORTED
+    assert attention(True, ws=None) == attention(True, nbytes=16) == attention(True, ws=P + 16) == WORKSPACE
+    for kw in (dict(batch=0), dict(tokens=0), dict(heads=0)):
+        assert attention(**kw) == attention(True, **kw) == B.OK
+    assert B.lib().brace_window_attention_forward(None, None) == B.lib().brace_window_attention_grad(None, P, 1, None) == BAD
+
+
+def test_attention_workspace():
+    f = B.lib().brace_window_attention_workspace_bytes
+    assert f(1, 100, 4, 2, 64, 0) > 0 and f(0, 0, 0, 0, 1, 0) >= 256
+    for bad in [(-1, 1, 1, 1, 1, 0), (1, -1, 1, 1, 1, 0), (1, 1, -1, 1, 1, 0), (1, 1, 3, 2, 1, 0), (1, 1, 1, 0, 1, 0),
+                (1, 1, 1, 1, 0, 0), (1, 1, 1, 1, 1, -1), (1, 1, 1, 1, 257, 0), (70000, 1, 1, 1, 1, 0)]:
+        assert f(*bad) == 0, bad
+    for kw in (dict(b=1), dict(b=3)):
+        sizes = [f(kw["b"], n, 4, 2, 64, 4) for n in (0, 1, 100, 128, 129, 1000, 10000)]
+        assert sizes == sorted(sizes)        # one for many tokens serves fewer
+
+
+def test_attention_binding_refuses():
+    p = B.WindowAttention(4, 8, 16, batch=2, kv_heads=2, device="cpu")
+    q, k = torch.zeros(2, 16, 4, 8), torch.zeros(2, 16, 2, 8)
+    lse = torch.zeros(2, 4, 16)
+    for args in [(q[:1], k, k, q), (q, q, k, q), (q, k, k[:, :5], q), (q, k, k, k), (q.double(),) * 4, (q, k.half(), k, q),
+                 (q, k, k, q.half()), (torch.zeros(2, 17, 4, 8), k, k, q), (q[..., :7], k, k, q), (q[0], k, k, q),
+                 (q.mT.contiguous().mT, k, k, q)]:
+        with pytest.raises(ValueError):
+            p.forward(*args)
+    for kw in [dict(lse=lse.half()), dict(lse=lse[:, :2]), dict(lse=lse.mT.contiguous().mT), dict(lengths=torch.zeros(2)),
+               dict(lengths=torch.zeros(3, dtype=torch.int32)), dict(lengths=torch.zeros(4, dtype=torch.int32)[::2])]:
+        with pytest.raises(ValueError):
+            p.forward(q, k, k, q, **kw)
+    with pytest.raises(ValueError):
+        p.grad(k, q, k, k, q, lse, q, k, k)
+    with pytest.raises(ValueError):      # the host's memory
+        p.forward(q, k, k, q, lse=lse)
+    with pytest.raises(B.BraceError):
+        B.WindowAttention(4, 8, 16, batch=2, kv_heads=2, grad=False, device="cpu").grad(q, q, k, k, q, lse, q, k, k)
