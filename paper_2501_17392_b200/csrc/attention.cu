@@ -5,6 +5,7 @@
 #include <cmath>
 
 #include "attention_rows.cuh"
+#include "attention_tiles.cuh"
 #include "host.cuh"
 
 using namespace brace;
@@ -67,6 +68,61 @@ AttnArgs attn_args(const brace_window_attention* e) {
   return a;
 }
 
+// Whether the tensor cores' kernels serve this tensor: its rows start on 16-byte boundaries, as loads by tensor maps and
+// wide stores ask for, and no dimension is broadcast.
+bool tiles_ok(const brace_heads& x, const brace_window_attention* e, int heads) {
+  auto stride_ok = [](int64_t s, int64_t n) { return n < 2 || (s > 0 && s % 8 == 0 && s < (int64_t)1 << 38); };
+  return aligned(x.d, 16) && stride_ok(x.ld, e->tokens) && stride_ok(x.head, heads) && stride_ok(x.stride, e->batch);
+}
+
+bool tiles_served(const brace_window_attention* e, bool grad) {
+  if (e->type == BRACE_TYPE_F32 || e->dim % 8 || e->dim > 128) return false;
+  if (!tiles_ok(e->q, e, e->heads) || !tiles_ok(e->k, e, e->kv_heads) || !tiles_ok(e->v, e, e->kv_heads)) return false;
+  if (!grad) return tiles_ok(e->out, e, e->heads);
+  return tiles_ok(e->dout, e, e->heads) && tiles_ok(e->dq, e, e->heads) && tiles_ok(e->dk, e, e->kv_heads) && tiles_ok(e->dv, e, e->kv_heads);
+}
+
+// Boxes of 64 dimensions x `rows` tokens, 128-byte swizzle, zeros outside.
+bool encode_map(CUtensorMap* map, const brace_heads& x, const brace_window_attention* e, int heads, int rows) {
+  EncodeFn enc = encode_fn();
+  if (!enc) return false;
+  auto bytes = [](int64_t s, int64_t n) { return (cuuint64_t)(n < 2 ? 16 : s * 2); };   // of one element's dimension: any
+  const cuuint64_t dim[4] = {(cuuint64_t)e->dim, (cuuint64_t)e->tokens, (cuuint64_t)heads, (cuuint64_t)e->batch};
+  const cuuint64_t stride[3] = {bytes(x.ld, e->tokens), bytes(x.head, heads), bytes(x.stride, e->batch)};
+  const cuuint32_t box[4] = {64, (cuuint32_t)rows, 1, 1}, one[4] = {1, 1, 1, 1};
+  return enc(map, e->type == BRACE_TYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, x.d, dim,
+             stride, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Lets a kernel use its shared memory on the current device (once per device and kernel).
+cudaError_t grant_smem(const void* kernel, std::atomic<uint64_t>& granted, int bytes) {
+  int dev = 0;
+  cudaError_t err = cudaGetDevice(&dev);
+  if (err != cudaSuccess) return err;
+  const uint64_t bit = 1ull << (dev & 63);
+  if (granted.load(std::memory_order_relaxed) & bit) return cudaSuccess;
+  err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (err == cudaSuccess) granted.fetch_or(bit, std::memory_order_relaxed);
+  return err;
+}
+
+template <typename T, int D, bool SHARED>
+cudaError_t launch_forward(const AttnMaps& maps, const AttnArgs& a, cudaStream_t st) {
+  static std::atomic<uint64_t> granted{0};
+  auto* kernel = attn_forward_kernel<T, D, SHARED>;
+  const cudaError_t err = grant_smem((const void*)kernel, granted, AttnShape<D>::kSmem);
+  if (err != cudaSuccess) return err;
+  const int rows = SHARED ? 128 : 256;
+  const dim3 grid((unsigned)((a.tokens + rows - 1) / rows), (unsigned)(SHARED ? a.heads / 2 : a.heads), (unsigned)a.batch);
+  return launch(kernel, grid, kAttnThreads, AttnShape<D>::kSmem, 1, st, maps, a);
+}
+
+template <typename F>
+cudaError_t with_half_type(int type, F&& f) {
+  return type == BRACE_TYPE_BF16 ? f(__nv_bfloat16{}) : f(__half{});
+}
+
 dim3 row_grid(const brace_window_attention* e, int heads) {
   return dim3((unsigned)((e->tokens + 3) / 4), (unsigned)heads, (unsigned)e->batch);
 }
@@ -82,6 +138,19 @@ int brace_window_attention_forward(const brace_window_attention* e, brace_stream
   if (!attn_common_ok(e, false) || !heads_ok(e->out, e, e->heads, true)) return BRACE_ERR_INVALID_ARG;
   const AttnArgs a = attn_args(e);
   const cudaStream_t st = (cudaStream_t)stream;
+  if (tiles_served(e, false)) {
+    AttnMaps maps = {};
+    if (!encode_map(&maps.q, e->q, e, e->heads, 128) || !encode_map(&maps.k, e->k, e, e->kv_heads, 128) ||
+        !encode_map(&maps.v, e->v, e, e->kv_heads, 128))
+      return cuda_fail_no_ctx(cudaErrorNotSupported);
+    const bool shared = a.share % 2 == 0;
+    const cudaError_t err = with_half_type(e->type, [&](auto t) {
+      using T = decltype(t);
+      if (e->dim <= 64) return shared ? launch_forward<T, 64, true>(maps, a, st) : launch_forward<T, 64, false>(maps, a, st);
+      return shared ? launch_forward<T, 128, true>(maps, a, st) : launch_forward<T, 128, false>(maps, a, st);
+    });
+    return err == cudaSuccess ? BRACE_OK : cuda_fail_no_ctx(err);
+  }
   const cudaError_t err = with_type(e->type, [&](auto t) {
     return launch(attn_forward_rows_kernel<decltype(t)>, row_grid(e, e->heads), kRowThreads, 0, 1, st, a);
   });
