@@ -657,7 +657,7 @@ typedef struct brace_heads {
  * v), results are rounded once. */
 typedef struct brace_window_attention {
   int32_t batch;           /* sequences, 0..65535                                                  */
-  int32_t tokens;          /* rows of a sequence, >= 0                                             */
+  int32_t tokens;          /* rows of a sequence, 0..2^29 (more: BRACE_ERR_UNSUPPORTED)            */
   int32_t heads, kv_heads; /* heads is a multiple of kv_heads; 0..65535                            */
   int32_t dim;             /* of a head, 1..256 (more: BRACE_ERR_UNSUPPORTED)                      */
   int32_t window, sinks;   /* window >= 1, sinks >= 0                                              */

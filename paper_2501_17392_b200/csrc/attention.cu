@@ -13,17 +13,50 @@ using namespace brace;
 namespace {
 
 bool attn_sizes_ok(int32_t batch, int32_t tokens, int32_t heads) { return batch >= 0 && tokens >= 0 && heads >= 0; }
-bool attn_served(int32_t batch, int32_t heads, int32_t dim) { return batch <= 65535 && heads <= 65535 && dim <= kHeadMost; }
+// positions, and sums of two of them, are 32-bit numbers
+bool attn_served(int32_t batch, int32_t tokens, int32_t heads, int32_t dim) {
+  return batch <= 65535 && tokens <= 1 << 29 && heads <= 65535 && dim <= kHeadMost;
+}
 
-size_t attn_bytes(int32_t batch, int32_t tokens, int32_t heads) {
-  return (size_t)round_up(std::max<int64_t>((int64_t)batch * tokens * heads * 4, 256), 256);
+constexpr int kGradCtas = 148 * 4;   // that the first tokens' tiles are shared out over
+
+// The first tokens' tiles and the most pieces of all of them together.
+struct FirstTiles {
+  int64_t tiles, pieces;   // of a sequence and kv head; of all
+};
+FirstTiles first_tiles(int32_t batch, int32_t tokens, int32_t heads, int32_t kv_heads, int32_t sinks) {
+  FirstTiles f = {};
+  f.tiles = (std::min(sinks, tokens) + (int64_t)127) / 128;
+  const int64_t all = f.tiles * batch * kv_heads;
+  if (all == 0) return f;
+  const int64_t blocks = ((int64_t)tokens + kBlock - 1) / kBlock * (heads / kv_heads);
+  f.pieces = std::min(std::max<int64_t>(kGradCtas, all), all * blocks);
+  return f;
+}
+
+// What the gradient keeps in its workspace: two numbers of every query, the ranges, the pieces' sums.
+struct GradPlan {
+  int64_t padded;
+  size_t off_shift, off_range, off_part, bytes;
+};
+GradPlan grad_plan(int32_t batch, int32_t tokens, int32_t heads, int32_t kv_heads, int32_t dim, int32_t sinks) {
+  GradPlan q;
+  q.padded = round_up(tokens, kBlock);
+  const int64_t numbers = round_up((int64_t)batch * heads * q.padded * 4, 256);
+  q.off_shift = (size_t)numbers;
+  q.off_range = (size_t)(2 * numbers);
+  q.off_part = q.off_range + (size_t)round_up((int64_t)batch * kv_heads * 8, 256);
+  const int64_t pieces = dim % 8 == 0 && dim <= 128 ? first_tiles(batch, tokens, heads, kv_heads, sinks).pieces : 0;
+  q.bytes = q.off_part + (size_t)(pieces * 2 * 128 * (dim <= 64 ? 64 : 128) * 4);
+  if (q.bytes < 256) q.bytes = 256;
+  return q;
 }
 
 int attn_check(const brace_window_attention* e) {
   if (!e || !attn_sizes_ok(e->batch, e->tokens, e->heads) || e->kv_heads < 0 || e->dim < 1) return BRACE_ERR_INVALID_ARG;
   if (!float_type(e->type) || e->window < 1 || e->sinks < 0 || !std::isfinite(e->scale)) return BRACE_ERR_INVALID_ARG;
   if (e->heads > 0 && (e->kv_heads < 1 || e->heads % e->kv_heads)) return BRACE_ERR_INVALID_ARG;
-  if (!attn_served(e->batch, e->heads, e->dim)) return BRACE_ERR_UNSUPPORTED;
+  if (!attn_served(e->batch, e->tokens, e->heads, e->dim)) return BRACE_ERR_UNSUPPORTED;
   return BRACE_OK;
 }
 
@@ -77,6 +110,7 @@ bool tiles_ok(const brace_heads& x, const brace_window_attention* e, int heads) 
 
 bool tiles_served(const brace_window_attention* e, bool grad) {
   if (e->type == BRACE_TYPE_F32 || e->dim % 8 || e->dim > 128) return false;
+  if ((e->tokens / kBlock + 1) * (int64_t)(e->heads / e->kv_heads) >= 1 << 30) return false;   // blocks of a tile of keys
   if (!tiles_ok(e->q, e, e->heads) || !tiles_ok(e->k, e, e->kv_heads) || !tiles_ok(e->v, e, e->kv_heads)) return false;
   if (!grad) return tiles_ok(e->out, e, e->heads);
   return tiles_ok(e->dout, e, e->heads) && tiles_ok(e->dq, e, e->heads) && tiles_ok(e->dk, e, e->kv_heads) && tiles_ok(e->dv, e, e->kv_heads);
@@ -116,6 +150,42 @@ cudaError_t launch_forward(const AttnMaps& maps, const AttnArgs& a, cudaStream_t
   const int rows = SHARED ? 128 : 256;
   const dim3 grid((unsigned)((a.tokens + rows - 1) / rows), (unsigned)(SHARED ? a.heads / 2 : a.heads), (unsigned)a.batch);
   return launch(kernel, grid, kAttnThreads, AttnShape<D>::kSmem, 1, st, maps, a);
+}
+
+template <typename T, int D, bool DKV>
+cudaError_t launch_grad(const AttnMaps& maps, const AttnArgs& a, cudaStream_t st) {
+  static std::atomic<uint64_t> granted{0};
+  auto* kernel = attn_grad_kernel<T, D, DKV>;
+  constexpr int smem = AttnGradShape<D, DKV>::kSmem;
+  const cudaError_t err = grant_smem((const void*)kernel, granted, smem);
+  if (err != cudaSuccess) return err;
+  const int tiles = (int)(((int64_t)a.tokens + 127) / 128);
+  const dim3 grid((unsigned)(DKV ? a.first_tiles * a.pieces + tiles - a.first_tiles : tiles), (unsigned)(DKV ? a.kv_heads : a.heads),
+                  (unsigned)a.batch);
+  return launch(kernel, grid, kAttnThreads, smem, 1, st, maps, a);
+}
+
+// The gradient on the tensor cores.
+template <typename T, int D>
+cudaError_t run_grad(const brace_window_attention* e, AttnArgs a, cudaStream_t st) {
+  AttnMaps queries = {}, keys = {};   // with the rows' boxes of 128 and the blocks' of 64: dq, and dk and dv
+  if (!encode_map(&queries.q, e->q, e, e->heads, 128) || !encode_map(&queries.dout, e->dout, e, e->heads, 128) ||
+      !encode_map(&queries.k, e->k, e, e->kv_heads, kBlock) || !encode_map(&queries.v, e->v, e, e->kv_heads, kBlock) ||
+      !encode_map(&keys.k, e->k, e, e->kv_heads, 128) || !encode_map(&keys.v, e->v, e, e->kv_heads, 128) ||
+      !encode_map(&keys.q, e->q, e, e->heads, kBlock) || !encode_map(&keys.dout, e->dout, e, e->heads, kBlock))
+    return cudaErrorNotSupported;
+  cudaError_t err = cudaSuccess;
+  if (std::is_same<T, __half>::value)
+    err = cudaMemsetAsync(a.range, 0, (size_t)a.batch * a.kv_heads * 8, st);
+  else
+    a.range = nullptr;
+  if (err == cudaSuccess)
+    err = launch(attn_prepare_kernel<T>, dim3((unsigned)(a.padded / kPrepRows), (unsigned)a.heads, (unsigned)a.batch), 256, 0, 1, st, a);
+  if (err == cudaSuccess) err = launch_grad<T, D, true>(keys, a, st);
+  if (err == cudaSuccess) err = launch_grad<T, D, false>(queries, a, st);
+  if (err == cudaSuccess && a.first_tiles)
+    err = launch(attn_join_kernel<T, D>, dim3((unsigned)(a.first_tiles * 32), (unsigned)a.kv_heads, (unsigned)a.batch), 128, 0, 1, st, a);
+  return err;
 }
 
 template <typename F>
@@ -161,8 +231,8 @@ size_t brace_window_attention_workspace_bytes(int32_t batch, int32_t tokens, int
                                               int32_t sinks) {
   if (!attn_sizes_ok(batch, tokens, heads) || kv_heads < 0 || dim < 1 || sinks < 0) return 0;
   if (heads > 0 && (kv_heads < 1 || heads % kv_heads)) return 0;
-  if (!attn_served(batch, heads, dim)) return 0;
-  return attn_bytes(batch, tokens, heads);
+  if (!attn_served(batch, tokens, heads, dim)) return 0;
+  return grad_plan(batch, tokens, heads, kv_heads, dim, sinks).bytes;
 }
 
 int brace_window_attention_grad(const brace_window_attention* e, void* d_workspace, size_t workspace_bytes,
@@ -180,8 +250,30 @@ int brace_window_attention_grad(const brace_window_attention* e, void* d_workspa
   a.dq = head_ref(e->dq);
   a.dk = head_ref(e->dk);
   a.dv = head_ref(e->dv);
-  a.delta = (float*)d_workspace;
+  const GradPlan q = grad_plan(e->batch, e->tokens, e->heads, e->kv_heads, e->dim, e->sinks);
+  char* ws = (char*)d_workspace;
+  a.delta = (float*)ws;
+  a.shift = (float*)(ws + q.off_shift);
+  a.range = (uint32_t*)(ws + q.off_range);
+  a.part = (float*)(ws + q.off_part);
+  a.padded = q.padded;
   const cudaStream_t st = (cudaStream_t)stream;
+  if (tiles_served(e, true)) {
+    // A tile of first tokens is shared out over as many CTAs as make a CTA's work that of a tile behind them, or as give
+    // every SM some.
+    const FirstTiles f = first_tiles(e->batch, e->tokens, e->heads, e->kv_heads, e->sinks);
+    a.first_tiles = (int)f.tiles;
+    if (f.tiles) {
+      const int64_t window = std::min<int64_t>(e->tokens, (int64_t)a.window + 127);
+      const int64_t even = ((int64_t)e->tokens + window - 1) / window, most = f.pieces / (f.tiles * e->batch * e->kv_heads);
+      a.pieces = (int)std::max<int64_t>(1, std::min(even, most));
+    }
+    const cudaError_t err = with_half_type(e->type, [&](auto t) {
+      using T = decltype(t);
+      return e->dim <= 64 ? run_grad<T, 64>(e, a, st) : run_grad<T, 128>(e, a, st);
+    });
+    return err == cudaSuccess ? BRACE_OK : cuda_fail_no_ctx(err);
+  }
   const cudaError_t err = with_type(e->type, [&](auto t) {
     using T = decltype(t);
     cudaError_t r = launch(attn_delta_kernel<T>, row_grid(e, e->heads), kRowThreads, 0, 1, st, a);

@@ -24,8 +24,13 @@ struct HeadRef {                           // element (b, t, h, d) lies at b * s
 
 struct AttnArgs {
   HeadRef q, k, v, out, dout, dq, dk, dv;
-  float *lse, *delta;                      // lse: (b, h, t) at b * stride_lse + h * head_lse + t; delta: [b][h][t]
+  float* lse;                              // (b, h, t) at b * stride_lse + h * head_lse + t
   int64_t stride_lse, head_lse;
+  float *delta, *shift;                    // [b][h][padded]: delta_i, and -log2(e) lse_i
+  uint32_t* range;                         // [b][kv head][2]: bits of the largest |do| and |v|
+  float* part;                             // [b][kv head][tile of first tokens][piece][dv, dk][128][D]
+  int64_t padded;                          // tokens, rounded up to 64
+  int first_tiles, pieces;
   const int32_t* lengths;
   int batch, tokens, heads, kv_heads, share, dim, window, sinks;
   float scale;
@@ -42,7 +47,7 @@ __device__ __forceinline__ float& attn_lse(const AttnArgs& p, int b, int h, int 
   return p.lse[b * p.stride_lse + h * p.head_lse + t];
 }
 __device__ __forceinline__ int64_t attn_delta(const AttnArgs& p, int b, int h, int t) {
-  return ((int64_t)b * p.heads + h) * p.tokens + t;
+  return ((int64_t)b * p.heads + h) * p.padded + t;
 }
 
 template <typename T>
@@ -140,7 +145,7 @@ __device__ __forceinline__ void dq_row(const AttnArgs& p, int b, int h, int i, i
 }
 
 template <typename T>
-__device__ __forceinline__ void dkv_row(const AttnArgs& p, int b, int g, int j, int n) {
+__device__ __forceinline__ void dkv_row(const AttnArgs& p, int b, int g, int j, int n, bool put_k = true, bool put_v = true) {
   const int lane = threadIdx.x & 31;
   float dk[kHeadLane] = {}, dv[kHeadLane] = {};
   const int end = j >= n ? j : j < p.sinks || p.window > n - j ? n : j + p.window;
@@ -158,8 +163,8 @@ __device__ __forceinline__ void dkv_row(const AttnArgs& p, int b, int g, int j, 
         add_row(dk, __shfl_sync(0xffffffffu, ds, t), head_row<const T>(p.q, b, i0 + t, h), p.dim);
       }
     }
-  put_row(head_row<T>(p.dk, b, j, g), dk, p.scale, p.dim);
-  put_row(head_row<T>(p.dv, b, j, g), dv, 1.f, p.dim);
+  if (put_k) put_row(head_row<T>(p.dk, b, j, g), dk, p.scale, p.dim);
+  if (put_v) put_row(head_row<T>(p.dv, b, j, g), dv, 1.f, p.dim);
 }
 
 constexpr int kRowThreads = 128;

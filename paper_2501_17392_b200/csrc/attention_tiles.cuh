@@ -8,6 +8,14 @@
 // the group's result in tensor memory.  While one group's threads are at their exponentials, the tensor cores work for the
 // other.  The result is scaled again only when a maximum has grown by more than 2^8 (the sum and P have room for that).
 //
+// Backward.  Two launches of one kernel, so that every result is summed in one order: the rows are queries and the columns
+// blocks of 64 keys (dq), or the rows are keys and the columns blocks of 64 queries of all heads that share them (dk, dv).
+// Per block: scores and dp = do v into tensor memory, a thread makes p and ds of a row's 64 columns and writes them back
+// over the two, rounded to the inputs' type, and the products with k (with do and q) add to the results in tensor memory.
+// Two groups of threads take the blocks by turns.  Tiles of first tokens are seen by all queries: their blocks are shared
+// out over several CTAs, whose float32 sums a last launch adds up.  In float16 ds is held times a power of two that the
+// largest |do| and |v| allow without overflow, since ds is often below what float16 holds at full precision.
+//
 // A product with P = 0 where a key is hidden gives NaN if that key's value is not finite.  A row whose result is not
 // finite is therefore computed again, key by key, from what it sees.
 #pragma once
@@ -30,7 +38,7 @@ struct AttnShape {
 };
 
 struct AttnMaps {
-  CUtensorMap q, k, v, dout;               // (dimension, token, head, sequence)
+  CUtensorMap q, k, v, dout;               // (dimension, token, head, sequence); boxes of 64 x 128, or of 64 x 64
 };
 
 // Both operands bfloat16 (format 1) or both float16 (format 0).
@@ -343,6 +351,405 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_forward_kernel(const __g
     tc_fence_after();
     tmem_free<1>(tmem, 512);
   }
+}
+
+// ---- backward
+
+constexpr int kBlock = 64;                 // columns of a block
+
+template <int D, bool DKV>
+struct AttnGradShape {
+  static constexpr int kTile = 128 * D * 2, kHalf = kBlock * D * 2;
+  static constexpr int kStage = 2 * kHalf + (DKV ? 1024 : 0);        // the block's two operands, and its queries' numbers
+  static constexpr int kStages = D == 64 ? 6 : 4;
+  static constexpr int kSmem = 1024 + 2 * kTile + kStages * kStage + 256;
+};
+
+constexpr int kPrepRows = 64;              // queries of a CTA that prepares the backward pass
+
+// delta, -log2(e) lse, and in float16 the ranges of do and v; 16 lanes a row.  grid: (padded / kPrepRows, heads, sequences)
+template <typename T>
+__global__ void __launch_bounds__(256) attn_prepare_kernel(const AttnArgs p) {
+  grid_trigger();
+  grid_wait();
+  const int h = blockIdx.y, b = blockIdx.z, n = attn_length(p, b), part = threadIdx.x & 15;
+  float most_do = 0.f, most_v = 0.f;
+  for (int i = blockIdx.x * kPrepRows + (threadIdx.x >> 4); i < (int)(blockIdx.x + 1) * kPrepRows; i += 16) {
+    float s = 0.f;
+    const bool here = i < n && 8 * part < p.dim;
+    if (here) {
+      Pack<T, 8> o, d;
+      o.load(head_row<const T>(p.out, b, i, h) + 8 * part);
+      d.load(head_row<const T>(p.dout, b, i, h) + 8 * part);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float x = to_f32(d.t[e]);
+        s = fmaf(to_f32(o.t[e]), x, s);
+        if (isfinite(x)) most_do = fmaxf(most_do, fabsf(x));
+      }
+      if (p.range && h % p.share == 0) {
+        Pack<T, 8> v;
+        v.load(head_row<const T>(p.v, b, i, h / p.share) + 8 * part);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float x = to_f32(v.t[e]);
+          if (isfinite(x)) most_v = fmaxf(most_v, fabsf(x));
+        }
+      }
+    }
+    for (int o = 8; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    if (part == 0) {
+      p.delta[attn_delta(p, b, h, i)] = i < n ? s : 0.f;
+      p.shift[attn_delta(p, b, h, i)] = i < n ? -kLog2e * attn_lse(p, b, h, i) : 0.f;
+    }
+  }
+  if (!p.range) return;
+  for (int o = 16; o; o >>= 1) {
+    most_do = fmaxf(most_do, __shfl_xor_sync(0xffffffffu, most_do, o));
+    most_v = fmaxf(most_v, __shfl_xor_sync(0xffffffffu, most_v, o));
+  }
+  if ((threadIdx.x & 31) == 0) {           // of numbers that are not negative the bits are in the same order
+    uint32_t* to = p.range + ((int64_t)b * p.kv_heads + h / p.share) * 2;
+    if (most_do > 0.f) atomicMax(to, __float_as_uint(most_do));
+    if (most_v > 0.f) atomicMax(to + 1, __float_as_uint(most_v));
+  }
+}
+
+// The power of two that ds is held times: |dp - delta| <= 2 D max|do| max|v| then stays below 2^15.
+__device__ __forceinline__ float attn_grad_scale(const AttnArgs& p, int b, int g) {
+  if (!p.range) return 1.f;
+  const uint32_t* r = p.range + ((int64_t)b * p.kv_heads + g) * 2;
+  const float bound = p.dim * __uint_as_float(r[0]) * __uint_as_float(r[1]);
+  return bound > 0.f ? ldexpf(1.f, 13 - ilogbf(bound)) : 1.f;
+}
+
+// What a CTA of the backward pass computes.
+struct GradWork {
+  int row0, begin, end;                    // first row; blocks
+  int per_head;                            // blocks of queries of a head (DKV)
+  int tile, piece;                         // of first tokens (DKV), or -1
+};
+
+// grid: DKV (pieces of the first tokens' tiles, then tiles; kv heads; sequences), else (tiles of queries, heads, sequences)
+template <typename T, int D, bool DKV>
+__global__ void __launch_bounds__(kAttnThreads, 1) attn_grad_kernel(const __grid_constant__ AttnMaps maps, const AttnArgs p) {
+  using Shape = AttnGradShape<D, DKV>;
+  constexpr int STAGES = Shape::kStages;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t base = (smem_addr(smem_raw) + 1023u) & ~1023u;
+  const uint32_t ring = base + 2 * Shape::kTile, bars = ring + STAGES * Shape::kStage;
+  const uint32_t full = bars, empty = full + 8 * STAGES, a_full = empty + 8 * STAGES;
+  const uint32_t s_full = a_full + 8, p_full = s_full + 16, o_full = p_full + 16, tail = o_full + 8;
+  volatile int* dead = (volatile int*)(smem_raw + (tail - smem_addr(smem_raw)));
+  uint32_t* tmem_slot = (uint32_t*)(smem_raw + (tail + 8 - smem_addr(smem_raw)));
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  if (threadIdx.x == 0) {
+    *dead = 0;
+    for (int s = 0; s < STAGES; ++s) {
+      mbar_init(full + 8 * s, 1);
+      mbar_init(empty + 8 * s, 1);
+    }
+    mbar_init(a_full, 1);
+    mbar_init(o_full, 1);
+    for (int r = 0; r < 2; ++r) {
+      mbar_init(s_full + 8 * r, 1);
+      mbar_init(p_full + 8 * r, 4);
+    }
+    mbar_init_visible();
+    tma_prefetch(&maps.q);
+    tma_prefetch(&maps.k);
+    tma_prefetch(&maps.v);
+    tma_prefetch(&maps.dout);
+  }
+  if (warp == 9) tmem_alloc<1>(smem_addr(tmem_slot), 512);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  grid_trigger();
+  grid_wait();
+  fence_async_global();
+
+  const int b = blockIdx.z, n = attn_length(p, b), g = DKV ? (int)blockIdx.y : (int)blockIdx.y / p.share;
+  GradWork w;
+  w.tile = w.piece = -1;
+  w.begin = w.end = 0;
+  w.per_head = 1;
+  if (DKV) {
+    const int x = blockIdx.x, first = p.first_tiles * p.pieces;
+    if (x < first) {
+      w.tile = x / p.pieces;
+      w.piece = x % p.pieces;
+    }
+    w.row0 = 128 * (x < first ? w.tile : p.first_tiles + x - first);
+  } else {
+    w.row0 = 128 * (int)(gridDim.x - 1 - blockIdx.x);       // the last queries first: they have the longest windows
+  }
+  const KeyBlocks keys(p, w.row0, min(n, w.row0 + 128), kBlock);
+  if (w.row0 < n) {
+    if (DKV) {
+      // the tile's queries: from its first key to the end of its last one's window, or all from there on
+      const int stop = w.row0 < p.sinks || p.window + 127 > n - w.row0 ? n : w.row0 + 127 + p.window;
+      w.per_head = (stop - w.row0 + kBlock - 1) / kBlock;
+      const int64_t all = (int64_t)w.per_head * p.share;
+      w.begin = w.piece < 0 ? 0 : (int)(all * w.piece / p.pieces);
+      w.end = w.piece < 0 ? (int)all : (int)(all * (w.piece + 1) / p.pieces);
+    } else {
+      w.end = keys.count;
+    }
+  }
+  const int count = w.end - w.begin;
+  auto block_head = [&](int k) { return DKV ? g * p.share + (w.begin + k) / w.per_head : (int)blockIdx.y; };
+  auto block_first = [&](int k) { return DKV ? w.row0 + (w.begin + k) % w.per_head * kBlock : keys.key(k, kBlock); };
+
+  if (warp == 8) {                         // loads
+    const bool lead = elect_one();
+    if (lead && count) {
+      mbar_expect_tx(a_full, 2 * Shape::kTile);
+      load_rows<D, 128>(base, DKV ? &maps.k : &maps.q, w.row0, DKV ? g : (int)blockIdx.y, b, a_full);
+      load_rows<D, 128>(base + Shape::kTile, DKV ? &maps.v : &maps.dout, w.row0, DKV ? g : (int)blockIdx.y, b, a_full);
+    }
+    __syncwarp();
+    int s = 0, issued = 0;
+    uint32_t ph = 0;
+    bool ok = true;
+    for (int k = 0; ok && k < count; ++k) {
+      if (!mbar_wait(empty + 8 * s, ph ^ 1u, dead)) {
+        ok = false;
+        break;
+      }
+      if (lead) {
+        const uint32_t at = ring + s * Shape::kStage, bar = full + 8 * s;
+        const int t = block_first(k), h = block_head(k);
+        mbar_expect_tx(bar, 2 * Shape::kHalf + (DKV ? 2 * kBlock * 4 : 0));
+        if (DKV) {     // the boxes of q and do have 64 rows here, those of k and v in the other pass
+          load_rows<D, kBlock>(at, &maps.q, t, h, b, bar);
+          load_rows<D, kBlock>(at + Shape::kHalf, &maps.dout, t, h, b, bar);
+          bulk_load(at + 2 * Shape::kHalf, p.shift + attn_delta(p, b, h, t), kBlock * 4, bar);
+          bulk_load(at + 2 * Shape::kHalf + kBlock * 4, p.delta + attn_delta(p, b, h, t), kBlock * 4, bar);
+        } else {
+          load_rows<D, kBlock>(at, &maps.k, t, g, b, bar);
+          load_rows<D, kBlock>(at + Shape::kHalf, &maps.v, t, g, b, bar);
+        }
+      }
+      __syncwarp();
+      ++issued;
+      if (++s == STAGES) {
+        s = 0;
+        ph ^= 1u;
+      }
+    }
+    if (!ok)     // gave up: let the copies in flight land before the memory goes
+      for (int i = issued > STAGES ? issued - STAGES : 0; i < issued; ++i)
+        mbar_wait(full + 8 * (i % STAGES), (uint32_t)(i / STAGES) & 1u, dead);
+  } else if (warp == 9) {                  // products
+    const bool lead = elect_one();
+    constexpr uint32_t kScores = attn_idesc<T>(kBlock, false), kSums = attn_idesc<T>(D, true);
+    const uint64_t a_desc = operand_desc(base, kBlock * 128), ring_desc = operand_desc(ring, kBlock * 128);
+    bool ok = count == 0 || mbar_wait(a_full, 0, dead);
+    auto scores = [&](int k) {
+      const int s = k % STAGES;
+      if (!mbar_wait(full + 8 * s, (uint32_t)(k / STAGES) & 1u, dead)) return false;
+      tc_fence_after();
+      if (lead) {
+        const uint64_t db = ring_desc + (uint64_t)(s * Shape::kStage >> 4);
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+          for (int i = 0; i < D / 16; ++i)
+            mma_f16<1>(tmem + 128 * (k & 1) + 64 * x,
+                       a_desc + (uint64_t)((x * Shape::kTile + (i / 4) * 16384 + (i % 4) * 32) >> 4),
+                       db + (uint64_t)((x * Shape::kHalf + (i / 4) * 8192 + (i % 4) * 32) >> 4), kScores, i > 0);
+        mma_commit<1>(s_full + 8 * (k & 1));
+      }
+      __syncwarp();
+      return true;
+    };
+    for (int k = 0; ok && k < 2 && k < count; ++k) ok = scores(k);
+    for (int k = 0; ok && k < count; ++k) {
+      const int s = k % STAGES;
+      if (!mbar_wait(p_full + 8 * (k & 1), (uint32_t)(k >> 1) & 1u, dead)) break;
+      tc_fence_after();
+      if (lead) {
+        const uint64_t db = ring_desc + (uint64_t)(s * Shape::kStage >> 4);
+        const uint32_t a = tmem + 128 * (k & 1);
+#pragma unroll
+        for (int i = 0; i < kBlock / 16; ++i) {
+          if (DKV) {
+            mma_f16_ts(tmem + 256, a + 8 * i, db + (uint64_t)((Shape::kHalf + 2048 * i) >> 4), kSums, k > 0 || i > 0);
+            mma_f16_ts(tmem + 256 + D, a + 64 + 8 * i, db + (uint64_t)(2048 * i >> 4), kSums, k > 0 || i > 0);
+          } else {
+            mma_f16_ts(tmem + 256, a + 64 + 8 * i, db + (uint64_t)(2048 * i >> 4), kSums, k > 0 || i > 0);
+          }
+        }
+        mma_commit<1>(empty + 8 * s);
+      }
+      __syncwarp();
+      if (k + 2 < count) ok = scores(k + 2);
+    }
+    if (lead) mma_commit<1>(o_full);
+    __syncwarp();
+  } else {                                 // a row a thread; the groups take the blocks by turns
+    const int r = warp >> 2, row = (warp & 3) * 32 + lane, at = w.row0 + row;
+    const uint32_t mine = tmem + ((uint32_t)((warp & 3) * 32) << 16), cells = mine + 128 * r;
+    const float c = p.scale * kLog2e, hold = count ? attn_grad_scale(p, b, g) : 1.f;
+    float shift = 0.f, delta = 0.f;
+    if (!DKV && at < n) {
+      shift = p.shift[attn_delta(p, b, blockIdx.y, at)];
+      delta = p.delta[attn_delta(p, b, blockIdx.y, at)];
+    }
+    uint32_t phase = 0;
+    bool ok = true;
+    for (int k = r; k < count; k += 2) {
+      const int s = k % STAGES;
+      // a block's numbers were copied by the asynchronous proxy: their own barrier makes them visible
+      if ((DKV && !mbar_wait(full + 8 * s, (uint32_t)(k / STAGES) & 1u, dead)) || !mbar_wait(s_full + 8 * r, phase, dead)) {
+        ok = false;
+        break;
+      }
+      phase ^= 1u;
+      tc_fence_after();
+      float x[kBlock], y[kBlock];
+      tmem_fetch64(cells, x);
+      tmem_fetch64(cells + 64, y);
+      tmem_loaded();
+      tmem_use(x);
+      tmem_use(y);
+      const float4* numbers = (const float4*)(smem_raw + (ring + s * Shape::kStage + 2 * Shape::kHalf - smem_addr(smem_raw)));
+#pragma unroll
+      for (int e = 0; e < kBlock; e += 4) {
+        float4 sh, de;
+        if (DKV) {
+          sh = numbers[e / 4];
+          de = numbers[kBlock / 4 + e / 4];
+        } else {
+          sh = make_float4(shift, shift, shift, shift);
+          de = make_float4(delta, delta, delta, delta);
+        }
+        const float shifts[4] = {sh.x, sh.y, sh.z, sh.w}, deltas[4] = {de.x, de.y, de.z, de.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          x[e + i] = exp2_fast(fmaf(x[e + i], c, shifts[i]));
+          y[e + i] = x[e + i] * (y[e + i] - deltas[i]);
+          if (std::is_same<T, __half>::value) y[e + i] *= hold;
+        }
+      }
+      const int t = block_first(k);
+      if (DKV) {
+        // query t + e: not before key `at`, before the end, in the key's window or the key one of the first tokens
+        if (t < w.row0 + 127 || t + kBlock > n || (t + kBlock > w.row0 + p.window && w.row0 + 127 >= p.sinks)) {
+          const int from = at - t, to = at < p.sinks || p.window > n - at ? n - t : at + p.window - t;
+#pragma unroll
+          for (int e = 0; e < kBlock; ++e) {
+            x[e] = e >= from && e < to ? x[e] : 0.f;
+            y[e] = e >= from && e < to ? y[e] : 0.f;
+          }
+        }
+      } else if (k < keys.nfirst) {
+        const int here = keys.first - t;
+        if (here < kBlock)
+#pragma unroll
+          for (int e = 0; e < kBlock; ++e) y[e] = e < here ? y[e] : 0.f;
+      } else if (t + kBlock - 1 > w.row0 || t <= w.row0 + 127 - p.window) {
+        const int last = at - t, early = at - p.window - t, first = p.sinks - t;
+#pragma unroll
+        for (int e = 0; e < kBlock; ++e) y[e] = e <= last && (e > early || e < first) ? y[e] : 0.f;
+      }
+      uint32_t word[kBlock / 2];
+      if (DKV) {
+#pragma unroll
+        for (int e = 0; e < kBlock; e += 2) word[e / 2] = pack2<T>(x[e], x[e + 1]);
+        tmem_store32(cells, word);
+      }
+#pragma unroll
+      for (int e = 0; e < kBlock; e += 2) word[e / 2] = pack2<T>(y[e], y[e + 1]);
+      tmem_store32(cells + 64, word);
+      tmem_stored();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(p_full + 8 * r);
+    }
+    if (ok && count) ok = mbar_wait(o_full, 0, dead);
+    tc_fence_after();
+    // dq: the first group writes; dv and dk: a group each
+    const bool exists = at < p.tokens, real = at < n;
+    if (DKV || r == 0) {
+      T* to = head_row<T>(DKV ? (r ? p.dk : p.dv) : p.dq, b, exists ? at : 0, DKV ? g : (int)blockIdx.y);
+      const float factor = !ok ? NAN : DKV && r == 0 ? 1.f : p.scale / hold;   // a wait that ran out shows in the result
+      float* part = nullptr;
+      if (DKV && w.piece >= 0)
+        part = p.part + (((((int64_t)b * p.kv_heads + g) * p.first_tiles + w.tile) * p.pieces + w.piece) * 2 + r) * 128 * D + row * D;
+      bool bad = false;
+      if (count) {
+#pragma unroll
+        for (int col = 0; col < D; col += 32) {
+          float o[32];
+          tmem_fetch32(mine + 256 + (DKV ? D * r : 0) + col, o);
+          tmem_loaded();
+          tmem_use(o);
+          if (DKV && part) {
+#pragma unroll
+            for (int e = 0; e < 32; e += 4)
+              *reinterpret_cast<float4*>(part + col + e) = make_float4(o[e] * factor, o[e + 1] * factor, o[e + 2] * factor, o[e + 3] * factor);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) bad |= !isfinite(o[e]) && col + e < p.dim;
+            if (real) put_columns(to, o, factor, col, p.dim);
+          }
+        }
+      } else if (DKV && part) {
+        for (int col = 0; col < D; col += 4) *reinterpret_cast<float4*>(part + col) = make_float4(0.f, 0.f, 0.f, 0.f);
+      }
+      if (exists && !real && !(DKV && part)) put_zeros(to, p.dim);
+      __syncwarp();   // what follows may write the same rows
+      unsigned again = __ballot_sync(0xffffffffu, bad && real && ok);
+      for (; again; again &= again - 1) {
+        const int i = w.row0 + (warp & 3) * 32 + __ffs(again) - 1;
+        if (DKV)
+          dkv_row<T>(p, b, g, i, n, r == 1, r == 0);
+        else
+          dq_row<T>(p, b, blockIdx.y, i, n);
+      }
+    }
+  }
+  __syncthreads();
+  if (*dead)     // a wait ran out: products may still be under way
+    for (int i = 0; i < 200; ++i) __nanosleep(1000);
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 9) {
+    tc_fence_after();
+    tmem_free<1>(tmem, 512);
+  }
+}
+
+// dv and dk of the first tokens' tiles from their pieces: a warp a row.  grid: (tiles * 32, kv heads, sequences)
+template <typename T, int D>
+__global__ void __launch_bounds__(128) attn_join_kernel(const AttnArgs p) {
+  grid_trigger();
+  grid_wait();
+  const int j = blockIdx.x * 4 + (threadIdx.x >> 5), g = blockIdx.y, b = blockIdx.z, lane = threadIdx.x & 31, n = attn_length(p, b);
+  if (j >= p.tokens) return;
+  bool bad = false;
+#pragma unroll
+  for (int r = 0; r < 2; ++r) {
+    T* to = head_row<T>(r ? p.dk : p.dv, b, j, g);
+    const float* from = p.part + ((((int64_t)b * p.kv_heads + g) * p.first_tiles + j / 128) * p.pieces * 2 + r) * 128 * D + j % 128 * D;
+#pragma unroll
+    for (int col = 0; col < D; col += 32) {
+      const int d = col + lane;
+      float sum = 0.f;
+      if (j < n)
+        for (int k = 0; k < p.pieces; ++k) sum += from[(int64_t)k * 2 * 128 * D + d];
+      if (d < p.dim) {
+        bad |= !isfinite(sum);
+        to[d] = from_f32<T>(sum);
+      }
+    }
+  }
+  __syncwarp();
+  if (__any_sync(0xffffffffu, bad)) dkv_row<T>(p, b, g, j, n);
 }
 
 }  // namespace brace
