@@ -17,7 +17,8 @@ _HEADERS = {
     "brace.cu": ("brace_kernels.cuh",),
     "operators.cu": ("elements.cuh", "embedding_kernels.cuh", "host.cuh", "ortho_kernels.cuh", "sm100.cuh"),
     "attention.cu": ("attention_rows.cuh", "attention_tiles.cuh", "elements.cuh", "host.cuh", "sm100.cuh"),
-    "layers.cu": ("clip_kernels.cuh", "elements.cuh", "host.cuh", "norm_kernels.cuh", "sm100.cuh"),
+    "clip.cu": ("clip_kernels.cuh", "elements.cuh", "host.cuh", "sm100.cuh"),
+    "norm.cu": ("elements.cuh", "host.cuh", "norm_kernels.cuh", "sm100.cuh"),
 }
 SOURCES = [os.path.join(PKG_DIR, "csrc", f) for f in _HEADERS]
 

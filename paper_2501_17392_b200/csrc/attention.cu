@@ -129,18 +129,6 @@ bool encode_map(CUtensorMap* map, const brace_heads& x, const brace_window_atten
              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Lets a kernel use its shared memory on the current device (once per device and kernel).
-cudaError_t grant_smem(const void* kernel, std::atomic<uint64_t>& granted, int bytes) {
-  int dev = 0;
-  cudaError_t err = cudaGetDevice(&dev);
-  if (err != cudaSuccess) return err;
-  const uint64_t bit = 1ull << (dev & 63);
-  if (granted.load(std::memory_order_relaxed) & bit) return cudaSuccess;
-  err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-  if (err == cudaSuccess) granted.fetch_or(bit, std::memory_order_relaxed);
-  return err;
-}
-
 template <typename T, int D, bool SHARED>
 cudaError_t launch_forward(const AttnMaps& maps, const AttnArgs& a, cudaStream_t st) {
   static std::atomic<uint64_t> granted{0};

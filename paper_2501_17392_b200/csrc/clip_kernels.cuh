@@ -1,11 +1,17 @@
 // Every client's gradient norm over many tensors, and the gradients clipped by it.
 //
 // norm_c = sqrt(sum over the client's tensors of sum x^2), f_c = min(1, max_norm / (norm_c + eps)), out = f_c x.
-// Bound by memory.  A call is a chain of launches; each clips some clients (whose values the launch before it has just
-// read, so that they come from L2) and sums the squares of the next ones.  A client's elements are shared out evenly over
-// its CTAs, each of which leaves one sum; who clips adds them up, in one order.  Squares are summed in float32 over the 8
-// or 16 values that a thread has at a time, and by this in float64; where a float32 sum leaves its comfortable range
-// (overflow, squares lost to underflow) those values are squared in float64.
+// Bound by memory: every value is read for its square, and read again once the norm is known.  A launch sums (a client's
+// elements shared out evenly over CTAs, each of which leaves one sum), a second one clips, the other way round, so that it
+// begins with what is still in L2.
+// 50 clients of 11.7 M float32 values (2.3 GB): 330 us to sum (7.1 TB/s) and 1113 in all (6.3 TB/s on what is read twice
+// and written once; a copy moves 6.6).  Tried and not kept: chains of launches that clip the clients which the launch before
+// summed, from L2 (1117 us: 4 to 5 us a launch are lost, and clients of 47 MB do not stay there); one cooperative launch
+// that holds 224 KB an SM in shared memory between its sum and its clipping (1496 us from registers, 1668 by bulk copies:
+// all CTAs wait for one another once a client).
+// Squares are summed in float32 over at most 16 values that a thread has at a time, and beyond that in float64, in one
+// order; where a float32 sum leaves its comfortable range (overflow, squares lost to underflow) those values are squared
+// in float64.
 #pragma once
 
 #include "elements.cuh"
@@ -13,7 +19,7 @@
 
 namespace brace {
 
-constexpr int kClipThreads = 256;
+constexpr int kClipThreads = 256, kClipResident = 4;   // of a CTA that only sums or only clips; CTAs of an SM
 constexpr int kClipUnit = 2048;      // elements: what a client's elements are shared out by
 constexpr int kClipNarrow = 1024;    // rows of a strided tensor shorter than this are walked element by element
 
@@ -23,14 +29,13 @@ struct ClipTensor {
   int64_t rows, cols;                // rows is 1 where both sides are one run of elements
   int64_t ld_in, ld_out, stride_in, stride_out;
   int64_t unit0, row_units;          // first unit of this tensor; units of a row (0: rows are walked together)
-  int32_t in_type, out_type;
 };
 
 struct ClipArgs {
   double* part;                      // [client][parts]
   float* norms;
   int64_t units, parts, part0;       // of this list; parts of all lists, and the first one of this list
-  int32_t clip_first, clip_count, sum_first, count;
+  int32_t count;                     // tensors of this list
   float max_norm, eps;
   int32_t zero_bad;                  // a client whose norm is not finite gets zeros
 };
@@ -40,105 +45,129 @@ struct ClipList {
   ClipTensor t[CAP];
 };
 
-// What the 256 threads do with a run of n elements: sum of squares of this thread's (CLIP = false), or out = factor x.
-template <typename TI, typename TO, int V, bool CLIP>
-__device__ __forceinline__ double clip_run(const TI* in, TO* out, int64_t n, float factor, bool zero) {
-  constexpr int U = 16 / V < 2 ? 2 : 16 / V;      // loads under way in a thread: 16 elements
+// A thread's values whose float32 sum of squares left its comfortable range, once more: `pieces` pieces of `width` values.
+template <typename T>
+__device__ __noinline__ double squares64(const T* x, int pieces, int width, int distance) {
   double acc = 0.0;
-  for (int64_t i0 = 0; i0 < n; i0 += kClipThreads * V * U) {
-    Pack<TI, V> x[U];
-    const int64_t at = i0 + threadIdx.x * V;
+  for (int u = 0; u < pieces; ++u)
+    for (int k = 0; k < width; ++k) {
+      const double d = to_f32(x[u * distance + k]);
+      acc = fma(d, d, acc);
+    }
+  return acc;
+}
+
+// What is done with the elements: their squares are summed, or they are clipped.
+template <bool CLIP_>
+struct ClipPass {
+  static constexpr bool CLIP = CLIP_;
+  float factor;
+  bool zero;
+  double acc;
+};
+
+// U pieces of V values of this thread, the pieces kThreads * V apart, those from piece `count` on not there (ALL: all are).
+template <typename TI, typename TO, int V, int U, bool ALL, typename P>
+__device__ __forceinline__ void clip_pieces(P& p, const TI* in, TO* out, int count) {
+  constexpr int kApart = kClipThreads * V;
+  Pack<TI, V> x[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (at + u * kClipThreads * V < n) x[u].load(in + at + u * kClipThreads * V);
-    if (CLIP) {
+  for (int u = 0; u < U; ++u)
+    if (ALL || u < count) x[u].load(in + u * kApart);
+  if (P::CLIP) {
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        Pack<TO, V> y;
+    for (int u = 0; u < U; ++u) {
+      Pack<TO, V> y;
 #pragma unroll
-        for (int k = 0; k < V; ++k) y.t[k] = from_f32<TO>(zero ? 0.f : to_f32(x[u].t[k]) * factor);
-        if (at + u * kClipThreads * V < n) y.store_stream(out + at + u * kClipThreads * V);
-      }
-    } else {
+      for (int k = 0; k < V; ++k) y.t[k] = from_f32<TO>(p.zero ? 0.f : to_f32(x[u].t[k]) * p.factor);
+      if (ALL || u < count) y.store_stream(out + u * kApart);
+    }
+  } else {
+    constexpr int kGroup = 16 / V < U ? 16 / V : U;      // pieces of a float32 sum
+#pragma unroll
+    for (int u0 = 0; u0 < U; u0 += kGroup) {
       float q = 0.f;
 #pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (at + u * kClipThreads * V < n)
+      for (int u = u0; u < u0 + kGroup; ++u)
+        if (ALL || u < count)
 #pragma unroll
           for (int k = 0; k < V; ++k) q = fmaf(to_f32(x[u].t[k]), to_f32(x[u].t[k]), q);
-      if (q >= 1e-20f && q <= 1e37f) {
-        acc += q;
-      } else {
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-          if (at + u * kClipThreads * V < n)
-#pragma unroll
-            for (int k = 0; k < V; ++k) {
-              const double d = to_f32(x[u].t[k]);
-              acc = fma(d, d, acc);
-            }
-      }
+      if (q >= 1e-20f && q <= 1e37f)
+        p.acc += q;
+      else if (ALL || u0 < count)
+        p.acc += squares64(in + u0 * kApart, ALL ? kGroup : min(kGroup, count - u0), V, kApart);
     }
   }
-  return acc;
+}
+
+// A run of n elements (a multiple of V).
+template <typename TI, typename TO, int V, typename P>
+__device__ __forceinline__ void clip_run(P& p, const TI* in, TO* out, int64_t n) {
+  constexpr int U = V == 1 ? 8 : 64 / (V * (int)sizeof(TI));     // 64 bytes under way in a thread
+  constexpr int kStep = kClipThreads * V * U;
+  in += threadIdx.x * V;
+  out += threadIdx.x * V;
+  for (; n >= kStep; n -= kStep, in += kStep, out += kStep) clip_pieces<TI, TO, V, U, true>(p, in, out, U);
+  const int rest = (int)n - (int)threadIdx.x * V;
+  if (rest > 0) clip_pieces<TI, TO, V, U, false>(p, in, out, (rest + kClipThreads * V - 1) / (kClipThreads * V));
 }
 
 // A run whose ends may lie anywhere: wide words where the addresses of both sides allow it, after the elements before the
 // first boundary.
-template <typename TI, typename TO, bool CLIP>
-__device__ __forceinline__ double clip_span(const TI* in, TO* out, int64_t n, float factor, bool zero) {
-  constexpr int V = sizeof(TI) == 4 && (!CLIP || sizeof(TO) == 4) ? 4 : 8;
-  constexpr int kAlignIn = V * sizeof(TI) < 16 ? V * sizeof(TI) : 16, kAlignOut = V * sizeof(TO) < 16 ? V * sizeof(TO) : 16;
-  int64_t head = ((kAlignIn - ((uintptr_t)in & (kAlignIn - 1))) & (kAlignIn - 1)) / sizeof(TI);
-  if (head > n) head = n;
-  if (CLIP && ((uintptr_t)(out + head) & (kAlignOut - 1))) return clip_run<TI, TO, 1, CLIP>(in, out, n, factor, zero);
-  const int64_t body = (n - head) / V * V, tail = n - head - body;
-  double acc = 0.0;
-  if (threadIdx.x < head) acc += clip_run<TI, TO, 1, CLIP>(in, out, head, factor, zero);
-  acc += clip_run<TI, TO, V, CLIP>(in + head, out + head, body, factor, zero);
-  if (threadIdx.x < tail) acc += clip_run<TI, TO, 1, CLIP>(in + head + body, out + head + body, tail, factor, zero);
-  return acc;
+template <typename TI, typename TO, typename P>
+__device__ __forceinline__ void clip_span(P& p, const TI* in, TO* out, int64_t n) {
+  constexpr int V = sizeof(TI) == 4 && sizeof(TO) == 4 ? 4 : 8;
+  int head = (int)(((16 - ((uintptr_t)in & 15)) & 15) / sizeof(TI));
+  if (head > n) head = (int)n;
+  if (P::CLIP && ((uintptr_t)(out + head) & 15)) {
+    clip_run<TI, TO, 1>(p, in, out, n);
+    return;
+  }
+  const int64_t body = (n - head) / V * V;
+  const int tail = (int)(n - head - body), t = (int)threadIdx.x;
+  clip_run<TI, TO, V>(p, in + head, out + head, body);
+  if (t < head + tail) {     // fewer than 16 elements: one a thread
+    const int64_t at = t < head ? t : body + t;
+    clip_pieces<TI, TO, 1, 1, true>(p, in + at, out + at, 1);
+  }
 }
 
-// Units [u0, u1) of one tensor of client c.  Calls, not copies: the kernel has one for each pair of types.
-template <typename TI, typename TO, bool CLIP>
-__device__ __noinline__ double clip_units(const ClipTensor& t, int64_t c, int64_t u0, int64_t u1, float factor, bool zero) {
+// Units [u0, u1) of one tensor of client c.
+template <typename TI, typename TO, typename P>
+__device__ __forceinline__ void clip_units(P& p, const ClipTensor& t, int64_t c, int64_t u0, int64_t u1) {
   const TI* in = static_cast<const TI*>(t.in) + c * t.stride_in;
-  TO* out = CLIP ? static_cast<TO*>(t.out) + c * t.stride_out : nullptr;
-  double acc = 0.0;
+  TO* out = static_cast<TO*>(t.out) + c * t.stride_out;     // summing does not look at it
   if (t.row_units) {
-    for (int64_t u = u0; u < u1;) {
-      const int64_t row = u / t.row_units, k = u - row * t.row_units;
-      const int64_t stop = u1 - u < t.row_units - k ? k + u1 - u : t.row_units;   // of this row
+    while (u0 < u1) {
+      const int64_t row = t.rows > 1 ? u0 / t.row_units : 0, k = u0 - row * t.row_units;
+      const int64_t stop = u1 - u0 < t.row_units - k ? k + u1 - u0 : t.row_units;   // of this row
       const int64_t a = k * kClipUnit, b = stop * kClipUnit < t.cols ? stop * kClipUnit : t.cols;
-      acc += clip_span<TI, TO, CLIP>(in + row * t.ld_in + a, CLIP ? out + row * t.ld_out + a : nullptr, b - a, factor, zero);
-      u += stop - k;
+      clip_span(p, in + row * t.ld_in + a, out + row * t.ld_out + a, b - a);
+      u0 += stop - k;
     }
-    return acc;
+    return;
   }
   const int64_t n = t.rows * t.cols, end = u1 * kClipUnit < n ? u1 * kClipUnit : n;
   for (int64_t e = u0 * kClipUnit + threadIdx.x; e < end; e += kClipThreads) {
     const int64_t row = e / t.cols, col = e - row * t.cols;
-    const float x = to_f32(in[row * t.ld_in + col]);
-    if (CLIP)
-      out[row * t.ld_out + col] = from_f32<TO>(zero ? 0.f : x * factor);
-    else
-      acc = fma((double)x, (double)x, acc);
+    clip_pieces<TI, TO, 1, 1, true>(p, in + row * t.ld_in + col, out + row * t.ld_out + col, 1);
   }
-  return acc;
 }
 
-template <bool CLIP>
-__device__ __forceinline__ double clip_tensor(const ClipTensor& t, int64_t c, int64_t u0, int64_t u1, float factor, bool zero) {
-  auto in_as = [&](auto to) {
-    using TO = decltype(to);
-    if (t.in_type == kTypeF32) return clip_units<float, TO, CLIP>(t, c, u0, u1, factor, zero);
-    if (t.in_type == kTypeBF16) return clip_units<__nv_bfloat16, TO, CLIP>(t, c, u0, u1, factor, zero);
-    return clip_units<__half, TO, CLIP>(t, c, u0, u1, factor, zero);
-  };
-  if (!CLIP || t.out_type == kTypeF32) return in_as(float{});
-  if (t.out_type == kTypeBF16) return in_as(__nv_bfloat16{});
-  return in_as(__half{});
+// f(tensor, first unit of it, end) for each of the list's tensors that has some of the units [u, end).
+template <int CAP, typename F>
+__device__ __forceinline__ void clip_walk(const ClipList<CAP>& list, int count, int64_t u, int64_t end, F&& f) {
+  int i = 0;
+  constexpr int kFirst = CAP >= 256 ? 256 : CAP >= 32 ? 32 : 8;
+  static_assert(CAP <= 2 * kFirst, "the steps reach every tensor");
+  for (int step = kFirst; step; step >>= 1)          // the last tensor that begins at u or before
+    if (i + step < count && list.t[i + step].unit0 <= u) i += step;
+  for (; u < end; ++i) {
+    const int64_t stop = i + 1 < count && list.t[i + 1].unit0 < end ? list.t[i + 1].unit0 : end;
+    const ClipTensor& t = list.t[i];
+    f(t, u - t.unit0, stop - t.unit0);
+    u = stop;
+  }
 }
 
 // Sum over the CTA, in every thread.
@@ -151,59 +180,49 @@ __device__ __forceinline__ double clip_block_sum(double v, double* cell) {
   return v;
 }
 
-__device__ __forceinline__ double clip_total(const ClipArgs& p, int64_t c, double* cell) {
+// Sum of client c's parts, in every thread.
+__device__ __forceinline__ double clip_total(const ClipArgs& a, int64_t c, double* cell) {
   double v = 0.0;
-  for (int64_t k = threadIdx.x; k < p.parts; k += kClipThreads) v += p.part[c * p.parts + k];
+  for (int64_t k = threadIdx.x; k < a.parts; k += kClipThreads) v += a.part[c * a.parts + k];
   return clip_block_sum(v, cell);
 }
 
-// CTAs (x, y): y below clip_count clips client clip_first + y, the others sum client sum_first + y - clip_count.
-template <int CAP>
-__global__ void __launch_bounds__(kClipThreads) clip_kernel(const ClipArgs p, const __grid_constant__ ClipList<CAP> list) {
+// All tensors of a launch are of the types TI and TO.  grid: (CTAs of a client, clients)
+template <typename TI, int CAP>
+__global__ void __launch_bounds__(kClipThreads, kClipResident) clip_sum_kernel(const ClipArgs a, const __grid_constant__ ClipList<CAP> list) {
   __shared__ double cell[kClipThreads / 32];
   grid_trigger();
   grid_wait();
-  const bool clip = (int)blockIdx.y < p.clip_count;
-  const int64_t c = clip ? p.clip_first + (int)blockIdx.y : p.sum_first + (int)blockIdx.y - p.clip_count;
-  float factor = 1.f;
-  bool zero = false;
-  if (clip) {
-    const double norm = sqrt(clip_total(p, c, cell));
-    const double f = norm == 0.0 ? 1.0 : (double)p.max_norm / (norm + (double)p.eps);
-    factor = f > 1.0 ? 1.f : (float)f;
-    zero = p.zero_bad && !isfinite(norm);
-    if (p.norms && threadIdx.x == 0 && blockIdx.x == 0 && p.part0 == 0) p.norms[c] = (float)norm;
-  }
-  int64_t u = p.units * blockIdx.x / gridDim.x;
-  const int64_t end = p.units * (blockIdx.x + 1) / gridDim.x;
-  int i = 0;
-  constexpr int kFirst = CAP >= 256 ? 256 : CAP >= 32 ? 32 : 8;
-  static_assert(CAP <= 2 * kFirst, "the steps reach every tensor");
-  for (int step = kFirst; step; step >>= 1)          // the last tensor that begins at u or before
-    if (i + step < p.count && list.t[i + step].unit0 <= u) i += step;
-  double acc = 0.0;
-  for (; u < end; ++i) {
-    const int64_t stop = i + 1 < p.count && list.t[i + 1].unit0 < end ? list.t[i + 1].unit0 : end;
-    if (stop <= u) continue;                         // a tensor without elements
-    const ClipTensor& t = list.t[i];
-    if (!clip)
-      acc += clip_tensor<false>(t, c, u - t.unit0, stop - t.unit0, 1.f, false);
-    else if (factor != 1.f || zero || t.in != t.out)
-      clip_tensor<true>(t, c, u - t.unit0, stop - t.unit0, factor, zero);
-    u = stop;
-  }
-  if (!clip) {
-    acc = clip_block_sum(acc, cell);
-    if (threadIdx.x == 0) p.part[c * p.parts + p.part0 + blockIdx.x] = acc;
-  }
+  const int64_t c = blockIdx.y;
+  ClipPass<false> p = {};
+  clip_walk(list, a.count, a.units * blockIdx.x / gridDim.x, a.units * (blockIdx.x + 1) / gridDim.x,
+            [&](const ClipTensor& t, int64_t u0, int64_t u1) { clip_units<TI, TI>(p, t, c, u0, u1); });
+  const double sum = clip_block_sum(p.acc, cell);
+  if (threadIdx.x == 0) a.part[c * a.parts + a.part0 + blockIdx.x] = sum;
 }
 
-__global__ void __launch_bounds__(kClipThreads) clip_norms_kernel(const ClipArgs p) {
+template <typename TI, typename TO, int CAP>
+__global__ void __launch_bounds__(kClipThreads, kClipResident) clip_apply_kernel(const ClipArgs a, const __grid_constant__ ClipList<CAP> list) {
   __shared__ double cell[kClipThreads / 32];
   grid_trigger();
   grid_wait();
-  const double total = clip_total(p, blockIdx.x, cell);
-  if (threadIdx.x == 0) p.norms[blockIdx.x] = (float)sqrt(total);
+  const int64_t c = gridDim.y - 1 - blockIdx.y, x = gridDim.x - 1 - blockIdx.x;
+  const double norm = sqrt(clip_total(a, c, cell)), f = norm == 0.0 ? 1.0 : (double)a.max_norm / (norm + (double)a.eps);
+  ClipPass<true> p = {};
+  p.factor = f > 1.0 ? 1.f : (float)f;      // NaN stays
+  p.zero = a.zero_bad && !isfinite(norm);
+  if (a.norms && threadIdx.x == 0 && x == 0 && a.part0 == 0) a.norms[c] = (float)norm;
+  clip_walk(list, a.count, a.units * x / gridDim.x, a.units * (x + 1) / gridDim.x, [&](const ClipTensor& t, int64_t u0, int64_t u1) {
+    if (p.factor != 1.f || p.zero || t.in != t.out) clip_units<TI, TO>(p, t, c, u0, u1);
+  });
+}
+
+__global__ void __launch_bounds__(kClipThreads) clip_norms_kernel(const ClipArgs a) {
+  __shared__ double cell[kClipThreads / 32];
+  grid_trigger();
+  grid_wait();
+  const double total = clip_total(a, blockIdx.x, cell);
+  if (threadIdx.x == 0) a.norms[blockIdx.x] = (float)sqrt(total);
 }
 
 }  // namespace brace

@@ -20,6 +20,9 @@ inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_
 inline int elem_bytes(int type) { return type == BRACE_TYPE_F32 || type == BRACE_TYPE_BITS ? 4 : 2; }
 inline bool float_type(int t) { return t == BRACE_TYPE_F32 || t == BRACE_TYPE_BF16 || t == BRACE_TYPE_F16; }
 
+inline bool typed(const void* p, int type) { return p && aligned(p, (size_t)elem_bytes(type)); }
+inline bool typed_or_null(const void* p, int type) { return !p || aligned(p, (size_t)elem_bytes(type)); }
+
 // Rows and matrices whose 8-element groups are whole 16-byte words.
 inline bool wide_rows(const void* p, int type, int64_t ld, int64_t s1, int64_t s2 = 0) {
   const int64_t per = 16 / elem_bytes(type);
@@ -73,6 +76,18 @@ cudaError_t with_type(int type, F&& f) {
   if (type == BRACE_TYPE_F32) return f(float{});
   if (type == BRACE_TYPE_BF16) return f(__nv_bfloat16{});
   return f(__half{});
+}
+
+// Lets a kernel use its shared memory on the current device (once per device and kernel).
+inline cudaError_t grant_smem(const void* kernel, std::atomic<uint64_t>& granted, int bytes) {
+  int dev = 0;
+  cudaError_t err = cudaGetDevice(&dev);
+  if (err != cudaSuccess) return err;
+  const uint64_t bit = 1ull << (dev & 63);
+  if (granted.load(std::memory_order_relaxed) & bit) return cudaSuccess;
+  err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (err == cudaSuccess) granted.fetch_or(bit, std::memory_order_relaxed);
+  return err;
 }
 
 using EncodeFn = decltype(&cuTensorMapEncodeTiled);

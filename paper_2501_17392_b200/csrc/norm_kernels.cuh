@@ -65,7 +65,7 @@ __device__ __forceinline__ void group_sum(float (&v)[N], int group, float (*cell
 
 // Forward.  Thread g of a row's G has the NV groups of V columns (i G + g) V .. + V.
 template <typename TX, typename TY, int V, int NV>
-__global__ void __launch_bounds__(kNormThreads) norm_forward_kernel(const NormArgs p) {
+__global__ void __launch_bounds__(kNormThreads, NV * V > 24 ? 2 : NV * V > 12 ? 3 : 4) norm_forward_kernel(const NormArgs p) {
   __shared__ float cell[2][kNormThreads / 32][2];
   grid_trigger();
   grid_wait();
@@ -133,7 +133,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_forward_kernel(const NormAr
 
 // Backward: dx, and this CTA's part of dweight and dbias (the whole of it where there is one CTA for a client).
 template <typename TX, typename TY, int V, int NV>
-__global__ void __launch_bounds__(kNormThreads) norm_grad_kernel(const NormArgs p) {
+__global__ void __launch_bounds__(kNormThreads, NV * V > 24 ? 1 : NV * V > 12 ? 2 : 3) norm_grad_kernel(const NormArgs p) {
   __shared__ float cell[2][kNormThreads / 32][2];
   __shared__ float sums[2][1024];    // rows of a warp or less have at most 1024 columns
   grid_trigger();

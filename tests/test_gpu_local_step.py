@@ -471,3 +471,42 @@ def test_workspaces_of_exactly_the_size():
     plan.clip(1.0)
     torch.cuda.synchronize()
     assert bool((whole[:at] == 255).all()) and bool((whole[at + need:] == 255).all())
+
+
+@pytest.mark.parametrize("c,shapes,tin,tout", [(3000, [(4001,)], F32, F32), (2500, [(33, 65), (7,), (2048,)], F32, BF16),
+                                               (150, [(100003,), (5,), (300, 301)], BF16, F32),
+                                               (12, [(1000, 1000), (999999,), (1,)], F32, F16),
+                                               (1, [(7000, 1001), (12_000_001,), (3,)], F32, F32),
+                                               (7, [(11, 13)] * 39 + [(1_500_000,)], F32, F32)])
+def test_clip_of_large_calls(c, shapes, tin, tout):
+    for at in (0, 1):
+        _, x = pieces(c, shapes, tin, seed=3, at=at, scale=1.0)
+        _, y = pieces(c, shapes, tout, seed=4, at=at)
+        total = math.sqrt(sum(math.prod(s) for s in shapes))
+        x[0] *= torch.linspace(0.2, 2, c, device="cuda").to(tin).view(-1, *[1] * (x[0].dim() - 1))
+        check_clip(x, y, total)
+    if tin == tout:
+        check_clip(x, None, total)
+
+
+def test_clip_of_a_large_call_in_a_graph():
+    x = randn(9, 2_000_003, seed=5)
+    y, norms = torch.empty_like(x), torch.empty(9, device="cuda")
+    plan = B.GradientClip([x], [y])
+    plan.clip(1000.0, norms=norms)
+    torch.cuda.synchronize()
+    want = y.clone(), norms.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        plan.clip(1000.0, norms=norms)
+    for _ in range(3):
+        y.zero_()
+        norms.zero_()
+        plan.workspace[256:].fill_(255)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, want[0]) and torch.equal(norms, want[1])
+    x[4, 77] = math.nan
+    graph.replay()
+    torch.cuda.synchronize()
+    assert bool(y[4].isnan().all()) and torch.equal(y[3], want[0][3]) and bool(norms[4].isnan())
