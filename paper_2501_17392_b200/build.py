@@ -16,7 +16,10 @@ OBJ_DIR = os.path.join(PKG_DIR, "_build")
 _HEADERS = {
     "brace.cu": ("brace_kernels.cuh",),
     "operators.cu": ("elements.cuh", "embedding_kernels.cuh", "host.cuh", "ortho_kernels.cuh", "sm100.cuh"),
-    "attention.cu": ("attention_rows.cuh", "attention_tiles.cuh", "elements.cuh", "host.cuh", "sm100.cuh"),
+    "attention.cu": ("attention_blocks.cuh", "attention_host.cuh", "attention_rows.cuh", "attention_tiles.cuh", "elements.cuh",
+                     "host.cuh", "sm100.cuh"),
+    "attention_float.cu": ("attention_blocks.cuh", "attention_float.cuh", "attention_host.cuh", "attention_rows.cuh",
+                           "elements.cuh", "host.cuh", "sm100.cuh"),
     "clip.cu": ("clip_kernels.cuh", "elements.cuh", "host.cuh", "sm100.cuh"),
     "norm.cu": ("elements.cuh", "host.cuh", "norm_kernels.cuh", "sm100.cuh"),
 }

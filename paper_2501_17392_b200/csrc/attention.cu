@@ -4,29 +4,29 @@
 #include <algorithm>
 #include <cmath>
 
-#include "attention_rows.cuh"
+#include "attention_host.cuh"
 #include "attention_tiles.cuh"
-#include "host.cuh"
 
 using namespace brace;
 
 namespace {
 
 bool attn_sizes_ok(int32_t batch, int32_t tokens, int32_t heads) { return batch >= 0 && tokens >= 0 && heads >= 0; }
-// positions, and sums of two of them, are 32-bit numbers
-bool attn_served(int32_t batch, int32_t tokens, int32_t heads, int32_t dim) {
-  return batch <= 65535 && tokens <= 1 << 29 && heads <= 65535 && dim <= kHeadMost;
+// positions, sums of two of them, and blocks of 32 queries of all heads that share a key are 32-bit numbers
+bool attn_served(int32_t batch, int32_t tokens, int32_t heads, int32_t kv_heads, int32_t dim) {
+  return batch <= 65535 && tokens <= 1 << 29 && heads <= 65535 && dim <= kHeadMost &&
+         (heads == 0 || (tokens / 32 + 2) * (int64_t)(heads / kv_heads) < (int64_t)1 << 31);
 }
 
 constexpr int kGradCtas = 148 * 4;   // that the first tokens' tiles are shared out over
 
-// The first tokens' tiles and the most pieces of all of them together.
+// The first tokens' tiles of `rows` keys, and the most pieces of all of them together.
 struct FirstTiles {
   int64_t tiles, pieces;   // of a sequence and kv head; of all
 };
-FirstTiles first_tiles(int32_t batch, int32_t tokens, int32_t heads, int32_t kv_heads, int32_t sinks) {
+FirstTiles first_tiles(int32_t batch, int32_t tokens, int32_t heads, int32_t kv_heads, int32_t sinks, int rows) {
   FirstTiles f = {};
-  f.tiles = (std::min(sinks, tokens) + (int64_t)127) / 128;
+  f.tiles = (std::min(sinks, tokens) + (int64_t)rows - 1) / rows;
   const int64_t all = f.tiles * batch * kv_heads;
   if (all == 0) return f;
   const int64_t blocks = ((int64_t)tokens + kBlock - 1) / kBlock * (heads / kv_heads);
@@ -46,8 +46,10 @@ GradPlan grad_plan(int32_t batch, int32_t tokens, int32_t heads, int32_t kv_head
   q.off_shift = (size_t)numbers;
   q.off_range = (size_t)(2 * numbers);
   q.off_part = q.off_range + (size_t)round_up((int64_t)batch * kv_heads * 8, 256);
-  const int64_t pieces = dim % 8 == 0 && dim <= 128 ? first_tiles(batch, tokens, heads, kv_heads, sinks).pieces : 0;
-  q.bytes = q.off_part + (size_t)(pieces * 2 * 128 * (dim <= 64 ? 64 : 128) * 4);
+  // of the tensor cores' kernels or of those in float32, whichever the call will take
+  const int64_t wide = first_tiles(batch, tokens, heads, kv_heads, sinks, 128).pieces * 128;
+  const int64_t narrow = first_tiles(batch, tokens, heads, kv_heads, sinks, kFloatRows).pieces * kFloatRows;
+  q.bytes = q.off_part + (size_t)(std::max(wide, narrow) * 2 * (dim <= 64 ? 64 : dim <= 128 ? 128 : 256) * 4);
   if (q.bytes < 256) q.bytes = 256;
   return q;
 }
@@ -56,7 +58,7 @@ int attn_check(const brace_window_attention* e) {
   if (!e || !attn_sizes_ok(e->batch, e->tokens, e->heads) || e->kv_heads < 0 || e->dim < 1) return BRACE_ERR_INVALID_ARG;
   if (!float_type(e->type) || e->window < 1 || e->sinks < 0 || !std::isfinite(e->scale)) return BRACE_ERR_INVALID_ARG;
   if (e->heads > 0 && (e->kv_heads < 1 || e->heads % e->kv_heads)) return BRACE_ERR_INVALID_ARG;
-  if (!attn_served(e->batch, e->tokens, e->heads, e->dim)) return BRACE_ERR_UNSUPPORTED;
+  if (!attn_served(e->batch, e->tokens, e->heads, e->kv_heads, e->dim)) return BRACE_ERR_UNSUPPORTED;
   return BRACE_OK;
 }
 
@@ -110,7 +112,6 @@ bool tiles_ok(const brace_heads& x, const brace_window_attention* e, int heads) 
 
 bool tiles_served(const brace_window_attention* e, bool grad) {
   if (e->type == BRACE_TYPE_F32 || e->dim % 8 || e->dim > 128) return false;
-  if ((e->tokens / kBlock + 1) * (int64_t)(e->heads / e->kv_heads) >= 1 << 30) return false;   // blocks of a tile of keys
   if (!tiles_ok(e->q, e, e->heads) || !tiles_ok(e->k, e, e->kv_heads) || !tiles_ok(e->v, e, e->kv_heads)) return false;
   if (!grad) return tiles_ok(e->out, e, e->heads);
   return tiles_ok(e->dout, e, e->heads) && tiles_ok(e->dq, e, e->heads) && tiles_ok(e->dk, e, e->kv_heads) && tiles_ok(e->dv, e, e->kv_heads);
@@ -172,7 +173,7 @@ cudaError_t run_grad(const brace_window_attention* e, AttnArgs a, cudaStream_t s
   if (err == cudaSuccess) err = launch_grad<T, D, true>(keys, a, st);
   if (err == cudaSuccess) err = launch_grad<T, D, false>(queries, a, st);
   if (err == cudaSuccess && a.first_tiles)
-    err = launch(attn_join_kernel<T, D>, dim3((unsigned)(a.first_tiles * 32), (unsigned)a.kv_heads, (unsigned)a.batch), 128, 0, 1, st, a);
+    err = launch(attn_join_kernel<T, D, 128>, dim3((unsigned)(a.first_tiles * 32), (unsigned)a.kv_heads, (unsigned)a.batch), 128, 0, 1, st, a);
   return err;
 }
 
@@ -181,8 +182,16 @@ cudaError_t with_half_type(int type, F&& f) {
   return type == BRACE_TYPE_BF16 ? f(__nv_bfloat16{}) : f(__half{});
 }
 
-dim3 row_grid(const brace_window_attention* e, int heads) {
-  return dim3((unsigned)((e->tokens + 3) / 4), (unsigned)heads, (unsigned)e->batch);
+// How the gradient's tiles of first tokens are shared out: over as many CTAs as make a CTA's work that of a tile behind
+// them, but no more than give every SM some.
+void share_out(const brace_window_attention* e, int rows, AttnArgs& a) {
+  const FirstTiles f = first_tiles(e->batch, e->tokens, e->heads, e->kv_heads, e->sinks, rows);
+  a.first_tiles = (int)f.tiles;
+  a.pieces = 0;
+  if (!f.tiles) return;
+  const int64_t window = std::min<int64_t>(e->tokens, (int64_t)a.window + rows - 1);
+  const int64_t even = ((int64_t)e->tokens + window - 1) / window, most = f.pieces / (f.tiles * e->batch * e->kv_heads);
+  a.pieces = (int)std::max<int64_t>(1, std::min(even, most));
 }
 
 }  // namespace
@@ -209,9 +218,7 @@ int brace_window_attention_forward(const brace_window_attention* e, brace_stream
     });
     return err == cudaSuccess ? BRACE_OK : cuda_fail_no_ctx(err);
   }
-  const cudaError_t err = with_type(e->type, [&](auto t) {
-    return launch(attn_forward_rows_kernel<decltype(t)>, row_grid(e, e->heads), kRowThreads, 0, 1, st, a);
-  });
+  const cudaError_t err = attn_forward_float(e->type, a, st);
   return err == cudaSuccess ? BRACE_OK : cuda_fail_no_ctx(err);
 }
 
@@ -219,7 +226,7 @@ size_t brace_window_attention_workspace_bytes(int32_t batch, int32_t tokens, int
                                               int32_t sinks) {
   if (!attn_sizes_ok(batch, tokens, heads) || kv_heads < 0 || dim < 1 || sinks < 0) return 0;
   if (heads > 0 && (kv_heads < 1 || heads % kv_heads)) return 0;
-  if (!attn_served(batch, tokens, heads, dim)) return 0;
+  if (!attn_served(batch, tokens, heads, kv_heads, dim)) return 0;
   return grad_plan(batch, tokens, heads, kv_heads, dim, sinks).bytes;
 }
 
@@ -247,28 +254,15 @@ int brace_window_attention_grad(const brace_window_attention* e, void* d_workspa
   a.padded = q.padded;
   const cudaStream_t st = (cudaStream_t)stream;
   if (tiles_served(e, true)) {
-    // A tile of first tokens is shared out over as many CTAs as make a CTA's work that of a tile behind them, or as give
-    // every SM some.
-    const FirstTiles f = first_tiles(e->batch, e->tokens, e->heads, e->kv_heads, e->sinks);
-    a.first_tiles = (int)f.tiles;
-    if (f.tiles) {
-      const int64_t window = std::min<int64_t>(e->tokens, (int64_t)a.window + 127);
-      const int64_t even = ((int64_t)e->tokens + window - 1) / window, most = f.pieces / (f.tiles * e->batch * e->kv_heads);
-      a.pieces = (int)std::max<int64_t>(1, std::min(even, most));
-    }
+    share_out(e, 128, a);
     const cudaError_t err = with_half_type(e->type, [&](auto t) {
       using T = decltype(t);
       return e->dim <= 64 ? run_grad<T, 64>(e, a, st) : run_grad<T, 128>(e, a, st);
     });
     return err == cudaSuccess ? BRACE_OK : cuda_fail_no_ctx(err);
   }
-  const cudaError_t err = with_type(e->type, [&](auto t) {
-    using T = decltype(t);
-    cudaError_t r = launch(attn_delta_kernel<T>, row_grid(e, e->heads), kRowThreads, 0, 1, st, a);
-    if (r == cudaSuccess) r = launch(attn_dq_rows_kernel<T>, row_grid(e, e->heads), kRowThreads, 0, 1, st, a);
-    if (r == cudaSuccess) r = launch(attn_dkv_rows_kernel<T>, row_grid(e, e->kv_heads), kRowThreads, 0, 1, st, a);
-    return r;
-  });
+  share_out(e, kFloatRows, a);
+  const cudaError_t err = attn_grad_float(e->type, a, st);
   return err == cudaSuccess ? BRACE_OK : cuda_fail_no_ctx(err);
 }
 

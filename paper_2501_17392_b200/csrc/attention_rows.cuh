@@ -1,4 +1,5 @@
-// Windowed attention, row by row: a warp computes one row of a result in float32, whatever the sizes, strides and types.
+// Windowed attention: formulas, arguments, and single rows.  A warp computes a row of a result in float32, whatever the
+// sizes, strides and types; the kernels do this for rows that hidden places have spoiled.
 //
 // Query i sees key j iff j <= i and (i - j < window or j < sinks), both below the sequence's length n.
 //   s_ij = scale q_i.k_j,  lse_i = log sum_j exp s_ij,  p_ij = exp(s_ij - lse_i),  o_i = sum_j p_ij v_j
@@ -165,45 +166,6 @@ __device__ __forceinline__ void dkv_row(const AttnArgs& p, int b, int g, int j, 
     }
   if (put_k) put_row(head_row<T>(p.dk, b, j, g), dk, p.scale, p.dim);
   if (put_v) put_row(head_row<T>(p.dv, b, j, g), dv, 1.f, p.dim);
-}
-
-constexpr int kRowThreads = 128;
-
-// grid: (tokens / 4, heads, batch)
-template <typename T>
-__global__ void __launch_bounds__(kRowThreads) attn_forward_rows_kernel(const AttnArgs p) {
-  grid_trigger();
-  grid_wait();
-  const int i = blockIdx.x * (kRowThreads / 32) + (threadIdx.x >> 5), b = blockIdx.z;
-  if (i < p.tokens) forward_row<T>(p, b, blockIdx.y, i, attn_length(p, b));
-}
-template <typename T>
-__global__ void __launch_bounds__(kRowThreads) attn_dq_rows_kernel(const AttnArgs p) {
-  grid_trigger();
-  grid_wait();
-  const int i = blockIdx.x * (kRowThreads / 32) + (threadIdx.x >> 5), b = blockIdx.z;
-  if (i < p.tokens) dq_row<T>(p, b, blockIdx.y, i, attn_length(p, b));
-}
-template <typename T>
-__global__ void __launch_bounds__(kRowThreads) attn_dkv_rows_kernel(const AttnArgs p) {
-  grid_trigger();
-  grid_wait();
-  const int j = blockIdx.x * (kRowThreads / 32) + (threadIdx.x >> 5), b = blockIdx.z;
-  if (j < p.tokens) dkv_row<T>(p, b, blockIdx.y, j, attn_length(p, b));
-}
-
-// delta_i = do_i.o_i, a warp a row.
-template <typename T>
-__global__ void __launch_bounds__(kRowThreads) attn_delta_kernel(const AttnArgs p) {
-  grid_trigger();
-  grid_wait();
-  const int i = blockIdx.x * (kRowThreads / 32) + (threadIdx.x >> 5), h = blockIdx.y, b = blockIdx.z;
-  if (i >= attn_length(p, b)) return;
-  const T *o = head_row<const T>(p.out, b, i, h), *dout = head_row<const T>(p.dout, b, i, h);
-  float s = 0.f;
-  for (int d = threadIdx.x & 31; d < p.dim; d += 32) s = fmaf(to_f32(o[d]), to_f32(dout[d]), s);
-  for (int o2 = 16; o2; o2 >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o2);
-  if ((threadIdx.x & 31) == 0) p.delta[attn_delta(p, b, h, i)] = s;
 }
 
 }  // namespace brace

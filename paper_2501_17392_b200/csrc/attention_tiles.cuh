@@ -22,7 +22,7 @@
 
 #include <type_traits>
 
-#include "attention_rows.cuh"
+#include "attention_blocks.cuh"
 
 namespace brace {
 
@@ -88,19 +88,6 @@ template <typename T>
 __device__ __forceinline__ void put_zeros(T* row, int dim) {
   for (int i = 0; i < dim; i += 8) *reinterpret_cast<uint4*>(row + i) = make_uint4(0, 0, 0, 0);
 }
-
-// The blocks of keys that a CTA walks: those of the first tokens that lie before the window of its first query, then the
-// window's, from the first key of the first query's window on.
-struct KeyBlocks {
-  int lo, first, nfirst, count;
-  __device__ __forceinline__ KeyBlocks(const AttnArgs& p, int q_first, int q_end, int width) {
-    lo = max(0, q_first - p.window + 1);
-    first = min(p.sinks, lo);
-    nfirst = (first + width - 1) / width;
-    count = nfirst + (q_end - lo + width - 1) / width;
-  }
-  __device__ __forceinline__ int key(int k, int width) const { return k < nfirst ? k * width : lo + (k - nfirst) * width; }
-};
 
 // grid: (pairs of groups, heads or pairs of heads, sequences)
 template <typename T, int D, bool SHARED>
@@ -423,18 +410,13 @@ __device__ __forceinline__ float attn_grad_scale(const AttnArgs& p, int b, int g
   return bound > 0.f ? ldexpf(1.f, 13 - ilogbf(bound)) : 1.f;
 }
 
-// What a CTA of the backward pass computes.
-struct GradWork {
-  int row0, begin, end;                    // first row; blocks
-  int per_head;                            // blocks of queries of a head (DKV)
-  int tile, piece;                         // of first tokens (DKV), or -1
-};
-
 // grid: DKV (pieces of the first tokens' tiles, then tiles; kv heads; sequences), else (tiles of queries, heads, sequences)
 template <typename T, int D, bool DKV>
 __global__ void __launch_bounds__(kAttnThreads, 1) attn_grad_kernel(const __grid_constant__ AttnMaps maps, const AttnArgs p) {
   using Shape = AttnGradShape<D, DKV>;
   constexpr int STAGES = Shape::kStages;
+  // float16: ds as the sum of two values.  With one, its rounding and the result's together are 1.5 times the result's alone
+  constexpr bool kTwo = std::is_same<T, __half>::value;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t base = (smem_addr(smem_raw) + 1023u) & ~1023u;
   const uint32_t ring = base + 2 * Shape::kTile, bars = ring + STAGES * Shape::kStage;
@@ -471,44 +453,16 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_grad_kernel(const __grid
   grid_wait();
   fence_async_global();
 
-  const int b = blockIdx.z, n = attn_length(p, b), g = DKV ? (int)blockIdx.y : (int)blockIdx.y / p.share;
-  GradWork w;
-  w.tile = w.piece = -1;
-  w.begin = w.end = 0;
-  w.per_head = 1;
-  if (DKV) {
-    const int x = blockIdx.x, first = p.first_tiles * p.pieces;
-    if (x < first) {
-      w.tile = x / p.pieces;
-      w.piece = x % p.pieces;
-    }
-    w.row0 = 128 * (x < first ? w.tile : p.first_tiles + x - first);
-  } else {
-    w.row0 = 128 * (int)(gridDim.x - 1 - blockIdx.x);       // the last queries first: they have the longest windows
-  }
-  const KeyBlocks keys(p, w.row0, min(n, w.row0 + 128), kBlock);
-  if (w.row0 < n) {
-    if (DKV) {
-      // the tile's queries: from its first key to the end of its last one's window, or all from there on
-      const int stop = w.row0 < p.sinks || p.window + 127 > n - w.row0 ? n : w.row0 + 127 + p.window;
-      w.per_head = (stop - w.row0 + kBlock - 1) / kBlock;
-      const int64_t all = (int64_t)w.per_head * p.share;
-      w.begin = w.piece < 0 ? 0 : (int)(all * w.piece / p.pieces);
-      w.end = w.piece < 0 ? (int)all : (int)(all * (w.piece + 1) / p.pieces);
-    } else {
-      w.end = keys.count;
-    }
-  }
-  const int count = w.end - w.begin;
-  auto block_head = [&](int k) { return DKV ? g * p.share + (w.begin + k) / w.per_head : (int)blockIdx.y; };
-  auto block_first = [&](int k) { return DKV ? w.row0 + (w.begin + k) % w.per_head * kBlock : keys.key(k, kBlock); };
+  const int b = blockIdx.z, n = attn_length(p, b);
+  const GradWork w(p, n, DKV, 128, kBlock);
+  const int g = DKV ? w.head : w.head / p.share, count = w.count;
 
   if (warp == 8) {                         // loads
     const bool lead = elect_one();
     if (lead && count) {
       mbar_expect_tx(a_full, 2 * Shape::kTile);
-      load_rows<D, 128>(base, DKV ? &maps.k : &maps.q, w.row0, DKV ? g : (int)blockIdx.y, b, a_full);
-      load_rows<D, 128>(base + Shape::kTile, DKV ? &maps.v : &maps.dout, w.row0, DKV ? g : (int)blockIdx.y, b, a_full);
+      load_rows<D, 128>(base, DKV ? &maps.k : &maps.q, w.row0, w.head, b, a_full);
+      load_rows<D, 128>(base + Shape::kTile, DKV ? &maps.v : &maps.dout, w.row0, w.head, b, a_full);
     }
     __syncwarp();
     int s = 0, issued = 0;
@@ -521,7 +475,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_grad_kernel(const __grid
       }
       if (lead) {
         const uint32_t at = ring + s * Shape::kStage, bar = full + 8 * s;
-        const int t = block_first(k), h = block_head(k);
+        const int t = w.first(k), h = w.head_of(k, p);
         mbar_expect_tx(bar, 2 * Shape::kHalf + (DKV ? 2 * kBlock * 4 : 0));
         if (DKV) {     // the boxes of q and do have 64 rows here, those of k and v in the other pass
           load_rows<D, kBlock>(at, &maps.q, t, h, b, bar);
@@ -582,6 +536,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_grad_kernel(const __grid
           } else {
             mma_f16_ts(tmem + 256, a + 64 + 8 * i, db + (uint64_t)(2048 * i >> 4), kSums, k > 0 || i > 0);
           }
+          if (kTwo) mma_f16_ts(tmem + 256 + (DKV ? D : 0), a + 96 + 8 * i, db + (uint64_t)(2048 * i >> 4), kSums, 1);
         }
         mma_commit<1>(empty + 8 * s);
       }
@@ -596,8 +551,8 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_grad_kernel(const __grid
     const float c = p.scale * kLog2e, hold = count ? attn_grad_scale(p, b, g) : 1.f;
     float shift = 0.f, delta = 0.f;
     if (!DKV && at < n) {
-      shift = p.shift[attn_delta(p, b, blockIdx.y, at)];
-      delta = p.delta[attn_delta(p, b, blockIdx.y, at)];
+      shift = p.shift[attn_delta(p, b, w.head, at)];
+      delta = p.delta[attn_delta(p, b, w.head, at)];
     }
     uint32_t phase = 0;
     bool ok = true;
@@ -632,10 +587,10 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_grad_kernel(const __grid
         for (int i = 0; i < 4; ++i) {
           x[e + i] = exp2_fast(fmaf(x[e + i], c, shifts[i]));
           y[e + i] = x[e + i] * (y[e + i] - deltas[i]);
-          if (std::is_same<T, __half>::value) y[e + i] *= hold;
+          if (kTwo) y[e + i] *= hold;
         }
       }
-      const int t = block_first(k);
+      const int t = w.first(k);
       if (DKV) {
         // query t + e: not before key `at`, before the end, in the key's window or the key one of the first tokens
         if (t < w.row0 + 127 || t + kBlock > n || (t + kBlock > w.row0 + p.window && w.row0 + 127 >= p.sinks)) {
@@ -646,8 +601,8 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_grad_kernel(const __grid
             y[e] = e >= from && e < to ? y[e] : 0.f;
           }
         }
-      } else if (k < keys.nfirst) {
-        const int here = keys.first - t;
+      } else if (k < w.keys.nfirst) {
+        const int here = w.keys.first - t;
         if (here < kBlock)
 #pragma unroll
           for (int e = 0; e < kBlock; ++e) y[e] = e < here ? y[e] : 0.f;
@@ -665,6 +620,14 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_grad_kernel(const __grid
 #pragma unroll
       for (int e = 0; e < kBlock; e += 2) word[e / 2] = pack2<T>(y[e], y[e + 1]);
       tmem_store32(cells + 64, word);
+      if (kTwo) {
+#pragma unroll
+        for (int e = 0; e < kBlock; e += 2) {
+          const float2 hi = __half22float2(reinterpret_cast<const __half2&>(word[e / 2]));
+          word[e / 2] = pack2<T>(y[e] - hi.x, y[e + 1] - hi.y);
+        }
+        tmem_store32(cells + 96, word);
+      }
       tmem_stored();
       tc_fence_before();
       __syncwarp();
@@ -675,11 +638,11 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_grad_kernel(const __grid
     // dq: the first group writes; dv and dk: a group each
     const bool exists = at < p.tokens, real = at < n;
     if (DKV || r == 0) {
-      T* to = head_row<T>(DKV ? (r ? p.dk : p.dv) : p.dq, b, exists ? at : 0, DKV ? g : (int)blockIdx.y);
+      T* to = head_row<T>(DKV ? (r ? p.dk : p.dv) : p.dq, b, exists ? at : 0, w.head);
       const float factor = !ok ? NAN : DKV && r == 0 ? 1.f : p.scale / hold;   // a wait that ran out shows in the result
       float* part = nullptr;
       if (DKV && w.piece >= 0)
-        part = p.part + (((((int64_t)b * p.kv_heads + g) * p.first_tiles + w.tile) * p.pieces + w.piece) * 2 + r) * 128 * D + row * D;
+        part = p.part + w.part_of(p, b, r, 128, D) + row * D;
       bool bad = false;
       if (count) {
 #pragma unroll
@@ -707,9 +670,9 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_grad_kernel(const __grid
       for (; again; again &= again - 1) {
         const int i = w.row0 + (warp & 3) * 32 + __ffs(again) - 1;
         if (DKV)
-          dkv_row<T>(p, b, g, i, n, r == 1, r == 0);
+          dkv_row<T>(p, b, w.head, i, n, r == 1, r == 0);
         else
-          dq_row<T>(p, b, blockIdx.y, i, n);
+          dq_row<T>(p, b, w.head, i, n);
       }
     }
   }
@@ -722,34 +685,6 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_grad_kernel(const __grid
     tc_fence_after();
     tmem_free<1>(tmem, 512);
   }
-}
-
-// dv and dk of the first tokens' tiles from their pieces: a warp a row.  grid: (tiles * 32, kv heads, sequences)
-template <typename T, int D>
-__global__ void __launch_bounds__(128) attn_join_kernel(const AttnArgs p) {
-  grid_trigger();
-  grid_wait();
-  const int j = blockIdx.x * 4 + (threadIdx.x >> 5), g = blockIdx.y, b = blockIdx.z, lane = threadIdx.x & 31, n = attn_length(p, b);
-  if (j >= p.tokens) return;
-  bool bad = false;
-#pragma unroll
-  for (int r = 0; r < 2; ++r) {
-    T* to = head_row<T>(r ? p.dk : p.dv, b, j, g);
-    const float* from = p.part + ((((int64_t)b * p.kv_heads + g) * p.first_tiles + j / 128) * p.pieces * 2 + r) * 128 * D + j % 128 * D;
-#pragma unroll
-    for (int col = 0; col < D; col += 32) {
-      const int d = col + lane;
-      float sum = 0.f;
-      if (j < n)
-        for (int k = 0; k < p.pieces; ++k) sum += from[(int64_t)k * 2 * 128 * D + d];
-      if (d < p.dim) {
-        bad |= !isfinite(sum);
-        to[d] = from_f32<T>(sum);
-      }
-    }
-  }
-  __syncwarp();
-  if (__any_sync(0xffffffffu, bad)) dkv_row<T>(p, b, g, j, n);
 }
 
 }  // namespace brace

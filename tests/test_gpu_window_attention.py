@@ -216,7 +216,12 @@ def test_what_is_hidden_has_no_effect(dtype, bad):
         plan.grad(dout, q, k, v, out, lse, *grads)
         return [out, lse.transpose(1, 2)[..., None], *grads]
 
-    fine = run()
+    # A row that a hidden place spoils is computed again in another order: both ways are within the bounds that are derived
+    # above, of the exact value, and so is what is compared here (not the two ways with one another).
+    fine = Plain(q[0], k[0], v[0], w, sinks, float(torch.tensor(plan.scale, dtype=F32)), dout[0])
+    fine = [(fine.out, fine.out_bound), (fine.lse[..., None], fine.lse_bound[..., None]), (fine.dq, fine.dq_bound),
+            (fine.dk, fine.dk_bound), (fine.dv, fine.dv_bound)]
+    fine = [[t.transpose(0, 1) for t in pair] for pair in fine]
     sees_it = sees(n, w, sinks)[:, at]
     # rows of k and v that a query reads that also reads `at`
     meets = (sees(n, w, sinks)[sees_it].any(0))
@@ -226,8 +231,8 @@ def test_what_is_hidden_has_no_effect(dtype, bad):
         got = run()
         t[0, at, 0, 5] = keep
         rows = [~sees_it, ~sees_it, ~sees_it, ~meets, ~meets]
-        for x, y, r in zip(fine, got, rows):
-            within(y[0, r], x[0, r].double(), 4 * U[dtype] * x[0, r].double().abs().amax())
+        for (x, bound), y, r in zip(fine, got, rows):
+            within(y[0, r], x[r], bound[r])
         assert not bool(got[0][0, sees_it][..., 5].isfinite().any()) if t is v else True
     keep = dout[0, at, 1, 7].clone()
     dout[0, at, 1, 7] = bad
@@ -235,8 +240,8 @@ def test_what_is_hidden_has_no_effect(dtype, bad):
     dout[0, at, 1, 7] = keep
     mine = sees(n, w, sinks)[at]
     this = torch.arange(n, device="cuda") == at
-    for x, y, r in zip(fine, got, [this & ~this | True, this | True, ~this, ~mine, ~mine]):
-        within(y[0, r], x[0, r].double(), 4 * U[dtype] * x[0, r].double().abs().amax())
+    for (x, bound), y, r in zip(fine, got, [this | True, this | True, ~this, ~mine, ~mine]):
+        within(y[0, r], x[r], bound[r])
     assert not bool(got[4][0, mine][..., 7].isfinite().any())
 
 
