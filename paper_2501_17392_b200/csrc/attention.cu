@@ -130,15 +130,14 @@ bool encode_map(CUtensorMap* map, const brace_heads& x, const brace_window_atten
              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <typename T, int D, bool SHARED>
+template <typename T, int D>
 cudaError_t launch_forward(const AttnMaps& maps, const AttnArgs& a, cudaStream_t st) {
   static std::atomic<uint64_t> granted{0};
-  auto* kernel = attn_forward_kernel<T, D, SHARED>;
+  auto* kernel = attn_forward_kernel<T, D>;
   const cudaError_t err = grant_smem((const void*)kernel, granted, AttnShape<D>::kSmem);
   if (err != cudaSuccess) return err;
-  const int rows = SHARED ? 128 : 256;
-  const dim3 grid((unsigned)((a.tokens + rows - 1) / rows), (unsigned)(SHARED ? a.heads / 2 : a.heads), (unsigned)a.batch);
-  return launch(kernel, grid, kAttnThreads, AttnShape<D>::kSmem, 1, st, maps, a);
+  const dim3 grid((unsigned)((a.tokens + 127) / 128), (unsigned)a.heads, (unsigned)a.batch);
+  return launch(kernel, grid, AttnShape<D>::kThreads, AttnShape<D>::kSmem, 1, st, maps, a);
 }
 
 template <typename T, int D, bool DKV>
@@ -210,11 +209,9 @@ int brace_window_attention_forward(const brace_window_attention* e, brace_stream
     if (!encode_map(&maps.q, e->q, e, e->heads, 128) || !encode_map(&maps.k, e->k, e, e->kv_heads, 128) ||
         !encode_map(&maps.v, e->v, e, e->kv_heads, 128))
       return cuda_fail_no_ctx(cudaErrorNotSupported);
-    const bool shared = a.share % 2 == 0;
     const cudaError_t err = with_half_type(e->type, [&](auto t) {
       using T = decltype(t);
-      if (e->dim <= 64) return shared ? launch_forward<T, 64, true>(maps, a, st) : launch_forward<T, 64, false>(maps, a, st);
-      return shared ? launch_forward<T, 128, true>(maps, a, st) : launch_forward<T, 128, false>(maps, a, st);
+      return e->dim <= 64 ? launch_forward<T, 64>(maps, a, st) : launch_forward<T, 128>(maps, a, st);
     });
     return err == cudaSuccess ? BRACE_OK : cuda_fail_no_ctx(err);
   }
