@@ -68,6 +68,9 @@ __device__ __forceinline__ float exp2_fast(float x) {
   return r;
 }
 
+// The lowest n bits set.
+__device__ __forceinline__ uint32_t low_bits(int n) { return n >= 32 ? ~0u : (1u << max(n, 0)) - 1u; }
+
 // ROWS rows of a head from token `t` on: D / 64 boxes of 64 columns.
 template <int D, int ROWS>
 __device__ __forceinline__ void load_rows(uint32_t dst, const CUtensorMap* map, int t, int head, int b, uint32_t bar) {
@@ -138,6 +141,8 @@ __global__ void __launch_bounds__(AttnShape<D>::kThreads, 2) attn_forward_kernel
   const int b = blockIdx.z, h = blockIdx.y, g = h / p.share, n = attn_length(p, b), q0 = 128 * (int)(gridDim.x - 1 - blockIdx.x);
   const KeyBlocks blocks(p, q0, min(n, q0 + 128), KEYS);
   const int count = q0 < n ? blocks.count : 0;
+  // a few first tokens: the rest of their block is left out
+  auto narrow = [&](int k) { return k < blocks.nfirst && blocks.first - k * KEYS <= 32; };
 
   if (warp == 4) {                         // loads: keys and values in the order in which the products take them
     const bool lead = elect_one();
@@ -207,7 +212,8 @@ __global__ void __launch_bounds__(AttnShape<D>::kThreads, 2) attn_forward_kernel
         const uint64_t db = ring_desc + (uint64_t)(s * Shape::kTile >> 4);
 #pragma unroll
         for (int i = 0; i < KEYS / 16; ++i)
-          mma_f16_ts(tmem + Shape::kResult, tmem + Shape::kP + 8 * i, db + i * (2048 >> 4), kValues, k > 0 || i > 0);
+          if (i < 2 || !narrow(k))
+            mma_f16_ts(tmem + Shape::kResult, tmem + Shape::kP + 8 * i, db + i * (2048 >> 4), kValues, k > 0 || i > 0);
         mma_commit<1>(p_done);
         mma_commit<1>(empty + 8 * s);
       }
@@ -221,16 +227,17 @@ __global__ void __launch_bounds__(AttnShape<D>::kThreads, 2) attn_forward_kernel
     const float c = fmaxf(fabsf(p.scale) * kLog2e, 1e-30f);
     const bool negative = p.scale < 0.f;
     float top = -INFINITY, total = 0.f;
-    bool ok = true;
-    for (int k = 0; k < count; ++k) {
-      if (!mbar_wait(s_full, (uint32_t)k & 1u, dead)) {
-        ok = false;
-        break;
+    // One block of which COLS columns are looked at; MASKED: those that are seen, in `seen`.
+    auto block = [&](auto cols, auto masked, int k, const uint32_t* seen) {
+      constexpr int COLS = decltype(cols)::value;
+      constexpr bool MASKED = decltype(masked)::value;
+      float s[COLS];
+      if constexpr (COLS == 32) {
+        tmem_fetch32(mine, s);
+      } else {
+        tmem_fetch64(mine, s);
+        tmem_fetch64(mine + 64, s + 64);
       }
-      tc_fence_after();
-      float s[KEYS];
-      tmem_fetch64(mine, s);
-      tmem_fetch64(mine + 64, s + 64);
       tmem_loaded();
       tmem_use(s);
       if (Shape::kApart) {
@@ -240,21 +247,13 @@ __global__ void __launch_bounds__(AttnShape<D>::kThreads, 2) attn_forward_kernel
       }
       if (negative)
 #pragma unroll
-        for (int e = 0; e < KEYS; ++e) s[e] = -s[e];
-      const int j = blocks.key(k, KEYS);
-      if (k < blocks.nfirst) {             // first tokens before the window: all queries see them
-        const int here = blocks.first - j;
-        if (here < KEYS)
+        for (int e = 0; e < COLS; ++e) s[e] = -s[e];
+      if (MASKED)
 #pragma unroll
-          for (int e = 0; e < KEYS; ++e) s[e] = e < here ? s[e] : -INFINITY;
-      } else if (j + KEYS - 1 > q0 || j <= q0 + 127 - p.window) {
-        const int last = i - j, early = i - p.window - j, first = p.sinks - j;   // e <= last, and e > early or e < first
+        for (int e = 0; e < COLS; ++e) s[e] = seen[e / 32] >> (e % 32) & 1u ? s[e] : -INFINITY;
+      float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-        for (int e = 0; e < KEYS; ++e) s[e] = e <= last && (e > early || e < first) ? s[e] : -INFINITY;
-      }
-      float m[4] = {s[0], s[1], s[2], s[3]};
-#pragma unroll
-      for (int e = 4; e < KEYS; ++e) m[e & 3] = fmaxf(m[e & 3], s[e]);
+      for (int e = 0; e < COLS; e += 2) m[e / 2 & 3] = fmaxf(m[e / 2 & 3], fmaxf(s[e], s[e + 1]));
       const float most = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
       if (top == -INFINITY) top = most;    // nothing summed yet
       const bool grown = (most - top) * c > kGrown, rescale = __any_sync(0xffffffffu, grown);
@@ -263,23 +262,22 @@ __global__ void __launch_bounds__(AttnShape<D>::kThreads, 2) attn_forward_kernel
         keep = exp2_fast((top - most) * c);
         top = most;
       }
-      total *= keep;
       const float shift = top == -INFINITY ? 0.f : -top * c;
-      float part[4] = {0.f, 0.f, 0.f, 0.f};
-      uint32_t w[KEYS / 2];
+      const uint64_t cc = pack_f32x2(c, c), shifts = pack_f32x2(shift, shift);
+      uint64_t part[4] = {0, 0, 0, 0};
+      uint32_t w[COLS / 2];
 #pragma unroll
-      for (int e = 0; e < KEYS; e += 2) {
-        const float x = exp2_fast(fmaf(s[e], c, shift)), y = exp2_fast(fmaf(s[e + 1], c, shift));
-        part[(e >> 1) & 3] += x + y;
-        w[e >> 1] = pack2<T>(x, y);
+      for (int e = 0; e < COLS; e += 2) {
+        float2 x = unpack_f32x2(fma_f32x2(pack_f32x2(s[e], s[e + 1]), cc, shifts));
+        x = make_float2(exp2_fast(x.x), exp2_fast(x.y));
+        part[e / 2 & 3] = add_f32x2(part[e / 2 & 3], pack_f32x2(x.x, x.y));
+        w[e / 2] = pack2<T>(x.x, x.y);
       }
-      total += (part[0] + part[1]) + (part[2] + part[3]);
+      const float2 sum = unpack_f32x2(add_f32x2(add_f32x2(part[0], part[1]), add_f32x2(part[2], part[3])));
+      total = fmaf(total, keep, sum.x + sum.y);
       // the product with the block before has read its P and is part of the result (with P in the scores' place it was
       // issued before these scores)
-      if (Shape::kApart && k && !mbar_wait(p_done, (uint32_t)(k - 1) & 1u, dead)) {
-        ok = false;
-        break;
-      }
+      if (Shape::kApart && k && !mbar_wait(p_done, (uint32_t)(k - 1) & 1u, dead)) return false;
       tc_fence_after();
       if (rescale && k) {
 #pragma unroll
@@ -293,12 +291,42 @@ __global__ void __launch_bounds__(AttnShape<D>::kThreads, 2) attn_forward_kernel
           tmem_store32(result + x, reinterpret_cast<const uint32_t*>(o));
         }
       }
-      tmem_store32(weights, w);
-      tmem_store32(weights + 32, w + 32);
+      if constexpr (COLS == 32) {
+        tmem_store16(weights, w);
+      } else {
+        tmem_store32(weights, w);
+        tmem_store32(weights + 32, w + 32);
+      }
       tmem_stored();
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(p_full);
+      return true;
+    };
+    using std::integral_constant;
+    using std::false_type;
+    using std::true_type;
+    bool ok = true;
+    for (int k = 0; ok && k < count; ++k) {
+      if (!mbar_wait(s_full, (uint32_t)k & 1u, dead)) {
+        ok = false;
+        break;
+      }
+      tc_fence_after();
+      const int j = blocks.key(k, KEYS);
+      const bool first = k < blocks.nfirst;
+      if (first || j + KEYS - 1 > q0 || j <= q0 + 127 - p.window) {
+        // first tokens before the window: all queries see them; else key j + e is not behind query i, and is in its window or
+        // one of the first tokens
+        uint32_t seen[KEYS / 32];
+#pragma unroll
+        for (int x = 0; x < KEYS; x += 32)
+          seen[x / 32] = first ? low_bits(blocks.first - j - x)
+                               : low_bits(i - j + 1 - x) & (~low_bits(i - p.window + 1 - j - x) | low_bits(p.sinks - j - x));
+        ok = narrow(k) ? block(integral_constant<int, 32>{}, true_type{}, k, seen) : block(integral_constant<int, KEYS>{}, true_type{}, k, seen);
+      } else {
+        ok = block(integral_constant<int, KEYS>{}, false_type{}, k, nullptr);
+      }
     }
     if (ok && count) ok = mbar_wait(p_done, (uint32_t)(count - 1) & 1u, dead);
     tc_fence_after();
