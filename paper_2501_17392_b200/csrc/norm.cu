@@ -29,23 +29,36 @@ int pow2_ceil(int64_t x) {
 struct NormShape {
   int v, nv, group, block, slots;
 };
-NormShape norm_shape(int dim, bool wide) {
+NormShape norm_shape(int dim, int v, int most) {
   NormShape s;
-  s.v = wide ? 8 : 1;
-  const int n = (dim + s.v - 1) / s.v, most = wide ? 4 : 32;
+  s.v = v;
+  const int n = (dim + v - 1) / v;
   s.group = std::max(std::min(32, pow2_ceil(n)), pow2_ceil((n + most - 1) / most));
   s.nv = (n + s.group - 1) / s.group;
   s.block = s.group > 32 ? s.group : kNormThreads;
   s.slots = s.block / s.group;
   return s;
 }
+// Through a ring: pieces of 16 bytes of x, so that a warp's reads of shared memory do not meet in a bank; 8 columns without,
+// or one where rows are not aligned.
+constexpr int kRingFrom = 256;   // columns: shorter rows are not worth a copy of their own
+NormShape norm_shape(int dim, int x_type, bool wide) {
+  if (!wide) return norm_shape(dim, 1, 32);
+  if (dim < kRingFrom) return norm_shape(dim, 8, 4);
+  return x_type == BRACE_TYPE_F32 ? norm_shape(dim, 4, 8) : norm_shape(dim, 8, 4);
+}
 
-constexpr int kNormForwardCtas = 148 * 4, kNormGradCtas = 148 * 3;
+constexpr int kSms = 148, kRingResident = 2, kMostResident = 16;   // CTAs of an SM: of 256 threads with rings; of any kind
+
+// CTAs of an SM; narrow ones make room for more.
+int resident_of(const NormShape& s, bool ring) {
+  return (ring ? kRingResident : norm_resident(s.v * s.nv)) * (kNormThreads / s.block);
+}
 
 // CTAs of a client's gradient.  More rows never give fewer.
-int64_t norm_parts(int32_t clients, int64_t rows, int32_t dim, int slots) {
+int64_t norm_parts(int32_t clients, int64_t rows, int32_t dim, int slots, int resident) {
   int64_t n = dim > kNormShort ? (rows + 31) / 32 : (rows + 4 * slots - 1) / (4 * slots);
-  int64_t most = dim > kNormShort ? (int64_t)kNormGradCtas * kNormThreads / dim : kNormGradCtas;
+  int64_t most = dim > kNormShort ? (int64_t)kSms * 4 * kNormThreads / dim : kSms * resident;
   most /= std::max(clients, 1);
   n = std::min(n, std::max<int64_t>(most, 1));
   return std::max<int64_t>(n, 1);
@@ -90,21 +103,36 @@ NormArgs norm_args(const brace_layer_norm* e) {
   return a;
 }
 
-// Calls f with the pieces a thread holds; scalars in three sizes.
+// Calls f with the pieces a thread holds without a ring: one of 8 columns, scalars in three sizes.
 template <typename F>
 cudaError_t with_pieces(const NormShape& s, F&& f) {
   using std::integral_constant;
-  if (s.v == 8) {
-    constexpr integral_constant<int, 8> v;
-    if (s.nv <= 1) return f(v, integral_constant<int, 1>{});
-    if (s.nv <= 2) return f(v, integral_constant<int, 2>{});
-    if (s.nv <= 3) return f(v, integral_constant<int, 3>{});
-    return f(v, integral_constant<int, 4>{});
-  }
+  if (s.v == 8) return f(integral_constant<int, 8>{}, integral_constant<int, 1>{});
   constexpr integral_constant<int, 1> v;
   if (s.nv <= 4) return f(v, integral_constant<int, 4>{});
   if (s.nv <= 12) return f(v, integral_constant<int, 12>{});
   return f(v, integral_constant<int, 32>{});
+}
+// And with one.
+template <typename TX, typename F>
+cudaError_t with_ring(const NormShape& s, F&& f) {
+  using std::integral_constant;
+  constexpr int V = 16 / (int)sizeof(TX), K = 8 / V;      // K pieces hold 8 columns
+  constexpr integral_constant<int, V> v;
+  const int n = (s.nv + K - 1) / K;
+  if (n <= 1) return f(v, integral_constant<int, K>{});
+  if (n <= 2) return f(v, integral_constant<int, 2 * K>{});
+  if (n <= 3) return f(v, integral_constant<int, 3 * K>{});
+  return f(v, integral_constant<int, 4 * K>{});
+}
+template <typename K>
+cudaError_t launch_ring(K* kernel, std::atomic<uint64_t>& granted, const NormShape& s, dim3 grid, int row_bytes, NormArgs a, cudaStream_t st) {
+  constexpr int kMost = kRingBytes + 1024;
+  const cudaError_t err = grant_smem((const void*)kernel, granted, kMost);
+  if (err != cudaSuccess) return err;
+  a.row_bytes = row_bytes;
+  a.stages = std::max(1, std::min(kRingMost, kRingBytes / (kNormThreads / s.block) / (s.slots * row_bytes)));
+  return launch(kernel, grid, s.block, 1024 + s.slots * a.stages * row_bytes, 1, st, a);
 }
 
 }  // namespace
@@ -124,16 +152,24 @@ int brace_layer_norm_forward(const brace_layer_norm* e, brace_stream_t stream) {
   const cudaStream_t st = (cudaStream_t)stream;
   const bool wide = e->dim % 8 == 0 && wide_rows(e->d_x, e->x_type, e->ld_x, e->stride_x) &&
                     wide_rows(e->d_y, e->y_type, e->ld_y, e->stride_y);
-  const NormShape s = norm_shape(e->dim, wide);
+  const NormShape s = norm_shape(e->dim, e->x_type, wide);
+  const bool ring = wide && e->dim >= kRingFrom;
+  const int resident = e->dim > kNormShort ? 4 : resident_of(s, ring);
   a.group = s.group;
   const int64_t slots = e->dim > kNormShort ? 1 : s.slots;
-  const int64_t ctas = std::min((e->rows + slots - 1) / slots, std::max<int64_t>(1, kNormForwardCtas / e->clients));
+  const int64_t ctas = std::min((e->rows + slots - 1) / slots, std::max<int64_t>(1, kSms * resident / e->clients));
   const dim3 grid((unsigned)ctas, (unsigned)e->clients);
   const cudaError_t err = with_type(e->x_type, [&](auto tx) {
     return with_type(e->y_type, [&](auto ty) {
       using TX = decltype(tx);
       using TY = decltype(ty);
       if (e->dim > kNormShort) return launch(norm_forward_long_kernel<TX, TY>, grid, kNormThreads, 0, 1, st, a);
+      if (ring)
+        return with_ring<TX>(s, [&](auto v, auto nv) {
+          static std::atomic<uint64_t> granted{0};
+          return launch_ring(norm_forward_ring_kernel<TX, TY, decltype(v)::value, decltype(nv)::value>, granted, s, grid,
+                             e->dim * (int)sizeof(TX), a, st);
+        });
       return with_pieces(s, [&](auto v, auto nv) {
         return launch(norm_forward_kernel<TX, TY, decltype(v)::value, decltype(nv)::value>, grid, s.block, 0, 1, st, a);
       });
@@ -144,8 +180,8 @@ int brace_layer_norm_forward(const brace_layer_norm* e, brace_stream_t stream) {
 
 size_t brace_layer_norm_workspace_bytes(int32_t clients, int64_t rows, int32_t dim) {
   if (!norm_sizes_ok(clients, rows, dim) || dim > kNormMostColumns) return 0;
-  const int slots = std::min(norm_shape(dim, false).slots, norm_shape((dim + 7) / 8 * 8, true).slots);
-  return (size_t)round_up(std::max<int64_t>(norm_parts(clients, rows, dim, slots) * clients * 2 * dim * 4, 256), 256);
+  const int slots = std::min(norm_shape(dim, BRACE_TYPE_F32, false).slots, norm_shape(dim, BRACE_TYPE_F32, true).slots);
+  return (size_t)round_up(std::max<int64_t>(norm_parts(clients, rows, dim, slots, kMostResident) * clients * 2 * dim * 4, 256), 256);
 }
 
 int brace_layer_norm_grad(const brace_layer_norm* e, void* d_workspace, size_t workspace_bytes, brace_stream_t stream) {
@@ -177,20 +213,27 @@ int brace_layer_norm_grad(const brace_layer_norm* e, void* d_workspace, size_t w
   const cudaStream_t st = (cudaStream_t)stream;
   const bool wide = e->dim % 8 == 0 && wide_rows(e->d_x, e->x_type, e->ld_x, e->stride_x) &&
                     wide_rows(e->d_y, e->y_type, e->ld_y, e->stride_y) && wide_rows(e->d_dx, e->x_type, e->ld_dx, e->stride_dx);
-  const NormShape s = norm_shape(e->dim, wide);
+  const NormShape s = norm_shape(e->dim, e->x_type, wide);
+  const bool ring = wide && e->dim >= kRingFrom;
   const bool is_long = e->dim > kNormShort;
   a.group = s.group;
-  a.parts = (int)norm_parts(e->clients, e->rows, e->dim, s.slots);
+  a.parts = (int)norm_parts(e->clients, e->rows, e->dim, s.slots, resident_of(s, ring));
   cudaError_t err = with_type(e->x_type, [&](auto tx) {
     return with_type(e->y_type, [&](auto ty) {
       using TX = decltype(tx);
       using TY = decltype(ty);
+      if (!is_long && ring)
+        return with_ring<TX>(s, [&](auto v, auto nv) {
+          static std::atomic<uint64_t> granted{0};
+          return launch_ring(norm_grad_ring_kernel<TX, TY, decltype(v)::value, decltype(nv)::value>, granted, s,
+                             dim3((unsigned)a.parts, (unsigned)e->clients), e->dim * (int)(sizeof(TX) + sizeof(TY)), a, st);
+        });
       if (!is_long)
         return with_pieces(s, [&](auto v, auto nv) {
           return launch(norm_grad_kernel<TX, TY, decltype(v)::value, decltype(nv)::value>,
                         dim3((unsigned)a.parts, (unsigned)e->clients), s.block, 0, 1, st, a);
         });
-      const int64_t ctas = std::min(std::max<int64_t>(e->rows, 1), std::max<int64_t>(1, kNormForwardCtas / e->clients));
+      const int64_t ctas = std::min(std::max<int64_t>(e->rows, 1), std::max<int64_t>(1, kSms * 4 / e->clients));
       const cudaError_t first = launch(norm_grad_long_kernel<TX, TY>, dim3((unsigned)ctas, (unsigned)e->clients), kNormThreads, 0, 1, st, a);
       if (first != cudaSuccess || !params) return first;
       return launch(norm_columns_kernel<TX, TY>,

@@ -6,6 +6,8 @@
 // variance is summed from differences, in a second pass that reads nothing), a thread always has the same columns, keeps
 // their weights in registers for all of its rows and, backward, the sums of their gradients; the CTAs' sums are joined by
 // a second launch, in one order.  Sums are float32.
+// Rows of 256 columns or more that start on 16-byte boundaries come through shared memory: each group has a ring of rows
+// that bulk copies fill ahead, so that what is under way does not depend on the registers.  Others are loaded by the threads.
 #pragma once
 
 #include "elements.cuh"
@@ -14,7 +16,12 @@
 namespace brace {
 
 constexpr int kNormThreads = 256;
+constexpr int kRingBytes = 96 * 1024;   // of a CTA's rings, two CTAs an SM
+constexpr int kRingMost = 8;            // rows of a ring
 constexpr int kNormShort = 8192;     // longest row that a CTA's registers hold, its weights and its gradients' sums beside it
+
+// CTAs of an SM that hold so many columns a thread in their registers.
+__host__ __device__ constexpr int norm_resident(int columns) { return columns > 12 ? 1 : columns > 8 ? 2 : 4; }
 
 struct NormArgs {
   const void *x, *weight, *bias;
@@ -25,6 +32,7 @@ struct NormArgs {
   int64_t ld_x, stride_x, stride_weight, stride_bias, ld_y, stride_y, stride_stats, ld_dx, stride_dx, stride_dweight, stride_dbias;
   int64_t rows;
   int dim, weight_type, grad_type, group, parts, accumulate;
+  int stages, row_bytes;             // of a ring
   float eps;
 };
 
@@ -65,7 +73,7 @@ __device__ __forceinline__ void group_sum(float (&v)[N], int group, float (*cell
 
 // Forward.  Thread g of a row's G has the NV groups of V columns (i G + g) V .. + V.
 template <typename TX, typename TY, int V, int NV>
-__global__ void __launch_bounds__(kNormThreads, NV * V > 24 ? 2 : NV * V > 12 ? 3 : 4) norm_forward_kernel(const NormArgs p) {
+__global__ void __launch_bounds__(kNormThreads, norm_resident(NV * V)) norm_forward_kernel(const NormArgs p) {
   __shared__ float cell[2][kNormThreads / 32][2];
   grid_trigger();
   grid_wait();
@@ -131,9 +139,59 @@ __global__ void __launch_bounds__(kNormThreads, NV * V > 24 ? 2 : NV * V > 12 ? 
   }
 }
 
+// This CTA's sums of dweight and dbias: to its part, or to the gradients where it is a client's only CTA.
+template <int V, int NV>
+__device__ __forceinline__ void norm_put_sums(const NormArgs& p, float (&dw)[NV * V], float (&db)[NV * V], float (*sums)[1024]) {
+  const int G = p.group, g = threadIdx.x % G;
+  const int64_t c = blockIdx.y;
+  // rows of one warp first, then the warps one after the other
+  for (int o = G; o < 32; o <<= 1)
+#pragma unroll
+    for (int i = 0; i < NV * V; ++i) {
+      dw[i] += __shfl_xor_sync(0xffffffffu, dw[i], o);
+      db[i] += __shfl_xor_sync(0xffffffffu, db[i], o);
+    }
+  const int warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+  if (G <= 32 && warps > 1) {
+    for (int t = 0; t < warps; ++t) {
+      if (warp == t && (threadIdx.x & 31) < G) {
+#pragma unroll
+        for (int i = 0; i < NV * V; ++i) {
+          const int col = (i / V * G + g) * V + i % V;
+          if (col < p.dim) {
+            if (t > 0) {
+              dw[i] += sums[0][col];
+              db[i] += sums[1][col];
+            }
+            sums[0][col] = dw[i];
+            sums[1][col] = db[i];
+          }
+        }
+      }
+      __syncthreads();
+    }
+    if (warp != warps - 1) return;
+  }
+  if ((threadIdx.x & 31) >= G) return;
+#pragma unroll
+  for (int i = 0; i < NV * V; ++i) {
+    const int col = (i / V * G + g) * V + i % V;
+    if (col >= p.dim) continue;
+    if (p.parts > 1) {
+      float* to = p.part + (c * p.parts + blockIdx.x) * 2 * (int64_t)p.dim + col;
+      to[0] = dw[i];
+      to[p.dim] = db[i];
+    } else {
+      const int64_t at_w = c * p.stride_dweight + col, at_b = c * p.stride_dbias + col;
+      if (p.dweight) store_any(p.dweight, p.grad_type, at_w, p.accumulate ? load_any(p.dweight, p.grad_type, at_w) + dw[i] : dw[i]);
+      if (p.dbias) store_any(p.dbias, p.grad_type, at_b, p.accumulate ? load_any(p.dbias, p.grad_type, at_b) + db[i] : db[i]);
+    }
+  }
+}
+
 // Backward: dx, and this CTA's part of dweight and dbias (the whole of it where there is one CTA for a client).
 template <typename TX, typename TY, int V, int NV>
-__global__ void __launch_bounds__(kNormThreads, NV * V > 24 ? 1 : NV * V > 12 ? 2 : 3) norm_grad_kernel(const NormArgs p) {
+__global__ void __launch_bounds__(kNormThreads, norm_resident(NV * V)) norm_grad_kernel(const NormArgs p) {
   __shared__ float cell[2][kNormThreads / 32][2];
   __shared__ float sums[2][1024];    // rows of a warp or less have at most 1024 columns
   grid_trigger();
@@ -198,50 +256,217 @@ __global__ void __launch_bounds__(kNormThreads, NV * V > 24 ? 1 : NV * V > 12 ? 
       o.store_plain(dx + row * p.ld_dx + col);
     }
   }
-  if (!params) return;
-  // rows of one warp first, then the warps one after the other
-  for (int o = G; o < 32; o <<= 1)
+  if (params) norm_put_sums<V, NV>(p, dw, db, sums);
+}
+
+// ---- rows through shared memory.  A group is a warp, or the whole CTA.
+
+struct Ring {
+  uint32_t rows, bars;      // addresses in shared memory
+  int stages, bytes;        // of the ring, of a row (of both tensors, backward)
+  volatile int* dead;
+};
+
+// The CTA's shared memory: the groups' barriers, then their rings.
+__device__ __forceinline__ Ring ring_of_group(const NormArgs& p, uint8_t* smem, int* dead) {
+  const int G = p.group, slot = threadIdx.x / G;
+  Ring r;
+  r.stages = p.stages;
+  r.bytes = p.row_bytes;
+  r.bars = smem_addr(smem) + slot * kRingMost * 8;
+  r.rows = smem_addr(smem) + 1024 + slot * p.stages * p.row_bytes;
+  r.dead = dead;
+  if (threadIdx.x == 0) *dead = 0;
+  if (threadIdx.x % G == 0)
+    for (int s = 0; s < p.stages; ++s) mbar_init(r.bars + 8 * s, 1);
+  if (threadIdx.x % G == 0) mbar_init_visible();
+  __syncthreads();
+  return r;
+}
+__device__ __forceinline__ void group_barrier(int G) {
+  if (G > 32)
+    __syncthreads();
+  else
+    __syncwarp();
+}
+
+// V columns of a row in shared memory.
+template <typename T, int V>
+__device__ __forceinline__ void ring_piece(Pack<T, V>& x, uint32_t addr) {
+  using W = typename Pack<T, V>::W;
 #pragma unroll
-    for (int i = 0; i < NV * V; ++i) {
-      dw[i] += __shfl_xor_sync(0xffffffffu, dw[i], o);
-      db[i] += __shfl_xor_sync(0xffffffffu, db[i], o);
-    }
-  const int warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-  if (G <= 32 && warps > 1) {
-    for (int t = 0; t < warps; ++t) {
-      if (warp == t && (threadIdx.x & 31) < G) {
-#pragma unroll
-        for (int i = 0; i < NV * V; ++i) {
-          const int col = (i / V * G + g) * V + i % V;
-          if (col < p.dim) {
-            if (t > 0) {
-              dw[i] += sums[0][col];
-              db[i] += sums[1][col];
-            }
-            sums[0][col] = dw[i];
-            sums[1][col] = db[i];
-          }
-        }
-      }
-      __syncthreads();
-    }
-    if (warp != warps - 1) return;
+  for (int i = 0; i < Pack<T, V>::kWords; ++i) {
+    if constexpr (sizeof(W) == 16)
+      asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                   : "=r"(reinterpret_cast<uint4*>(x.t)[i].x), "=r"(reinterpret_cast<uint4*>(x.t)[i].y),
+                     "=r"(reinterpret_cast<uint4*>(x.t)[i].z), "=r"(reinterpret_cast<uint4*>(x.t)[i].w)
+                   : "r"(addr + 16 * i));
+    else
+      asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];"
+                   : "=r"(reinterpret_cast<uint2*>(x.t)[i].x), "=r"(reinterpret_cast<uint2*>(x.t)[i].y)
+                   : "r"(addr + 8 * i));
   }
-  if ((threadIdx.x & 31) >= G) return;
+}
+
+template <typename TX, typename TY, int V, int NV>
+__global__ void __launch_bounds__(kNormThreads, 2) norm_forward_ring_kernel(const NormArgs p) {
+  extern __shared__ __align__(1024) uint8_t smem[];
+  __shared__ float cell[2][kNormThreads / 32][2];
+  __shared__ int dead;
+  const Ring ring = ring_of_group(p, smem, &dead);
+  grid_trigger();
+  grid_wait();
+  const int G = p.group, slot = threadIdx.x / G, g = threadIdx.x % G, slots = blockDim.x / G;
+  const int64_t c = blockIdx.y, step = (int64_t)gridDim.x * slots, first = (int64_t)blockIdx.x * slots + slot;
+  const float inv = 1.f / (float)p.dim;
+  const TX* x = static_cast<const TX*>(p.x) + c * p.stride_x;
+  TY* y = static_cast<TY*>(p.y) + c * p.stride_y;
+  auto fetch = [&](int64_t row, int s) {
+    mbar_expect_tx(ring.bars + 8 * s, ring.bytes);
+    bulk_load(ring.rows + s * ring.bytes, x + row * p.ld_x, ring.bytes, ring.bars + 8 * s);
+  };
+  if (g == 0) {
+    fence_async_global();
+    for (int s = 0; s < ring.stages; ++s)
+      if (first + s * step < p.rows) fetch(first + s * step, s);
+  }
+  float w[NV * V], b[NV * V];
 #pragma unroll
   for (int i = 0; i < NV * V; ++i) {
     const int col = (i / V * G + g) * V + i % V;
-    if (col >= p.dim) continue;
-    if (p.parts > 1) {
-      float* to = p.part + (c * p.parts + blockIdx.x) * 2 * (int64_t)p.dim + col;
-      to[0] = dw[i];
-      to[p.dim] = db[i];
-    } else {
-      const int64_t at_w = c * p.stride_dweight + col, at_b = c * p.stride_dbias + col;
-      if (p.dweight) store_any(p.dweight, p.grad_type, at_w, p.accumulate ? load_any(p.dweight, p.grad_type, at_w) + dw[i] : dw[i]);
-      if (p.dbias) store_any(p.dbias, p.grad_type, at_b, p.accumulate ? load_any(p.dbias, p.grad_type, at_b) + db[i] : db[i]);
+    w[i] = p.weight && col < p.dim ? load_any(p.weight, p.weight_type, c * p.stride_weight + col) : 1.f;
+    b[i] = p.bias && col < p.dim ? load_any(p.bias, p.weight_type, c * p.stride_bias + col) : 0.f;
+  }
+  int turn = 0, s = 0;
+  uint32_t phase = 0;
+  for (int64_t row = first; row < p.rows; row += step) {
+    const bool ok = mbar_wait(ring.bars + 8 * s, phase, ring.dead);
+    float v[NV * V], sum[1] = {0.f};
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int col = (i * G + g) * V;
+      Pack<TX, V> raw;
+      if (col < p.dim) ring_piece(raw, ring.rows + s * ring.bytes + col * (int)sizeof(TX));
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        v[i * V + k] = col < p.dim ? to_f32(raw.t[k]) : 0.f;
+        sum[0] += v[i * V + k];
+      }
+    }
+    group_barrier(G);      // all have read the row
+    if (g == 0 && row + ring.stages * step < p.rows) fetch(row + ring.stages * step, s);
+    if (++s == ring.stages) {
+      s = 0;
+      phase ^= 1u;
+    }
+    group_sum(sum, G, cell, turn);
+    const float mean = ok ? sum[0] * inv : NAN;      // a wait that ran out shows in the result
+    sum[0] = 0.f;
+#pragma unroll
+    for (int i = 0; i < NV * V; ++i) {
+      v[i] -= mean;
+      if ((i / V * G + g) * V < p.dim) sum[0] = fmaf(v[i], v[i], sum[0]);
+    }
+    group_sum(sum, G, cell, turn);
+    const float rstd = 1.f / sqrtf(fmaf(sum[0], inv, p.eps));
+    if (g == 0) {
+      if (p.mean) p.mean[c * p.stride_stats + row] = mean;
+      if (p.rstd) p.rstd[c * p.stride_stats + row] = rstd;
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int col = (i * G + g) * V;
+      Pack<TY, V> o;
+#pragma unroll
+      for (int k = 0; k < V; ++k) o.t[k] = from_f32<TY>(fmaf(v[i * V + k] * rstd, w[i * V + k], b[i * V + k]));
+      if (col < p.dim) o.store_plain(y + row * p.ld_y + col);
     }
   }
+}
+
+template <typename TX, typename TY, int V, int NV>
+__global__ void __launch_bounds__(kNormThreads, 2) norm_grad_ring_kernel(const NormArgs p) {
+  extern __shared__ __align__(1024) uint8_t smem[];
+  __shared__ float cell[2][kNormThreads / 32][2];
+  __shared__ float sums[2][1024];
+  __shared__ int dead;
+  const Ring ring = ring_of_group(p, smem, &dead);
+  grid_trigger();
+  grid_wait();
+  const int G = p.group, slot = threadIdx.x / G, g = threadIdx.x % G, slots = blockDim.x / G;
+  const int64_t c = blockIdx.y, step = (int64_t)gridDim.x * slots, first = (int64_t)blockIdx.x * slots + slot;
+  const float inv = 1.f / (float)p.dim;
+  const TX* x = static_cast<const TX*>(p.x) + c * p.stride_x;
+  const TY* dy = static_cast<const TY*>(p.y) + c * p.stride_y;
+  TX* dx = static_cast<TX*>(p.dx) + c * p.stride_dx;
+  const int x_bytes = p.dim * (int)sizeof(TX);
+  auto fetch = [&](int64_t row, int s) {
+    mbar_expect_tx(ring.bars + 8 * s, ring.bytes);
+    bulk_load(ring.rows + s * ring.bytes, x + row * p.ld_x, x_bytes, ring.bars + 8 * s);
+    bulk_load(ring.rows + s * ring.bytes + x_bytes, dy + row * p.ld_y, ring.bytes - x_bytes, ring.bars + 8 * s);
+  };
+  if (g == 0) {
+    fence_async_global();
+    for (int s = 0; s < ring.stages; ++s)
+      if (first + s * step < p.rows) fetch(first + s * step, s);
+  }
+  float w[NV * V], dw[NV * V], db[NV * V];
+#pragma unroll
+  for (int i = 0; i < NV * V; ++i) {
+    const int col = (i / V * G + g) * V + i % V;
+    w[i] = p.weight && col < p.dim ? load_any(p.weight, p.weight_type, c * p.stride_weight + col) : 1.f;
+    dw[i] = db[i] = 0.f;
+  }
+  int turn = 0, s = 0;
+  uint32_t phase = 0;
+  for (int64_t row = first; row < p.rows; row += step) {
+    const float mean = p.mean[c * p.stride_stats + row], rstd = p.rstd[c * p.stride_stats + row];
+    const float poison = mbar_wait(ring.bars + 8 * s, phase, ring.dead) ? 0.f : NAN;      // a wait that ran out shows in the result
+    const uint32_t at = ring.rows + s * ring.bytes;
+    float t[2] = {poison, 0.f};
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int col = (i * G + g) * V;
+      if (col >= p.dim) continue;
+      Pack<TX, V> xr;
+      Pack<TY, V> yr;
+      ring_piece(xr, at + col * (int)sizeof(TX));
+      ring_piece(yr, at + x_bytes + col * (int)sizeof(TY));
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        const int e = i * V + k;
+        const float xh = (to_f32(xr.t[k]) - mean) * rstd, d = to_f32(yr.t[k]), gr = d * w[e];
+        t[0] += gr;
+        t[1] = fmaf(gr, xh, t[1]);
+        dw[e] = fmaf(d, xh, dw[e]);
+        db[e] += d;
+      }
+    }
+    group_sum(t, G, cell, turn);
+    const float m1 = t[0] * inv, m2 = t[1] * inv;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {      // the row once more: it is still there
+      const int col = (i * G + g) * V;
+      if (col >= p.dim) continue;
+      Pack<TX, V> xr, o;
+      Pack<TY, V> yr;
+      ring_piece(xr, at + col * (int)sizeof(TX));
+      ring_piece(yr, at + x_bytes + col * (int)sizeof(TY));
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        const float xh = (to_f32(xr.t[k]) - mean) * rstd;
+        o.t[k] = from_f32<TX>(rstd * (fmaf(-xh, m2, to_f32(yr.t[k]) * w[i * V + k]) - m1));
+      }
+      o.store_plain(dx + row * p.ld_dx + col);
+    }
+    group_barrier(G);      // all have read the row
+    if (g == 0 && row + ring.stages * step < p.rows) fetch(row + ring.stages * step, s);
+    if (++s == ring.stages) {
+      s = 0;
+      phase ^= 1u;
+    }
+  }
+  if (p.dweight || p.dbias) norm_put_sums<V, NV>(p, dw, db, sums);
 }
 
 // dweight and dbias from the CTAs' parts: 32 columns a CTA, a warp takes every 8th part.
