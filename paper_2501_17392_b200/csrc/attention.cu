@@ -140,39 +140,34 @@ cudaError_t launch_forward(const AttnMaps& maps, const AttnArgs& a, cudaStream_t
   return launch(kernel, grid, AttnShape<D>::kThreads, AttnShape<D>::kSmem, 1, st, maps, a);
 }
 
-template <typename T, int D, bool DKV>
-cudaError_t launch_grad(const AttnMaps& maps, const AttnArgs& a, cudaStream_t st) {
-  static std::atomic<uint64_t> granted{0};
-  auto* kernel = attn_grad_kernel<T, D, DKV>;
-  constexpr int smem = AttnGradShape<D, DKV>::kSmem;
-  const cudaError_t err = grant_smem((const void*)kernel, granted, smem);
-  if (err != cudaSuccess) return err;
-  const int tiles = (int)(((int64_t)a.tokens + 127) / 128);
-  const dim3 grid((unsigned)(DKV ? a.first_tiles * a.pieces + tiles - a.first_tiles : tiles), (unsigned)(DKV ? a.kv_heads : a.heads),
-                  (unsigned)a.batch);
-  return launch(kernel, grid, kAttnThreads, smem, 1, st, maps, a);
-}
-
 // The gradient on the tensor cores.
 template <typename T, int D>
 cudaError_t run_grad(const brace_window_attention* e, AttnArgs a, cudaStream_t st) {
-  AttnMaps queries = {}, keys = {};   // with the rows' boxes of 128 and the blocks' of 64: dq, and dk and dv
+  AttnMaps queries = {}, keys = {};   // for dq, and for dk and dv
   if (!encode_map(&queries.q, e->q, e, e->heads, 128) || !encode_map(&queries.dout, e->dout, e, e->heads, 128) ||
-      !encode_map(&queries.k, e->k, e, e->kv_heads, kBlock) || !encode_map(&queries.v, e->v, e, e->kv_heads, kBlock) ||
-      !encode_map(&keys.k, e->k, e, e->kv_heads, 128) || !encode_map(&keys.v, e->v, e, e->kv_heads, 128) ||
+      !encode_map(&queries.k, e->k, e, e->kv_heads, 128) || !encode_map(&queries.v, e->v, e, e->kv_heads, 128) ||
       !encode_map(&keys.q, e->q, e, e->heads, kBlock) || !encode_map(&keys.dout, e->dout, e, e->heads, kBlock))
     return cudaErrorNotSupported;
+  keys.k = queries.k;
+  keys.v = queries.v;
+  constexpr bool kTwo = std::is_same<T, __half>::value;
+  const unsigned tiles = (unsigned)((a.tokens + 127) / 128), heads = (unsigned)a.heads, kv_heads = (unsigned)a.kv_heads, batch = (unsigned)a.batch;
   cudaError_t err = cudaSuccess;
-  if (std::is_same<T, __half>::value)
+  if (kTwo)
     err = cudaMemsetAsync(a.range, 0, (size_t)a.batch * a.kv_heads * 8, st);
   else
     a.range = nullptr;
+  if (err == cudaSuccess) err = launch(attn_prepare_kernel<T>, dim3((unsigned)(a.padded / kPrepRows), heads, batch), 256, 0, 1, st, a);
+  static std::atomic<uint64_t> granted_dkv{0}, granted_dq{0};
+  if (err == cudaSuccess) err = grant_smem((const void*)attn_dkv_kernel<T, D>, granted_dkv, DkvShape<D>::kSmem);
   if (err == cudaSuccess)
-    err = launch(attn_prepare_kernel<T>, dim3((unsigned)(a.padded / kPrepRows), (unsigned)a.heads, (unsigned)a.batch), 256, 0, 1, st, a);
-  if (err == cudaSuccess) err = launch_grad<T, D, true>(keys, a, st);
-  if (err == cudaSuccess) err = launch_grad<T, D, false>(queries, a, st);
+    err = launch(attn_dkv_kernel<T, D>, dim3(a.first_tiles * a.pieces + tiles - a.first_tiles, kv_heads, batch), kAttnThreads,
+                 DkvShape<D>::kSmem, 1, st, keys, a);
+  if (err == cudaSuccess) err = grant_smem((const void*)attn_dq_kernel<T, D>, granted_dq, DqShape<D, kTwo>::kSmem);
+  if (err == cudaSuccess)
+    err = launch(attn_dq_kernel<T, D>, dim3(tiles, heads, batch), kAttnThreads, DqShape<D, kTwo>::kSmem, 1, st, queries, a);
   if (err == cudaSuccess && a.first_tiles)
-    err = launch(attn_join_kernel<T, D, 128>, dim3((unsigned)(a.first_tiles * 32), (unsigned)a.kv_heads, (unsigned)a.batch), 128, 0, 1, st, a);
+    err = launch(attn_join_kernel<T, D, 128>, dim3((unsigned)(a.first_tiles * 32), kv_heads, batch), 128, 0, 1, st, a);
   return err;
 }
 

@@ -8,13 +8,17 @@
 // that).  Two CTAs share an SM: one's exponentials go on while the tensor cores work for the other, and one begins or ends
 // while the other is under way.
 //
-// Backward.  Two launches of one kernel, so that every result is summed in one order: the rows are queries and the columns
-// blocks of 64 keys (dq), or the rows are keys and the columns blocks of 64 queries of all heads that share them (dk, dv).
-// Per block: scores and dp = do v into tensor memory, a thread makes p and ds of a row's 64 columns and writes them back
-// over the two, rounded to the inputs' type, and the products with k (with do and q) add to the results in tensor memory.
-// Two groups of threads take the blocks by turns.  Tiles of first tokens are seen by all queries: their blocks are shared
-// out over several CTAs, whose float32 sums a last launch adds up.  In float16 ds is held times a power of two that the
-// largest |do| and |v| allow without overflow, since ds is often below what float16 holds at full precision.
+// Backward, in two kernels, so that every result is summed in one order.  Scores and dp = do v of a block go into tensor memory,
+// a thread makes p and ds of its columns and writes them back there, rounded to the inputs' type, and the products with k (with
+// do and q) add to the results.
+//   * dq: 128 queries by blocks of 128 keys; eight warps, half of a row a thread.  ds has a place of its own, so that the next
+//     block's scores are made meanwhile.
+//   * dk and dv: 128 keys by blocks of 64 queries of all heads that share them; two groups of four warps take the blocks by
+//     turns.  With both results there is no such room: p and ds take the scores' and dp's place, and a group's next scores wait
+//     for their products.  Tiles of first tokens are seen by all queries: their blocks are shared out over several CTAs, whose
+//     float32 sums a last launch adds up.
+// In float16 ds is held times a power of two that the largest |do| and |v| allow without overflow, since ds is often below what
+// float16 holds at full precision.
 //
 // A product with P = 0 where a key is hidden gives NaN if that key's value is not finite.  A row whose result is not
 // finite is therefore computed again, key by key, from what it sees.
@@ -26,7 +30,7 @@
 
 namespace brace {
 
-constexpr int kAttnThreads = 320;          // two groups of four warps, a warp that loads, a warp that issues products
+constexpr int kAttnThreads = 320;          // of the backward pass: eight warps, one that loads, one that issues products
 constexpr float kGrown = 8.f;              // log2 of what a maximum may grow by before the result is scaled again
 
 // Of the forward pass, two CTAs an SM.  With D = 64 a CTA's half of the tensor memory holds a block's scores, its P and the
@@ -43,7 +47,7 @@ struct AttnShape {
 };
 
 struct AttnMaps {
-  CUtensorMap q, k, v, dout;               // (dimension, token, head, sequence); boxes of 64 x 128, or of 64 x 64
+  CUtensorMap q, k, v, dout;               // (dimension, token, head, sequence); boxes of 64 x 128, or of 64 x kBlock
 };
 
 // Both operands bfloat16 (format 1) or both float16 (format 0).
@@ -366,15 +370,31 @@ __global__ void __launch_bounds__(AttnShape<D>::kThreads, 2) attn_forward_kernel
 
 // ---- backward
 
-constexpr int kBlock = 64;                 // columns of a block
+constexpr int kBlock = 64;                 // queries of a block (dk, dv)
 
-template <int D, bool DKV>
-struct AttnGradShape {
+template <int D>
+struct DkvShape {
   static constexpr int kTile = 128 * D * 2, kHalf = kBlock * D * 2;
-  static constexpr int kStage = 2 * kHalf + (DKV ? 1024 : 0);        // the block's two operands, and its queries' numbers
+  static constexpr int kStage = 2 * kHalf + 1024;          // a block's queries and do, and its queries' numbers
   static constexpr int kStages = D == 64 ? 6 : 4;
   static constexpr int kSmem = 1024 + 2 * kTile + kStages * kStage + 256;
 };
+
+template <int D, bool TWO>
+struct DqShape {
+  static constexpr int kTile = 128 * D * 2;
+  static constexpr int kRingK = 3, kRingV = D == 64 ? 3 : 2;       // blocks; a block's values are free again once dp is made
+  static constexpr int kSmem = (2 + kRingK + kRingV) * kTile + 256;
+  static_assert(kSmem <= 232448, "shared memory");
+  static constexpr int kDs = 256 + D;      // columns of tensor memory: scores, dp, dq, ds (in float16 two values of it)
+  static_assert(kDs + (TWO ? 128 : 64) <= 512, "tensor memory");
+};
+
+__device__ __forceinline__ float4 lds_f32x4(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr));
+  return v;
+}
 
 constexpr int kPrepRows = 64;              // queries of a CTA that prepares the backward pass
 
@@ -434,17 +454,243 @@ __device__ __forceinline__ float attn_grad_scale(const AttnArgs& p, int b, int g
   return bound > 0.f ? ldexpf(1.f, 13 - ilogbf(bound)) : 1.f;
 }
 
-// grid: DKV (pieces of the first tokens' tiles, then tiles; kv heads; sequences), else (tiles of queries, heads, sequences)
-template <typename T, int D, bool DKV>
-__global__ void __launch_bounds__(kAttnThreads, 1) attn_grad_kernel(const __grid_constant__ AttnMaps maps, const AttnArgs p) {
-  using Shape = AttnGradShape<D, DKV>;
-  constexpr int STAGES = Shape::kStages;
+// dq.  grid: that of GradWork
+template <typename T, int D>
+__global__ void __launch_bounds__(kAttnThreads, 1) attn_dq_kernel(const __grid_constant__ AttnMaps maps, const AttnArgs p) {
   // float16: ds as the sum of two values.  With one, its rounding and the result's together are 1.5 times the result's alone
   constexpr bool kTwo = std::is_same<T, __half>::value;
+  using Shape = DqShape<D, kTwo>;
+  constexpr int RK = Shape::kRingK, RV = Shape::kRingV, BLOCK = 128, COLS = BLOCK / 2;
+  extern __shared__ __align__(1024) uint8_t smem_raw[];
+  const uint32_t base = smem_addr(smem_raw), ring_k = base + 2 * Shape::kTile, ring_v = ring_k + RK * Shape::kTile;
+  const uint32_t bars = ring_v + RV * Shape::kTile;
+  const uint32_t full_k = bars, empty_k = full_k + 24, full_v = empty_k + 24, empty_v = full_v + 24;
+  // the rows are there; scores and dp are there, have been read; ds is there, its product is complete
+  const uint32_t a_full = empty_v + 24, s_full = a_full + 8, s_free = s_full + 8, p_full = s_free + 8, p_done = p_full + 8, tail = p_done + 8;
+  volatile int* dead = (volatile int*)(smem_raw + (tail - base));
+  uint32_t* tmem_slot = (uint32_t*)(smem_raw + (tail + 8 - base));
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  if (threadIdx.x == 0) {
+    *dead = 0;
+    for (int s = 0; s < 3; ++s) {
+      mbar_init(full_k + 8 * s, 1);
+      mbar_init(empty_k + 8 * s, 1);
+      mbar_init(full_v + 8 * s, 1);
+      mbar_init(empty_v + 8 * s, 1);
+    }
+    mbar_init(a_full, 1);
+    mbar_init(s_full, 1);
+    mbar_init(s_free, 8);
+    mbar_init(p_full, 8);
+    mbar_init(p_done, 1);
+    mbar_init_visible();
+    tma_prefetch(&maps.q);
+    tma_prefetch(&maps.k);
+    tma_prefetch(&maps.v);
+    tma_prefetch(&maps.dout);
+  }
+  if (warp == 9) tmem_alloc<1>(smem_addr(tmem_slot), 512);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  grid_trigger();
+  grid_wait();
+  fence_async_global();
+
+  const int b = blockIdx.z, n = attn_length(p, b);
+  const GradWork w(p, n, false, 128, BLOCK);
+  const int h = w.head, g = h / p.share, count = w.count;
+
+  if (warp == 8) {                         // loads
+    const bool lead = elect_one();
+    if (lead && count) {
+      mbar_expect_tx(a_full, 2 * Shape::kTile);
+      load_rows<D, 128>(base, &maps.q, w.row0, h, b, a_full);
+      load_rows<D, 128>(base + Shape::kTile, &maps.dout, w.row0, h, b, a_full);
+    }
+    __syncwarp();
+    int issued = 0;
+    bool ok = true;
+    for (int k = 0; k < count; ++k) {
+      const int sk = k % RK, sv = k % RV, t = w.first(k);
+      if (!(ok = mbar_wait(empty_v + 8 * sv, (uint32_t)(k / RV + 1) & 1u, dead))) break;
+      if (lead) {
+        mbar_expect_tx(full_v + 8 * sv, Shape::kTile);
+        load_rows<D, BLOCK>(ring_v + sv * Shape::kTile, &maps.v, t, g, b, full_v + 8 * sv);
+      }
+      __syncwarp();
+      if (!(ok = mbar_wait(empty_k + 8 * sk, (uint32_t)(k / RK + 1) & 1u, dead))) break;
+      if (lead) {
+        mbar_expect_tx(full_k + 8 * sk, Shape::kTile);
+        load_rows<D, BLOCK>(ring_k + sk * Shape::kTile, &maps.k, t, g, b, full_k + 8 * sk);
+      }
+      __syncwarp();
+      ++issued;
+    }
+    if (!ok) {   // gave up: let the copies in flight land before the memory goes
+      for (int k = max(issued - 2, 0); k < issued; ++k) {
+        mbar_wait(full_k + 8 * (k % RK), (uint32_t)(k / RK) & 1u, dead);
+        mbar_wait(full_v + 8 * (k % RV), (uint32_t)(k / RV) & 1u, dead);
+      }
+    }
+  } else if (warp == 9) {                  // products
+    const bool lead = elect_one();
+    constexpr uint32_t kScores = attn_idesc<T>(BLOCK, false), kSums = attn_idesc<T>(D, true);
+    const uint64_t a_desc = operand_desc(base, 16384), desc_k = operand_desc(ring_k, 16384), desc_v = operand_desc(ring_v, 16384);
+    auto scores = [&](int k) {
+      const int sk = k % RK, sv = k % RV;
+      if (!mbar_wait(full_k + 8 * sk, (uint32_t)(k / RK) & 1u, dead)) return false;
+      if (!mbar_wait(full_v + 8 * sv, (uint32_t)(k / RV) & 1u, dead)) return false;
+      if (k && !mbar_wait(s_free, (uint32_t)(k - 1) & 1u, dead)) return false;
+      tc_fence_after();
+      if (lead) {
+        const uint64_t bk = desc_k + (uint64_t)(sk * Shape::kTile >> 4), bv = desc_v + (uint64_t)(sv * Shape::kTile >> 4);
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+          for (int i = 0; i < D / 16; ++i) {
+            const uint64_t step = (uint64_t)((i / 4) * 16384 + (i % 4) * 32) >> 4;
+            mma_f16<1>(tmem + 128 * x, a_desc + (uint64_t)(x * Shape::kTile >> 4) + step, (x ? bv : bk) + step, kScores, i > 0);
+          }
+        mma_commit<1>(s_full);
+        mma_commit<1>(empty_v + 8 * sv);
+      }
+      __syncwarp();
+      return true;
+    };
+    bool ok = count > 0 && mbar_wait(a_full, 0, dead) && scores(0);
+    for (int k = 0; ok && k < count; ++k) {
+      if (k + 1 < count && !(ok = scores(k + 1))) break;      // as soon as these have been read
+      const int sk = k % RK;
+      if (!mbar_wait(p_full, (uint32_t)k & 1u, dead)) break;
+      tc_fence_after();
+      if (lead) {
+        const uint64_t bk = desc_k + (uint64_t)(sk * Shape::kTile >> 4);
+#pragma unroll
+        for (int i = 0; i < BLOCK / 16; ++i) {
+          mma_f16_ts(tmem + 256, tmem + Shape::kDs + 8 * i, bk + i * (2048 >> 4), kSums, k > 0 || i > 0);
+          if (kTwo) mma_f16_ts(tmem + 256, tmem + Shape::kDs + 64 + 8 * i, bk + i * (2048 >> 4), kSums, 1);
+        }
+        mma_commit<1>(empty_k + 8 * sk);
+        mma_commit<1>(p_done);
+      }
+      __syncwarp();
+    }
+  } else {                                 // half of a row a thread
+    const int half = warp >> 2, row = (warp & 3) * 32 + lane, at = w.row0 + row;
+    const uint32_t mine = tmem + ((uint32_t)((warp & 3) * 32) << 16), words = mine + Shape::kDs + 32 * half;
+    const float c = p.scale * kLog2e, hold = count ? attn_grad_scale(p, b, g) : 1.f;
+    float shift = 0.f, delta = 0.f;
+    if (at < n) {
+      shift = p.shift[attn_delta(p, b, h, at)];
+      delta = p.delta[attn_delta(p, b, h, at)];
+    }
+    bool ok = true;
+    for (int k = 0; k < count; ++k) {
+      const int t = w.first(k) + COLS * half;
+      if (!mbar_wait(s_full, (uint32_t)k & 1u, dead)) {
+        ok = false;
+        break;
+      }
+      tc_fence_after();
+      float x[COLS], y[COLS];
+      tmem_fetch64(mine + COLS * half, x);
+      tmem_fetch64(mine + 128 + COLS * half, y);
+      tmem_loaded();
+      tmem_use(x);
+      tmem_use(y);
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(s_free);
+#pragma unroll
+      for (int e = 0; e < COLS; ++e) {
+        x[e] = exp2_fast(fmaf(x[e], c, shift)) * (y[e] - delta);
+        if (kTwo) x[e] *= hold;
+      }
+      const bool first = k < w.keys.nfirst;
+      if (first || t + COLS - 1 > w.row0 || t <= w.row0 + 127 - p.window) {
+        // first tokens before the window: all queries see them; else key t + e is not behind query `at`, and is in its window or
+        // one of the first tokens
+#pragma unroll
+        for (int i = 0; i < COLS; i += 32) {
+          const uint32_t seen = first ? low_bits(w.keys.first - t - i)
+                                      : low_bits(at - t + 1 - i) & (~low_bits(at - p.window + 1 - t - i) | low_bits(p.sinks - t - i));
+#pragma unroll
+          for (int e = 0; e < 32; ++e) x[i + e] = seen >> e & 1u ? x[i + e] : 0.f;
+        }
+      }
+      // the product with the block before has read its ds
+      if (k && !mbar_wait(p_done, (uint32_t)(k - 1) & 1u, dead)) {
+        ok = false;
+        break;
+      }
+      tc_fence_after();
+      uint32_t word[COLS / 2];
+#pragma unroll
+      for (int e = 0; e < COLS; e += 2) word[e / 2] = pack2<T>(x[e], x[e + 1]);
+      tmem_store32(words, word);
+      if (kTwo) {
+#pragma unroll
+        for (int e = 0; e < COLS; e += 2) {
+          const float2 hi = __half22float2(reinterpret_cast<const __half2&>(word[e / 2]));
+          word[e / 2] = pack2<T>(x[e] - hi.x, x[e + 1] - hi.y);
+        }
+        tmem_store32(words + 64, word);
+      }
+      tmem_stored();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(p_full);
+    }
+    if (ok && count) ok = mbar_wait(p_done, (uint32_t)(count - 1) & 1u, dead);
+    tc_fence_after();
+    const bool exists = at < p.tokens, real = at < n;
+    if (half == 0) {
+      T* to = head_row<T>(p.dq, b, exists ? at : 0, h);
+      const float factor = ok ? p.scale / hold : NAN;   // a wait that ran out shows in the result
+      bool bad = false;
+      if (count) {
+#pragma unroll
+        for (int col = 0; col < D; col += 32) {
+          float o[32];
+          tmem_fetch32(mine + 256 + col, o);
+          tmem_loaded();
+          tmem_use(o);
+#pragma unroll
+          for (int e = 0; e < 32; ++e) bad |= !isfinite(o[e]) && col + e < p.dim;
+          if (real) put_columns(to, o, factor, col, p.dim);
+        }
+      }
+      if (exists && !real) put_zeros(to, p.dim);
+      __syncwarp();   // what follows may write the same rows
+      unsigned again = __ballot_sync(0xffffffffu, bad && real && ok);
+      for (; again; again &= again - 1) dq_row<T>(p, b, h, w.row0 + warp * 32 + __ffs(again) - 1, n);
+    }
+  }
+  __syncthreads();
+  if (*dead)     // a wait ran out: products may still be under way
+    for (int i = 0; i < 200; ++i) __nanosleep(1000);
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 9) {
+    tc_fence_after();
+    tmem_free<1>(tmem, 512);
+  }
+}
+
+// dk and dv.  grid: that of GradWork
+template <typename T, int D>
+__global__ void __launch_bounds__(kAttnThreads, 1) attn_dkv_kernel(const __grid_constant__ AttnMaps maps, const AttnArgs p) {
+  constexpr bool kTwo = std::is_same<T, __half>::value;
+  using Shape = DkvShape<D>;
+  constexpr int STAGES = Shape::kStages;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t base = (smem_addr(smem_raw) + 1023u) & ~1023u;
   const uint32_t ring = base + 2 * Shape::kTile, bars = ring + STAGES * Shape::kStage;
   const uint32_t full = bars, empty = full + 8 * STAGES, a_full = empty + 8 * STAGES;
+  // of each group: scores and dp are there; p and ds are there
   const uint32_t s_full = a_full + 8, p_full = s_full + 16, o_full = p_full + 16, tail = o_full + 8;
   volatile int* dead = (volatile int*)(smem_raw + (tail - smem_addr(smem_raw)));
   uint32_t* tmem_slot = (uint32_t*)(smem_raw + (tail + 8 - smem_addr(smem_raw)));
@@ -478,15 +724,15 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_grad_kernel(const __grid
   fence_async_global();
 
   const int b = blockIdx.z, n = attn_length(p, b);
-  const GradWork w(p, n, DKV, 128, kBlock);
-  const int g = DKV ? w.head : w.head / p.share, count = w.count;
+  const GradWork w(p, n, true, 128, kBlock);
+  const int g = w.head, count = w.count;
 
   if (warp == 8) {                         // loads
     const bool lead = elect_one();
     if (lead && count) {
       mbar_expect_tx(a_full, 2 * Shape::kTile);
-      load_rows<D, 128>(base, DKV ? &maps.k : &maps.q, w.row0, w.head, b, a_full);
-      load_rows<D, 128>(base + Shape::kTile, DKV ? &maps.v : &maps.dout, w.row0, w.head, b, a_full);
+      load_rows<D, 128>(base, &maps.k, w.row0, g, b, a_full);
+      load_rows<D, 128>(base + Shape::kTile, &maps.v, w.row0, g, b, a_full);
     }
     __syncwarp();
     int s = 0, issued = 0;
@@ -500,16 +746,11 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_grad_kernel(const __grid
       if (lead) {
         const uint32_t at = ring + s * Shape::kStage, bar = full + 8 * s;
         const int t = w.first(k), h = w.head_of(k, p);
-        mbar_expect_tx(bar, 2 * Shape::kHalf + (DKV ? 2 * kBlock * 4 : 0));
-        if (DKV) {     // the boxes of q and do have 64 rows here, those of k and v in the other pass
-          load_rows<D, kBlock>(at, &maps.q, t, h, b, bar);
-          load_rows<D, kBlock>(at + Shape::kHalf, &maps.dout, t, h, b, bar);
-          bulk_load(at + 2 * Shape::kHalf, p.shift + attn_delta(p, b, h, t), kBlock * 4, bar);
-          bulk_load(at + 2 * Shape::kHalf + kBlock * 4, p.delta + attn_delta(p, b, h, t), kBlock * 4, bar);
-        } else {
-          load_rows<D, kBlock>(at, &maps.k, t, g, b, bar);
-          load_rows<D, kBlock>(at + Shape::kHalf, &maps.v, t, g, b, bar);
-        }
+        mbar_expect_tx(bar, 2 * Shape::kHalf + 2 * kBlock * 4);
+        load_rows<D, kBlock>(at, &maps.q, t, h, b, bar);
+        load_rows<D, kBlock>(at + Shape::kHalf, &maps.dout, t, h, b, bar);
+        bulk_load(at + 2 * Shape::kHalf, p.shift + attn_delta(p, b, h, t), kBlock * 4, bar);
+        bulk_load(at + 2 * Shape::kHalf + kBlock * 4, p.delta + attn_delta(p, b, h, t), kBlock * 4, bar);
       }
       __syncwarp();
       ++issued;
@@ -546,21 +787,19 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_grad_kernel(const __grid
     };
     for (int k = 0; ok && k < 2 && k < count; ++k) ok = scores(k);
     for (int k = 0; ok && k < count; ++k) {
-      const int s = k % STAGES;
-      if (!mbar_wait(p_full + 8 * (k & 1), (uint32_t)(k >> 1) & 1u, dead)) break;
+      const int s = k % STAGES, r = k & 1;
+      if (!mbar_wait(p_full + 8 * r, (uint32_t)(k >> 1) & 1u, dead)) break;
       tc_fence_after();
       if (lead) {
         const uint64_t db = ring_desc + (uint64_t)(s * Shape::kStage >> 4);
-        const uint32_t a = tmem + 128 * (k & 1);
+        const uint32_t a_p = tmem + 128 * r, a_ds = a_p + 64;
 #pragma unroll
         for (int i = 0; i < kBlock / 16; ++i) {
-          if (DKV) {
-            mma_f16_ts(tmem + 256, a + 8 * i, db + (uint64_t)((Shape::kHalf + 2048 * i) >> 4), kSums, k > 0 || i > 0);
-            mma_f16_ts(tmem + 256 + D, a + 64 + 8 * i, db + (uint64_t)(2048 * i >> 4), kSums, k > 0 || i > 0);
-          } else {
-            mma_f16_ts(tmem + 256, a + 64 + 8 * i, db + (uint64_t)(2048 * i >> 4), kSums, k > 0 || i > 0);
-          }
-          if (kTwo) mma_f16_ts(tmem + 256 + (DKV ? D : 0), a + 96 + 8 * i, db + (uint64_t)(2048 * i >> 4), kSums, 1);
+          const uint64_t b1 = db + (uint64_t)(2048 * i >> 4), b2 = b1 + (Shape::kHalf >> 4);
+          const uint32_t add = k > 0 || i > 0;
+          mma_f16_ts(tmem + 256, a_p + 8 * i, b2, kSums, add);
+          mma_f16_ts(tmem + 256 + D, a_ds + 8 * i, b1, kSums, add);
+          if (kTwo) mma_f16_ts(tmem + 256 + D, a_ds + 32 + 8 * i, b1, kSums, 1);
         }
         mma_commit<1>(empty + 8 * s);
       }
@@ -573,17 +812,12 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_grad_kernel(const __grid
     const int r = warp >> 2, row = (warp & 3) * 32 + lane, at = w.row0 + row;
     const uint32_t mine = tmem + ((uint32_t)((warp & 3) * 32) << 16), cells = mine + 128 * r;
     const float c = p.scale * kLog2e, hold = count ? attn_grad_scale(p, b, g) : 1.f;
-    float shift = 0.f, delta = 0.f;
-    if (!DKV && at < n) {
-      shift = p.shift[attn_delta(p, b, w.head, at)];
-      delta = p.delta[attn_delta(p, b, w.head, at)];
-    }
     uint32_t phase = 0;
     bool ok = true;
     for (int k = r; k < count; k += 2) {
       const int s = k % STAGES;
       // a block's numbers were copied by the asynchronous proxy: their own barrier makes them visible
-      if ((DKV && !mbar_wait(full + 8 * s, (uint32_t)(k / STAGES) & 1u, dead)) || !mbar_wait(s_full + 8 * r, phase, dead)) {
+      if (!mbar_wait(full + 8 * s, (uint32_t)(k / STAGES) & 1u, dead) || !mbar_wait(s_full + 8 * r, phase, dead)) {
         ok = false;
         break;
       }
@@ -595,18 +829,16 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_grad_kernel(const __grid
       tmem_loaded();
       tmem_use(x);
       tmem_use(y);
-      const float4* numbers = (const float4*)(smem_raw + (ring + s * Shape::kStage + 2 * Shape::kHalf - smem_addr(smem_raw)));
+      // the queries' numbers, read ahead of their use
+      const uint32_t numbers = ring + s * Shape::kStage + 2 * Shape::kHalf;
+      float4 sh = lds_f32x4(numbers), de = lds_f32x4(numbers + kBlock * 4);
 #pragma unroll
       for (int e = 0; e < kBlock; e += 4) {
-        float4 sh, de;
-        if (DKV) {
-          sh = numbers[e / 4];
-          de = numbers[kBlock / 4 + e / 4];
-        } else {
-          sh = make_float4(shift, shift, shift, shift);
-          de = make_float4(delta, delta, delta, delta);
-        }
         const float shifts[4] = {sh.x, sh.y, sh.z, sh.w}, deltas[4] = {de.x, de.y, de.z, de.w};
+        if (e + 4 < kBlock) {
+          sh = lds_f32x4(numbers + 4 * (e + 4));
+          de = lds_f32x4(numbers + 4 * (kBlock + e + 4));
+        }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           x[e + i] = exp2_fast(fmaf(x[e + i], c, shifts[i]));
@@ -615,32 +847,23 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_grad_kernel(const __grid
         }
       }
       const int t = w.first(k);
-      if (DKV) {
-        // query t + e: not before key `at`, before the end, in the key's window or the key one of the first tokens
-        if (t < w.row0 + 127 || t + kBlock > n || (t + kBlock > w.row0 + p.window && w.row0 + 127 >= p.sinks)) {
-          const int from = at - t, to = at < p.sinks || p.window > n - at ? n - t : at + p.window - t;
+      // query t + e: not before key `at`, before the end, in the key's window or the key one of the first tokens
+      if (t < w.row0 + 127 || t + kBlock > n || (t + kBlock > w.row0 + p.window && w.row0 + 127 >= p.sinks)) {
+        const int to = at < p.sinks || p.window > n - at ? n - t : at + p.window - t;
 #pragma unroll
-          for (int e = 0; e < kBlock; ++e) {
-            x[e] = e >= from && e < to ? x[e] : 0.f;
-            y[e] = e >= from && e < to ? y[e] : 0.f;
+        for (int i = 0; i < kBlock; i += 32) {
+          const uint32_t seen = low_bits(to - i) & ~low_bits(at - t - i);
+#pragma unroll
+          for (int e = 0; e < 32; ++e) {
+            x[i + e] = seen >> e & 1u ? x[i + e] : 0.f;
+            y[i + e] = seen >> e & 1u ? y[i + e] : 0.f;
           }
         }
-      } else if (k < w.keys.nfirst) {
-        const int here = w.keys.first - t;
-        if (here < kBlock)
-#pragma unroll
-          for (int e = 0; e < kBlock; ++e) y[e] = e < here ? y[e] : 0.f;
-      } else if (t + kBlock - 1 > w.row0 || t <= w.row0 + 127 - p.window) {
-        const int last = at - t, early = at - p.window - t, first = p.sinks - t;
-#pragma unroll
-        for (int e = 0; e < kBlock; ++e) y[e] = e <= last && (e > early || e < first) ? y[e] : 0.f;
       }
       uint32_t word[kBlock / 2];
-      if (DKV) {
 #pragma unroll
-        for (int e = 0; e < kBlock; e += 2) word[e / 2] = pack2<T>(x[e], x[e + 1]);
-        tmem_store32(cells, word);
-      }
+      for (int e = 0; e < kBlock; e += 2) word[e / 2] = pack2<T>(x[e], x[e + 1]);
+      tmem_store32(cells, word);
 #pragma unroll
       for (int e = 0; e < kBlock; e += 2) word[e / 2] = pack2<T>(y[e], y[e + 1]);
       tmem_store32(cells + 64, word);
@@ -659,46 +882,36 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_grad_kernel(const __grid
     }
     if (ok && count) ok = mbar_wait(o_full, 0, dead);
     tc_fence_after();
-    // dq: the first group writes; dv and dk: a group each
+    // the first group writes dv, the second one dk
     const bool exists = at < p.tokens, real = at < n;
-    if (DKV || r == 0) {
-      T* to = head_row<T>(DKV ? (r ? p.dk : p.dv) : p.dq, b, exists ? at : 0, w.head);
-      const float factor = !ok ? NAN : DKV && r == 0 ? 1.f : p.scale / hold;   // a wait that ran out shows in the result
-      float* part = nullptr;
-      if (DKV && w.piece >= 0)
-        part = p.part + w.part_of(p, b, r, 128, D) + row * D;
-      bool bad = false;
-      if (count) {
+    T* to = head_row<T>(r ? p.dk : p.dv, b, exists ? at : 0, g);
+    const float factor = !ok ? NAN : r ? p.scale / hold : 1.f;   // a wait that ran out shows in the result
+    float* part = w.piece >= 0 ? p.part + w.part_of(p, b, r, 128, D) + row * D : nullptr;
+    bool bad = false;
+    if (count) {
 #pragma unroll
-        for (int col = 0; col < D; col += 32) {
-          float o[32];
-          tmem_fetch32(mine + 256 + (DKV ? D * r : 0) + col, o);
-          tmem_loaded();
-          tmem_use(o);
-          if (DKV && part) {
+      for (int col = 0; col < D; col += 32) {
+        float o[32];
+        tmem_fetch32(mine + 256 + D * r + col, o);
+        tmem_loaded();
+        tmem_use(o);
+        if (part) {
 #pragma unroll
-            for (int e = 0; e < 32; e += 4)
-              *reinterpret_cast<float4*>(part + col + e) = make_float4(o[e] * factor, o[e + 1] * factor, o[e + 2] * factor, o[e + 3] * factor);
-          } else {
+          for (int e = 0; e < 32; e += 4)
+            *reinterpret_cast<float4*>(part + col + e) = make_float4(o[e] * factor, o[e + 1] * factor, o[e + 2] * factor, o[e + 3] * factor);
+        } else {
 #pragma unroll
-            for (int e = 0; e < 32; ++e) bad |= !isfinite(o[e]) && col + e < p.dim;
-            if (real) put_columns(to, o, factor, col, p.dim);
-          }
+          for (int e = 0; e < 32; ++e) bad |= !isfinite(o[e]) && col + e < p.dim;
+          if (real) put_columns(to, o, factor, col, p.dim);
         }
-      } else if (DKV && part) {
-        for (int col = 0; col < D; col += 4) *reinterpret_cast<float4*>(part + col) = make_float4(0.f, 0.f, 0.f, 0.f);
       }
-      if (exists && !real && !(DKV && part)) put_zeros(to, p.dim);
-      __syncwarp();   // what follows may write the same rows
-      unsigned again = __ballot_sync(0xffffffffu, bad && real && ok);
-      for (; again; again &= again - 1) {
-        const int i = w.row0 + (warp & 3) * 32 + __ffs(again) - 1;
-        if (DKV)
-          dkv_row<T>(p, b, w.head, i, n, r == 1, r == 0);
-        else
-          dq_row<T>(p, b, w.head, i, n);
-      }
+    } else if (part) {
+      for (int col = 0; col < D; col += 4) *reinterpret_cast<float4*>(part + col) = make_float4(0.f, 0.f, 0.f, 0.f);
     }
+    if (exists && !real && !part) put_zeros(to, p.dim);
+    __syncwarp();   // what follows may write the same rows
+    unsigned again = __ballot_sync(0xffffffffu, bad && real && ok);
+    for (; again; again &= again - 1) dkv_row<T>(p, b, g, w.row0 + (warp & 3) * 32 + __ffs(again) - 1, n, r == 1, r == 0);
   }
   __syncthreads();
   if (*dead)     // a wait ran out: products may still be under way
