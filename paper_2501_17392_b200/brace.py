@@ -102,6 +102,11 @@ class WindowAttentionArgs(C.Structure):
                 ("dout", Heads), ("dq", Heads), ("dk", Heads), ("dv", Heads)]
 
 
+# where the tensors lie in it
+_Q, _K, _V, _OUT, _DOUT, _DQ, _DK, _DV = (getattr(WindowAttentionArgs, f).offset
+                                          for f in ("q", "k", "v", "out", "dout", "dq", "dk", "dv"))
+
+
 class BraceError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -433,6 +438,9 @@ class Brace:
 _FLOATS = {torch.float32: TYPE_F32, torch.bfloat16: TYPE_BF16, torch.float16: TYPE_F16}
 _ID_BYTES = {torch.int64: 8, torch.int32: 4}
 _EMBEDDING = struct.Struct("@ii10q4if")       # the fields of EmbeddingArgs
+_LAYER_NORM = struct.Struct("@ii21q5if")      # of LayerNormArgs
+_ATTENTION = struct.Struct("@8ifq")           # of WindowAttentionArgs, up to the tensors
+_HEADS = struct.Struct("@4q")                 # of Heads
 
 
 def _launch_stream(stream, device: int, same: bool) -> int:
@@ -661,55 +669,68 @@ class LayerNorm:
         if shape != (c, n, d) and not (c == 1 and shape == (n, d)):
             raise ValueError(f"{name} has shape {tuple(shape)}, not {(c, n, d)}")
         kind, st = _FLOATS.get(t.dtype), t.stride()
-        if kind is None or (d > 1 and st[-1] != 1):
+        if kind is None or (st[-1] != 1 and d > 1):
             raise ValueError(f"{name} is of type {t.dtype} with strides {st}")
         # the stride of a dimension of one element has no meaning
         return kind, st[-2] if n > 1 else d, st[0] if c > 1 else 0
 
-    def _vector(self, t, name: str, shared: bool):
+    def _vector(self, t: torch.Tensor, name: str, shared: bool):
         """(element type, stride between clients) of a weight, a bias or a gradient of them."""
-        if t is None:
-            return None, 0
-        c, d = self.clients, self.dim
-        if t.shape != (c, d) and not ((c == 1 or shared) and t.shape == (d,)):
-            raise ValueError(f"{name} has shape {tuple(t.shape)}, not {(c, d)}")
+        c, d, shape = self.clients, self.dim, t.shape
+        if shape != (c, d) and not ((c == 1 or shared) and shape == (d,)):
+            raise ValueError(f"{name} has shape {tuple(shape)}, not {(c, d)}")
         kind, st = _FLOATS.get(t.dtype), t.stride()
-        if kind is None or (d > 1 and st[-1] != 1):
+        if kind is None or (st[-1] != 1 and d > 1):
             raise ValueError(f"{name} is of type {t.dtype} with strides {st}")
         return kind, st[0] if c > 1 and len(st) == 2 else 0
 
-    def _fill(self, x, y, mean, rstd, weight, bias) -> LayerNormArgs:
-        e, n = self._args, x.shape[-2] if x.dim() >= 2 else -1
+    def _pair(self, t, u, name: str, shared: bool):
+        """(pointer, stride) of a weight and a bias, or of their gradients, and their element type."""
+        tp = ts = up = us = 0
+        kind = other = None
+        if t is not None:
+            kind, ts = self._vector(t, name + "weight", shared)
+            tp = t.data_ptr()
+        if u is not None:
+            other, us = self._vector(u, name + "bias", shared)
+            up = u.data_ptr()
+            if kind is not None and kind != other:
+                raise ValueError(f"{name}weight and {name}bias have different types")
+        return tp, ts, up, us, kind if kind is not None else other if other is not None else TYPE_F32
+
+    def _stat(self, t: torch.Tensor, name: str, n: int) -> int:
+        """Stride between the clients of a row's mean or rstd."""
+        c, shape, st = self.clients, t.shape, t.stride()
+        if t.dtype is not torch.float32 or (shape != (c, n) and not (c == 1 and shape == (n,))):
+            raise ValueError(f"{name} has shape {tuple(shape)} and type {t.dtype}, not {(c, n)} and float32")
+        if st[-1] != 1 and n > 1:
+            raise ValueError(f"{name}: the last dimension is not contiguous")
+        return st[0] if c > 1 else n
+
+    def _count(self, x: torch.Tensor) -> int:
+        n = x.shape[-2] if x.dim() >= 2 else -1
         if not 0 <= n <= self.rows:
             raise ValueError(f"x has shape {tuple(x.shape)}: at most {self.rows} rows")
-        e.clients, e.dim, e.rows, e.eps = self.clients, self.dim, n, self.eps
-        e.x_type, e.ld_x, e.stride_x = self._rows(x, "x", n)
-        e.y_type, e.ld_y, e.stride_y = self._rows(y, "y", n)
-        wt, e.stride_weight = self._vector(weight, "weight", True)
-        bt, e.stride_bias = self._vector(bias, "bias", True)
-        if wt is not None and bt is not None and wt != bt:
-            raise ValueError("weight and bias have different types")
-        e.weight_type = wt if wt is not None else bt if bt is not None else TYPE_F32
-        e.stride_stats = n
-        for t, name in ((mean, "mean"), (rstd, "rstd")):
-            if t is None:
-                continue
-            if t.dtype != torch.float32 or (t.shape != (self.clients, n) and not (self.clients == 1 and t.shape == (n,))):
-                raise ValueError(f"{name} has shape {tuple(t.shape)} and type {t.dtype}, not {(self.clients, n)} and float32")
-            if n > 1 and t.stride(-1) != 1:
-                raise ValueError(f"{name}: the last dimension is not contiguous")
-        if self.clients > 1:
-            strides = {t.stride(0) for t in (mean, rstd) if t is not None}
-            if len(strides) > 1:
-                raise ValueError("mean and rstd have different strides")
-            e.stride_stats = strides.pop() if strides else n
-        e.d_x, e.d_y, e.d_mean, e.d_rstd = x.data_ptr(), y.data_ptr(), _ptr(mean), _ptr(rstd)
-        e.d_weight, e.d_bias = _ptr(weight), _ptr(bias)
-        return e
+        return n
+
+    def _stats(self, mean, rstd, n: int) -> int:
+        m, r = None if mean is None else self._stat(mean, "mean", n), None if rstd is None else self._stat(rstd, "rstd", n)
+        if m is not None and r is not None and m != r:
+            raise ValueError("mean and rstd have different strides")
+        return m if m is not None else r if r is not None else n
 
     def forward_status(self, x, y, weight=None, bias=None, mean=None, rstd=None, stream=None) -> int:
-        e, at = self._fill(x, y, mean, rstd, weight, bias), x.get_device()
-        same = all(t is None or t.get_device() == at for t in (y, weight, bias, mean, rstd))
+        n, at = self._count(x), x.get_device()
+        xt, xl, xs = self._rows(x, "x", n)
+        yt, yl, ys = self._rows(y, "y", n)
+        wp, ws, bp, bs, wt = self._pair(weight, bias, "", True)
+        same = y.get_device() == at
+        for t in (weight, bias, mean, rstd):
+            same = same and (t is None or t.get_device() == at)
+        e = self._args
+        _LAYER_NORM.pack_into(e, 0, self.clients, self.dim, n, x.data_ptr(), xl, xs, wp, ws, bp, bs, y.data_ptr(), yl, ys,
+                              _ptr(mean), _ptr(rstd), self._stats(mean, rstd, n), 0, 0, 0, 0, 0, 0, 0, xt, yt, wt, TYPE_F32, 0,
+                              self.eps)
         return lib().brace_layer_norm_forward(e, _launch_stream(stream, at, same))
 
     def forward(self, x: torch.Tensor, y: torch.Tensor, weight: torch.Tensor | None = None,
@@ -720,21 +741,24 @@ class LayerNorm:
 
     def grad_status(self, dy, x, mean, rstd, dx, weight=None, dweight=None, dbias=None, accumulate: bool = False,
                     stream=None) -> int:
-        e, ws, n = self._fill(x, dy, mean, rstd, weight, None), self.workspace, x.shape[-2]
-        kind, e.ld_dx, e.stride_dx = self._rows(dx, "dx", n)
-        if kind != e.x_type:
+        n, at, buf = self._count(x), x.get_device(), self.workspace
+        xt, xl, xs = self._rows(x, "x", n)
+        yt, yl, ys = self._rows(dy, "dy", n)
+        kind, dl, ds = self._rows(dx, "dx", n)
+        if kind != xt:
             raise ValueError(f"dx is of type {dx.dtype}, x of {x.dtype}")
-        wt, e.stride_dweight = self._vector(dweight, "dweight", False)
-        bt, e.stride_dbias = self._vector(dbias, "dbias", False)
-        if wt is not None and bt is not None and wt != bt:
-            raise ValueError("dweight and dbias have different types")
-        e.grad_type = wt if wt is not None else bt if bt is not None else TYPE_F32
-        e.d_dx, e.d_dweight, e.d_dbias, e.accumulate = dx.data_ptr(), _ptr(dweight), _ptr(dbias), int(accumulate)
-        if ws is None:      # refused
+        wp, ws, _, _, wt = self._pair(weight, None, "", True)
+        gp, gs, hp, hs, gt = self._pair(dweight, dbias, "d", False)
+        same = dy.get_device() == at == dx.get_device() == mean.get_device() == rstd.get_device()
+        for t in (weight, dweight, dbias, buf):
+            same = same and (t is None or t.get_device() == at)
+        e = self._args
+        _LAYER_NORM.pack_into(e, 0, self.clients, self.dim, n, x.data_ptr(), xl, xs, wp, ws, 0, 0, dy.data_ptr(), yl, ys,
+                              mean.data_ptr(), rstd.data_ptr(), self._stats(mean, rstd, n), dx.data_ptr(), dl, ds, gp, gs, hp, hs,
+                              xt, yt, wt, gt, accumulate, self.eps)
+        if buf is None:      # refused
             return lib().brace_layer_norm_grad(e, 0, 0, 0)
-        at = x.get_device()
-        same = all(t is None or t.get_device() == at for t in (dy, mean, rstd, dx, weight, dweight, dbias, ws))
-        return lib().brace_layer_norm_grad(e, ws.data_ptr(), ws.numel(), _launch_stream(stream, at, same))
+        return lib().brace_layer_norm_grad(e, buf.data_ptr(), buf.numel(), _launch_stream(stream, at, same))
 
     def grad(self, dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor, dx: torch.Tensor,
              weight: torch.Tensor | None = None, dweight: torch.Tensor | None = None,
@@ -764,42 +788,42 @@ class WindowAttention:
             need = int(lib().brace_window_attention_workspace_bytes(batch, tokens, heads, self.kv_heads, dim, sinks))
             workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=device)
         self.workspace = workspace
-        e = self._args = WindowAttentionArgs()
-        e.batch, e.heads, e.kv_heads, e.dim = batch, heads, self.kv_heads, dim
-        e.window, e.sinks, e.scale = window, sinks, self.scale
+        self._args = WindowAttentionArgs()
 
-    def _heads(self, to: Heads, t: torch.Tensor, name: str, n: int, heads: int, dtype):
-        if t.shape != (self.batch, n, heads, self.dim):
-            raise ValueError(f"{name} has shape {tuple(t.shape)}, not {(self.batch, n, heads, self.dim)}")
-        st = t.stride()
-        if t.dtype != dtype or (self.dim > 1 and st[3] != 1):
+    def _heads(self, field: int, t: torch.Tensor, name: str, n: int, heads: int, dtype):
+        b, d, shape, st = self.batch, self.dim, t.shape, t.stride()
+        if shape != (b, n, heads, d):
+            raise ValueError(f"{name} has shape {tuple(shape)}, not {(b, n, heads, d)}")
+        if t.dtype is not dtype or (st[3] != 1 and d > 1):
             raise ValueError(f"{name} is of type {t.dtype} with strides {st}, q of type {dtype}")
         # the stride of a dimension of one element has no meaning
-        to.d, to.stride, to.ld, to.head = t.data_ptr(), st[0] if self.batch > 1 else 0, st[1], st[2] if heads > 1 else 0
+        _HEADS.pack_into(self._args, field, t.data_ptr(), st[1], st[2] if heads > 1 else 0, st[0] if b > 1 else 0)
 
     def _fill(self, q, k, v, out, lse, lengths) -> WindowAttentionArgs:
         e, n, dtype = self._args, q.shape[1] if q.dim() == 4 else -1, q.dtype
-        if not 0 <= n <= self.tokens or dtype not in _FLOATS:
+        kind, h, g = _FLOATS.get(dtype), self.heads, self.kv_heads
+        if not 0 <= n <= self.tokens or kind is None:
             raise ValueError(f"q has shape {tuple(q.shape)} and type {dtype}: at most {self.tokens} tokens")
-        e.tokens, e.type = n, _FLOATS[dtype]
-        self._heads(e.q, q, "q", n, self.heads, dtype)
-        self._heads(e.k, k, "k", n, self.kv_heads, dtype)
-        self._heads(e.v, v, "v", n, self.kv_heads, dtype)
-        self._heads(e.out, out, "out", n, self.heads, dtype)
+        self._heads(_Q, q, "q", n, h, dtype)
+        self._heads(_K, k, "k", n, g, dtype)
+        self._heads(_V, v, "v", n, g, dtype)
+        self._heads(_OUT, out, "out", n, h, dtype)
         if lse is not None:
-            if lse.dtype != torch.float32 or lse.shape != (self.batch, self.heads, n) or (n > 1 and lse.stride(2) != 1):
-                raise ValueError(f"lse has shape {tuple(lse.shape)} and type {lse.dtype}, not "
-                                 f"{(self.batch, self.heads, n)} and float32")
-            e.stride_lse, e.head_lse = lse.stride(0), lse.stride(1)
-        if lengths is not None and (lengths.dtype != torch.int32 or lengths.shape != (self.batch,)
+            st = lse.stride()
+            if lse.dtype is not torch.float32 or lse.shape != (self.batch, h, n) or (st[2] != 1 and n > 1):
+                raise ValueError(f"lse has shape {tuple(lse.shape)} and type {lse.dtype}, not {(self.batch, h, n)} and float32")
+            e.stride_lse, e.head_lse = st[0], st[1]
+        if lengths is not None and (lengths.dtype is not torch.int32 or lengths.shape != (self.batch,)
                                     or (self.batch > 1 and lengths.stride(0) != 1)):
             raise ValueError(f"lengths have shape {tuple(lengths.shape)} and type {lengths.dtype}, not {(self.batch,)} and int32")
-        e.d_lse, e.d_lengths = _ptr(lse), _ptr(lengths)
+        _ATTENTION.pack_into(e, 0, self.batch, n, h, g, self.dim, self.window, self.sinks, kind, self.scale, _ptr(lengths))
+        e.d_lse = _ptr(lse)
         return e
 
     def forward_status(self, q, k, v, out, lse=None, lengths=None, stream=None) -> int:
         e, at = self._fill(q, k, v, out, lse, lengths), q.get_device()
-        same = all(t is None or t.get_device() == at for t in (k, v, out, lse, lengths))
+        same = (k.get_device() == at == v.get_device() == out.get_device() and (lse is None or lse.get_device() == at)
+                and (lengths is None or lengths.get_device() == at))
         return lib().brace_window_attention_forward(e, _launch_stream(stream, at, same))
 
     def forward(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor,
@@ -809,10 +833,10 @@ class WindowAttention:
 
     def grad_status(self, dout, q, k, v, out, lse, dq, dk, dv, lengths=None, stream=None) -> int:
         e, ws, n = self._fill(q, k, v, out, lse, lengths), self.workspace, q.shape[1]
-        self._heads(e.dout, dout, "dout", n, self.heads, q.dtype)
-        self._heads(e.dq, dq, "dq", n, self.heads, q.dtype)
-        self._heads(e.dk, dk, "dk", n, self.kv_heads, q.dtype)
-        self._heads(e.dv, dv, "dv", n, self.kv_heads, q.dtype)
+        self._heads(_DOUT, dout, "dout", n, self.heads, q.dtype)
+        self._heads(_DQ, dq, "dq", n, self.heads, q.dtype)
+        self._heads(_DK, dk, "dk", n, self.kv_heads, q.dtype)
+        self._heads(_DV, dv, "dv", n, self.kv_heads, q.dtype)
         if ws is None:      # refused
             return lib().brace_window_attention_grad(e, 0, 0, 0)
         at = q.get_device()

@@ -14,6 +14,9 @@ using namespace brace;
 namespace {
 
 constexpr int kClipCtas = 148 * 2 * kClipResident;        // of a launch: two rounds, the second one evens the first one out
+// Units of a client that a cluster takes in one launch: two launches are as fast from some 200,000 elements on.  A CTA is given
+// kClusterShare of them before another one is.
+constexpr int64_t kClusterUnits = 64, kClusterShare = 2;
 constexpr int kClipSmall = 8, kClipList = 40, kClipLongList = 340;   // tensors of a launch: its arguments hold them
 
 // One run of elements on both sides (the gradients' alone where nothing is written).
@@ -69,8 +72,10 @@ cudaError_t with_list(int pair, int cap, F&& f) {
   });
 }
 
+enum { kSum, kApply, kCluster };
+
 // One launch for the tensors of `a`, all of one pair of types.
-cudaError_t launch_clip(bool clip, int pair, int cap, int clients, const ClipArgs& a, const ClipTensor* tensors, int64_t ctas,
+cudaError_t launch_clip(int what, int pair, int cap, int clients, const ClipArgs& a, const ClipTensor* tensors, int64_t ctas,
                         cudaStream_t st) {
   return with_list(pair, cap, [&](auto ti, auto to, auto n) {
     using TI = decltype(ti);
@@ -78,8 +83,9 @@ cudaError_t launch_clip(bool clip, int pair, int cap, int clients, const ClipArg
     ClipList<CAP> list;
     std::memcpy(list.t, tensors, sizeof(ClipTensor) * a.count);
     const dim3 grid((unsigned)ctas, (unsigned)clients);
-    return clip ? launch(clip_apply_kernel<TI, decltype(to), CAP>, grid, kClipThreads, 0, 1, st, a, list)
-                : launch(clip_sum_kernel<TI, CAP>, grid, kClipThreads, 0, 1, st, a, list);
+    if (what == kSum) return launch(clip_sum_kernel<TI, CAP>, grid, kClipThreads, 0, 1, st, a, list);
+    if (what == kApply) return launch(clip_apply_kernel<TI, decltype(to), CAP>, grid, kClipThreads, 0, 1, st, a, list);
+    return launch(clip_cluster_kernel<TI, decltype(to), CAP>, grid, kClipThreads, 0, (int)ctas, st, a, list);
   });
 }
 
@@ -119,13 +125,24 @@ int run_clip(int32_t clients, const brace_tensor* t, int32_t count, bool clip, C
   };
   a.part = (double*)ws;
   a.parts = 0;
-  for (ClipTake at = {}; take(at);) a.parts += std::min(a.units, most);
+  int launches = 0;
+  for (ClipTake at = {}; take(at); ++launches) a.parts += std::min(a.units, most);
   cudaError_t err = cudaSuccess;
-  for (int pass = 0; pass <= (int)clip; ++pass) {      // sums, then clips
+  if (clip && launches == 1) {
+    ClipTake at = {};
+    take(at);
+    if (a.units <= kClusterUnits) {
+      int64_t ctas = 1;
+      while (ctas < kClusterMost && ctas * kClusterShare < a.units) ctas *= 2;
+      err = launch_clip(kCluster, at.pair, cap, clients, a, tensors, ctas, st);
+      return err == cudaSuccess ? BRACE_OK : cuda_fail_no_ctx(err);
+    }
+  }
+  for (int what = kSum; what <= (clip ? kApply : kSum); ++what) {
     a.part0 = 0;
     for (ClipTake at = {}; err == cudaSuccess && take(at);) {
       const int64_t ctas = std::min(a.units, most);
-      err = launch_clip(pass == 1, at.pair, cap, clients, a, tensors, ctas, st);
+      err = launch_clip(what, at.pair, cap, clients, a, tensors, ctas, st);
       a.part0 += ctas;
     }
   }

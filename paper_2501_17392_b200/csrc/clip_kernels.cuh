@@ -20,6 +20,7 @@
 namespace brace {
 
 constexpr int kClipThreads = 256, kClipResident = 4;   // of a CTA that only sums or only clips; CTAs of an SM
+constexpr int kClusterMost = 8;                        // CTAs of a cluster that has a client of few elements
 constexpr int kClipUnit = 2048;      // elements: what a client's elements are shared out by
 constexpr int kClipNarrow = 1024;    // rows of a strided tensor shorter than this are walked element by element
 
@@ -116,10 +117,12 @@ __device__ __forceinline__ void clip_run(P& p, const TI* in, TO* out, int64_t n)
 // first boundary.
 template <typename TI, typename TO, typename P>
 __device__ __forceinline__ void clip_span(P& p, const TI* in, TO* out, int64_t n) {
-  constexpr int V = sizeof(TI) == 4 && sizeof(TO) == 4 ? 4 : 8;
-  int head = (int)(((16 - ((uintptr_t)in & 15)) & 15) / sizeof(TI));
+  // neighbouring threads take neighbouring words of the wider type, so that a warp's access is one run of memory
+  constexpr int V = sizeof(TI) == 4 || sizeof(TO) == 4 ? 4 : 8;
+  constexpr uintptr_t kIn = V * sizeof(TI) - 1, kOut = V * sizeof(TO) - 1;
+  int head = (int)(((kIn + 1 - ((uintptr_t)in & kIn)) & kIn) / sizeof(TI));
   if (head > n) head = (int)n;
-  if (P::CLIP && ((uintptr_t)(out + head) & 15)) {
+  if (P::CLIP && ((uintptr_t)(out + head) & kOut)) {
     clip_run<TI, TO, 1>(p, in, out, n);
     return;
   }
@@ -187,6 +190,12 @@ __device__ __forceinline__ double clip_total(const ClipArgs& a, int64_t c, doubl
   return clip_block_sum(v, cell);
 }
 
+__device__ __forceinline__ void clip_factor(const ClipArgs& a, double norm, ClipPass<true>& p) {
+  const double f = norm == 0.0 ? 1.0 : (double)a.max_norm / (norm + (double)a.eps);
+  p.factor = f > 1.0 ? 1.f : (float)f;      // NaN stays
+  p.zero = a.zero_bad && !isfinite(norm);
+}
+
 // All tensors of a launch are of the types TI and TO.  grid: (CTAs of a client, clients)
 template <typename TI, int CAP>
 __global__ void __launch_bounds__(kClipThreads, kClipResident) clip_sum_kernel(const ClipArgs a, const __grid_constant__ ClipList<CAP> list) {
@@ -207,12 +216,36 @@ __global__ void __launch_bounds__(kClipThreads, kClipResident) clip_apply_kernel
   grid_trigger();
   grid_wait();
   const int64_t c = gridDim.y - 1 - blockIdx.y, x = gridDim.x - 1 - blockIdx.x;
-  const double norm = sqrt(clip_total(a, c, cell)), f = norm == 0.0 ? 1.0 : (double)a.max_norm / (norm + (double)a.eps);
+  const double norm = sqrt(clip_total(a, c, cell));
   ClipPass<true> p = {};
-  p.factor = f > 1.0 ? 1.f : (float)f;      // NaN stays
-  p.zero = a.zero_bad && !isfinite(norm);
+  clip_factor(a, norm, p);
   if (a.norms && threadIdx.x == 0 && x == 0 && a.part0 == 0) a.norms[c] = (float)norm;
   clip_walk(list, a.count, a.units * x / gridDim.x, a.units * (x + 1) / gridDim.x, [&](const ClipTensor& t, int64_t u0, int64_t u1) {
+    if (p.factor != 1.f || p.zero || t.in != t.out) clip_units<TI, TO>(p, t, c, u0, u1);
+  });
+}
+
+// Clients of few elements in one launch: a cluster has a client, its CTAs tell one another their sums.  What a CTA reads twice
+// is its own.  grid: (CTAs of a cluster, clients)
+template <typename TI, typename TO, int CAP>
+__global__ void __launch_bounds__(kClipThreads, kClipResident) clip_cluster_kernel(const ClipArgs a, const __grid_constant__ ClipList<CAP> list) {
+  __shared__ double cell[kClipThreads / 32];
+  __shared__ double sums[kClusterMost];
+  grid_trigger();
+  grid_wait();
+  const int64_t c = blockIdx.y, from = a.units * blockIdx.x / gridDim.x, to = a.units * (blockIdx.x + 1) / gridDim.x;
+  ClipPass<false> s = {};
+  clip_walk(list, a.count, from, to, [&](const ClipTensor& t, int64_t u0, int64_t u1) { clip_units<TI, TI>(s, t, c, u0, u1); });
+  const double sum = clip_block_sum(s.acc, cell);
+  if (threadIdx.x < gridDim.x) st_cluster_f64(map_to_rank(smem_addr(sums + cluster_rank()), threadIdx.x), sum);
+  cluster_sync();
+  double total = 0.0;
+  for (int k = 0; k < (int)gridDim.x; ++k) total += sums[k];
+  const double norm = sqrt(total);
+  ClipPass<true> p = {};
+  clip_factor(a, norm, p);
+  if (a.norms && threadIdx.x == 0 && blockIdx.x == 0) a.norms[c] = (float)norm;
+  clip_walk(list, a.count, from, to, [&](const ClipTensor& t, int64_t u0, int64_t u1) {
     if (p.factor != 1.f || p.zero || t.in != t.out) clip_units<TI, TO>(p, t, c, u0, u1);
   });
 }
