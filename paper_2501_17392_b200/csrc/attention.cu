@@ -159,13 +159,14 @@ cudaError_t run_grad(const brace_window_attention* e, AttnArgs a, cudaStream_t s
     a.range = nullptr;
   if (err == cudaSuccess) err = launch(attn_prepare_kernel<T>, dim3((unsigned)(a.padded / kPrepRows), heads, batch), 256, 0, 1, st, a);
   static std::atomic<uint64_t> granted_dkv{0}, granted_dq{0};
+  // dq first: dk and dv take the delta that it may have made
+  if (err == cudaSuccess) err = grant_smem((const void*)attn_dq_kernel<T, D>, granted_dq, DqShape<D, kTwo>::kSmem);
+  if (err == cudaSuccess)
+    err = launch(attn_dq_kernel<T, D>, dim3(tiles, heads, batch), kAttnThreads, DqShape<D, kTwo>::kSmem, 1, st, queries, a);
   if (err == cudaSuccess) err = grant_smem((const void*)attn_dkv_kernel<T, D>, granted_dkv, DkvShape<D>::kSmem);
   if (err == cudaSuccess)
     err = launch(attn_dkv_kernel<T, D>, dim3(a.first_tiles * a.pieces + tiles - a.first_tiles, kv_heads, batch), kAttnThreads,
                  DkvShape<D>::kSmem, 1, st, keys, a);
-  if (err == cudaSuccess) err = grant_smem((const void*)attn_dq_kernel<T, D>, granted_dq, DqShape<D, kTwo>::kSmem);
-  if (err == cudaSuccess)
-    err = launch(attn_dq_kernel<T, D>, dim3(tiles, heads, batch), kAttnThreads, DqShape<D, kTwo>::kSmem, 1, st, queries, a);
   if (err == cudaSuccess && a.first_tiles)
     err = launch(attn_join_kernel<T, D, 128>, dim3((unsigned)(a.first_tiles * 32), kv_heads, batch), 128, 0, 1, st, a);
   return err;

@@ -50,8 +50,9 @@ cudaError_t attn_grad_float(int type, const AttnArgs& a, cudaStream_t st) {
       using T = decltype(t);
       constexpr int D = decltype(d)::value;
       cudaError_t err = launch(attn_prepare_float_kernel<T>, dim3((unsigned)(a.padded / 8), (unsigned)a.heads, (unsigned)a.batch), 256, 0, 1, st, a);
-      if (err == cudaSuccess) err = launch_grad<T, D, true>(a, st);
+      // dq first: dk and dv take the delta that it may have made
       if (err == cudaSuccess) err = launch_grad<T, D, false>(a, st);
+      if (err == cudaSuccess) err = launch_grad<T, D, true>(a, st);
       if (err == cudaSuccess && a.first_tiles)
         err = launch(attn_join_kernel<T, D, kFloatRows>, dim3((unsigned)(a.first_tiles * (kFloatRows / 4)), (unsigned)a.kv_heads, (unsigned)a.batch),
                      128, 0, 1, st, a);

@@ -226,8 +226,20 @@ __global__ void __launch_bounds__(kFloatThreads, 1) attn_grad_float_kernel(const
         }
       }
   }
-  for (int k = 0; k < w.count; ++k) {
+  // the pass that makes dq walks few blocks twice: first for delta, then for ds
+  const int first_pass = !DKV && sizeof(T) == 2 && w.count * BLOCK <= kExactKeys ? w.count : 0;
+  float sum[4] = {};                                          // of p dp
+  for (int step = 0; step < w.count + first_pass; ++step) {
+    const int k = step < first_pass ? step : step - first_pass;
     const int t = w.first(k), h = w.head_of(k, p), end = DKV || k >= w.keys.nfirst ? n : w.keys.first;
+    if (first_pass && step == first_pass)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        for (int o = 8; o; o >>= 1) sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], o);
+        delta[i] = sum[i];
+        const int at = w.row0 + 4 * ty + i;
+        if (tx == 0 && at < n) p.delta[attn_delta(p, b, w.head, at)] = delta[i];
+      }
     __syncthreads();
     float_tile<T, D, BLOCK>(b1, DKV ? p.q : p.k, b, h, t, n, p.dim);
     float_tile<T, D, BLOCK>(b2, DKV ? p.dout : p.v, b, h, t, n, p.dim);
@@ -249,9 +261,13 @@ __global__ void __launch_bounds__(kFloatThreads, 1) attn_grad_float_kernel(const
         const float x = exp2f(fmaf(s[i][e], c, DKV ? numbers[col] : shift[i]));
         const int cell = (4 * ty + i) * (BLOCK + 4) + col;
         if (DKV) sp[cell] = seen ? x : 0.f;
-        sds[cell] = seen ? x * (y[i][e] - (DKV ? numbers[BLOCK + col] : delta[i])) : 0.f;
+        if (step < first_pass)
+          sum[i] += seen ? x * y[i][e] : 0.f;
+        else
+          sds[cell] = seen ? x * (y[i][e] - (DKV ? numbers[BLOCK + col] : delta[i])) : 0.f;
       }
     }
+    if (step < first_pass) continue;
     __syncthreads();
     if constexpr (DKV) float_sums<D, BLOCK>(sp, b2, r0);
     float_sums<D, BLOCK>(sds, b1, r1);

@@ -384,7 +384,7 @@ template <int D, bool TWO>
 struct DqShape {
   static constexpr int kTile = 128 * D * 2;
   static constexpr int kRingK = 3, kRingV = D == 64 ? 3 : 2;       // blocks; a block's values are free again once dp is made
-  static constexpr int kSmem = (2 + kRingK + kRingV) * kTile + 256;
+  static constexpr int kSmem = (2 + kRingK + kRingV) * kTile + 256 + 2 * 128 * 4;
   static_assert(kSmem <= 232448, "shared memory");
   static constexpr int kDs = 256 + D;      // columns of tensor memory: scores, dp, dq, ds (in float16 two values of it)
   static_assert(kDs + (TWO ? 128 : 64) <= 512, "tensor memory");
@@ -469,6 +469,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_dq_kernel(const __grid_c
   const uint32_t a_full = empty_v + 24, s_full = a_full + 8, s_free = s_full + 8, p_full = s_free + 8, p_done = p_full + 8, tail = p_done + 8;
   volatile int* dead = (volatile int*)(smem_raw + (tail - base));
   uint32_t* tmem_slot = (uint32_t*)(smem_raw + (tail + 8 - base));
+  float* sums = (float*)(smem_raw + (tail + 16 - base));      // [half][row]
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
@@ -501,7 +502,10 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_dq_kernel(const __grid_c
 
   const int b = blockIdx.z, n = attn_length(p, b);
   const GradWork w(p, n, false, 128, BLOCK);
-  const int h = w.head, g = h / p.share, count = w.count;
+  const int h = w.head, g = h / p.share;
+  // few blocks are walked twice: first for delta, then for ds
+  const int blocks = w.count, first_pass = blocks * 128 <= kExactKeys ? blocks : 0, count = blocks + first_pass;
+  auto block_of = [&](int k) { return k < first_pass ? k : k - first_pass; };
 
   if (warp == 8) {                         // loads
     const bool lead = elect_one();
@@ -514,7 +518,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_dq_kernel(const __grid_c
     int issued = 0;
     bool ok = true;
     for (int k = 0; k < count; ++k) {
-      const int sk = k % RK, sv = k % RV, t = w.first(k);
+      const int sk = k % RK, sv = k % RV, t = w.first(block_of(k));
       if (!(ok = mbar_wait(empty_v + 8 * sv, (uint32_t)(k / RV + 1) & 1u, dead))) break;
       if (lead) {
         mbar_expect_tx(full_v + 8 * sv, Shape::kTile);
@@ -556,6 +560,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_dq_kernel(const __grid_c
           }
         mma_commit<1>(s_full);
         mma_commit<1>(empty_v + 8 * sv);
+        if (k < first_pass) mma_commit<1>(empty_k + 8 * sk);
       }
       __syncwarp();
       return true;
@@ -563,14 +568,15 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_dq_kernel(const __grid_c
     bool ok = count > 0 && mbar_wait(a_full, 0, dead) && scores(0);
     for (int k = 0; ok && k < count; ++k) {
       if (k + 1 < count && !(ok = scores(k + 1))) break;      // as soon as these have been read
+      if (k < first_pass) continue;
       const int sk = k % RK;
-      if (!mbar_wait(p_full, (uint32_t)k & 1u, dead)) break;
+      if (!mbar_wait(p_full, (uint32_t)(k - first_pass) & 1u, dead)) break;
       tc_fence_after();
       if (lead) {
         const uint64_t bk = desc_k + (uint64_t)(sk * Shape::kTile >> 4);
 #pragma unroll
         for (int i = 0; i < BLOCK / 16; ++i) {
-          mma_f16_ts(tmem + 256, tmem + Shape::kDs + 8 * i, bk + i * (2048 >> 4), kSums, k > 0 || i > 0);
+          mma_f16_ts(tmem + 256, tmem + Shape::kDs + 8 * i, bk + i * (2048 >> 4), kSums, k > first_pass || i > 0);
           if (kTwo) mma_f16_ts(tmem + 256, tmem + Shape::kDs + 64 + 8 * i, bk + i * (2048 >> 4), kSums, 1);
         }
         mma_commit<1>(empty_k + 8 * sk);
@@ -588,8 +594,9 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_dq_kernel(const __grid_c
       delta = p.delta[attn_delta(p, b, h, at)];
     }
     bool ok = true;
+    float sum = 0.f;                       // of p dp
     for (int k = 0; k < count; ++k) {
-      const int t = w.first(k) + COLS * half;
+      const int t = w.first(block_of(k)) + COLS * half;
       if (!mbar_wait(s_full, (uint32_t)k & 1u, dead)) {
         ok = false;
         break;
@@ -604,12 +611,18 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_dq_kernel(const __grid_c
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(s_free);
+      if (first_pass && k == first_pass) {      // delta is complete: the two halves of a row put it together
+        sums[half * 128 + row] = sum;
+        asm volatile("bar.sync 1, 256;" ::: "memory");
+        delta = sum + sums[(half ^ 1) * 128 + row];
+        if (half == 0 && at < n) p.delta[attn_delta(p, b, h, at)] = delta;
+      }
 #pragma unroll
       for (int e = 0; e < COLS; ++e) {
-        x[e] = exp2_fast(fmaf(x[e], c, shift)) * (y[e] - delta);
-        if (kTwo) x[e] *= hold;
+        x[e] = exp2_fast(fmaf(x[e], c, shift)) * (k < first_pass ? y[e] : y[e] - delta);
+        if (kTwo && k >= first_pass) x[e] *= hold;
       }
-      const bool first = k < w.keys.nfirst;
+      const bool first = block_of(k) < w.keys.nfirst;
       if (first || t + COLS - 1 > w.row0 || t <= w.row0 + 127 - p.window) {
         // first tokens before the window: all queries see them; else key t + e is not behind query `at`, and is in its window or
         // one of the first tokens
@@ -621,8 +634,13 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_dq_kernel(const __grid_c
           for (int e = 0; e < 32; ++e) x[i + e] = seen >> e & 1u ? x[i + e] : 0.f;
         }
       }
+      if (k < first_pass) {
+#pragma unroll
+        for (int e = 0; e < COLS; e += 4) sum += (x[e] + x[e + 1]) + (x[e + 2] + x[e + 3]);
+        continue;
+      }
       // the product with the block before has read its ds
-      if (k && !mbar_wait(p_done, (uint32_t)(k - 1) & 1u, dead)) {
+      if (k > first_pass && !mbar_wait(p_done, (uint32_t)(k - first_pass - 1) & 1u, dead)) {
         ok = false;
         break;
       }
@@ -644,7 +662,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_dq_kernel(const __grid_c
       __syncwarp();
       if (lane == 0) mbar_arrive(p_full);
     }
-    if (ok && count) ok = mbar_wait(p_done, (uint32_t)(count - 1) & 1u, dead);
+    if (ok && count) ok = mbar_wait(p_done, (uint32_t)(blocks - 1) & 1u, dead);
     tc_fence_after();
     const bool exists = at < p.tokens, real = at < n;
     if (half == 0) {
