@@ -23,15 +23,33 @@ struct FloatShape {
   static constexpr int kGrad = (2 * kFloatRows * kLd + 2 * kBlock * kLd + 2 * kFloatRows * (kBlock + 4) + 2 * kBlock) * 4;
 };
 
-// Rows t .. t + ROWS of a head as float32; 0 from the sequence's end and from the head's dimension (to a multiple of 4) on.
-template <typename T, int D, int ROWS>
-__device__ __forceinline__ void float_tile(float* to, const HeadRef& x, int b, int h, int t, int n, int dim) {
+// Rows t .. t + ROWS of one or two heads as float32; 0 from the sequence's end and from the head's dimension on.  A warp reads
+// some rows of both before it writes any: the reads are under way together.
+template <typename T, int D, int ROWS, bool TWO>
+__device__ __forceinline__ void float_tiles(float* to, const HeadRef& x, float* to2, const HeadRef& x2, int b, int h, int t, int n, int dim) {
+  constexpr int W = kFloatThreads / 32, P = D / 32, G = D == 256 ? 2 : 4;      // warps; values of a lane and row; rows at a time
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-#pragma unroll 4
-  for (int r = warp; r < ROWS; r += kFloatThreads / 32) {
-    const T* row = head_row<const T>(x, b, t + r < n ? t + r : 0, h);
+#pragma unroll 1
+  for (int r0 = warp; r0 < ROWS; r0 += W * G) {
+    float v[TWO ? 2 : 1][G][P];
 #pragma unroll
-    for (int d = lane; d < D; d += 32) to[r * (D + 4) + d] = t + r < n && d < dim ? to_f32(row[d]) : 0.f;
+    for (int i = 0; i < G; ++i) {
+      const int row = t + r0 + i * W;
+#pragma unroll
+      for (int k = 0; k < P; ++k) {
+        const int d = lane + 32 * k;
+        const bool here = row < n && d < dim;
+        v[0][i][k] = here ? to_f32(head_row<const T>(x, b, row, h)[d]) : 0.f;
+        if (TWO) v[TWO][i][k] = here ? to_f32(head_row<const T>(x2, b, row, h)[d]) : 0.f;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < G; ++i)
+#pragma unroll
+      for (int k = 0; k < P; ++k) {
+        to[(r0 + i * W) * (D + 4) + lane + 32 * k] = v[0][i][k];
+        if (TWO) to2[(r0 + i * W) * (D + 4) + lane + 32 * k] = v[TWO][i][k];
+      }
   }
 }
 
@@ -127,12 +145,11 @@ __global__ void __launch_bounds__(kFloatThreads, D == 64 ? 3 : 1) attn_forward_f
   if (threadIdx.x < N) again[threadIdx.x] = 0;
   const KeyBlocks keys(p, q0, min(n, q0 + N), N);
   const int count = q0 < n ? keys.count : 0;
-  if (count) float_tile<T, D, N>(sq, p.q, b, h, q0, n, p.dim);
+  if (count) float_tiles<T, D, N, false>(sq, p.q, nullptr, p.q, b, h, q0, n, p.dim);
   for (int k = 0; k < count; ++k) {
     const int j0 = keys.key(k, N), end = k < keys.nfirst ? keys.first : n;
     __syncthreads();
-    float_tile<T, D, N>(sk, p.k, b, g, j0, n, p.dim);
-    float_tile<T, D, N>(sv, p.v, b, g, j0, n, p.dim);
+    float_tiles<T, D, N, true>(sk, p.k, sv, p.v, b, g, j0, n, p.dim);
     __syncthreads();
     float s[4][4];
     float_scores<D, 4>(sq, sk, p.dim, s);
@@ -214,8 +231,7 @@ __global__ void __launch_bounds__(kFloatThreads, 1) attn_grad_float_kernel(const
   if (threadIdx.x < N) again[threadIdx.x] = 0;
   float shift[4] = {}, delta[4] = {};
   if (w.count) {
-    float_tile<T, D, N>(a1, DKV ? p.k : p.q, b, w.head, w.row0, n, p.dim);
-    float_tile<T, D, N>(a2, DKV ? p.v : p.dout, b, w.head, w.row0, n, p.dim);
+    float_tiles<T, D, N, true>(a1, DKV ? p.k : p.q, a2, DKV ? p.v : p.dout, b, w.head, w.row0, n, p.dim);
     if (!DKV)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -241,8 +257,7 @@ __global__ void __launch_bounds__(kFloatThreads, 1) attn_grad_float_kernel(const
         if (tx == 0 && at < n) p.delta[attn_delta(p, b, w.head, at)] = delta[i];
       }
     __syncthreads();
-    float_tile<T, D, BLOCK>(b1, DKV ? p.q : p.k, b, h, t, n, p.dim);
-    float_tile<T, D, BLOCK>(b2, DKV ? p.dout : p.v, b, h, t, n, p.dim);
+    float_tiles<T, D, BLOCK, true>(b1, DKV ? p.q : p.k, b2, DKV ? p.dout : p.v, b, h, t, n, p.dim);
     if (DKV && threadIdx.x < 2 * BLOCK) {
       const int i = threadIdx.x % BLOCK;
       numbers[threadIdx.x] = t + i < n ? (threadIdx.x < BLOCK ? p.shift : p.delta)[attn_delta(p, b, h, t + i)] : 0.f;
