@@ -18,20 +18,17 @@ bool attn_served(int32_t batch, int32_t tokens, int32_t heads, int32_t kv_heads,
          (heads == 0 || (tokens / 32 + 2) * (int64_t)(heads / kv_heads) < (int64_t)1 << 31);
 }
 
-constexpr int kGradCtas = 148 * 4;   // that the first tokens' tiles are shared out over
+constexpr int kSms = 148, kGradCtas = 4 * kSms;   // the most that the first tokens' tiles are shared out over
 
-// The first tokens' tiles of `rows` keys, and the most pieces of all of them together.
-struct FirstTiles {
-  int64_t tiles, pieces;   // of a sequence and kv head; of all
-};
-FirstTiles first_tiles(int32_t batch, int32_t tokens, int32_t heads, int32_t kv_heads, int32_t sinks, int rows) {
-  FirstTiles f = {};
-  f.tiles = (std::min(sinks, tokens) + (int64_t)rows - 1) / rows;
-  const int64_t all = f.tiles * batch * kv_heads;
-  if (all == 0) return f;
-  const int64_t blocks = ((int64_t)tokens + kBlock - 1) / kBlock * (heads / kv_heads);
-  f.pieces = std::min(std::max<int64_t>(kGradCtas, all), all * blocks);
-  return f;
+int64_t tiles_of(int32_t tokens, int rows) { return ((int64_t)tokens + rows - 1) / rows; }
+
+// The most pieces, of all tiles together, that the gradient of dk and dv is made of (share_out).  More tokens never give fewer.
+int64_t most_pieces(int32_t batch, int32_t tokens, int32_t heads, int32_t kv_heads, int32_t sinks, int rows) {
+  if (heads == 0) return 0;
+  const int64_t each = (int64_t)batch * kv_heads, blocks = tiles_of(tokens, kBlock) * (heads / kv_heads);   // of a tile, at most
+  const int64_t first = tiles_of(std::min(sinks, tokens), rows) * each;
+  return std::max(std::min(std::max<int64_t>(kGradCtas, first), first * blocks),
+                  std::min<int64_t>(kSms, tiles_of(tokens, rows) * each * blocks));
 }
 
 // What the gradient keeps in its workspace: two numbers of every query, the ranges, the pieces' sums.
@@ -47,8 +44,8 @@ GradPlan grad_plan(int32_t batch, int32_t tokens, int32_t heads, int32_t kv_head
   q.off_range = (size_t)(2 * numbers);
   q.off_part = q.off_range + (size_t)round_up((int64_t)batch * kv_heads * 8, 256);
   // of the tensor cores' kernels or of those in float32, whichever the call will take
-  const int64_t wide = first_tiles(batch, tokens, heads, kv_heads, sinks, 128).pieces * 128;
-  const int64_t narrow = first_tiles(batch, tokens, heads, kv_heads, sinks, kFloatRows).pieces * kFloatRows;
+  const int64_t wide = most_pieces(batch, tokens, heads, kv_heads, sinks, 128) * 128;
+  const int64_t narrow = most_pieces(batch, tokens, heads, kv_heads, sinks, kFloatRows) * kFloatRows;
   q.bytes = q.off_part + (size_t)(std::max(wide, narrow) * 2 * (dim <= 64 ? 64 : dim <= 128 ? 128 : 256) * 4);
   if (q.bytes < 256) q.bytes = 256;
   return q;
@@ -177,16 +174,23 @@ cudaError_t with_half_type(int type, F&& f) {
   return type == BRACE_TYPE_BF16 ? f(__nv_bfloat16{}) : f(__half{});
 }
 
-// How the gradient's tiles of first tokens are shared out: over as many CTAs as make a CTA's work that of a tile behind
-// them, but no more than give every SM some.
-void share_out(const brace_window_attention* e, int rows, AttnArgs& a) {
-  const FirstTiles f = first_tiles(e->batch, e->tokens, e->heads, e->kv_heads, e->sinks, rows);
-  a.first_tiles = (int)f.tiles;
+// How many CTAs a tile of keys is shared out over, and which tiles are.  Those of first tokens, which all queries see: as many as
+// make a CTA's work that of a tile behind them, but no more than give every SM some.  All of them, where there are tiles for less
+// than half of the SMs and work for more than one CTA in each (`least` blocks: what is saved has to be more than a launch that
+// joins): 3 x 501 tokens, 2 heads read by 6, float32, 108 -> @SHARED@ us.
+void share_out(const brace_window_attention* e, int rows, int least, AttnArgs& a) {
+  const int64_t tiles = tiles_of(e->tokens, rows), first = tiles_of(std::min(e->sinks, e->tokens), rows), each = (int64_t)e->batch * e->kv_heads;
+  const int64_t window = std::min<int64_t>(e->tokens, (int64_t)a.window + rows - 1), blocks = tiles_of((int32_t)window, kBlock) * a.share;
+  a.first_tiles = (int)first;
   a.pieces = 0;
-  if (!f.tiles) return;
-  const int64_t window = std::min<int64_t>(e->tokens, (int64_t)a.window + rows - 1);
-  const int64_t even = ((int64_t)e->tokens + window - 1) / window, most = f.pieces / (f.tiles * e->batch * e->kv_heads);
-  a.pieces = (int)std::max<int64_t>(1, std::min(even, most));
+  if (first) {
+    const int64_t even = (e->tokens + window - 1) / window;
+    a.pieces = (int)std::max<int64_t>(1, std::min(even, most_pieces(e->batch, e->tokens, e->heads, e->kv_heads, e->sinks, rows) / (first * each)));
+  }
+  if (tiles * each * 2 <= kSms && blocks >= least) {
+    a.first_tiles = (int)tiles;
+    a.pieces = (int)std::min(kSms / (tiles * each), blocks);
+  }
 }
 
 }  // namespace
@@ -247,14 +251,14 @@ int brace_window_attention_grad(const brace_window_attention* e, void* d_workspa
   a.padded = q.padded;
   const cudaStream_t st = (cudaStream_t)stream;
   if (tiles_served(e, true)) {
-    share_out(e, 128, a);
+    share_out(e, 128, 16, a);
     const cudaError_t err = with_half_type(e->type, [&](auto t) {
       using T = decltype(t);
       return e->dim <= 64 ? run_grad<T, 64>(e, a, st) : run_grad<T, 128>(e, a, st);
     });
     return err == cudaSuccess ? BRACE_OK : cuda_fail_no_ctx(err);
   }
-  share_out(e, kFloatRows, a);
+  share_out(e, kFloatRows, 3, a);
   const cudaError_t err = attn_grad_float(e->type, a, st);
   return err == cudaSuccess ? BRACE_OK : cuda_fail_no_ctx(err);
 }
