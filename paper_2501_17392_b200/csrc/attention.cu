@@ -22,13 +22,16 @@ constexpr int kSms = 148, kGradCtas = 4 * kSms;   // the most that the first tok
 
 int64_t tiles_of(int32_t tokens, int rows) { return ((int64_t)tokens + rows - 1) / rows; }
 
+// CTAs that few tiles are shared out over: one an SM, two of the kernels in float32 (of 64 rows).
+int64_t spread(int rows) { return kSms * (128 / rows); }
+
 // The most pieces, of all tiles together, that the gradient of dk and dv is made of (share_out).  More tokens never give fewer.
 int64_t most_pieces(int32_t batch, int32_t tokens, int32_t heads, int32_t kv_heads, int32_t sinks, int rows) {
   if (heads == 0) return 0;
   const int64_t each = (int64_t)batch * kv_heads, blocks = tiles_of(tokens, kBlock) * (heads / kv_heads);   // of a tile, at most
   const int64_t first = tiles_of(std::min(sinks, tokens), rows) * each;
   return std::max(std::min(std::max<int64_t>(kGradCtas, first), first * blocks),
-                  std::min<int64_t>(kSms, tiles_of(tokens, rows) * each * blocks));
+                  std::min<int64_t>(spread(rows), tiles_of(tokens, rows) * each * blocks));
 }
 
 // What the gradient keeps in its workspace: two numbers of every query, the ranges, the pieces' sums.
@@ -177,7 +180,8 @@ cudaError_t with_half_type(int type, F&& f) {
 // How many CTAs a tile of keys is shared out over, and which tiles are.  Those of first tokens, which all queries see: as many as
 // make a CTA's work that of a tile behind them, but no more than give every SM some.  All of them, where there are tiles for less
 // than half of the SMs and work for more than one CTA in each (`least` blocks: what is saved has to be more than a launch that
-// joins): 3 x 501 tokens, 2 heads read by 6, float32, 108 -> @SHARED@ us.
+// joins): 3 x 501 tokens, 2 heads read by 6, float32, 118 -> 96 us; 1000 tokens, 8 heads on one of 64,
+// bfloat16, 128 -> 43 us.
 void share_out(const brace_window_attention* e, int rows, int least, AttnArgs& a) {
   const int64_t tiles = tiles_of(e->tokens, rows), first = tiles_of(std::min(e->sinks, e->tokens), rows), each = (int64_t)e->batch * e->kv_heads;
   const int64_t window = std::min<int64_t>(e->tokens, (int64_t)a.window + rows - 1), blocks = tiles_of((int32_t)window, kBlock) * a.share;
@@ -189,7 +193,7 @@ void share_out(const brace_window_attention* e, int rows, int least, AttnArgs& a
   }
   if (tiles * each * 2 <= kSms && blocks >= least) {
     a.first_tiles = (int)tiles;
-    a.pieces = (int)std::min(kSms / (tiles * each), blocks);
+    a.pieces = (int)std::min(spread(rows) / (tiles * each), blocks);
   }
 }
 
