@@ -13,7 +13,7 @@ using namespace brace;
 
 namespace {
 
-constexpr int kClipCtas = 148 * 2 * kClipResident;        // of a launch: two rounds, the second one evens the first one out
+constexpr int kClipCtas = 148 * 4 * kClipResident;        // of a launch: four rounds, the last ones even the first ones out
 // Units of a client that a cluster takes in one launch: two launches are as fast from some 200,000 elements on.  A CTA is given
 // kClusterShare of them before another one is.
 constexpr int64_t kClusterUnits = 64, kClusterShare = 2;

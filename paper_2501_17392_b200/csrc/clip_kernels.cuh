@@ -4,9 +4,9 @@
 // Bound by memory: every value is read for its square, and read again once the norm is known.  A launch sums (a client's
 // elements shared out evenly over CTAs, each of which leaves one sum), a second one clips, the other way round, so that it
 // begins with what is still in L2.
-// 50 clients of 11.7 M float32 values (2.3 GB): 330 us to sum (7.1 TB/s) and 1113 in all (6.3 TB/s on what is read twice
+// 50 clients of 11.7 M float32 values (2.3 GB): 327 us to sum (7.2 TB/s) and 1081 in all (6.5 TB/s on what is read twice
 // and written once; a copy moves 6.6).  Tried and not kept: chains of launches that clip the clients which the launch before
-// summed, from L2 (1117 us: 4 to 5 us a launch are lost, and clients of 47 MB do not stay there); one cooperative launch
+// summed, from L2 (1117 us where two passes took 1113: 4 to 5 us a launch are lost, and clients of 47 MB do not stay there); one cooperative launch
 // that holds 224 KB an SM in shared memory between its sum and its clipping (1496 us from registers, 1668 by bulk copies:
 // all CTAs wait for one another once a client).
 // Squares are summed in float32 over at most 16 values that a thread has at a time, and beyond that in float64, in one
@@ -19,7 +19,7 @@
 
 namespace brace {
 
-constexpr int kClipThreads = 256, kClipResident = 4;   // of a CTA that only sums or only clips; CTAs of an SM
+constexpr int kClipThreads = 256, kClipResident = 2;   // of a CTA that only sums or only clips; CTAs of an SM
 constexpr int kClusterMost = 8;                        // CTAs of a cluster that has a client of few elements
 constexpr int kClipUnit = 2048;      // elements: what a client's elements are shared out by
 constexpr int kClipNarrow = 1024;    // rows of a strided tensor shorter than this are walked element by element
@@ -104,7 +104,7 @@ __device__ __forceinline__ void clip_pieces(P& p, const TI* in, TO* out, int cou
 // A run of n elements (a multiple of V).
 template <typename TI, typename TO, int V, typename P>
 __device__ __forceinline__ void clip_run(P& p, const TI* in, TO* out, int64_t n) {
-  constexpr int U = V == 1 ? 8 : 64 / (V * (int)sizeof(TI));     // 64 bytes under way in a thread
+  constexpr int U = V == 1 ? 8 : 128 / (V * (int)sizeof(TI));     // 128 bytes under way in a thread
   constexpr int kStep = kClipThreads * V * U;
   in += threadIdx.x * V;
   out += threadIdx.x * V;
