@@ -47,12 +47,19 @@ NormShape norm_shape(int dim, int x_type, bool wide) {
   if (dim < kRingFrom) return norm_shape(dim, 8, 4);
   return x_type == BRACE_TYPE_F32 ? norm_shape(dim, 4, 8) : norm_shape(dim, 8, 4);
 }
+// Of the gradient: a thread has twice as much to keep for each column.  Of rows that take several warps it is given half as many,
+// so that more threads are there (4 x 8192 rows of 2048 in bfloat16: 177 -> 114 us; rows of 768 would leave a warp for two, and
+// take 264 us for 147).
+NormShape norm_grad_shape(int dim, int x_type, bool wide) {
+  if (!wide || dim <= 1024 || dim > 4096) return norm_shape(dim, x_type, wide);
+  return x_type == BRACE_TYPE_F32 ? norm_shape(dim, 4, 4) : norm_shape(dim, 8, 2);
+}
 
-constexpr int kSms = 148, kRingResident = 2, kMostResident = 16;   // CTAs of an SM: of 256 threads with rings; of any kind
+constexpr int kSms = 148, kMostResident = 16;   // CTAs of an SM, of any kind
 
 // CTAs of an SM; narrow ones make room for more.
 int resident_of(const NormShape& s, bool ring) {
-  return (ring ? kRingResident : norm_resident(s.v * s.nv)) * (kNormThreads / s.block);
+  return (ring ? ring_resident(s.v * s.nv) : norm_resident(s.v * s.nv)) * (kNormThreads / s.block);
 }
 
 // CTAs of a client's gradient.  More rows never give fewer.
@@ -127,11 +134,10 @@ cudaError_t with_ring(const NormShape& s, F&& f) {
 }
 template <typename K>
 cudaError_t launch_ring(K* kernel, std::atomic<uint64_t>& granted, const NormShape& s, dim3 grid, int row_bytes, NormArgs a, cudaStream_t st) {
-  constexpr int kMost = kRingBytes + 1024;
-  const cudaError_t err = grant_smem((const void*)kernel, granted, kMost);
+  const cudaError_t err = grant_smem((const void*)kernel, granted, ring_bytes(32) + 1024);
   if (err != cudaSuccess) return err;
   a.row_bytes = row_bytes;
-  a.stages = std::max(1, std::min(kRingMost, kRingBytes / (kNormThreads / s.block) / (s.slots * row_bytes)));
+  a.stages = std::max(1, std::min(kRingMost, ring_bytes(s.v * s.nv) / (kNormThreads / s.block) / (s.slots * row_bytes)));
   return launch(kernel, grid, s.block, 1024 + s.slots * a.stages * row_bytes, 1, st, a);
 }
 
@@ -213,7 +219,7 @@ int brace_layer_norm_grad(const brace_layer_norm* e, void* d_workspace, size_t w
   const cudaStream_t st = (cudaStream_t)stream;
   const bool wide = e->dim % 8 == 0 && wide_rows(e->d_x, e->x_type, e->ld_x, e->stride_x) &&
                     wide_rows(e->d_y, e->y_type, e->ld_y, e->stride_y) && wide_rows(e->d_dx, e->x_type, e->ld_dx, e->stride_dx);
-  const NormShape s = norm_shape(e->dim, e->x_type, wide);
+  const NormShape s = norm_grad_shape(e->dim, e->x_type, wide);
   const bool ring = wide && e->dim >= kRingFrom;
   const bool is_long = e->dim > kNormShort;
   a.group = s.group;

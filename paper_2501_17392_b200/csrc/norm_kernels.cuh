@@ -16,7 +16,9 @@
 namespace brace {
 
 constexpr int kNormThreads = 256;
-constexpr int kRingBytes = 96 * 1024;   // of a CTA's rings, two CTAs an SM
+// CTAs of an SM whose threads have so many columns of rows that come through rings; bytes of such a CTA's rings
+__host__ __device__ constexpr int ring_resident(int columns) { return columns <= 16 ? 3 : 2; }
+__host__ __device__ constexpr int ring_bytes(int columns) { return columns <= 16 ? 62 * 1024 : 96 * 1024; }
 constexpr int kRingMost = 8;            // rows of a ring
 constexpr int kNormShort = 8192;     // longest row that a CTA's registers hold, its weights and its gradients' sums beside it
 
@@ -309,7 +311,7 @@ __device__ __forceinline__ void ring_piece(Pack<T, V>& x, uint32_t addr) {
 }
 
 template <typename TX, typename TY, int V, int NV>
-__global__ void __launch_bounds__(kNormThreads, 2) norm_forward_ring_kernel(const NormArgs p) {
+__global__ void __launch_bounds__(kNormThreads, ring_resident(NV * V)) norm_forward_ring_kernel(const NormArgs p) {
   extern __shared__ __align__(1024) uint8_t smem[];
   __shared__ float cell[2][kNormThreads / 32][2];
   __shared__ int dead;
@@ -385,7 +387,7 @@ __global__ void __launch_bounds__(kNormThreads, 2) norm_forward_ring_kernel(cons
 }
 
 template <typename TX, typename TY, int V, int NV>
-__global__ void __launch_bounds__(kNormThreads, 2) norm_grad_ring_kernel(const NormArgs p) {
+__global__ void __launch_bounds__(kNormThreads, ring_resident(NV * V)) norm_grad_ring_kernel(const NormArgs p) {
   extern __shared__ __align__(1024) uint8_t smem[];
   __shared__ float cell[2][kNormThreads / 32][2];
   __shared__ float sums[2][1024];
