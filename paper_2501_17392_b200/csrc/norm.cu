@@ -65,7 +65,7 @@ int resident_of(const NormShape& s, bool ring) {
 // CTAs of a client's gradient.  More rows never give fewer.
 int64_t norm_parts(int32_t clients, int64_t rows, int32_t dim, int slots, int resident) {
   int64_t n = dim > kNormShort ? (rows + 31) / 32 : (rows + 4 * slots - 1) / (4 * slots);
-  int64_t most = dim > kNormShort ? (int64_t)kSms * 4 * kNormThreads / dim : kSms * resident;
+  int64_t most = dim > kNormShort ? std::max<int64_t>((int64_t)kSms * 16 * kNormThreads / dim, 1) : kSms * resident;
   most /= std::max(clients, 1);
   n = std::min(n, std::max<int64_t>(most, 1));
   return std::max<int64_t>(n, 1);
@@ -169,7 +169,9 @@ int brace_layer_norm_forward(const brace_layer_norm* e, brace_stream_t stream) {
     return with_type(e->y_type, [&](auto ty) {
       using TX = decltype(tx);
       using TY = decltype(ty);
-      if (e->dim > kNormShort) return launch(norm_forward_long_kernel<TX, TY>, grid, kNormThreads, 0, 1, st, a);
+      if (e->dim > kNormShort)
+        return wide ? launch(norm_forward_long_kernel<TX, TY, 8>, grid, kNormThreads, 0, 1, st, a)
+                    : launch(norm_forward_long_kernel<TX, TY, 1>, grid, kNormThreads, 0, 1, st, a);
       if (ring)
         return with_ring<TX>(s, [&](auto v, auto nv) {
           static std::atomic<uint64_t> granted{0};
@@ -240,11 +242,14 @@ int brace_layer_norm_grad(const brace_layer_norm* e, void* d_workspace, size_t w
                         dim3((unsigned)a.parts, (unsigned)e->clients), s.block, 0, 1, st, a);
         });
       const int64_t ctas = std::min(std::max<int64_t>(e->rows, 1), std::max<int64_t>(1, kSms * 4 / e->clients));
-      const cudaError_t first = launch(norm_grad_long_kernel<TX, TY>, dim3((unsigned)ctas, (unsigned)e->clients), kNormThreads, 0, 1, st, a);
+      const dim3 rows((unsigned)ctas, (unsigned)e->clients);
+      const cudaError_t first = wide ? launch(norm_grad_long_kernel<TX, TY, 8>, rows, kNormThreads, 0, 1, st, a)
+                                     : launch(norm_grad_long_kernel<TX, TY, 1>, rows, kNormThreads, 0, 1, st, a);
       if (first != cudaSuccess || !params) return first;
-      return launch(norm_columns_kernel<TX, TY>,
-                    dim3((unsigned)((e->dim + kNormThreads - 1) / kNormThreads), (unsigned)a.parts, (unsigned)e->clients),
-                    kNormThreads, 0, 1, st, a);
+      const int per = kNormThreads * (wide ? 8 : 1);
+      const dim3 columns((unsigned)((e->dim + per - 1) / per), (unsigned)a.parts, (unsigned)e->clients);
+      return wide ? launch(norm_columns_kernel<TX, TY, 8>, columns, kNormThreads, 0, 1, st, a)
+                  : launch(norm_columns_kernel<TX, TY, 1>, columns, kNormThreads, 0, 1, st, a);
     });
   });
   if (err == cudaSuccess && params && (is_long || a.parts > 1))

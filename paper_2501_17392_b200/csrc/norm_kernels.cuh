@@ -497,7 +497,28 @@ __global__ void __launch_bounds__(256) norm_join_kernel(const NormArgs p) {
 // ---- rows longer than kNormShort: a CTA walks a row more than once (the later passes find it in L1 or L2), and the
 // weights' gradients take a pass of their own.
 
-template <typename TX, typename TY>
+// f(first column, the V values of x there, those of y) for this thread's pieces of a row.
+template <typename TX, typename TY, int V, typename F>
+__device__ __forceinline__ void norm_pieces(const TX* x, const TY* y, int dim, F&& f) {
+  constexpr int U = V == 1 ? 8 : 2;      // pieces under way
+  for (int i0 = threadIdx.x * V; i0 < dim; i0 += kNormThreads * V * U) {
+    Pack<TX, V> a[U];
+    Pack<TY, V> b[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int i = i0 + u * kNormThreads * V;
+      if (i < dim) {
+        a[u].load(x + i);
+        if (y) b[u].load(y + i);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (i0 + u * kNormThreads * V < dim) f(i0 + u * kNormThreads * V, a[u], b[u]);
+  }
+}
+
+template <typename TX, typename TY, int V>
 __global__ void __launch_bounds__(kNormThreads) norm_forward_long_kernel(const NormArgs p) {
   __shared__ float cell[2][kNormThreads / 32][2];
   grid_trigger();
@@ -508,33 +529,42 @@ __global__ void __launch_bounds__(kNormThreads) norm_forward_long_kernel(const N
   for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
     const TX* x = static_cast<const TX*>(p.x) + c * p.stride_x + row * p.ld_x;
     TY* y = static_cast<TY*>(p.y) + c * p.stride_y + row * p.ld_y;
+    const TY* none = nullptr;
     float s[1] = {0.f};
-#pragma unroll 8
-    for (int i = threadIdx.x; i < p.dim; i += kNormThreads) s[0] += to_f32(x[i]);
+    norm_pieces<TX, TY, V>(x, none, p.dim, [&](int, const Pack<TX, V>& a, const Pack<TY, V>&) {
+#pragma unroll
+      for (int k = 0; k < V; ++k) s[0] += to_f32(a.t[k]);
+    });
     group_sum(s, kNormThreads, cell, turn);
     const float mean = s[0] * inv;
     s[0] = 0.f;
-#pragma unroll 8
-    for (int i = threadIdx.x; i < p.dim; i += kNormThreads) {
-      const float d = to_f32(x[i]) - mean;
-      s[0] = fmaf(d, d, s[0]);
-    }
+    norm_pieces<TX, TY, V>(x, none, p.dim, [&](int, const Pack<TX, V>& a, const Pack<TY, V>&) {
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        const float d = to_f32(a.t[k]) - mean;
+        s[0] = fmaf(d, d, s[0]);
+      }
+    });
     group_sum(s, kNormThreads, cell, turn);
     const float rstd = 1.f / sqrtf(fmaf(s[0], inv, p.eps));
     if (threadIdx.x == 0) {
       if (p.mean) p.mean[c * p.stride_stats + row] = mean;
       if (p.rstd) p.rstd[c * p.stride_stats + row] = rstd;
     }
-#pragma unroll 4
-    for (int i = threadIdx.x; i < p.dim; i += kNormThreads) {
-      const float w = p.weight ? load_any(p.weight, p.weight_type, c * p.stride_weight + i) : 1.f;
-      const float b = p.bias ? load_any(p.bias, p.weight_type, c * p.stride_bias + i) : 0.f;
-      y[i] = from_f32<TY>(fmaf((to_f32(x[i]) - mean) * rstd, w, b));
-    }
+    norm_pieces<TX, TY, V>(x, none, p.dim, [&](int i, const Pack<TX, V>& a, const Pack<TY, V>&) {
+      Pack<TY, V> o;
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        const float w = p.weight ? load_any(p.weight, p.weight_type, c * p.stride_weight + i + k) : 1.f;
+        const float b = p.bias ? load_any(p.bias, p.weight_type, c * p.stride_bias + i + k) : 0.f;
+        o.t[k] = from_f32<TY>(fmaf((to_f32(a.t[k]) - mean) * rstd, w, b));
+      }
+      o.store_plain(y + i);
+    });
   }
 }
 
-template <typename TX, typename TY>
+template <typename TX, typename TY, int V>
 __global__ void __launch_bounds__(kNormThreads) norm_grad_long_kernel(const NormArgs p) {
   __shared__ float cell[2][kNormThreads / 32][2];
   grid_trigger();
@@ -547,45 +577,61 @@ __global__ void __launch_bounds__(kNormThreads) norm_grad_long_kernel(const Norm
     const TY* dy = static_cast<const TY*>(p.y) + c * p.stride_y + row * p.ld_y;
     TX* dx = static_cast<TX*>(p.dx) + c * p.stride_dx + row * p.ld_dx;
     const float mean = p.mean[c * p.stride_stats + row], rstd = p.rstd[c * p.stride_stats + row];
+    auto weight = [&](int i) { return p.weight ? load_any(p.weight, p.weight_type, c * p.stride_weight + i) : 1.f; };
     float s[2] = {0.f, 0.f};
-#pragma unroll 4
-    for (int i = threadIdx.x; i < p.dim; i += kNormThreads) {
-      const float w = p.weight ? load_any(p.weight, p.weight_type, c * p.stride_weight + i) : 1.f;
-      const float gr = to_f32(dy[i]) * w;
-      s[0] += gr;
-      s[1] = fmaf(gr, (to_f32(x[i]) - mean) * rstd, s[1]);
-    }
+    norm_pieces<TX, TY, V>(x, dy, p.dim, [&](int i, const Pack<TX, V>& a, const Pack<TY, V>& d) {
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        const float gr = to_f32(d.t[k]) * weight(i + k);
+        s[0] += gr;
+        s[1] = fmaf(gr, (to_f32(a.t[k]) - mean) * rstd, s[1]);
+      }
+    });
     group_sum(s, kNormThreads, cell, turn);
     const float m1 = s[0] * inv, m2 = s[1] * inv;
-#pragma unroll 4
-    for (int i = threadIdx.x; i < p.dim; i += kNormThreads) {
-      const float w = p.weight ? load_any(p.weight, p.weight_type, c * p.stride_weight + i) : 1.f;
-      const float xh = (to_f32(x[i]) - mean) * rstd;
-      dx[i] = from_f32<TX>(rstd * (fmaf(-xh, m2, to_f32(dy[i]) * w) - m1));
-    }
+    norm_pieces<TX, TY, V>(x, dy, p.dim, [&](int i, const Pack<TX, V>& a, const Pack<TY, V>& d) {
+      Pack<TX, V> o;
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        const float xh = (to_f32(a.t[k]) - mean) * rstd;
+        o.t[k] = from_f32<TX>(rstd * (fmaf(-xh, m2, to_f32(d.t[k]) * weight(i + k)) - m1));
+      }
+      o.store_plain(dx + i);
+    });
   }
 }
 
-// Part blockIdx.y (every parts-th row) of dweight and dbias, a column a thread.
-template <typename TX, typename TY>
+// Part blockIdx.y (every parts-th row) of dweight and dbias, V columns a thread.
+template <typename TX, typename TY, int V>
 __global__ void __launch_bounds__(kNormThreads) norm_columns_kernel(const NormArgs p) {
   grid_trigger();
   grid_wait();
   const int64_t c = blockIdx.z;
-  const int col = blockIdx.x * kNormThreads + threadIdx.x;
+  const int col = (blockIdx.x * kNormThreads + threadIdx.x) * V;
   if (col >= p.dim) return;
   const TX* x = static_cast<const TX*>(p.x) + c * p.stride_x + col;
   const TY* dy = static_cast<const TY*>(p.y) + c * p.stride_y + col;
-  float dw = 0.f, db = 0.f;
+  float dw[V] = {}, db[V] = {};
 #pragma unroll 4
   for (int64_t row = blockIdx.y; row < p.rows; row += p.parts) {
-    const float d = to_f32(dy[row * p.ld_y]);
-    dw = fmaf(d, (to_f32(x[row * p.ld_x]) - p.mean[c * p.stride_stats + row]) * p.rstd[c * p.stride_stats + row], dw);
-    db += d;
+    Pack<TX, V> a;
+    Pack<TY, V> d;
+    a.load(x + row * p.ld_x);
+    d.load(dy + row * p.ld_y);
+    const float mean = p.mean[c * p.stride_stats + row], rstd = p.rstd[c * p.stride_stats + row];
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+      const float g = to_f32(d.t[k]);
+      dw[k] = fmaf(g, (to_f32(a.t[k]) - mean) * rstd, dw[k]);
+      db[k] += g;
+    }
   }
   float* to = p.part + (c * p.parts + blockIdx.y) * 2 * (int64_t)p.dim + col;
-  to[0] = dw;
-  to[p.dim] = db;
+#pragma unroll
+  for (int k = 0; k < V; ++k) {
+    to[k] = dw[k];
+    to[p.dim + k] = db[k];
+  }
 }
 
 }  // namespace brace

@@ -135,7 +135,7 @@ def test_norm_lengths(d):
     check_norm(1, 3, d, pad=1, at=1, seed=20)
 
 
-@pytest.mark.parametrize("d", [8193, 10007, 16384, 70001])
+@pytest.mark.parametrize("d", [8193, 8200, 10007, 16384, 70001, 70008])
 def test_norm_long_rows(d):
     check_norm(2, 70, d)
 
