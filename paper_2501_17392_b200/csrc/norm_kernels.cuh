@@ -497,6 +497,38 @@ __global__ void __launch_bounds__(256) norm_join_kernel(const NormArgs p) {
 // ---- rows longer than kNormShort: a CTA walks a row more than once (the later passes find it in L1 or L2), and the
 // weights' gradients take a pass of their own.
 
+// V weights from index i, by words of 16 bytes where they lie so.  Read one by one, by lanes that are V columns apart, they
+// bound these kernels: 2000 x 16384 in bfloat16 takes 51 us forward and 118 us back with the one, 95 and 160 with the other.
+template <int V>
+__device__ __forceinline__ bool even_weights(const void* p, int type, int64_t i) {
+  return V == 8 && ((reinterpret_cast<uintptr_t>(p) + i * (type == kTypeF32 ? 4 : 2)) & 15) == 0;
+}
+template <int V>
+__device__ __forceinline__ void load_weights(const void* p, int type, int64_t i, bool even, float none, float (&to)[V]) {
+  if (!p) {
+#pragma unroll
+    for (int k = 0; k < V; ++k) to[k] = none;
+  } else if (!even) {
+#pragma unroll
+    for (int k = 0; k < V; ++k) to[k] = load_any(p, type, i + k);
+  } else if (type == kTypeF32) {
+    Pack<float, V> a;
+    a.load(static_cast<const float*>(p) + i);
+#pragma unroll
+    for (int k = 0; k < V; ++k) to[k] = a.t[k];
+  } else if (type == kTypeBF16) {
+    Pack<__nv_bfloat16, V> a;
+    a.load(static_cast<const __nv_bfloat16*>(p) + i);
+#pragma unroll
+    for (int k = 0; k < V; ++k) to[k] = to_f32(a.t[k]);
+  } else {
+    Pack<__half, V> a;
+    a.load(static_cast<const __half*>(p) + i);
+#pragma unroll
+    for (int k = 0; k < V; ++k) to[k] = to_f32(a.t[k]);
+  }
+}
+
 // f(first column, the V values of x there, those of y) for this thread's pieces of a row.
 template <typename TX, typename TY, int V, typename F>
 __device__ __forceinline__ void norm_pieces(const TX* x, const TY* y, int dim, F&& f) {
@@ -525,6 +557,8 @@ __global__ void __launch_bounds__(kNormThreads) norm_forward_long_kernel(const N
   grid_wait();
   const int64_t c = blockIdx.y;
   const float inv = 1.f / (float)p.dim;
+  const bool even_w = even_weights<V>(p.weight, p.weight_type, c * p.stride_weight);
+  const bool even_b = even_weights<V>(p.bias, p.weight_type, c * p.stride_bias);
   int turn = 0;
   for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
     const TX* x = static_cast<const TX*>(p.x) + c * p.stride_x + row * p.ld_x;
@@ -553,12 +587,11 @@ __global__ void __launch_bounds__(kNormThreads) norm_forward_long_kernel(const N
     }
     norm_pieces<TX, TY, V>(x, none, p.dim, [&](int i, const Pack<TX, V>& a, const Pack<TY, V>&) {
       Pack<TY, V> o;
+      float w[V], b[V];
+      load_weights<V>(p.weight, p.weight_type, c * p.stride_weight + i, even_w, 1.f, w);
+      load_weights<V>(p.bias, p.weight_type, c * p.stride_bias + i, even_b, 0.f, b);
 #pragma unroll
-      for (int k = 0; k < V; ++k) {
-        const float w = p.weight ? load_any(p.weight, p.weight_type, c * p.stride_weight + i + k) : 1.f;
-        const float b = p.bias ? load_any(p.bias, p.weight_type, c * p.stride_bias + i + k) : 0.f;
-        o.t[k] = from_f32<TY>(fmaf((to_f32(a.t[k]) - mean) * rstd, w, b));
-      }
+      for (int k = 0; k < V; ++k) o.t[k] = from_f32<TY>(fmaf((to_f32(a.t[k]) - mean) * rstd, w[k], b[k]));
       o.store_plain(y + i);
     });
   }
@@ -571,18 +604,20 @@ __global__ void __launch_bounds__(kNormThreads) norm_grad_long_kernel(const Norm
   grid_wait();
   const int64_t c = blockIdx.y;
   const float inv = 1.f / (float)p.dim;
+  const bool even = even_weights<V>(p.weight, p.weight_type, c * p.stride_weight);
   int turn = 0;
   for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
     const TX* x = static_cast<const TX*>(p.x) + c * p.stride_x + row * p.ld_x;
     const TY* dy = static_cast<const TY*>(p.y) + c * p.stride_y + row * p.ld_y;
     TX* dx = static_cast<TX*>(p.dx) + c * p.stride_dx + row * p.ld_dx;
     const float mean = p.mean[c * p.stride_stats + row], rstd = p.rstd[c * p.stride_stats + row];
-    auto weight = [&](int i) { return p.weight ? load_any(p.weight, p.weight_type, c * p.stride_weight + i) : 1.f; };
     float s[2] = {0.f, 0.f};
     norm_pieces<TX, TY, V>(x, dy, p.dim, [&](int i, const Pack<TX, V>& a, const Pack<TY, V>& d) {
+      float w[V];
+      load_weights<V>(p.weight, p.weight_type, c * p.stride_weight + i, even, 1.f, w);
 #pragma unroll
       for (int k = 0; k < V; ++k) {
-        const float gr = to_f32(d.t[k]) * weight(i + k);
+        const float gr = to_f32(d.t[k]) * w[k];
         s[0] += gr;
         s[1] = fmaf(gr, (to_f32(a.t[k]) - mean) * rstd, s[1]);
       }
@@ -591,10 +626,12 @@ __global__ void __launch_bounds__(kNormThreads) norm_grad_long_kernel(const Norm
     const float m1 = s[0] * inv, m2 = s[1] * inv;
     norm_pieces<TX, TY, V>(x, dy, p.dim, [&](int i, const Pack<TX, V>& a, const Pack<TY, V>& d) {
       Pack<TX, V> o;
+      float w[V];
+      load_weights<V>(p.weight, p.weight_type, c * p.stride_weight + i, even, 1.f, w);
 #pragma unroll
       for (int k = 0; k < V; ++k) {
         const float xh = (to_f32(a.t[k]) - mean) * rstd;
-        o.t[k] = from_f32<TX>(rstd * (fmaf(-xh, m2, to_f32(d.t[k]) * weight(i + k)) - m1));
+        o.t[k] = from_f32<TX>(rstd * (fmaf(-xh, m2, to_f32(d.t[k]) * w[k]) - m1));
       }
       o.store_plain(dx + i);
     });
