@@ -113,8 +113,8 @@ bool tiles_ok(const brace_heads& x, const brace_window_attention* e, int heads) 
 bool tiles_served(const brace_window_attention* e, bool grad) {
   if (e->type == BRACE_TYPE_F32 || e->dim % 8 || e->dim > 128) return false;
   if (!tiles_ok(e->q, e, e->heads) || !tiles_ok(e->k, e, e->kv_heads) || !tiles_ok(e->v, e, e->kv_heads)) return false;
-  if (!grad) return tiles_ok(e->out, e, e->heads);
-  return tiles_ok(e->dout, e, e->heads) && tiles_ok(e->dq, e, e->heads) && tiles_ok(e->dk, e, e->kv_heads) && tiles_ok(e->dv, e, e->kv_heads);
+  if (!tiles_ok(e->out, e, e->heads)) return false;
+  return !grad || (tiles_ok(e->dout, e, e->heads) && tiles_ok(e->dq, e, e->heads) && tiles_ok(e->dk, e, e->kv_heads) && tiles_ok(e->dv, e, e->kv_heads));
 }
 
 // Boxes of 64 dimensions x `rows` tokens, 128-byte swizzle, zeros outside.

@@ -309,6 +309,29 @@ def test_broadcast_inputs(dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("odd", ["q", "k", "v", "out", "dout", "dq", "dk", "dv"])
+def test_one_tensor_on_no_boundary(odd, dtype):
+    """All tensors on 16-byte boundaries but one."""
+    n, heads = 200, {"k": 2, "v": 2, "dk": 2, "dv": 2}
+    t = {}
+    for i, name in enumerate(("q", "k", "v", "out", "dout", "dq", "dk", "dv")):
+        h = heads.get(name, 4)
+        x = randn(2, n, h, 64, seed=i, scale=0.1 if name == "dout" else 1.0).to(dtype)
+        if name == odd:
+            flat = torch.empty(x.numel() + 1, device="cuda", dtype=dtype)[1:]
+            x = flat.copy_(x.flatten()).view(x.shape)
+        t[name] = x
+    plan = B.WindowAttention(4, 64, n, batch=2, kv_heads=2, window=90, sinks=3)
+    lse = torch.empty(2, 4, n, device="cuda")
+    plan.forward(t["q"], t["k"], t["v"], t["out"], lse=lse)
+    plan.grad(t["dout"], t["q"], t["k"], t["v"], t["out"], lse, t["dq"], t["dk"], t["dv"])
+    for i in range(2):
+        w = Plain(t["q"][i], t["k"][i], t["v"][i], 90, 3, plan.scale, t["dout"][i])
+        for name in ("out", "dq", "dk", "dv"):
+            within(t[name][i], getattr(w, name).transpose(0, 1), getattr(w, name + "_bound").transpose(0, 1), name)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 def test_on_another_stream_and_in_a_graph(dtype):
     b, n = 2, 333
     q, k, v = views(b, n, (4, 2), 64, dtype, 3)
