@@ -231,12 +231,14 @@ template <typename TI, typename TO, int CAP>
 __global__ void __launch_bounds__(kClipThreads, kClipResident) clip_cluster_kernel(const ClipArgs a, const __grid_constant__ ClipList<CAP> list) {
   __shared__ double cell[kClipThreads / 32];
   __shared__ double sums[kClusterMost];
+  cluster_arrive();
   grid_trigger();
   grid_wait();
   const int64_t c = blockIdx.y, from = a.units * blockIdx.x / gridDim.x, to = a.units * (blockIdx.x + 1) / gridDim.x;
   ClipPass<false> s = {};
   clip_walk(list, a.count, from, to, [&](const ClipTensor& t, int64_t u0, int64_t u1) { clip_units<TI, TI>(s, t, c, u0, u1); });
   const double sum = clip_block_sum(s.acc, cell);
+  cluster_wait();     // all CTAs have begun: their shared memory is theirs
   if (threadIdx.x < gridDim.x) st_cluster_f64(map_to_rank(smem_addr(sums + cluster_rank()), threadIdx.x), sum);
   cluster_sync();
   double total = 0.0;
