@@ -629,10 +629,11 @@ int brace_gradient_norm(int32_t clients, const brace_tensor* h_tensors, int32_t 
 
 /* Every client's tensors times min(1, max_norm / (norm + eps)), norm as above over
  * all of the client's tensors; the product is rounded once.  d_norms may be NULL.
- * Errors of both: INVALID_ARG (null, negative size, ld < cols, bad type,
- * misaligned pointer, stride_out 0 with several clients, d_out = d_in with another
- * layout, max_norm or eps negative or not finite), WORKSPACE, UNSUPPORTED (more
- * than 2^46 values a client), CUDA. */
+ * Errors of both: INVALID_ARG (null, negative size, more than 65535 clients,
+ * ld < cols, bad type, misaligned pointer; of clipping also stride_out 0 with
+ * several clients, d_out = d_in with another layout, two tensors of one d_out,
+ * max_norm or eps negative or not finite), WORKSPACE, UNSUPPORTED (more than 2^46
+ * values a client), CUDA. */
 int brace_gradient_clip(int32_t clients, const brace_tensor* h_tensors, int32_t count, float max_norm, float eps,
                         int32_t nonfinite, float* d_norms, void* d_workspace, size_t workspace_bytes,
                         brace_stream_t stream);
@@ -672,7 +673,8 @@ typedef struct brace_window_attention {
 } brace_window_attention;
 
 /* Errors: INVALID_ARG (null, size out of range, bad type, misaligned pointer,
- * negative stride, rows of a result or of lse that overlap), UNSUPPORTED, CUDA. */
+ * negative stride, rows of a result or of lse that overlap), UNSUPPORTED (also
+ * (tokens / 32 + 2) heads / kv_heads of 2^31 or more), CUDA. */
 int brace_window_attention_forward(const brace_window_attention* e, brace_stream_t stream);
 
 /* Bytes of workspace of brace_window_attention_grad; 0 if the arguments are
@@ -684,7 +686,9 @@ size_t brace_window_attention_workspace_bytes(int32_t batch, int32_t tokens, int
  * With p_ij = exp(s_ij - lse_i) and ds_ij = p_ij (dout_i.v_j - dout_i.out_i):
  *   dq_i = scale sum_j ds_ij k_j
  *   dk_j = scale sum ds_ij q_i,  dv_j = sum p_ij dout_i   over the queries and heads that read j
- * in one order: the same bits every time.  Errors as above, and WORKSPACE. */
+ * in one order: the same bits every time.  For bfloat16 and float16 queries of few
+ * keys dout_i.out_i is summed anew as sum_j p_ij dout_i.v_j, without the rounding
+ * of out.  Errors as above, and WORKSPACE. */
 int brace_window_attention_grad(const brace_window_attention* e, void* d_workspace, size_t workspace_bytes,
                                 brace_stream_t stream);
 

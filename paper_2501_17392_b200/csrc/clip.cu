@@ -4,6 +4,9 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <functional>
+#include <memory>
+#include <new>
 #include <type_traits>
 
 #include "clip_kernels.cuh"
@@ -37,6 +40,19 @@ int clip_cap(int32_t count) { return count <= kClipSmall ? kClipSmall : count <=
 // Most CTAs of a client in a launch.
 int64_t clip_ctas(int32_t clients) { return std::max(kClipCtas / std::max(clients, 1), 1); }
 
+// Whether two tensors are written to one place: their CTAs would race on it.
+bool clip_twice(const brace_tensor* t, int32_t count) {
+  const void* few[kClipLongList];
+  std::unique_ptr<const void*[]> many(count > kClipLongList ? new (std::nothrow) const void*[count] : nullptr);
+  if (count > kClipLongList && !many) return false;      // no memory to look
+  const void** p = many ? many.get() : few;
+  int n = 0;
+  for (int i = 0; i < count; ++i)
+    if (t[i].rows && t[i].cols) p[n++] = t[i].d_out;
+  std::sort(p, p + n, std::less<const void*>());
+  return std::adjacent_find(p, p + n) != p + n;
+}
+
 int clip_check(int32_t clients, const brace_tensor* t, int32_t count, bool clip) {
   if (clients < 0 || clients > 65535 || count < 0 || (count > 0 && !t)) return BRACE_ERR_INVALID_ARG;
   constexpr int64_t most = (int64_t)1 << 46;
@@ -56,7 +72,7 @@ int clip_check(int32_t clients, const brace_tensor* t, int32_t count, bool clip)
                               (clients > 1 && x.stride_in != x.stride_out)))
       return BRACE_ERR_INVALID_ARG;
   }
-  return BRACE_OK;
+  return clip && clients > 0 && clip_twice(t, count) ? BRACE_ERR_INVALID_ARG : BRACE_OK;
 }
 
 // Calls f with a value of the pair's two element types and the list's size.

@@ -116,6 +116,15 @@ def test_clip_refuses():
     assert B.lib().brace_gradient_clip(1, None, 3, 1.0, 0.0, 0, P, P, 1 << 40, None) == BAD
 
 
+@pytest.mark.parametrize("count", [2, 341, 1000])
+def test_clip_refuses_two_tensors_of_one_place(count):
+    """Both would be clipped there, in no order.  Empty tensors are written nowhere."""
+    apart = [tensor(d_in=P + 4096 * i, d_out=P + 4096 * i) for i in range(count)]
+    assert clip(*apart, apart[0], nbytes=8) == BAD
+    assert gradient_norm(*apart, apart[0], nbytes=8) == WORKSPACE
+    assert clip(*apart, tensor(rows=0, d_out=P), nbytes=8) == WORKSPACE
+
+
 def test_clip_workspace():
     f = B.lib().brace_clip_workspace_bytes
     one = (B.TensorArgs * 1)(tensor())
