@@ -135,7 +135,7 @@ __global__ void __launch_bounds__(kFloatThreads, D == 64 ? 3 : 1) attn_forward_f
   grid_wait();
   const int b = blockIdx.z, h = blockIdx.y, g = h / p.share, n = attn_length(p, b), q0 = N * (int)(gridDim.x - 1 - blockIdx.x);
   const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
-  const float c = fmaxf(fabsf(p.scale) * kLog2e, 1e-30f), sign = p.scale < 0.f ? -1.f : 1.f;
+  const float c = fmaxf(fabsf(p.scale) * kLog2e, kTinyScale), sign = p.scale < 0.f ? -1.f : 1.f;
   float acc[4][D / 16] = {}, top[4], total[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -214,7 +214,7 @@ __global__ void __launch_bounds__(256) attn_prepare_float_kernel(const AttnArgs 
   }
 }
 
-// grid as that of attn_grad_kernel
+// grid: that of GradWork
 template <typename T, int D, bool DKV>
 __global__ void __launch_bounds__(kFloatThreads, 1) attn_grad_float_kernel(const AttnArgs p) {
   constexpr int LD = D + 4, N = kFloatRows, BLOCK = FloatShape<D>::kBlock, C = BLOCK / 16;

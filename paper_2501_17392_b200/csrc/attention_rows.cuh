@@ -22,6 +22,7 @@ constexpr int kHeadLane = kHeadMost / 32;  // of a lane
 // 2.52e-3 -> 2.40e-3 (53 -> 64); window 4096, 2.53e-3 -> 2.39e-3 (175 -> 226, where only the first queries are worth it).
 constexpr int kExactKeys = 640;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kTinyScale = 1.4e-45f;      // for a scale of 0: a score times it is less than 2^-20, a hidden one's -inf stays so
 
 struct HeadRef {                           // element (b, t, h, d) lies at b * stride + t * ld + h * head + d
   void* p;

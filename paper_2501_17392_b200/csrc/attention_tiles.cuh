@@ -228,7 +228,7 @@ __global__ void __launch_bounds__(AttnShape<D>::kThreads, 2) attn_forward_kernel
     const int row = warp * 32 + lane, i = q0 + row;
     const uint32_t mine = tmem + ((uint32_t)(warp * 32) << 16), weights = mine + Shape::kP, result = mine + Shape::kResult;
     // scores of 0 where the scale is 0, and -inf stays -inf
-    const float c = fmaxf(fabsf(p.scale) * kLog2e, 1e-30f);
+    const float c = fmaxf(fabsf(p.scale) * kLog2e, kTinyScale);
     const bool negative = p.scale < 0.f;
     float top = -INFINITY, total = 0.f;
     // One block of which COLS columns are looked at; MASKED: those that are seen, in `seen`.
@@ -466,7 +466,8 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_dq_kernel(const __grid_c
   const uint32_t bars = ring_v + RV * Shape::kTile;
   const uint32_t full_k = bars, empty_k = full_k + 24, full_v = empty_k + 24, empty_v = full_v + 24;
   // the rows are there; scores and dp are there, have been read; ds is there, its product is complete
-  const uint32_t a_full = empty_v + 24, s_full = a_full + 8, s_free = s_full + 8, p_full = s_free + 8, p_done = p_full + 8, tail = p_done + 8;
+  const uint32_t a_full = empty_v + 24, s_full = a_full + 8, s_free = s_full + 8, p_full = s_free + 8, p_done = p_full + 8;
+  const uint32_t d_full = p_done + 8, tail = d_full + 8;      // the halves' sums of p dp are there
   volatile int* dead = (volatile int*)(smem_raw + (tail - base));
   uint32_t* tmem_slot = (uint32_t*)(smem_raw + (tail + 8 - base));
   float* sums = (float*)(smem_raw + (tail + 16 - base));      // [half][row]
@@ -485,6 +486,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_dq_kernel(const __grid_c
     mbar_init(s_free, 8);
     mbar_init(p_full, 8);
     mbar_init(p_done, 1);
+    mbar_init(d_full, 8);
     mbar_init_visible();
     tma_prefetch(&maps.q);
     tma_prefetch(&maps.k);
@@ -613,7 +615,12 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_dq_kernel(const __grid_c
       if (lane == 0) mbar_arrive(s_free);
       if (first_pass && k == first_pass) {      // delta is complete: the two halves of a row put it together
         sums[half * 128 + row] = sum;
-        asm volatile("bar.sync 1, 256;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) mbar_arrive(d_full);
+        if (!mbar_wait(d_full, 0, dead)) {
+          ok = false;
+          break;
+        }
         delta = sum + sums[(half ^ 1) * 128 + row];
         if (half == 0 && at < n) p.delta[attn_delta(p, b, h, at)] = delta;
       }

@@ -200,6 +200,12 @@ def test_scales(dtype):
     check(1, 200, (2, 2), 64, 90, 2, dtype, dsize=30.0)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_small_scales_of_large_values(dtype):
+    check(1, 200, (2, 2), 64, 90, 2, dtype, scale=2.0 ** -113, size=2.0 ** 55)     # scores as of a scale of 1/8 at size 1
+    check(1, 200, (2, 2), 64, 90, 2, dtype, scale=0.0, size=2.0 ** 50)
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("bad", [math.nan, math.inf])
 def test_what_is_hidden_has_no_effect(dtype, bad):
