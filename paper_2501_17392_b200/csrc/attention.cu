@@ -153,13 +153,14 @@ cudaError_t run_grad(const brace_window_attention* e, AttnArgs a, cudaStream_t s
   constexpr bool kTwo = std::is_same<T, __half>::value;
   const unsigned tiles = (unsigned)((a.tokens + 127) / 128), heads = (unsigned)a.heads, kv_heads = (unsigned)a.kv_heads, batch = (unsigned)a.batch;
   cudaError_t err = cudaSuccess;
-  if (kTwo)
+  if (kTwo) {
     err = cudaMemsetAsync(a.range, 0, (size_t)a.batch * a.kv_heads * 8, st);
-  else
+    if (err == cudaSuccess) err = launch(attn_prepare_kernel, dim3((unsigned)(a.padded / kPrepRows), heads, batch), 256, 0, 1, st, a);
+  } else {
     a.range = nullptr;
-  if (err == cudaSuccess) err = launch(attn_prepare_kernel<T>, dim3((unsigned)(a.padded / kPrepRows), heads, batch), 256, 0, 1, st, a);
+  }
   static std::atomic<uint64_t> granted_dkv{0}, granted_dq{0};
-  // dq first: dk and dv take the delta that it may have made
+  // dq first: dk and dv take the numbers of the queries that it made
   if (err == cudaSuccess) err = grant_smem((const void*)attn_dq_kernel<T, D>, granted_dq, DqShape<D, kTwo>::kSmem);
   if (err == cudaSuccess)
     err = launch(attn_dq_kernel<T, D>, dim3(tiles, heads, batch), kAttnThreads, DqShape<D, kTwo>::kSmem, 1, st, queries, a);

@@ -398,9 +398,10 @@ __device__ __forceinline__ float4 lds_f32x4(uint32_t addr) {
 
 constexpr int kPrepRows = 64;              // queries of a CTA that prepares the backward pass
 
-// delta, -log2(e) lse, and in float16 the ranges of do and v; 16 lanes a row.  grid: (padded / kPrepRows, heads, sequences)
-template <typename T>
+// float16: delta, -log2(e) lse, and the ranges of do and v, which have to be known before ds is held; 16 lanes a row.  (In
+// bfloat16 the kernel that makes dq makes the two numbers.)  grid: (padded / kPrepRows, heads, sequences)
 __global__ void __launch_bounds__(256) attn_prepare_kernel(const AttnArgs p) {
+  using T = __half;
   grid_trigger();
   grid_wait();
   const int h = blockIdx.y, b = blockIdx.z, n = attn_length(p, b), part = threadIdx.x & 15;
@@ -418,7 +419,7 @@ __global__ void __launch_bounds__(256) attn_prepare_kernel(const AttnArgs p) {
         s = fmaf(to_f32(o.t[e]), x, s);
         if (isfinite(x)) most_do = fmaxf(most_do, fabsf(x));
       }
-      if (p.range && h % p.share == 0) {
+      if (h % p.share == 0) {
         Pack<T, 8> v;
         v.load(head_row<const T>(p.v, b, i, h / p.share) + 8 * part);
 #pragma unroll
@@ -434,7 +435,6 @@ __global__ void __launch_bounds__(256) attn_prepare_kernel(const AttnArgs p) {
       p.shift[attn_delta(p, b, h, i)] = i < n ? -kLog2e * attn_lse(p, b, h, i) : 0.f;
     }
   }
-  if (!p.range) return;
   for (int o = 16; o; o >>= 1) {
     most_do = fmaxf(most_do, __shfl_xor_sync(0xffffffffu, most_do, o));
     most_v = fmaxf(most_v, __shfl_xor_sync(0xffffffffu, most_v, o));
@@ -590,14 +590,42 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_dq_kernel(const __grid_c
     const int half = warp >> 2, row = (warp & 3) * 32 + lane, at = w.row0 + row;
     const uint32_t mine = tmem + ((uint32_t)((warp & 3) * 32) << 16), words = mine + Shape::kDs + 32 * half;
     const float c = p.scale * kLog2e, hold = count ? attn_grad_scale(p, b, g) : 1.f;
-    float shift = 0.f, delta = 0.f;
-    if (at < n) {
-      shift = p.shift[attn_delta(p, b, h, at)];
-      delta = p.delta[attn_delta(p, b, h, at)];
-    }
+    float shift = 0.f, delta = 0.f, sum = 0.f;      // sum: of p dp, or of do and the output
     bool ok = true;
-    float sum = 0.f;                       // of p dp
-    for (int k = 0; k < count; ++k) {
+    auto whole_row = [&] {                 // the two halves of a row put its delta together
+      sums[half * 128 + row] = sum;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(d_full);
+      if (!mbar_wait(d_full, 0, dead)) return false;
+      delta = sum + sums[(half ^ 1) * 128 + row];
+      if (half == 0 && at < p.padded) p.delta[attn_delta(p, b, h, at)] = at < n ? delta : 0.f;
+      return true;
+    };
+    if constexpr (kTwo) {
+      if (at < n) {
+        shift = p.shift[attn_delta(p, b, h, at)];
+        delta = p.delta[attn_delta(p, b, h, at)];
+      }
+    } else if (count) {                    // the two numbers of this row, while the first loads are under way
+      if (at < n) shift = -kLog2e * attn_lse(p, b, h, at);
+      if (half == 0 && at < p.padded) p.shift[attn_delta(p, b, h, at)] = shift;
+      if (!first_pass) {
+        if (at < n) {
+          const T *o = head_row<const T>(p.out, b, at, h), *dout = head_row<const T>(p.dout, b, at, h);
+#pragma unroll
+          for (int col = half * (D / 2); col < (half + 1) * (D / 2); col += 8) {
+            if (col >= p.dim) break;
+            Pack<T, 8> x, y;
+            x.load(o + col);
+            y.load(dout + col);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum = fmaf(to_f32(x.t[e]), to_f32(y.t[e]), sum);
+          }
+        }
+        ok = whole_row();
+      }
+    }
+    for (int k = 0; ok && k < count; ++k) {
       const int t = w.first(block_of(k)) + COLS * half;
       if (!mbar_wait(s_full, (uint32_t)k & 1u, dead)) {
         ok = false;
@@ -613,17 +641,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_dq_kernel(const __grid_c
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(s_free);
-      if (first_pass && k == first_pass) {      // delta is complete: the two halves of a row put it together
-        sums[half * 128 + row] = sum;
-        __syncwarp();
-        if (lane == 0) mbar_arrive(d_full);
-        if (!mbar_wait(d_full, 0, dead)) {
-          ok = false;
-          break;
-        }
-        delta = sum + sums[(half ^ 1) * 128 + row];
-        if (half == 0 && at < n) p.delta[attn_delta(p, b, h, at)] = delta;
-      }
+      if (first_pass && k == first_pass && !(ok = whole_row())) break;      // delta is complete
 #pragma unroll
       for (int e = 0; e < COLS; ++e) {
         x[e] = exp2_fast(fmaf(x[e], c, shift)) * (k < first_pass ? y[e] : y[e] - delta);
