@@ -590,16 +590,12 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_dq_kernel(const __grid_c
     const int half = warp >> 2, row = (warp & 3) * 32 + lane, at = w.row0 + row;
     const uint32_t mine = tmem + ((uint32_t)((warp & 3) * 32) << 16), words = mine + Shape::kDs + 32 * half;
     const float c = p.scale * kLog2e, hold = count ? attn_grad_scale(p, b, g) : 1.f;
-    float shift = 0.f, delta = 0.f, sum = 0.f;      // sum: of p dp, or of do and the output
+    float shift = 0.f, delta = 0.f, sum = 0.f;      // sum: of p dp
     bool ok = true;
-    auto whole_row = [&] {                 // the two halves of a row put its delta together
-      sums[half * 128 + row] = sum;
+    auto meet = [&] {                      // all rows' sums are in shared memory
       __syncwarp();
       if (lane == 0) mbar_arrive(d_full);
-      if (!mbar_wait(d_full, 0, dead)) return false;
-      delta = sum + sums[(half ^ 1) * 128 + row];
-      if (half == 0 && at < p.padded) p.delta[attn_delta(p, b, h, at)] = at < n ? delta : 0.f;
-      return true;
+      return mbar_wait(d_full, 0, dead);
     };
     if constexpr (kTwo) {
       if (at < n) {
@@ -609,20 +605,34 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_dq_kernel(const __grid_c
     } else if (count) {                    // the two numbers of this row, while the first loads are under way
       if (at < n) shift = -kLog2e * attn_lse(p, b, h, at);
       if (half == 0 && at < p.padded) p.shift[attn_delta(p, b, h, at)] = shift;
-      if (!first_pass) {
-        if (at < n) {
-          const T *o = head_row<const T>(p.out, b, at, h), *dout = head_row<const T>(p.dout, b, at, h);
+      if (!first_pass) {                   // 16 lanes a row, 8 rows at a time
+#pragma unroll 1
+        for (int r0 = warp * 16; r0 < warp * 16 + 16; r0 += 8) {
+          Pack<T, 8> x[4], y[4];
+          float s[4];
 #pragma unroll
-          for (int col = half * (D / 2); col < (half + 1) * (D / 2); col += 8) {
-            if (col >= p.dim) break;
-            Pack<T, 8> x, y;
-            x.load(o + col);
-            y.load(dout + col);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) sum = fmaf(to_f32(x.t[e]), to_f32(y.t[e]), sum);
+          for (int r = 0; r < 4; ++r) {
+            const int i = min(w.row0 + r0 + 2 * r + (lane >> 4), n - 1), col = min(8 * (lane & 15), p.dim - 8);
+            x[r].load(head_row<const T>(p.out, b, i, h) + col);
+            y[r].load(head_row<const T>(p.dout, b, i, h) + col);
           }
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            s[r] = 0.f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) s[r] = fmaf(to_f32(x[r].t[e]), to_f32(y[r].t[e]), s[r]);
+            if (8 * (lane & 15) >= p.dim) s[r] = 0.f;
+          }
+          for (int o = 8; o; o >>= 1)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) s[r] += __shfl_xor_sync(0xffffffffu, s[r], o);
+          if ((lane & 15) == 0)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) sums[r0 + 2 * r + (lane >> 4)] = s[r];
         }
-        ok = whole_row();
+        ok = ok && meet();
+        delta = sums[row];
+        if (half == 0 && at < p.padded) p.delta[attn_delta(p, b, h, at)] = at < n ? delta : 0.f;
       }
     }
     for (int k = 0; ok && k < count; ++k) {
@@ -641,7 +651,12 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_dq_kernel(const __grid_c
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(s_free);
-      if (first_pass && k == first_pass && !(ok = whole_row())) break;      // delta is complete
+      if (first_pass && k == first_pass) {      // delta is complete: the two halves of a row put it together
+        sums[half * 128 + row] = sum;
+        if (!(ok = meet())) break;
+        delta = sum + sums[(half ^ 1) * 128 + row];
+        if (half == 0 && at < p.padded) p.delta[attn_delta(p, b, h, at)] = at < n ? delta : 0.f;
+      }
 #pragma unroll
       for (int e = 0; e < COLS; ++e) {
         x[e] = exp2_fast(fmaf(x[e], c, shift)) * (k < first_pass ? y[e] : y[e] - delta);
