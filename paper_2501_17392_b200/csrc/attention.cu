@@ -22,7 +22,7 @@ constexpr int kSms = 148, kGradCtas = 4 * kSms;   // the most that the first tok
 
 int64_t tiles_of(int32_t tokens, int rows) { return ((int64_t)tokens + rows - 1) / rows; }
 
-// CTAs that few tiles are shared out over: one an SM, two of the kernels in float32 (of 64 rows).
+// CTAs that few tiles are shared out over: one an SM, and of the kernels in float32, whose tiles have 64 rows, two after one another.
 int64_t spread(int rows) { return kSms * (128 / rows); }
 
 // The most pieces, of all tiles together, that the gradient of dk and dv is made of (share_out).  More tokens never give fewer.

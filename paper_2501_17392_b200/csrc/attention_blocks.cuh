@@ -1,5 +1,5 @@
 // Windowed attention: the blocks of columns that a CTA walks, what a CTA of the backward pass computes, and how the pieces
-// of the first tokens' tiles are joined.
+// of tiles of keys that are shared out are joined.
 #pragma once
 
 #include "attention_rows.cuh"
@@ -20,12 +20,12 @@ struct KeyBlocks {
 };
 
 // What a CTA of the backward pass computes: `rows` rows of dq, or of dk and dv (dkv), over its blocks of `width` columns.
-// Tiles of keys with first tokens among them are seen by all queries: each is shared out over p.pieces CTAs, which leave
-// float32 sums.  grid: dkv (pieces of the first tokens' tiles, then tiles; kv heads; sequences), else (tiles of queries, heads,
-// sequences)
+// The first p.first_tiles tiles of keys (those with first tokens, which all queries see, or all where there are few) are each
+// shared out over p.pieces CTAs, which leave float32 sums.  grid: dkv (pieces of those tiles, then tiles; kv heads; sequences),
+// else (tiles of queries, heads, sequences)
 struct GradWork {
   int row0, head, count;                   // first row; head of the rows; blocks
-  int tile, piece;                         // of first tokens, or -1
+  int tile, piece;                         // that is shared out, or -1
   int begin, per_head, width;              // first block, blocks of queries of a head (dkv)
   KeyBlocks keys;                          // (dq)
   bool dkv;
@@ -64,7 +64,7 @@ struct GradWork {
   }
 };
 
-// dv and dk of the first tokens' tiles from their pieces: a warp a row.  grid: (rows of the tiles / 4, kv heads, sequences)
+// dv and dk of the tiles that are shared out from their pieces: a warp a row.  grid: (rows of the tiles / 4, kv heads, sequences)
 template <typename T, int D, int ROWS>
 __global__ void __launch_bounds__(128) attn_join_kernel(const AttnArgs p) {
   grid_trigger();

@@ -18,8 +18,8 @@ constexpr int kHeadMost = 256;             // longest head dimension
 constexpr int kHeadLane = kHeadMost / 32;  // of a lane
 // delta_i = do_i.o_i has the rounding of o_i in it, which a row of few keys does not average out.  Queries that see at most so
 // many keys sum it anew, in float32, from p and dp.  2 x 4096 tokens, 4 heads of 64, error of dq before and after, and the time
-// of the gradient: window 2, bfloat16 4.4e-3 -> 2.3e-3 (36 -> 39 us), float16 5.1e-4 -> 2.1e-4 (41 -> 46); window 512, bfloat16
-// 2.52e-3 -> 2.40e-3 (53 -> 64); window 4096, 2.53e-3 -> 2.39e-3 (175 -> 226, where only the first queries are worth it).
+// of the gradient: window 2, bfloat16 4.4e-3 -> 2.3e-3 (30 -> 33 us), float16 5.1e-4 -> 2.1e-4 (41 -> 46); window 512, bfloat16
+// 2.52e-3 -> 2.40e-3 (48 -> 57); window 4096, where only the first queries see so few, 2.53e-3 -> 2.42e-3 (170 -> 171).
 constexpr int kExactKeys = 640;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kTinyScale = 1.4e-45f;      // for a scale of 0: a score times it is less than 2^-20, a hidden one's -inf stays so
@@ -35,7 +35,7 @@ struct AttnArgs {
   int64_t stride_lse, head_lse;
   float *delta, *shift;                    // [b][h][padded]: delta_i, and -log2(e) lse_i
   uint32_t* range;                         // [b][kv head][2]: bits of the largest |do| and |v|
-  float* part;                             // [b][kv head][tile of first tokens][piece][dv, dk][128][D]
+  float* part;                             // [b][kv head][tile that is shared out][piece][dv, dk][rows][D]
   int64_t padded;                          // tokens, rounded up to 64
   int first_tiles, pieces;
   const int32_t* lengths;

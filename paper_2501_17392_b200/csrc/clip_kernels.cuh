@@ -4,7 +4,7 @@
 // Bound by memory: every value is read for its square, and read again once the norm is known.  A launch sums (a client's
 // elements shared out evenly over CTAs, each of which leaves one sum), a second one clips, the other way round, so that it
 // begins with what is still in L2.
-// 50 clients of 11.7 M float32 values (2.3 GB): 327 us to sum (7.2 TB/s) and 1081 in all (6.5 TB/s on what is read twice
+// 50 clients of 11.7 M float32 values (2.3 GB): 327 us to sum (7.2 TB/s) and 1092 in all (6.4 TB/s on what is read twice
 // and written once; a copy moves 6.6).  Tried and not kept: chains of launches that clip the clients which the launch before
 // summed, from L2 (1117 us where two passes took 1113: 4 to 5 us a launch are lost, and clients of 47 MB do not stay there); one cooperative launch
 // that holds 224 KB an SM in shared memory between its sum and its clipping (1496 us from registers, 1668 by bulk copies:
