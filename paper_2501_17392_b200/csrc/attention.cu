@@ -25,13 +25,20 @@ int64_t tiles_of(int32_t tokens, int rows) { return ((int64_t)tokens + rows - 1)
 // CTAs that few tiles are shared out over: one an SM, and of the kernels in float32, whose tiles have 64 rows, two after one another.
 int64_t spread(int rows) { return kSms * (128 / rows); }
 
+// Tiles of keys whose sums on the tensor cores are longer than 1024 blocks (65,536 queries) are shared out over up to four CTAs.  The
+// sums are cut off, not rounded, at every step, which shows in float16, and few long CTAs leave SMs idle.  8192 tokens, 64 heads
+// on one of 64: float16, error of dk 6.0e-4 -> 3.6e-4 and of dv 4.1e-4 -> 3.2e-4 (their rounding alone 2.0e-4), 5.3 -> 3.3 ms;
+// bfloat16 4.3 -> 2.7 ms.  The workspace is then up to twice q's size at 32,768 tokens, 8 heads on one.
+int64_t long_pieces(int64_t blocks) { return std::min<int64_t>((blocks + 1023) / 1024, 4); }
+
 // The most pieces, of all tiles together, that the gradient of dk and dv is made of (share_out).  More tokens never give fewer.
 int64_t most_pieces(int32_t batch, int32_t tokens, int32_t heads, int32_t kv_heads, int32_t sinks, int rows) {
   if (heads == 0) return 0;
   const int64_t each = (int64_t)batch * kv_heads, blocks = tiles_of(tokens, kBlock) * (heads / kv_heads);   // of a tile, at most
   const int64_t first = tiles_of(std::min(sinks, tokens), rows) * each;
-  return std::max(std::min(std::max<int64_t>(kGradCtas, first), first * blocks),
-                  std::min<int64_t>(spread(rows), tiles_of(tokens, rows) * each * blocks));
+  const int64_t tiles = tiles_of(tokens, rows) * each;
+  return std::max({std::min(std::max<int64_t>(kGradCtas, first), first * blocks), std::min<int64_t>(spread(rows), tiles * blocks),
+                   rows == 128 && long_pieces(blocks) > 1 ? tiles * long_pieces(blocks) : 0});
 }
 
 // What the gradient keeps in its workspace: two numbers of every query, the ranges, the pieces' sums.
@@ -195,6 +202,11 @@ void share_out(const brace_window_attention* e, int rows, int least, AttnArgs& a
   if (tiles * each * 2 <= kSms && blocks >= least) {
     a.first_tiles = (int)tiles;
     a.pieces = (int)std::min(spread(rows) / (tiles * each), blocks);
+  }
+  const int64_t split = rows == 128 ? long_pieces(blocks) : 1;
+  if (split > 1 && (a.first_tiles == 0 || a.pieces <= split)) {     // no tile with first tokens in fewer pieces than above
+    a.first_tiles = (int)tiles;
+    a.pieces = (int)split;
   }
 }
 

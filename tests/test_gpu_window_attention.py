@@ -190,6 +190,12 @@ def test_long_sequences(dtype):
     check(1, 2500, (1, 1), 128, 2500, 0, dtype)
 
 
+@pytest.mark.parametrize("dtype", [F16, BF16])
+def test_long_sums(dtype):
+    """More than 65,536 queries read a key, and there are tiles for all SMs: each tile's sums are made of two pieces."""
+    check(9, 1100, (64, 1), 40, 1100, 3, dtype, lengths=[1100] * 7 + [777, 1099])
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 def test_scales(dtype):
     check(1, 200, (2, 2), 64, 90, 2, dtype, scale=0.0)
