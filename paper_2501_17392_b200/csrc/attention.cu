@@ -18,17 +18,18 @@ bool attn_served(int32_t batch, int32_t tokens, int32_t heads, int32_t kv_heads,
          (heads == 0 || (tokens / 32 + 2) * (int64_t)(heads / kv_heads) < (int64_t)1 << 31);
 }
 
-constexpr int kSms = 148, kGradCtas = 4 * kSms;   // the most that the first tokens' tiles are shared out over
+constexpr int kSms = 148, kGradCtas = 4 * kSms;   // the most that tiles are shared out over, but for long sums
 
 int64_t tiles_of(int32_t tokens, int rows) { return ((int64_t)tokens + rows - 1) / rows; }
 
 // CTAs that few tiles are shared out over: one an SM, and of the kernels in float32, whose tiles have 64 rows, two after one another.
 int64_t spread(int rows) { return kSms * (128 / rows); }
 
-// Tiles of keys whose sums on the tensor cores are longer than 1024 blocks (65,536 queries) are shared out over up to four CTAs.  The
-// sums are cut off, not rounded, at every step, which shows in float16, and few long CTAs leave SMs idle.  8192 tokens, 64 heads
-// on one of 64: float16, error of dk 6.0e-4 -> 3.6e-4 and of dv 4.1e-4 -> 3.2e-4 (their rounding alone 2.0e-4), 5.3 -> 3.3 ms;
-// bfloat16 4.3 -> 2.7 ms.  The workspace is then up to twice q's size at 32,768 tokens, 8 heads on one.
+// Sums on the tensor cores are cut off, not rounded, at every step, which shows in float16 after some 100,000 queries: tiles of
+// keys whose sums are longer than 1024 blocks (65,536 queries) are shared out over up to four CTAs, more where tiles are few
+// (share_out).  8192 tokens, 64 heads on one of 64, two CTAs a tile against nine: error of dk 6.0e-4 -> 2.4e-4 and of dv 4.1e-4 -> 2.9e-4
+// (their rounding alone 2.0e-4), 5.3 -> 3.1 ms; bfloat16 4.3 -> 2.6 ms.  The workspace is then up to twice q's size at 32,768
+// tokens, 8 heads on one.
 int64_t long_pieces(int64_t blocks) { return std::min<int64_t>((blocks + 1023) / 1024, 4); }
 
 // The most pieces, of all tiles together, that the gradient of dk and dv is made of (share_out).  More tokens never give fewer.
@@ -189,8 +190,7 @@ cudaError_t with_half_type(int type, F&& f) {
 // How many CTAs a tile of keys is shared out over, and which tiles are.  Those of first tokens, which all queries see: as many as
 // make a CTA's work that of a tile behind them, but no more than give every SM some.  All of them, where there are tiles for less
 // than half of the SMs and work for more than one CTA in each (`least` blocks: what is saved has to be more than a launch that
-// joins): 3 x 501 tokens, 2 heads read by 6, float32, 118 -> 96 us; 1000 tokens, 8 heads on one of 64,
-// bfloat16, 128 -> 43 us.
+// joins): 3 x 501 tokens, 2 heads read by 6, float32, 118 -> 96 us; 1000 tokens, 8 heads on one of 64, bfloat16, 128 -> 43 us.
 void share_out(const brace_window_attention* e, int rows, int least, AttnArgs& a) {
   const int64_t tiles = tiles_of(e->tokens, rows), first = tiles_of(std::min(e->sinks, e->tokens), rows), each = (int64_t)e->batch * e->kv_heads;
   const int64_t window = std::min<int64_t>(e->tokens, (int64_t)a.window + rows - 1), blocks = tiles_of((int32_t)window, kBlock) * a.share;
