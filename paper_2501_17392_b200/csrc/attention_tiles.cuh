@@ -39,6 +39,9 @@ namespace brace {
 
 constexpr int kAttnThreads = 320;          // of the backward pass: eight warps, one that loads, one that issues products
 constexpr float kGrown = 8.f;              // log2 of what a maximum may grow by before the result is scaled again
+// log2 of what float16 P is held times: float16 keeps no full precision below 2^-14, which the weights of many keys beside a
+// few large ones fall below.  2^7 times the 2^8 of a grown maximum is the most that it holds.
+constexpr float kHalfUp = 7.f;
 
 // Of the forward pass, two CTAs an SM.  With D = 64 a CTA's half of the tensor memory holds a block's scores, its P and the
 // result; with D = 128 P takes the scores' place, and the next scores have to wait for its product.
@@ -237,6 +240,7 @@ __global__ void __launch_bounds__(AttnShape<D>::kThreads, 2) attn_forward_kernel
     // scores of 0 where the scale is 0, and -inf stays -inf
     const float c = fmaxf(fabsf(p.scale) * kLog2e, kTinyScale);
     const bool negative = p.scale < 0.f;
+    constexpr float kUp = std::is_same<T, __half>::value ? kHalfUp : 0.f;
     float top = -INFINITY, total = 0.f;
     // One block of which COLS columns are looked at; MASKED: those that are seen, in `seen`.
     auto block = [&](auto cols, auto masked, int k, const uint32_t* seen) {
@@ -273,7 +277,7 @@ __global__ void __launch_bounds__(AttnShape<D>::kThreads, 2) attn_forward_kernel
         keep = exp2_fast((top - most) * c);
         top = most;
       }
-      const float shift = top == -INFINITY ? 0.f : -top * c;
+      const float shift = top == -INFINITY ? 0.f : fmaf(-top, c, kUp);
       const uint64_t cc = pack_f32x2(c, c), shifts = pack_f32x2(shift, shift);
       uint64_t part[4] = {0, 0, 0, 0};
       uint32_t w[COLS / 2];
@@ -358,7 +362,7 @@ __global__ void __launch_bounds__(AttnShape<D>::kThreads, 2) attn_forward_kernel
       }
     }
     if (exists && !real) put_zeros(out, p.dim);
-    if (exists && p.lse) attn_lse(p, b, h, i) = real ? (top * c + log2f(total)) * kLn2 : -INFINITY;
+    if (exists && p.lse) attn_lse(p, b, h, i) = real ? (top * c + (log2f(total) - kUp)) * kLn2 : -INFINITY;
     __syncwarp();   // what follows may write the same rows
     // a key that some row of the tile does not see, or a key that it sees, is not finite
     unsigned again = __ballot_sync(0xffffffffu, bad && real && ok);
