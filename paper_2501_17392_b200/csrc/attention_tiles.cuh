@@ -19,8 +19,8 @@
 //     turns.  With both results there is no such room: p and ds take the scores' and dp's place, and a group's next scores wait
 //     for their products.  Tiles of first tokens are seen by all queries: their blocks are shared out over several CTAs, whose
 //     float32 sums a last launch adds up.
-// In float16 ds is held times a power of two that the largest |do| and |v| allow without overflow, since ds is often below what
-// float16 holds at full precision.
+// In float16 P, p and ds are held times powers of two, since they are often below what float16 holds at full precision: P times
+// 2^7 (kHalfUp), p times 2^15, ds times what the largest |do| and |v| allow without overflow.
 //
 // Bound by the chain of a block rather than by a unit: forward, 8192 tokens, 12 heads of 64, window 1024, 66 us, with the
 // exponentials' unit busy for 45 % of the cycles, issue 30 %, matrix instructions 22 %; the operations alone would take 15 us.  Backward,
@@ -382,6 +382,7 @@ __global__ void __launch_bounds__(AttnShape<D>::kThreads, 2) attn_forward_kernel
 // ---- backward
 
 constexpr int kBlock = 64;                 // queries of a block (dk, dv)
+constexpr float kWeightUp = 32768.f;       // float16 p (at most 1) is held times this, so that small weights keep their precision too
 
 template <int D>
 struct DkvShape {
@@ -931,7 +932,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_dkv_kernel(const __grid_
       }
       uint32_t word[kBlock / 2];
 #pragma unroll
-      for (int e = 0; e < kBlock; e += 2) word[e / 2] = pack2<T>(x[e], x[e + 1]);
+      for (int e = 0; e < kBlock; e += 2) word[e / 2] = kTwo ? pack2<T>(x[e] * kWeightUp, x[e + 1] * kWeightUp) : pack2<T>(x[e], x[e + 1]);
       tmem_store32(cells, word);
 #pragma unroll
       for (int e = 0; e < kBlock; e += 2) word[e / 2] = pack2<T>(y[e], y[e + 1]);
@@ -954,7 +955,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_dkv_kernel(const __grid_
     // the first group writes dv, the second one dk
     const bool exists = at < p.tokens, real = at < n;
     T* to = head_row<T>(r ? p.dk : p.dv, b, exists ? at : 0, g);
-    const float factor = !ok ? NAN : r ? p.scale / hold : 1.f;   // a wait that ran out shows in the result
+    const float factor = !ok ? NAN : r ? p.scale / hold : kTwo ? 1.f / kWeightUp : 1.f;   // a wait that ran out shows in the result
     float* part = w.piece >= 0 ? p.part + w.part_of(p, b, r, 128, D) + row * D : nullptr;
     bool bad = false;
     if (count) {

@@ -39,3 +39,24 @@ def test_small_weights_beside_a_large_one(n, dtype):
         bound = bound - (2.0 ** -24 - 2.0 ** -32) * (sees(n, n, 0).double() @ w.v.abs())
     within(out[0], w.out.transpose(0, 1), bound.transpose(0, 1), "out")
     within(lse[0], w.lse, w.lse_bound, "lse")
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n", [40, 300, 1500])
+def test_small_weights_in_the_gradient_of_values(n, dtype):
+    """As under loss scaling: large do.  p, at most 1, is held times 2^15 in float16: half a step of its smallest numbers is
+    2^-40."""
+    q, k, v, do = one_large_weight(n, dtype, 1.0)
+    do *= 100.0
+    plan = B.WindowAttention(2, 64, n, window=n)
+    out, lse = torch.empty_like(q), torch.empty(1, 2, n, device="cuda")
+    plan.forward(q, k, v, out, lse=lse)
+    dq, dk, dv = (torch.empty_like(q) for _ in range(3))
+    plan.grad(do, q, k, v, out, lse, dq, dk, dv)
+    w = Plain(q[0], k[0], v[0], n, 0, plan.scale, do[0])
+    bound = w.dv_bound
+    if dtype == F16:
+        bound = bound - (2.0 ** -24 - 2.0 ** -40) * (sees(n, n, 0).double().mT @ do[0].transpose(0, 1).double().abs())
+    within(dv[0], w.dv.transpose(0, 1), bound.transpose(0, 1), "dv")
+    within(dq[0], w.dq.transpose(0, 1), w.dq_bound.transpose(0, 1), "dq")
+    within(dk[0], w.dk.transpose(0, 1), w.dk_bound.transpose(0, 1), "dk")
