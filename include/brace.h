@@ -677,8 +677,13 @@ typedef struct brace_window_attention {
  * (tokens / 32 + 2) heads / kv_heads of 2^31 or more), CUDA. */
 int brace_window_attention_forward(const brace_window_attention* e, brace_stream_t stream);
 
-/* Bytes of workspace of brace_window_attention_grad; 0 if the arguments are
- * invalid or not supported. */
+/* Bytes of workspace of brace_window_attention_grad with this window (it serves
+ * fewer tokens and shorter windows too), and of any window; 0 if the arguments
+ * are invalid or not supported.  Float32 sums make the difference: where more
+ * than 65,536 queries read a key, up to 4 kv_heads / heads times the size of
+ * 16-bit queries. */
+size_t brace_window_attention_window_workspace_bytes(int32_t batch, int32_t tokens, int32_t heads, int32_t kv_heads,
+                                                     int32_t dim, int32_t window, int32_t sinks);
 size_t brace_window_attention_workspace_bytes(int32_t batch, int32_t tokens, int32_t heads, int32_t kv_heads, int32_t dim,
                                               int32_t sinks);
 

@@ -163,6 +163,7 @@ SIGNATURES = {
     "brace_layer_norm_grad": (C.c_int, [C.POINTER(LayerNormArgs), C.c_void_p, C.c_size_t, C.c_void_p]),
     "brace_window_attention_forward": (C.c_int, [C.POINTER(WindowAttentionArgs), C.c_void_p]),
     "brace_window_attention_workspace_bytes": (C.c_size_t, [C.c_int32] * 6),
+    "brace_window_attention_window_workspace_bytes": (C.c_size_t, [C.c_int32] * 7),
     "brace_window_attention_grad": (C.c_int, [C.POINTER(WindowAttentionArgs), C.c_void_p, C.c_size_t, C.c_void_p]),
     "brace_clip_workspace_bytes": (C.c_size_t, [C.c_int32, C.POINTER(TensorArgs), C.c_int32]),
     "brace_gradient_norm": (C.c_int, [C.c_int32, C.POINTER(TensorArgs), C.c_int32, C.c_void_p, C.c_void_p, C.c_size_t,
@@ -785,7 +786,7 @@ class WindowAttention:
         self.kv_heads = heads if kv_heads is None else kv_heads
         self.window, self.sinks, self.scale = window, sinks, dim ** -0.5 if scale is None else scale
         if grad and workspace is None:
-            need = int(lib().brace_window_attention_workspace_bytes(batch, tokens, heads, self.kv_heads, dim, sinks))
+            need = int(lib().brace_window_attention_window_workspace_bytes(batch, tokens, heads, self.kv_heads, dim, window, sinks))
             workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=device)
         self.workspace = workspace
         self._args = WindowAttentionArgs()

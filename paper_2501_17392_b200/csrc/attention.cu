@@ -20,35 +20,53 @@ bool attn_served(int32_t batch, int32_t tokens, int32_t heads, int32_t kv_heads,
 
 constexpr int kSms = 148, kGradCtas = 4 * kSms;   // the most that tiles are shared out over, but for long sums
 
+// Head dimensions that the tensor cores' kernels serve.
+bool tiles_dim(int32_t dim) { return dim % 8 == 0 && dim <= 128; }
+
 int64_t tiles_of(int32_t tokens, int rows) { return ((int64_t)tokens + rows - 1) / rows; }
 
 // CTAs that few tiles are shared out over: one an SM, and of the kernels in float32, whose tiles have 64 rows, two after one another.
 int64_t spread(int rows) { return kSms * (128 / rows); }
 
-// Sums on the tensor cores are cut off, not rounded, at every step, which shows in float16 after some 100,000 queries: tiles of
-// keys whose sums are longer than 1024 blocks (65,536 queries) are shared out over up to four CTAs, more where tiles are few
-// (share_out).  8192 tokens, 64 heads on one of 64, two CTAs a tile against nine: error of dk 6.0e-4 -> 2.4e-4 and of dv 4.1e-4 -> 2.9e-4
-// (their rounding alone 2.0e-4), 5.3 -> 3.1 ms; bfloat16 4.3 -> 2.6 ms.  The workspace is then up to twice q's size at 32,768
-// tokens, 8 heads on one.
-int64_t long_pieces(int64_t blocks) { return std::min<int64_t>((blocks + 1023) / 1024, 4); }
+// Long sums (kLongBlocks) of up to some hundred tiles are shared out over up to four CTAs a tile, so that the last ones to work
+// keep the SMs busy; kLongCtas of them all together take a third of a GB of workspace at most.
+constexpr int kLongCtas = 4 * kGradCtas;
+int64_t long_pieces(int64_t blocks) { return std::min<int64_t>((blocks + kLongBlocks - 1) / kLongBlocks, 4); }
 
-// The most pieces, of all tiles together, that the gradient of dk and dv is made of (share_out).  More tokens never give fewer.
-int64_t most_pieces(int32_t batch, int32_t tokens, int32_t heads, int32_t kv_heads, int32_t sinks, int rows) {
-  if (heads == 0) return 0;
-  const int64_t each = (int64_t)batch * kv_heads, blocks = tiles_of(tokens, kBlock) * (heads / kv_heads);   // of a tile, at most
-  const int64_t first = tiles_of(std::min(sinks, tokens), rows) * each;
-  const int64_t tiles = tiles_of(tokens, rows) * each;
-  return std::max({std::min(std::max<int64_t>(kGradCtas, first), first * blocks), std::min<int64_t>(spread(rows), tiles * blocks),
-                   rows == 128 ? std::min<int64_t>(kGradCtas, tiles * blocks) : 0,
-                   rows == 128 && long_pieces(blocks) > 1 ? tiles * long_pieces(blocks) : 0});
+// Blocks of queries that a tile of keys behind the first tokens is seen by, at most.
+int64_t blocks_of(int32_t tokens, int32_t heads, int32_t kv_heads, int32_t window, int rows) {
+  return tiles_of((int32_t)std::min<int64_t>(tokens, (int64_t)window + rows - 1), kBlock) * (heads / kv_heads);
 }
 
-// What the gradient keeps in its workspace: two numbers of every query, the ranges, the pieces' sums.
+// What the gradient of dk and dv needs of float32 sums: the most pieces of all tiles that are shared out together (share_out),
+// and one sum for each tile whose CTA takes them out of the tensor cores now and then.  More tokens, or a longer window, never
+// give fewer.
+struct Parts {
+  int64_t shared, own;
+};
+Parts most_parts(int32_t batch, int32_t tokens, int32_t heads, int32_t kv_heads, int32_t window, int32_t sinks, int rows) {
+  if (heads == 0) return {0, 0};
+  const int64_t each = (int64_t)batch * kv_heads, blocks = blocks_of(tokens, heads, kv_heads, tokens, rows);   // of a tile, at most
+  const int64_t first = tiles_of(std::min(sinks, tokens), rows) * each;
+  const int64_t tiles = tiles_of(tokens, rows) * each;
+  Parts x;
+  x.shared = std::max(std::min(std::max<int64_t>(kGradCtas, first), first * blocks), std::min<int64_t>(spread(rows), tiles * blocks));
+  x.own = 0;
+  if (rows == 128) {
+    const int64_t seen = blocks_of(tokens, heads, kv_heads, window, rows);
+    x.shared = std::max({x.shared, std::min<int64_t>(kGradCtas, tiles * blocks), long_pieces(seen) > 1 ? std::min<int64_t>(kLongCtas, tiles * long_pieces(seen)) : 0});
+    if (seen > kLongBlocks) x.own = tiles;
+  }
+  return x;
+}
+
+// What the gradient keeps in its workspace: two numbers of every query, the ranges, float32 sums.  These are a few hundred MB at
+// most, but for windows of more than 65,536 / (heads / kv_heads) queries: there up to 4 kv_heads / heads times q's size more.
 struct GradPlan {
   int64_t padded;
   size_t off_shift, off_range, off_part, bytes;
 };
-GradPlan grad_plan(int32_t batch, int32_t tokens, int32_t heads, int32_t kv_heads, int32_t dim, int32_t sinks) {
+GradPlan grad_plan(int32_t batch, int32_t tokens, int32_t heads, int32_t kv_heads, int32_t dim, int32_t window, int32_t sinks) {
   GradPlan q;
   q.padded = round_up(tokens, kBlock);
   const int64_t numbers = round_up((int64_t)batch * heads * q.padded * 4, 256);
@@ -56,9 +74,13 @@ GradPlan grad_plan(int32_t batch, int32_t tokens, int32_t heads, int32_t kv_head
   q.off_range = (size_t)(2 * numbers);
   q.off_part = q.off_range + (size_t)round_up((int64_t)batch * kv_heads * 8, 256);
   // of the tensor cores' kernels or of those in float32, whichever the call will take
-  const int64_t wide = most_pieces(batch, tokens, heads, kv_heads, sinks, 128) * 128;
-  const int64_t narrow = most_pieces(batch, tokens, heads, kv_heads, sinks, kFloatRows) * kFloatRows;
-  q.bytes = q.off_part + (size_t)(std::max(wide, narrow) * 2 * (dim <= 64 ? 64 : dim <= 128 ? 128 : 256) * 4);
+  const Parts narrow = most_parts(batch, tokens, heads, kv_heads, window, sinks, kFloatRows);
+  int64_t rows = narrow.shared * kFloatRows;
+  if (tiles_dim(dim)) {
+    const Parts wide = most_parts(batch, tokens, heads, kv_heads, window, sinks, 128);
+    rows = std::max(rows, (wide.shared + wide.own) * 128);
+  }
+  q.bytes = q.off_part + (size_t)(rows * 2 * (dim <= 64 ? 64 : dim <= 128 ? 128 : 256) * 4);
   if (q.bytes < 256) q.bytes = 256;
   return q;
 }
@@ -120,7 +142,7 @@ bool tiles_ok(const brace_heads& x, const brace_window_attention* e, int heads) 
 }
 
 bool tiles_served(const brace_window_attention* e, bool grad) {
-  if (e->type == BRACE_TYPE_F32 || e->dim % 8 || e->dim > 128) return false;
+  if (e->type == BRACE_TYPE_F32 || !tiles_dim(e->dim)) return false;
   if (!tiles_ok(e->q, e, e->heads) || !tiles_ok(e->k, e, e->kv_heads) || !tiles_ok(e->v, e, e->kv_heads)) return false;
   if (!tiles_ok(e->out, e, e->heads)) return false;
   return !grad || (tiles_ok(e->dout, e, e->heads) && tiles_ok(e->dq, e, e->heads) && tiles_ok(e->dk, e, e->kv_heads) && tiles_ok(e->dv, e, e->kv_heads));
@@ -193,24 +215,26 @@ cudaError_t with_half_type(int type, F&& f) {
 // joins): 3 x 501 tokens, 2 heads read by 6, float32, 118 -> 96 us; 1000 tokens, 8 heads on one of 64, bfloat16, 128 -> 43 us.
 void share_out(const brace_window_attention* e, int rows, int least, AttnArgs& a) {
   const int64_t tiles = tiles_of(e->tokens, rows), first = tiles_of(std::min(e->sinks, e->tokens), rows), each = (int64_t)e->batch * e->kv_heads;
-  const int64_t window = std::min<int64_t>(e->tokens, (int64_t)a.window + rows - 1), blocks = tiles_of((int32_t)window, kBlock) * a.share;
+  const int64_t window = std::min<int64_t>(e->tokens, (int64_t)a.window + rows - 1), blocks = blocks_of(e->tokens, e->heads, e->kv_heads, a.window, rows);
+  const Parts most = most_parts(e->batch, e->tokens, e->heads, e->kv_heads, a.window, e->sinks, rows);
   a.first_tiles = (int)first;
   a.pieces = 0;
   if (first) {
     const int64_t even = (e->tokens + window - 1) / window;
-    a.pieces = (int)std::max<int64_t>(1, std::min(even, most_pieces(e->batch, e->tokens, e->heads, e->kv_heads, e->sinks, rows) / (first * each)));
+    a.pieces = (int)std::max<int64_t>(1, std::min(even, most.shared / (first * each)));
   }
   if (tiles * each * 2 <= kSms && blocks >= least) {
     a.first_tiles = (int)tiles;
     a.pieces = (int)std::min(spread(rows) / (tiles * each), blocks);
   }
-  // On the tensor cores: no sum too long, and four CTAs an SM one after another where that leaves each 64 blocks (window as long
-  // as the text, bfloat16: 4096 tokens, 16 heads on 2 of 128, 371 -> 280 us; 8192, 32 on 4, window 4096, 1480 -> 1348).
-  const int64_t split = rows == 128 ? std::max(long_pieces(blocks), std::min(kGradCtas / (tiles * each), blocks / 64)) : 1;
+  // On the tensor cores: long sums, and four CTAs an SM one after another where that leaves each 64 blocks (window as long as the
+  // text, bfloat16: 4096 tokens, 16 heads on 2 of 128, 371 -> 280 us; 8192, 32 on 4, window 4096, 1480 -> 1348).
+  const int64_t split = rows == 128 ? std::max(std::min(long_pieces(blocks), kLongCtas / (tiles * each)), std::min(kGradCtas / (tiles * each), blocks / 64)) : 1;
   if (split > 1 && (a.first_tiles == 0 || a.pieces <= split)) {     // no tile with first tokens in fewer pieces than above
     a.first_tiles = (int)tiles;
     a.pieces = (int)split;
   }
+  a.parts = (int)(a.first_tiles * a.pieces + (most.own ? tiles - a.first_tiles : 0));
 }
 
 }  // namespace
@@ -239,12 +263,17 @@ int brace_window_attention_forward(const brace_window_attention* e, brace_stream
   return err == cudaSuccess ? BRACE_OK : cuda_fail_no_ctx(err);
 }
 
-size_t brace_window_attention_workspace_bytes(int32_t batch, int32_t tokens, int32_t heads, int32_t kv_heads, int32_t dim,
-                                              int32_t sinks) {
-  if (!attn_sizes_ok(batch, tokens, heads) || kv_heads < 0 || dim < 1 || sinks < 0) return 0;
+size_t brace_window_attention_window_workspace_bytes(int32_t batch, int32_t tokens, int32_t heads, int32_t kv_heads, int32_t dim,
+                                                     int32_t window, int32_t sinks) {
+  if (!attn_sizes_ok(batch, tokens, heads) || kv_heads < 0 || dim < 1 || window < 1 || sinks < 0) return 0;
   if (heads > 0 && (kv_heads < 1 || heads % kv_heads)) return 0;
   if (!attn_served(batch, tokens, heads, kv_heads, dim)) return 0;
-  return grad_plan(batch, tokens, heads, kv_heads, dim, sinks).bytes;
+  return grad_plan(batch, tokens, heads, kv_heads, dim, window, sinks).bytes;
+}
+
+size_t brace_window_attention_workspace_bytes(int32_t batch, int32_t tokens, int32_t heads, int32_t kv_heads, int32_t dim,
+                                              int32_t sinks) {
+  return brace_window_attention_window_workspace_bytes(batch, tokens, heads, kv_heads, dim, INT32_MAX, sinks);
 }
 
 int brace_window_attention_grad(const brace_window_attention* e, void* d_workspace, size_t workspace_bytes,
@@ -255,14 +284,14 @@ int brace_window_attention_grad(const brace_window_attention* e, void* d_workspa
   if (!attn_common_ok(e, true) || !heads_ok(e->out, e, e->heads, false) || !heads_ok(e->dout, e, e->heads, false) ||
       !heads_ok(e->dq, e, e->heads, true) || !heads_ok(e->dk, e, e->kv_heads, true) || !heads_ok(e->dv, e, e->kv_heads, true))
     return BRACE_ERR_INVALID_ARG;
-  const size_t need = brace_window_attention_workspace_bytes(e->batch, e->tokens, e->heads, e->kv_heads, e->dim, e->sinks);
+  const size_t need = brace_window_attention_window_workspace_bytes(e->batch, e->tokens, e->heads, e->kv_heads, e->dim, e->window, e->sinks);
   if (!d_workspace || workspace_bytes < need || !aligned(d_workspace, 256)) return BRACE_ERR_WORKSPACE;
   AttnArgs a = attn_args(e);
   a.dout = head_ref(e->dout);
   a.dq = head_ref(e->dq);
   a.dk = head_ref(e->dk);
   a.dv = head_ref(e->dv);
-  const GradPlan q = grad_plan(e->batch, e->tokens, e->heads, e->kv_heads, e->dim, e->sinks);
+  const GradPlan q = grad_plan(e->batch, e->tokens, e->heads, e->kv_heads, e->dim, e->window, e->sinks);
   char* ws = (char*)d_workspace;
   a.delta = (float*)ws;
   a.shift = (float*)(ws + q.off_shift);

@@ -58,9 +58,10 @@ struct GradWork {
     return dkv ? head * p.share + (begin + k) / per_head : head / p.share;
   }
   __device__ __forceinline__ int first(int k) const { return dkv ? row0 + (begin + k) % per_head * width : keys.key(k, width); }
-  // where this piece's sums of dv (which = 0) or dk lie
+  // where this CTA's float32 sums of dv (which = 0) or dk lie: those of a piece, or of a tile of its own
   __device__ __forceinline__ int64_t part_of(const AttnArgs& p, int b, int which, int rows, int d) const {
-    return (((((int64_t)b * p.kv_heads + head) * p.first_tiles + tile) * p.pieces + piece) * 2 + which) * rows * d;
+    const int at = piece >= 0 ? tile * p.pieces + piece : p.first_tiles * (p.pieces - 1) + row0 / rows;
+    return ((((int64_t)b * p.kv_heads + head) * p.parts + at) * 2 + which) * rows * d;
   }
 };
 
@@ -75,7 +76,7 @@ __global__ void __launch_bounds__(128) attn_join_kernel(const AttnArgs p) {
 #pragma unroll
   for (int r = 0; r < 2; ++r) {
     T* to = head_row<T>(r ? p.dk : p.dv, b, j, g);
-    const float* from = p.part + ((((int64_t)b * p.kv_heads + g) * p.first_tiles + j / ROWS) * p.pieces * 2 + r) * ROWS * D + j % ROWS * D;
+    const float* from = p.part + ((((int64_t)b * p.kv_heads + g) * p.parts + j / ROWS * p.pieces) * 2 + r) * ROWS * D + j % ROWS * D;
 #pragma unroll
     for (int col = 0; col < D; col += 32) {
       const int d = col + lane;

@@ -111,6 +111,28 @@ __device__ __forceinline__ void put_zeros(T* row, int dim) {
   for (int i = 0; i < dim; i += 8) *reinterpret_cast<uint4*>(row + i) = make_uint4(0, 0, 0, 0);
 }
 
+// v += 32 columns of this row's sums at `part`.
+__device__ __forceinline__ void add_to(float (&v)[32], const float* part) {
+#pragma unroll
+  for (int e = 0; e < 32; e += 4) {
+    const float4 x = *reinterpret_cast<const float4*>(part + e);
+    v[e] += x.x;
+    v[e + 1] += x.y;
+    v[e + 2] += x.z;
+    v[e + 3] += x.w;
+  }
+}
+// 32 columns of a result in tensor memory to this row's sums at `part`, added to what is there (`more`) or the first ones.
+__device__ __forceinline__ void add_sums(uint32_t result, float* part, bool more) {
+  float v[32];
+  tmem_fetch32(result, v);
+  tmem_loaded();
+  tmem_use(v);
+  if (more) add_to(v, part);
+#pragma unroll
+  for (int e = 0; e < 32; e += 4) *reinterpret_cast<float4*>(part + e) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+}
+
 // grid: (tiles of 128 queries, heads, sequences)
 template <typename T, int D>
 __global__ void __launch_bounds__(AttnShape<D>::kThreads, 2) attn_forward_kernel(const __grid_constant__ AttnMaps maps, const AttnArgs p) {
@@ -382,6 +404,12 @@ __global__ void __launch_bounds__(AttnShape<D>::kThreads, 2) attn_forward_kernel
 // ---- backward
 
 constexpr int kBlock = 64;                 // queries of a block (dk, dv)
+// The tensor cores cut a sum off at every step of 16 queries, by 2e-7 of it on average: sums of one sign come out 1e-7 too small
+// for each step.  A CTA that sums more than kLongBlocks blocks (65,536 queries: 4e-4, close to half a step of float16) therefore
+// adds what it has to float32 sums in the workspace after every kFoldBlocks and begins anew.  17,000 tokens, 64 heads on one of
+// 64, window 4096, do > 0, one float16 CTA a tile: error of dv 1.5e-3 -> 2.4e-4 and of dk 4.4e-4 -> 2.1e-4
+// (their rounding alone 2.2e-4 and 2.1e-4).
+constexpr int kLongBlocks = 1024, kFoldBlocks = 256;
 constexpr float kWeightUp = 32768.f;       // float16 p (at most 1) is held times this, so that small weights keep their precision too
 
 template <int D>
@@ -760,8 +788,8 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_dkv_kernel(const __grid_
   const uint32_t base = (smem_addr(smem_raw) + 1023u) & ~1023u;
   const uint32_t ring = base + 2 * Shape::kTile, bars = ring + STAGES * Shape::kStage;
   const uint32_t full = bars, empty = full + 8 * STAGES, a_full = empty + 8 * STAGES;
-  // of each group: scores and dp are there; p and ds are there
-  const uint32_t s_full = a_full + 8, p_full = s_full + 16, o_full = p_full + 16, tail = o_full + 8;
+  // of each group: scores and dp are there; p and ds are there; the sums that it writes are complete
+  const uint32_t s_full = a_full + 8, p_full = s_full + 16, o_full = p_full + 16, tail = o_full + 16;
   volatile int* dead = (volatile int*)(smem_raw + (tail - smem_addr(smem_raw)));
   uint32_t* tmem_slot = (uint32_t*)(smem_raw + (tail + 8 - smem_addr(smem_raw)));
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -773,8 +801,8 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_dkv_kernel(const __grid_
       mbar_init(empty + 8 * s, 1);
     }
     mbar_init(a_full, 1);
-    mbar_init(o_full, 1);
     for (int r = 0; r < 2; ++r) {
+      mbar_init(o_full + 8 * r, 1);
       mbar_init(s_full + 8 * r, 1);
       mbar_init(p_full + 8 * r, 4);
     }
@@ -796,6 +824,10 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_dkv_kernel(const __grid_
   const int b = blockIdx.z, n = attn_length(p, b);
   const GradWork w(p, n, true, 128, kBlock);
   const int g = w.head, count = w.count;
+  // The first group takes dv out before block k's products where k is a multiple of kFoldBlocks, the second one dk before those
+  // of the block behind it: each of them before it hands over its own block.
+  const bool fold = count > kLongBlocks;
+  auto fresh = [&](int k, int r) { return fold && k > r && k % kFoldBlocks == r; };
 
   if (warp == 8) {                         // loads
     const bool lead = elect_one();
@@ -866,25 +898,43 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_dkv_kernel(const __grid_
 #pragma unroll
         for (int i = 0; i < kBlock / 16; ++i) {
           const uint64_t b1 = db + (uint64_t)(2048 * i >> 4), b2 = b1 + (Shape::kHalf >> 4);
-          const uint32_t add = k > 0 || i > 0;
-          mma_f16_ts(tmem + 256, a_p + 8 * i, b2, kSums, add);
-          mma_f16_ts(tmem + 256 + D, a_ds + 8 * i, b1, kSums, add);
+          mma_f16_ts(tmem + 256, a_p + 8 * i, b2, kSums, i > 0 || (k > 0 && !fresh(k, 0)));
+          mma_f16_ts(tmem + 256 + D, a_ds + 8 * i, b1, kSums, i > 0 || (k > 0 && !fresh(k, 1)));
           if (kTwo) mma_f16_ts(tmem + 256 + D, a_ds + 32 + 8 * i, b1, kSums, 1);
         }
         mma_commit<1>(empty + 8 * s);
+        if (k + 1 < count)
+          for (int x = 0; x < 2; ++x)
+            if (fresh(k + 1, x)) mma_commit<1>(o_full + 8 * x);
       }
       __syncwarp();
       if (k + 2 < count) ok = scores(k + 2);
     }
-    if (lead) mma_commit<1>(o_full);
+    if (lead) {
+      mma_commit<1>(o_full);
+      mma_commit<1>(o_full + 8);
+    }
     __syncwarp();
   } else {                                 // a row a thread; the groups take the blocks by turns
     const int r = warp >> 2, row = (warp & 3) * 32 + lane, at = w.row0 + row;
     const uint32_t mine = tmem + ((uint32_t)((warp & 3) * 32) << 16), cells = mine + 128 * r;
     const float c = p.scale * kLog2e, hold = count ? attn_grad_scale(p, b, g) : 1.f;
-    uint32_t phase = 0;
+    // the first group writes dv, the second one dk
+    const uint32_t result = mine + 256 + D * r;
+    float* part = w.piece >= 0 || fold ? p.part + w.part_of(p, b, r, 128, D) + row * D : nullptr;
+    uint32_t phase = 0, folds = 0;
     bool ok = true;
     for (int k = r; k < count; k += 2) {
+      if (fresh(k, r)) {
+        if (!mbar_wait(o_full + 8 * r, folds & 1u, dead)) {
+          ok = false;
+          break;
+        }
+        tc_fence_after();
+#pragma unroll 1
+        for (int col = 0; col < D; col += 32) add_sums(result + col, part + col, folds > 0);
+        ++folds;
+      }
       const int s = k % STAGES;
       // a block's numbers were copied by the asynchronous proxy: their own barrier makes them visible
       if (!mbar_wait(full + 8 * s, (uint32_t)(k / STAGES) & 1u, dead) || !mbar_wait(s_full + 8 * r, phase, dead)) {
@@ -950,22 +1000,21 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_dkv_kernel(const __grid_
       __syncwarp();
       if (lane == 0) mbar_arrive(p_full + 8 * r);
     }
-    if (ok && count) ok = mbar_wait(o_full, 0, dead);
+    if (ok && count) ok = mbar_wait(o_full + 8 * r, folds & 1u, dead);
     tc_fence_after();
-    // the first group writes dv, the second one dk
     const bool exists = at < p.tokens, real = at < n;
     T* to = head_row<T>(r ? p.dk : p.dv, b, exists ? at : 0, g);
     const float factor = !ok ? NAN : r ? p.scale / hold : kTwo ? 1.f / kWeightUp : 1.f;   // a wait that ran out shows in the result
-    float* part = w.piece >= 0 ? p.part + w.part_of(p, b, r, 128, D) + row * D : nullptr;
     bool bad = false;
     if (count) {
 #pragma unroll
       for (int col = 0; col < D; col += 32) {
         float o[32];
-        tmem_fetch32(mine + 256 + D * r + col, o);
+        tmem_fetch32(result + col, o);
         tmem_loaded();
         tmem_use(o);
-        if (part) {
+        if (folds) add_to(o, part + col);
+        if (w.piece >= 0) {
 #pragma unroll
           for (int e = 0; e < 32; e += 4)
             *reinterpret_cast<float4*>(part + col + e) = make_float4(o[e] * factor, o[e + 1] * factor, o[e + 2] * factor, o[e + 3] * factor);
@@ -975,10 +1024,10 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_dkv_kernel(const __grid_
           if (real) put_columns(to, o, factor, col, p.dim);
         }
       }
-    } else if (part) {
+    } else if (w.piece >= 0) {
       for (int col = 0; col < D; col += 4) *reinterpret_cast<float4*>(part + col) = make_float4(0.f, 0.f, 0.f, 0.f);
     }
-    if (exists && !real && !part) put_zeros(to, p.dim);
+    if (exists && !real && w.piece < 0) put_zeros(to, p.dim);
     __syncwarp();   // what follows may write the same rows
     unsigned again = __ballot_sync(0xffffffffu, bad && real && ok);
     for (; again; again &= again - 1) dkv_row<T>(p, b, g, w.row0 + (warp & 3) * 32 + __ffs(again) - 1, n, r == 1, r == 0);
