@@ -4,8 +4,8 @@
 // Forward.  A CTA has 128 queries and walks the blocks of 128 keys that they see: the first tokens', then the window's.  Per
 // block: scores S = Q K^T into tensor memory; a thread takes a query's scores into registers, masks them, brings its running
 // maximum up to date and writes exp2 of the differences, rounded to the inputs' type, back to tensor memory as P; P V is added
-// to the result there.  The result is scaled again only when a maximum has grown by more than 2^8 (the sum and P have room for
-// that).  Two CTAs share an SM: one's exponentials go on while the tensor cores work for the other, and one begins or ends
+// to the result there.  The result is scaled again only when a maximum has grown by more than 2^8, or 2^6.9 in float16 (the sum and
+// P have room for that).  Two CTAs share an SM: one's exponentials go on while the tensor cores work for the other, and one begins or ends
 // while the other is under way.
 //
 // Backward, in two kernels, so that every result is summed in one order.  Scores and dp = do v of a block go into tensor memory,
@@ -20,7 +20,7 @@
 //     for their products.  Tiles of first tokens are seen by all queries: their blocks are shared out over several CTAs, whose
 //     float32 sums a last launch adds up.
 // In float16 P, p and ds are held times powers of two, since they are often below what float16 holds at full precision: P times
-// 2^7 (kHalfUp), p times 2^15, ds times what the largest |do| and |v| allow without overflow.
+// 2^9 (AttnRange), p times 2^15, ds times what the largest |do| and |v| allow without overflow.
 //
 // Bound by the chain of a block rather than by a unit: forward, 8192 tokens, 12 heads of 64, window 1024, 66 us, with the
 // exponentials' unit busy for 45 % of the cycles, issue 30 %, matrix instructions 22 %; the operations alone would take 15 us.  Backward,
@@ -38,10 +38,15 @@
 namespace brace {
 
 constexpr int kAttnThreads = 320;          // of the backward pass: eight warps, one that loads, one that issues products
-constexpr float kGrown = 8.f;              // log2 of what a maximum may grow by before the result is scaled again
-// log2 of what float16 P is held times: float16 keeps no full precision below 2^-14, which the weights of many keys beside a
-// few large ones fall below.  2^7 times the 2^8 of a grown maximum is the most that it holds.
-constexpr float kHalfUp = 7.f;
+// log2 of what a maximum may grow by before the result is scaled again, and of what P is held times.  float16 keeps no full
+// precision below 2^-14, which the weights of many keys beside a few large ones fall below: 2^9 times the 2^6.9 of a grown
+// maximum is the most that it holds (weights of 2^-25 beside one of 1: off by 0.7 % with 2^7 and 2^8, 0.2 % with these; 2^11 and
+// 2^4 rescale more often: 4 x 4096 tokens, 16 heads on 4 of 128, 189 us for 180).
+template <typename T>
+struct AttnRange {
+  static constexpr bool kHalf = std::is_same<T, __half>::value;
+  static constexpr float kGrown = kHalf ? 6.9f : 8.f, kUp = kHalf ? 9.f : 0.f;
+};
 
 // Of the forward pass, two CTAs an SM.  With D = 64 a CTA's half of the tensor memory holds a block's scores, its P and the
 // result; with D = 128 P takes the scores' place, and the next scores have to wait for its product.
@@ -262,7 +267,7 @@ __global__ void __launch_bounds__(AttnShape<D>::kThreads, 2) attn_forward_kernel
     // scores of 0 where the scale is 0, and -inf stays -inf
     const float c = fmaxf(fabsf(p.scale) * kLog2e, kTinyScale);
     const bool negative = p.scale < 0.f;
-    constexpr float kUp = std::is_same<T, __half>::value ? kHalfUp : 0.f;
+    constexpr float kGrown = AttnRange<T>::kGrown, kUp = AttnRange<T>::kUp;
     float top = -INFINITY, total = 0.f;
     // One block of which COLS columns are looked at; MASKED: those that are seen, in `seen`.
     auto block = [&](auto cols, auto masked, int k, const uint32_t* seen) {
