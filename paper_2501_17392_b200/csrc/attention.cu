@@ -161,14 +161,22 @@ bool encode_map(CUtensorMap* map, const brace_heads& x, const brace_window_atten
              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <typename T, int D>
+// Blocks of 128 keys that a tile of queries walks, at most.
+int64_t key_blocks(int32_t tokens, int32_t window, int32_t sinks) {
+  if (window >= tokens) return tiles_of(tokens, 128);
+  return std::min(tiles_of(tokens, 128) + 1, tiles_of(std::min(sinks, tokens), 128) + tiles_of((int32_t)std::min<int64_t>(tokens, (int64_t)window + 127), 128));
+}
+
+template <typename T, int D, bool LONG>
 cudaError_t launch_forward(const AttnMaps& maps, const AttnArgs& a, cudaStream_t st) {
+  using Shape = AttnShape<D, LONG>;
+  static_assert(Shape::kSmem * Shape::kCtas <= 232448, "shared memory");
   static std::atomic<uint64_t> granted{0};
-  auto* kernel = attn_forward_kernel<T, D>;
-  const cudaError_t err = grant_smem((const void*)kernel, granted, AttnShape<D>::kSmem);
+  auto* kernel = attn_forward_kernel<T, D, LONG>;
+  const cudaError_t err = grant_smem((const void*)kernel, granted, Shape::kSmem);
   if (err != cudaSuccess) return err;
   const dim3 grid((unsigned)((a.tokens + 127) / 128), (unsigned)a.heads, (unsigned)a.batch);
-  return launch(kernel, grid, AttnShape<D>::kThreads, AttnShape<D>::kSmem, 1, st, maps, a);
+  return launch(kernel, grid, Shape::kThreads, Shape::kSmem, 1, st, maps, a);
 }
 
 // The gradient on the tensor cores.
@@ -255,7 +263,9 @@ int brace_window_attention_forward(const brace_window_attention* e, brace_stream
       return cuda_fail_no_ctx(cudaErrorNotSupported);
     const cudaError_t err = with_half_type(e->type, [&](auto t) {
       using T = decltype(t);
-      return e->dim <= 64 ? launch_forward<T, 64>(maps, a, st) : launch_forward<T, 128>(maps, a, st);
+      const bool longer = key_blocks(a.tokens, a.window, a.sinks) > (std::is_same<T, __half>::value ? 1 : 4) * (kLongKeys / 128);
+      if (e->dim <= 64) return longer ? launch_forward<T, 64, true>(maps, a, st) : launch_forward<T, 64, false>(maps, a, st);
+      return longer ? launch_forward<T, 128, true>(maps, a, st) : launch_forward<T, 128, false>(maps, a, st);
     });
     return err == cudaSuccess ? BRACE_OK : cuda_fail_no_ctx(err);
   }

@@ -49,17 +49,28 @@ struct AttnRange {
 };
 
 // Of the forward pass, two CTAs an SM.  With D = 64 a CTA's half of the tensor memory holds a block's scores, its P and the
-// result; with D = 128 P takes the scores' place, and the next scores have to wait for its product.
-template <int D>
+// result; with D = 128 P takes the scores' place, and the next scores have to wait for its product.  LONG keeps float32 sums in
+// shared memory beside (attn_forward_kernel); of D = 128 that leaves room for one CTA.
+template <int D, bool LONG>
 struct AttnShape {
   static constexpr int kKeys = 128;
   static constexpr bool kApart = D == 64;                  // P has a place of its own
   static constexpr int kTile = 128 * D * 2;                // bytes of 128 rows: D / 64 blocks of 64 columns
-  static constexpr int kStages = D == 64 ? 5 : 2;
-  static constexpr int kSmem = 1024 + (1 + kStages) * kTile + 256;
+  static constexpr int kStages = LONG ? (D == 64 ? 3 : 4) : D == 64 ? 5 : 2;
+  static constexpr int kKept = LONG ? 128 * D * 4 : 0;     // bytes of the sums
+  static constexpr int kSmem = 1024 + (1 + kStages) * kTile + kKept + 256;
+  static constexpr int kCtas = LONG && D == 128 ? 1 : 2;   // of an SM
   static constexpr int kP = kApart ? 128 : 0, kResult = kApart ? 192 : 128, kColumns = 256;   // of tensor memory
   static constexpr int kThreads = 192;                     // four warps of queries, one that loads, one that issues products
 };
+
+// Sums on the tensor cores are cut off at every step of 16 keys (or queries), by 2e-7 of the sum on average: sums of one sign come out
+// 1e-7 too small for each step.  262,144 keys, values of one sign: 1.7e-3 too small, where half a step of float16 is 4.9e-4 and
+// of bfloat16 3.9e-3.  From 65,536 keys on in float16, four times as many in bfloat16, what has been summed is therefore taken out
+// after every 16,384 of them and added up in float32, to nearest: 1.0e-4.  131,072 tokens, 2 heads on one, all keys, float16: heads of
+// 64 5.8 -> 5.9 ms, heads of 128 (one CTA an SM) 8.4 -> 11.4.
+constexpr int kLongKeys = 65536;
+constexpr int kFoldKeys = 128;             // blocks of keys
 
 struct AttnMaps {
   CUtensorMap q, k, v, dout;               // (dimension, token, head, sequence); boxes of 64 x 128, or of 64 x kBlock
@@ -138,14 +149,15 @@ __device__ __forceinline__ void add_sums(uint32_t result, float* part, bool more
   for (int e = 0; e < 32; e += 4) *reinterpret_cast<float4*>(part + e) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
 }
 
-// grid: (tiles of 128 queries, heads, sequences)
-template <typename T, int D>
-__global__ void __launch_bounds__(AttnShape<D>::kThreads, 2) attn_forward_kernel(const __grid_constant__ AttnMaps maps, const AttnArgs p) {
-  using Shape = AttnShape<D>;
+// LONG: sums over more than kLongKeys.  grid: (tiles of 128 queries, heads, sequences)
+template <typename T, int D, bool LONG>
+__global__ void __launch_bounds__(AttnShape<D, LONG>::kThreads, AttnShape<D, LONG>::kCtas)
+    attn_forward_kernel(const __grid_constant__ AttnMaps maps, const AttnArgs p) {
+  using Shape = AttnShape<D, LONG>;
   constexpr int STAGES = Shape::kStages, KEYS = Shape::kKeys;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t base = (smem_addr(smem_raw) + 1023u) & ~1023u;
-  const uint32_t ring = base + Shape::kTile, bars = ring + STAGES * Shape::kTile;
+  const uint32_t ring = base + Shape::kTile, bars = ring + STAGES * Shape::kTile + Shape::kKept;
   const uint32_t full = bars, empty = full + 8 * STAGES, q_full = empty + 8 * STAGES;
   // scores are there, scores have been read, P is there, its product is complete
   const uint32_t s_full = q_full + 8, s_free = s_full + 8, p_full = s_free + 8, p_done = p_full + 8, tail = p_done + 8;
@@ -254,7 +266,8 @@ __global__ void __launch_bounds__(AttnShape<D>::kThreads, 2) attn_forward_kernel
 #pragma unroll
         for (int i = 0; i < KEYS / 16; ++i)
           if (i < 2 || !narrow(k))
-            mma_f16_ts(tmem + Shape::kResult, tmem + Shape::kP + 8 * i, db + i * (2048 >> 4), kValues, k > 0 || i > 0);
+            mma_f16_ts(tmem + Shape::kResult, tmem + Shape::kP + 8 * i, db + i * (2048 >> 4), kValues,
+                       i > 0 || (LONG ? k % kFoldKeys > 0 : k > 0));
         mma_commit<1>(p_done);
         mma_commit<1>(empty + 8 * s);
       }
@@ -268,6 +281,7 @@ __global__ void __launch_bounds__(AttnShape<D>::kThreads, 2) attn_forward_kernel
     const float c = fmaxf(fabsf(p.scale) * kLog2e, kTinyScale);
     const bool negative = p.scale < 0.f;
     constexpr float kGrown = AttnRange<T>::kGrown, kUp = AttnRange<T>::kUp;
+    float* kept = (float*)(smem_raw + (ring + STAGES * Shape::kTile - smem_addr(smem_raw))) + row;      // column x at 128 x
     float top = -INFINITY, total = 0.f;
     // One block of which COLS columns are looked at; MASKED: those that are seen, in `seen`.
     auto block = [&](auto cols, auto masked, int k, const uint32_t* seen) {
@@ -321,7 +335,26 @@ __global__ void __launch_bounds__(AttnShape<D>::kThreads, 2) attn_forward_kernel
       // issued before these scores)
       if (Shape::kApart && k && !mbar_wait(p_done, (uint32_t)(k - 1) & 1u, dead)) return false;
       tc_fence_after();
-      if (rescale && k) {
+      if constexpr (LONG) {
+        if (k && (rescale || k % kFoldKeys == 0)) {      // the sums before, and the result where the product begins anew
+#pragma unroll 1
+          for (int x = 0; x < D; x += 16) {
+            float o[16];
+            tmem_load16(result + x, o);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              float& sum = kept[(x + e) * 128];
+              if (k % kFoldKeys == 0)
+                sum = (k > kFoldKeys ? sum + o[e] : o[e]) * keep;
+              else {
+                if (k > kFoldKeys) sum *= keep;
+                o[e] *= keep;
+              }
+            }
+            if (k % kFoldKeys) tmem_store16(result + x, reinterpret_cast<const uint32_t*>(o));
+          }
+        }
+      } else if (rescale && k) {
 #pragma unroll
         for (int x = 0; x < D; x += 32) {
           float o[32];
@@ -383,6 +416,9 @@ __global__ void __launch_bounds__(AttnShape<D>::kThreads, 2) attn_forward_kernel
         tmem_fetch32(result + x, o);
         tmem_loaded();
         tmem_use(o);
+        if (LONG && count > kFoldKeys)
+#pragma unroll
+          for (int e = 0; e < 32; ++e) o[e] += kept[(x + e) * 128];
 #pragma unroll
         for (int e = 0; e < 32; ++e) bad |= !isfinite(o[e]) && x + e < p.dim;
         if (real) put_columns(out, o, factor, x, p.dim);
@@ -409,9 +445,8 @@ __global__ void __launch_bounds__(AttnShape<D>::kThreads, 2) attn_forward_kernel
 // ---- backward
 
 constexpr int kBlock = 64;                 // queries of a block (dk, dv)
-// The tensor cores cut a sum off at every step of 16 queries, by 2e-7 of it on average: sums of one sign come out 1e-7 too small
-// for each step.  A CTA that sums more than kLongBlocks blocks (65,536 queries: 4e-4, close to half a step of float16) therefore
-// adds what it has to float32 sums in the workspace after every kFoldBlocks and begins anew.  17,000 tokens, 64 heads on one of
+// Long sums as in the forward pass: a CTA that sums more than kLongBlocks blocks (65,536 queries: 4e-4 are lost, close to half a
+// step of float16) adds what it has to float32 sums in the workspace after every kFoldBlocks and begins anew.  17,000 tokens, 64 heads on one of
 // 64, window 4096, do > 0, one float16 CTA a tile: error of dv 1.5e-3 -> 2.4e-4 and of dk 4.4e-4 -> 2.1e-4
 // (their rounding alone 2.2e-4 and 2.1e-4).
 constexpr int kLongBlocks = 1024, kFoldBlocks = 256;

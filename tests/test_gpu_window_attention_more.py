@@ -7,7 +7,7 @@ import pytest
 import torch
 
 from paper_2501_17392_b200 import brace as B
-from test_gpu_window_attention import BF16, F16, F32, Plain, randn, sees, within
+from test_gpu_window_attention import BF16, F16, F32, Plain, randn, sees, u, within
 
 pytestmark = pytest.mark.gpu
 
@@ -145,3 +145,23 @@ def test_fewer_tokens_than_the_plan_is_for(n, dtype):
         w = Plain(q[i], k[i], v[i], 90, 3, plan.scale, do[i])
         for got, name in zip((out, *grads), ("out", "dq", "dk", "dv")):
             within(got[i], getattr(w, name).transpose(0, 1), getattr(w, name + "_bound").transpose(0, 1), name)
+
+
+@pytest.mark.parametrize("dtype,n,dim,ramp", [(F16, 262144, 64, False), (F16, 262144, 128, True), (F16, 200001, 64, True),
+                                              (BF16, 600000, 128, False), (BF16, 540001, 64, True)])
+def test_sums_of_one_sign_over_many_keys(dtype, n, dim, ramp):
+    """As over many queries: 262,144 keys with values of one sign came out 1.7e-3 too small, 9 times float16's rounding.
+    `ramp`: later keys have larger scores, so that results are scaled again under way."""
+    q, k, v = (randn(1, n, 1, dim, seed=s) for s in range(3))
+    if ramp:
+        k *= torch.linspace(0.2, 2.5, n, device="cuda")[:, None, None]
+    q, k, v = q.to(dtype), k.to(dtype), v.abs().to(dtype)
+    out, lse = torch.empty_like(q), torch.empty(1, 1, n, device="cuda")
+    plan = B.WindowAttention(1, dim, n, window=n, sinks=5, grad=False)
+    plan.forward(q, k, v, out, lse=lse)
+    for a in (0, 5000, 16300, n // 2, n - 300):
+        i = torch.arange(a, a + 200, device="cuda")
+        s = (q[0, i, 0].double() @ k[0, :, 0].double().T * plan.scale).masked_fill(torch.arange(n, device="cuda") > i[:, None], -math.inf)
+        assert worse(out[0, i, 0], s.softmax(-1) @ v[0, :, 0].double()) < (1.5 if a else 2)
+        # a score is off by (dim + 2) 2^-23 of its products' absolute sum, below 8 dim in all
+        assert float((lse[0, 0, i] - s.logsumexp(-1)).abs().max()) < plan.scale * (dim + 2) * 2.0 ** -23 * 8 * dim + 2.0 ** -19 + 20 * u
