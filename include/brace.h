@@ -681,7 +681,8 @@ int brace_window_attention_forward(const brace_window_attention* e, brace_stream
  * fewer tokens and shorter windows too), and of any window; 0 if the arguments
  * are invalid or not supported.  Float32 sums make the difference: where more
  * than 65,536 queries read a key, up to 4 kv_heads / heads times the size of
- * 16-bit queries. */
+ * 16-bit queries, and where a query sees more than 65,536 keys, at least twice
+ * that size. */
 size_t brace_window_attention_window_workspace_bytes(int32_t batch, int32_t tokens, int32_t heads, int32_t kv_heads,
                                                      int32_t dim, int32_t window, int32_t sinks);
 size_t brace_window_attention_workspace_bytes(int32_t batch, int32_t tokens, int32_t heads, int32_t kv_heads, int32_t dim,

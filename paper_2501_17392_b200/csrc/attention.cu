@@ -60,8 +60,15 @@ Parts most_parts(int32_t batch, int32_t tokens, int32_t heads, int32_t kv_heads,
   return x;
 }
 
+// Blocks of 128 keys that a tile of queries walks, at most.
+int64_t key_blocks(int32_t tokens, int32_t window, int32_t sinks) {
+  if (window >= tokens) return tiles_of(tokens, 128);
+  return std::min(tiles_of(tokens, 128) + 1, tiles_of(std::min(sinks, tokens), 128) + tiles_of((int32_t)std::min<int64_t>(tokens, (int64_t)window + 127), 128));
+}
+
 // What the gradient keeps in its workspace: two numbers of every query, the ranges, float32 sums.  These are a few hundred MB at
-// most, but for windows of more than 65,536 / (heads / kv_heads) queries: there up to 4 kv_heads / heads times q's size more.
+// most, but for windows of more than 65,536 / (heads / kv_heads) queries, where there are up to 4 kv_heads / heads times q's size
+// more, and those of more than 65,536 keys, where there is at least twice q's size.
 struct GradPlan {
   int64_t padded;
   size_t off_shift, off_range, off_part, bytes;
@@ -79,6 +86,8 @@ GradPlan grad_plan(int32_t batch, int32_t tokens, int32_t heads, int32_t kv_head
   if (tiles_dim(dim)) {
     const Parts wide = most_parts(batch, tokens, heads, kv_heads, window, sinks, 128);
     rows = std::max(rows, (wide.shared + wide.own) * 128);
+    // dq's come first, in the same place
+    if (key_blocks(tokens, window, sinks) > kLongKeys / 128) rows = std::max(rows, tiles_of(tokens, 128) * batch * heads * 64);
   }
   q.bytes = q.off_part + (size_t)(rows * 2 * (dim <= 64 ? 64 : dim <= 128 ? 128 : 256) * 4);
   if (q.bytes < 256) q.bytes = 256;
@@ -159,12 +168,6 @@ bool encode_map(CUtensorMap* map, const brace_heads& x, const brace_window_atten
   return enc(map, e->type == BRACE_TYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, x.d, dim,
              stride, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
-// Blocks of 128 keys that a tile of queries walks, at most.
-int64_t key_blocks(int32_t tokens, int32_t window, int32_t sinks) {
-  if (window >= tokens) return tiles_of(tokens, 128);
-  return std::min(tiles_of(tokens, 128) + 1, tiles_of(std::min(sinks, tokens), 128) + tiles_of((int32_t)std::min<int64_t>(tokens, (int64_t)window + 127), 128));
 }
 
 template <typename T, int D, bool LONG>

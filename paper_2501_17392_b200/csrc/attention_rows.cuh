@@ -35,7 +35,8 @@ struct AttnArgs {
   int64_t stride_lse, head_lse;
   float *delta, *shift;                    // [b][h][padded]: delta_i, and -log2(e) lse_i
   uint32_t* range;                         // [b][kv head][2]: bits of the largest |do| and |v|
-  float* part;                             // float32 sums of dv and dk: [b][kv head][parts][dv, dk][rows][D]
+  float* part;                             // float32 sums: of dv and dk [b][kv head][parts][dv, dk][rows][D], before that of dq
+                                           // [b][head][tile][rows][D]
   int64_t padded;                          // tokens, rounded up to 64
   int first_tiles, pieces, parts;          // parts: the shared tiles' pieces, then (of long sums) one of each other tile
   const int32_t* lengths;

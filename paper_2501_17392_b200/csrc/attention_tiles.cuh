@@ -588,6 +588,10 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_dq_kernel(const __grid_c
   // few blocks are walked twice: first for delta, then for ds
   const int blocks = w.count, first_pass = blocks * 128 <= kExactKeys ? blocks : 0, count = blocks + first_pass;
   auto block_of = [&](int k) { return k < first_pass ? k : k - first_pass; };
+  // long sums as in the forward pass (there is one pass over so many keys): the sums taken out lie in the workspace.  600,000 keys
+  // that are the values, float16: dq 1.1e-3 too small -> 4e-5
+  const bool fold = count > kLongKeys / BLOCK;
+  auto fresh = [&](int k) { return fold && k > 0 && k % kFoldKeys == 0; };
 
   if (warp == 8) {                         // loads
     const bool lead = elect_one();
@@ -658,7 +662,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_dq_kernel(const __grid_c
         const uint64_t bk = desc_k + (uint64_t)(sk * Shape::kTile >> 4);
 #pragma unroll
         for (int i = 0; i < BLOCK / 16; ++i) {
-          mma_f16_ts(tmem + 256, tmem + Shape::kDs + 8 * i, bk + i * (2048 >> 4), kSums, k > first_pass || i > 0);
+          mma_f16_ts(tmem + 256, tmem + Shape::kDs + 8 * i, bk + i * (2048 >> 4), kSums, i > 0 || (k > first_pass && !fresh(k)));
           if (kTwo) mma_f16_ts(tmem + 256, tmem + Shape::kDs + 64 + 8 * i, bk + i * (2048 >> 4), kSums, 1);
         }
         mma_commit<1>(empty_k + 8 * sk);
@@ -671,6 +675,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_dq_kernel(const __grid_c
     const uint32_t mine = tmem + ((uint32_t)((warp & 3) * 32) << 16), words = mine + Shape::kDs + 32 * half;
     const float c = p.scale * kLog2e, hold = count ? attn_grad_scale(p, b, g) : 1.f;
     float shift = 0.f, delta = 0.f, sum = 0.f;      // sum: of p dp
+    float* part = p.part + ((((int64_t)b * p.heads + h) * gridDim.x + w.row0 / 128) * 128 + row) * D;
     bool ok = true;
     auto meet = [&] {                      // all rows' sums are in shared memory
       __syncwarp();
@@ -765,6 +770,9 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_dq_kernel(const __grid_c
         break;
       }
       tc_fence_after();
+      if (half == 0 && fresh(k))
+#pragma unroll 1
+        for (int col = 0; col < D; col += 32) add_sums(mine + 256 + col, part + col, k > kFoldKeys);
       uint32_t word[COLS / 2];
 #pragma unroll
       for (int e = 0; e < COLS; e += 2) word[e / 2] = pack2<T>(x[e], x[e + 1]);
@@ -796,6 +804,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_dq_kernel(const __grid_c
           tmem_fetch32(mine + 256 + col, o);
           tmem_loaded();
           tmem_use(o);
+          if (fold) add_to(o, part + col);
 #pragma unroll
           for (int e = 0; e < 32; ++e) bad |= !isfinite(o[e]) && col + e < p.dim;
           if (real) put_columns(to, o, factor, col, p.dim);

@@ -7,7 +7,7 @@ import pytest
 import torch
 
 from paper_2501_17392_b200 import brace as B
-from test_gpu_window_attention import BF16, F16, F32, Plain, randn, sees, u, within
+from test_gpu_window_attention import BF16, F16, F32, U, Plain, randn, sees, u, within
 
 pytestmark = pytest.mark.gpu
 
@@ -125,6 +125,57 @@ def test_sums_of_one_sign_over_many_queries(dtype, dim, sinks):
     assert worse(dk[0, :m, 0], wk) < 1.5 and worse(dv[0, :m, 0], wv) < 1.5
     assert torch.equal(dk[:, m:], before[0][:, m:]) and torch.equal(dv[:, m:], before[1][:, m:])
     assert bool((whole[:at] == 255).all()) and bool((whole[at + need:] == 255).all())
+
+
+def dq_of_long_text(k, v, do, seed=0):
+    """dq of a text with one head, all of which is seen, in a workspace of exactly the size that is asked for (it holds dq's sums
+    and, later, those of dk and dv); a function that gives some rows' exact values and the sums of absolute values."""
+    n, dim = k.shape[1], k.shape[3]
+    q = randn(1, n, 1, dim, seed=seed).to(k.dtype)
+    need = int(B.lib().brace_window_attention_window_workspace_bytes(1, n, 1, 1, dim, n, 0))
+    whole = torch.full((need + 1024,), 255, dtype=torch.uint8, device="cuda")
+    at = -whole.data_ptr() % 256 + 256
+    plan = B.WindowAttention(1, dim, n, window=n, workspace=whole[at:at + need])
+    out, lse = torch.empty_like(q), torch.empty(1, 1, n, device="cuda")
+    plan.forward(q, k, v, out, lse=lse)
+    dq, dk, dv = (torch.empty_like(t) for t in (q, k, v))
+    plan.grad(do, q, k, v, out, lse, dq, dk, dv)
+    assert bool((whole[:at] == 255).all()) and bool((whole[at + need:] == 255).all())
+
+    def exact(i):
+        p = (q[0, i, 0].double() @ k[0, :, 0].double().T * plan.scale).masked_fill(torch.arange(n, device="cuda") > i[:, None], -math.inf).softmax(-1)
+        # delta as the formula has it, from the rounded output
+        ds = p * (do[0, i, 0].double() @ v[0, :, 0].double().T - (do[0, i, 0].double() * out[0, i, 0].double()).sum(-1, keepdim=True))
+        return ds @ k[0, :, 0].double() * plan.scale, ds.abs() @ k[0, :, 0].double().abs() * plan.scale
+
+    return dq[0, :, 0], exact
+
+
+@pytest.mark.parametrize("dtype,n,dim", [(F16, 140001, 64), (F16, 131072, 128), (F16, 600000, 64), (BF16, 600000, 64)])
+def test_sums_of_one_sign_over_many_keys_in_the_gradient(dtype, n, dim):
+    """Keys that are the values: a query's dq grows evenly along the text, as its do.  What the steps of 16 keys cut off is at most
+    1e-7 of the whole each, twice in float16's two planes; without taking sums out 600,000 keys leave 1.1e-3, 5.6 times
+    float16's rounding.  Taken out every 16,384 keys it is at most 2 * 1.0e-4, as much as the rounding: a factor below sqrt(2)."""
+    v, do = randn(1, n, 1, dim, seed=1).to(dtype), randn(1, n, 1, dim, seed=2, scale=1e-2).to(dtype)
+    dq, exact = dq_of_long_text(v, v, do)
+    i = torch.arange(n - 200, n, device="cuda")
+    assert worse(dq[i], exact(i)[0]) < 1.5
+
+
+@pytest.mark.parametrize("dtype,n,dim", [(F16, 140001, 64), (F16, 131072, 128), (BF16, 140001, 64)])
+def test_sums_over_many_keys_that_nearly_cancel(dtype, n, dim):
+    """dq of values that rise along the text and keys of one sign: what is left is some 240 times smaller than the sums of
+    absolute values.  A step cuts off 2e-7 of what is summed so far, which is at most the absolute sum of its 16,384 keys
+    (of the first 65,536 where there are fewer: 4096 steps, twice as many in float16, of a sum that is half of it on average):
+    2048 * 2e-7 = 4.1e-4, or 8192 * 2e-7 / 2 = 8.2e-4, of the absolute sums and the rounding of the result (another 2^-8 at
+    most, and of ds to bfloat16 on the way)."""
+    k, v, do = (randn(1, n, 1, dim, seed=s) for s in (1, 2, 3))
+    v += torch.linspace(-1, 1, n, device="cuda")[:, None, None]
+    dq, exact = dq_of_long_text(k.abs().to(dtype), v.to(dtype), (do.abs() * 1e-2).to(dtype))
+    for a in (60000, n - 200):
+        i = torch.arange(a, a + 200, device="cuda")
+        want, size = exact(i)
+        within(dq[i], want, (4.1e-4 if a > 65536 else 8.2e-4) * size + U[dtype] * want.abs())
 
 
 @pytest.mark.parametrize("dtype", TYPES)

@@ -30,8 +30,8 @@ def test_workspace_of_a_window():
 @pytest.mark.parametrize("heads,kv,dim", [(32, 32, 128), (16, 4, 64), (8, 8, 200)])
 def test_long_texts_with_short_windows_take_little(n, heads, kv, dim):
     """Two numbers of a query, and a third of a GB at most where no key is read by more than 65,536 queries; else 4 kv / heads
-    of the queries' size more (head dimensions that the tensor cores do not take need no such sums)."""
+    of the queries' size more, or twice that size (head dimensions that the tensor cores do not take need no such sums)."""
     numbers, most = 8 * n * heads, 4 * 592 * 2 * 128 * max(dim, 128) * 4
     assert B.lib().brace_window_attention_window_workspace_bytes(1, n, heads, kv, dim, 1024, 4) <= numbers + most + 4096
-    own = 0 if dim > 128 else 4 * (n + 127) * kv * dim * 2
+    own = 0 if dim > 128 else (n + 127) * dim * 2 * max(4 * kv, 2 * heads)
     assert B.lib().brace_window_attention_workspace_bytes(1, n, heads, kv, dim, 4) <= numbers + most + own + 4096
