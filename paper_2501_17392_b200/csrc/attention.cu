@@ -266,7 +266,8 @@ int brace_window_attention_forward(const brace_window_attention* e, brace_stream
       return cuda_fail_no_ctx(cudaErrorNotSupported);
     const cudaError_t err = with_half_type(e->type, [&](auto t) {
       using T = decltype(t);
-      const bool longer = key_blocks(a.tokens, a.window, a.sinks) > (std::is_same<T, __half>::value ? 1 : 4) * (kLongKeys / 128);
+      const int least = e->dim > 64 && !std::is_same<T, __half>::value ? 4 * kLongKeys : kLongKeys;
+      const bool longer = key_blocks(a.tokens, a.window, a.sinks) > least / 128;
       if (e->dim <= 64) return longer ? launch_forward<T, 64, true>(maps, a, st) : launch_forward<T, 64, false>(maps, a, st);
       return longer ? launch_forward<T, 128, true>(maps, a, st) : launch_forward<T, 128, false>(maps, a, st);
     });

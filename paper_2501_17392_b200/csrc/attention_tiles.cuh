@@ -64,11 +64,11 @@ struct AttnShape {
   static constexpr int kThreads = 192;                     // four warps of queries, one that loads, one that issues products
 };
 
-// Sums on the tensor cores are cut off at every step of 16 keys (or queries), by 2e-7 of the sum on average: sums of one sign come out
-// 1e-7 too small for each step.  262,144 keys, values of one sign: 1.7e-3 too small, where half a step of float16 is 4.9e-4 and
-// of bfloat16 3.9e-3.  From 65,536 keys on in float16, four times as many in bfloat16, what has been summed is therefore taken out
-// after every 16,384 of them and added up in float32, to nearest: 1.0e-4.  131,072 tokens, 2 heads on one, all keys, float16: heads of
-// 64 5.8 -> 5.9 ms, heads of 128 (one CTA an SM) 8.4 -> 11.4.
+// Sums on the tensor cores are cut off at every step of 16 keys (or queries), by 2e-7 of the sum on average: sums of one sign come
+// out 1e-7 too small for each step.  262,144 keys, values of one sign: 1.7e-3 too small, where half a step of float16 is 4.9e-4
+// and of bfloat16 3.9e-3.  From 65,536 keys on (four times as many in bfloat16 with D = 128, where it costs most) what has been
+// summed is therefore taken out after every 16,384 of them and added up in float32, to nearest: 1.0e-4.  131,072 tokens, 2 heads
+// on one, all keys, float16: heads of 64 5.8 -> 5.9 ms, heads of 128 (one CTA an SM) 8.4 -> 11.4.
 constexpr int kLongKeys = 65536;
 constexpr int kFoldKeys = 128;             // blocks of keys
 
