@@ -673,7 +673,9 @@ typedef struct brace_window_attention {
 } brace_window_attention;
 
 /* Errors: INVALID_ARG (null, size out of range, bad type, misaligned pointer,
- * negative stride, rows of a result or of lse that overlap), UNSUPPORTED (also
+ * negative stride, rows of a result or of lse that overlap: of each dimension
+ * a step is no shorter than what those of smaller strides reach over),
+ * UNSUPPORTED (also
  * (tokens / 32 + 2) heads / kv_heads of 2^31 or more), CUDA. */
 int brace_window_attention_forward(const brace_window_attention* e, brace_stream_t stream);
 

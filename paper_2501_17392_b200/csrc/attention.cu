@@ -3,6 +3,8 @@
 
 #include <algorithm>
 #include <cmath>
+#include <initializer_list>
+#include <utility>
 
 #include "attention_host.cuh"
 #include "attention_tiles.cuh"
@@ -102,12 +104,28 @@ int attn_check(const brace_window_attention* e) {
   return BRACE_OK;
 }
 
+// Whether runs of `run` elements lie apart: of each dimension (elements, stride) with more than one element, from the smallest
+// stride on, a step is no shorter than what all those before it reach over.
+bool apart(int64_t run, std::initializer_list<std::pair<int64_t, int64_t>> dims) {
+  std::pair<int64_t, int64_t> by_stride[3];
+  int n = 0;
+  for (const auto& d : dims)
+    if (d.first > 1) by_stride[n++] = {d.second, d.first};
+  std::sort(by_stride, by_stride + n);
+  for (int i = 0; i < n; ++i) {
+    const int64_t stride = by_stride[i].first, more = by_stride[i].second - 1;
+    if (stride < run) return false;
+    run = stride > (INT64_MAX - run) / more ? INT64_MAX : run + stride * more;
+  }
+  return true;
+}
+
 // A tensor that is read: any strides that are not negative; one that is written: a place of its own for every row.
 bool heads_ok(const brace_heads& x, const brace_window_attention* e, int heads, bool written) {
   if (!x.d || !aligned(x.d, (size_t)elem_bytes(e->type))) return false;
   if (x.ld < 0 || x.head < 0 || x.stride < 0) return false;
   if (!written) return true;
-  return (e->tokens < 2 || x.ld >= e->dim) && (heads < 2 || x.head >= e->dim) && (e->batch < 2 || x.stride >= e->dim);
+  return apart(e->dim, {{e->tokens, x.ld}, {heads, x.head}, {e->batch, x.stride}});
 }
 
 HeadRef head_ref(const brace_heads& x) { return HeadRef{x.d, x.ld, x.head, x.stride}; }
@@ -117,7 +135,7 @@ bool attn_common_ok(const brace_window_attention* e, bool grad) {
     return false;
   if (!aligned(e->d_lengths, 4) || !aligned(e->d_lse, 4) || (grad && !e->d_lse)) return false;
   if (!e->d_lse) return true;
-  return (e->heads < 2 || e->head_lse >= e->tokens) && (e->batch < 2 || e->stride_lse >= e->tokens);
+  return apart(e->tokens, {{e->heads, e->head_lse}, {e->batch, e->stride_lse}});
 }
 
 AttnArgs attn_args(const brace_window_attention* e) {
