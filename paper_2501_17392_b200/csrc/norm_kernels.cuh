@@ -285,6 +285,18 @@ __device__ __forceinline__ Ring ring_of_group(const NormArgs& p, uint8_t* smem, 
   __syncthreads();
   return r;
 }
+// A wait ran out at stage `s`: lets the rows that are under way land (or the limit run out again) before the CTA's memory goes.
+// For the thread that fetches, which then fetches no more; stages that nothing is on its way to end at the limit.
+__device__ __forceinline__ void ring_give_up(const Ring& ring, int s, uint32_t phase) {
+#pragma unroll 1
+  for (int i = 0; i < ring.stages; ++i) {
+    mbar_wait(ring.bars + 8 * s, phase, ring.dead);
+    if (++s == ring.stages) {
+      s = 0;
+      phase ^= 1u;
+    }
+  }
+}
 __device__ __forceinline__ void group_barrier(int G) {
   if (G > 32)
     __syncthreads();
@@ -341,9 +353,10 @@ __global__ void __launch_bounds__(kNormThreads, ring_resident(NV * V)) norm_forw
   }
   int turn = 0, s = 0;
   uint32_t phase = 0;
+  bool ok = true;
   for (int64_t row = first; row < p.rows; row += step) {
-    const bool ok = mbar_wait(ring.bars + 8 * s, phase, ring.dead);
-    float v[NV * V], sum[1] = {0.f};
+    ok = ok && mbar_wait(ring.bars + 8 * s, phase, ring.dead);
+    float v[NV * V], sum[1] = {ok ? 0.f : NAN};      // a wait that ran out shows in the result
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int col = (i * G + g) * V;
@@ -356,13 +369,13 @@ __global__ void __launch_bounds__(kNormThreads, ring_resident(NV * V)) norm_forw
       }
     }
     group_barrier(G);      // all have read the row
-    if (g == 0 && row + ring.stages * step < p.rows) fetch(row + ring.stages * step, s);
-    if (++s == ring.stages) {
+    if (g == 0 && ok && row + ring.stages * step < p.rows) fetch(row + ring.stages * step, s);
+    if (ok && ++s == ring.stages) {
       s = 0;
       phase ^= 1u;
     }
     group_sum(sum, G, cell, turn);
-    const float mean = ok ? sum[0] * inv : NAN;      // a wait that ran out shows in the result
+    const float mean = sum[0] * inv;
     sum[0] = 0.f;
 #pragma unroll
     for (int i = 0; i < NV * V; ++i) {
@@ -384,6 +397,7 @@ __global__ void __launch_bounds__(kNormThreads, ring_resident(NV * V)) norm_forw
       if (col < p.dim) o.store_plain(y + row * p.ld_y + col);
     }
   }
+  if (!ok && g == 0) ring_give_up(ring, s, phase);
 }
 
 template <typename TX, typename TY, int V, int NV>
@@ -421,11 +435,12 @@ __global__ void __launch_bounds__(kNormThreads, ring_resident(NV * V)) norm_grad
   }
   int turn = 0, s = 0;
   uint32_t phase = 0;
+  bool ok = true;
   for (int64_t row = first; row < p.rows; row += step) {
     const float mean = p.mean[c * p.stride_stats + row], rstd = p.rstd[c * p.stride_stats + row];
-    const float poison = mbar_wait(ring.bars + 8 * s, phase, ring.dead) ? 0.f : NAN;      // a wait that ran out shows in the result
+    ok = ok && mbar_wait(ring.bars + 8 * s, phase, ring.dead);
     const uint32_t at = ring.rows + s * ring.bytes;
-    float t[2] = {poison, 0.f};
+    float t[2] = {ok ? 0.f : NAN, 0.f};      // a wait that ran out shows in the results
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int col = (i * G + g) * V;
@@ -462,12 +477,16 @@ __global__ void __launch_bounds__(kNormThreads, ring_resident(NV * V)) norm_grad
       o.store_plain(dx + row * p.ld_dx + col);
     }
     group_barrier(G);      // all have read the row
-    if (g == 0 && row + ring.stages * step < p.rows) fetch(row + ring.stages * step, s);
-    if (++s == ring.stages) {
+    if (g == 0 && ok && row + ring.stages * step < p.rows) fetch(row + ring.stages * step, s);
+    if (ok && ++s == ring.stages) {
       s = 0;
       phase ^= 1u;
     }
   }
+  if (!ok)
+#pragma unroll
+    for (int i = 0; i < NV * V; ++i) dw[i] = db[i] = NAN;
+  if (!ok && g == 0) ring_give_up(ring, s, phase);
   if (p.dweight || p.dbias) norm_put_sums<V, NV>(p, dw, db, sums);
 }
 
