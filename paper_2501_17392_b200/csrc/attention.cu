@@ -200,9 +200,9 @@ cudaError_t launch_forward(const AttnMaps& maps, const AttnArgs& a, cudaStream_t
   return launch(kernel, grid, Shape::kThreads, Shape::kSmem, 1, st, maps, a);
 }
 
-// The gradient on the tensor cores.
+// The gradient on the tensor cores.  `sums`: the most blocks that a CTA of the kernel that makes dk and dv sums.
 template <typename T, int D>
-cudaError_t run_grad(const brace_window_attention* e, AttnArgs a, cudaStream_t st) {
+cudaError_t run_grad(const brace_window_attention* e, AttnArgs a, int64_t sums, cudaStream_t st) {
   AttnMaps queries = {}, keys = {};   // for dq, and for dk and dv
   if (!encode_map(&queries.q, e->q, e, e->heads, 128) || !encode_map(&queries.dout, e->dout, e, e->heads, 128) ||
       !encode_map(&queries.k, e->k, e, e->kv_heads, 128) || !encode_map(&queries.v, e->v, e, e->kv_heads, 128) ||
@@ -219,14 +219,18 @@ cudaError_t run_grad(const brace_window_attention* e, AttnArgs a, cudaStream_t s
   } else {
     a.range = nullptr;
   }
-  static std::atomic<uint64_t> granted_dkv{0}, granted_dq{0};
+  // kernels that take sums out are 2 to 3 % slower where there is nothing to take out
+  const bool long_dq = key_blocks(a.tokens, a.window, a.sinks) > kLongKeys / 128, long_dkv = sums > kLongBlocks;
+  auto* dq = long_dq ? attn_dq_kernel<T, D, true> : attn_dq_kernel<T, D, false>;
+  auto* dkv = long_dkv ? attn_dkv_kernel<T, D, true> : attn_dkv_kernel<T, D, false>;
+  static std::atomic<uint64_t> granted_dkv[2], granted_dq[2];
   // dq first: dk and dv take the numbers of the queries that it made
-  if (err == cudaSuccess) err = grant_smem((const void*)attn_dq_kernel<T, D>, granted_dq, DqShape<D, kTwo>::kSmem);
+  if (err == cudaSuccess) err = grant_smem((const void*)dq, granted_dq[long_dq], DqShape<D, kTwo>::kSmem);
   if (err == cudaSuccess)
-    err = launch(attn_dq_kernel<T, D>, dim3(tiles, heads, batch), kAttnThreads, DqShape<D, kTwo>::kSmem, 1, st, queries, a);
-  if (err == cudaSuccess) err = grant_smem((const void*)attn_dkv_kernel<T, D>, granted_dkv, DkvShape<D>::kSmem);
+    err = launch(dq, dim3(tiles, heads, batch), kAttnThreads, DqShape<D, kTwo>::kSmem, 1, st, queries, a);
+  if (err == cudaSuccess) err = grant_smem((const void*)dkv, granted_dkv[long_dkv], DkvShape<D>::kSmem);
   if (err == cudaSuccess)
-    err = launch(attn_dkv_kernel<T, D>, dim3(a.first_tiles * a.pieces + tiles - a.first_tiles, kv_heads, batch), kAttnThreads,
+    err = launch(dkv, dim3(a.first_tiles * a.pieces + tiles - a.first_tiles, kv_heads, batch), kAttnThreads,
                  DkvShape<D>::kSmem, 1, st, keys, a);
   if (err == cudaSuccess && a.first_tiles)
     err = launch(attn_join_kernel<T, D, 128>, dim3((unsigned)(a.first_tiles * 32), kv_heads, batch), 128, 0, 1, st, a);
@@ -242,7 +246,8 @@ cudaError_t with_half_type(int type, F&& f) {
 // make a CTA's work that of a tile behind them, but no more than give every SM some.  All of them, where there are tiles for less
 // than half of the SMs and work for more than one CTA in each (`least` blocks: what is saved has to be more than a launch that
 // joins): 3 x 501 tokens, 2 heads read by 6, float32, 118 -> 96 us; 1000 tokens, 8 heads on one of 64, bfloat16, 128 -> 43 us.
-void share_out(const brace_window_attention* e, int rows, int least, AttnArgs& a) {
+// Returns the most blocks that a CTA then sums.
+int64_t share_out(const brace_window_attention* e, int rows, int least, AttnArgs& a) {
   const int64_t tiles = tiles_of(e->tokens, rows), first = tiles_of(std::min(e->sinks, e->tokens), rows), each = (int64_t)e->batch * e->kv_heads;
   const int64_t window = std::min<int64_t>(e->tokens, (int64_t)a.window + rows - 1), blocks = blocks_of(e->tokens, e->heads, e->kv_heads, a.window, rows);
   const Parts most = most_parts(e->batch, e->tokens, e->heads, e->kv_heads, a.window, e->sinks, rows);
@@ -264,6 +269,8 @@ void share_out(const brace_window_attention* e, int rows, int least, AttnArgs& a
     a.pieces = (int)split;
   }
   a.parts = (int)(a.first_tiles * a.pieces + (most.own ? tiles - a.first_tiles : 0));
+  const int64_t longest = first ? tiles_of(e->tokens, kBlock) * a.share : blocks;       // of the tiles that are shared out
+  return std::max(a.first_tiles ? (longest + a.pieces - 1) / a.pieces : 0, a.first_tiles < tiles ? blocks : 0);
 }
 
 }  // namespace
@@ -332,10 +339,10 @@ int brace_window_attention_grad(const brace_window_attention* e, void* d_workspa
   a.padded = q.padded;
   const cudaStream_t st = (cudaStream_t)stream;
   if (tiles_served(e, true)) {
-    share_out(e, 128, 16, a);
+    const int64_t sums = share_out(e, 128, 16, a);
     const cudaError_t err = with_half_type(e->type, [&](auto t) {
       using T = decltype(t);
-      return e->dim <= 64 ? run_grad<T, 64>(e, a, st) : run_grad<T, 128>(e, a, st);
+      return e->dim <= 64 ? run_grad<T, 64>(e, a, sums, st) : run_grad<T, 128>(e, a, sums, st);
     });
     return err == cudaSuccess ? BRACE_OK : cuda_fail_no_ctx(err);
   }

@@ -534,8 +534,8 @@ __device__ __forceinline__ float attn_grad_scale(const AttnArgs& p, int b, int g
   return bound > 0.f ? ldexpf(1.f, 13 - ilogbf(bound)) : 1.f;
 }
 
-// dq.  grid: that of GradWork
-template <typename T, int D>
+// dq.  LONG: sums over more than kLongKeys.  grid: that of GradWork
+template <typename T, int D, bool LONG>
 __global__ void __launch_bounds__(kAttnThreads, 1) attn_dq_kernel(const __grid_constant__ AttnMaps maps, const AttnArgs p) {
   // float16: ds as the sum of two values.  With one, its rounding and the result's together are 1.5 times the result's alone
   constexpr bool kTwo = std::is_same<T, __half>::value;
@@ -590,7 +590,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_dq_kernel(const __grid_c
   auto block_of = [&](int k) { return k < first_pass ? k : k - first_pass; };
   // long sums as in the forward pass (there is one pass over so many keys): the sums taken out lie in the workspace.  600,000 keys
   // that are the values, float16: dq 1.1e-3 too small -> 4e-5
-  const bool fold = count > kLongKeys / BLOCK;
+  const bool fold = LONG && count > kLongKeys / BLOCK;
   auto fresh = [&](int k) { return fold && k > 0 && k % kFoldKeys == 0; };
 
   if (warp == 8) {                         // loads
@@ -827,8 +827,8 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_dq_kernel(const __grid_c
   }
 }
 
-// dk and dv.  grid: that of GradWork
-template <typename T, int D>
+// dk and dv.  LONG: sums over more than kLongBlocks blocks.  grid: that of GradWork
+template <typename T, int D, bool LONG>
 __global__ void __launch_bounds__(kAttnThreads, 1) attn_dkv_kernel(const __grid_constant__ AttnMaps maps, const AttnArgs p) {
   constexpr bool kTwo = std::is_same<T, __half>::value;
   using Shape = DkvShape<D>;
@@ -875,7 +875,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_dkv_kernel(const __grid_
   const int g = w.head, count = w.count;
   // The first group takes dv out before block k's products where k is a multiple of kFoldBlocks, the second one dk before those
   // of the block behind it: each of them before it hands over its own block.
-  const bool fold = count > kLongBlocks;
+  const bool fold = LONG && count > kLongBlocks;
   auto fresh = [&](int k, int r) { return fold && k > r && k % kFoldBlocks == r; };
 
   if (warp == 8) {                         // loads
@@ -968,9 +968,8 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_dkv_kernel(const __grid_
     const int r = warp >> 2, row = (warp & 3) * 32 + lane, at = w.row0 + row;
     const uint32_t mine = tmem + ((uint32_t)((warp & 3) * 32) << 16), cells = mine + 128 * r;
     const float c = p.scale * kLog2e, hold = count ? attn_grad_scale(p, b, g) : 1.f;
-    // the first group writes dv, the second one dk
-    const uint32_t result = mine + 256 + D * r;
-    float* part = w.piece >= 0 || fold ? p.part + w.part_of(p, b, r, 128, D) + row * D : nullptr;
+    const uint32_t result = mine + 256 + D * r;      // the first group has dv, the second one dk
+    auto sums = [&] { return p.part + w.part_of(p, b, r, 128, D) + row * D; };
     uint32_t phase = 0, folds = 0;
     bool ok = true;
     for (int k = r; k < count; k += 2) {
@@ -981,7 +980,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_dkv_kernel(const __grid_
         }
         tc_fence_after();
 #pragma unroll 1
-        for (int col = 0; col < D; col += 32) add_sums(result + col, part + col, folds > 0);
+        for (int col = 0; col < D; col += 32) add_sums(result + col, sums() + col, folds > 0);
         ++folds;
       }
       const int s = k % STAGES;
@@ -1054,6 +1053,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_dkv_kernel(const __grid_
     const bool exists = at < p.tokens, real = at < n;
     T* to = head_row<T>(r ? p.dk : p.dv, b, exists ? at : 0, g);
     const float factor = !ok ? NAN : r ? p.scale / hold : kTwo ? 1.f / kWeightUp : 1.f;   // a wait that ran out shows in the result
+    float* part = w.piece >= 0 || (LONG && folds) ? sums() : nullptr;
     bool bad = false;
     if (count) {
 #pragma unroll
@@ -1062,7 +1062,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_dkv_kernel(const __grid_
         tmem_fetch32(result + col, o);
         tmem_loaded();
         tmem_use(o);
-        if (folds) add_to(o, part + col);
+        if (LONG && folds) add_to(o, part + col);
         if (w.piece >= 0) {
 #pragma unroll
           for (int e = 0; e < 32; e += 4)
