@@ -108,6 +108,14 @@ __device__ __forceinline__ void load_rows(uint32_t dst, const CUtensorMap* map, 
   for (int x = 0; x < D / 64; ++x) tma_load<1>(dst + x * ROWS * 128, map, 64 * x, t, head, b, bar);
 }
 
+// After `issued` loads into a ring of STAGES: whoever gave up waiting, or did not wait, what is under way lands before the CTA's
+// memory goes.
+template <int STAGES>
+__device__ __forceinline__ void rows_landed(uint32_t full, int issued, volatile int* dead) {
+#pragma unroll 1
+  for (int i = max(issued - STAGES, 0); i < issued; ++i) mbar_wait(full + 8 * (i % STAGES), (uint32_t)(i / STAGES) & 1u, dead);
+}
+
 // dst[0..dim) = v * factor, 32 columns from `col` on, of one row.
 template <typename T>
 __device__ __forceinline__ void put_columns(T* row, const float (&v)[32], float factor, int col, int dim) {
@@ -206,12 +214,8 @@ __global__ void __launch_bounds__(AttnShape<D, LONG>::kThreads, AttnShape<D, LON
     __syncwarp();
     int s = 0, issued = 0;
     uint32_t ph = 0;
-    bool ok = true;
-    for (int i = 0; ok && i < 2 * count; ++i) {
-      if (!mbar_wait(empty + 8 * s, ph ^ 1u, dead)) {
-        ok = false;
-        break;
-      }
+    for (int i = 0; i < 2 * count; ++i) {
+      if (!mbar_wait(empty + 8 * s, ph ^ 1u, dead)) break;
       if (lead) {
         // P apart: the keys of block 0; then, with the values of each block, the keys of the next one before them
         const bool last = i == 2 * count - 1, values = Shape::kApart ? last || (i > 0 && (i & 1) == 0) : i & 1;
@@ -226,9 +230,8 @@ __global__ void __launch_bounds__(AttnShape<D, LONG>::kThreads, AttnShape<D, LON
         ph ^= 1u;
       }
     }
-    if (!ok)     // gave up: let the copies in flight land before the memory goes
-      for (int i = issued > STAGES ? issued - STAGES : 0; i < issued; ++i)
-        mbar_wait(full + 8 * (i % STAGES), (uint32_t)(i / STAGES) & 1u, dead);
+    if (count) mbar_wait(q_full, 0, dead);
+    rows_landed<STAGES>(full, issued, dead);
   } else if (warp == 5) {                  // products
     const bool lead = elect_one();
     constexpr uint32_t kScores = attn_idesc<T>(KEYS, false), kValues = attn_idesc<T>(D, true);
@@ -601,30 +604,27 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_dq_kernel(const __grid_c
       load_rows<D, 128>(base + Shape::kTile, &maps.dout, w.row0, h, b, a_full);
     }
     __syncwarp();
-    int issued = 0;
-    bool ok = true;
+    int issued_k = 0, issued_v = 0;
     for (int k = 0; k < count; ++k) {
       const int sk = k % RK, sv = k % RV, t = w.first(block_of(k));
-      if (!(ok = mbar_wait(empty_v + 8 * sv, (uint32_t)(k / RV + 1) & 1u, dead))) break;
+      if (!mbar_wait(empty_v + 8 * sv, (uint32_t)(k / RV + 1) & 1u, dead)) break;
       if (lead) {
         mbar_expect_tx(full_v + 8 * sv, Shape::kTile);
         load_rows<D, BLOCK>(ring_v + sv * Shape::kTile, &maps.v, t, g, b, full_v + 8 * sv);
       }
       __syncwarp();
-      if (!(ok = mbar_wait(empty_k + 8 * sk, (uint32_t)(k / RK + 1) & 1u, dead))) break;
+      ++issued_v;
+      if (!mbar_wait(empty_k + 8 * sk, (uint32_t)(k / RK + 1) & 1u, dead)) break;
       if (lead) {
         mbar_expect_tx(full_k + 8 * sk, Shape::kTile);
         load_rows<D, BLOCK>(ring_k + sk * Shape::kTile, &maps.k, t, g, b, full_k + 8 * sk);
       }
       __syncwarp();
-      ++issued;
+      ++issued_k;
     }
-    if (!ok) {   // gave up: let the copies in flight land before the memory goes
-      for (int k = max(issued - 2, 0); k < issued; ++k) {
-        mbar_wait(full_k + 8 * (k % RK), (uint32_t)(k / RK) & 1u, dead);
-        mbar_wait(full_v + 8 * (k % RV), (uint32_t)(k / RV) & 1u, dead);
-      }
-    }
+    if (count) mbar_wait(a_full, 0, dead);
+    rows_landed<RK>(full_k, issued_k, dead);
+    rows_landed<RV>(full_v, issued_v, dead);
   } else if (warp == 9) {                  // products
     const bool lead = elect_one();
     constexpr uint32_t kScores = attn_idesc<T>(BLOCK, false), kSums = attn_idesc<T>(D, true);
@@ -888,12 +888,8 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_dkv_kernel(const __grid_
     __syncwarp();
     int s = 0, issued = 0;
     uint32_t ph = 0;
-    bool ok = true;
-    for (int k = 0; ok && k < count; ++k) {
-      if (!mbar_wait(empty + 8 * s, ph ^ 1u, dead)) {
-        ok = false;
-        break;
-      }
+    for (int k = 0; k < count; ++k) {
+      if (!mbar_wait(empty + 8 * s, ph ^ 1u, dead)) break;
       if (lead) {
         const uint32_t at = ring + s * Shape::kStage, bar = full + 8 * s;
         const int t = w.first(k), h = w.head_of(k, p);
@@ -910,9 +906,8 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_dkv_kernel(const __grid_
         ph ^= 1u;
       }
     }
-    if (!ok)     // gave up: let the copies in flight land before the memory goes
-      for (int i = issued > STAGES ? issued - STAGES : 0; i < issued; ++i)
-        mbar_wait(full + 8 * (i % STAGES), (uint32_t)(i / STAGES) & 1u, dead);
+    if (count) mbar_wait(a_full, 0, dead);
+    rows_landed<STAGES>(full, issued, dead);
   } else if (warp == 9) {                  // products
     const bool lead = elect_one();
     constexpr uint32_t kScores = attn_idesc<T>(kBlock, false), kSums = attn_idesc<T>(D, true);
