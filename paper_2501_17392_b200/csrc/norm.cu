@@ -55,7 +55,7 @@ NormShape norm_grad_shape(int dim, int x_type, bool wide) {
   return x_type == BRACE_TYPE_F32 ? norm_shape(dim, 4, 4) : norm_shape(dim, 8, 2);
 }
 
-constexpr int kSms = 148, kMostResident = 16;   // CTAs of an SM, of any kind
+constexpr int kSms = 148;
 
 // CTAs of an SM; narrow ones make room for more.
 int resident_of(const NormShape& s, bool ring) {
@@ -188,8 +188,14 @@ int brace_layer_norm_forward(const brace_layer_norm* e, brace_stream_t stream) {
 
 size_t brace_layer_norm_workspace_bytes(int32_t clients, int64_t rows, int32_t dim) {
   if (!norm_sizes_ok(clients, rows, dim) || dim > kNormMostColumns) return 0;
-  const int slots = std::min(norm_shape(dim, BRACE_TYPE_F32, false).slots, norm_shape(dim, BRACE_TYPE_F32, true).slots);
-  return (size_t)round_up(std::max<int64_t>(norm_parts(clients, rows, dim, slots, kMostResident) * clients * 2 * dim * 4, 256), 256);
+  int64_t parts = 1;
+  for (const bool wide : {false, true})      // of any types and alignment
+    for (const int type : {BRACE_TYPE_F32, BRACE_TYPE_BF16}) {
+      if (wide && dim % 8) continue;
+      const NormShape s = norm_grad_shape(dim, type, wide);
+      parts = std::max(parts, norm_parts(clients, rows, dim, s.slots, resident_of(s, wide && dim >= kRingFrom)));
+    }
+  return (size_t)round_up(std::max<int64_t>(parts * clients * 2 * dim * 4, 256), 256);
 }
 
 int brace_layer_norm_grad(const brace_layer_norm* e, void* d_workspace, size_t workspace_bytes, brace_stream_t stream) {
