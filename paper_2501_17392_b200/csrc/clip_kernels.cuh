@@ -62,7 +62,7 @@ __device__ __noinline__ double squares64(const T* x, int pieces, int width, int 
 template <bool CLIP_>
 struct ClipPass {
   static constexpr bool CLIP = CLIP_;
-  float factor;
+  float factor, rest;                // what a value is multiplied by, one after the other (clip_factor)
   bool zero;
   double acc;
 };
@@ -80,7 +80,7 @@ __device__ __forceinline__ void clip_pieces(P& p, const TI* in, TO* out, int cou
     for (int u = 0; u < U; ++u) {
       Pack<TO, V> y;
 #pragma unroll
-      for (int k = 0; k < V; ++k) y.t[k] = from_f32<TO>(p.zero ? 0.f : to_f32(x[u].t[k]) * p.factor);
+      for (int k = 0; k < V; ++k) y.t[k] = from_f32<TO>(p.zero ? 0.f : to_f32(x[u].t[k]) * p.factor * p.rest);
       if (ALL || u < count) y.store_stream(out + u * kApart);
     }
   } else {
@@ -191,7 +191,12 @@ __device__ __forceinline__ double clip_total(const ClipArgs& a, int64_t c, doubl
 }
 
 __device__ __forceinline__ void clip_factor(const ClipArgs& a, double norm, ClipPass<true>& p) {
-  const double f = norm == 0.0 ? 1.0 : (double)a.max_norm / (norm + (double)a.eps);
+  double f = norm == 0.0 ? 1.0 : (double)a.max_norm / (norm + (double)a.eps);
+  // float32 has fewer bits below 2^-126, where the norm of values near its largest ones takes the factor: half of its exponent
+  // then goes into a power of two.  What the first product loses below 2^-126 is less than the result can hold.
+  const int half = f < 0x1p-100 && f > 0.0 ? ilogb(f) / 2 : 0;
+  f = ldexp(f, -half);
+  p.rest = (float)ldexp(1.0, half);
   p.factor = f > 1.0 ? 1.f : (float)f;      // NaN stays
   p.zero = a.zero_bad && !isfinite(norm);
 }
