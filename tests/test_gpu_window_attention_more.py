@@ -217,3 +217,25 @@ def test_sums_of_one_sign_over_many_keys(dtype, n, dim, ramp):
         assert worse(out[0, i, 0], s.softmax(-1) @ v[0, :, 0].double()) < (1.5 if a else 2)
         # a score is off by (dim + 2) 2^-23 of its products' absolute sum, below 8 dim in all
         assert float((lse[0, 0, i] - s.logsumexp(-1)).abs().max()) < plan.scale * (dim + 2) * 2.0 ** -23 * 8 * dim + 2.0 ** -19 + 20 * u
+
+
+@pytest.mark.parametrize("batch,heads", [(5, 32), (19, 16)])
+def test_long_sums_of_many_tiles(batch, heads):
+    """320 tiles of keys that 262,144 queries read, each shared out over four CTAs, and 1216 that 131,072 read, each a CTA's own:
+    it takes its sums out on the way.  The last sequence is shorter.  do has both signs: what up to 4096 steps cut off is less than
+    float16's rounding."""
+    n, dim, short = 8192, 64, 5001
+    q, do = (randn(batch, n, heads, dim, seed=s).to(F16) for s in (1, 2))
+    do *= 1e-2
+    k, v = (randn(batch, n, 1, dim, seed=s).to(F16) for s in (3, 4))
+    lengths = torch.tensor([n] * (batch - 1) + [short], dtype=torch.int32, device="cuda")
+    plan = B.WindowAttention(heads, dim, n, batch=batch, kv_heads=1, window=n)
+    out, lse = torch.empty_like(q), torch.empty(batch, heads, n, device="cuda")
+    plan.forward(q, k, v, out, lse=lse, lengths=lengths)
+    dq, dk, dv = (torch.empty_like(t) for t in (q, k, v))
+    plan.workspace.fill_(255)
+    plan.grad(do, q, k, v, out, lse, dq, dk, dv, lengths=lengths)
+    for b, m in ((0, n), (batch - 1, short)):
+        wq, wk, wv = banded(q[b, :m], k[b, :m], v[b, :m], do[b, :m], n, 0, plan.scale)
+        assert worse(dk[b, :m, 0], wk) < 1.5 and worse(dv[b, :m, 0], wv) < 1.5 and worse(dq[b, :m], wq) < 2
+        assert bool((dk[b, m:] == 0).all()) and bool((dv[b, m:] == 0).all()) and bool((dq[b, m:] == 0).all())
