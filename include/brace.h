@@ -653,9 +653,12 @@ typedef struct brace_heads {
  *   s_ij = scale q_i.k_j,  lse_i = log sum_j exp s_ij,  out_i = sum_j exp(s_ij - lse_i) v_j
  * over the keys that i sees; what a hidden place holds has no effect.  Rows from
  * a sequence's length on are 0 in every result, and lse -infinity there, whatever
- * the inputs hold.  Products and sums are float32 (of bfloat16 and float16 inputs
- * on the tensor cores: exp(..) is rounded to the inputs' type for the sum over
- * v), results are rounded once. */
+ * the inputs hold.  Products and sums are float32, results are rounded once.  Of
+ * bfloat16 and float16 inputs on the tensor cores, exp(..) is rounded to the
+ * inputs' type for the sum over v (float16: times 2^9), and a sum is cut off
+ * rather than rounded at every step: one of values of one sign comes out up to
+ * 4e-4 too small over 65,536 keys, and no further over more (bfloat16 heads of
+ * more than 64: 1.7e-3 over 262,144, and no further). */
 typedef struct brace_window_attention {
   int32_t batch;           /* sequences, 0..65535                                                  */
   int32_t tokens;          /* rows of a sequence, 0..2^29 (more: BRACE_ERR_UNSUPPORTED)            */
@@ -694,7 +697,9 @@ size_t brace_window_attention_workspace_bytes(int32_t batch, int32_t tokens, int
  * With p_ij = exp(s_ij - lse_i) and ds_ij = p_ij (dout_i.v_j - dout_i.out_i):
  *   dq_i = scale sum_j ds_ij k_j
  *   dk_j = scale sum ds_ij q_i,  dv_j = sum p_ij dout_i   over the queries and heads that read j
- * in one order: the same bits every time.  For bfloat16 and float16 queries of few
+ * in one order: the same bits every time.  On the tensor cores p and ds are
+ * rounded to bfloat16 for these sums, in float16 p times 2^15 is, and ds is kept as
+ * two values; sums are cut off as above.  For bfloat16 and float16 queries of few
  * keys dout_i.out_i is summed anew as sum_j p_ij dout_i.v_j, without the rounding
  * of out.  Errors as above, and WORKSPACE. */
 int brace_window_attention_grad(const brace_window_attention* e, void* d_workspace, size_t workspace_bytes,

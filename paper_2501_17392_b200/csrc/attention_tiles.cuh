@@ -4,9 +4,9 @@
 // Forward.  A CTA has 128 queries and walks the blocks of 128 keys that they see: the first tokens', then the window's.  Per
 // block: scores S = Q K^T into tensor memory; a thread takes a query's scores into registers, masks them, brings its running
 // maximum up to date and writes exp2 of the differences, rounded to the inputs' type, back to tensor memory as P; P V is added
-// to the result there.  The result is scaled again only when a maximum has grown by more than 2^8, or 2^6.9 in float16 (the sum and
-// P have room for that).  Two CTAs share an SM: one's exponentials go on while the tensor cores work for the other, and one begins or ends
-// while the other is under way.
+// to the result there.  The result is scaled again only when a maximum has grown by more than 2^8, or 2^6.9 in float16 (the sum
+// and P have room for that).  Two CTAs share an SM: one's exponentials go on while the tensor cores work for the other, and one
+// begins or ends while the other is under way.
 //
 // Backward, in two kernels, so that every result is summed in one order.  Scores and dp = do v of a block go into tensor memory,
 // a thread makes p and ds of its columns and writes them back there, rounded to the inputs' type, and the products with k (with
@@ -23,9 +23,9 @@
 // 2^9 (AttnRange), p times 2^15, ds times what the largest |do| and |v| allow without overflow.
 //
 // Bound by the chain of a block rather than by a unit: forward, 8192 tokens, 12 heads of 64, window 1024, 66 us, with the
-// exponentials' unit busy for 45 % of the cycles, issue 30 %, matrix instructions 22 %; the operations alone would take 15 us.  Backward,
-// 4 x 4096 tokens, 16 heads on 4 of 128, window 1024, 566 us (183): matrix instructions 41 % (dq) and 54 % (dk, dv), of which
-// those with 64 queries run at half the rate.
+// exponentials' unit busy for 45 % of the cycles, issue 30 %, matrix instructions 22 %; the operations alone would take 15 us.
+// Backward, 4 x 4096 tokens, 16 heads on 4 of 128, window 1024, 558 us (183): matrix instructions 41 % (dq) and 54 % (dk, dv).
+// Scores and dp are made in both kernels, seven products for the five of the formulas, and those of 64 queries run at half rate.
 //
 // A product with P = 0 where a key is hidden gives NaN if that key's value is not finite.  A row whose result is not
 // finite is therefore computed again, key by key, from what it sees.

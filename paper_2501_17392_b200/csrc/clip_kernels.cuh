@@ -1,7 +1,7 @@
 // Every client's gradient norm over many tensors, and the gradients clipped by it.
 //
 // norm_c = sqrt(sum over the client's tensors of sum x^2), f_c = min(1, max_norm / (norm_c + eps)), out = f_c x.
-// Bound by memory: every value is read for its square, and read again once the norm is known.  A launch sums (a client's
+// Bound by memory where values are not 0: every value is read for its square, and read again once the norm is known.  A launch sums (a client's
 // elements shared out evenly over CTAs, each of which leaves one sum), a second one clips, the other way round, so that it
 // begins with what is still in L2.
 // 50 clients of 11.7 M float32 values (2.3 GB): 327 us to sum (7.2 TB/s) and 1092 in all (6.4 TB/s on what is read twice
@@ -11,7 +11,8 @@
 // all CTAs wait for one another once a client).
 // Squares are summed in float32 over at most 16 values that a thread has at a time, and beyond that in float64, in one
 // order; where a float32 sum leaves its comfortable range (overflow, squares lost to underflow) those values are squared
-// in float64.
+// in float64.  So are 16 zeros, at the price of instructions: the norms of 8 clients' tables of 50,000 x 768 take 176 us dense, 235
+// with all rows but 8192 zero and 306 all zero (bfloat16 96, 227, 274), clipping into float32 rows 572, 624 and 694 (422, 541, 586).
 #pragma once
 
 #include "elements.cuh"
