@@ -239,3 +239,35 @@ def test_long_sums_of_many_tiles(batch, heads):
         wq, wk, wv = banded(q[b, :m], k[b, :m], v[b, :m], do[b, :m], n, 0, plan.scale)
         assert worse(dk[b, :m, 0], wk) < 1.5 and worse(dv[b, :m, 0], wv) < 1.5 and worse(dq[b, :m], wq) < 2
         assert bool((dk[b, m:] == 0).all()) and bool((dv[b, m:] == 0).all()) and bool((dq[b, m:] == 0).all())
+
+
+@pytest.mark.parametrize("dtype,dim", [(F16, 64), (F16, 128), (BF16, 64)])
+def test_long_windows_behind_first_tokens(dtype, dim):
+    """A window of more than 65,536 keys and a few first tokens before it, whose block is cut short; one text ends early.  do has
+    both signs."""
+    n, heads, window, sinks, lengths = 100001, 2, 70000, 5, [100001, 80000]
+    q, do = (randn(2, n, heads, dim, seed=s).to(dtype) for s in (1, 2))
+    do *= 1e-2
+    k, v = (randn(2, n, 1, dim, seed=s).to(dtype) for s in (3, 4))
+    ln = torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    plan = B.WindowAttention(heads, dim, n, batch=2, kv_heads=1, window=window, sinks=sinks)
+    out, lse = torch.empty_like(q), torch.empty(2, heads, n, device="cuda")
+    plan.forward(q, k, v.abs(), out, lse=lse, lengths=ln)
+    for b, m in enumerate(lengths):
+        for a in (100, 65600, 75000, m - 200):
+            i = torch.arange(a, a + 200, device="cuda")
+            j = torch.arange(m, device="cuda")
+            back = i[:, None] - j
+            hidden = (back < 0) | ((back >= window) & (j >= sinks))
+            for h in range(heads):
+                s = (q[b, i, h].double() @ k[b, :m, 0].double().T * plan.scale).masked_fill(hidden, -math.inf)
+                assert worse(out[b, i, h], s.softmax(-1) @ v[b, :m, 0].double().abs()) < (2 if a < 1000 or a == 65600 or dtype == F16 else 1.5)
+    plan.forward(q, k, v, out, lse=lse, lengths=ln)
+    dq, dk, dv = (torch.empty_like(t) for t in (q, k, v))
+    plan.grad(do, q, k, v, out, lse, dq, dk, dv, lengths=ln)
+    for b, m in enumerate(lengths):
+        wq, wk, wv = banded(q[b, :m], k[b, :m], v[b, :m], do[b, :m], window, sinks, plan.scale)
+        # bfloat16: p and ds are rounded for the sums, each as much as the result is
+        most = 2.5 if dtype == BF16 else 2
+        assert worse(dq[b, :m], wq) < most and worse(dk[b, :m, 0], wk) < most and worse(dv[b, :m, 0], wv) < most
+        assert not any(bool(t[b, m:].any()) for t in (out, dq, dk, dv))
