@@ -428,7 +428,7 @@ __global__ void __launch_bounds__(AttnShape<D, LONG>::kThreads, AttnShape<D, LON
       }
     }
     if (exists && !real) put_zeros(out, p.dim);
-    if (exists && p.lse) attn_lse(p, b, h, i) = real ? (top * c + (log2f(total) - kUp)) * kLn2 : -INFINITY;
+    if (exists && p.lse) attn_lse(p, b, h, i) = !real ? -INFINITY : ok ? (top * c + (log2f(total) - kUp)) * kLn2 : NAN;
     __syncwarp();   // what follows may write the same rows
     // a key that some row of the tile does not see, or a key that it sees, is not finite
     unsigned again = __ballot_sync(0xffffffffu, bad && real && ok);
@@ -792,6 +792,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_dq_kernel(const __grid_c
     }
     if (ok && count) ok = mbar_wait(p_done, (uint32_t)(blocks - 1) & 1u, dead);
     tc_fence_after();
+    if (!kTwo && !ok && at < p.padded) p.delta[attn_delta(p, b, h, at)] = NAN;      // which may not have been made: dk shows it
     const bool exists = at < p.tokens, real = at < n;
     if (half == 0) {
       T* to = head_row<T>(p.dq, b, exists ? at : 0, h);
@@ -934,7 +935,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_dkv_kernel(const __grid_
     for (int k = 0; ok && k < 2 && k < count; ++k) ok = scores(k);
     for (int k = 0; ok && k < count; ++k) {
       const int s = k % STAGES, r = k & 1;
-      if (!mbar_wait(p_full + 8 * r, (uint32_t)(k >> 1) & 1u, dead)) break;
+      if (!(ok = mbar_wait(p_full + 8 * r, (uint32_t)(k >> 1) & 1u, dead))) break;
       tc_fence_after();
       if (lead) {
         const uint64_t db = ring_desc + (uint64_t)(s * Shape::kStage >> 4);
@@ -954,7 +955,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_dkv_kernel(const __grid_
       __syncwarp();
       if (k + 2 < count) ok = scores(k + 2);
     }
-    if (lead) {
+    if (lead && ok) {      // else who waits for the sums gives up too
       mma_commit<1>(o_full);
       mma_commit<1>(o_full + 8);
     }
