@@ -108,8 +108,7 @@ __device__ __forceinline__ void load_rows(uint32_t dst, const CUtensorMap* map, 
   for (int x = 0; x < D / 64; ++x) tma_load<1>(dst + x * ROWS * 128, map, 64 * x, t, head, b, bar);
 }
 
-// After `issued` loads into a ring of STAGES: whoever gave up waiting, or did not wait, what is under way lands before the CTA's
-// memory goes.
+// After `issued` loads into a ring of STAGES, once a wait ran out: what is under way lands before the CTA's memory goes.
 template <int STAGES>
 __device__ __forceinline__ void rows_landed(uint32_t full, int issued, volatile int* dead) {
 #pragma unroll 1
@@ -230,8 +229,7 @@ __global__ void __launch_bounds__(AttnShape<D, LONG>::kThreads, AttnShape<D, LON
         ph ^= 1u;
       }
     }
-    if (count) mbar_wait(q_full, 0, dead);
-    rows_landed<STAGES>(full, issued, dead);
+    dead[1] = issued;
   } else if (warp == 5) {                  // products
     const bool lead = elect_one();
     constexpr uint32_t kScores = attn_idesc<T>(KEYS, false), kValues = attn_idesc<T>(D, true);
@@ -435,8 +433,13 @@ __global__ void __launch_bounds__(AttnShape<D, LONG>::kThreads, AttnShape<D, LON
     for (; again; again &= again - 1) forward_row<T>(p, b, h, q0 + warp * 32 + __ffs(again) - 1, n);
   }
   __syncthreads();
-  if (*dead)     // a wait ran out: products may still be under way
+  if (*dead) {   // a wait ran out: loads and products may still be under way
+    if (warp == 4 && count) {
+      mbar_wait(q_full, 0, dead);
+      rows_landed<STAGES>(full, dead[1], dead);
+    }
     for (int i = 0; i < 200; ++i) __nanosleep(1000);
+  }
   tc_fence_before();
   __syncthreads();
   if (warp == 5) {
@@ -622,9 +625,8 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_dq_kernel(const __grid_c
       __syncwarp();
       ++issued_k;
     }
-    if (count) mbar_wait(a_full, 0, dead);
-    rows_landed<RK>(full_k, issued_k, dead);
-    rows_landed<RV>(full_v, issued_v, dead);
+    dead[1] = issued_k;
+    dead[3] = issued_v;
   } else if (warp == 9) {                  // products
     const bool lead = elect_one();
     constexpr uint32_t kScores = attn_idesc<T>(BLOCK, false), kSums = attn_idesc<T>(D, true);
@@ -818,8 +820,14 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_dq_kernel(const __grid_c
     }
   }
   __syncthreads();
-  if (*dead)     // a wait ran out: products may still be under way
+  if (*dead) {   // a wait ran out: loads and products may still be under way
+    if (warp == 8 && count) {
+      mbar_wait(a_full, 0, dead);
+      rows_landed<RK>(full_k, dead[1], dead);
+      rows_landed<RV>(full_v, dead[3], dead);
+    }
     for (int i = 0; i < 200; ++i) __nanosleep(1000);
+  }
   tc_fence_before();
   __syncthreads();
   if (warp == 9) {
@@ -907,8 +915,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_dkv_kernel(const __grid_
         ph ^= 1u;
       }
     }
-    if (count) mbar_wait(a_full, 0, dead);
-    rows_landed<STAGES>(full, issued, dead);
+    dead[1] = issued;
   } else if (warp == 9) {                  // products
     const bool lead = elect_one();
     constexpr uint32_t kScores = attn_idesc<T>(kBlock, false), kSums = attn_idesc<T>(D, true);
@@ -1078,8 +1085,13 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_dkv_kernel(const __grid_
     for (; again; again &= again - 1) dkv_row<T>(p, b, g, w.row0 + (warp & 3) * 32 + __ffs(again) - 1, n, r == 1, r == 0);
   }
   __syncthreads();
-  if (*dead)     // a wait ran out: products may still be under way
+  if (*dead) {   // a wait ran out: loads and products may still be under way
+    if (warp == 8 && count) {
+      mbar_wait(a_full, 0, dead);
+      rows_landed<STAGES>(full, dead[1], dead);
+    }
     for (int i = 0; i < 200; ++i) __nanosleep(1000);
+  }
   tc_fence_before();
   __syncthreads();
   if (warp == 9) {
