@@ -286,6 +286,7 @@ __device__ __forceinline__ Ring ring_of_group(const NormArgs& p, uint8_t* smem, 
   __syncthreads();
   return r;
 }
+constexpr uint32_t kGaveUp = 2;      // beside the parity of a thread's phase: a wait ran out, and it waits no more
 // A wait ran out at stage `s`: lets the rows that are under way land (or the limit run out again) before the CTA's memory goes.
 // For the thread that fetches, which then fetches no more; stages that nothing is on its way to end at the limit.
 __device__ __forceinline__ void ring_give_up(const Ring& ring, int s, uint32_t phase) {
@@ -354,10 +355,13 @@ __global__ void __launch_bounds__(kNormThreads, ring_resident(NV * V)) norm_forw
   }
   int turn = 0, s = 0;
   uint32_t phase = 0;
-  bool ok = true;
+  int64_t limit = p.rows;      // of rows that are fetched: 0 once a wait ran out
   for (int64_t row = first; row < p.rows; row += step) {
-    ok = ok && mbar_wait(ring.bars + 8 * s, phase, ring.dead);
-    float v[NV * V], sum[1] = {ok ? 0.f : NAN};      // a wait that ran out shows in the result
+    if (!mbar_wait(ring.bars + 8 * s, phase, ring.dead)) {
+      if (g == 0 && limit) ring_give_up(ring, s, phase);
+      limit = 0;
+    }
+    float v[NV * V], sum[1] = {0.f};
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int col = (i * G + g) * V;
@@ -370,13 +374,13 @@ __global__ void __launch_bounds__(kNormThreads, ring_resident(NV * V)) norm_forw
       }
     }
     group_barrier(G);      // all have read the row
-    if (g == 0 && ok && row + ring.stages * step < p.rows) fetch(row + ring.stages * step, s);
-    if (ok && ++s == ring.stages) {
+    if (g == 0 && row + ring.stages * step < limit) fetch(row + ring.stages * step, s);
+    if (++s == ring.stages) {
       s = 0;
       phase ^= 1u;
     }
     group_sum(sum, G, cell, turn);
-    const float mean = sum[0] * inv;
+    const float mean = limit ? sum[0] * inv : NAN;      // a wait that ran out shows in the result
     sum[0] = 0.f;
 #pragma unroll
     for (int i = 0; i < NV * V; ++i) {
@@ -398,7 +402,6 @@ __global__ void __launch_bounds__(kNormThreads, ring_resident(NV * V)) norm_forw
       if (col < p.dim) o.store_plain(y + row * p.ld_y + col);
     }
   }
-  if (!ok && g == 0) ring_give_up(ring, s, phase);
 }
 
 template <typename TX, typename TY, int V, int NV>
@@ -435,13 +438,12 @@ __global__ void __launch_bounds__(kNormThreads, ring_resident(NV * V)) norm_grad
     dw[i] = db[i] = 0.f;
   }
   int turn = 0, s = 0;
-  uint32_t phase = 0;
-  bool ok = true;
+  uint32_t phase = 0;      // and kGaveUp
   for (int64_t row = first; row < p.rows; row += step) {
     const float mean = p.mean[c * p.stride_stats + row], rstd = p.rstd[c * p.stride_stats + row];
-    ok = ok && mbar_wait(ring.bars + 8 * s, phase, ring.dead);
+    if (phase < kGaveUp && !mbar_wait(ring.bars + 8 * s, phase, ring.dead)) phase |= kGaveUp;
     const uint32_t at = ring.rows + s * ring.bytes;
-    float t[2] = {ok ? 0.f : NAN, 0.f};      // a wait that ran out shows in the results
+    float t[2] = {phase < kGaveUp ? 0.f : NAN, 0.f};      // a wait that ran out shows in the results
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int col = (i * G + g) * V;
@@ -478,16 +480,16 @@ __global__ void __launch_bounds__(kNormThreads, ring_resident(NV * V)) norm_grad
       o.store_plain(dx + row * p.ld_dx + col);
     }
     group_barrier(G);      // all have read the row
-    if (g == 0 && ok && row + ring.stages * step < p.rows) fetch(row + ring.stages * step, s);
-    if (ok && ++s == ring.stages) {
+    if (g == 0 && phase < kGaveUp && row + ring.stages * step < p.rows) fetch(row + ring.stages * step, s);
+    if (phase < kGaveUp && ++s == ring.stages) {
       s = 0;
       phase ^= 1u;
     }
   }
-  if (!ok)
+  if (phase >= kGaveUp)
 #pragma unroll
     for (int i = 0; i < NV * V; ++i) dw[i] = db[i] = NAN;
-  if (!ok && g == 0) ring_give_up(ring, s, phase);
+  if (phase >= kGaveUp && g == 0) ring_give_up(ring, s, phase & 1u);
   if (p.dweight || p.dbias) norm_put_sums<V, NV>(p, dw, db, sums);
 }
 
