@@ -22,9 +22,9 @@
 // In float16 P, p and ds are held times powers of two, since they are often below what float16 holds at full precision: P times
 // 2^9 (AttnRange), p times 2^15, ds times what the largest |do| and |v| allow without overflow.
 //
-// Bound by the chain of a block rather than by a unit: forward, 8192 tokens, 12 heads of 64, window 1024, 66 us, with the
+// Bound by the chain of a block rather than by a unit: forward, 8192 tokens, 12 heads of 64, window 1024, 64 us, with the
 // exponentials' unit busy for 45 % of the cycles, issue 30 %, matrix instructions 22 %; the operations alone would take 15 us.
-// Backward, 4 x 4096 tokens, 16 heads on 4 of 128, window 1024, 558 us (183): matrix instructions 41 % (dq) and 54 % (dk, dv).
+// Backward, 4 x 4096 tokens, 16 heads on 4 of 128, window 1024, 559 us (183): matrix instructions 41 % (dq) and 54 % (dk, dv).
 // Scores and dp are made in both kernels, seven products for the five of the formulas, and those of 64 queries run at half rate.
 //
 // A product with P = 0 where a key is hidden gives NaN if that key's value is not finite.  A row whose result is not

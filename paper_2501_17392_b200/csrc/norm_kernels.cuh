@@ -3,7 +3,7 @@
 // Row t of client c: mean = sum x / D, var = sum (x - mean)^2 / D, rstd = 1 / sqrt(var + eps), xh = (x - mean) rstd,
 // y = xh w + b.  Backward, g = dy w: dx = rstd (g - sum g / D - xh sum(g xh) / D), dw = sum_t dy xh, db = sum_t dy.
 // Every activation is read once and written once.  Bound by memory in float32; in 16 bits by instructions (16 x 8192 x 768 forward
-// from float32 to bfloat16 109 us, 0.85 of the copy rate; 8 x 8192 x 768 from bfloat16 to bfloat16 52 us for 31).  G threads hold a row in registers (so that the
+// from float32 to bfloat16 108 us, 0.85 of the copy rate; 8 x 8192 x 768 from bfloat16 to bfloat16 52 us for 31).  G threads hold a row in registers (so that the
 // variance is summed from differences, in a second pass that reads nothing), a thread always has the same columns, keeps
 // their weights in registers for all of its rows and, backward, the sums of their gradients; the CTAs' sums are joined by
 // a second launch, in one order.  Sums are float32.
